@@ -23,7 +23,9 @@ LIB = os.path.join(HERE, "libsom.so")
 SOURCES = ["som_api.cpp", "som_train.hip", "som_train_pipe.hip", "som_train_pipe_stream.hip",
            "som_train_panel.hip",
            "som_eval.hip", "som_eval_half.hip", "som_util.hip", "som_pca.hip", "som_sparse.hip", "som_batch.hip",
-           "som_stream.hip"]
+           "som_stream.hip",
+           "som_local_api.cpp", "som_local_rows.hip", "som_product_f32.hip",
+           "som_product_bf16.hip", "som_product_f16.hip", "som_route.hip", "som_adamw.hip"]
 ARCH = "gfx950"
 
 
@@ -53,7 +55,13 @@ def common_flags() -> list:
 UNIFORM_EXIT_SOURCES = ("som_train.hip", "som_train_pipe.hip", "som_train_panel.hip")
 
 
+# The optimizer rounds every operation by itself (som_adamw.hip).
+UNCONTRACTED_SOURCES = ("som_adamw.hip",)
+
+
 def unit_flags(src: str) -> list:
+    if src in UNCONTRACTED_SOURCES:
+        return ["-ffp-contract=off"]
     if src in UNIFORM_EXIT_SOURCES:
         return ["-mllvm", "-structurizecfg-skip-uniform-regions=true"]
     return []
@@ -75,7 +83,7 @@ def _compile(src: str) -> str:
 
 
 def build(verbose: bool = True) -> str:
-    with ThreadPoolExecutor(max_workers=min(5, len(SOURCES))) as ex:
+    with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
         objs = list(ex.map(_compile, SOURCES))
     tmp = LIB + ".tmp"
     cmd = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp] + objs

@@ -73,6 +73,30 @@ struct som_map {
     int64_t eval_cap = 0;
 };
 
+namespace som {
+
+// True when [p, p + bytes) lies inside one device allocation.
+bool device_range_ok(const void *p, uint64_t bytes) {
+    if (!p) return false;
+    hipPointerAttribute_t attr;
+    if (hipPointerGetAttributes(&attr, p) != hipSuccess) {
+        (void)hipGetLastError();
+        return false;
+    }
+    if (attr.type != hipMemoryTypeDevice && attr.type != hipMemoryTypeManaged) return false;
+    hipDeviceptr_t base = nullptr;
+    size_t size = 0;
+    if (hipMemGetAddressRange(&base, &size, const_cast<void *>(p)) != hipSuccess) {
+        (void)hipGetLastError();
+        return false;
+    }
+    const uintptr_t b = reinterpret_cast<uintptr_t>(base);
+    const uintptr_t q = reinterpret_cast<uintptr_t>(p);
+    return q >= b && bytes <= size && q - b <= size - bytes;
+}
+
+}  // namespace som
+
 namespace {
 
 constexpr uint64_t kMaxBytesDefault = 64ull << 30;  // per-map device memory cap
@@ -94,25 +118,7 @@ som_status from_hip(hipError_t e) {
     return SOM_E_DEVICE;
 }
 
-// True when [p, p + bytes) lies inside one device allocation.
-bool device_range_ok(const void *p, uint64_t bytes) {
-    if (!p) return false;
-    hipPointerAttribute_t attr;
-    if (hipPointerGetAttributes(&attr, p) != hipSuccess) {
-        (void)hipGetLastError();
-        return false;
-    }
-    if (attr.type != hipMemoryTypeDevice && attr.type != hipMemoryTypeManaged) return false;
-    hipDeviceptr_t base = nullptr;
-    size_t size = 0;
-    if (hipMemGetAddressRange(&base, &size, const_cast<void *>(p)) != hipSuccess) {
-        (void)hipGetLastError();
-        return false;
-    }
-    const uintptr_t b = reinterpret_cast<uintptr_t>(base);
-    const uintptr_t q = reinterpret_cast<uintptr_t>(p);
-    return q >= b && bytes <= size && q - b <= size - bytes;
-}
+using som::device_range_ok;
 
 bool schedule_ok(const som_schedule *s) {
     if (s->lr_decay != SOM_DECAY_LINEAR && s->lr_decay != SOM_DECAY_EXPONENTIAL) return false;

@@ -7,6 +7,9 @@
 
 namespace som {
 
+// True when [p, p + bytes) lies inside one device allocation (som_api.cpp).
+bool device_range_ok(const void *p, uint64_t bytes);
+
 // Threads per workgroup of the persistent training kernel.
 constexpr int kTrainBlock = 256;
 // Grid-exchange slot layout: 64-bit key = dist_bits << 32 | tag << 24 | unit.

@@ -1,0 +1,687 @@
+// Host side of the local models: the C ABI declared in include/som_local.h.
+// Validates every argument before any device work, lays out the caller's work
+// memory, chooses how each product runs, and enqueues the kernels.
+#include "som_local.h"
+#include "som_internal.h"
+#include "som_local_internal.h"
+
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+#include <new>
+#include <vector>
+
+namespace som {
+
+// How a product runs.  Few rows: the kernel that streams w.  Otherwise the tile
+// and the number of parts of the contraction with the least estimated time:
+// rounds of workgroups over the compute units, slabs in each, and the pass that
+// joins the parts.
+ProductPlan plan_product(const ProductArgs &a, int num_cus) {
+    ProductPlan best{};
+    const int64_t experts = a.offsets ? a.experts : 1;
+    const int64_t slab = 128 / type_size(a.type);
+    if (a.mode == kForward && a.m <= 64 * experts && (a.offsets || a.m <= 64)) {
+        const int64_t per = (a.m + experts - 1) / experts;
+        best.tile = per <= 16 ? 16 : 64;
+        const int64_t groups = (a.n + 15) / 16 * std::min(a.m, a.m / best.tile + experts);
+        // sixteen waves where four would leave the chip short of loads in flight
+        best.waves = groups * 4 < (int64_t)num_cus * 16 && a.k >= 8 * slab ? 16 : 4;
+        best.splits = 1;
+        return best;
+    }
+    // microseconds of a slab on all the workgroups that a compute unit holds
+    struct Shape { int32_t tile, held; double half, single; };
+    static const Shape shapes[] = {{256, 1, 1.2, 7.5}, {128, 2, 0.75, 3.8}, {64, 4, 0.5, 2.0}};
+    double least = INFINITY;
+    for (const Shape &s : shapes) {
+        const int64_t tn = (a.n + s.tile - 1) / s.tile;
+        int64_t tm, k = a.k;
+        if (a.mode == kWeight) {
+            tm = (a.m + s.tile - 1) / s.tile * experts;
+            k = (a.k + experts - 1) / experts;
+        } else {
+            // an expert's last tile is half empty
+            tm = a.offsets ? a.m / s.tile + (std::min(experts, a.m) + 1) / 2
+                           : (a.m + s.tile - 1) / s.tile;
+        }
+        const int64_t slabs = std::max<int64_t>(1, (k + slab - 1) / slab);
+        const int64_t rows = a.mode == kWeight ? a.m * experts : a.m;
+        for (int32_t parts = 1; parts <= 32 && parts <= slabs; parts *= 2) {
+            const int64_t floats =
+                parts > 1 ? parts * rows * (tn * s.tile + 1) : 0;
+            if (floats > (int64_t)1 << 30) break;
+            const double rounds =
+                std::ceil((double)(tm * tn * parts) / ((double)num_cus * s.held));
+            const double each = ((slabs + parts - 1) / parts) *
+                                    (a.type == kF32 ? s.single : s.half) + 4.0;
+            const double join = parts > 1 ? 4.0 + floats * 4.0 / 2.5e6 : 0.0;
+            const double time = rounds * each + join;
+            if (time < least) {
+                least = time;
+                best.tile = s.tile;
+                best.splits = parts;
+                best.partial_floats = floats;
+            }
+        }
+    }
+    return best;
+}
+
+}  // namespace som
+
+namespace {
+
+using som::ProductArgs;
+using som::ProductPlan;
+
+som_status from_hip(hipError_t e) {
+    if (e == hipSuccess) return SOM_OK;
+    if (e == hipErrorOutOfMemory || e == hipErrorMemoryAllocation) return SOM_E_OOM;
+    if (e == hipErrorInvalidValue) return SOM_E_UNSUPPORTED;  // a grid beyond its limits
+    return SOM_E_DEVICE;
+}
+
+bool type_ok(int32_t t) { return t == SOM_F32 || t == SOM_BF16 || t == SOM_F16; }
+bool activation_ok(int32_t a) { return a >= SOM_ACT_NONE && a <= SOM_ACT_SILU; }
+
+// rows rows of cols elements, ld apart, at p.
+bool rows_ok(const void *p, int64_t rows, int64_t cols, int64_t ld, int size) {
+    if (rows == 0 || cols == 0) return true;
+    if (!p || ld < cols || reinterpret_cast<uintptr_t>(p) % size != 0) return false;
+    unsigned __int128 elems = (unsigned __int128)(rows - 1) * (uint64_t)ld + (uint64_t)cols;
+    if (elems > (unsigned __int128)1 << 56) return false;
+    return som::device_range_ok(p, (uint64_t)elems * size);
+}
+bool rows_ok_or_null(const void *p, int64_t rows, int64_t cols, int64_t ld, int size) {
+    return !p || rows_ok(p, rows, cols, ld, size);
+}
+
+int compute_units() {
+    static int cus = [] {
+        int dev = 0, v = 0;
+        if (hipGetDevice(&dev) != hipSuccess ||
+            hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) {
+            (void)hipGetLastError();
+            v = 256;
+        }
+        return v > 0 ? v : 256;
+    }();
+    return cus;
+}
+
+// Takes pieces of the caller's work memory, or, without one, adds up what they need.
+struct Carver {
+    char *base;
+    uint64_t used = 0;
+    explicit Carver(void *p) : base(static_cast<char *>(p)) {}
+    template <typename T = void>
+    T *take(uint64_t bytes) {
+        char *at = base ? base + used : nullptr;
+        used += (bytes + 255) / 256 * 256;
+        return reinterpret_cast<T *>(at);
+    }
+};
+
+// A matrix as a product reads it.
+struct Operand {
+    const void *p;
+    int64_t ld;
+};
+
+int64_t rounded(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+// One side of a product: the caller's rows where they lie in whole 16-byte
+// pieces, else (or where a slope has to be applied) a copy whose rows do.
+struct SideCopy {
+    som::RowsArgs rows{};
+    bool needed = false;
+};
+Operand whole_rows(Carver &work, SideCopy &copy, int32_t type, const void *p, int64_t rows,
+                   int64_t cols, int64_t ld, const void *z = nullptr, int32_t activation = 0) {
+    const int size = som::type_size(type), per = 16 / size;
+    const bool whole = reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % per == 0 && cols % per == 0;
+    if (whole && !z) return {p, ld};
+    const int64_t ldd = rounded(cols, per);
+    void *to = work.take((uint64_t)rows * ldd * size);
+    copy.needed = true;
+    copy.rows.type = type;
+    copy.rows.activation = activation;
+    copy.rows.src = p;
+    copy.rows.z = z;
+    copy.rows.dst = to;
+    copy.rows.rows = rows;
+    copy.rows.cols = cols;
+    copy.rows.lds = ld;
+    copy.rows.ldz = cols;
+    copy.rows.ldd = ldd;
+    return {to, ldd};
+}
+
+bool four(const void *p, int64_t ld, int size) {
+    return reinterpret_cast<uintptr_t>(p) % (4 * size) == 0 && ld % 4 == 0;
+}
+
+hipError_t launch_product(const ProductArgs &a, const ProductPlan &plan, hipStream_t s) {
+    switch (a.type) {
+        case SOM_F32: return som::launch_product_f32(a, plan, s);
+        case SOM_BF16: return som::launch_product_bf16(a, plan, s);
+        default: return som::launch_product_f16(a, plan, s);
+    }
+}
+
+// One product of a call, planned, with its parts' memory.
+struct Product {
+    ProductArgs a{};
+    ProductPlan plan{};
+    void place(Carver &work) {
+        plan = som::plan_product(a, compute_units());
+        if (plan.splits > 1) {
+            a.partial = work.take<float>((uint64_t)plan.partial_floats * 4);
+            a.partial_rows = a.mode == som::kWeight ? a.m * (a.offsets ? a.experts : 1) : a.m;
+        }
+    }
+};
+
+// What a call enqueues, over the caller's work memory.
+struct LinearForward {
+    SideCopy x, w;
+    Product product;
+    LinearForward(const som_linear_call &c, Carver &work) {
+        const int size = som::type_size(c.type);
+        const int64_t rows = c.experts ? c.n * c.k : c.n;
+        const int64_t xrows = c.gather ? c.n : rows;
+        const int64_t wrows = (int64_t)c.outer * std::max(1, c.experts);
+        ProductArgs &a = product.a;
+        a.mode = som::kForward;
+        a.type = c.type;
+        a.activation = c.activation;
+        a.m = rows, a.n = c.outer, a.k = c.inner;
+        a.offsets = c.experts ? c.offsets : nullptr;
+        a.experts = c.experts, a.per = c.k;
+        a.list = c.experts && c.gather ? c.order : nullptr;
+        a.bias = c.bias;
+        a.residual = c.residual, a.ldr = c.ldr;
+        a.y = c.y, a.z = c.z;
+        a.vec = (four(c.y, c.outer, size) && (!c.z || four(c.z, c.outer, size)) ? som::kVecOut : 0) |
+                (c.bias && four(c.bias, c.outer, size) ? som::kVecBias : 0) |
+                (c.residual && four(c.residual, c.ldr, size) ? som::kVecResidual : 0);
+        product.place(work);
+        Operand A{c.x, c.ldx}, B{c.w, c.inner};
+        if (product.plan.waves) {   // reads any rows
+            const int per = 16 / size;
+            product.plan.aligned = reinterpret_cast<uintptr_t>(c.x) % 16 == 0 &&
+                                   reinterpret_cast<uintptr_t>(c.w) % 16 == 0 &&
+                                   c.ldx % per == 0 && c.inner % per == 0;
+        } else {
+            A = whole_rows(work, x, c.type, c.x, xrows, c.inner, c.ldx);
+            B = whole_rows(work, w, c.type, c.w, wrows, c.inner, c.inner);
+        }
+        a.a = A.p, a.lda = A.ld;
+        a.b = B.p, a.ldb = B.ld, a.batch_b = B.ld * c.outer;
+    }
+};
+
+struct LinearBackward {
+    SideCopy x, w, dz;
+    Product input, weight;
+    bool has_input, has_weight;
+    LinearBackward(const som_linear_call &c, Carver &work) {
+        const int size = som::type_size(c.type);
+        const int64_t rows = c.experts ? c.n * c.k : c.n;
+        const int64_t xrows = c.gather ? c.n : rows;
+        const int64_t wrows = (int64_t)c.outer * std::max(1, c.experts);
+        has_input = c.dx != nullptr;
+        has_weight = c.dw != nullptr || c.dbias != nullptr;
+        const Operand Z = whole_rows(work, dz, c.type, c.dy, rows, c.outer, c.lddy,
+                                     c.activation != SOM_ACT_NONE ? c.z : nullptr, c.activation);
+        if (has_input) {
+            const Operand W = whole_rows(work, w, c.type, c.w, wrows, c.inner, c.inner);
+            ProductArgs &a = input.a;
+            a.mode = som::kInput;
+            a.type = c.type;
+            a.m = rows, a.n = c.inner, a.k = c.outer;
+            a.offsets = c.experts ? c.offsets : nullptr;
+            a.experts = c.experts, a.per = 1;
+            a.a = Z.p, a.lda = Z.ld;
+            a.b = W.p, a.ldb = W.ld, a.batch_b = W.ld * c.outer;
+            a.y = c.dx;
+            a.slope = c.slope_z, a.activation = c.slope_activation;
+            a.vec = (four(c.dx, c.inner, size) ? som::kVecOut : 0) |
+                    (c.slope_z && four(c.slope_z, c.inner, size) ? som::kVecSlope : 0);
+            input.place(work);
+        }
+        if (has_weight) {
+            const Operand X = whole_rows(work, x, c.type, c.x, xrows, c.inner, c.ldx);
+            ProductArgs &a = weight.a;
+            a.mode = som::kWeight;
+            a.type = c.type;
+            a.m = c.outer, a.n = c.inner, a.k = rows;
+            a.offsets = c.experts ? c.offsets : nullptr;
+            a.experts = c.experts, a.per = c.k;
+            a.list = c.experts && c.gather ? c.order : nullptr;
+            a.a = Z.p, a.lda = Z.ld;
+            a.b = X.p, a.ldb = X.ld;
+            a.y = c.dw, a.bias_grad = c.dbias;
+            a.vec = four(c.dw, c.inner, size) ? som::kVecOut : 0;
+            weight.place(work);
+        }
+    }
+};
+
+// The sizes and types of a call; the pointers are checked apart, where a call
+// is about to run.
+som_status linear_sizes_ok(const som_linear_call *c) {
+    if (!c || !type_ok(c->type) || !activation_ok(c->activation) || c->n < 0 || c->inner <= 0 ||
+        c->outer <= 0 || c->experts < 0)
+        return SOM_E_ARG;
+    if (c->experts ? c->k <= 0 : (c->k != 0 || c->gather)) return SOM_E_ARG;
+    if (c->ldx < c->inner) return SOM_E_ARG;
+    const __int128 rows = (__int128)c->n * (c->experts ? c->k : 1);
+    if (c->experts && rows > INT32_MAX) return SOM_E_UNSUPPORTED;
+    if (rows > (__int128)1 << 40) return SOM_E_UNSUPPORTED;
+    if ((int64_t)c->outer * std::max(1, c->experts) > INT32_MAX) return SOM_E_UNSUPPORTED;
+    return SOM_OK;
+}
+
+bool linear_common_ok(const som_linear_call &c) {
+    const int size = som::type_size(c.type);
+    const int64_t rows = c.experts ? c.n * c.k : c.n, xrows = c.gather ? c.n : rows;
+    const int64_t wrows = (int64_t)c.outer * std::max(1, c.experts);
+    if (!rows_ok(c.w, wrows, c.inner, c.inner, size)) return false;
+    if (!rows_ok(c.x, xrows, c.inner, c.ldx, size)) return false;
+    if (c.experts) {
+        if (!rows_ok(c.offsets, 1, c.experts + 1, c.experts + 1, 4)) return false;
+        if (c.gather && !rows_ok(c.order, 1, rows, rows, 4)) return false;
+    }
+    return true;
+}
+
+som_status work_ok(const Carver &need, const som_linear_call &c) {
+    if (need.used == 0) return SOM_OK;
+    if (!c.workspace || reinterpret_cast<uintptr_t>(c.workspace) % 256 != 0 ||
+        c.workspace_bytes < need.used || !som::device_range_ok(c.workspace, need.used))
+        return SOM_E_ARG;
+    return SOM_OK;
+}
+
+hipError_t run_copy(const SideCopy &c, hipStream_t s) {
+    return c.needed ? som::launch_rows_copy(c.rows, s) : hipSuccess;
+}
+
+}  // namespace
+
+extern "C" {
+
+som_status som_linear_workspace(const som_linear_call *c, int32_t backward, uint64_t *bytes) {
+    if (!bytes) return SOM_E_ARG;
+    const som_status st = linear_sizes_ok(c);
+    if (st != SOM_OK) return st;
+    Carver need(nullptr);
+    if (backward) LinearBackward(*c, need);
+    else LinearForward(*c, need);
+    *bytes = c->n ? need.used : 0;
+    return SOM_OK;
+}
+
+som_status som_linear(const som_linear_call *c) {
+    som_status st = linear_sizes_ok(c);
+    if (st != SOM_OK) return st;
+    const int size = som::type_size(c->type);
+    const int64_t rows = c->experts ? c->n * c->k : c->n;
+    if (c->n && !c->y) return SOM_E_ARG;
+    if (!linear_common_ok(*c) || !rows_ok(c->y, rows, c->outer, c->outer, size) ||
+        !rows_ok_or_null(c->z, rows, c->outer, c->outer, size) ||
+        !rows_ok_or_null(c->bias, std::max(1, c->experts), c->outer, c->outer, size) ||
+        !rows_ok_or_null(c->residual, rows, c->outer, c->ldr, size))
+        return SOM_E_ARG;
+    if (c->n == 0) return SOM_OK;
+    Carver need(nullptr);
+    LinearForward(*c, need);
+    st = work_ok(need, *c);
+    if (st != SOM_OK) return st;
+    Carver work(c->workspace);
+    const LinearForward f(*c, work);
+    const hipStream_t s = reinterpret_cast<hipStream_t>(c->stream);
+    hipError_t e = run_copy(f.x, s);
+    if (e == hipSuccess) e = run_copy(f.w, s);
+    if (e == hipSuccess) e = launch_product(f.product.a, f.product.plan, s);
+    return from_hip(e);
+}
+
+som_status som_linear_backward(const som_linear_call *c) {
+    som_status st = linear_sizes_ok(c);
+    if (st != SOM_OK) return st;
+    if (!activation_ok(c->slope_activation)) return SOM_E_ARG;
+    const int size = som::type_size(c->type);
+    const int64_t rows = c->experts ? c->n * c->k : c->n;
+    const int64_t wrows = (int64_t)c->outer * std::max(1, c->experts);
+    if (!c->dw && c->dbias) return SOM_E_ARG;   // the bias's sums come with dw's product
+    if (!linear_common_ok(*c) || !rows_ok(c->dy, rows, c->outer, c->lddy, size) ||
+        (c->activation != SOM_ACT_NONE && !rows_ok(c->z, rows, c->outer, c->outer, size)) ||
+        !rows_ok_or_null(c->dx, rows, c->inner, c->inner, size) ||
+        !rows_ok_or_null(c->dw, wrows, c->inner, c->inner, size) ||
+        !rows_ok_or_null(c->dbias, wrows, 1, 1, size) ||
+        !rows_ok_or_null(c->slope_z, rows, c->inner, c->inner, size))
+        return SOM_E_ARG;
+    const hipStream_t s = reinterpret_cast<hipStream_t>(c->stream);
+    Carver need(nullptr);
+    LinearBackward(*c, need);
+    if (c->n) {
+        st = work_ok(need, *c);
+        if (st != SOM_OK) return st;
+    }
+    Carver work(c->workspace);
+    LinearBackward b(*c, work);
+    if (c->n == 0) {   // no rows: nothing to copy, dx is empty, the sums are 0
+        b.has_input = false;
+        b.dz.needed = b.x.needed = false;
+        if (b.has_weight) b.weight.plan.splits = 1;
+    }
+    hipError_t e = run_copy(b.dz, s);
+    if (e == hipSuccess && b.has_input) {
+        e = run_copy(b.w, s);
+        if (e == hipSuccess) e = launch_product(b.input.a, b.input.plan, s);
+    }
+    if (e == hipSuccess && b.has_weight) {
+        e = run_copy(b.x, s);
+        if (e == hipSuccess) e = launch_product(b.weight.a, b.weight.plan, s);
+    }
+    return from_hip(e);
+}
+
+static som_status route_ok(const som_route_call *c) {
+    if (!c || !type_ok(c->type) || (c->gate != SOM_GATE_SOFTMAX && c->gate != SOM_GATE_SIGMOID))
+        return SOM_E_ARG;
+    if (c->n < 0 || c->experts < 1 || c->experts > som::kMaxExperts || c->k < 1 ||
+        c->k > std::min(c->experts, som::kMaxChoices))
+        return SOM_E_ARG;
+    if (c->groups < 1 || c->groups > som::kMaxGroups || c->experts % c->groups != 0 ||
+        c->top_groups < 1 || c->top_groups > c->groups || c->group_best < 1 || c->group_best > 2)
+        return SOM_E_ARG;
+    if (!isfinite(c->scale) || c->lds < c->experts) return SOM_E_ARG;
+    if ((__int128)c->n * c->k > INT32_MAX) return SOM_E_UNSUPPORTED;
+    if (!rows_ok(c->scores, c->n, c->experts, c->lds, som::type_size(c->type)) ||
+        !rows_ok(c->index, c->n, c->k, c->k, 4) || !rows_ok(c->weight, c->n, c->k, c->k, 4) ||
+        !rows_ok_or_null(c->bias, 1, c->experts, c->experts, 4))
+        return SOM_E_ARG;
+    return SOM_OK;
+}
+
+static som::RouteArgs route_args(const som_route_call &c) {
+    som::RouteArgs a{};
+    a.type = c.type;
+    a.softmax = c.gate == SOM_GATE_SOFTMAX;
+    a.n = c.n;
+    a.experts = c.experts;
+    a.k = c.k;
+    a.groups = c.groups;
+    a.top_groups = c.top_groups;
+    a.group_best = c.group_best;
+    a.renormalise = c.renormalise != 0;
+    a.scale = c.scale;
+    a.scores = c.scores;
+    a.lds = c.lds;
+    a.bias = c.bias;
+    a.index = c.index;
+    a.weight = c.weight;
+    a.dweight = c.dweight;
+    a.dweight_type = c.dweight_type;
+    a.dscores = c.dscores;
+    return a;
+}
+
+som_status som_route(const som_route_call *c) {
+    const som_status st = route_ok(c);
+    if (st != SOM_OK) return st;
+    return from_hip(som::launch_route(route_args(*c), reinterpret_cast<hipStream_t>(c->stream)));
+}
+
+som_status som_route_backward(const som_route_call *c) {
+    const som_status st = route_ok(c);
+    if (st != SOM_OK) return st;
+    if (!type_ok(c->dweight_type) ||
+        !rows_ok(c->dweight, c->n, c->k, c->k, som::type_size(c->dweight_type)) ||
+        !rows_ok(c->dscores, c->n, c->experts, c->experts, som::type_size(c->type)))
+        return SOM_E_ARG;
+    return from_hip(
+        som::launch_route_backward(route_args(*c), reinterpret_cast<hipStream_t>(c->stream)));
+}
+
+som_status som_dispatch_workspace(int64_t n, int32_t k, int32_t experts, uint64_t *bytes) {
+    if (!bytes || n < 0 || k < 1 || experts < 1 || experts > som::kMaxExperts) return SOM_E_ARG;
+    if ((__int128)n * k > INT32_MAX) return SOM_E_UNSUPPORTED;
+    const int32_t blocks = som::dispatch_blocks(n * k);
+    *bytes = blocks > 1 ? (uint64_t)blocks * experts * 4 : 0;
+    return SOM_OK;
+}
+
+som_status som_dispatch(const int32_t *index, int64_t n, int32_t k, int32_t experts,
+                        int32_t *offsets, int32_t *order, int32_t *place, void *work,
+                        uint64_t work_bytes, void *stream) {
+    uint64_t need = 0;
+    const som_status st = som_dispatch_workspace(n, k, experts, &need);
+    if (st != SOM_OK) return st;
+    if (!rows_ok(index, n, k, k, 4) || !rows_ok(offsets, 1, experts + 1, experts + 1, 4) ||
+        !rows_ok(order, n, k, k, 4) || !rows_ok(place, n, k, k, 4))
+        return SOM_E_ARG;
+    if (need && (work_bytes < need || !rows_ok(work, 1, need / 4, need / 4, 4))) return SOM_E_ARG;
+    som::DispatchArgs a{};
+    a.index = index;
+    a.slots = n * k;
+    a.experts = experts;
+    a.offsets = offsets;
+    a.order = order;
+    a.place = place;
+    a.counts = static_cast<int32_t *>(work);
+    a.blocks = som::dispatch_blocks(a.slots);
+    return from_hip(som::launch_dispatch(a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+static som_status combine_ok(int32_t type, int64_t n, int32_t k, int32_t width, const void *y,
+                             const float *weight, const int32_t *place) {
+    if (!type_ok(type) || n < 0 || k < 1 || width < 1) return SOM_E_ARG;
+    if ((__int128)n * k > INT32_MAX) return SOM_E_UNSUPPORTED;
+    if (!rows_ok_or_null(y, n * k, width, width, som::type_size(type)) ||
+        !rows_ok_or_null(weight, n, k, k, 4) || !rows_ok(place, n, k, k, 4))
+        return SOM_E_ARG;
+    return SOM_OK;
+}
+
+som_status som_combine(int32_t type, int64_t n, int32_t k, int32_t width, const void *y,
+                       const float *weight, const int32_t *place, const void *residual,
+                       int64_t ldr, void *out, void *stream) {
+    const som_status st = combine_ok(type, n, k, width, y, weight, place);
+    if (st != SOM_OK) return st;
+    const int size = som::type_size(type);
+    if ((n && !y) || !rows_ok_or_null(residual, n, width, ldr, size) ||
+        !rows_ok(out, n, width, width, size))
+        return SOM_E_ARG;
+    som::CombineArgs a{};
+    a.type = type, a.k = k, a.n = n, a.width = width;
+    a.y = y, a.weight = weight, a.place = place;
+    a.residual = residual, a.ldr = ldr, a.out = out;
+    return from_hip(som::launch_combine(a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+som_status som_combine_backward(int32_t type, int64_t n, int32_t k, int32_t width,
+                                const void *dout, int64_t ldd, const void *y,
+                                const float *weight, const int32_t *place, void *dy,
+                                void *dweight, void *stream) {
+    const som_status st = combine_ok(type, n, k, width, y, weight, place);
+    if (st != SOM_OK) return st;
+    const int size = som::type_size(type);
+    if ((n && dweight && !y) || !rows_ok(dout, n, width, ldd, size) ||
+        !rows_ok(dy, n * k, width, width, size) || !rows_ok_or_null(dweight, n, k, k, size))
+        return SOM_E_ARG;
+    som::CombineArgs a{};
+    a.type = type, a.k = k, a.n = n, a.width = width;
+    a.y = y, a.weight = weight, a.place = place;
+    a.dout = dout, a.ldd = ldd, a.dy = dy, a.dweight = dweight;
+    return from_hip(som::launch_combine_backward(a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------ AdamW
+struct som_adamw {
+    int device = 0;
+    int32_t bits = 32, count = 0;
+    std::vector<int64_t> counts;         // elements of each tensor
+    std::vector<int32_t> first_chunk;    // of each launch of up to kAdamwGrads tensors
+    som::AdamwChunk *chunks = nullptr;   // device
+    som::AdamwTensor *tensors = nullptr; // device
+    void *mean = nullptr, *square = nullptr;
+    float *mean_scale = nullptr, *square_scale = nullptr, *master = nullptr;
+};
+
+extern "C" {
+
+int64_t som_adamw_room(const som_adamw_tensor *tensors, int32_t count) {
+    if (!tensors || count < 0) return -1;
+    int64_t room = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        if (tensors[i].count < 0 || tensors[i].count > (int64_t)1 << 48) return -1;
+        room += rounded(tensors[i].count, som::kAdamwBlock);
+    }
+    return room;
+}
+
+som_status som_adamw_destroy(som_adamw *opt) {
+    if (!opt) return SOM_OK;
+    hipError_t e = hipSuccess;
+    if (opt->chunks) e = hipFree(opt->chunks);
+    if (opt->tensors) {
+        const hipError_t f = hipFree(opt->tensors);
+        if (e == hipSuccess) e = f;
+    }
+    delete opt;
+    return from_hip(e);
+}
+
+static som_status adamw_create(const som_adamw_tensor *tensors, int32_t count, int32_t bits,
+                               void *mean, void *square, float *mean_scale, float *square_scale,
+                               float *master, som_adamw **out) {
+    const int64_t room = som_adamw_room(tensors, count);
+    const int64_t blocks = room / som::kAdamwBlock;
+    const int size = bits == 8 ? 1 : 4;
+    if (!rows_ok(mean, 1, room, room, size) || !rows_ok(square, 1, room, room, size) ||
+        !rows_ok_or_null(master, 1, room, room, 4))
+        return SOM_E_ARG;
+    // read four elements at a time, from multiples of four
+    const uintptr_t all = reinterpret_cast<uintptr_t>(mean) | reinterpret_cast<uintptr_t>(square);
+    if (all % (4 * size) != 0 || reinterpret_cast<uintptr_t>(master) % 16 != 0) return SOM_E_ARG;
+    if (bits == 8 && (!rows_ok(mean_scale, 1, blocks, blocks, 4) ||
+                      !rows_ok(square_scale, 1, blocks, blocks, 4)))
+        return SOM_E_ARG;
+    std::vector<som::AdamwChunk> chunks;
+    std::vector<som::AdamwTensor> table;
+    som_adamw *o = new som_adamw;
+    *out = o;   // released by the caller on failure
+    o->bits = bits;
+    o->count = count;
+    o->mean = mean, o->square = square;
+    o->mean_scale = mean_scale, o->square_scale = square_scale, o->master = master;
+    constexpr int32_t kStep = som::kAdamwChunk / som::kAdamwBlock;
+    int64_t state = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        const som_adamw_tensor &t = tensors[i];
+        if (!type_ok(t.type) ||
+            (t.count && !rows_ok(t.param, 1, t.count, t.count, som::type_size(t.type))))
+            return SOM_E_ARG;
+        if (i % som::kAdamwGrads == 0) o->first_chunk.push_back((int32_t)chunks.size());
+        const int64_t nblocks = rounded(t.count, som::kAdamwBlock) / som::kAdamwBlock;
+        if (nblocks > INT32_MAX - kStep ||
+            (int64_t)chunks.size() + nblocks / kStep + 1 > INT32_MAX)
+            return SOM_E_UNSUPPORTED;
+        for (int64_t b = 0; b < nblocks; b += kStep)
+            chunks.push_back({i % som::kAdamwGrads, (int32_t)b});
+        table.push_back({t.param, t.count, state, t.type, 0});
+        o->counts.push_back(t.count);
+        state += nblocks * som::kAdamwBlock;
+    }
+    o->first_chunk.push_back((int32_t)chunks.size());
+    hipError_t e = hipGetDevice(&o->device);
+    if (!chunks.empty()) {
+        const size_t cb = chunks.size() * sizeof(chunks[0]), tb = table.size() * sizeof(table[0]);
+        if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void **>(&o->chunks), cb);
+        if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void **>(&o->tensors), tb);
+        if (e == hipSuccess) e = hipMemcpy(o->chunks, chunks.data(), cb, hipMemcpyHostToDevice);
+        if (e == hipSuccess) e = hipMemcpy(o->tensors, table.data(), tb, hipMemcpyHostToDevice);
+        if (e == hipSuccess) e = hipDeviceSynchronize();
+    }
+    return from_hip(e);
+}
+
+som_status som_adamw_create(const som_adamw_tensor *tensors, int32_t count, int32_t bits,
+                            void *mean, void *square, float *mean_scale, float *square_scale,
+                            float *master, som_adamw **out) {
+    if (!out) return SOM_E_ARG;
+    *out = nullptr;
+    if (som_adamw_room(tensors, count) < 0 || count == 0 || (bits != 8 && bits != 32))
+        return SOM_E_ARG;
+    if ((bits == 8) != (mean_scale != nullptr) || (bits == 8) != (square_scale != nullptr))
+        return SOM_E_ARG;
+    som_adamw *o = nullptr;
+    som_status st;
+    try {
+        st = adamw_create(tensors, count, bits, mean, square, mean_scale, square_scale, master, &o);
+    } catch (const std::bad_alloc &) {
+        st = SOM_E_OOM;
+    } catch (...) {
+        st = SOM_E_DEVICE;
+    }
+    if (st != SOM_OK) {
+        (void)som_adamw_destroy(o);
+        return st;
+    }
+    *out = o;
+    return SOM_OK;
+}
+
+som_status som_adamw_step(som_adamw *o, const void *const *grads, const int32_t *grad_types,
+                          int64_t step, double lr, double beta1, double beta2, double eps,
+                          double weight_decay, void *stream) {
+    if (!o || !grads || !grad_types || step < 1) return SOM_E_ARG;
+    if (!(lr >= 0.0) || !(eps >= 0.0) || !(weight_decay >= 0.0) || isinf(lr) || isinf(eps) ||
+        isinf(weight_decay) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0))
+        return SOM_E_ARG;
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess) return SOM_E_DEVICE;
+    if (dev != o->device) return SOM_E_ARG;
+    for (int32_t i = 0; i < o->count; ++i) {
+        if (!type_ok(grad_types[i])) return SOM_E_ARG;
+        if (!rows_ok(grads[i], 1, o->counts[i], o->counts[i], som::type_size(grad_types[i])))
+            return SOM_E_ARG;
+    }
+    som::AdamwArgs a{};
+    a.mean = o->mean, a.square = o->square;
+    a.mean_scale = o->mean_scale, a.square_scale = o->square_scale;
+    a.master = o->master;
+    a.beta1 = (float)beta1;
+    a.rest1 = (float)(1.0 - beta1);
+    a.beta2 = (float)beta2;
+    a.rest2 = (float)(1.0 - beta2);
+    a.decay = (float)(1.0 - lr * weight_decay);
+    a.rate = (float)(lr / (1.0 - pow(beta1, (double)step)));
+    a.root_scale = (float)(1.0 / sqrt(1.0 - pow(beta2, (double)step)));
+    a.eps = (float)eps;
+    for (int32_t l = 0; l * som::kAdamwGrads < o->count; ++l) {
+        const int32_t t0 = l * som::kAdamwGrads;
+        const int32_t tensors = std::min(o->count - t0, (int32_t)som::kAdamwGrads);
+        for (int32_t i = 0; i < tensors; ++i) {
+            a.grads[i] = grads[t0 + i];
+            a.grad_type[i] = (unsigned char)grad_types[t0 + i];
+        }
+        a.chunks = o->chunks + o->first_chunk[l];
+        a.tensors = o->tensors + t0;
+        a.nchunks = o->first_chunk[l + 1] - o->first_chunk[l];
+        const hipError_t e = som::launch_adamw(a, o->bits == 8,
+                                               reinterpret_cast<hipStream_t>(stream));
+        if (e != hipSuccess) return from_hip(e);
+    }
+    return SOM_OK;
+}
+
+}  // extern "C"

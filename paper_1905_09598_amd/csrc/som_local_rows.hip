@@ -1,0 +1,186 @@
+// Row-wise passes of the local models: operand rows copied to whole 16-byte
+// pieces (with the activation's slope applied on the way where a gradient needs
+// it), and the experts' answers joined per document, with their gradients.  All
+// are bound by memory: each element is read and written once, 16 bytes a lane
+// where the rows allow it.
+#include "som_local_internal.h"
+
+namespace som {
+namespace {
+
+constexpr int kThreads = 256;
+
+// N neighbouring values of a row, `left` of them there.
+template <typename T, int N>
+__device__ inline void read_some(const T *p, int64_t left, bool vec, float (&v)[N]) {
+    if (vec && left >= N) {
+        typedef T tn __attribute__((ext_vector_type(N)));
+        const tn q = *reinterpret_cast<const tn *>(p);
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = (float)q[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = e < left ? (float)p[e] : 0.f;
+    }
+}
+template <typename T, int N>
+__device__ inline void write_some(T *p, int64_t left, bool vec, const float (&v)[N]) {
+    if (vec && left >= N) {
+        typedef T tn __attribute__((ext_vector_type(N)));
+        tn q;
+#pragma unroll
+        for (int e = 0; e < N; ++e) q[e] = (T)v[e];
+        *reinterpret_cast<tn *>(p) = q;
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (e < left) p[e] = (T)v[e];
+    }
+}
+
+enum { kVecSrc = 1, kVecZ = 2, kVecDout = 1, kVecRows = 2, kVecRes = 4 };
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void rows_copy_kernel(RowsArgs a, int vec) {
+    constexpr int N = 16 / sizeof(T);
+    const int64_t pieces = a.ldd / N;   // of a row; ldd is a multiple of N
+    const int64_t q = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int64_t row = q / pieces, col = q % pieces * N;
+    if (row >= a.rows) return;
+    float v[N], z[N];
+    read_some<T, N>(static_cast<const T *>(a.src) + row * a.lds + col, a.cols - col, vec & kVecSrc,
+                    v);
+    if (a.z) {
+        read_some<T, N>(static_cast<const T *>(a.z) + row * a.ldz + col, a.cols - col, vec & kVecZ,
+                        z);
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = col + e < a.cols ? v[e] * activation_slope(z[e], a.activation) : 0.f;
+    }
+    write_some<T, N>(static_cast<T *>(a.dst) + row * a.ldd + col, N, true, v);
+}
+
+// 16 bytes of a document's row a thread.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a, int vec) {
+    constexpr int N = 16 / sizeof(T);
+    const int64_t pieces = (a.width + N - 1) / N;
+    const int64_t q = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int64_t i = q / pieces, col = q % pieces * N, left = a.width - col;
+    if (i >= a.n) return;
+    float sum[N], y[N], first[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) sum[e] = 0.f;
+    for (int j = 0; j < a.k; ++j) {
+        const int p = a.place[i * a.k + j];
+        const float w = a.weight ? a.weight[i * a.k + j] : 1.f;
+        if (p >= 0) {
+            read_some<T, N>(static_cast<const T *>(a.y) + p * a.width + col, left, vec & kVecRows,
+                            y);
+#pragma unroll
+            for (int e = 0; e < N; ++e) sum[e] = fmaf(w, y[e], sum[e]);
+        } else if (w != w) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) sum[e] = w;
+        }
+    }
+    if (a.residual) {
+        read_some<T, N>(static_cast<const T *>(a.residual) + i * a.ldr + col, left, vec & kVecRes,
+                        first);
+#pragma unroll
+        for (int e = 0; e < N; ++e) sum[e] += first[e];
+    }
+    write_some<T, N>(static_cast<T *>(a.out) + i * a.width + col, left, vec & kVecRows, sum);
+}
+
+// One choice of a document a wave: its row of dy, and the product of the two
+// rows, summed over the lanes in a fixed order.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void combine_backward_kernel(CombineArgs a, int vec) {
+    constexpr int N = 16 / sizeof(T);
+    const int lane = threadIdx.x & 63;
+    const int64_t s = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+    if (s >= a.n * a.k) return;
+    const int64_t i = s / a.k;
+    const int p = a.place[s];
+    float dot = 0.f;
+    if (p >= 0) {
+        const float w = a.weight ? a.weight[s] : 1.f;
+        const T *from = static_cast<const T *>(a.dout) + i * a.ldd;
+        const T *y = static_cast<const T *>(a.y) + p * a.width;
+        T *to = static_cast<T *>(a.dy) + p * a.width;
+        for (int64_t col = lane * N; col < a.width; col += 64 * N) {
+            float d[N], v[N];
+            read_some<T, N>(from + col, a.width - col, vec & kVecDout, d);
+            if (a.dweight) {
+                read_some<T, N>(y + col, a.width - col, vec & kVecRows, v);
+#pragma unroll
+                for (int e = 0; e < N; ++e) dot = fmaf(d[e], v[e], dot);
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e) d[e] *= w;
+            write_some<T, N>(to + col, a.width - col, vec & kVecRows, d);
+        }
+    }
+    if (a.dweight) {
+        for (int o = 32; o; o >>= 1) dot += __shfl_xor(dot, o);
+        if (lane == 0) static_cast<T *>(a.dweight)[s] = (T)dot;
+    }
+}
+
+bool whole_pieces(const void *p, int64_t ld, int size) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * size % 16 == 0;
+}
+
+template <typename F>
+hipError_t by_type(int32_t type, F f) {
+    switch (type) {
+        case kF32: f(float()); break;
+        case kBF16: f(__bf16()); break;
+        default: f(_Float16()); break;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rows_copy(const RowsArgs &a, hipStream_t stream) {
+    const int size = type_size(a.type);
+    const int64_t pieces = a.rows * (a.ldd * size / 16);
+    if (pieces == 0) return hipSuccess;
+    if ((pieces + kThreads - 1) / kThreads > INT32_MAX) return hipErrorInvalidValue;
+    const int vec = (whole_pieces(a.src, a.lds, size) ? kVecSrc : 0) |
+                    (a.z && whole_pieces(a.z, a.ldz, size) ? kVecZ : 0);
+    const unsigned blocks = (unsigned)((pieces + kThreads - 1) / kThreads);
+    return by_type(a.type, [&](auto t) {
+        rows_copy_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a, vec);
+    });
+}
+
+hipError_t launch_combine(const CombineArgs &a, hipStream_t stream) {
+    const int size = type_size(a.type);
+    const int64_t pieces = a.n * ((a.width * size + 15) / 16);
+    if (pieces == 0) return hipSuccess;
+    if ((pieces + kThreads - 1) / kThreads > INT32_MAX) return hipErrorInvalidValue;
+    const int vec = (whole_pieces(a.y, a.width, size) && whole_pieces(a.out, a.width, size)
+                         ? kVecRows : 0) |
+                    (a.residual && whole_pieces(a.residual, a.ldr, size) ? kVecRes : 0);
+    const unsigned blocks = (unsigned)((pieces + kThreads - 1) / kThreads);
+    return by_type(a.type, [&](auto t) {
+        combine_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a, vec);
+    });
+}
+
+hipError_t launch_combine_backward(const CombineArgs &a, hipStream_t stream) {
+    const int size = type_size(a.type);
+    const int64_t slots = a.n * a.k;
+    if (slots == 0) return hipSuccess;
+    const int vec = (whole_pieces(a.dout, a.ldd, size) ? kVecDout : 0) |
+                    ((!a.y || whole_pieces(a.y, a.width, size)) && whole_pieces(a.dy, a.width, size)
+                         ? kVecRows : 0);
+    const unsigned blocks = (unsigned)((slots + kThreads / 64 - 1) / (kThreads / 64));
+    return by_type(a.type, [&](auto t) {
+        combine_backward_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a, vec);
+    });
+}
+
+}  // namespace som

@@ -1,0 +1,580 @@
+// Routing: which experts a document goes to, with which weights, and the
+// documents in the order of their experts.
+//
+// route: a row of scores lies in the registers of 16 lanes or of a wave, V
+// neighbours to a lane, so that the lowest lane and element of equal values is the
+// lowest expert; rows of more than 2048 experts lie in LDS, one to a workgroup.
+// The k choices are k maxima over the row: one per lane, joined across the
+// lanes.  Bound by these maxima (about 20 k instructions a row), not by the
+// read of the scores.
+#include "som_local_internal.h"
+
+#include <math.h>
+
+namespace som {
+namespace {
+
+constexpr int kRouteThreads = 256;
+
+template <int LANES, typename F>
+__device__ inline float across(float v, F join) {
+    // rotations within rows of 16 lanes, then across the rows
+    v = join(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x128, 0xf, 0xf, false)));
+    v = join(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x124, 0xf, 0xf, false)));
+    v = join(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x122, 0xf, 0xf, false)));
+    v = join(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x121, 0xf, 0xf, false)));
+    if (LANES == 64) {
+        v = join(v, __shfl_xor(v, 16));
+        v = join(v, __shfl_xor(v, 32));
+    }
+    return v;
+}
+template <int LANES>
+__device__ inline float across_max(float v) {
+    return across<LANES>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+// In the same order for every lane: the sum is the same in all of them.
+template <int LANES>
+__device__ inline float across_sum(float v) {
+    return across<LANES>(v, [](float a, float b) { return a + b; });
+}
+
+// The lanes of this lane's row of LANES for which `is` holds, the row's first
+// lane in bit 0.
+template <int LANES>
+__device__ inline unsigned long long row_ballot(bool is) {
+    const unsigned long long all = __ballot(is);
+    return LANES == 64 ? all : all >> (threadIdx.x & 48) & 0xffff;
+}
+
+__device__ inline float sigmoid(float s) { return 1.f / (1.f + expf(-s)); }
+
+// The value that the choice goes by; -infinity: closed.
+__device__ inline float choice_value(float s, bool softmax, const float *bias, int e) {
+    float v = softmax ? s : sigmoid(s);
+    if (bias) v += bias[e];
+    return s > -INFINITY && v > -INFINITY ? v : -INFINITY;
+}
+
+// Whether a score makes its whole row invalid.
+__device__ inline bool spoils(float s, bool softmax) {
+    return s != s || (softmax && s == INFINITY);
+}
+
+// The groups that stay, as bits.  Lane g < groups holds group g's value.
+template <int LANES>
+__device__ inline unsigned long long groups_that_stay(float value, int lane, int groups, int top) {
+    int before = 0;
+    for (int h = 0; h < groups; ++h) {
+        const float other = __shfl(value, h, LANES);
+        before += other > value || (other == value && h < lane) ? 1 : 0;
+    }
+    return row_ballot<LANES>(lane < groups && before < top && value > -INFINITY);
+}
+
+// A row's weights from its choices: lane j holds choice j (index at, -1 for none).
+// `low`, `total`: the row's largest score and sum of e^(s - low) (softmax that is
+// not renormalised).
+template <typename T, int LANES>
+__device__ inline void write_choices(const RouteArgs &a, int64_t row, int lane, int at, bool bad,
+                                     float low, float total) {
+    const T *s = static_cast<const T *>(a.scores) + row * a.lds;
+    const bool here = lane < a.k && at >= 0;
+    const float score = here ? (float)s[at] : -INFINITY;
+    float w = 0.f;
+    if (a.softmax) {
+        if (a.renormalise) {
+            float top = across_max<LANES>(score);
+            top = top > -INFINITY ? top : 0.f;
+            const float e = here ? expf(score - top) : 0.f;
+            const float sum = across_sum<LANES>(e);
+            w = sum > 0.f ? e / sum : 0.f;
+        } else if (here) {
+            w = expf(score - low) / total;
+        }
+    } else {
+        w = here ? sigmoid(score) : 0.f;
+        if (a.renormalise) {
+            const float sum = across_sum<LANES>(w);
+            w = sum > 0.f ? w / sum : 0.f;
+        }
+    }
+    if (lane < a.k) {
+        a.index[row * a.k + lane] = bad ? -1 : at;
+        a.weight[row * a.k + lane] = bad ? NAN : w * a.scale;
+    }
+}
+
+// LANES lanes a row, V experts a lane.
+template <typename T, int LANES, int V>
+__global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, int vec) {
+    constexpr int kRows = kRouteThreads / LANES;
+    extern __shared__ float shared[];  // with groups: kRows x (experts + 1) values
+    const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
+    const int64_t row = (int64_t)blockIdx.x * kRows + slot;
+    const bool there = row < a.n;
+    const T *s = static_cast<const T *>(a.scores) + (there ? row : a.n - 1) * a.lds;
+    const int e0 = lane * V;
+    float x[V], pick[V];
+    if (vec && e0 + V <= a.experts) {
+        typedef T tv __attribute__((ext_vector_type(16 / sizeof(T))));
+        constexpr int kPer = 16 / sizeof(T);
+#pragma unroll
+        for (int p = 0; p < V / kPer; ++p) {
+            const tv q = reinterpret_cast<const tv *>(s + e0)[p];
+#pragma unroll
+            for (int c = 0; c < kPer; ++c) x[p * kPer + c] = (float)q[c];
+        }
+        if (V < kPer) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[v] = (float)s[e0 + v];
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = e0 + v < a.experts ? (float)s[e0 + v] : -INFINITY;
+    }
+    bool spoilt = false;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        spoilt |= spoils(x[v], a.softmax);
+        pick[v] = e0 + v < a.experts ? choice_value(x[v], a.softmax, a.bias, e0 + v) : -INFINITY;
+    }
+    const bool bad = row_ballot<LANES>(spoilt) != 0;
+
+    float low = -INFINITY, total = 1.f;
+    if (a.softmax && !a.renormalise) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) low = fmaxf(low, x[v]);
+        low = across_max<LANES>(low);
+        low = low > -INFINITY ? low : 0.f;
+        total = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) total += expf(x[v] - low);
+        total = across_sum<LANES>(total);
+        total = total > 0.f ? total : 1.f;
+    }
+
+    if (a.groups > 1) {
+        const int per = a.experts / a.groups;
+        float *mine = shared + slot * (a.experts + 1);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (e0 + v < a.experts) mine[e0 + v] = pick[v];
+        __syncthreads();
+        float value = -INFINITY;
+        for (int g = lane; g < a.groups; g += LANES) {  // groups <= LANES
+            float best = -INFINITY, next = -INFINITY;
+            for (int e = 0; e < per; ++e) {
+                const float v = mine[g * per + e];
+                next = fmaxf(next, fminf(best, v));
+                best = fmaxf(best, v);
+            }
+            value = a.group_best == 2 && next > -INFINITY ? best + next : best;
+        }
+        const unsigned long long stay = groups_that_stay<LANES>(value, lane, a.groups, a.top_groups);
+        int left = per - e0 % per;
+        unsigned long long bits = e0 < a.experts ? stay >> e0 / per : 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (!(bits & 1)) pick[v] = -INFINITY;
+            if (--left == 0) bits >>= 1, left = per;
+        }
+    }
+
+    int at = -1;
+    for (int j = 0; j < a.k; ++j) {
+        float best = pick[0];
+#pragma unroll
+        for (int v = 1; v < V; ++v) best = fmaxf(best, pick[v]);
+        const float top = across_max<LANES>(best);
+        const unsigned long long who = row_ballot<LANES>(best == top);
+        const int first = __ffsll((long long)who) - 1;
+        int mine = 0;
+#pragma unroll
+        for (int v = V - 1; v >= 0; --v) mine = pick[v] == top ? v : mine;
+        const int won = __shfl(e0 + mine, first, LANES);
+        if (lane == j) at = top > -INFINITY ? won : -1;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (e0 + v == won) pick[v] = -INFINITY;
+    }
+    if (there) write_choices<T, LANES>(a, row, lane, at, bad, low, total);
+}
+
+// One row a workgroup of 256 threads, its values in LDS; thread t looks after
+// experts t, t + 256, ...
+template <typename T>
+__global__ __launch_bounds__(kRouteThreads) void route_long_kernel(RouteArgs a) {
+    extern __shared__ float pick[];    // experts values
+    __shared__ float part[4];
+    __shared__ int where[4];
+    __shared__ float group_value[kMaxGroups];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int64_t row = blockIdx.x;
+    const T *s = static_cast<const T *>(a.scores) + row * a.lds;
+    bool spoilt = false;
+    float low = -INFINITY;
+    for (int e = t; e < a.experts; e += kRouteThreads) {
+        const float x = (float)s[e];
+        spoilt |= spoils(x, a.softmax);
+        low = fmaxf(low, x);
+        pick[e] = choice_value(x, a.softmax, a.bias, e);
+    }
+    const bool bad = __syncthreads_or(spoilt);
+    float total = 1.f;
+    if (a.softmax && !a.renormalise) {
+        low = across_max<64>(low);
+        if (lane == 0) part[wave] = low;
+        __syncthreads();
+        low = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+        low = low > -INFINITY ? low : 0.f;
+        __syncthreads();
+        total = 0.f;
+        for (int e = t; e < a.experts; e += kRouteThreads) total += expf((float)s[e] - low);
+        total = across_sum<64>(total);
+        if (lane == 0) part[wave] = total;
+        __syncthreads();
+        total = (part[0] + part[1]) + (part[2] + part[3]);
+        total = total > 0.f ? total : 1.f;
+        __syncthreads();
+    }
+    if (a.groups > 1) {
+        const int per = a.experts / a.groups;
+        for (int g = wave; g < a.groups; g += 4) {
+            float best = -INFINITY, next = -INFINITY;
+            for (int e = lane; e < per; e += 64) {
+                const float v = pick[g * per + e];
+                next = fmaxf(next, fminf(best, v));
+                best = fmaxf(best, v);
+            }
+            for (int o = 1; o < 64; o <<= 1) {
+                const float b = __shfl_xor(best, o), n = __shfl_xor(next, o);
+                next = fmaxf(fmaxf(next, n), fminf(best, b));
+                best = fmaxf(best, b);
+            }
+            if (lane == 0)
+                group_value[g] = a.group_best == 2 && next > -INFINITY ? best + next : best;
+        }
+        __syncthreads();
+        const float value = lane < a.groups ? group_value[lane] : -INFINITY;
+        const unsigned long long stay = groups_that_stay<64>(value, lane, a.groups, a.top_groups);
+        for (int e = t; e < a.experts; e += kRouteThreads)
+            if (!(stay >> (e / per) & 1)) pick[e] = -INFINITY;
+    }
+    // the best of this thread's experts; found anew only by the thread that won
+    float best = -INFINITY;
+    int which = a.experts;
+    const auto look = [&] {
+        best = -INFINITY;
+        which = a.experts;
+        for (int e = t; e < a.experts; e += kRouteThreads)
+            if (pick[e] > best) best = pick[e], which = e;
+    };
+    look();
+    int at = -1;
+    for (int j = 0; j < a.k; ++j) {
+        float top = best;
+        int won = which;
+        for (int o = 1; o < 64; o <<= 1) {
+            const float b = __shfl_xor(top, o);
+            const int w = __shfl_xor(won, o);
+            if (b > top || (b == top && w < won)) top = b, won = w;
+        }
+        if (lane == 0) part[wave] = top, where[wave] = won;
+        __syncthreads();
+        top = part[0], won = where[0];
+#pragma unroll
+        for (int w = 1; w < 4; ++w)
+            if (part[w] > top || (part[w] == top && where[w] < won)) top = part[w], won = where[w];
+        if (lane == j) at = top > -INFINITY ? won : -1;
+        if (top > -INFINITY && which == won) {
+            pick[won] = -INFINITY;
+            look();
+        }
+        __syncthreads();
+    }
+    if (wave == 0) write_choices<T, 64>(a, row, lane, at, bad, low, total);
+}
+
+// Gradient of the scores.  LANES lanes a row: lane j works out choice j's part,
+// then the row is written once, the choices' parts put in from LDS.  Bound by
+// the write of the rows (and their read, for a softmax over the whole row).
+template <typename T, typename G, int LANES>
+__global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(RouteArgs a, int width) {
+    constexpr int kRows = kRouteThreads / LANES;
+    extern __shared__ float shared[];  // kRows x width: the choices' parts
+    const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
+    const int64_t row = (int64_t)blockIdx.x * kRows + slot;
+    const bool there = row < a.n;
+    const int64_t r = there ? row : a.n - 1;
+    const T *s = static_cast<const T *>(a.scores) + r * a.lds;
+    T *out = static_cast<T *>(a.dscores) + r * a.experts;
+    float *mine = shared + slot * width;
+    const int at = lane < a.k ? a.index[r * a.k + lane] : -1;
+    const bool here = at >= 0 && at < a.experts;
+    const float weight = lane < a.k ? a.weight[r * a.k + lane] : 0.f;
+    float g = here ? (float)static_cast<const G *>(a.dweight)[r * a.k + lane] : 0.f;
+    const bool bad = row_ballot<LANES>(weight != weight) != 0;
+    const float score = here ? (float)s[at] : -INFINITY;
+    float part;               // of the chosen score
+    float mean = 0.f, low = 0.f, total = 1.f;
+    const bool whole = a.softmax && !a.renormalise;
+    if (a.softmax) {
+        mean = across_sum<LANES>(g * weight);  // scale sum of g p
+        part = weight * (g - (a.scale != 0.f ? mean / a.scale : 0.f));
+        if (whole) {
+            low = -INFINITY;
+            for (int e = lane; e < a.experts; e += LANES) low = fmaxf(low, (float)s[e]);
+            low = across_max<LANES>(low);
+            low = low > -INFINITY ? low : 0.f;
+            total = 0.f;
+            for (int e = lane; e < a.experts; e += LANES) total += expf((float)s[e] - low);
+            total = across_sum<LANES>(total);
+            total = total > 0.f ? total : 1.f;
+            part = a.scale * g;
+        }
+    } else {
+        const float p = here ? sigmoid(score) : 0.f;
+        float by = a.scale;
+        if (a.renormalise) {
+            const float sum = across_sum<LANES>(p);
+            const float inner = across_sum<LANES>(g * p);
+            by = sum > 0.f ? a.scale / sum : 0.f;
+            g -= sum > 0.f ? inner / sum : 0.f;
+        }
+        part = by * g * p * (1.f - p);
+    }
+    for (int e0 = 0; e0 < a.experts; e0 += width) {
+        const int e1 = e0 + width < a.experts ? e0 + width : a.experts;
+        for (int e = e0 + lane; e < e1; e += LANES) mine[e - e0] = bad ? NAN : 0.f;
+        __syncthreads();
+        if (here && at >= e0 && at < e1 && !bad) mine[at - e0] = part;
+        __syncthreads();
+        if (there) {
+            for (int e = e0 + lane; e < e1; e += LANES) {
+                float v = mine[e - e0];
+                if (whole) v = expf((float)s[e] - low) / total * (v - mean);
+                out[e] = (T)v;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// --------------------------------------------------------------- dispatch
+// A stable counting sort of the slots by expert.  Workgroup b takes the slots of
+// chunk b, its four waves a quarter each, in order.  count: the chunk's slots per
+// expert.  place: every workgroup adds up the counts of the chunks before it
+// and of all of them (read from the caches), so that no launch lies between; the
+// rank of a slot among its wave's 64 comes from the lanes that hold the same
+// expert.  Whole numbers only: the order does not depend on timing.
+constexpr int kChunk = 4096, kSortThreads = 256, kSortWaves = kSortThreads / 64;
+
+__device__ inline int expert_at(const DispatchArgs &a, int64_t s, int64_t end) {
+    const int e = s < end ? a.index[s] : -1;
+    return e >= 0 && e < a.experts ? e : -1;
+}
+
+__global__ __launch_bounds__(kSortThreads) void dispatch_count_kernel(DispatchArgs a) {
+    extern __shared__ int hist[];
+    for (int e = threadIdx.x; e < a.experts; e += kSortThreads) hist[e] = 0;
+    __syncthreads();
+    const int64_t s0 = (int64_t)blockIdx.x * kChunk;
+    const int64_t end = s0 + kChunk < a.slots ? s0 + kChunk : a.slots;
+    for (int64_t s = s0 + threadIdx.x; s < end; s += kSortThreads) {
+        const int e = expert_at(a, s, end);
+        if (e >= 0) atomicAdd(&hist[e], 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.experts; e += kSortThreads)
+        a.counts[(int64_t)blockIdx.x * a.experts + e] = hist[e];
+}
+
+// WAVES: waves that rank (4, or 1 where four histograms do not fit in LDS).
+template <int WAVES>
+__global__ __launch_bounds__(kSortThreads) void dispatch_place_kernel(DispatchArgs a) {
+    extern __shared__ int base[];   // WAVES x experts
+    __shared__ int sums[kSortWaves + 1];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int64_t s0 = (int64_t)blockIdx.x * kChunk;
+    const int64_t end = s0 + kChunk < a.slots ? s0 + kChunk : a.slots;
+    constexpr int kPart = kChunk / WAVES;
+    for (int e = t; e < WAVES * a.experts; e += kSortThreads) base[e] = 0;
+    __syncthreads();
+    if (WAVES > 1 || a.blocks == 1) {
+        for (int64_t s = s0 + t; s < end; s += kSortThreads) {
+            const int e = expert_at(a, s, end);
+            if (e >= 0) atomicAdd(&base[(int)((s - s0) / kPart) * a.experts + e], 1);
+        }
+        __syncthreads();
+    }
+    // expert by expert, 256 at a time: the chunk's first row, then the waves'
+    int before = 0;   // rows of the experts below these 256
+    for (int e0 = 0; e0 < a.experts; e0 += kSortThreads) {
+        const int e = e0 + t;
+        int all = 0, prior = 0;
+        if (e < a.experts) {
+            if (a.blocks == 1) {
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) all += base[w * a.experts + e];
+            } else {
+                for (int b = 0; b < a.blocks; ++b) {
+                    const int c = a.counts[(int64_t)b * a.experts + e];
+                    all += c;
+                    prior += b < (int)blockIdx.x ? c : 0;
+                }
+            }
+        }
+        int sum = all;   // inclusive over the lanes
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(sum, o);
+            if (lane >= o) sum += v;
+        }
+        if (lane == 63) sums[wave] = sum;
+        __syncthreads();
+        int first = before + sum - all;
+        for (int w = 0; w < wave; ++w) first += sums[w];
+        int next = before;
+        for (int w = 0; w < kSortWaves; ++w) next += sums[w];
+        if (e < a.experts) {
+            if (blockIdx.x == 0) a.offsets[e] = first;
+            int at = first + prior;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                const int c = base[w * a.experts + e];
+                base[w * a.experts + e] = at;
+                at += c;
+            }
+        }
+        before = next;
+        __syncthreads();
+    }
+    if (blockIdx.x == 0 && t == 0) a.offsets[a.experts] = before;
+    for (int64_t p = before + (int64_t)blockIdx.x * kSortThreads + t; p < a.slots;
+         p += (int64_t)gridDim.x * kSortThreads)
+        a.order[p] = -1;
+    if (wave >= WAVES) return;
+    int *mine = base + wave * a.experts;
+    const int64_t w0 = s0 + (int64_t)wave * kPart;
+    for (int64_t g0 = w0; g0 < w0 + kPart && g0 < end; g0 += 64) {
+        const int64_t s = g0 + lane;
+        const int e = expert_at(a, s, end);
+        // the lanes that hold the same expert
+        unsigned long long same = __ballot(e >= 0);
+        for (int b = 1; b < a.experts; b <<= 1) {
+            const unsigned long long ones = __ballot(e & b);
+            same &= e & b ? ones : ~ones;
+        }
+        if (e >= 0) {
+            const int rank = __popcll(same & ((1ull << lane) - 1));
+            const int p = mine[e] + rank;
+            a.order[p] = (int)s;
+            a.place[s] = p;
+        } else if (s < end) {
+            a.place[s] = -1;
+        }
+        // the wave's reads of the rows counted so far come before the leaders' writes
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (e >= 0 && __ffsll((long long)same) - 1 == lane) mine[e] += __popcll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
+// Lets a kernel have `bytes` of dynamic LDS where, with its own, they pass 64 KB.
+template <typename K>
+hipError_t room_for(K kernel, size_t bytes) {
+    if (bytes <= 60 * 1024) return hipSuccess;
+    return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+template <typename T>
+hipError_t launch_route_type(const RouteArgs &a, hipStream_t stream) {
+    const bool wide = a.k > 16 || a.groups > 16;
+    const auto blocks = [&](int rows) { return (unsigned)((a.n + rows - 1) / rows); };
+    const int vec = a.lds % (16 / (int)sizeof(T)) == 0 &&
+                    reinterpret_cast<uintptr_t>(a.scores) % 16 == 0;
+    const auto lds = [&](int rows) {
+        return a.groups > 1 ? (size_t)rows * (a.experts + 1) * sizeof(float) : 0;
+    };
+    if (a.experts <= 64 && !wide)
+        route_kernel<T, 16, 4><<<blocks(16), kRouteThreads, lds(16), stream>>>(a, vec);
+    else if (a.experts <= 256 && !wide)
+        route_kernel<T, 16, 16><<<blocks(16), kRouteThreads, lds(16), stream>>>(a, vec);
+    else if (a.experts <= 512)
+        route_kernel<T, 64, 8><<<blocks(4), kRouteThreads, lds(4), stream>>>(a, vec);
+    else if (a.experts <= 2048)
+        route_kernel<T, 64, 32><<<blocks(4), kRouteThreads, lds(4), stream>>>(a, vec);
+    else {
+        const hipError_t e = room_for(route_long_kernel<T>, a.experts * sizeof(float));
+        if (e != hipSuccess) return e;
+        route_long_kernel<T><<<(unsigned)a.n, kRouteThreads, a.experts * sizeof(float), stream>>>(a);
+    }
+    return hipGetLastError();
+}
+
+template <typename T, typename G>
+hipError_t launch_backward_types(const RouteArgs &a, hipStream_t stream) {
+    const auto blocks = [&](int rows) { return (unsigned)((a.n + rows - 1) / rows); };
+    if (a.experts <= 512 && a.k <= 16)
+        route_backward_kernel<T, G, 16><<<blocks(16), kRouteThreads,
+                                          16 * a.experts * sizeof(float), stream>>>(a, a.experts);
+    else {
+        const int width = a.experts < 2048 ? a.experts : 2048;
+        route_backward_kernel<T, G, 64><<<blocks(4), kRouteThreads, 4 * width * sizeof(float),
+                                          stream>>>(a, width);
+    }
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_backward_type(const RouteArgs &a, hipStream_t stream) {
+    switch (a.dweight_type) {
+        case kF32: return launch_backward_types<T, float>(a, stream);
+        case kBF16: return launch_backward_types<T, __bf16>(a, stream);
+        default: return launch_backward_types<T, _Float16>(a, stream);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_route(const RouteArgs &a, hipStream_t stream) {
+    if (a.n == 0) return hipSuccess;
+    switch (a.type) {
+        case kF32: return launch_route_type<float>(a, stream);
+        case kBF16: return launch_route_type<__bf16>(a, stream);
+        default: return launch_route_type<_Float16>(a, stream);
+    }
+}
+
+hipError_t launch_route_backward(const RouteArgs &a, hipStream_t stream) {
+    if (a.n == 0) return hipSuccess;
+    switch (a.type) {
+        case kF32: return launch_backward_type<float>(a, stream);
+        case kBF16: return launch_backward_type<__bf16>(a, stream);
+        default: return launch_backward_type<_Float16>(a, stream);
+    }
+}
+
+int32_t dispatch_blocks(int64_t slots) {
+    return slots <= kChunk ? 1 : (int32_t)((slots + kChunk - 1) / kChunk);
+}
+
+hipError_t launch_dispatch(const DispatchArgs &a, hipStream_t stream) {
+    const size_t one = a.experts * sizeof(int);
+    if (a.blocks > 1) {
+        const hipError_t e = room_for(dispatch_count_kernel, one);
+        if (e != hipSuccess) return e;
+        dispatch_count_kernel<<<a.blocks, kSortThreads, one, stream>>>(a);
+    }
+    if (a.experts <= 2048) {
+        dispatch_place_kernel<4><<<a.blocks, kSortThreads, 4 * one, stream>>>(a);
+    } else {
+        const hipError_t e = room_for(dispatch_place_kernel<1>, one);
+        if (e != hipSuccess) return e;
+        dispatch_place_kernel<1><<<a.blocks, kSortThreads, one, stream>>>(a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace som

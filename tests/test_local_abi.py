@@ -1,0 +1,137 @@
+"""The local models' C entries: exported, and refusing bad arguments on the host
+before any device work (no GPU needed)."""
+import ctypes as C
+import os
+import re
+
+import pytest
+
+import paper_1905_09598_amd as som
+from paper_1905_09598_amd import local
+
+HEADER = os.path.join(os.path.dirname(os.path.dirname(__file__)), "include", "som_local.h")
+
+
+def status(code):
+    return som.STATUS[code]
+
+
+def test_library_exports_every_declared_symbol():
+    text = open(HEADER).read()
+    names = set(re.findall(r"^\s*(?:som_status|int64_t)\s+(som_\w+)\s*\(", text, flags=re.M))
+    assert names == set(local.EXPORTED)
+    for name in names:
+        assert hasattr(local.lib(), name), name
+
+
+@pytest.mark.parametrize("struct,binding", [("som_linear_call", local._LinearCall),
+                                            ("som_route_call", local._RouteCall),
+                                            ("som_adamw_tensor", local._AdamwTensor)])
+def test_structures_have_the_header_s_fields_in_order(struct, binding):
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    body = re.search(r"typedef struct %s \{(.*?)\}" % struct, text, flags=re.S).group(1)
+    fields = []
+    for line in body.split(";"):
+        line = line.strip()
+        if line:
+            kind = re.match(r"(?:const\s+)?(\w+)", line).group(1)
+            for part in re.sub(r"^(?:const\s+)?\w+", "", line, count=1).split(","):
+                fields.append((part.strip().lstrip("*").strip(),
+                               "pointer" if "*" in part else kind))
+    size = {"int32_t": 4, "int64_t": 8, "uint64_t": 8, "float": 4, "pointer": 8}
+    assert [f[0] for f in binding._fields_] == [f[0] for f in fields]
+    assert [C.sizeof(f[1]) for f in binding._fields_] == [size[f[1]] for f in fields]
+
+
+def _linear(**change):
+    values = dict(type=0, n=4, inner=8, outer=8, ldx=8, lddy=8)
+    values.update(change)
+    return local._LinearCall(**values)
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(type=3), "SOM_E_ARG"), (dict(activation=-1), "SOM_E_ARG"),
+    (dict(activation=4), "SOM_E_ARG"), (dict(n=-1), "SOM_E_ARG"), (dict(inner=0), "SOM_E_ARG"),
+    (dict(outer=-2), "SOM_E_ARG"), (dict(ldx=7), "SOM_E_ARG"), (dict(experts=-1), "SOM_E_ARG"),
+    (dict(experts=2, k=0), "SOM_E_ARG"), (dict(k=2), "SOM_E_ARG"), (dict(gather=1), "SOM_E_ARG"),
+    (dict(experts=4, k=2, n=1 << 31), "SOM_E_UNSUPPORTED"),
+    (dict(experts=1 << 20, k=1, outer=1 << 20), "SOM_E_UNSUPPORTED"), ({}, "SOM_E_ARG")])
+def test_linear_refuses(change, want):
+    L = local.lib()
+    call = _linear(**change)          # without arrays: even good sizes are refused
+    assert status(L.som_linear(C.byref(call))) == want
+    assert status(L.som_linear_backward(C.byref(call))) == want
+    need = C.c_uint64()
+    assert status(L.som_linear_workspace(C.byref(call), 0, C.byref(need))) == (
+        want if change else "SOM_OK")
+
+
+def test_null_calls():
+    L = local.lib()
+    need = C.c_uint64()
+    assert L.som_linear(None) == 1 and L.som_linear_backward(None) == 1
+    assert L.som_linear_workspace(None, 0, C.byref(need)) == 1
+    assert L.som_linear_workspace(C.byref(_linear()), 0, None) == 1
+    assert L.som_route(None) == 1 and L.som_route_backward(None) == 1
+    assert L.som_dispatch(None, 4, 2, 8, None, None, None, None, 0, None) == 1
+    assert L.som_dispatch_workspace(4, 2, 8, None) == 1
+    assert L.som_combine(0, 4, 2, 8, None, None, None, None, 0, None, None) == 1
+    assert L.som_combine_backward(0, 4, 2, 8, None, 8, None, None, None, None, None, None) == 1
+    assert L.som_adamw_destroy(None) == 0
+    assert L.som_adamw_step(None, None, None, 1, 0.1, 0.9, 0.9, 1e-8, 0.0, None) == 1
+    assert L.som_adamw_create(None, 1, 32, None, None, None, None, None, None) == 1
+
+
+@pytest.mark.parametrize("change", [
+    dict(type=5), dict(gate=2), dict(n=-1), dict(experts=0), dict(experts=16385, lds=16385),
+    dict(k=0), dict(k=9), dict(groups=3), dict(groups=0), dict(top_groups=2), dict(group_best=0),
+    dict(group_best=3), dict(scale=float("inf")), dict(lds=7), {}])
+def test_route_refuses(change):
+    values = dict(n=3, experts=8, k=2, groups=1, top_groups=1, group_best=1, scale=1.0, lds=8)
+    values.update(change)
+    call = local._RouteCall(**values)
+    assert status(local.lib().som_route(C.byref(call))) == "SOM_E_ARG"
+    assert status(local.lib().som_route_backward(C.byref(call))) == "SOM_E_ARG"
+
+
+def test_slots_beyond_32_bits():
+    L, need = local.lib(), C.c_uint64()
+    assert status(L.som_dispatch_workspace(1 << 30, 4, 8, C.byref(need))) == "SOM_E_UNSUPPORTED"
+    assert status(L.som_dispatch_workspace(1 << 20, 4, 0, C.byref(need))) == "SOM_E_ARG"
+    call = local._RouteCall(n=1 << 31, experts=8, k=2, groups=1, top_groups=1, group_best=1,
+                            scale=1.0, lds=8)
+    assert status(L.som_route(C.byref(call))) == "SOM_E_UNSUPPORTED"
+    assert L.som_combine(0, 1 << 31, 2, 8, None, None, None, None, 0, None, None) == 6
+
+
+def test_workspace_grows_with_what_a_call_needs():
+    L, need = local.lib(), C.c_uint64()
+
+    def bytes_of(backward=0, **change):
+        call = _linear(**change)
+        assert L.som_linear_workspace(C.byref(call), backward, C.byref(need)) == 0
+        return need.value
+
+    whole = dict(n=4096, inner=512, outer=4096, ldx=512, type=1)
+    assert bytes_of(**whole) == 0                      # aligned, enough tiles
+    odd = bytes_of(**dict(whole, inner=511, ldx=511))
+    assert odd >= (4096 + 4096) * 512 * 2              # both operands in whole pieces
+    assert bytes_of(n=0) == 0
+
+
+def test_adamw_room_and_refusals():
+    L = local.lib()
+    table = (local._AdamwTensor * 3)(local._AdamwTensor(None, 1, 0),
+                                     local._AdamwTensor(None, 256, 0),
+                                     local._AdamwTensor(None, 257, 0))
+    assert L.som_adamw_room(table, 3) == 256 + 256 + 512
+    assert L.som_adamw_room(None, 3) == -1
+    out = C.c_void_p()
+    for bits in (16, 0):
+        assert L.som_adamw_create(table, 3, bits, 1, 1, None, None, None, C.byref(out)) == 1
+    assert L.som_adamw_create(table, 3, 8, 1, 1, None, None, None, C.byref(out)) == 1
+    assert L.som_adamw_create(table, 0, 32, 1, 1, None, None, None, C.byref(out)) == 1
+    assert L.som_adamw_create(table, 3, 32, None, None, None, None, None, C.byref(out)) == 1
+    assert not out.value
+    table[1].count = -1
+    assert L.som_adamw_room(table, 3) == -1
