@@ -97,8 +97,8 @@ som_status som_linear_workspace(const som_linear_call *call, int32_t backward, u
 
 /* Errors of both: SOM_E_ARG (a bad type, activation or size, a missing or too
  * short array, inner != outer strides out of range, a workspace that is missing,
- * misaligned or too small), SOM_E_UNSUPPORTED (more than 2^31 - 1 slots, tiles
- * or experts x outer rows), SOM_E_DEVICE. */
+ * misaligned or too small), SOM_E_UNSUPPORTED (inner or outer above 4,000,000,
+ * more than 2^31 - 1 slots, tiles or experts x outer rows), SOM_E_DEVICE. */
 som_status som_linear(const som_linear_call *call);
 som_status som_linear_backward(const som_linear_call *call);
 

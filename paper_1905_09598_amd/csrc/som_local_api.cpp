@@ -33,7 +33,7 @@ ProductPlan plan_product(const ProductArgs &a, int num_cus) {
     }
     // microseconds of a slab on all the workgroups that a compute unit holds
     struct Shape { int32_t tile, held; double half, single; };
-    static const Shape shapes[] = {{256, 1, 1.2, 7.5}, {128, 2, 0.75, 3.8}, {64, 4, 0.5, 2.0}};
+    static const Shape shapes[] = {{256, 1, 1.6, 7.5}, {128, 2, 1.0, 3.8}, {64, 4, 0.7, 2.0}};
     double least = INFINITY;
     for (const Shape &s : shapes) {
         const int64_t tn = (a.n + s.tile - 1) / s.tile;
@@ -50,7 +50,7 @@ ProductPlan plan_product(const ProductArgs &a, int num_cus) {
         const int64_t rows = a.mode == kWeight ? a.m * experts : a.m;
         for (int32_t parts = 1; parts <= 32 && parts <= slabs; parts *= 2) {
             const int64_t floats =
-                parts > 1 ? parts * rows * (tn * s.tile + 1) : 0;
+                parts > 1 ? parts * rows * (tn * s.tile) : 0;
             if (floats > (int64_t)1 << 30) break;
             const double rounds =
                 std::ceil((double)(tm * tn * parts) / ((double)num_cus * s.held));
@@ -133,29 +133,38 @@ struct Operand {
 int64_t rounded(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 // One side of a product: the caller's rows where they lie in whole 16-byte
-// pieces, else (or where a slope has to be applied) a copy whose rows do.
+// pieces within a tile's reach, else (or where a slope has to be applied) a copy
+// whose rows do.  *list: the side's rows are named by it; a matrix that is too long
+// to be reached by it is copied row by row of the list, and *list becomes null.
 struct SideCopy {
     som::RowsArgs rows{};
     bool needed = false;
 };
 Operand whole_rows(Carver &work, SideCopy &copy, int32_t type, const void *p, int64_t rows,
-                   int64_t cols, int64_t ld, const void *z = nullptr, int32_t activation = 0) {
-    const int size = som::type_size(type), per = 16 / size;
-    const bool whole = reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % per == 0 && cols % per == 0;
-    if (whole && !z) return {p, ld};
-    const int64_t ldd = rounded(cols, per);
-    void *to = work.take((uint64_t)rows * ldd * size);
+                   int64_t cols, int64_t ld, const void *z = nullptr, int32_t activation = 0,
+                   const int32_t **list = nullptr, int32_t per = 1, int64_t listed = 0) {
+    const int size = som::type_size(type), elems = 16 / size;
+    const bool whole = reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % elems == 0 &&
+                       cols % elems == 0 && som::tile_reaches(ld, size);
+    const int64_t ldd = rounded(cols, elems);
+    const bool far = list && *list && rows * (whole ? ld : ldd) * size >= (int64_t)1 << 32;
+    if (whole && !z && !far) return {p, ld};
+    const int64_t high = far ? listed : rows;
+    void *to = work.take((uint64_t)high * ldd * size);
     copy.needed = true;
     copy.rows.type = type;
     copy.rows.activation = activation;
     copy.rows.src = p;
     copy.rows.z = z;
     copy.rows.dst = to;
-    copy.rows.rows = rows;
+    copy.rows.rows = high;
     copy.rows.cols = cols;
     copy.rows.lds = ld;
     copy.rows.ldz = cols;
     copy.rows.ldd = ldd;
+    copy.rows.list = far ? *list : nullptr;
+    copy.rows.per = per;
+    if (far) *list = nullptr;
     return {to, ldd};
 }
 
@@ -215,7 +224,8 @@ struct LinearForward {
                                    reinterpret_cast<uintptr_t>(c.w) % 16 == 0 &&
                                    c.ldx % per == 0 && c.inner % per == 0;
         } else {
-            A = whole_rows(work, x, c.type, c.x, xrows, c.inner, c.ldx);
+            A = whole_rows(work, x, c.type, c.x, xrows, c.inner, c.ldx, nullptr, 0, &a.list, c.k,
+                           rows);
             B = whole_rows(work, w, c.type, c.w, wrows, c.inner, c.inner);
         }
         a.a = A.p, a.lda = A.ld;
@@ -226,6 +236,7 @@ struct LinearForward {
 struct LinearBackward {
     SideCopy x, w, dz;
     Product input, weight;
+    som::SumsArgs sums{};
     bool has_input, has_weight;
     LinearBackward(const som_linear_call &c, Carver &work) {
         const int size = som::type_size(c.type);
@@ -233,7 +244,7 @@ struct LinearBackward {
         const int64_t xrows = c.gather ? c.n : rows;
         const int64_t wrows = (int64_t)c.outer * std::max(1, c.experts);
         has_input = c.dx != nullptr;
-        has_weight = c.dw != nullptr || c.dbias != nullptr;
+        has_weight = c.dw != nullptr;
         const Operand Z = whole_rows(work, dz, c.type, c.dy, rows, c.outer, c.lddy,
                                      c.activation != SOM_ACT_NONE ? c.z : nullptr, c.activation);
         if (has_input) {
@@ -253,7 +264,6 @@ struct LinearBackward {
             input.place(work);
         }
         if (has_weight) {
-            const Operand X = whole_rows(work, x, c.type, c.x, xrows, c.inner, c.ldx);
             ProductArgs &a = weight.a;
             a.mode = som::kWeight;
             a.type = c.type;
@@ -261,11 +271,22 @@ struct LinearBackward {
             a.offsets = c.experts ? c.offsets : nullptr;
             a.experts = c.experts, a.per = c.k;
             a.list = c.experts && c.gather ? c.order : nullptr;
+            const Operand X = whole_rows(work, x, c.type, c.x, xrows, c.inner, c.ldx, nullptr, 0,
+                                         &a.list, c.k, rows);
             a.a = Z.p, a.lda = Z.ld;
             a.b = X.p, a.ldb = X.ld;
-            a.y = c.dw, a.bias_grad = c.dbias;
+            a.y = c.dw;
             a.vec = four(c.dw, c.inner, size) ? som::kVecOut : 0;
             weight.place(work);
+        }
+        if (c.dbias) {
+            sums.type = c.type;
+            sums.src = Z.p;
+            sums.rows = rows, sums.cols = c.outer, sums.ld = Z.ld;
+            sums.offsets = c.experts ? c.offsets : nullptr;
+            sums.experts = c.experts;
+            sums.out = c.dbias;
+            sums.partial = work.take<float>((uint64_t)som::sums_partial(sums) * 4);
         }
     }
 };
@@ -278,6 +299,7 @@ som_status linear_sizes_ok(const som_linear_call *c) {
         return SOM_E_ARG;
     if (c->experts ? c->k <= 0 : (c->k != 0 || c->gather)) return SOM_E_ARG;
     if (c->ldx < c->inner) return SOM_E_ARG;
+    if (c->inner > som::kMaxWidth || c->outer > som::kMaxWidth) return SOM_E_UNSUPPORTED;
     const __int128 rows = (__int128)c->n * (c->experts ? c->k : 1);
     if (c->experts && rows > INT32_MAX) return SOM_E_UNSUPPORTED;
     if (rows > (__int128)1 << 40) return SOM_E_UNSUPPORTED;
@@ -357,7 +379,6 @@ som_status som_linear_backward(const som_linear_call *c) {
     const int size = som::type_size(c->type);
     const int64_t rows = c->experts ? c->n * c->k : c->n;
     const int64_t wrows = (int64_t)c->outer * std::max(1, c->experts);
-    if (!c->dw && c->dbias) return SOM_E_ARG;   // the bias's sums come with dw's product
     if (!linear_common_ok(*c) || !rows_ok(c->dy, rows, c->outer, c->lddy, size) ||
         (c->activation != SOM_ACT_NONE && !rows_ok(c->z, rows, c->outer, c->outer, size)) ||
         !rows_ok_or_null(c->dx, rows, c->inner, c->inner, size) ||
@@ -388,6 +409,7 @@ som_status som_linear_backward(const som_linear_call *c) {
         e = run_copy(b.x, s);
         if (e == hipSuccess) e = launch_product(b.weight.a, b.weight.plan, s);
     }
+    if (e == hipSuccess && c->dbias) e = som::launch_sums(b.sums, s);
     return from_hip(e);
 }
 

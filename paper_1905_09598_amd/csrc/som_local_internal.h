@@ -13,11 +13,42 @@ enum : int32_t { kForward = 0, kInput = 1, kWeight = 2 };               // which
 
 inline int type_size(int32_t type) { return type == kF32 ? 4 : 2; }
 
+// The activations and their slopes, on the hardware's exponential and reciprocal
+// (each within one unit in the last place): an exact division or the library's
+// error function would take longer than the products they follow (gelu of
+// 8192 x 8192 sums: 110 us of 440).  The normal distribution's tail
+//     q = 1 - Phi(|z|) = (a1 t + ... + a5 t^5) e^(-z^2 / 2) / 2,
+//     t = 1 / (1 + p |z| / sqrt 2)
+// is Abramowitz and Stegun, formula 7.1.26, off by at most 7.5e-8; its exponential
+// is the slope's too, and for negative z the tail itself is the value, so nothing
+// cancels.
+__device__ inline float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+
+__device__ inline void normal(float z, float *below, float *bell) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
+    const float e = exp_fast(-0.5f * z * z);
+    float s = fmaf(t, 1.061405429f, -1.453152027f);
+    s = fmaf(t, s, 1.421413741f);
+    s = fmaf(t, s, -0.284496736f);
+    s = fmaf(t, s, 0.254829592f);
+    const float tail = 0.5f * t * s * e;
+    *below = z > 0.f ? 1.f - tail : tail;
+    *bell = e;
+}
+
+__device__ inline float sigmoid_fast(float z) {
+    return __builtin_amdgcn_rcpf(1.f + exp_fast(-z));
+}
+
 __device__ inline float activate(float z, int32_t kind) {
     switch (kind) {
         case kActRelu: return z > 0.f ? z : (z != z ? z : 0.f);
-        case kActGelu: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-        case kActSilu: return z / (1.f + expf(-z));
+        case kActGelu: {
+            float below, bell;
+            normal(z, &below, &bell);
+            return z * below;
+        }
+        case kActSilu: return z * sigmoid_fast(z);
         default: return z;
     }
 }
@@ -25,24 +56,50 @@ __device__ inline float activate(float z, int32_t kind) {
 __device__ inline float activation_slope(float z, int32_t kind) {
     switch (kind) {
         case kActRelu: return z > 0.f ? 1.f : 0.f;
-        case kActGelu:
-            return 0.5f * (1.f + erff(z * 0.70710678118654752f)) +
-                   z * expf(-0.5f * z * z) * 0.39894228040143268f;
+        case kActGelu: {
+            float below, bell;
+            normal(z, &below, &bell);
+            return fmaf(z * bell, 0.39894228040143268f, below);
+        }
         case kActSilu: {
-            const float q = 1.f / (1.f + expf(-z));
-            return q * (1.f + z * (1.f - q));
+            const float q = sigmoid_fast(z);
+            return fmaf(z * q, 1.f - q, q);
         }
         default: return 1.f;
     }
 }
 
+// Largest e in [0, experts) whose first tile offsets[e] / tile + e is at most
+// t, or with tile = 0 whose first row is at most t: 64 places tested at a time.
+// (An expert of c rows from row o on has the tiles from o / tile + e on; the next
+// one's begin at least ceil(c / tile) later, and the last ones may be empty.)
+__device__ inline int expert_of(const int32_t *offsets, int experts, int tile, int64_t t) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, span = experts;
+    while (span > 1) {
+        const int width = (span + 63) / 64;
+        const int e = lo + lane * width;
+        const bool at_most = lane * width < span &&
+                             (tile ? (int64_t)(offsets[e] / tile) + e : (int64_t)offsets[e]) <= t;
+        const int last = 63 - __clzll(__ballot(at_most) | 1);
+        lo += last * width;
+        span = span - last * width < width ? span - last * width : width;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
 // Which of a product's arrays can be reached four elements at a time.
 enum : int32_t { kVecOut = 1, kVecBias = 2, kVecResidual = 4, kVecSlope = 8 };
+
+// The tiles' kernels reach an operand's elements by 32-bit offsets within a tile's
+// rows, and within a whole listed matrix (som_product.h).
+constexpr int64_t kMaxWidth = 4000000;
+inline bool tile_reaches(int64_t ld, int size) { return ld * size * 256 < ((int64_t)1 << 32); }
 
 // C = A B^T, C of m rows and n columns, contraction k (som_product.h).
 //   forward  A = x (m x k), B = w (n x k):      y = act(C + bias) + residual
 //   input    A = dz (m x k), B = w (k x n):     dx = C [* slope of z]
-//   weight   A = dz (k x m), B = x (k x n):     dw = C, bias_grad = sums of dz
+//   weight   A = dz (k x m), B = x (k x n):     dw = C
 // Routed (offsets): forward and input take the m rows by expert, offsets[e] ..
 // of B + e batch_b; weight sums offsets[e] .. into dw + e m n.  list: forward,
 // row r of A is A's row list[r] / per; weight, row s of B is B's row
@@ -54,11 +111,11 @@ struct ProductArgs {
     int64_t m, n, k;
     const void *bias, *residual, *slope;
     int64_t ldr;
-    void *y, *z, *bias_grad;
+    void *y, *z;
     const int32_t *offsets, *list;
     int32_t experts, per;
     int32_t splits;       // parts of the contraction
-    float *partial;       // splits x partial_rows x whole tiles, then splits x partial_rows
+    float *partial;       // splits x partial_rows x whole tiles
     int64_t partial_rows;
 };
 
@@ -72,14 +129,31 @@ struct ProductPlan {
 };
 
 // Copies `rows` rows of `cols` elements, `lds` apart, to rows of ldd >= cols
-// elements filled up with zeros; with z (rows ldz apart), times act'(z).
+// elements filled up with zeros; with z (rows ldz apart), times act'(z); with a
+// list, row r is src's row list[r] / per, or zeros where list[r] is negative.
 struct RowsArgs {
     int32_t type, activation;
     const void *src, *z;
     void *dst;
     int64_t rows, cols, lds, ldz, ldd;
+    const int32_t *list;
+    int32_t per;
 };
 hipError_t launch_rows_copy(const RowsArgs &a, hipStream_t stream);
+
+// out[e] = sums of the rows of src (cols elements, ld apart) of expert e, or of all
+// rows without offsets.
+struct SumsArgs {
+    int32_t type;
+    const void *src;
+    int64_t rows, cols, ld;
+    const int32_t *offsets;
+    int32_t experts;
+    void *out;
+    float *partial;         // sums_partial() floats
+};
+int64_t sums_partial(const SumsArgs &a);
+hipError_t launch_sums(const SumsArgs &a, hipStream_t stream);
 
 struct CombineArgs {
     int32_t type, k;

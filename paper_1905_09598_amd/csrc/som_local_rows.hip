@@ -48,8 +48,9 @@ __global__ __launch_bounds__(kThreads) void rows_copy_kernel(RowsArgs a, int vec
     const int64_t row = q / pieces, col = q % pieces * N;
     if (row >= a.rows) return;
     float v[N], z[N];
-    read_some<T, N>(static_cast<const T *>(a.src) + row * a.lds + col, a.cols - col, vec & kVecSrc,
-                    v);
+    const int64_t from = a.list ? a.list[row] : row;
+    read_some<T, N>(static_cast<const T *>(a.src) + (a.list ? from / a.per : from) * a.lds + col,
+                    from < 0 ? 0 : a.cols - col, vec & kVecSrc, v);
     if (a.z) {
         read_some<T, N>(static_cast<const T *>(a.z) + row * a.ldz + col, a.cols - col, vec & kVecZ,
                         z);
@@ -57,6 +58,74 @@ __global__ __launch_bounds__(kThreads) void rows_copy_kernel(RowsArgs a, int vec
         for (int e = 0; e < N; ++e) v[e] = col + e < a.cols ? v[e] * activation_slope(z[e], a.activation) : 0.f;
     }
     write_some<T, N>(static_cast<T *>(a.dst) + row * a.ldd + col, N, true, v);
+}
+
+// Sums of rows, in fp32 and in a fixed order: a workgroup takes 32 pieces of 16
+// bytes of up to kSumRows rows of one expert (all of them if DIRECT), 32 rows at
+// a time, joins its 32 sums a column through LDS, and writes them, or parts that
+// join_sums_kernel adds up.
+constexpr int kSumThreads = 1024, kSumPieces = 32, kSumLanes = kSumThreads / kSumPieces;
+constexpr int kSumRows = 512;
+
+template <typename T, bool DIRECT>
+__global__ __launch_bounds__(kSumThreads) void sums_kernel(SumsArgs a, int vec) {
+    constexpr int N = 16 / sizeof(T);
+    __shared__ float part[kSumLanes][kSumPieces * N + 4];
+    const int piece = threadIdx.x % kSumPieces, lane = threadIdx.x / kSumPieces;
+    int64_t first = (int64_t)blockIdx.y * kSumRows, end = a.rows;
+    int e = 0;
+    if (DIRECT) {
+        e = blockIdx.y;
+        first = a.offsets ? a.offsets[e] : 0;
+        if (a.offsets) end = a.offsets[e + 1];
+    } else {
+        if (a.offsets) {
+            e = expert_of(a.offsets, a.experts, kSumRows, blockIdx.y);
+            first = a.offsets[e] + ((int64_t)blockIdx.y - (a.offsets[e] / kSumRows + e)) * kSumRows;
+            end = a.offsets[e + 1];
+        }
+        end = first + kSumRows < end ? first + kSumRows : end;
+        if (first >= end) return;
+    }
+    const int64_t col = ((int64_t)blockIdx.x * kSumPieces + piece) * N, left = a.cols - col;
+    float sum[N];
+#pragma unroll
+    for (int c = 0; c < N; ++c) sum[c] = 0.f;
+    if (left > 0) {
+#pragma unroll 4
+        for (int64_t r = first + lane; r < end; r += kSumLanes) {
+            float v[N];
+            read_some<T, N>(static_cast<const T *>(a.src) + r * a.ld + col, left, vec, v);
+#pragma unroll
+            for (int c = 0; c < N; ++c) sum[c] += v[c];
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < N; ++c) part[lane][piece * N + c] = sum[c];
+    __syncthreads();
+    const int c = threadIdx.x;
+    const int64_t at = (int64_t)blockIdx.x * kSumPieces * N + c;
+    if (c < kSumPieces * N && at < a.cols) {
+        float v = 0.f;
+        for (int l = 0; l < kSumLanes; ++l) v += part[l][c];
+        if (DIRECT) static_cast<T *>(a.out)[e * a.cols + at] = (T)v;
+        else a.partial[blockIdx.y * a.cols + at] = v;
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void join_sums_kernel(SumsArgs a) {
+    const int64_t col = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int e = blockIdx.y;
+    if (col >= a.cols) return;
+    int64_t first = 0, count = (a.rows + kSumRows - 1) / kSumRows;
+    if (a.offsets) {
+        first = a.offsets[e] / kSumRows + e;
+        count = (a.offsets[e + 1] - a.offsets[e] + kSumRows - 1) / kSumRows;
+    }
+    float v = 0.f;
+    for (int64_t p = 0; p < count; ++p) v += a.partial[(first + p) * a.cols + col];
+    static_cast<T *>(a.out)[e * a.cols + col] = (T)v;
 }
 
 // 16 bytes of a document's row a thread.
@@ -153,6 +222,38 @@ hipError_t launch_rows_copy(const RowsArgs &a, hipStream_t stream) {
     const unsigned blocks = (unsigned)((pieces + kThreads - 1) / kThreads);
     return by_type(a.type, [&](auto t) {
         rows_copy_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a, vec);
+    });
+}
+
+// One pass where an expert has few rows: the sums of 32 rows at a time then take
+// no longer than the second launch.
+static bool sums_direct(const SumsArgs &a) {
+    return a.rows <= (int64_t)(a.offsets ? a.experts : 1) * 1024;
+}
+static int64_t sums_parts(const SumsArgs &a) {
+    return a.offsets ? a.rows / kSumRows + a.experts : (a.rows + kSumRows - 1) / kSumRows;
+}
+
+int64_t sums_partial(const SumsArgs &a) { return sums_direct(a) ? 0 : sums_parts(a) * a.cols; }
+
+hipError_t launch_sums(const SumsArgs &a, hipStream_t stream) {
+    const int size = type_size(a.type);
+    const int experts = a.offsets ? a.experts : 1;
+    const bool direct = sums_direct(a);
+    const int64_t high = direct ? experts : sums_parts(a);
+    const int64_t wide = (a.cols * size + 16 * kSumPieces - 1) / (16 * kSumPieces);
+    if (high > 65535 || experts > 65535) return hipErrorInvalidValue;
+    const int vec = whole_pieces(a.src, a.ld, size);
+    const dim3 grid((unsigned)wide, (unsigned)high);
+    const dim3 join((unsigned)((a.cols + kThreads - 1) / kThreads), experts);
+    return by_type(a.type, [&](auto t) {
+        using T = decltype(t);
+        if (direct) {
+            sums_kernel<T, true><<<grid, kSumThreads, 0, stream>>>(a, vec);
+        } else {
+            sums_kernel<T, false><<<grid, kSumThreads, 0, stream>>>(a, vec);
+            join_sums_kernel<T><<<join, kThreads, 0, stream>>>(a);
+        }
     });
 }
 

@@ -29,6 +29,7 @@
 #include "som_local_internal.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace som {
 namespace {
@@ -69,7 +70,9 @@ __device__ inline f4 multiply<float>(i4 b, i4 a, f4 c) {
 }
 
 // ---------------------------------------------------------------- one side
-// ROWS rows (or columns) of a tile, loaded by WAVES waves.
+// ROWS rows (or columns) of a tile, loaded by WAVES waves.  A lane's source is a
+// 32-bit offset from a base that all lanes share and that moves from slab to
+// slab (the launcher sees to it that the offsets fit).
 template <typename T, bool ACROSS, int ROWS, int WAVES>
 struct Side {
     static constexpr int kElems = 16 / sizeof(T);           // elements of a 16-byte piece
@@ -80,8 +83,8 @@ struct Side {
     static constexpr int kUnitPieces = 16 / kElems;
     static_assert(kLoads * WAVES * 8 == ROWS, "whole loads");
 
-    const char *src[kLoads];  // this lane's source of the next slab, by load
-    int64_t at[kLoads];       // its contraction index there
+    const char *base;
+    uint32_t off[kLoads];
     int64_t step;             // bytes from slab to slab
 
     // What the units of contraction step s are exchanged with.
@@ -89,107 +92,113 @@ struct Side {
         const int f = sizeof(T) == 2 ? (s & 3) | ((s >> 3) & 1) << 2 : (s >> 2) & 3;
         return f & (kUnits - 1);
     }
+    // The 16-byte place in the LDS slab that load j of this lane fills.
+    static __device__ int place(int j) {
+        return ((threadIdx.x >> 6) * kLoads + j) * 64 + (threadIdx.x & 63);
+    }
+    // Its contraction index within the slab.
+    static __device__ int index(int j) {
+        const int q = place(j);
+        return ACROSS ? q / kPieces : ((q & 7) ^ (q >> 3 & 7)) * kElems;
+    }
+    // across: the column it holds, the last whole piece's beyond the matrix.
+    static __device__ int64_t column(int j, int64_t col0, int64_t cols) {
+        const int q = place(j), s = q / kPieces, at = q % kPieces;
+        const int unit = (at / kUnitPieces) ^ twist(s);
+        const int64_t c = col0 + unit * 16 + (at % kUnitPieces) * kElems;
+        return c < cols ? c : (cols - 1) / kElems * kElems;
+    }
 
     // Rows row0 .. of a side of `rows` rows whose element (r, c) is p[r * ld + c]
-    // (along), or columns row0 .. of one whose element is p[c * ld + r]
-    // (across); `list`: row r is the side's row list[r] / per.  k0: where the
-    // contraction begins, counted from p.
-    __device__ void begin(const void *p, int64_t ld, int64_t row0, int64_t rows, int64_t k0,
+    // (along), or columns row0 .. of one whose element is p[c * ld + r] (across),
+    // from contraction index k0 on; `list`: row r is the side's row list[r] / per.
+    __device__ void begin(const T *p, int64_t ld, int64_t row0, int64_t rows, int64_t k0,
                           const int32_t *list, int per) {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        base = reinterpret_cast<const char *>(p + (ACROSS ? k0 * ld : k0 + (list ? 0 : row0 * ld)));
+        step = ACROSS ? kSlab * ld * (int64_t)sizeof(T) : 128;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int q = (wave * kLoads + j) * 64 + lane;  // 16-byte place in the LDS slab
-            const char *base = static_cast<const char *>(p);
             if (ACROSS) {
-                const int s = q / kPieces, place = q % kPieces;
-                const int unit = (place / kUnitPieces) ^ twist(s);
-                const int64_t c = row0 + unit * 16 + (place % kUnitPieces) * kElems;
-                const int64_t col = c < rows ? c : (rows - 1) / kElems * kElems;
-                at[j] = k0 + s;
-                src[j] = base + ((at[j] * ld) + col) * (int64_t)sizeof(T);
+                off[j] = (uint32_t)((index(j) * ld + column(j, row0, rows)) * (int64_t)sizeof(T));
             } else {
-                const int r = q >> 3, piece = (q & 7) ^ (r & 7);
-                int64_t row = row0 + r < rows ? row0 + r : rows - 1;
-                if (list) row = list[row] / per;
-                at[j] = k0 + piece * kElems;
-                src[j] = base + (row * ld + at[j]) * (int64_t)sizeof(T);
+                const int r = place(j) >> 3;
+                int64_t row = row0 + r < rows ? r : rows - 1 - row0;
+                if (list) row = list[row0 + row] / per;
+                off[j] = (uint32_t)((row * ld + index(j)) * (int64_t)sizeof(T));
             }
         }
-        step = ACROSS ? kSlab * ld * (int64_t)sizeof(T) : 128;
     }
 
-    // Load the next slab into `lds`; contraction indices from k_end on are zeros.
-    __device__ void load(char *lds, int64_t k_end, bool whole) {
+    // Load the next slab into `lds`.  CHECK: `left` contraction indices are left, the
+    // rest are zeros.
+    template <bool CHECK>
+    __device__ void load(char *lds, int64_t left) {
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const char *from = src[j];
-            if (!whole && at[j] >= k_end) from = reinterpret_cast<const char *>(&kZeros);
+            const char *from = base + off[j];
+            if (CHECK && index(j) >= left) from = reinterpret_cast<const char *>(&kZeros);
             __builtin_amdgcn_global_load_lds((GlobalPtr)from,
                                              (LdsPtr)(lds + (wave * kLoads + j) * 1024), 16, 0, 0);
-            src[j] += step;
-            at[j] += kSlab;
         }
+        base += step;
     }
 
-    // As load, of an across side whose contraction step s is the side's row
-    // list[s] / per: the sources are found anew for each slab.
-    __device__ void load_listed(char *lds, const void *p, int64_t ld, int64_t row0, int64_t rows,
-                                int64_t k_end, const int32_t (&row)[kLoads]) {
-        const int lane = threadIdx.x & 63;
-        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    // An across side whose contraction step s is the matrix's row list[s] / per:
+    // the list's entries for the next slab (it points at the slab's first), and the
+    // offsets that they give.
+    __device__ static void entries(const int32_t *list, int64_t left, int32_t (&row)[kLoads]) {
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int q = (wave * kLoads + j) * 64 + lane;
-            const int s = q / kPieces, place = q % kPieces;
-            const int unit = (place / kUnitPieces) ^ twist(s);
-            const int64_t c = row0 + unit * 16 + (place % kUnitPieces) * kElems;
-            const int64_t col = c < rows ? c : (rows - 1) / kElems * kElems;
-            const char *from = static_cast<const char *>(p) +
-                               (row[j] * ld + col) * (int64_t)sizeof(T);
-            if (at[j] >= k_end) from = reinterpret_cast<const char *>(&kZeros);
-            __builtin_amdgcn_global_load_lds((GlobalPtr)from,
-                                             (LdsPtr)(lds + (wave * kLoads + j) * 1024), 16, 0, 0);
-            at[j] += kSlab;
-        }
+        for (int j = 0; j < kLoads; ++j) row[j] = index(j) < left ? list[index(j)] : 0;
     }
-
-    // The rows of the next slab's contraction steps (0 past k_end).
-    __device__ void rows_of(const int32_t *list, int per, int64_t k_end, int ahead,
-                            int32_t (&row)[kLoads]) const {
+    __device__ void follow(const int32_t (&row)[kLoads], int per, int64_t ld, int64_t col0,
+                           int64_t cols) {
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int64_t s = at[j] + (int64_t)ahead * kSlab;
-            row[j] = s < k_end ? list[s] / per : 0;
-        }
+        for (int j = 0; j < kLoads; ++j)
+            off[j] = (uint32_t)(((int64_t)(row[j] / per) * ld + column(j, col0, cols)) *
+                                (int64_t)sizeof(T));
     }
+};
 
-    // Fragment of rows r0 .. r0 + 15 and half h (64 bytes of contraction) of a slab.
-    static __device__ i4 fragment(const char *lds, int r0, int h) {
+// Where a wave's F fragments lie in a side's LDS slab: one offset that depends on
+// the lane.  Fragment f's differs from it by a constant (along), or by an
+// exclusive or, as the fragments' numbers and the twist are (across); that is done
+// anew for every slab, so that it takes an instruction and not a register.
+template <typename T, bool ACROSS, int ROWS, int F>
+struct Fragments {
+    static_assert((F & (F - 1)) == 0, "the first fragment's number is a multiple of F");
+    static constexpr int kRow = ROWS * sizeof(T);   // across: bytes of a contraction step
+    int at;
+
+    // The wave's fragments begin at row r0 of the tile.
+    __device__ void begin(int r0) {
         const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
         if (!ACROSS) {
-            const int r = r0 + i;
-            return *reinterpret_cast<const i4 *>(lds + r * 128 + (((h * 4 + g) ^ (r & 7)) << 4));
+            at = (r0 + i) * 128 + ((g ^ (i & 7)) << 4);
+        } else {
+            const int s = sizeof(T) == 2 ? 8 * g + (i >> 2) : 4 * g;
+            const int unit = r0 / 16 ^ Side<T, true, ROWS, ROWS / 8>::twist(s);
+            at = s * kRow + unit * 16 * (int)sizeof(T) + (sizeof(T) == 2 ? (i & 3) * 8 : i * 4);
         }
-        constexpr int kRow = ROWS * sizeof(T);
+    }
+    // Fragment f, half h (64 bytes of contraction) of the slab at lds + slab, a
+    // multiple of all that is exchanged.
+    __device__ i4 read(const char *lds, int slab, int f, int h) const {
+        if (!ACROSS)
+            return *reinterpret_cast<const i4 *>(lds + ((slab + at) ^ (h * 64)) + f * 16 * 128);
+        const char *from = lds + ((slab + at) ^ (f * 16 * (int)sizeof(T)));
         if (sizeof(T) == 2) {
             s4 v[2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int s = 32 * h + 8 * g + 4 * e + (i >> 2);
-                const char *from = lds + s * kRow + (((r0 >> 4) ^ twist(s)) << 5) + (i & 3) * 8;
-                v[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4)from);
-            }
+            for (int e = 0; e < 2; ++e)
+                v[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (LdsS4)(from + (32 * h + 4 * e) * kRow));
             return __builtin_bit_cast(i4, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
         }
         i4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int s = 16 * h + 4 * g + e;
-            v[e] = *reinterpret_cast<const int *>(lds + s * kRow + (((r0 >> 4) ^ twist(s)) << 6) +
-                                                  i * 4);
-        }
+        for (int e = 0; e < 4; ++e)
+            v[e] = *reinterpret_cast<const int *>(from + (16 * h + e) * kRow);
         return v;
     }
 };
@@ -214,88 +223,143 @@ __device__ inline void band_tile(int64_t t, int64_t tm, int64_t tn, int64_t *m, 
     *n = in / high;
 }
 
-// Largest e in [0, experts) whose first tile offsets[e] / tile + e is at most
-// t, or with tile = 0 whose first row is at most t: 64 places tested at a time.
-// (An expert of c rows from row o on has the tiles from o / tile + e on; the next
-// one's begin at least ceil(c / tile) later, and the last ones may be empty.)
-__device__ inline int expert_of(const int32_t *offsets, int experts, int tile, int64_t t) {
-    const int lane = threadIdx.x & 63;
-    int lo = 0, span = experts;
-    while (span > 1) {
-        const int width = (span + 63) / 64;
-        const int e = lo + lane * width;
-        const bool at_most = lane * width < span &&
-                             (tile ? (int64_t)(offsets[e] / tile) + e : (int64_t)offsets[e]) <= t;
-        const int last = 63 - __clzll(__ballot(at_most) | 1);
-        lo += last * width;
-        span = span - last * width < width ? span - last * width : width;
-    }
-    return __builtin_amdgcn_readfirstlane(lo);
-}
-
-// Four neighbouring values of a row to and from memory, `left` of them there.
-template <typename T>
-__device__ inline f4 read4(const T *p, int left, bool vec) {
-    f4 v = {0.f, 0.f, 0.f, 0.f};
-    if (vec && left >= 4) {
-        typedef T t4 __attribute__((ext_vector_type(4)));
-        const t4 q = *reinterpret_cast<const t4 *>(p);
+// N neighbouring values of a row to and from memory, `left` of them there.
+template <typename T, int N>
+struct Piece {
+    typedef T Vec __attribute__((ext_vector_type(N)));
+    Vec v;
+    __device__ void read(const T *p, int left, bool vec) {
+        if (vec && left >= N) {
+            v = *reinterpret_cast<const Vec *>(p);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (float)q[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < left) v[e] = (float)p[e];
-    }
-    return v;
-}
-template <typename T>
-__device__ inline void write4(T *p, f4 v, int left, bool vec) {
-    if (vec && left >= 4) {
-        typedef T t4 __attribute__((ext_vector_type(4)));
-        t4 q;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) q[e] = (T)v[e];
-        *reinterpret_cast<t4 *>(p) = q;
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < left) p[e] = (T)v[e];
-    }
-}
-
-// What happens to four sums of output row `row`, columns `col` .. of batch
-// `batch`, before they are rounded and stored.
-template <typename T, int MODE>
-__device__ inline void epilogue(const ProductArgs &a, int64_t row, int64_t col, int batch, f4 v) {
-    const int left = (int)(a.n - col < 4 ? a.n - col : 4);
-    const int64_t at = ((MODE == kWeight ? batch * a.m : 0) + row) * a.n + col;
-    if (MODE == kForward) {
-        if (a.bias)
-            v += read4(static_cast<const T *>(a.bias) + batch * a.n + col, left, a.vec & kVecBias);
-        if (a.z) write4(static_cast<T *>(a.z) + at, v, left, a.vec & kVecOut);
-        if (a.activation != kActNone) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = activate(v[e], a.activation);
+            for (int e = 0; e < N; ++e) v[e] = e < left ? p[e] : (T)0.f;
         }
-        if (a.residual)
-            v += read4(static_cast<const T *>(a.residual) + row * a.ldr + col, left,
-                       a.vec & kVecResidual);
     }
-    if (MODE == kInput && a.slope) {
-        const f4 z = read4(static_cast<const T *>(a.slope) + at, left, a.vec & kVecSlope);
+    __device__ void write(T *p, int left, bool vec) const {
+        if (vec && left >= N) {
+            *reinterpret_cast<Vec *>(p) = v;
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] *= activation_slope(z[e], a.activation);
+            for (int e = 0; e < N; ++e)
+                if (e < left) p[e] = v[e];
+        }
     }
-    write4(static_cast<T *>(a.y) + at, v, left, a.vec & kVecOut);
+};
+
+// The activation, or its slope, of N values.
+template <int N>
+__device__ inline void activate_all(float (&v)[N], int32_t kind) {
+    if (kind == kActNone) return;
+    if (kind == kActRelu) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = activate(v[e], kActRelu);
+    } else if (kind == kActGelu) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = activate(v[e], kActGelu);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = activate(v[e], kActSilu);
+    }
+}
+template <int N>
+__device__ inline void slopes_all(float (&v)[N], int32_t kind) {
+    if (kind == kActRelu) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = activation_slope(v[e], kActRelu);
+    } else if (kind == kActGelu) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = activation_slope(v[e], kActGelu);
+    } else if (kind == kActSilu) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = activation_slope(v[e], kActSilu);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = 1.f;
+    }
 }
 
-template <typename T, int MODE, int TM, int TN, int WM, int WN>
-__global__ __launch_bounds__(WM *WN * 64, TM == 256 ? 2 : 1) void product_kernel(ProductArgs a) {
+// Waits until at most COUNT of this wave's loads are under way.
+template <int COUNT>
+__device__ inline void wait_loads() {
+    __builtin_amdgcn_s_waitcnt((COUNT & 15) | (COUNT >> 4 & 3) << 14 | 0x0F70);
+}
+
+template <int V>
+using Int = std::integral_constant<int, V>;
+
+// What happens to N sums of output row `row`, columns `col` .. of batch `batch`,
+// before they are rounded and stored: in two steps, so that the reads of several
+// rows can be under way together.
+template <typename T, int MODE, int N>
+struct Epilogue {
+    const ProductArgs &a;
+    int64_t col;
+    int batch, left;
+    float bias[N];
+    __device__ Epilogue(const ProductArgs &args, int64_t c, int b) : a(args), col(c), batch(b) {
+        left = (int)(a.n - col < N ? a.n - col : N);
+        Piece<T, N> p;
+        const bool there = MODE == kForward && a.bias && left > 0;
+        if (there)
+            p.read(static_cast<const T *>(a.bias) + batch * a.n + col, left, a.vec & kVecBias);
+#pragma unroll
+        for (int e = 0; e < N; ++e) bias[e] = there ? (float)p.v[e] : 0.f;
+    }
+    // The row's residual (forward) or slope argument (input).
+    __device__ void read(int64_t row, Piece<T, N> &extra) const {
+        if (MODE == kForward && a.residual)
+            extra.read(static_cast<const T *>(a.residual) + row * a.ldr + col, left,
+                       a.vec & kVecResidual);
+        if (MODE == kInput && a.slope)
+            extra.read(static_cast<const T *>(a.slope) + row * a.n + col, left, a.vec & kVecSlope);
+    }
+    __device__ void write(int64_t row, const Piece<T, N> &extra, float (&v)[N]) const {
+        const int64_t at = ((MODE == kWeight ? batch * a.m : 0) + row) * a.n + col;
+        Piece<T, N> out;
+        if (MODE == kForward) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] += bias[e];
+            if (a.z) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) out.v[e] = (T)v[e];
+                out.write(static_cast<T *>(a.z) + at, left, a.vec & kVecOut);
+            }
+            activate_all(v, a.activation);
+            if (a.residual) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[e] += (float)extra.v[e];
+            }
+        }
+        if (MODE == kInput && a.slope) {
+            float z[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) z[e] = (float)extra.v[e];
+            slopes_all(z, a.activation);
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] *= z[e];
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) out.v[e] = (T)v[e];
+        out.write(static_cast<T *>(a.y) + at, left, a.vec & kVecOut);
+    }
+};
+
+// A workgroup's tile: WM x WN waves of (TM / WM) x (TN / WN).  Per slab, with the
+// fragments of its first half in registers:
+//   read the second half's fragments; multiply the first
+//   wait: the next slab has landed, and nobody reads this one any more
+//   load the slab after the next in its place; read the next slab's first half;
+//   multiply the second half
+// so that the matrix cores always have fragments in hand, and a load has a slab's
+// time to arrive.
+template <typename T, int MODE, bool LISTED, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) {
     constexpr bool kAcrossA = MODE == kWeight, kAcrossB = MODE != kForward;
     using SideA = Side<T, kAcrossA, TM, WM * WN>;
     using SideB = Side<T, kAcrossB, TN, WM * WN>;
-    constexpr int FM = TM / WM / 16, FN = TN / WN / 16;  // fragments of a wave's tile
+    constexpr int kTileM = TM / WM, kTileN = TN / WN;    // of a wave
+    constexpr int FM = kTileM / 16, FN = kTileN / 16;    // its fragments
     constexpr int kSlab = SideA::kSlab;
     constexpr int kBytes = (TM + TN) * 128;              // of a slab
     extern __shared__ __align__(16) char lds[];
@@ -334,100 +398,157 @@ __global__ __launch_bounds__(WM *WN * 64, TM == 256 ? 2 : 1) void product_kernel
     }
     const T *pa = static_cast<const T *>(a.a), *pb = static_cast<const T *>(a.b);
     if (MODE != kWeight) pb += batch * a.batch_b;
-    const bool listed = MODE == kWeight && a.list;  // side B's rows by the list
 
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int wm = wave / WN * (TM / WM), wn = wave % WN * (TN / WN);
+    const int wm = wave / WN * kTileM, wn = wave % WN * kTileN;
 
     f4 acc[FM][FN];
 #pragma unroll
     for (int x = 0; x < FM; ++x)
 #pragma unroll
         for (int y = 0; y < FN; ++y) acc[x][y] = f4{0.f, 0.f, 0.f, 0.f};
-    // gradient of the bias: the sums of side A over the contraction, as a product
-    // with ones on the workgroups and waves of the first columns
-    const bool sums = MODE == kWeight && a.bias_grad && col0 == 0 && wn == 0;
-    f4 sum[MODE == kWeight ? FM : 1];
-#pragma unroll
-    for (int x = 0; x < (MODE == kWeight ? FM : 1); ++x) sum[x] = f4{0.f, 0.f, 0.f, 0.f};
-    i4 ones;
-    {
-        const int one = sizeof(T) == 4 ? 0x3f800000
-                        : __is_same(T, __bf16) ? 0x3f803f80 : 0x3c003c00;
-        ones = i4{one, one, one, one};
-    }
-
     const int64_t slabs = (k_end - k0 + kSlab - 1) / kSlab;
     if (slabs > 0) {
         SideA sa;
         SideB sb;
+        Fragments<T, kAcrossA, TM, FM> ra;
+        Fragments<T, kAcrossB, TN, FN> rb;
         sa.begin(pa, a.lda, row0, row_end, k0, MODE == kWeight ? nullptr : a.list, a.per);
-        sb.begin(pb, a.ldb, col0, a.n, k0, nullptr, 1);
-        int32_t row[SideB::kLoads];
-        if (MODE == kWeight && listed) sb.rows_of(a.list, a.per, k_end, 0, row);
-        const auto load = [&](int64_t s) {
-            char *to = lds + (s & 1) * kBytes;
-            const bool whole = k0 + (s + 1) * kSlab <= k_end;
-            sa.load(to, k_end, whole);
-            if (MODE == kWeight && listed) {
-                sb.load_listed(to + TM * 128, pb, a.ldb, col0, a.n, k_end, row);
-                sb.rows_of(a.list, a.per, k_end, 0, row);
-            } else {
-                sb.load(to + TM * 128, k_end, whole);
+        sb.begin(pb, a.ldb, col0, a.n, LISTED ? 0 : k0, nullptr, 1);
+        ra.begin(wm);
+        rb.begin(wn);
+        int32_t entry[SideB::kLoads];
+        if (LISTED) {
+            sb.step = 0;
+            SideB::entries(a.list + k0, k_end - k0, entry);
+        }
+        // the offsets of the slab that is loaded next, and the list beyond it
+        const auto follow = [&](int64_t s) {
+            if (LISTED) {
+                sb.follow(entry, a.per, a.ldb, col0, a.n);
+                SideB::entries(a.list + k0 + (s + 1) * kSlab, k_end - k0 - (s + 1) * kSlab, entry);
             }
         };
-        load(0);
-        for (int64_t s = 0; s < slabs; ++s) {
-            __builtin_amdgcn_s_waitcnt(0x0F70);  // this wave's loads of slab s are in LDS
-            __syncthreads();                     // and everyone's; slab s - 1 is no longer read
-            if (s + 1 < slabs) load(s + 1);
-            const char *la = lds + (s & 1) * kBytes, *lb = la + TM * 128;
+        const auto load = [&](auto check, int64_t s) {
+            char *to = lds + (s & 1) * kBytes;
+            const int64_t left = k_end - k0 - s * kSlab;
+            sa.template load<decltype(check)::value>(to, left);
+            sb.template load<decltype(check)::value>(to + TM * 128, left);
+        };
+        i4 fa[2][FM], fb[2][FN];
+        const auto read = [&](int64_t s, auto half) {
+            constexpr int h = decltype(half)::value;
+            const int la = (int)(s & 1) * kBytes, lb = la + TM * 128;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                i4 fa[FM], fb[FN];
+            for (int y = 0; y < FN; ++y) fb[h][y] = rb.read(lds, lb, y, h);
 #pragma unroll
-                for (int x = 0; x < FM; ++x) fa[x] = SideA::fragment(la, wm + 16 * x, h);
+            for (int x = 0; x < FM; ++x) fa[h][x] = ra.read(lds, la, x, h);
+        };
+        const auto times = [&](auto half) {
+            constexpr int h = decltype(half)::value;
 #pragma unroll
-                for (int y = 0; y < FN; ++y) fb[y] = SideB::fragment(lb, wn + 16 * y, h);
+            for (int x = 0; x < FM; ++x)
 #pragma unroll
-                for (int x = 0; x < FM; ++x)
+                for (int y = 0; y < FN; ++y)
+                    acc[x][y] = multiply<T>(fb[h][y], fa[h][x], acc[x][y]);
+        };
+        // slab s; loading slab s + 2 (2: of a whole slab, 1: perhaps the last, in part),
+        // or only going on to slab s + 1 (0), or not even that (-1)
+        const auto slab = [&](auto what, int64_t s) {
+            constexpr int k = decltype(what)::value;
+            if (k > 0) follow(s + 2);
+            read(s, Int<1>());
+            times(Int<0>());
+            __builtin_amdgcn_sched_barrier(0);   // the products come before the waits
+            if (k < 0) {
+                times(Int<1>());
+                return;
+            }
+            wait_loads<0>();                     // the next slab has landed
+            __syncthreads();                     // for everyone; this one is no longer read
+            if (k == 2) load(Int<0>(), s + 2);
+            if (k == 1) load(Int<1>(), s + 2);
+            read(s + 1, Int<0>());
+            times(Int<1>());
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        follow(0);
+        load(Int<1>(), 0);
+        if (slabs > 1) {
+            follow(1);
+            load(Int<1>(), 1);
+        }
+        // all but the second slab's loads have landed
+        if (slabs > 1 && !LISTED) wait_loads<SideA::kLoads + SideB::kLoads>();
+        else wait_loads<0>();
+        __syncthreads();
+        read(0, Int<0>());
+        int64_t s = 0;
+        for (; s + 3 < slabs; ++s) slab(Int<2>(), s);
+        if (s + 2 < slabs) slab(Int<1>(), s++);
+        if (s + 1 < slabs) slab(Int<0>(), s++);
+        slab(Int<-1>(), s);
+    }
+
+    // Through LDS, so that a lane holds 16 bytes of a row of the result: the
+    // waves' own parts, 64 rows at a time, quads of columns exchanged by row so that
+    // all banks are met.
+    __syncthreads();
+    constexpr int N = 16 / sizeof(T), kQuads = kTileN / 4;
+    constexpr int kFits = 2 * kBytes / (WM * WN * kTileN * 4);   // rows of a wave's part
+    constexpr int kMost = kFits >= 64 ? 64 : kFits >= 32 ? 32 : 16;
+    constexpr int kRowsAt = kTileM < kMost ? kTileM : kMost;
+    constexpr int kLanes = kTileN / N, kPass = 64 / kLanes;
+    constexpr int kGroup = kRowsAt / kPass < 4 ? kRowsAt / kPass : 4;
+    static_assert(WM * WN * kRowsAt * kTileN * 4 <= 2 * kBytes, "fits in the slabs' LDS");
+    f4 *mine = reinterpret_cast<f4 *>(lds) + wave * (kRowsAt * kQuads);
+    const int64_t col = col0 + wn + lane % kLanes * N;
+    Epilogue<T, MODE, N> end(a, col < a.n ? col : 0, batch);
 #pragma unroll
-                    for (int y = 0; y < FN; ++y)
-                        acc[x][y] = multiply<T>(fb[y], fa[x], acc[x][y]);
-                if (MODE == kWeight && sums) {
+    for (int x0 = 0; x0 < FM; x0 += kRowsAt / 16) {
 #pragma unroll
-                    for (int x = 0; x < FM; ++x) sum[x] = multiply<T>(ones, fa[x], sum[x]);
+        for (int x = 0; x < kRowsAt / 16; ++x)
+#pragma unroll
+            for (int y = 0; y < FN; ++y)
+                mine[(16 * x + i) * kQuads + ((4 * y + g) ^ (i & (kQuads - 1)))] = acc[x0 + x][y];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int64_t first = row0 + wm + 16 * x0 + lane / kLanes;
+#pragma unroll 1
+        for (int p = 0; p < kRowsAt / kPass; p += kGroup) {
+            Piece<T, N> extra[kGroup];
+            if (a.splits == 1 && col < a.n) {
+#pragma unroll
+                for (int q = 0; q < kGroup; ++q)
+                    if (first + (p + q) * kPass < row_end)
+                        end.read(first + (p + q) * kPass, extra[q]);
+            }
+#pragma unroll
+            for (int q = 0; q < kGroup; ++q) {
+                const int r = (p + q) * kPass + lane / kLanes;
+                const int64_t row = first + (p + q) * kPass;
+                float v[N];
+#pragma unroll
+                for (int e = 0; e < N / 4; ++e) {
+                    const f4 u = mine[r * kQuads + ((lane % kLanes * (N / 4) + e) ^
+                                                    (r & 15 & (kQuads - 1)))];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) v[4 * e + c] = u[c];
+                }
+                if (row >= row_end || col >= a.n) continue;
+                if (a.splits > 1) {  // columns are padded to whole tiles
+                    const int64_t at = MODE == kWeight ? (int64_t)batch * a.m + row : row;
+                    f4 *to = reinterpret_cast<f4 *>(
+                        a.partial + (blockIdx.y * a.partial_rows + at) * (tn * TN) + col);
+#pragma unroll
+                    for (int e = 0; e < N / 4; ++e)
+                        to[e] = f4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
+                } else {
+                    end.write(row, extra[q], v);
                 }
             }
         }
-    }
-
-#pragma unroll
-    for (int x = 0; x < FM; ++x) {
-        const int64_t row = row0 + wm + 16 * x + i;
-        if (row >= row_end) continue;
-#pragma unroll
-        for (int y = 0; y < FN; ++y) {
-            const int64_t col = col0 + wn + 16 * y + 4 * g;
-            if (col >= a.n) continue;
-            if (a.splits > 1) {  // columns are padded to whole tiles
-                const int64_t ld = tn * TN;
-                const int64_t r = MODE == kWeight ? (int64_t)batch * a.m + row : row;
-                *reinterpret_cast<f4 *>(a.partial + (blockIdx.y * a.partial_rows + r) * ld + col) =
-                    acc[x][y];
-            } else {
-                epilogue<T, MODE>(a, row, col, batch, acc[x][y]);
-            }
-        }
-        if (MODE == kWeight && sums && g == 0) {
-            const int64_t r = (int64_t)batch * a.m + row;
-            if (a.splits > 1)
-                a.partial[a.splits * a.partial_rows * tn * TN + blockIdx.y * a.partial_rows + r] =
-                    sum[x][0];
-            else
-                static_cast<T *>(a.bias_grad)[r] = (T)sum[x][0];
-        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
@@ -457,14 +578,12 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a, int64_t ld) {
             f4 v = {0.f, 0.f, 0.f, 0.f};
             for (int s = 0; s < a.splits; ++s)
                 v += *reinterpret_cast<const f4 *>(a.partial + (s * a.partial_rows + r) * ld + col);
-            epilogue<T, MODE>(a, row, col, batch, v);
+            float u[4] = {v[0], v[1], v[2], v[3]};
+            const Epilogue<T, MODE, 4> end(a, col, batch);
+            Piece<T, 4> extra;
+            end.read(row, extra);
+            end.write(row, extra, u);
         }
-    }
-    if (MODE == kWeight && a.bias_grad && q < a.partial_rows) {
-        float v = 0.f;
-        for (int s = 0; s < a.splits; ++s)
-            v += a.partial[a.splits * a.partial_rows * ld + s * a.partial_rows + q];
-        static_cast<T *>(a.bias_grad)[q] = (T)v;
     }
 }
 
@@ -543,11 +662,17 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(ProductArgs a, int by_
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) v += part[w][r][lane];
         const int64_t row = row0 + 16 * r + i, col = col0 + 4 * g;
-        if (row < row_end && col < a.n) epilogue<T, kForward>(a, row, col, batch, v);
+        if (row < row_end && col < a.n) {
+            float u[4] = {v[0], v[1], v[2], v[3]};
+            const Epilogue<T, kForward, 4> end(a, col, batch);
+            Piece<T, 4> extra;
+            end.read(row, extra);
+            end.write(row, extra, u);
+        }
     }
 }
 
-template <typename T, int MODE, int TM, int TN, int WM, int WN>
+template <typename T, int MODE, bool LISTED, int TM, int TN, int WM, int WN>
 hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
     const int64_t tn = (a.n + TN - 1) / TN;
     const int64_t tm = MODE == kWeight ? (a.m + TM - 1) / TM * (a.offsets ? a.experts : 1)
@@ -555,7 +680,7 @@ hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
                                        : (a.m + TM - 1) / TM;
     if (tm * tn > INT32_MAX) return hipErrorInvalidValue;
     constexpr int kLds = 2 * (TM + TN) * 128;
-    const auto kernel = product_kernel<T, MODE, TM, TN, WM, WN>;
+    const auto kernel = product_kernel<T, MODE, LISTED, TM, TN, WM, WN>;
     if (kLds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
@@ -563,19 +688,20 @@ hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
     }
     kernel<<<dim3((unsigned)(tm * tn), a.splits), WM * WN * 64, kLds, stream>>>(a);
     if (a.splits > 1) {
-        const int64_t quads = std::max(a.partial_rows * ((a.n + 3) / 4), a.partial_rows);
+        const int64_t quads = a.partial_rows * ((a.n + 3) / 4);
         if ((quads + 255) / 256 > INT32_MAX) return hipErrorInvalidValue;
         join_kernel<T, MODE><<<(unsigned)((quads + 255) / 256), 256, 0, stream>>>(a, tn * TN);
     }
     return hipGetLastError();
 }
 
-template <typename T, int MODE>
+// LISTED: side B's rows (weight) are named by the list.
+template <typename T, int MODE, bool LISTED>
 hipError_t launch_mode(const ProductArgs &a, const ProductPlan &p, hipStream_t stream) {
     switch (p.tile) {
-        case 256: return launch_tiles<T, MODE, 256, 256, 2, 4>(a, stream);
-        case 128: return launch_tiles<T, MODE, 128, 128, 2, 2>(a, stream);
-        default: return launch_tiles<T, MODE, 64, 64, 2, 2>(a, stream);
+        case 256: return launch_tiles<T, MODE, LISTED, 256, 256, 2, 4>(a, stream);
+        case 128: return launch_tiles<T, MODE, LISTED, 128, 128, 2, 2>(a, stream);
+        default: return launch_tiles<T, MODE, LISTED, 64, 64, 2, 2>(a, stream);
     }
 }
 
@@ -603,9 +729,10 @@ hipError_t launch_product(ProductArgs a, const ProductPlan &p, hipStream_t strea
                             : launch_rows<T, 4, 16>(a, al, stream);
     }
     switch (a.mode) {
-        case kForward: return launch_mode<T, kForward>(a, p, stream);
-        case kInput: return launch_mode<T, kInput>(a, p, stream);
-        default: return launch_mode<T, kWeight>(a, p, stream);
+        case kForward: return launch_mode<T, kForward, false>(a, p, stream);
+        case kInput: return launch_mode<T, kInput, false>(a, p, stream);
+        default: return a.list ? launch_mode<T, kWeight, true>(a, p, stream)
+                               : launch_mode<T, kWeight, false>(a, p, stream);
     }
 }
 
