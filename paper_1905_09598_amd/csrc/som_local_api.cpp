@@ -17,25 +17,28 @@ namespace som {
 // How a product runs.  Few rows: the kernel that streams w.  Otherwise the tile
 // and the number of parts of the contraction with the least estimated time:
 // rounds of workgroups over the compute units, slabs in each, and the pass that
-// joins the parts.
-ProductPlan plan_product(const ProductArgs &a, int num_cus) {
+// joins the parts.  aligned: whether both sides lie in whole 16-byte pieces.
+ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus) {
     ProductPlan best{};
+    best.aligned = aligned;
     const int64_t experts = a.offsets ? a.experts : 1;
     const int64_t slab = 128 / type_size(a.type);
-    if (a.mode == kForward && a.m <= 64 * experts && (a.offsets || a.m <= 64)) {
-        const int64_t per = (a.m + experts - 1) / experts;
-        best.tile = per <= 16 ? 16 : 64;
+    if (a.mode == kForward && a.m <= 16 * experts) {
+        best.tile = 16;
         const int64_t groups = (a.n + 15) / 16 * std::min(a.m, a.m / best.tile + experts);
         // sixteen waves where four would leave the chip short of loads in flight
         best.waves = groups * 4 < (int64_t)num_cus * 16 && a.k >= 8 * slab ? 16 : 4;
         best.splits = 1;
         return best;
     }
-    // microseconds of a slab on all the workgroups that a compute unit holds
-    struct Shape { int32_t tile, held; double half, single; };
-    static const Shape shapes[] = {{256, 1, 1.6, 7.5}, {128, 2, 1.0, 3.8}, {64, 4, 0.7, 2.0}};
-    double least = INFINITY;
+    // microseconds of a slab on all the workgroups that a compute unit holds: 16-bit
+    // types, fp32, and what unaligned rows add
+    struct Shape { int32_t tile, held; double half, single, unaligned; };
+    static const Shape shapes[] = {
+        {256, 1, 1.6, 7.5, 0}, {128, 2, 1.0, 3.8, 0.6}, {64, 4, 0.7, 2.0, 0.6}};
+    best.time = INFINITY;
     for (const Shape &s : shapes) {
+        if (!aligned && s.tile == 256) continue;
         const int64_t tn = (a.n + s.tile - 1) / s.tile;
         int64_t tm, k = a.k;
         if (a.mode == kWeight) {
@@ -49,17 +52,17 @@ ProductPlan plan_product(const ProductArgs &a, int num_cus) {
         const int64_t slabs = std::max<int64_t>(1, (k + slab - 1) / slab);
         const int64_t rows = a.mode == kWeight ? a.m * experts : a.m;
         for (int32_t parts = 1; parts <= 32 && parts <= slabs; parts *= 2) {
-            const int64_t floats =
-                parts > 1 ? parts * rows * (tn * s.tile) : 0;
+            const int64_t floats = parts > 1 ? parts * rows * (tn * s.tile) : 0;
             if (floats > (int64_t)1 << 30) break;
             const double rounds =
                 std::ceil((double)(tm * tn * parts) / ((double)num_cus * s.held));
             const double each = ((slabs + parts - 1) / parts) *
-                                    (a.type == kF32 ? s.single : s.half) + 4.0;
+                                    ((a.type == kF32 ? s.single : s.half) +
+                                     (aligned ? 0.0 : s.unaligned)) + 4.0;
             const double join = parts > 1 ? 4.0 + floats * 4.0 / 2.5e6 : 0.0;
             const double time = rounds * each + join;
-            if (time < least) {
-                least = time;
+            if (time < best.time) {
+                best.time = time;
                 best.tile = s.tile;
                 best.splits = parts;
                 best.partial_floats = floats;
@@ -124,52 +127,56 @@ struct Carver {
     }
 };
 
-// A matrix as a product reads it.
-struct Operand {
-    const void *p;
-    int64_t ld;
-};
-
 int64_t rounded(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
-// One side of a product: the caller's rows where they lie in whole 16-byte
-// pieces within a tile's reach, else (or where a slope has to be applied) a copy
-// whose rows do.  *list: the side's rows are named by it; a matrix that is too long
-// to be reached by it is copied row by row of the list, and *list becomes null.
-struct SideCopy {
-    som::RowsArgs rows{};
-    bool needed = false;
-};
-Operand whole_rows(Carver &work, SideCopy &copy, int32_t type, const void *p, int64_t rows,
-                   int64_t cols, int64_t ld, const void *z = nullptr, int32_t activation = 0,
-                   const int32_t **list = nullptr, int32_t per = 1, int64_t listed = 0) {
-    const int size = som::type_size(type), elems = 16 / size;
-    const bool whole = reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % elems == 0 &&
-                       cols % elems == 0 && som::tile_reaches(ld, size);
-    const int64_t ldd = rounded(cols, elems);
-    const bool far = list && *list && rows * (whole ? ld : ldd) * size >= (int64_t)1 << 32;
-    if (whole && !z && !far) return {p, ld};
-    const int64_t high = far ? listed : rows;
-    void *to = work.take((uint64_t)high * ldd * size);
-    copy.needed = true;
-    copy.rows.type = type;
-    copy.rows.activation = activation;
-    copy.rows.src = p;
-    copy.rows.z = z;
-    copy.rows.dst = to;
-    copy.rows.rows = high;
-    copy.rows.cols = cols;
-    copy.rows.lds = ld;
-    copy.rows.ldz = cols;
-    copy.rows.ldd = ldd;
-    copy.rows.list = far ? *list : nullptr;
-    copy.rows.per = per;
-    if (far) *list = nullptr;
-    return {to, ldd};
-}
+// One side of a product as the caller has it, and how it is read.
+struct SideRows {
+    const void *p = nullptr;
+    int64_t rows = 0, cols = 0, ld = 0;
+    const int32_t **list = nullptr;  // names `listed` of the rows, list[r] / per
+    int32_t per = 1;
+    int64_t listed = 0;
+    som::RowsArgs copy{};
+    bool copied = false;
 
-bool four(const void *p, int64_t ld, int size) {
-    return reinterpret_cast<uintptr_t>(p) % (4 * size) == 0 && ld % 4 == 0;
+    // Whole 16-byte pieces.
+    bool whole(int size) const {
+        return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % (16 / size) == 0 &&
+               cols % (16 / size) == 0;
+    }
+    // Beyond the offsets of the tiles' kernels: these rows have to be copied, in
+    // the order of the list if it is the listed matrix that is too long.
+    bool far(int size) const { return list && *list && rows * ld * size >= (int64_t)1 << 32; }
+    bool beyond(int size) const { return far(size) || !som::tile_reaches(ld, size); }
+    double copy_time(int size) const { return 3.0 + (double)rows * cols * size * 2 / 4.0e6; }
+
+    // A copy in whole pieces; with z, times act'(z).
+    void make_copy(Carver &work, int32_t type, const void *z = nullptr, int32_t activation = 0) {
+        const int size = som::type_size(type);
+        const int64_t ldd = rounded(cols, 16 / size);
+        const bool by_list = list && *list && rows * ldd * size >= (int64_t)1 << 32;
+        const int64_t high = by_list ? listed : rows;
+        copied = true;
+        copy.type = type;
+        copy.activation = activation;
+        copy.src = p;
+        copy.z = z;
+        copy.dst = work.take((uint64_t)high * ldd * size);
+        copy.rows = high;
+        copy.cols = cols;
+        copy.lds = ld;
+        copy.ldz = cols;
+        copy.ldd = ldd;
+        copy.list = by_list ? *list : nullptr;
+        copy.per = per;
+        if (by_list) *list = nullptr;
+        p = copy.dst, ld = ldd, rows = high;
+    }
+};
+
+// Rows that can be reached 16 bytes at a time.
+bool pieces(const void *p, int64_t ld, int size) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * size % 16 == 0;
 }
 
 hipError_t launch_product(const ProductArgs &a, const ProductPlan &plan, hipStream_t s) {
@@ -180,12 +187,32 @@ hipError_t launch_product(const ProductArgs &a, const ProductPlan &plan, hipStre
     }
 }
 
-// One product of a call, planned, with its parts' memory.
+// One product of a call, planned, with its parts' memory.  Sides that are not
+// whole are read as they are by the kernels that can, or copied first where that
+// and the faster kernels take less time.
 struct Product {
     ProductArgs a{};
     ProductPlan plan{};
-    void place(Carver &work) {
-        plan = som::plan_product(a, compute_units());
+    void place(Carver &work, SideRows &A, SideRows &B) {
+        const int size = som::type_size(a.type);
+        const auto needs = [&](const SideRows &s) { return !s.whole(size) && !s.copied; };
+        plan = som::plan_product(a, !needs(A) && !needs(B), compute_units());
+        if (!plan.waves) {
+            if (A.beyond(size)) A.make_copy(work, a.type);
+            if (B.beyond(size)) B.make_copy(work, a.type);
+            double copies = 0.0;
+            if (needs(A)) copies += A.copy_time(size);
+            if (needs(B)) copies += B.copy_time(size);
+            const ProductPlan whole = som::plan_product(a, true, compute_units());
+            if (whole.time + copies < plan.time || copies == 0.0) {
+                if (needs(A)) A.make_copy(work, a.type);
+                if (needs(B)) B.make_copy(work, a.type);
+                plan = whole;
+            }
+        }
+        a.a = A.p, a.lda = A.ld;
+        a.b = B.p, a.ldb = B.ld;
+        a.batch_b = B.ld * (a.mode == som::kForward ? a.n : a.k);
         if (plan.splits > 1) {
             a.partial = work.take<float>((uint64_t)plan.partial_floats * 4);
             a.partial_rows = a.mode == som::kWeight ? a.m * (a.offsets ? a.experts : 1) : a.m;
@@ -195,13 +222,11 @@ struct Product {
 
 // What a call enqueues, over the caller's work memory.
 struct LinearForward {
-    SideCopy x, w;
+    SideRows x, w;
     Product product;
     LinearForward(const som_linear_call &c, Carver &work) {
         const int size = som::type_size(c.type);
         const int64_t rows = c.experts ? c.n * c.k : c.n;
-        const int64_t xrows = c.gather ? c.n : rows;
-        const int64_t wrows = (int64_t)c.outer * std::max(1, c.experts);
         ProductArgs &a = product.a;
         a.mode = som::kForward;
         a.type = c.type;
@@ -213,77 +238,65 @@ struct LinearForward {
         a.bias = c.bias;
         a.residual = c.residual, a.ldr = c.ldr;
         a.y = c.y, a.z = c.z;
-        a.vec = (four(c.y, c.outer, size) && (!c.z || four(c.z, c.outer, size)) ? som::kVecOut : 0) |
-                (c.bias && four(c.bias, c.outer, size) ? som::kVecBias : 0) |
-                (c.residual && four(c.residual, c.ldr, size) ? som::kVecResidual : 0);
-        product.place(work);
-        Operand A{c.x, c.ldx}, B{c.w, c.inner};
-        if (product.plan.waves) {   // reads any rows
-            const int per = 16 / size;
-            product.plan.aligned = reinterpret_cast<uintptr_t>(c.x) % 16 == 0 &&
-                                   reinterpret_cast<uintptr_t>(c.w) % 16 == 0 &&
-                                   c.ldx % per == 0 && c.inner % per == 0;
-        } else {
-            A = whole_rows(work, x, c.type, c.x, xrows, c.inner, c.ldx, nullptr, 0, &a.list, c.k,
-                           rows);
-            B = whole_rows(work, w, c.type, c.w, wrows, c.inner, c.inner);
-        }
-        a.a = A.p, a.lda = A.ld;
-        a.b = B.p, a.ldb = B.ld, a.batch_b = B.ld * c.outer;
+        a.vec = (pieces(c.y, c.outer, size) && (!c.z || pieces(c.z, c.outer, size)) ? som::kVecOut
+                                                                                    : 0) |
+                (c.bias && pieces(c.bias, c.outer, size) ? som::kVecBias : 0) |
+                (c.residual && pieces(c.residual, c.ldr, size) ? som::kVecResidual : 0);
+        x.p = c.x, x.rows = c.gather ? c.n : rows, x.cols = c.inner, x.ld = c.ldx;
+        x.list = &a.list, x.per = c.k, x.listed = rows;
+        w.p = c.w, w.rows = (int64_t)c.outer * std::max(1, c.experts);
+        w.cols = c.inner, w.ld = c.inner;
+        product.place(work, x, w);
     }
 };
 
 struct LinearBackward {
-    SideCopy x, w, dz;
+    SideRows x, w, dz;
     Product input, weight;
     som::SumsArgs sums{};
     bool has_input, has_weight;
     LinearBackward(const som_linear_call &c, Carver &work) {
         const int size = som::type_size(c.type);
         const int64_t rows = c.experts ? c.n * c.k : c.n;
-        const int64_t xrows = c.gather ? c.n : rows;
-        const int64_t wrows = (int64_t)c.outer * std::max(1, c.experts);
+        const int32_t *const offsets = c.experts ? c.offsets : nullptr;
         has_input = c.dx != nullptr;
         has_weight = c.dw != nullptr;
-        const Operand Z = whole_rows(work, dz, c.type, c.dy, rows, c.outer, c.lddy,
-                                     c.activation != SOM_ACT_NONE ? c.z : nullptr, c.activation);
+        dz.p = c.dy, dz.rows = rows, dz.cols = c.outer, dz.ld = c.lddy;
+        if (c.activation != SOM_ACT_NONE) dz.make_copy(work, c.type, c.z, c.activation);
         if (has_input) {
-            const Operand W = whole_rows(work, w, c.type, c.w, wrows, c.inner, c.inner);
             ProductArgs &a = input.a;
             a.mode = som::kInput;
             a.type = c.type;
             a.m = rows, a.n = c.inner, a.k = c.outer;
-            a.offsets = c.experts ? c.offsets : nullptr;
+            a.offsets = offsets;
             a.experts = c.experts, a.per = 1;
-            a.a = Z.p, a.lda = Z.ld;
-            a.b = W.p, a.ldb = W.ld, a.batch_b = W.ld * c.outer;
             a.y = c.dx;
             a.slope = c.slope_z, a.activation = c.slope_activation;
-            a.vec = (four(c.dx, c.inner, size) ? som::kVecOut : 0) |
-                    (c.slope_z && four(c.slope_z, c.inner, size) ? som::kVecSlope : 0);
-            input.place(work);
+            a.vec = (pieces(c.dx, c.inner, size) ? som::kVecOut : 0) |
+                    (c.slope_z && pieces(c.slope_z, c.inner, size) ? som::kVecSlope : 0);
+            w.p = c.w, w.rows = (int64_t)c.outer * std::max(1, c.experts);
+            w.cols = c.inner, w.ld = c.inner;
+            input.place(work, dz, w);
         }
         if (has_weight) {
             ProductArgs &a = weight.a;
             a.mode = som::kWeight;
             a.type = c.type;
             a.m = c.outer, a.n = c.inner, a.k = rows;
-            a.offsets = c.experts ? c.offsets : nullptr;
+            a.offsets = offsets;
             a.experts = c.experts, a.per = c.k;
             a.list = c.experts && c.gather ? c.order : nullptr;
-            const Operand X = whole_rows(work, x, c.type, c.x, xrows, c.inner, c.ldx, nullptr, 0,
-                                         &a.list, c.k, rows);
-            a.a = Z.p, a.lda = Z.ld;
-            a.b = X.p, a.ldb = X.ld;
             a.y = c.dw;
-            a.vec = four(c.dw, c.inner, size) ? som::kVecOut : 0;
-            weight.place(work);
+            a.vec = pieces(c.dw, c.inner, size) ? som::kVecOut : 0;
+            x.p = c.x, x.rows = c.gather ? c.n : rows, x.cols = c.inner, x.ld = c.ldx;
+            x.list = &a.list, x.per = c.k, x.listed = rows;
+            weight.place(work, dz, x);
         }
         if (c.dbias) {
             sums.type = c.type;
-            sums.src = Z.p;
-            sums.rows = rows, sums.cols = c.outer, sums.ld = Z.ld;
-            sums.offsets = c.experts ? c.offsets : nullptr;
+            sums.src = dz.p;
+            sums.rows = rows, sums.cols = c.outer, sums.ld = dz.ld;
+            sums.offsets = offsets;
             sums.experts = c.experts;
             sums.out = c.dbias;
             sums.partial = work.take<float>((uint64_t)som::sums_partial(sums) * 4);
@@ -328,8 +341,8 @@ som_status work_ok(const Carver &need, const som_linear_call &c) {
     return SOM_OK;
 }
 
-hipError_t run_copy(const SideCopy &c, hipStream_t s) {
-    return c.needed ? som::launch_rows_copy(c.rows, s) : hipSuccess;
+hipError_t run_copy(const SideRows &side, hipStream_t s) {
+    return side.copied ? som::launch_rows_copy(side.copy, s) : hipSuccess;
 }
 
 }  // namespace
@@ -397,18 +410,14 @@ som_status som_linear_backward(const som_linear_call *c) {
     LinearBackward b(*c, work);
     if (c->n == 0) {   // no rows: nothing to copy, dx is empty, the sums are 0
         b.has_input = false;
-        b.dz.needed = b.x.needed = false;
+        b.dz.copied = b.x.copied = b.w.copied = false;
         if (b.has_weight) b.weight.plan.splits = 1;
     }
     hipError_t e = run_copy(b.dz, s);
-    if (e == hipSuccess && b.has_input) {
-        e = run_copy(b.w, s);
-        if (e == hipSuccess) e = launch_product(b.input.a, b.input.plan, s);
-    }
-    if (e == hipSuccess && b.has_weight) {
-        e = run_copy(b.x, s);
-        if (e == hipSuccess) e = launch_product(b.weight.a, b.weight.plan, s);
-    }
+    if (e == hipSuccess) e = run_copy(b.w, s);
+    if (e == hipSuccess) e = run_copy(b.x, s);
+    if (e == hipSuccess && b.has_input) e = launch_product(b.input.a, b.input.plan, s);
+    if (e == hipSuccess && b.has_weight) e = launch_product(b.weight.a, b.weight.plan, s);
     if (e == hipSuccess && c->dbias) e = som::launch_sums(b.sums, s);
     return from_hip(e);
 }

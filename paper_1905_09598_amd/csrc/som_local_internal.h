@@ -124,7 +124,8 @@ struct ProductPlan {
     int32_t tile;         // rows and columns of a tile: 256, 128 or 64; of few rows, rows: 16 or 64
     int32_t waves;        // few rows: waves of a workgroup; otherwise 0
     int32_t splits;       // parts of the contraction
-    bool aligned;         // few rows: both sides lie in whole 16-byte pieces
+    bool aligned;         // both sides lie in whole 16-byte pieces
+    double time;          // estimated microseconds
     int64_t partial_floats;
 };
 
@@ -224,7 +225,7 @@ struct AdamwArgs {
 };
 hipError_t launch_adamw(const AdamwArgs &a, bool eight, hipStream_t stream);
 
-ProductPlan plan_product(const ProductArgs &a, int num_cus);
+ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus);
 // One per element type (som_product_*.hip).
 hipError_t launch_product_f32(ProductArgs a, const ProductPlan &p, hipStream_t stream);
 hipError_t launch_product_bf16(ProductArgs a, const ProductPlan &p, hipStream_t stream);

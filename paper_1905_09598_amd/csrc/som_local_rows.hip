@@ -61,11 +61,11 @@ __global__ __launch_bounds__(kThreads) void rows_copy_kernel(RowsArgs a, int vec
 }
 
 // Sums of rows, in fp32 and in a fixed order: a workgroup takes 32 pieces of 16
-// bytes of up to kSumRows rows of one expert (all of them if DIRECT), 32 rows at
-// a time, joins its 32 sums a column through LDS, and writes them, or parts that
-// join_sums_kernel adds up.
-constexpr int kSumThreads = 1024, kSumPieces = 32, kSumLanes = kSumThreads / kSumPieces;
-constexpr int kSumRows = 512;
+// bytes of up to kSumRows rows of one expert (all of them if DIRECT), eight rows
+// at a time, joins its eight sums a column through LDS, and writes them, or parts
+// that join_sums_kernel adds up, eight at a time too.
+constexpr int kSumThreads = 256, kSumPieces = 32, kSumLanes = kSumThreads / kSumPieces;
+constexpr int kSumRows = 128;
 
 template <typename T, bool DIRECT>
 __global__ __launch_bounds__(kSumThreads) void sums_kernel(SumsArgs a, int vec) {
@@ -114,18 +114,27 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(SumsArgs a, int vec) 
 }
 
 template <typename T>
-__global__ __launch_bounds__(kThreads) void join_sums_kernel(SumsArgs a) {
-    const int64_t col = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int e = blockIdx.y;
-    if (col >= a.cols) return;
+__global__ __launch_bounds__(kSumThreads) void join_sums_kernel(SumsArgs a) {
+    constexpr int kCols = kSumThreads / kSumLanes;
+    __shared__ float part[kSumLanes][kCols];
+    const int c = threadIdx.x % kCols, lane = threadIdx.x / kCols, e = blockIdx.y;
+    const int64_t col = (int64_t)blockIdx.x * kCols + c;
     int64_t first = 0, count = (a.rows + kSumRows - 1) / kSumRows;
     if (a.offsets) {
         first = a.offsets[e] / kSumRows + e;
         count = (a.offsets[e + 1] - a.offsets[e] + kSumRows - 1) / kSumRows;
     }
     float v = 0.f;
-    for (int64_t p = 0; p < count; ++p) v += a.partial[(first + p) * a.cols + col];
-    static_cast<T *>(a.out)[e * a.cols + col] = (T)v;
+    if (col < a.cols) {
+#pragma unroll 4
+        for (int64_t p = lane; p < count; p += kSumLanes) v += a.partial[(first + p) * a.cols + col];
+    }
+    part[lane][c] = v;
+    __syncthreads();
+    if (lane == 0 && col < a.cols) {
+        for (int l = 1; l < kSumLanes; ++l) v += part[l][c];
+        static_cast<T *>(a.out)[e * a.cols + col] = (T)v;
+    }
 }
 
 // 16 bytes of a document's row a thread.
@@ -225,10 +234,9 @@ hipError_t launch_rows_copy(const RowsArgs &a, hipStream_t stream) {
     });
 }
 
-// One pass where an expert has few rows: the sums of 32 rows at a time then take
-// no longer than the second launch.
+// One pass where an expert has few rows.
 static bool sums_direct(const SumsArgs &a) {
-    return a.rows <= (int64_t)(a.offsets ? a.experts : 1) * 1024;
+    return a.rows <= (int64_t)(a.offsets ? a.experts : 1) * 32;
 }
 static int64_t sums_parts(const SumsArgs &a) {
     return a.offsets ? a.rows / kSumRows + a.experts : (a.rows + kSumRows - 1) / kSumRows;
@@ -245,14 +253,15 @@ hipError_t launch_sums(const SumsArgs &a, hipStream_t stream) {
     if (high > 65535 || experts > 65535) return hipErrorInvalidValue;
     const int vec = whole_pieces(a.src, a.ld, size);
     const dim3 grid((unsigned)wide, (unsigned)high);
-    const dim3 join((unsigned)((a.cols + kThreads - 1) / kThreads), experts);
+    constexpr int kCols = kSumThreads / kSumLanes;
+    const dim3 join((unsigned)((a.cols + kCols - 1) / kCols), experts);
     return by_type(a.type, [&](auto t) {
         using T = decltype(t);
         if (direct) {
             sums_kernel<T, true><<<grid, kSumThreads, 0, stream>>>(a, vec);
         } else {
             sums_kernel<T, false><<<grid, kSumThreads, 0, stream>>>(a, vec);
-            join_sums_kernel<T><<<join, kThreads, 0, stream>>>(a);
+            join_sums_kernel<T><<<join, kSumThreads, 0, stream>>>(a);
         }
     });
 }

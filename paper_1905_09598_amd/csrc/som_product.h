@@ -22,8 +22,8 @@
 //   across  contraction step s holds its columns in units of 16, in the order
 //           u ^ f(s): the steps that are read together lie on different banks.
 //           16-bit types are transposed by the reading instruction.
-// Rows beyond C are read from its last row and not stored; the contraction is
-// filled up from 16 bytes of zeros.
+// Rows beyond C are read from its last row, columns from its first, and not
+// stored; the contraction is filled up from 16 bytes of zeros.
 #pragma once
 
 #include "som_local_internal.h"
@@ -73,7 +73,12 @@ __device__ inline f4 multiply<float>(i4 b, i4 a, f4 c) {
 // ROWS rows (or columns) of a tile, loaded by WAVES waves.  A lane's source is a
 // 32-bit offset from a base that all lanes share and that moves from slab to
 // slab (the launcher sees to it that the offsets fit).
-template <typename T, bool ACROSS, int ROWS, int WAVES>
+//
+// DMA: pieces go straight to LDS; they have to be whole and 16-byte aligned (the
+// columns of an across side a multiple of a piece, so that none crosses a row's
+// end).  Without, rows may begin anywhere: pieces go through registers, and those
+// that cross a row's end are read element by element.
+template <typename T, bool ACROSS, bool DMA, int ROWS, int WAVES>
 struct Side {
     static constexpr int kElems = 16 / sizeof(T);           // elements of a 16-byte piece
     static constexpr int kSlab = 128 / sizeof(T);           // contraction of a slab
@@ -86,6 +91,7 @@ struct Side {
     const char *base;
     uint32_t off[kLoads];
     int64_t step;             // bytes from slab to slab
+    i4 held[DMA ? 1 : kLoads];
 
     // What the units of contraction step s are exchanged with.
     static __device__ int twist(int s) {
@@ -101,12 +107,12 @@ struct Side {
         const int q = place(j);
         return ACROSS ? q / kPieces : ((q & 7) ^ (q >> 3 & 7)) * kElems;
     }
-    // across: the column it holds, the last whole piece's beyond the matrix.
+    // across: the column it holds, another one beyond the matrix.
     static __device__ int64_t column(int j, int64_t col0, int64_t cols) {
         const int q = place(j), s = q / kPieces, at = q % kPieces;
         const int unit = (at / kUnitPieces) ^ twist(s);
         const int64_t c = col0 + unit * 16 + (at % kUnitPieces) * kElems;
-        return c < cols ? c : (cols - 1) / kElems * kElems;
+        return c < cols ? c : 0;
     }
 
     // Rows row0 .. of a side of `rows` rows whose element (r, c) is p[r * ld + c]
@@ -129,19 +135,43 @@ struct Side {
         }
     }
 
-    // Load the next slab into `lds`.  CHECK: `left` contraction indices are left, the
-    // rest are zeros.
+    // Load the next slab, with DMA into `lds`.  CHECK: `left` contraction indices are
+    // left, the rest are zeros.  across: columns col0 .. of `cols`.
     template <bool CHECK>
-    __device__ void load(char *lds, int64_t left) {
+    __device__ void load(char *lds, int64_t left, int64_t col0, int64_t cols) {
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const char *from = base + off[j];
-            if (CHECK && index(j) >= left) from = reinterpret_cast<const char *>(&kZeros);
-            __builtin_amdgcn_global_load_lds((GlobalPtr)from,
-                                             (LdsPtr)(lds + (wave * kLoads + j) * 1024), 16, 0, 0);
+            if (DMA) {
+                if (CHECK && index(j) >= left) from = reinterpret_cast<const char *>(&kZeros);
+                __builtin_amdgcn_global_load_lds((GlobalPtr)from,
+                                                 (LdsPtr)(lds + (wave * kLoads + j) * 1024), 16, 0,
+                                                 0);
+            } else {
+                int64_t here = kElems;   // elements of the piece that are there
+                if (ACROSS) here = cols - column(j, col0, cols);
+                if (CHECK && ACROSS && index(j) >= left) here = 0;
+                if (CHECK && !ACROSS) here = left - index(j);
+                if (here >= kElems) {
+                    __builtin_memcpy(&held[j], __builtin_assume_aligned(from, sizeof(T)), 16);
+                } else {
+                    typedef T Vec __attribute__((ext_vector_type(kElems)));
+                    Vec v;
+#pragma unroll
+                    for (int e = 0; e < kElems; ++e)
+                        v[e] = e < here ? reinterpret_cast<const T *>(from)[e] : (T)0.f;
+                    held[j] = __builtin_bit_cast(i4, v);
+                }
+            }
         }
         base += step;
+    }
+    // Without DMA: what was loaded last, into `lds`.
+    __device__ void store(char *lds) const {
+#pragma unroll
+        for (int j = 0; j < (DMA ? 0 : kLoads); ++j)
+            *reinterpret_cast<i4 *>(lds + place(j) * 16) = held[j];
     }
 
     // An across side whose contraction step s is the matrix's row list[s] / per:
@@ -177,7 +207,7 @@ struct Fragments {
             at = (r0 + i) * 128 + ((g ^ (i & 7)) << 4);
         } else {
             const int s = sizeof(T) == 2 ? 8 * g + (i >> 2) : 4 * g;
-            const int unit = r0 / 16 ^ Side<T, true, ROWS, ROWS / 8>::twist(s);
+            const int unit = r0 / 16 ^ Side<T, true, true, ROWS, ROWS / 8>::twist(s);
             at = s * kRow + unit * 16 * (int)sizeof(T) + (sizeof(T) == 2 ? (i & 3) * 8 : i * 4);
         }
     }
@@ -353,11 +383,11 @@ struct Epilogue {
 //   multiply the second half
 // so that the matrix cores always have fragments in hand, and a load has a slab's
 // time to arrive.
-template <typename T, int MODE, bool LISTED, int TM, int TN, int WM, int WN>
+template <typename T, int MODE, bool LISTED, bool DMA, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) {
     constexpr bool kAcrossA = MODE == kWeight, kAcrossB = MODE != kForward;
-    using SideA = Side<T, kAcrossA, TM, WM * WN>;
-    using SideB = Side<T, kAcrossB, TN, WM * WN>;
+    using SideA = Side<T, kAcrossA, DMA, TM, WM * WN>;
+    using SideB = Side<T, kAcrossB, DMA, TN, WM * WN>;
     constexpr int kTileM = TM / WM, kTileN = TN / WN;    // of a wave
     constexpr int FM = kTileM / 16, FN = kTileN / 16;    // its fragments
     constexpr int kSlab = SideA::kSlab;
@@ -433,8 +463,12 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
         const auto load = [&](auto check, int64_t s) {
             char *to = lds + (s & 1) * kBytes;
             const int64_t left = k_end - k0 - s * kSlab;
-            sa.template load<decltype(check)::value>(to, left);
-            sb.template load<decltype(check)::value>(to + TM * 128, left);
+            sa.template load<decltype(check)::value>(to, left, row0, row_end);
+            sb.template load<decltype(check)::value>(to + TM * 128, left, col0, a.n);
+        };
+        const auto store = [&](int64_t s) {
+            sa.store(lds + (s & 1) * kBytes);
+            sb.store(lds + (s & 1) * kBytes + TM * 128);
         };
         i4 fa[2][FM], fb[2][FN];
         const auto read = [&](int64_t s, auto half) {
@@ -465,7 +499,8 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
                 times(Int<1>());
                 return;
             }
-            wait_loads<0>();                     // the next slab has landed
+            if (DMA) wait_loads<0>();            // the next slab has landed
+            else store(s + 1);
             __syncthreads();                     // for everyone; this one is no longer read
             if (k == 2) load(Int<0>(), s + 2);
             if (k == 1) load(Int<1>(), s + 2);
@@ -475,13 +510,14 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
         };
         follow(0);
         load(Int<1>(), 0);
+        store(0);
         if (slabs > 1) {
             follow(1);
             load(Int<1>(), 1);
         }
         // all but the second slab's loads have landed
-        if (slabs > 1 && !LISTED) wait_loads<SideA::kLoads + SideB::kLoads>();
-        else wait_loads<0>();
+        if (DMA && slabs > 1 && !LISTED) wait_loads<SideA::kLoads + SideB::kLoads>();
+        else if (DMA) wait_loads<0>();
         __syncthreads();
         read(0, Int<0>());
         int64_t s = 0;
@@ -672,7 +708,7 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(ProductArgs a, int by_
     }
 }
 
-template <typename T, int MODE, bool LISTED, int TM, int TN, int WM, int WN>
+template <typename T, int MODE, bool LISTED, bool DMA, int TM, int TN, int WM, int WN>
 hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
     const int64_t tn = (a.n + TN - 1) / TN;
     const int64_t tm = MODE == kWeight ? (a.m + TM - 1) / TM * (a.offsets ? a.experts : 1)
@@ -680,7 +716,7 @@ hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
                                        : (a.m + TM - 1) / TM;
     if (tm * tn > INT32_MAX) return hipErrorInvalidValue;
     constexpr int kLds = 2 * (TM + TN) * 128;
-    const auto kernel = product_kernel<T, MODE, LISTED, TM, TN, WM, WN>;
+    const auto kernel = product_kernel<T, MODE, LISTED, DMA, TM, TN, WM, WN>;
     if (kLds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
@@ -698,10 +734,13 @@ hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
 // LISTED: side B's rows (weight) are named by the list.
 template <typename T, int MODE, bool LISTED>
 hipError_t launch_mode(const ProductArgs &a, const ProductPlan &p, hipStream_t stream) {
+    if (!p.aligned)
+        return p.tile == 128 ? launch_tiles<T, MODE, LISTED, false, 128, 128, 2, 2>(a, stream)
+                             : launch_tiles<T, MODE, LISTED, false, 64, 64, 2, 2>(a, stream);
     switch (p.tile) {
-        case 256: return launch_tiles<T, MODE, LISTED, 256, 256, 2, 4>(a, stream);
-        case 128: return launch_tiles<T, MODE, LISTED, 128, 128, 2, 2>(a, stream);
-        default: return launch_tiles<T, MODE, LISTED, 64, 64, 2, 2>(a, stream);
+        case 256: return launch_tiles<T, MODE, LISTED, true, 256, 256, 2, 4>(a, stream);
+        case 128: return launch_tiles<T, MODE, LISTED, true, 128, 128, 2, 2>(a, stream);
+        default: return launch_tiles<T, MODE, LISTED, true, 64, 64, 2, 2>(a, stream);
     }
 }
 

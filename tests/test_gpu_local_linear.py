@@ -214,9 +214,8 @@ def test_refusals():
     with pytest.raises(ValueError):
         local.linear_backward(dy[:, :8], x, w)
     # the C entry: a workspace that is too small, and arrays past their allocation
-    call = local._dense_call(torch.zeros(300, 33, device="cuda"), torch.zeros(40, 33, device="cuda"),
-                             "none")
-    y = torch.zeros(300, 40, device="cuda")
+    x, w, y = (torch.zeros(*s, device="cuda") for s in ((40, 20000), (24, 20000), (40, 24)))
+    call = local._dense_call(x, w, "none")     # a contraction that is split
     call.y = y.data_ptr()
     assert som.STATUS[local.lib().som_linear(call)] == "SOM_E_ARG"
     call.n = 1 << 38
