@@ -16,14 +16,15 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Four neighbours of a packed array, `left` of them there; packed arrays of
-// 16-bit types may begin at any element.
+// Four neighbours of a packed array, `left` of them there.  Arrays begin at any
+// element: the hardware takes 16 bytes at any address.
 template <typename T>
 __device__ inline void read_typed(const void *p, int64_t at, int left, float (&v)[4]) {
+    typedef T Vec __attribute__((ext_vector_type(4)));
     const T *from = static_cast<const T *>(p) + at;
-    if (left >= 4 && reinterpret_cast<uintptr_t>(from) % (4 * sizeof(T)) == 0) {
-        typedef T t4 __attribute__((ext_vector_type(4)));
-        const t4 q = *reinterpret_cast<const t4 *>(from);
+    if (left >= 4) {
+        Vec q;
+        __builtin_memcpy(&q, __builtin_assume_aligned(from, sizeof(T)), sizeof(Vec));
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = (float)q[e];
     } else {
@@ -33,13 +34,13 @@ __device__ inline void read_typed(const void *p, int64_t at, int left, float (&v
 }
 template <typename T>
 __device__ inline void write_typed(void *p, int64_t at, int left, const float (&v)[4]) {
+    typedef T Vec __attribute__((ext_vector_type(4)));
     T *to = static_cast<T *>(p) + at;
-    if (left >= 4 && reinterpret_cast<uintptr_t>(to) % (4 * sizeof(T)) == 0) {
-        typedef T t4 __attribute__((ext_vector_type(4)));
-        t4 q;
+    if (left >= 4) {
+        Vec q;
 #pragma unroll
         for (int e = 0; e < 4; ++e) q[e] = (T)v[e];
-        *reinterpret_cast<t4 *>(to) = q;
+        __builtin_memcpy(__builtin_assume_aligned(to, sizeof(T)), &q, sizeof(Vec));
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)

@@ -26,8 +26,12 @@ ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus) {
     if (a.mode == kForward && a.m <= 16 * experts) {
         best.tile = 16;
         const int64_t groups = (a.n + 15) / 16 * std::min(a.m, a.m / best.tile + experts);
-        // sixteen waves where four would leave the chip short of loads in flight
-        best.waves = groups * 4 < (int64_t)num_cus * 16 && a.k >= 8 * slab ? 16 : 4;
+        // as few waves to a workgroup as keep the chip's loads in flight (16 waves of
+        // four slabs a compute unit), so that all workgroups run at once
+        best.waves = 4;
+        while (best.waves < 16 && groups * best.waves < (int64_t)num_cus * 16 &&
+               a.k > best.waves * slab)
+            best.waves *= 2;
         best.splits = 1;
         return best;
     }
@@ -174,11 +178,6 @@ struct SideRows {
     }
 };
 
-// Rows that can be reached 16 bytes at a time.
-bool pieces(const void *p, int64_t ld, int size) {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * size % 16 == 0;
-}
-
 hipError_t launch_product(const ProductArgs &a, const ProductPlan &plan, hipStream_t s) {
     switch (a.type) {
         case SOM_F32: return som::launch_product_f32(a, plan, s);
@@ -225,7 +224,6 @@ struct LinearForward {
     SideRows x, w;
     Product product;
     LinearForward(const som_linear_call &c, Carver &work) {
-        const int size = som::type_size(c.type);
         const int64_t rows = c.experts ? c.n * c.k : c.n;
         ProductArgs &a = product.a;
         a.mode = som::kForward;
@@ -238,10 +236,6 @@ struct LinearForward {
         a.bias = c.bias;
         a.residual = c.residual, a.ldr = c.ldr;
         a.y = c.y, a.z = c.z;
-        a.vec = (pieces(c.y, c.outer, size) && (!c.z || pieces(c.z, c.outer, size)) ? som::kVecOut
-                                                                                    : 0) |
-                (c.bias && pieces(c.bias, c.outer, size) ? som::kVecBias : 0) |
-                (c.residual && pieces(c.residual, c.ldr, size) ? som::kVecResidual : 0);
         x.p = c.x, x.rows = c.gather ? c.n : rows, x.cols = c.inner, x.ld = c.ldx;
         x.list = &a.list, x.per = c.k, x.listed = rows;
         w.p = c.w, w.rows = (int64_t)c.outer * std::max(1, c.experts);
@@ -256,7 +250,6 @@ struct LinearBackward {
     som::SumsArgs sums{};
     bool has_input, has_weight;
     LinearBackward(const som_linear_call &c, Carver &work) {
-        const int size = som::type_size(c.type);
         const int64_t rows = c.experts ? c.n * c.k : c.n;
         const int32_t *const offsets = c.experts ? c.offsets : nullptr;
         has_input = c.dx != nullptr;
@@ -272,8 +265,6 @@ struct LinearBackward {
             a.experts = c.experts, a.per = 1;
             a.y = c.dx;
             a.slope = c.slope_z, a.activation = c.slope_activation;
-            a.vec = (pieces(c.dx, c.inner, size) ? som::kVecOut : 0) |
-                    (c.slope_z && pieces(c.slope_z, c.inner, size) ? som::kVecSlope : 0);
             w.p = c.w, w.rows = (int64_t)c.outer * std::max(1, c.experts);
             w.cols = c.inner, w.ld = c.inner;
             input.place(work, dz, w);
@@ -287,7 +278,6 @@ struct LinearBackward {
             a.experts = c.experts, a.per = c.k;
             a.list = c.experts && c.gather ? c.order : nullptr;
             a.y = c.dw;
-            a.vec = pieces(c.dw, c.inner, size) ? som::kVecOut : 0;
             x.p = c.x, x.rows = c.gather ? c.n : rows, x.cols = c.inner, x.ld = c.ldx;
             x.list = &a.list, x.per = c.k, x.listed = rows;
             weight.place(work, dz, x);

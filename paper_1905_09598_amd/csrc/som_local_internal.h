@@ -88,9 +88,6 @@ __device__ inline int expert_of(const int32_t *offsets, int experts, int tile, i
     return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// Which of a product's arrays can be reached four elements at a time.
-enum : int32_t { kVecOut = 1, kVecBias = 2, kVecResidual = 4, kVecSlope = 8 };
-
 // The tiles' kernels reach an operand's elements by 32-bit offsets within a tile's
 // rows, and within a whole listed matrix (som_product.h).
 constexpr int64_t kMaxWidth = 4000000;
@@ -105,7 +102,7 @@ inline bool tile_reaches(int64_t ld, int size) { return ld * size * 256 < ((int6
 // row r of A is A's row list[r] / per; weight, row s of B is B's row
 // list[s] / per.  Rows past offsets[experts] are not touched.
 struct ProductArgs {
-    int32_t mode, type, activation, vec;
+    int32_t mode, type, activation;
     const void *a, *b;
     int64_t lda, ldb, batch_b;
     int64_t m, n, k;
@@ -121,7 +118,7 @@ struct ProductArgs {
 
 // How a product runs.
 struct ProductPlan {
-    int32_t tile;         // rows and columns of a tile: 256, 128 or 64; of few rows, rows: 16 or 64
+    int32_t tile;         // rows and columns of a tile: 256, 128 or 64; of few rows, rows: 16
     int32_t waves;        // few rows: waves of a workgroup; otherwise 0
     int32_t splits;       // parts of the contraction
     bool aligned;         // both sides lie in whole 16-byte pieces

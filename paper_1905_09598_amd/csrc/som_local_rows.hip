@@ -10,12 +10,14 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// N neighbouring values of a row, `left` of them there.
+// N neighbouring values of a row, `left` of them there.  Rows begin at any
+// element: the hardware takes 16 bytes at any address.
 template <typename T, int N>
-__device__ inline void read_some(const T *p, int64_t left, bool vec, float (&v)[N]) {
-    if (vec && left >= N) {
-        typedef T tn __attribute__((ext_vector_type(N)));
-        const tn q = *reinterpret_cast<const tn *>(p);
+__device__ inline void read_some(const T *p, int64_t left, float (&v)[N]) {
+    typedef T Vec __attribute__((ext_vector_type(N)));
+    if (left >= N) {
+        Vec q;
+        __builtin_memcpy(&q, __builtin_assume_aligned(p, sizeof(T)), sizeof(Vec));
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = (float)q[e];
     } else {
@@ -24,13 +26,13 @@ __device__ inline void read_some(const T *p, int64_t left, bool vec, float (&v)[
     }
 }
 template <typename T, int N>
-__device__ inline void write_some(T *p, int64_t left, bool vec, const float (&v)[N]) {
-    if (vec && left >= N) {
-        typedef T tn __attribute__((ext_vector_type(N)));
-        tn q;
+__device__ inline void write_some(T *p, int64_t left, const float (&v)[N]) {
+    typedef T Vec __attribute__((ext_vector_type(N)));
+    if (left >= N) {
+        Vec q;
 #pragma unroll
         for (int e = 0; e < N; ++e) q[e] = (T)v[e];
-        *reinterpret_cast<tn *>(p) = q;
+        __builtin_memcpy(__builtin_assume_aligned(p, sizeof(T)), &q, sizeof(Vec));
     } else {
 #pragma unroll
         for (int e = 0; e < N; ++e)
@@ -38,10 +40,8 @@ __device__ inline void write_some(T *p, int64_t left, bool vec, const float (&v)
     }
 }
 
-enum { kVecSrc = 1, kVecZ = 2, kVecDout = 1, kVecRows = 2, kVecRes = 4 };
-
 template <typename T>
-__global__ __launch_bounds__(kThreads) void rows_copy_kernel(RowsArgs a, int vec) {
+__global__ __launch_bounds__(kThreads) void rows_copy_kernel(RowsArgs a) {
     constexpr int N = 16 / sizeof(T);
     const int64_t pieces = a.ldd / N;   // of a row; ldd is a multiple of N
     const int64_t q = (int64_t)blockIdx.x * kThreads + threadIdx.x;
@@ -50,14 +50,13 @@ __global__ __launch_bounds__(kThreads) void rows_copy_kernel(RowsArgs a, int vec
     float v[N], z[N];
     const int64_t from = a.list ? a.list[row] : row;
     read_some<T, N>(static_cast<const T *>(a.src) + (a.list ? from / a.per : from) * a.lds + col,
-                    from < 0 ? 0 : a.cols - col, vec & kVecSrc, v);
+                    from < 0 ? 0 : a.cols - col, v);
     if (a.z) {
-        read_some<T, N>(static_cast<const T *>(a.z) + row * a.ldz + col, a.cols - col, vec & kVecZ,
-                        z);
+        read_some<T, N>(static_cast<const T *>(a.z) + row * a.ldz + col, a.cols - col, z);
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = col + e < a.cols ? v[e] * activation_slope(z[e], a.activation) : 0.f;
     }
-    write_some<T, N>(static_cast<T *>(a.dst) + row * a.ldd + col, N, true, v);
+    write_some<T, N>(static_cast<T *>(a.dst) + row * a.ldd + col, N, v);
 }
 
 // Sums of rows, in fp32 and in a fixed order: a workgroup takes 32 pieces of 16
@@ -68,7 +67,7 @@ constexpr int kSumThreads = 256, kSumPieces = 32, kSumLanes = kSumThreads / kSum
 constexpr int kSumRows = 128;
 
 template <typename T, bool DIRECT>
-__global__ __launch_bounds__(kSumThreads) void sums_kernel(SumsArgs a, int vec) {
+__global__ __launch_bounds__(kSumThreads) void sums_kernel(SumsArgs a) {
     constexpr int N = 16 / sizeof(T);
     __shared__ float part[kSumLanes][kSumPieces * N + 4];
     const int piece = threadIdx.x % kSumPieces, lane = threadIdx.x / kSumPieces;
@@ -95,7 +94,7 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(SumsArgs a, int vec) 
 #pragma unroll 4
         for (int64_t r = first + lane; r < end; r += kSumLanes) {
             float v[N];
-            read_some<T, N>(static_cast<const T *>(a.src) + r * a.ld + col, left, vec, v);
+            read_some<T, N>(static_cast<const T *>(a.src) + r * a.ld + col, left, v);
 #pragma unroll
             for (int c = 0; c < N; ++c) sum[c] += v[c];
         }
@@ -139,7 +138,7 @@ __global__ __launch_bounds__(kSumThreads) void join_sums_kernel(SumsArgs a) {
 
 // 16 bytes of a document's row a thread.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a, int vec) {
+__global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a) {
     constexpr int N = 16 / sizeof(T);
     const int64_t pieces = (a.width + N - 1) / N;
     const int64_t q = (int64_t)blockIdx.x * kThreads + threadIdx.x;
@@ -152,8 +151,7 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a, int ve
         const int p = a.place[i * a.k + j];
         const float w = a.weight ? a.weight[i * a.k + j] : 1.f;
         if (p >= 0) {
-            read_some<T, N>(static_cast<const T *>(a.y) + p * a.width + col, left, vec & kVecRows,
-                            y);
+            read_some<T, N>(static_cast<const T *>(a.y) + p * a.width + col, left, y);
 #pragma unroll
             for (int e = 0; e < N; ++e) sum[e] = fmaf(w, y[e], sum[e]);
         } else if (w != w) {
@@ -162,18 +160,17 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a, int ve
         }
     }
     if (a.residual) {
-        read_some<T, N>(static_cast<const T *>(a.residual) + i * a.ldr + col, left, vec & kVecRes,
-                        first);
+        read_some<T, N>(static_cast<const T *>(a.residual) + i * a.ldr + col, left, first);
 #pragma unroll
         for (int e = 0; e < N; ++e) sum[e] += first[e];
     }
-    write_some<T, N>(static_cast<T *>(a.out) + i * a.width + col, left, vec & kVecRows, sum);
+    write_some<T, N>(static_cast<T *>(a.out) + i * a.width + col, left, sum);
 }
 
 // One choice of a document a wave: its row of dy, and the product of the two
 // rows, summed over the lanes in a fixed order.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void combine_backward_kernel(CombineArgs a, int vec) {
+__global__ __launch_bounds__(kThreads) void combine_backward_kernel(CombineArgs a) {
     constexpr int N = 16 / sizeof(T);
     const int lane = threadIdx.x & 63;
     const int64_t s = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
@@ -188,25 +185,21 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(CombineArgs 
         T *to = static_cast<T *>(a.dy) + p * a.width;
         for (int64_t col = lane * N; col < a.width; col += 64 * N) {
             float d[N], v[N];
-            read_some<T, N>(from + col, a.width - col, vec & kVecDout, d);
+            read_some<T, N>(from + col, a.width - col, d);
             if (a.dweight) {
-                read_some<T, N>(y + col, a.width - col, vec & kVecRows, v);
+                read_some<T, N>(y + col, a.width - col, v);
 #pragma unroll
                 for (int e = 0; e < N; ++e) dot = fmaf(d[e], v[e], dot);
             }
 #pragma unroll
             for (int e = 0; e < N; ++e) d[e] *= w;
-            write_some<T, N>(to + col, a.width - col, vec & kVecRows, d);
+            write_some<T, N>(to + col, a.width - col, d);
         }
     }
     if (a.dweight) {
         for (int o = 32; o; o >>= 1) dot += __shfl_xor(dot, o);
         if (lane == 0) static_cast<T *>(a.dweight)[s] = (T)dot;
     }
-}
-
-bool whole_pieces(const void *p, int64_t ld, int size) {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * size % 16 == 0;
 }
 
 template <typename F>
@@ -226,11 +219,9 @@ hipError_t launch_rows_copy(const RowsArgs &a, hipStream_t stream) {
     const int64_t pieces = a.rows * (a.ldd * size / 16);
     if (pieces == 0) return hipSuccess;
     if ((pieces + kThreads - 1) / kThreads > INT32_MAX) return hipErrorInvalidValue;
-    const int vec = (whole_pieces(a.src, a.lds, size) ? kVecSrc : 0) |
-                    (a.z && whole_pieces(a.z, a.ldz, size) ? kVecZ : 0);
     const unsigned blocks = (unsigned)((pieces + kThreads - 1) / kThreads);
     return by_type(a.type, [&](auto t) {
-        rows_copy_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a, vec);
+        rows_copy_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a);
     });
 }
 
@@ -251,16 +242,15 @@ hipError_t launch_sums(const SumsArgs &a, hipStream_t stream) {
     const int64_t high = direct ? experts : sums_parts(a);
     const int64_t wide = (a.cols * size + 16 * kSumPieces - 1) / (16 * kSumPieces);
     if (high > 65535 || experts > 65535) return hipErrorInvalidValue;
-    const int vec = whole_pieces(a.src, a.ld, size);
     const dim3 grid((unsigned)wide, (unsigned)high);
     constexpr int kCols = kSumThreads / kSumLanes;
     const dim3 join((unsigned)((a.cols + kCols - 1) / kCols), experts);
     return by_type(a.type, [&](auto t) {
         using T = decltype(t);
         if (direct) {
-            sums_kernel<T, true><<<grid, kSumThreads, 0, stream>>>(a, vec);
+            sums_kernel<T, true><<<grid, kSumThreads, 0, stream>>>(a);
         } else {
-            sums_kernel<T, false><<<grid, kSumThreads, 0, stream>>>(a, vec);
+            sums_kernel<T, false><<<grid, kSumThreads, 0, stream>>>(a);
             join_sums_kernel<T><<<join, kSumThreads, 0, stream>>>(a);
         }
     });
@@ -271,25 +261,18 @@ hipError_t launch_combine(const CombineArgs &a, hipStream_t stream) {
     const int64_t pieces = a.n * ((a.width * size + 15) / 16);
     if (pieces == 0) return hipSuccess;
     if ((pieces + kThreads - 1) / kThreads > INT32_MAX) return hipErrorInvalidValue;
-    const int vec = (whole_pieces(a.y, a.width, size) && whole_pieces(a.out, a.width, size)
-                         ? kVecRows : 0) |
-                    (a.residual && whole_pieces(a.residual, a.ldr, size) ? kVecRes : 0);
     const unsigned blocks = (unsigned)((pieces + kThreads - 1) / kThreads);
     return by_type(a.type, [&](auto t) {
-        combine_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a, vec);
+        combine_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a);
     });
 }
 
 hipError_t launch_combine_backward(const CombineArgs &a, hipStream_t stream) {
-    const int size = type_size(a.type);
     const int64_t slots = a.n * a.k;
     if (slots == 0) return hipSuccess;
-    const int vec = (whole_pieces(a.dout, a.ldd, size) ? kVecDout : 0) |
-                    ((!a.y || whole_pieces(a.y, a.width, size)) && whole_pieces(a.dy, a.width, size)
-                         ? kVecRows : 0);
     const unsigned blocks = (unsigned)((slots + kThreads / 64 - 1) / (kThreads / 64));
     return by_type(a.type, [&](auto t) {
-        combine_backward_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a, vec);
+        combine_backward_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a);
     });
 }
 

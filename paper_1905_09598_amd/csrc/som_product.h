@@ -253,22 +253,23 @@ __device__ inline void band_tile(int64_t t, int64_t tm, int64_t tn, int64_t *m, 
     *n = in / high;
 }
 
-// N neighbouring values of a row to and from memory, `left` of them there.
+// N neighbouring values of a row to and from memory, `left` of them there.  Rows
+// begin at any element: the hardware takes 16 bytes at any address.
 template <typename T, int N>
 struct Piece {
     typedef T Vec __attribute__((ext_vector_type(N)));
     Vec v;
-    __device__ void read(const T *p, int left, bool vec) {
-        if (vec && left >= N) {
-            v = *reinterpret_cast<const Vec *>(p);
+    __device__ void read(const T *p, int left) {
+        if (left >= N) {
+            __builtin_memcpy(&v, __builtin_assume_aligned(p, sizeof(T)), sizeof(Vec));
         } else {
 #pragma unroll
             for (int e = 0; e < N; ++e) v[e] = e < left ? p[e] : (T)0.f;
         }
     }
-    __device__ void write(T *p, int left, bool vec) const {
-        if (vec && left >= N) {
-            *reinterpret_cast<Vec *>(p) = v;
+    __device__ void write(T *p, int left) const {
+        if (left >= N) {
+            __builtin_memcpy(__builtin_assume_aligned(p, sizeof(T)), &v, sizeof(Vec));
         } else {
 #pragma unroll
             for (int e = 0; e < N; ++e)
@@ -332,17 +333,16 @@ struct Epilogue {
         Piece<T, N> p;
         const bool there = MODE == kForward && a.bias && left > 0;
         if (there)
-            p.read(static_cast<const T *>(a.bias) + batch * a.n + col, left, a.vec & kVecBias);
+            p.read(static_cast<const T *>(a.bias) + batch * a.n + col, left);
 #pragma unroll
         for (int e = 0; e < N; ++e) bias[e] = there ? (float)p.v[e] : 0.f;
     }
     // The row's residual (forward) or slope argument (input).
     __device__ void read(int64_t row, Piece<T, N> &extra) const {
         if (MODE == kForward && a.residual)
-            extra.read(static_cast<const T *>(a.residual) + row * a.ldr + col, left,
-                       a.vec & kVecResidual);
+            extra.read(static_cast<const T *>(a.residual) + row * a.ldr + col, left);
         if (MODE == kInput && a.slope)
-            extra.read(static_cast<const T *>(a.slope) + row * a.n + col, left, a.vec & kVecSlope);
+            extra.read(static_cast<const T *>(a.slope) + row * a.n + col, left);
     }
     __device__ void write(int64_t row, const Piece<T, N> &extra, float (&v)[N]) const {
         const int64_t at = ((MODE == kWeight ? batch * a.m : 0) + row) * a.n + col;
@@ -353,7 +353,7 @@ struct Epilogue {
             if (a.z) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) out.v[e] = (T)v[e];
-                out.write(static_cast<T *>(a.z) + at, left, a.vec & kVecOut);
+                out.write(static_cast<T *>(a.z) + at, left);
             }
             activate_all(v, a.activation);
             if (a.residual) {
@@ -371,7 +371,7 @@ struct Epilogue {
         }
 #pragma unroll
         for (int e = 0; e < N; ++e) out.v[e] = (T)v[e];
-        out.write(static_cast<T *>(a.y) + at, left, a.vec & kVecOut);
+        out.write(static_cast<T *>(a.y) + at, left);
     }
 };
 
@@ -623,83 +623,72 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a, int64_t ld) {
     }
 }
 
-// Forward product of few rows (16 R at a time): bound by one read of w.  A
-// workgroup takes 16 columns of C, its waves take the contraction's slabs in
-// turn, straight from memory into the fragments (no LDS: w is used once, x
-// comes from the caches), several slabs in flight, and join their sums through
-// LDS in order.  VEC: pieces are 16-byte aligned; otherwise they are read
-// element by element.
-template <typename T, bool VEC>
+// Forward product of few rows, 16 at a time: bound by one read of w.  A workgroup
+// takes 16 columns of C, its waves take the contraction's slabs in turn, straight
+// from memory into the fragments (no LDS: w is used once, x comes from the
+// caches), four slabs in flight, and join their sums through LDS in order.
+template <typename T, bool CHECK>
 __device__ inline i4 piece(const T *row, int64_t k, int64_t k_end) {
     constexpr int kElems = 16 / sizeof(T);
-    if (VEC) {
-        const void *from = k < k_end ? static_cast<const void *>(row + k) : &kZeros;
-        return *static_cast<const i4 *>(from);
-    }
-    typedef T te __attribute__((ext_vector_type(kElems)));
-    te v;
+    Piece<T, kElems> p;
+    if (!CHECK || k + kElems <= k_end) {
+        p.read(row + k, kElems);
+    } else {
 #pragma unroll
-    for (int e = 0; e < kElems; ++e) v[e] = k + e < k_end ? row[k + e] : (T)0.f;
-    return __builtin_bit_cast(i4, v);
+        for (int e = 0; e < kElems; ++e) p.v[e] = k + e < k_end ? row[k + e] : (T)0.f;
+    }
+    return __builtin_bit_cast(i4, p.v);
 }
 
-template <typename T, int R, int WAVES, bool VEC>
+template <typename T, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void rows_kernel(ProductArgs a, int by_row) {
-    constexpr int kElems = 16 / sizeof(T), kSlab = 128 / sizeof(T), kAhead = R == 1 ? 4 : 2;
-    __shared__ f4 part[WAVES][R][64];
+    constexpr int kElems = 16 / sizeof(T), kSlab = 128 / sizeof(T), kAhead = 4;
+    __shared__ f4 part[WAVES][64];
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
     int batch = 0;
-    int64_t row0 = (int64_t)blockIdx.y * 16 * R, row_end = a.m;
+    int64_t row0 = (int64_t)blockIdx.y * 16, row_end = a.m;
     if (a.offsets) {
         const int64_t t = blockIdx.y;
-        batch = expert_of(a.offsets, a.experts, by_row ? 0 : 16 * R, t);
+        batch = expert_of(a.offsets, a.experts, by_row ? 0 : 16, t);
         const int64_t first = a.offsets[batch];
         row_end = a.offsets[batch + 1];
-        row0 = by_row ? t : first + (t - (first / (16 * R) + batch)) * (16 * R);
-        if (row0 >= row_end || (by_row && (t - first) % (16 * R) != 0)) return;
+        row0 = by_row ? t : first + (t - (first / 16 + batch)) * 16;
+        if (row0 >= row_end || (by_row && (t - first) % 16 != 0)) return;
     }
     const int64_t col0 = (int64_t)blockIdx.x * 16;
     const T *wr = static_cast<const T *>(a.b) + batch * a.batch_b +
                   (col0 + i < a.n ? col0 + i : a.n - 1) * a.ldb;
-    const T *xr[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        int64_t row = row0 + 16 * r + i < row_end ? row0 + 16 * r + i : row_end - 1;
-        if (a.list) row = a.list[row] / a.per;
-        xr[r] = static_cast<const T *>(a.a) + row * a.lda;
-    }
-    f4 acc[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) acc[r] = f4{0.f, 0.f, 0.f, 0.f};
-    for (int64_t k = (int64_t)wave * kSlab; k < a.k; k += (int64_t)kAhead * WAVES * kSlab) {
-        i4 fw[kAhead][2], fx[kAhead][2][R];
+    int64_t xrow = row0 + i < row_end ? row0 + i : row_end - 1;
+    if (a.list) xrow = a.list[xrow] / a.per;
+    const T *xr = static_cast<const T *>(a.a) + xrow * a.lda;
+    f4 acc = {0.f, 0.f, 0.f, 0.f};
+    const auto slabs = [&](auto check, int64_t k) {
+        i4 fw[kAhead][2], fx[kAhead][2];
 #pragma unroll
         for (int s = 0; s < kAhead; ++s)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int64_t c = k + (int64_t)s * WAVES * kSlab + (h * 4 + g) * kElems;
-                fw[s][h] = piece<T, VEC>(wr, c, a.k);
-#pragma unroll
-                for (int r = 0; r < R; ++r) fx[s][h][r] = piece<T, VEC>(xr[r], c, a.k);
+                fw[s][h] = piece<T, decltype(check)::value>(wr, c, a.k);
+                fx[s][h] = piece<T, decltype(check)::value>(xr, c, a.k);
             }
 #pragma unroll
         for (int s = 0; s < kAhead; ++s)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < R; ++r)
-                    acc[r] = multiply<T>(fw[s][h], fx[s][h][r], acc[r]);
-    }
-#pragma unroll
-    for (int r = 0; r < R; ++r) part[wave][r][lane] = acc[r];
+            for (int h = 0; h < 2; ++h) acc = multiply<T>(fw[s][h], fx[s][h], acc);
+    };
+    int64_t k = (int64_t)wave * kSlab;
+    for (; k + ((kAhead - 1) * WAVES + 1) * kSlab <= a.k; k += (int64_t)kAhead * WAVES * kSlab)
+        slabs(Int<0>(), k);
+    if (k < a.k) slabs(Int<1>(), k);
+    part[wave][lane] = acc;
     __syncthreads();
-    for (int r = wave; r < R; r += WAVES) {
-        f4 v = part[0][r][lane];
+    if (wave == 0) {
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) v += part[w][r][lane];
-        const int64_t row = row0 + 16 * r + i, col = col0 + 4 * g;
+        for (int w = 1; w < WAVES; ++w) acc += part[w][lane];
+        const int64_t row = row0 + i, col = col0 + 4 * g;
         if (row < row_end && col < a.n) {
-            float u[4] = {v[0], v[1], v[2], v[3]};
+            float u[4] = {acc[0], acc[1], acc[2], acc[3]};
             const Epilogue<T, kForward, 4> end(a, col, batch);
             Piece<T, 4> extra;
             end.read(row, extra);
@@ -744,28 +733,27 @@ hipError_t launch_mode(const ProductArgs &a, const ProductPlan &p, hipStream_t s
     }
 }
 
-template <typename T, int R, int WAVES>
-hipError_t launch_rows(const ProductArgs &a, bool aligned, hipStream_t stream) {
-    const int64_t tiles = a.offsets ? a.m / (16 * R) + a.experts : (a.m + 16 * R - 1) / (16 * R);
+template <typename T, int WAVES>
+hipError_t launch_rows(const ProductArgs &a, hipStream_t stream) {
+    // a workgroup per 16 rows of an expert, or, with fewer rows than that could
+    // make, per row, of which every sixteenth of an expert goes on
+    const int64_t tiles = a.offsets ? a.m / 16 + a.experts : (a.m + 15) / 16;
     const int by_row = a.offsets && a.m < tiles;
     const int64_t high = by_row ? a.m : tiles;
     const int64_t wide = (a.n + 15) / 16;
     if (high > 65535 || wide > INT32_MAX) return hipErrorInvalidValue;
     const dim3 grid((unsigned)wide, (unsigned)high);
-    if (aligned) rows_kernel<T, R, WAVES, true><<<grid, WAVES * 64, 0, stream>>>(a, by_row);
-    else rows_kernel<T, R, WAVES, false><<<grid, WAVES * 64, 0, stream>>>(a, by_row);
+    rows_kernel<T, WAVES><<<grid, WAVES * 64, 0, stream>>>(a, by_row);
     return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_product(ProductArgs a, const ProductPlan &p, hipStream_t stream) {
     a.splits = p.splits;
-    if (p.tile <= 64 && p.waves) {
-        const bool al = p.aligned;
-        if (p.tile == 16) return p.waves == 4 ? launch_rows<T, 1, 4>(a, al, stream)
-                                              : launch_rows<T, 1, 16>(a, al, stream);
-        return p.waves == 4 ? launch_rows<T, 4, 4>(a, al, stream)
-                            : launch_rows<T, 4, 16>(a, al, stream);
+    switch (p.waves) {
+        case 4: return launch_rows<T, 4>(a, stream);
+        case 8: return launch_rows<T, 8>(a, stream);
+        case 16: return launch_rows<T, 16>(a, stream);
     }
     switch (a.mode) {
         case kForward: return launch_mode<T, kForward, false>(a, p, stream);
