@@ -8,8 +8,7 @@
  * to a constant per document, x . (w_u / tau) - |w_u|^2 / (2 tau): one product with
  * a bias (som_linear).  The k best of them and their softmax (som_route) are a
  * soft form of the map's best-matching units; with k = 1 the BMU itself.  Each
- * document is then answered by its experts (som_linear, routed) and the answers
- * are joined (som_combine).
+ * document is then answered by its experts (som_experts).
  *
  * Conventions shared with som.h: every call returns a som_status, none throws
  * or aborts; arguments are validated before any device work; device pointers
@@ -17,7 +16,7 @@
  * allocator) and stay the caller's; calls are ordered on the `stream` they are
  * given (a hipStream_t, NULL for the null stream), return after enqueueing,
  * and can be captured into a graph.  Calls keep no state of their own: work
- * memory is the caller's (som_linear_workspace says how much), must be 256-byte
+ * memory is the caller's (som_*_workspace say how much), must be 256-byte
  * aligned, and may be reused once the stream has passed the call.
  * Calls on different streams and host threads are independent.
  *
@@ -45,62 +44,99 @@ typedef enum som_activation {
 
 /* A product with its epilogue,
  *     z = x w^T + bias,    y = act(z) + residual,
- * of x (n x inner) and w (outer x inner); or, with experts > 0, routed: every
- * expert e has its own w_e and bias_e, and the rows are the n k slots of a
- * dispatch (som_dispatch) in the order of their experts, offsets[e] ..
- * offsets[e + 1] - 1 being expert e's.  With gather, x has n rows and slot row p
- * takes document order[p] / k; without, x has n k rows in that order.  y, z and
- * a residual then have n k rows too; rows from offsets[experts] on (absent
- * slots) are neither read nor written.
+ * of x (n x inner) and w (outer x inner).
  *
  * Gradients (som_linear_backward), from dy, with dz = dy act'(z):
  *     dx = dz w    dw = dz^T x    dbias = sum of dz's rows
- * (routed: per expert, a gathered x's dx per slot: som_combine adds it up).
- * The residual's gradient is dy itself.  An expert without rows gets dw = 0 and
- * dbias = 0.  With slope_z, dx is multiplied by act'(slope_z) of
- * slope_activation before it is stored: the dz of the layer below.
- * For 16-bit types dz is held in that type for the two products, as the matrix
- * instructions take it. */
+ * The residual's gradient is dy itself.  With an activation, dz is held in the
+ * element type for the two products, as the matrix instructions take it. */
 typedef struct som_linear_call {
-    int32_t type;              /* som_type of x, w, bias, residual, y, z, gradients  */
+    int32_t type;              /* som_type of all matrices                           */
     int32_t activation;        /* som_activation                                     */
     int64_t n;                 /* rows (documents); 0 is allowed                     */
-    int32_t inner, outer;      /* > 0                                                */
+    int32_t inner, outer;      /* 1 .. 4,000,000                                     */
     const void *x;
     int64_t ldx;               /* elements from row to row, >= inner                 */
-    const void *w;             /* packed outer x inner, or experts x outer x inner   */
-    const void *bias;          /* outer, or experts x outer; NULL for none           */
+    const void *w;             /* packed outer x inner                               */
+    const void *bias;          /* outer; NULL for none                               */
     const void *residual;      /* NULL for none (forward only)                       */
     int64_t ldr;               /* >= outer                                           */
     void *y;                   /* packed, forward's result                           */
     void *z;                   /* packed; forward writes it unless NULL; backward
                                   reads it unless activation is NONE               */
-    int32_t experts, k;        /* 0, 0: one matrix for all rows                      */
-    int32_t gather;
-    const int32_t *offsets;    /* experts + 1                                        */
-    const int32_t *order;      /* n k                                                */
     const void *dy;            /* backward                                           */
     int64_t lddy;              /* >= outer                                           */
     void *dx, *dw, *dbias;     /* packed; each NULL if not wanted                    */
-    const void *slope_z;       /* packed like dx, or NULL                            */
-    int32_t slope_activation;
     void *workspace;
     uint64_t workspace_bytes;
     void *stream;
 } som_linear_call;
 
 /* Bytes of work memory that the call needs (0: none, workspace may be NULL):
- * parts of a split contraction, copies of operands whose rows are not whole
- * 16-byte pieces, and dz.  A function of the sizes, leading dimensions, pointer
- * alignments and which pointers are NULL. */
+ * parts of a split contraction or of sums, copies of operands whose rows are not
+ * whole 16-byte pieces where that is the faster way, and dz.  A function of the
+ * sizes, leading dimensions, pointer alignments and which pointers are NULL. */
 som_status som_linear_workspace(const som_linear_call *call, int32_t backward, uint64_t *bytes);
 
 /* Errors of both: SOM_E_ARG (a bad type, activation or size, a missing or too
- * short array, inner != outer strides out of range, a workspace that is missing,
+ * short array, a leading dimension below its row, a workspace that is missing,
  * misaligned or too small), SOM_E_UNSUPPORTED (inner or outer above 4,000,000,
- * more than 2^31 - 1 slots, tiles or experts x outer rows), SOM_E_DEVICE. */
+ * more than 2^31 - 1 tiles), SOM_E_DEVICE. */
 som_status som_linear(const som_linear_call *call);
 som_status som_linear_backward(const som_linear_call *call);
+
+/* The experts' answers to the documents x (n x inner) that are routed to them,
+ * joined: for document i with experts e = index[i][j] and weights g = weight[i][j],
+ *     z = w1_e x_i + b1_e,   h = act(z),   answer = w2_e h + b2_e,
+ *     y_i = residual_i + sum over j of g answer,
+ * or, with w2 NULL, local linear maps: answer = w1_e x_i + b1_e (activation NONE).
+ * The routing comes as som_dispatch gives it; a slot whose expert is -1 adds
+ * nothing, unless its weight is NaN: then the document's y is NaN.
+ *
+ * For a gradient, forward has to keep z and scaled = g h (both n k x hidden,
+ * rows in the experts' order; without w2 nothing is kept).  From dy,
+ *     dweight = <dy_i, answer>  (of the element type; 0 for absent slots)
+ *     dz = g (w2_e^T dy_i) act'(z)
+ *     dw2_e = sum of dy_i scaled^T,  db2_e = sum of g dy_i
+ *     dw1_e = sum of dz x_i^T,  db1_e = sum of dz,  dx_i = sum over j of w1_e^T dz
+ * An expert without documents gets zeros.  The residual's gradient is dy.
+ * Rounded to the element type on the way: h (scaled apart, from the same sums), z
+ * where the slope is taken of it, dz; answers and each slot's part of dx are joined
+ * in fp32. */
+typedef struct som_experts_call {
+    int32_t type;              /* som_type of all matrices                           */
+    int32_t activation;        /* som_activation                                     */
+    int64_t n;                 /* documents; 0 is allowed                            */
+    int32_t k, experts;        /* choices of a document; n k <= 2^31 - 1             */
+    int32_t inner, hidden;     /* 1 .. 4,000,000; x's width, w1's rows               */
+    int32_t outer;             /* w2's rows; without w2 equal to hidden              */
+    const void *x;
+    int64_t ldx;
+    const void *w1, *b1;       /* packed experts x hidden x inner, experts x hidden  */
+    const void *w2, *b2;       /* packed experts x outer x hidden, experts x outer;
+                                  a bias NULL for none                               */
+    const void *residual;      /* n x outer, NULL for none (forward only)            */
+    int64_t ldr;
+    const float *weight;       /* n x k; NULL for 1                                  */
+    const int32_t *offsets, *order, *place;  /* som_dispatch's                       */
+    void *y;                   /* packed n x outer                                   */
+    void *z, *scaled;          /* kept for the gradient; forward: both or neither    */
+    const void *dy;            /* n x outer, backward                                */
+    int64_t lddy;
+    void *dx;                  /* packed n x inner; each gradient NULL if not wanted */
+    void *dweight;             /* packed n x k                                       */
+    void *dw1, *db1, *dw2, *db2;
+    void *workspace;
+    uint64_t workspace_bytes;
+    void *stream;
+} som_experts_call;
+
+/* Errors: as som_linear, and SOM_E_ARG (b2 without w2, an activation, kept arrays
+ * or another outer without w2, only one of z and scaled). */
+som_status som_experts_workspace(const som_experts_call *call, int32_t backward,
+                                 uint64_t *bytes);
+som_status som_experts(const som_experts_call *call);
+som_status som_experts_backward(const som_experts_call *call);
 
 /* Routing of n documents by their scores s (n x experts) to k experts each.
  *     p = softmax(s) over the row, or 1 / (1 + e^-s)
@@ -139,6 +175,10 @@ typedef struct som_route_call {
     const void *dweight;       /* n x k, packed                                      */
     int32_t dweight_type;      /* som_type                                           */
     void *dscores;             /* n x experts, packed                                */
+    int32_t *offsets;          /* NULL, or with order and place: as som_dispatch     */
+    int32_t *order, *place;
+    void *workspace;           /* som_dispatch_workspace bytes                       */
+    uint64_t workspace_bytes;
     void *stream;
 } som_route_call;
 
@@ -157,22 +197,6 @@ som_status som_dispatch_workspace(int64_t n, int32_t k, int32_t experts, uint64_
 som_status som_dispatch(const int32_t *index, int64_t n, int32_t k, int32_t experts,
                         int32_t *offsets, int32_t *order, int32_t *place, void *work,
                         uint64_t work_bytes, void *stream);
-
-/* out[i] = residual[i] + sum over j of weight[i][j] y[place[i][j]]: the answers y
- * (rows in the experts' order, width elements, packed) joined per document, in the
- * order of j.  weight NULL: 1.  Absent slots add nothing, unless their weight is
- * NaN: then the row is NaN. */
-som_status som_combine(int32_t type, int64_t n, int32_t k, int32_t width, const void *y,
-                       const float *weight, const int32_t *place, const void *residual,
-                       int64_t ldr, void *out, void *stream);
-
-/* Its gradient: dy[place[i][j]] = weight[i][j] dout[i] (rows of absent slots are not
- * written) and dweight[i][j] = <dout[i], y[place[i][j]]> (0 if absent), both of
- * `type`. */
-som_status som_combine_backward(int32_t type, int64_t n, int32_t k, int32_t width,
-                                const void *dout, int64_t ldd, const void *y,
-                                const float *weight, const int32_t *place, void *dy,
-                                void *dweight, void *stream);
 
 /* AdamW over many tensors at once.  Step t of element p with gradient g:
  *     m = beta1 m + (1 - beta1) g        v = beta2 v + (1 - beta2) g^2

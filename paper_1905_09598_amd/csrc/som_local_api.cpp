@@ -55,7 +55,8 @@ ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus) {
         }
         const int64_t slabs = std::max<int64_t>(1, (k + slab - 1) / slab);
         const int64_t rows = a.mode == kWeight ? a.m * experts : a.m;
-        for (int32_t parts = 1; parts <= 32 && parts <= slabs; parts *= 2) {
+        const int32_t most = a.mode == kGate ? 1 : 32;   // its rows' dots need whole sums
+        for (int32_t parts = 1; parts <= most && parts <= slabs; parts *= 2) {
             const int64_t floats = parts > 1 ? parts * rows * (tn * s.tile) : 0;
             if (floats > (int64_t)1 << 30) break;
             const double rounds =
@@ -219,28 +220,53 @@ struct Product {
     }
 };
 
+hipError_t run_copy(const SideRows &side, hipStream_t s) {
+    return side.copied ? som::launch_rows_copy(side.copy, s) : hipSuccess;
+}
+
+hipError_t run(const Product &p, hipStream_t s) { return launch_product(p.a, p.plan, s); }
+
+// Runs the steps of a call in order, up to the first that fails.
+template <typename... Step>
+hipError_t in_order(Step... steps) {
+    hipError_t e = hipSuccess;
+    (void)((e = steps(), e == hipSuccess) && ...);
+    return e;
+}
+
+SideRows side(const void *p, int64_t rows, int64_t cols, int64_t ld) {
+    SideRows s;
+    s.p = p, s.rows = rows, s.cols = cols, s.ld = ld;
+    return s;
+}
+// Rows named by the order of the slots: a product's *list is set, and cleared again
+// where a copy in that order takes the rows' place.
+void by_slot(SideRows &s, const int32_t **list, const int32_t *order, int32_t k, int64_t slots) {
+    *list = order;
+    s.list = list, s.per = k, s.listed = slots;
+}
+
 // What a call enqueues, over the caller's work memory.
 struct LinearForward {
     SideRows x, w;
     Product product;
     LinearForward(const som_linear_call &c, Carver &work) {
-        const int64_t rows = c.experts ? c.n * c.k : c.n;
         ProductArgs &a = product.a;
         a.mode = som::kForward;
         a.type = c.type;
         a.activation = c.activation;
-        a.m = rows, a.n = c.outer, a.k = c.inner;
-        a.offsets = c.experts ? c.offsets : nullptr;
-        a.experts = c.experts, a.per = c.k;
-        a.list = c.experts && c.gather ? c.order : nullptr;
+        a.m = c.n, a.n = c.outer, a.k = c.inner;
+        a.per = 1;
         a.bias = c.bias;
         a.residual = c.residual, a.ldr = c.ldr;
         a.y = c.y, a.z = c.z;
-        x.p = c.x, x.rows = c.gather ? c.n : rows, x.cols = c.inner, x.ld = c.ldx;
-        x.list = &a.list, x.per = c.k, x.listed = rows;
-        w.p = c.w, w.rows = (int64_t)c.outer * std::max(1, c.experts);
-        w.cols = c.inner, w.ld = c.inner;
+        x = side(c.x, c.n, c.inner, c.ldx);
+        w = side(c.w, c.outer, c.inner, c.inner);
         product.place(work, x, w);
+    }
+    hipError_t enqueue(hipStream_t s) const {
+        return in_order([&] { return run_copy(x, s); }, [&] { return run_copy(w, s); },
+                        [&] { return run(product, s); });
     }
 };
 
@@ -248,49 +274,252 @@ struct LinearBackward {
     SideRows x, w, dz;
     Product input, weight;
     som::SumsArgs sums{};
-    bool has_input, has_weight;
+    bool has_input, has_weight, has_rows;
     LinearBackward(const som_linear_call &c, Carver &work) {
-        const int64_t rows = c.experts ? c.n * c.k : c.n;
-        const int32_t *const offsets = c.experts ? c.offsets : nullptr;
-        has_input = c.dx != nullptr;
+        has_input = c.dx != nullptr && c.n;
         has_weight = c.dw != nullptr;
-        dz.p = c.dy, dz.rows = rows, dz.cols = c.outer, dz.ld = c.lddy;
+        has_rows = c.n != 0;
+        dz = side(c.dy, c.n, c.outer, c.lddy);
         if (c.activation != SOM_ACT_NONE) dz.make_copy(work, c.type, c.z, c.activation);
         if (has_input) {
             ProductArgs &a = input.a;
             a.mode = som::kInput;
             a.type = c.type;
-            a.m = rows, a.n = c.inner, a.k = c.outer;
-            a.offsets = offsets;
-            a.experts = c.experts, a.per = 1;
+            a.m = c.n, a.n = c.inner, a.k = c.outer;
+            a.per = 1;
             a.y = c.dx;
-            a.slope = c.slope_z, a.activation = c.slope_activation;
-            w.p = c.w, w.rows = (int64_t)c.outer * std::max(1, c.experts);
-            w.cols = c.inner, w.ld = c.inner;
+            w = side(c.w, c.outer, c.inner, c.inner);
             input.place(work, dz, w);
         }
         if (has_weight) {
             ProductArgs &a = weight.a;
             a.mode = som::kWeight;
             a.type = c.type;
-            a.m = c.outer, a.n = c.inner, a.k = rows;
-            a.offsets = offsets;
-            a.experts = c.experts, a.per = c.k;
-            a.list = c.experts && c.gather ? c.order : nullptr;
+            a.m = c.outer, a.n = c.inner, a.k = c.n;
+            a.per = 1;
             a.y = c.dw;
-            x.p = c.x, x.rows = c.gather ? c.n : rows, x.cols = c.inner, x.ld = c.ldx;
-            x.list = &a.list, x.per = c.k, x.listed = rows;
+            x = side(c.x, c.n, c.inner, c.ldx);
             weight.place(work, dz, x);
         }
         if (c.dbias) {
             sums.type = c.type;
             sums.src = dz.p;
-            sums.rows = rows, sums.cols = c.outer, sums.ld = dz.ld;
-            sums.offsets = offsets;
-            sums.experts = c.experts;
+            sums.rows = c.n, sums.cols = c.outer, sums.ld = dz.ld;
             sums.out = c.dbias;
             sums.partial = work.take<float>((uint64_t)som::sums_partial(sums) * 4);
         }
+    }
+    hipError_t enqueue(hipStream_t s) const {
+        const auto copy = [&](const SideRows &r) { return has_rows ? run_copy(r, s) : hipSuccess; };
+        return in_order([&] { return copy(dz); }, [&] { return copy(w); }, [&] { return copy(x); },
+                        [&] { return has_input ? run(input, s) : hipSuccess; },
+                        [&] { return has_weight ? run(weight, s) : hipSuccess; },
+                        [&] { return sums.out ? som::launch_sums(sums, s) : hipSuccess; });
+    }
+};
+
+// The experts' answers: the routed products, in fp32, then the join.
+struct ExpertsForward {
+    SideRows x, h, w1, w2;
+    Product first, second;
+    som::CombineArgs join{};
+    bool two;
+    ExpertsForward(const som_experts_call &c, Carver &work) {
+        const int size = som::type_size(c.type);
+        const int64_t slots = c.n * c.k;
+        two = c.w2 != nullptr;
+        float *const answers = work.take<float>((uint64_t)slots * c.outer * 4);
+        void *const hidden = two ? work.take((uint64_t)slots * c.hidden * size) : nullptr;
+        ProductArgs &a = first.a;
+        a.mode = som::kForward;
+        a.type = c.type;
+        a.m = slots, a.n = c.hidden, a.k = c.inner;
+        a.offsets = c.offsets, a.experts = c.experts, a.per = c.k;
+        a.slots = c.order, a.gates = c.weight;
+        a.bias = c.b1;
+        a.activation = c.activation;
+        a.wide = !two;
+        a.y = two ? hidden : answers;
+        a.z = c.z, a.scaled = c.scaled;
+        x = side(c.x, c.n, c.inner, c.ldx);
+        by_slot(x, &a.list, c.order, c.k, slots);
+        w1 = side(c.w1, (int64_t)c.experts * c.hidden, c.inner, c.inner);
+        first.place(work, x, w1);
+        if (two) {
+            ProductArgs &b = second.a;
+            b.mode = som::kForward;
+            b.type = c.type;
+            b.m = slots, b.n = c.outer, b.k = c.hidden;
+            b.offsets = c.offsets, b.experts = c.experts, b.per = c.k;
+            b.bias = c.b2;
+            b.wide = 1;
+            b.y = answers;
+            h = side(hidden, slots, c.hidden, c.hidden);
+            w2 = side(c.w2, (int64_t)c.experts * c.outer, c.hidden, c.hidden);
+            second.place(work, h, w2);
+        }
+        join.type = c.type, join.k = c.k;
+        join.n = c.n, join.width = c.outer;
+        join.y = answers, join.weight = c.weight, join.place = c.place;
+        join.residual = c.residual, join.ldr = c.ldr;
+        join.out = c.y;
+    }
+    hipError_t enqueue(hipStream_t s) const {
+        return in_order([&] { return run_copy(x, s); }, [&] { return run_copy(w1, s); },
+                        [&] { return run(first, s); },
+                        [&] { return two ? run_copy(h, s) : hipSuccess; },
+                        [&] { return two ? run_copy(w2, s) : hipSuccess; },
+                        [&] { return two ? run(second, s) : hipSuccess; },
+                        [&] { return som::launch_combine(join, s); });
+    }
+};
+
+// Their gradients.  The last layer (w2, or w1 alone) takes its gradient from the
+// documents' rows of dy, found by slot, and the weights come in after the sums:
+//     C = w^T dy,  dweight = <C, u> + <dy, bias>  with u the layer's input,
+//     the input's gradient g C (times the slope), dw = dy (g u)^T.
+struct ExpertsBackward {
+    SideRows dy_gate, dy_weight, w_last, scaled, dz_input, dz_weight, w1, x;
+    Product gate, last_weight, input, first_weight;
+    som::SumsArgs last_sums{}, first_sums{};
+    som::CombineArgs join{};
+    som::DweightArgs dweight{};
+    bool two, has_rows, has_gate, has_sums, has_input;
+    ExpertsBackward(const som_experts_call &c, Carver &work) {
+        const int size = som::type_size(c.type);
+        const int64_t slots = c.n * c.k;
+        two = c.w2 != nullptr;
+        has_rows = slots != 0;
+        const int32_t width = two ? c.hidden : c.inner;   // of the last layer's input
+        const bool first = two && (c.dw1 || c.db1 || c.dx);
+        has_gate = has_rows && (c.dweight || first || (!two && c.dx));
+        has_input = has_rows && two && c.dx;
+        void *dz = nullptr;
+        float *parts = nullptr;
+        if (c.dx) parts = work.take<float>((uint64_t)slots * c.inner * 4);
+        if (has_gate) {
+            ProductArgs &a = gate.a;
+            a.mode = som::kGate;
+            a.type = c.type;
+            a.m = slots, a.n = width, a.k = c.outer;
+            a.offsets = c.offsets, a.experts = c.experts, a.per = c.k;
+            a.slots = c.order, a.gates = c.weight;
+            a.activation = two ? c.activation : SOM_ACT_NONE;
+            a.argument = two ? c.z : c.x;
+            a.ld_argument = two ? c.hidden : c.ldx;
+            a.argument_listed = !two;
+            a.wide = !two;
+            if (two) dz = work.take((uint64_t)slots * c.hidden * size);
+            // without dx of local linear maps the products' rows are not wanted
+            if (!two && !parts) parts = work.take<float>((uint64_t)slots * c.inner * 4);
+            a.y = two ? dz : parts;
+            dy_gate = side(c.dy, c.n, c.outer, c.lddy);
+            by_slot(dy_gate, &a.list, c.order, c.k, slots);
+            w_last = side(two ? c.w2 : c.w1, (int64_t)c.experts * c.outer, width, width);
+            gate.place(work, dy_gate, w_last);
+            a.dot_cols = som::plan_dot_cols(gate.plan, a.n);
+            a.dots = work.take<float>((uint64_t)slots * a.dot_cols * 4);
+        }
+        void *const dw_last = two ? c.dw2 : c.dw1, *const db_last = two ? c.db2 : c.db1;
+        const void *const b_last = two ? c.b2 : c.b1;
+        if (dw_last) {
+            ProductArgs &a = last_weight.a;
+            a.mode = som::kWeight;
+            a.type = c.type;
+            a.m = c.outer, a.n = width, a.k = slots;
+            a.offsets = c.offsets, a.experts = c.experts, a.per = c.k;
+            a.list_of_a = 1;
+            a.y = dw_last;
+            dy_weight = side(c.dy, c.n, c.outer, c.lddy);
+            by_slot(dy_weight, &a.list, c.order, c.k, slots);
+            scaled = side(two ? c.scaled : c.x, two ? slots : c.n, width, two ? width : c.ldx);
+            if (!two) {   // g x, by slot
+                scaled.rows = slots;
+                scaled.make_copy(work, c.type);
+                scaled.copy.list = c.order;
+                scaled.copy.per = c.k;
+                scaled.copy.gates = c.weight;
+            }
+            last_weight.place(work, dy_weight, scaled);
+        }
+        has_sums = db_last || (c.dweight && b_last);
+        if (has_sums) {
+            som::SumsArgs &s = last_sums;
+            s.type = c.type;
+            s.src = c.dy;
+            s.rows = slots, s.cols = c.outer, s.ld = c.lddy;
+            s.offsets = c.offsets, s.experts = c.experts;
+            s.list = c.order, s.per = c.k, s.gates = c.weight;
+            s.out = db_last;
+            s.partial = work.take<float>((uint64_t)som::sums_partial(s) * 4);
+            if (c.dweight && b_last) {
+                s.bias = b_last;
+                s.dot_cols = som::sums_dot_cols(s);
+                s.dots = work.take<float>((uint64_t)slots * s.dot_cols * 4);
+            }
+        }
+        dweight.type = c.type;
+        dweight.slots = slots;
+        dweight.place = c.place;
+        dweight.dots[0] = gate.a.dots, dweight.cols[0] = gate.a.dot_cols;
+        dweight.dots[1] = last_sums.dots, dweight.cols[1] = last_sums.dot_cols;
+        dweight.dweight = c.dweight;
+        if (two && c.dw1) {
+            ProductArgs &a = first_weight.a;
+            a.mode = som::kWeight;
+            a.type = c.type;
+            a.m = c.hidden, a.n = c.inner, a.k = slots;
+            a.offsets = c.offsets, a.experts = c.experts, a.per = c.k;
+            a.y = c.dw1;
+            dz_weight = side(dz, slots, c.hidden, c.hidden);
+            x = side(c.x, c.n, c.inner, c.ldx);
+            by_slot(x, &a.list, c.order, c.k, slots);
+            first_weight.place(work, dz_weight, x);
+        }
+        if (two && c.db1) {
+            som::SumsArgs &s = first_sums;
+            s.type = c.type;
+            s.src = dz;
+            s.rows = slots, s.cols = c.hidden, s.ld = c.hidden;
+            s.offsets = c.offsets, s.experts = c.experts;
+            s.out = c.db1;
+            s.partial = work.take<float>((uint64_t)som::sums_partial(s) * 4);
+        }
+        if (has_input) {
+            ProductArgs &a = input.a;
+            a.mode = som::kInput;
+            a.type = c.type;
+            a.m = slots, a.n = c.inner, a.k = c.hidden;
+            a.offsets = c.offsets, a.experts = c.experts, a.per = c.k;
+            a.wide = 1;
+            a.y = parts;
+            dz_input = side(dz, slots, c.hidden, c.hidden);
+            w1 = side(c.w1, (int64_t)c.experts * c.hidden, c.inner, c.inner);
+            input.place(work, dz_input, w1);
+        }
+        join.type = c.type, join.k = c.k;
+        join.n = c.n, join.width = c.inner;
+        join.y = parts, join.place = c.place;
+        join.out = c.dx;
+    }
+    hipError_t enqueue(hipStream_t s) const {
+        const auto copy = [&](const SideRows &r) { return has_rows ? run_copy(r, s) : hipSuccess; };
+        const auto product = [&](bool wanted, const Product &p) {
+            return wanted ? run(p, s) : hipSuccess;
+        };
+        return in_order(
+            [&] { return copy(dy_gate); }, [&] { return copy(w_last); },
+            [&] { return product(has_gate, gate); },
+            [&] { return copy(dy_weight); }, [&] { return copy(scaled); },
+            [&] { return product(last_weight.a.y, last_weight); },
+            [&] { return has_sums ? som::launch_sums(last_sums, s) : hipSuccess; },
+            [&] { return dweight.dweight ? som::launch_dweight(dweight, s) : hipSuccess; },
+            [&] { return copy(dz_weight); }, [&] { return copy(x); },
+            [&] { return product(first_weight.a.y, first_weight); },
+            [&] { return first_sums.out ? som::launch_sums(first_sums, s) : hipSuccess; },
+            [&] { return copy(dz_input); }, [&] { return copy(w1); },
+            [&] { return product(has_input, input); },
+            [&] { return join.out ? som::launch_combine(join, s) : hipSuccess; });
     }
 };
 
@@ -298,41 +527,65 @@ struct LinearBackward {
 // is about to run.
 som_status linear_sizes_ok(const som_linear_call *c) {
     if (!c || !type_ok(c->type) || !activation_ok(c->activation) || c->n < 0 || c->inner <= 0 ||
-        c->outer <= 0 || c->experts < 0)
+        c->outer <= 0 || c->ldx < c->inner)
         return SOM_E_ARG;
-    if (c->experts ? c->k <= 0 : (c->k != 0 || c->gather)) return SOM_E_ARG;
-    if (c->ldx < c->inner) return SOM_E_ARG;
-    if (c->inner > som::kMaxWidth || c->outer > som::kMaxWidth) return SOM_E_UNSUPPORTED;
-    const __int128 rows = (__int128)c->n * (c->experts ? c->k : 1);
-    if (c->experts && rows > INT32_MAX) return SOM_E_UNSUPPORTED;
-    if (rows > (__int128)1 << 40) return SOM_E_UNSUPPORTED;
-    if ((int64_t)c->outer * std::max(1, c->experts) > INT32_MAX) return SOM_E_UNSUPPORTED;
+    if (c->inner > som::kMaxWidth || c->outer > som::kMaxWidth || c->n > (int64_t)1 << 40)
+        return SOM_E_UNSUPPORTED;
     return SOM_OK;
 }
 
-bool linear_common_ok(const som_linear_call &c) {
+som_status experts_sizes_ok(const som_experts_call *c) {
+    if (!c || !type_ok(c->type) || !activation_ok(c->activation) || c->n < 0 || c->k < 1 ||
+        c->experts < 1 || c->inner < 1 || c->hidden < 1 || c->outer < 1 || c->ldx < c->inner)
+        return SOM_E_ARG;
+    if (!c->w2 && (c->b2 || c->z || c->scaled || c->dw2 || c->db2 || c->outer != c->hidden ||
+                   c->activation != SOM_ACT_NONE))
+        return SOM_E_ARG;
+    if (c->inner > som::kMaxWidth || c->hidden > som::kMaxWidth || c->outer > som::kMaxWidth ||
+        (__int128)c->n * c->k > INT32_MAX ||
+        (int64_t)c->experts * std::max(c->hidden, c->outer) > INT32_MAX)
+        return SOM_E_UNSUPPORTED;
+    return SOM_OK;
+}
+
+bool experts_common_ok(const som_experts_call &c) {
     const int size = som::type_size(c.type);
-    const int64_t rows = c.experts ? c.n * c.k : c.n, xrows = c.gather ? c.n : rows;
-    const int64_t wrows = (int64_t)c.outer * std::max(1, c.experts);
-    if (!rows_ok(c.w, wrows, c.inner, c.inner, size)) return false;
-    if (!rows_ok(c.x, xrows, c.inner, c.ldx, size)) return false;
-    if (c.experts) {
-        if (!rows_ok(c.offsets, 1, c.experts + 1, c.experts + 1, 4)) return false;
-        if (c.gather && !rows_ok(c.order, 1, rows, rows, 4)) return false;
-    }
-    return true;
+    const int64_t slots = c.n * c.k, e = c.experts;
+    return rows_ok(c.x, c.n, c.inner, c.ldx, size) &&
+           rows_ok(c.w1, e * c.hidden, c.inner, c.inner, size) &&
+           rows_ok_or_null(c.b1, e, c.hidden, c.hidden, size) &&
+           rows_ok_or_null(c.w2, e * c.outer, c.hidden, c.hidden, size) &&
+           rows_ok_or_null(c.b2, e, c.outer, c.outer, size) &&
+           rows_ok_or_null(c.weight, 1, slots, slots, 4) &&
+           rows_ok(c.offsets, 1, e + 1, e + 1, 4) && rows_ok(c.order, 1, slots, slots, 4) &&
+           rows_ok(c.place, 1, slots, slots, 4);
 }
 
-som_status work_ok(const Carver &need, const som_linear_call &c) {
+som_status work_ok(const Carver &need, void *workspace, uint64_t bytes) {
     if (need.used == 0) return SOM_OK;
-    if (!c.workspace || reinterpret_cast<uintptr_t>(c.workspace) % 256 != 0 ||
-        c.workspace_bytes < need.used || !som::device_range_ok(c.workspace, need.used))
+    if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 != 0 || bytes < need.used ||
+        !som::device_range_ok(workspace, need.used))
         return SOM_E_ARG;
     return SOM_OK;
 }
 
-hipError_t run_copy(const SideRows &side, hipStream_t s) {
-    return side.copied ? som::launch_rows_copy(side.copy, s) : hipSuccess;
+// Lays a call out over its work memory, once to see what it needs, and enqueues it.
+template <typename Plan, typename Call>
+som_status enqueue(const Call &c) {
+    Carver need(nullptr);
+    Plan(c, need);
+    const som_status st = work_ok(need, c.workspace, c.workspace_bytes);
+    if (st != SOM_OK) return st;
+    Carver work(c.workspace);
+    return from_hip(Plan(c, work).enqueue(reinterpret_cast<hipStream_t>(c.stream)));
+}
+
+template <typename Forward, typename Backward, typename Call>
+uint64_t workspace(const Call &c, bool backward) {
+    Carver need(nullptr);
+    if (backward) Backward(c, need);
+    else Forward(c, need);
+    return need.used;
 }
 
 }  // namespace
@@ -342,74 +595,76 @@ extern "C" {
 som_status som_linear_workspace(const som_linear_call *c, int32_t backward, uint64_t *bytes) {
     if (!bytes) return SOM_E_ARG;
     const som_status st = linear_sizes_ok(c);
-    if (st != SOM_OK) return st;
-    Carver need(nullptr);
-    if (backward) LinearBackward(*c, need);
-    else LinearForward(*c, need);
-    *bytes = c->n ? need.used : 0;
-    return SOM_OK;
+    if (st == SOM_OK) *bytes = c->n ? workspace<LinearForward, LinearBackward>(*c, backward) : 0;
+    return st;
 }
 
 som_status som_linear(const som_linear_call *c) {
-    som_status st = linear_sizes_ok(c);
+    const som_status st = linear_sizes_ok(c);
     if (st != SOM_OK) return st;
     const int size = som::type_size(c->type);
-    const int64_t rows = c->experts ? c->n * c->k : c->n;
-    if (c->n && !c->y) return SOM_E_ARG;
-    if (!linear_common_ok(*c) || !rows_ok(c->y, rows, c->outer, c->outer, size) ||
-        !rows_ok_or_null(c->z, rows, c->outer, c->outer, size) ||
-        !rows_ok_or_null(c->bias, std::max(1, c->experts), c->outer, c->outer, size) ||
-        !rows_ok_or_null(c->residual, rows, c->outer, c->ldr, size))
+    if (!rows_ok(c->w, c->outer, c->inner, c->inner, size) ||
+        !rows_ok(c->x, c->n, c->inner, c->ldx, size) ||
+        !rows_ok(c->y, c->n, c->outer, c->outer, size) ||
+        !rows_ok_or_null(c->z, c->n, c->outer, c->outer, size) ||
+        !rows_ok_or_null(c->bias, 1, c->outer, c->outer, size) ||
+        !rows_ok_or_null(c->residual, c->n, c->outer, c->ldr, size))
         return SOM_E_ARG;
-    if (c->n == 0) return SOM_OK;
-    Carver need(nullptr);
-    LinearForward(*c, need);
-    st = work_ok(need, *c);
-    if (st != SOM_OK) return st;
-    Carver work(c->workspace);
-    const LinearForward f(*c, work);
-    const hipStream_t s = reinterpret_cast<hipStream_t>(c->stream);
-    hipError_t e = run_copy(f.x, s);
-    if (e == hipSuccess) e = run_copy(f.w, s);
-    if (e == hipSuccess) e = launch_product(f.product.a, f.product.plan, s);
-    return from_hip(e);
+    return c->n ? enqueue<LinearForward>(*c) : SOM_OK;
 }
 
 som_status som_linear_backward(const som_linear_call *c) {
-    som_status st = linear_sizes_ok(c);
+    const som_status st = linear_sizes_ok(c);
     if (st != SOM_OK) return st;
-    if (!activation_ok(c->slope_activation)) return SOM_E_ARG;
     const int size = som::type_size(c->type);
-    const int64_t rows = c->experts ? c->n * c->k : c->n;
-    const int64_t wrows = (int64_t)c->outer * std::max(1, c->experts);
-    if (!linear_common_ok(*c) || !rows_ok(c->dy, rows, c->outer, c->lddy, size) ||
-        (c->activation != SOM_ACT_NONE && !rows_ok(c->z, rows, c->outer, c->outer, size)) ||
-        !rows_ok_or_null(c->dx, rows, c->inner, c->inner, size) ||
-        !rows_ok_or_null(c->dw, wrows, c->inner, c->inner, size) ||
-        !rows_ok_or_null(c->dbias, wrows, 1, 1, size) ||
-        !rows_ok_or_null(c->slope_z, rows, c->inner, c->inner, size))
+    if (!rows_ok(c->w, c->outer, c->inner, c->inner, size) ||
+        !rows_ok(c->x, c->n, c->inner, c->ldx, size) ||
+        !rows_ok(c->dy, c->n, c->outer, c->lddy, size) ||
+        (c->activation != SOM_ACT_NONE && !rows_ok(c->z, c->n, c->outer, c->outer, size)) ||
+        !rows_ok_or_null(c->dx, c->n, c->inner, c->inner, size) ||
+        !rows_ok_or_null(c->dw, c->outer, c->inner, c->inner, size) ||
+        !rows_ok_or_null(c->dbias, 1, c->outer, c->outer, size))
         return SOM_E_ARG;
-    const hipStream_t s = reinterpret_cast<hipStream_t>(c->stream);
-    Carver need(nullptr);
-    LinearBackward(*c, need);
-    if (c->n) {
-        st = work_ok(need, *c);
-        if (st != SOM_OK) return st;
-    }
-    Carver work(c->workspace);
-    LinearBackward b(*c, work);
-    if (c->n == 0) {   // no rows: nothing to copy, dx is empty, the sums are 0
-        b.has_input = false;
-        b.dz.copied = b.x.copied = b.w.copied = false;
-        if (b.has_weight) b.weight.plan.splits = 1;
-    }
-    hipError_t e = run_copy(b.dz, s);
-    if (e == hipSuccess) e = run_copy(b.w, s);
-    if (e == hipSuccess) e = run_copy(b.x, s);
-    if (e == hipSuccess && b.has_input) e = launch_product(b.input.a, b.input.plan, s);
-    if (e == hipSuccess && b.has_weight) e = launch_product(b.weight.a, b.weight.plan, s);
-    if (e == hipSuccess && c->dbias) e = som::launch_sums(b.sums, s);
-    return from_hip(e);
+    return enqueue<LinearBackward>(*c);
+}
+
+som_status som_experts_workspace(const som_experts_call *c, int32_t backward, uint64_t *bytes) {
+    if (!bytes) return SOM_E_ARG;
+    const som_status st = experts_sizes_ok(c);
+    if (st == SOM_OK) *bytes = c->n ? workspace<ExpertsForward, ExpertsBackward>(*c, backward) : 0;
+    return st;
+}
+
+som_status som_experts(const som_experts_call *c) {
+    const som_status st = experts_sizes_ok(c);
+    if (st != SOM_OK) return st;
+    const int size = som::type_size(c->type);
+    const int64_t slots = c->n * c->k;
+    if ((c->z != nullptr) != (c->scaled != nullptr)) return SOM_E_ARG;
+    if (!experts_common_ok(*c) || !rows_ok(c->y, c->n, c->outer, c->outer, size) ||
+        !rows_ok_or_null(c->z, slots, c->hidden, c->hidden, size) ||
+        !rows_ok_or_null(c->scaled, slots, c->hidden, c->hidden, size) ||
+        !rows_ok_or_null(c->residual, c->n, c->outer, c->ldr, size))
+        return SOM_E_ARG;
+    return c->n ? enqueue<ExpertsForward>(*c) : SOM_OK;
+}
+
+som_status som_experts_backward(const som_experts_call *c) {
+    const som_status st = experts_sizes_ok(c);
+    if (st != SOM_OK) return st;
+    const int size = som::type_size(c->type);
+    const int64_t slots = c->n * c->k, e = c->experts;
+    if (!experts_common_ok(*c) || !rows_ok(c->dy, c->n, c->outer, c->lddy, size) ||
+        (c->w2 && (!rows_ok(c->z, slots, c->hidden, c->hidden, size) ||
+                   !rows_ok(c->scaled, slots, c->hidden, c->hidden, size))) ||
+        !rows_ok_or_null(c->dx, c->n, c->inner, c->inner, size) ||
+        !rows_ok_or_null(c->dweight, c->n, c->k, c->k, size) ||
+        !rows_ok_or_null(c->dw1, e * c->hidden, c->inner, c->inner, size) ||
+        !rows_ok_or_null(c->db1, e, c->hidden, c->hidden, size) ||
+        !rows_ok_or_null(c->dw2, e * c->outer, c->hidden, c->hidden, size) ||
+        !rows_ok_or_null(c->db2, e, c->outer, c->outer, size))
+        return SOM_E_ARG;
+    return enqueue<ExpertsBackward>(*c);
 }
 
 static som_status route_ok(const som_route_call *c) {
@@ -453,12 +708,6 @@ static som::RouteArgs route_args(const som_route_call &c) {
     return a;
 }
 
-som_status som_route(const som_route_call *c) {
-    const som_status st = route_ok(c);
-    if (st != SOM_OK) return st;
-    return from_hip(som::launch_route(route_args(*c), reinterpret_cast<hipStream_t>(c->stream)));
-}
-
 som_status som_route_backward(const som_route_call *c) {
     const som_status st = route_ok(c);
     if (st != SOM_OK) return st;
@@ -478,16 +727,17 @@ som_status som_dispatch_workspace(int64_t n, int32_t k, int32_t experts, uint64_
     return SOM_OK;
 }
 
-som_status som_dispatch(const int32_t *index, int64_t n, int32_t k, int32_t experts,
-                        int32_t *offsets, int32_t *order, int32_t *place, void *work,
-                        uint64_t work_bytes, void *stream) {
-    uint64_t need = 0;
-    const som_status st = som_dispatch_workspace(n, k, experts, &need);
-    if (st != SOM_OK) return st;
-    if (!rows_ok(index, n, k, k, 4) || !rows_ok(offsets, 1, experts + 1, experts + 1, 4) ||
-        !rows_ok(order, n, k, k, 4) || !rows_ok(place, n, k, k, 4))
-        return SOM_E_ARG;
-    if (need && (work_bytes < need || !rows_ok(work, 1, need / 4, need / 4, 4))) return SOM_E_ARG;
+static bool dispatch_ok(int64_t n, int32_t k, int32_t experts, const int32_t *offsets,
+                        const int32_t *order, const int32_t *place, const void *work,
+                        uint64_t work_bytes, uint64_t need) {
+    return rows_ok(offsets, 1, experts + 1, experts + 1, 4) && rows_ok(order, n, k, k, 4) &&
+           rows_ok(place, n, k, k, 4) &&
+           (!need || (work_bytes >= need && rows_ok(work, 1, need / 4, need / 4, 4)));
+}
+
+static som::DispatchArgs dispatch_args(const int32_t *index, int64_t n, int32_t k,
+                                       int32_t experts, int32_t *offsets, int32_t *order,
+                                       int32_t *place, void *work) {
     som::DispatchArgs a{};
     a.index = index;
     a.slots = n * k;
@@ -497,50 +747,42 @@ som_status som_dispatch(const int32_t *index, int64_t n, int32_t k, int32_t expe
     a.place = place;
     a.counts = static_cast<int32_t *>(work);
     a.blocks = som::dispatch_blocks(a.slots);
-    return from_hip(som::launch_dispatch(a, reinterpret_cast<hipStream_t>(stream)));
+    return a;
 }
 
-static som_status combine_ok(int32_t type, int64_t n, int32_t k, int32_t width, const void *y,
-                             const float *weight, const int32_t *place) {
-    if (!type_ok(type) || n < 0 || k < 1 || width < 1) return SOM_E_ARG;
-    if ((__int128)n * k > INT32_MAX) return SOM_E_UNSUPPORTED;
-    if (!rows_ok_or_null(y, n * k, width, width, som::type_size(type)) ||
-        !rows_ok_or_null(weight, n, k, k, 4) || !rows_ok(place, n, k, k, 4))
-        return SOM_E_ARG;
-    return SOM_OK;
-}
-
-som_status som_combine(int32_t type, int64_t n, int32_t k, int32_t width, const void *y,
-                       const float *weight, const int32_t *place, const void *residual,
-                       int64_t ldr, void *out, void *stream) {
-    const som_status st = combine_ok(type, n, k, width, y, weight, place);
+som_status som_dispatch(const int32_t *index, int64_t n, int32_t k, int32_t experts,
+                        int32_t *offsets, int32_t *order, int32_t *place, void *work,
+                        uint64_t work_bytes, void *stream) {
+    uint64_t need = 0;
+    const som_status st = som_dispatch_workspace(n, k, experts, &need);
     if (st != SOM_OK) return st;
-    const int size = som::type_size(type);
-    if ((n && !y) || !rows_ok_or_null(residual, n, width, ldr, size) ||
-        !rows_ok(out, n, width, width, size))
+    if (!rows_ok(index, n, k, k, 4) ||
+        !dispatch_ok(n, k, experts, offsets, order, place, work, work_bytes, need))
         return SOM_E_ARG;
-    som::CombineArgs a{};
-    a.type = type, a.k = k, a.n = n, a.width = width;
-    a.y = y, a.weight = weight, a.place = place;
-    a.residual = residual, a.ldr = ldr, a.out = out;
-    return from_hip(som::launch_combine(a, reinterpret_cast<hipStream_t>(stream)));
+    return from_hip(som::launch_dispatch(
+        dispatch_args(index, n, k, experts, offsets, order, place, work),
+        reinterpret_cast<hipStream_t>(stream)));
 }
 
-som_status som_combine_backward(int32_t type, int64_t n, int32_t k, int32_t width,
-                                const void *dout, int64_t ldd, const void *y,
-                                const float *weight, const int32_t *place, void *dy,
-                                void *dweight, void *stream) {
-    const som_status st = combine_ok(type, n, k, width, y, weight, place);
+som_status som_route(const som_route_call *c) {
+    const som_status st = route_ok(c);
     if (st != SOM_OK) return st;
-    const int size = som::type_size(type);
-    if ((n && dweight && !y) || !rows_ok(dout, n, width, ldd, size) ||
-        !rows_ok(dy, n * k, width, width, size) || !rows_ok_or_null(dweight, n, k, k, size))
-        return SOM_E_ARG;
-    som::CombineArgs a{};
-    a.type = type, a.k = k, a.n = n, a.width = width;
-    a.y = y, a.weight = weight, a.place = place;
-    a.dout = dout, a.ldd = ldd, a.dy = dy, a.dweight = dweight;
-    return from_hip(som::launch_combine_backward(a, reinterpret_cast<hipStream_t>(stream)));
+    uint64_t need = 0;
+    if (c->offsets) {
+        (void)som_dispatch_workspace(c->n, c->k, c->experts, &need);
+        if (!dispatch_ok(c->n, c->k, c->experts, c->offsets, c->order, c->place, c->workspace,
+                         c->workspace_bytes, need))
+            return SOM_E_ARG;
+    }
+    const hipStream_t s = reinterpret_cast<hipStream_t>(c->stream);
+    return from_hip(in_order(
+        [&] { return som::launch_route(route_args(*c), s); },
+        [&] {
+            return c->offsets ? som::launch_dispatch(
+                                    dispatch_args(c->index, c->n, c->k, c->experts, c->offsets,
+                                                  c->order, c->place, c->workspace), s)
+                              : hipSuccess;
+        }));
 }
 
 }  // extern "C"

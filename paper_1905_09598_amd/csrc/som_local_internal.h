@@ -9,7 +9,7 @@ namespace som {
 
 enum : int32_t { kF32 = 0, kBF16 = 1, kF16 = 2 };                       // som_type
 enum : int32_t { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };  // som_activation
-enum : int32_t { kForward = 0, kInput = 1, kWeight = 2 };               // which product
+enum : int32_t { kForward = 0, kInput = 1, kWeight = 2, kGate = 3 };    // which product
 
 inline int type_size(int32_t type) { return type == kF32 ? 4 : 2; }
 
@@ -40,32 +40,26 @@ __device__ inline float sigmoid_fast(float z) {
     return __builtin_amdgcn_rcpf(1.f + exp_fast(-z));
 }
 
-__device__ inline float activate(float z, int32_t kind) {
+// The activation and, where it is wanted, its slope.
+__device__ inline float activate(float z, int32_t kind, float *slope = nullptr) {
     switch (kind) {
-        case kActRelu: return z > 0.f ? z : (z != z ? z : 0.f);
+        case kActRelu:
+            if (slope) *slope = z > 0.f ? 1.f : 0.f;
+            return z > 0.f ? z : (z != z ? z : 0.f);
         case kActGelu: {
             float below, bell;
             normal(z, &below, &bell);
+            if (slope) *slope = fmaf(z * bell, 0.39894228040143268f, below);
             return z * below;
-        }
-        case kActSilu: return z * sigmoid_fast(z);
-        default: return z;
-    }
-}
-
-__device__ inline float activation_slope(float z, int32_t kind) {
-    switch (kind) {
-        case kActRelu: return z > 0.f ? 1.f : 0.f;
-        case kActGelu: {
-            float below, bell;
-            normal(z, &below, &bell);
-            return fmaf(z * bell, 0.39894228040143268f, below);
         }
         case kActSilu: {
             const float q = sigmoid_fast(z);
-            return fmaf(z * q, 1.f - q, q);
+            if (slope) *slope = fmaf(z * q, 1.f - q, q);
+            return z * q;
         }
-        default: return 1.f;
+        default:
+            if (slope) *slope = 1.f;
+            return z;
     }
 }
 
@@ -94,23 +88,33 @@ constexpr int64_t kMaxWidth = 4000000;
 inline bool tile_reaches(int64_t ld, int size) { return ld * size * 256 < ((int64_t)1 << 32); }
 
 // C = A B^T, C of m rows and n columns, contraction k (som_product.h).
-//   forward  A = x (m x k), B = w (n x k):      y = act(C + bias) + residual
-//   input    A = dz (m x k), B = w (k x n):     dx = C [* slope of z]
-//   weight   A = dz (k x m), B = x (k x n):     dw = C
-// Routed (offsets): forward and input take the m rows by expert, offsets[e] ..
-// of B + e batch_b; weight sums offsets[e] .. into dw + e m n.  list: forward,
-// row r of A is A's row list[r] / per; weight, row s of B is B's row
-// list[s] / per.  Rows past offsets[experts] are not touched.
+//   forward  A = x (m x k), B = w (n x k):      z = C + bias, y = act(z) + residual,
+//                                               scaled = gate act(z)
+//   input    A = dz (m x k), B = w (k x n):     y = C
+//   gate     A = dout (m x k), B = w (k x n):   y = gate C act'(argument),
+//                                               dots: parts of <C, act(argument)>
+//   weight   A = dz (k x m), B = x (k x n):     y = C
+// Routed (offsets): the m rows of forward, input and gate lie by expert, offsets[e]
+// .. of B + e batch_b; weight sums offsets[e] .. into y + e m n.  Rows past
+// offsets[experts] are not touched.  list: row r of A (forward, gate) or row s of B
+// or A (weight) is the matrix's row list[.] / per.  slots: the slot of each row.
 struct ProductArgs {
     int32_t mode, type, activation;
+    int32_t wide;                     // y holds fp32 (not in weight)
     const void *a, *b;
     int64_t lda, ldb, batch_b;
     int64_t m, n, k;
-    const void *bias, *residual, *slope;
+    const void *bias, *residual;
     int64_t ldr;
-    void *y, *z;
-    const int32_t *offsets, *list;
-    int32_t experts, per;
+    void *y, *z, *scaled;
+    const int32_t *offsets, *list, *slots;
+    int32_t experts, per, list_of_a;
+    const float *gates;               // by slot; gate: null for 1
+    const void *argument;             // gate: rows of n, ld_argument apart
+    int64_t ld_argument;
+    int32_t argument_listed;          // row r's is the document's, slots[r] / per
+    float *dots;                      // gate: m x dot_cols
+    int32_t dot_cols;
     int32_t splits;       // parts of the contraction
     float *partial;       // splits x partial_rows x whole tiles
     int64_t partial_rows;
@@ -128,7 +132,8 @@ struct ProductPlan {
 
 // Copies `rows` rows of `cols` elements, `lds` apart, to rows of ldd >= cols
 // elements filled up with zeros; with z (rows ldz apart), times act'(z); with a
-// list, row r is src's row list[r] / per, or zeros where list[r] is negative.
+// list, row r is src's row list[r] / per, or zeros where list[r] is negative, times
+// gates[list[r]] if there are any.
 struct RowsArgs {
     int32_t type, activation;
     const void *src, *z;
@@ -136,38 +141,56 @@ struct RowsArgs {
     int64_t rows, cols, lds, ldz, ldd;
     const int32_t *list;
     int32_t per;
+    const float *gates;     // times gates[list[r]]
 };
 hipError_t launch_rows_copy(const RowsArgs &a, hipStream_t stream);
 
 // out[e] = sums of the rows of src (cols elements, ld apart) of expert e, or of all
-// rows without offsets.
+// rows without offsets.  With a list, row r is src's row list[r] / per times
+// gates[list[r]], and dots holds the parts of <src's row, bias of the row's expert>:
+// rows x dot_cols.
 struct SumsArgs {
     int32_t type;
     const void *src;
     int64_t rows, cols, ld;
     const int32_t *offsets;
     int32_t experts;
-    void *out;
+    const int32_t *list;
+    int32_t per;
+    const float *gates;
+    const void *bias;
+    float *dots;
+    int32_t dot_cols;
+    void *out;              // null: dots alone
     float *partial;         // sums_partial() floats
 };
+int32_t sums_dot_cols(const SumsArgs &a);
 int64_t sums_partial(const SumsArgs &a);
 hipError_t launch_sums(const SumsArgs &a, hipStream_t stream);
 
+// out[i] = residual[i] + sum over j of weight[i][j] y[place[i][j]], y in fp32.
 struct CombineArgs {
     int32_t type, k;
     int64_t n, width;
-    const void *y;          // rows in the experts' order
+    const float *y;         // rows in the experts' order
     const float *weight;    // n x k, or null
     const int32_t *place;   // n x k
-    const void *residual;   // forward
+    const void *residual;
     int64_t ldr;
     void *out;
-    const void *dout;       // backward
-    int64_t ldd;
-    void *dy, *dweight;
 };
 hipError_t launch_combine(const CombineArgs &a, hipStream_t stream);
-hipError_t launch_combine_backward(const CombineArgs &a, hipStream_t stream);
+
+// dweight[s] = sums of the parts of row place[s] in both arrays (0 if absent).
+struct DweightArgs {
+    int32_t type;
+    int64_t slots;
+    const int32_t *place;
+    const float *dots[2];
+    int32_t cols[2];
+    void *dweight;
+};
+hipError_t launch_dweight(const DweightArgs &a, hipStream_t stream);
 
 // som_route.hip; the fields are som_route_call's.
 constexpr int kMaxExperts = 16384, kMaxChoices = 64, kMaxGroups = 64;
@@ -223,6 +246,11 @@ struct AdamwArgs {
 hipError_t launch_adamw(const AdamwArgs &a, bool eight, hipStream_t stream);
 
 ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus);
+// Parts of a row's dots: columns of one wave each.
+inline int32_t plan_dot_cols(const ProductPlan &p, int64_t n) {
+    const int64_t wide = p.tile == 64 ? 32 : 64;
+    return (int32_t)((n + wide - 1) / wide);
+}
 // One per element type (som_product_*.hip).
 hipError_t launch_product_f32(ProductArgs a, const ProductPlan &p, hipStream_t stream);
 hipError_t launch_product_bf16(ProductArgs a, const ProductPlan &p, hipStream_t stream);

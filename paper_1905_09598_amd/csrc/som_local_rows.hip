@@ -40,6 +40,12 @@ __device__ inline void write_some(T *p, int64_t left, const float (&v)[N]) {
     }
 }
 
+__device__ inline float slope_of(float z, int32_t kind) {
+    float s;
+    (void)activate(z, kind, &s);
+    return s;
+}
+
 template <typename T>
 __global__ __launch_bounds__(kThreads) void rows_copy_kernel(RowsArgs a) {
     constexpr int N = 16 / sizeof(T);
@@ -51,10 +57,15 @@ __global__ __launch_bounds__(kThreads) void rows_copy_kernel(RowsArgs a) {
     const int64_t from = a.list ? a.list[row] : row;
     read_some<T, N>(static_cast<const T *>(a.src) + (a.list ? from / a.per : from) * a.lds + col,
                     from < 0 ? 0 : a.cols - col, v);
+    if (a.gates) {
+        const float g = from < 0 ? 0.f : a.gates[from];
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] *= g;
+    }
     if (a.z) {
         read_some<T, N>(static_cast<const T *>(a.z) + row * a.ldz + col, a.cols - col, z);
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = col + e < a.cols ? v[e] * activation_slope(z[e], a.activation) : 0.f;
+        for (int e = 0; e < N; ++e) v[e] = col + e < a.cols ? v[e] * slope_of(z[e], a.activation) : 0.f;
     }
     write_some<T, N>(static_cast<T *>(a.dst) + row * a.ldd + col, N, v);
 }
@@ -66,7 +77,7 @@ __global__ __launch_bounds__(kThreads) void rows_copy_kernel(RowsArgs a) {
 constexpr int kSumThreads = 256, kSumPieces = 32, kSumLanes = kSumThreads / kSumPieces;
 constexpr int kSumRows = 128;
 
-template <typename T, bool DIRECT>
+template <typename T, bool DIRECT, bool LISTED>
 __global__ __launch_bounds__(kSumThreads) void sums_kernel(SumsArgs a) {
     constexpr int N = 16 / sizeof(T);
     __shared__ float part[kSumLanes][kSumPieces * N + 4];
@@ -87,18 +98,44 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(SumsArgs a) {
         if (first >= end) return;
     }
     const int64_t col = ((int64_t)blockIdx.x * kSumPieces + piece) * N, left = a.cols - col;
-    float sum[N];
+    float sum[N], bias[N];
 #pragma unroll
-    for (int c = 0; c < N; ++c) sum[c] = 0.f;
-    if (left > 0) {
-#pragma unroll 4
-        for (int64_t r = first + lane; r < end; r += kSumLanes) {
-            float v[N];
-            read_some<T, N>(static_cast<const T *>(a.src) + r * a.ld + col, left, v);
+    for (int c = 0; c < N; ++c) sum[c] = bias[c] = 0.f;
+    if (LISTED && a.dots && left > 0)
+        read_some<T, N>(static_cast<const T *>(a.bias) + e * a.cols + col, left, bias);
+    constexpr int kAhead = 4;   // rows whose reads are under way together
+    for (int64_t r0 = first + lane; r0 < end; r0 += kAhead * kSumLanes) {
+        float v[kAhead][N], gate[kAhead];
 #pragma unroll
-            for (int c = 0; c < N; ++c) sum[c] += v[c];
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t r = r0 + u * kSumLanes;
+            int64_t row = r;
+            gate[u] = 1.f;
+            if (LISTED && r < end) {
+                const int slot = a.list[r];
+                if (a.gates) gate[u] = a.gates[slot];
+                row = slot / a.per;
+            }
+            read_some<T, N>(static_cast<const T *>(a.src) + row * a.ld + col,
+                            r < end ? left : 0, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+#pragma unroll
+            for (int c = 0; c < N; ++c)
+                sum[c] = LISTED ? fmaf(gate[u], v[u][c], sum[c]) : sum[c] + v[u][c];
+            if (LISTED && a.dots) {   // the 32 lanes of a row together
+                float dot = 0.f;
+#pragma unroll
+                for (int c = 0; c < N; ++c) dot = fmaf(v[u][c], bias[c], dot);
+#pragma unroll
+                for (int o = 1; o < kSumPieces; o <<= 1) dot += __shfl_xor(dot, o);
+                const int64_t r = r0 + u * kSumLanes;
+                if (piece == 0 && r < end) a.dots[r * a.dot_cols + blockIdx.x] = dot;
+            }
         }
     }
+    if (LISTED && !a.out) return;
 #pragma unroll
     for (int c = 0; c < N; ++c) part[lane][piece * N + c] = sum[c];
     __syncthreads();
@@ -151,7 +188,7 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a) {
         const int p = a.place[i * a.k + j];
         const float w = a.weight ? a.weight[i * a.k + j] : 1.f;
         if (p >= 0) {
-            read_some<T, N>(static_cast<const T *>(a.y) + p * a.width + col, left, y);
+            read_some<float, N>(a.y + p * a.width + col, left, y);
 #pragma unroll
             for (int e = 0; e < N; ++e) sum[e] = fmaf(w, y[e], sum[e]);
         } else if (w != w) {
@@ -167,39 +204,21 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a) {
     write_some<T, N>(static_cast<T *>(a.out) + i * a.width + col, left, sum);
 }
 
-// One choice of a document a wave: its row of dy, and the product of the two
-// rows, summed over the lanes in a fixed order.
+// Four lanes a slot.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void combine_backward_kernel(CombineArgs a) {
-    constexpr int N = 16 / sizeof(T);
-    const int lane = threadIdx.x & 63;
-    const int64_t s = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-    if (s >= a.n * a.k) return;
-    const int64_t i = s / a.k;
-    const int p = a.place[s];
-    float dot = 0.f;
+__global__ __launch_bounds__(kThreads) void dweight_kernel(DweightArgs a) {
+    const int64_t s = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / 4;
+    const int lane = threadIdx.x & 3;
+    const int p = s < a.slots ? a.place[s] : -1;
+    float v = 0.f;
     if (p >= 0) {
-        const float w = a.weight ? a.weight[s] : 1.f;
-        const T *from = static_cast<const T *>(a.dout) + i * a.ldd;
-        const T *y = static_cast<const T *>(a.y) + p * a.width;
-        T *to = static_cast<T *>(a.dy) + p * a.width;
-        for (int64_t col = lane * N; col < a.width; col += 64 * N) {
-            float d[N], v[N];
-            read_some<T, N>(from + col, a.width - col, d);
-            if (a.dweight) {
-                read_some<T, N>(y + col, a.width - col, v);
 #pragma unroll
-                for (int e = 0; e < N; ++e) dot = fmaf(d[e], v[e], dot);
-            }
-#pragma unroll
-            for (int e = 0; e < N; ++e) d[e] *= w;
-            write_some<T, N>(to + col, a.width - col, d);
-        }
+        for (int h = 0; h < 2; ++h)
+            for (int c = lane; c < a.cols[h]; c += 4) v += a.dots[h][(int64_t)p * a.cols[h] + c];
     }
-    if (a.dweight) {
-        for (int o = 32; o; o >>= 1) dot += __shfl_xor(dot, o);
-        if (lane == 0) static_cast<T *>(a.dweight)[s] = (T)dot;
-    }
+    v += __shfl_xor(v, 1);
+    v += __shfl_xor(v, 2);
+    if (s < a.slots && lane == 0) static_cast<T *>(a.dweight)[s] = (T)v;
 }
 
 template <typename F>
@@ -233,6 +252,11 @@ static int64_t sums_parts(const SumsArgs &a) {
     return a.offsets ? a.rows / kSumRows + a.experts : (a.rows + kSumRows - 1) / kSumRows;
 }
 
+int32_t sums_dot_cols(const SumsArgs &a) {
+    const int64_t wide = 16 * kSumPieces / type_size(a.type);
+    return (int32_t)((a.cols + wide - 1) / wide);
+}
+
 int64_t sums_partial(const SumsArgs &a) { return sums_direct(a) ? 0 : sums_parts(a) * a.cols; }
 
 hipError_t launch_sums(const SumsArgs &a, hipStream_t stream) {
@@ -248,10 +272,12 @@ hipError_t launch_sums(const SumsArgs &a, hipStream_t stream) {
     return by_type(a.type, [&](auto t) {
         using T = decltype(t);
         if (direct) {
-            sums_kernel<T, true><<<grid, kSumThreads, 0, stream>>>(a);
+            if (a.list) sums_kernel<T, true, true><<<grid, kSumThreads, 0, stream>>>(a);
+            else sums_kernel<T, true, false><<<grid, kSumThreads, 0, stream>>>(a);
         } else {
-            sums_kernel<T, false><<<grid, kSumThreads, 0, stream>>>(a);
-            join_sums_kernel<T><<<join, kSumThreads, 0, stream>>>(a);
+            if (a.list) sums_kernel<T, false, true><<<grid, kSumThreads, 0, stream>>>(a);
+            else sums_kernel<T, false, false><<<grid, kSumThreads, 0, stream>>>(a);
+            if (a.out) join_sums_kernel<T><<<join, kSumThreads, 0, stream>>>(a);
         }
     });
 }
@@ -267,12 +293,11 @@ hipError_t launch_combine(const CombineArgs &a, hipStream_t stream) {
     });
 }
 
-hipError_t launch_combine_backward(const CombineArgs &a, hipStream_t stream) {
-    const int64_t slots = a.n * a.k;
-    if (slots == 0) return hipSuccess;
-    const unsigned blocks = (unsigned)((slots + kThreads / 64 - 1) / (kThreads / 64));
+hipError_t launch_dweight(const DweightArgs &a, hipStream_t stream) {
+    if (a.slots == 0) return hipSuccess;
+    const unsigned blocks = (unsigned)((a.slots * 4 + kThreads - 1) / kThreads);
     return by_type(a.type, [&](auto t) {
-        combine_backward_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a);
+        dweight_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a);
     });
 }
 

@@ -278,35 +278,35 @@ struct Piece {
     }
 };
 
-// The activation, or its slope, of N values.
+// The activation of N values.
 template <int N>
 __device__ inline void activate_all(float (&v)[N], int32_t kind) {
-    if (kind == kActNone) return;
     if (kind == kActRelu) {
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = activate(v[e], kActRelu);
     } else if (kind == kActGelu) {
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = activate(v[e], kActGelu);
-    } else {
+    } else if (kind == kActSilu) {
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = activate(v[e], kActSilu);
     }
 }
+// The activation of N values in place of them, and its slopes.
 template <int N>
-__device__ inline void slopes_all(float (&v)[N], int32_t kind) {
+__device__ inline void slopes_all(float (&v)[N], float (&slope)[N], int32_t kind) {
     if (kind == kActRelu) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = activation_slope(v[e], kActRelu);
+        for (int e = 0; e < N; ++e) v[e] = activate(v[e], kActRelu, &slope[e]);
     } else if (kind == kActGelu) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = activation_slope(v[e], kActGelu);
+        for (int e = 0; e < N; ++e) v[e] = activate(v[e], kActGelu, &slope[e]);
     } else if (kind == kActSilu) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = activation_slope(v[e], kActSilu);
+        for (int e = 0; e < N; ++e) v[e] = activate(v[e], kActSilu, &slope[e]);
     } else {
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = 1.f;
+        for (int e = 0; e < N; ++e) slope[e] = 1.f;
     }
 }
 
@@ -328,50 +328,80 @@ struct Epilogue {
     int64_t col;
     int batch, left;
     float bias[N];
+    // Beside a row's sums: its residual (forward) or the argument of its activation
+    // (gate), and the weight of its slot.
+    struct Row {
+        Piece<T, N> piece;
+        float gate;
+    };
     __device__ Epilogue(const ProductArgs &args, int64_t c, int b) : a(args), col(c), batch(b) {
         left = (int)(a.n - col < N ? a.n - col : N);
         Piece<T, N> p;
         const bool there = MODE == kForward && a.bias && left > 0;
-        if (there)
-            p.read(static_cast<const T *>(a.bias) + batch * a.n + col, left);
+        if (there) p.read(static_cast<const T *>(a.bias) + batch * a.n + col, left);
 #pragma unroll
         for (int e = 0; e < N; ++e) bias[e] = there ? (float)p.v[e] : 0.f;
     }
-    // The row's residual (forward) or slope argument (input).
-    __device__ void read(int64_t row, Piece<T, N> &extra) const {
-        if (MODE == kForward && a.residual)
-            extra.read(static_cast<const T *>(a.residual) + row * a.ldr + col, left);
-        if (MODE == kInput && a.slope)
-            extra.read(static_cast<const T *>(a.slope) + row * a.n + col, left);
+    __device__ void read(int64_t row, Row &r) const {
+        if (MODE == kForward) {
+            if (a.residual)
+                r.piece.read(static_cast<const T *>(a.residual) + row * a.ldr + col, left);
+            if (a.scaled) r.gate = a.gates ? a.gates[a.slots[row]] : 1.f;
+        }
+        if (MODE == kGate) {
+            const int slot = a.slots[row];
+            r.gate = a.gates ? a.gates[slot] : 1.f;
+            r.piece.read(static_cast<const T *>(a.argument) +
+                             (a.argument_listed ? slot / a.per : row) * a.ld_argument + col,
+                         left);
+        }
     }
-    __device__ void write(int64_t row, const Piece<T, N> &extra, float (&v)[N]) const {
-        const int64_t at = ((MODE == kWeight ? batch * a.m : 0) + row) * a.n + col;
+    __device__ void store(void *to, int64_t at, const float (&v)[N]) const {
         Piece<T, N> out;
+#pragma unroll
+        for (int e = 0; e < N; ++e) out.v[e] = (T)v[e];
+        out.write(static_cast<T *>(to) + at, left);
+    }
+    // gate: returns the sum of the products with the activation.
+    __device__ float write(int64_t row, const Row &r, float (&v)[N]) const {
+        const int64_t at = ((MODE == kWeight ? batch * a.m : 0) + row) * a.n + col;
+        float dot = 0.f;
         if (MODE == kForward) {
 #pragma unroll
             for (int e = 0; e < N; ++e) v[e] += bias[e];
-            if (a.z) {
-#pragma unroll
-                for (int e = 0; e < N; ++e) out.v[e] = (T)v[e];
-                out.write(static_cast<T *>(a.z) + at, left);
-            }
+            if (a.z) store(a.z, at, v);
             activate_all(v, a.activation);
+            if (a.scaled) {
+                float u[N];
+#pragma unroll
+                for (int e = 0; e < N; ++e) u[e] = r.gate * v[e];
+                store(a.scaled, at, u);
+            }
             if (a.residual) {
 #pragma unroll
-                for (int e = 0; e < N; ++e) v[e] += (float)extra.v[e];
+                for (int e = 0; e < N; ++e) v[e] += (float)r.piece.v[e];
             }
         }
-        if (MODE == kInput && a.slope) {
-            float z[N];
+        if (MODE == kGate) {
+            float h[N], slope[N];
 #pragma unroll
-            for (int e = 0; e < N; ++e) z[e] = (float)extra.v[e];
-            slopes_all(z, a.activation);
+            for (int e = 0; e < N; ++e) h[e] = (float)r.piece.v[e];
+            slopes_all(h, slope, a.activation);
 #pragma unroll
-            for (int e = 0; e < N; ++e) v[e] *= z[e];
+            for (int e = 0; e < N; ++e) {
+                dot = e < left ? fmaf(v[e], h[e], dot) : dot;
+                v[e] *= r.gate * slope[e];
+            }
         }
+        if ((MODE == kForward || MODE == kInput || MODE == kGate) && a.wide) {
+            Piece<float, N> out;
 #pragma unroll
-        for (int e = 0; e < N; ++e) out.v[e] = (T)v[e];
-        out.write(static_cast<T *>(a.y) + at, left);
+            for (int e = 0; e < N; ++e) out.v[e] = v[e];
+            out.write(static_cast<float *>(a.y) + at, left);
+        } else {
+            store(a.y, at, v);
+        }
+        return dot;
     }
 };
 
@@ -383,9 +413,10 @@ struct Epilogue {
 //   multiply the second half
 // so that the matrix cores always have fragments in hand, and a load has a slab's
 // time to arrive.
-template <typename T, int MODE, bool LISTED, bool DMA, int TM, int TN, int WM, int WN>
+template <typename T, int MODE, int LIST, bool DMA, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) {
     constexpr bool kAcrossA = MODE == kWeight, kAcrossB = MODE != kForward;
+    constexpr bool LISTED = LIST != 0;
     using SideA = Side<T, kAcrossA, DMA, TM, WM * WN>;
     using SideB = Side<T, kAcrossB, DMA, TN, WM * WN>;
     constexpr int kTileM = TM / WM, kTileN = TN / WN;    // of a wave
@@ -444,21 +475,24 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
         SideB sb;
         Fragments<T, kAcrossA, TM, FM> ra;
         Fragments<T, kAcrossB, TN, FN> rb;
-        sa.begin(pa, a.lda, row0, row_end, k0, MODE == kWeight ? nullptr : a.list, a.per);
-        sb.begin(pb, a.ldb, col0, a.n, LISTED ? 0 : k0, nullptr, 1);
+        sa.begin(pa, a.lda, row0, row_end, LIST == 2 ? 0 : k0, MODE == kWeight ? nullptr : a.list,
+                 a.per);
+        sb.begin(pb, a.ldb, col0, a.n, LIST == 1 ? 0 : k0, nullptr, 1);
         ra.begin(wm);
         rb.begin(wn);
-        int32_t entry[SideB::kLoads];
-        if (LISTED) {
-            sb.step = 0;
-            SideB::entries(a.list + k0, k_end - k0, entry);
-        }
+        int32_t entry[LIST == 2 ? SideA::kLoads : SideB::kLoads];
+        const auto entries = [&](int64_t s) {
+            if constexpr (LIST == 1) SideB::entries(a.list + k0 + s * kSlab, k_end - k0 - s * kSlab, entry);
+            if constexpr (LIST == 2) SideA::entries(a.list + k0 + s * kSlab, k_end - k0 - s * kSlab, entry);
+        };
+        if (LIST == 1) sb.step = 0;
+        if (LIST == 2) sa.step = 0;
+        entries(0);
         // the offsets of the slab that is loaded next, and the list beyond it
         const auto follow = [&](int64_t s) {
-            if (LISTED) {
-                sb.follow(entry, a.per, a.ldb, col0, a.n);
-                SideB::entries(a.list + k0 + (s + 1) * kSlab, k_end - k0 - (s + 1) * kSlab, entry);
-            }
+            if constexpr (LIST == 1) sb.follow(entry, a.per, a.ldb, col0, a.n);
+            if constexpr (LIST == 2) sa.follow(entry, a.per, a.lda, row0, row_end);
+            entries(s + 1);
         };
         const auto load = [&](auto check, int64_t s) {
             char *to = lds + (s & 1) * kBytes;
@@ -552,7 +586,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
         const int64_t first = row0 + wm + 16 * x0 + lane / kLanes;
 #pragma unroll 1
         for (int p = 0; p < kRowsAt / kPass; p += kGroup) {
-            Piece<T, N> extra[kGroup];
+            typename Epilogue<T, MODE, N>::Row extra[kGroup];
             if (a.splits == 1 && col < a.n) {
 #pragma unroll
                 for (int q = 0; q < kGroup; ++q)
@@ -571,16 +605,23 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
 #pragma unroll
                     for (int c = 0; c < 4; ++c) v[4 * e + c] = u[c];
                 }
-                if (row >= row_end || col >= a.n) continue;
-                if (a.splits > 1) {  // columns are padded to whole tiles
+                const bool there = row < row_end && col < a.n;
+                float dot = 0.f;
+                if (there && a.splits > 1) {  // columns are padded to whole tiles
                     const int64_t at = MODE == kWeight ? (int64_t)batch * a.m + row : row;
                     f4 *to = reinterpret_cast<f4 *>(
                         a.partial + (blockIdx.y * a.partial_rows + at) * (tn * TN) + col);
 #pragma unroll
                     for (int e = 0; e < N / 4; ++e)
                         to[e] = f4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
-                } else {
-                    end.write(row, extra[q], v);
+                } else if (there) {
+                    dot = end.write(row, extra[q], v);
+                }
+                if (MODE == kGate) {   // the lanes of a row together
+#pragma unroll
+                    for (int o = 1; o < kLanes; o <<= 1) dot += __shfl_xor(dot, o);
+                    if (there && lane % kLanes == 0)
+                        a.dots[row * a.dot_cols + (col0 + wn) / kTileN] = dot;
                 }
             }
         }
@@ -616,7 +657,7 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a, int64_t ld) {
                 v += *reinterpret_cast<const f4 *>(a.partial + (s * a.partial_rows + r) * ld + col);
             float u[4] = {v[0], v[1], v[2], v[3]};
             const Epilogue<T, MODE, 4> end(a, col, batch);
-            Piece<T, 4> extra;
+            typename Epilogue<T, MODE, 4>::Row extra;
             end.read(row, extra);
             end.write(row, extra, u);
         }
@@ -690,14 +731,14 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(ProductArgs a, int by_
         if (row < row_end && col < a.n) {
             float u[4] = {acc[0], acc[1], acc[2], acc[3]};
             const Epilogue<T, kForward, 4> end(a, col, batch);
-            Piece<T, 4> extra;
+            typename Epilogue<T, kForward, 4>::Row extra;
             end.read(row, extra);
             end.write(row, extra, u);
         }
     }
 }
 
-template <typename T, int MODE, bool LISTED, bool DMA, int TM, int TN, int WM, int WN>
+template <typename T, int MODE, int LIST, bool DMA, int TM, int TN, int WM, int WN>
 hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
     const int64_t tn = (a.n + TN - 1) / TN;
     const int64_t tm = MODE == kWeight ? (a.m + TM - 1) / TM * (a.offsets ? a.experts : 1)
@@ -705,14 +746,14 @@ hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
                                        : (a.m + TM - 1) / TM;
     if (tm * tn > INT32_MAX) return hipErrorInvalidValue;
     constexpr int kLds = 2 * (TM + TN) * 128;
-    const auto kernel = product_kernel<T, MODE, LISTED, DMA, TM, TN, WM, WN>;
+    const auto kernel = product_kernel<T, MODE, LIST, DMA, TM, TN, WM, WN>;
     if (kLds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
         if (e != hipSuccess) return e;
     }
     kernel<<<dim3((unsigned)(tm * tn), a.splits), WM * WN * 64, kLds, stream>>>(a);
-    if (a.splits > 1) {
+    if (MODE != kGate && a.splits > 1) {
         const int64_t quads = a.partial_rows * ((a.n + 3) / 4);
         if ((quads + 255) / 256 > INT32_MAX) return hipErrorInvalidValue;
         join_kernel<T, MODE><<<(unsigned)((quads + 255) / 256), 256, 0, stream>>>(a, tn * TN);
@@ -720,16 +761,16 @@ hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// LISTED: side B's rows (weight) are named by the list.
-template <typename T, int MODE, bool LISTED>
+// LIST: which side's rows the list names in a weight product, 1 B's, 2 A's.
+template <typename T, int MODE, int LIST>
 hipError_t launch_mode(const ProductArgs &a, const ProductPlan &p, hipStream_t stream) {
     if (!p.aligned)
-        return p.tile == 128 ? launch_tiles<T, MODE, LISTED, false, 128, 128, 2, 2>(a, stream)
-                             : launch_tiles<T, MODE, LISTED, false, 64, 64, 2, 2>(a, stream);
+        return p.tile == 128 ? launch_tiles<T, MODE, LIST, false, 128, 128, 2, 2>(a, stream)
+                             : launch_tiles<T, MODE, LIST, false, 64, 64, 2, 2>(a, stream);
     switch (p.tile) {
-        case 256: return launch_tiles<T, MODE, LISTED, true, 256, 256, 2, 4>(a, stream);
-        case 128: return launch_tiles<T, MODE, LISTED, true, 128, 128, 2, 2>(a, stream);
-        default: return launch_tiles<T, MODE, LISTED, true, 64, 64, 2, 2>(a, stream);
+        case 256: return launch_tiles<T, MODE, LIST, true, 256, 256, 2, 4>(a, stream);
+        case 128: return launch_tiles<T, MODE, LIST, true, 128, 128, 2, 2>(a, stream);
+        default: return launch_tiles<T, MODE, LIST, true, 64, 64, 2, 2>(a, stream);
     }
 }
 
@@ -756,10 +797,13 @@ hipError_t launch_product(ProductArgs a, const ProductPlan &p, hipStream_t strea
         case 16: return launch_rows<T, 16>(a, stream);
     }
     switch (a.mode) {
-        case kForward: return launch_mode<T, kForward, false>(a, p, stream);
-        case kInput: return launch_mode<T, kInput, false>(a, p, stream);
-        default: return a.list ? launch_mode<T, kWeight, true>(a, p, stream)
-                               : launch_mode<T, kWeight, false>(a, p, stream);
+        case kForward: return launch_mode<T, kForward, 0>(a, p, stream);
+        case kInput: return launch_mode<T, kInput, 0>(a, p, stream);
+        case kGate: return launch_mode<T, kGate, 0>(a, p, stream);
+        default:
+            return !a.list       ? launch_mode<T, kWeight, 0>(a, p, stream)
+                   : a.list_of_a ? launch_mode<T, kWeight, 2>(a, p, stream)
+                                 : launch_mode<T, kWeight, 1>(a, p, stream);
     }
 }
 

@@ -24,16 +24,16 @@ from __future__ import annotations
 
 import ctypes as C
 import dataclasses
-from typing import Any, Optional
+from typing import Optional
 
 import torch
 
-from . import SomError, _check, _current_stream, lib as _lib
+from . import SomError, _check, lib as _lib
 
 __all__ = [
     "ACTIVATIONS", "GATES", "EXPORTED", "SomError", "Routing", "ExpertsGradient", "AdamW", "linear",
     "linear_backward", "route", "route_backward", "dispatch", "experts", "experts_backward",
-    "combine", "combine_backward", "gate_from_map",
+    "gate_from_map",
 ]
 
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
@@ -43,10 +43,10 @@ STATE_BLOCK = 256
 
 # Every symbol include/som_local.h declares.
 EXPORTED = (
-    "som_linear_workspace", "som_linear", "som_linear_backward", "som_route",
-    "som_route_backward", "som_dispatch_workspace", "som_dispatch", "som_combine",
-    "som_combine_backward", "som_adamw_room", "som_adamw_create", "som_adamw_destroy",
-    "som_adamw_step",
+    "som_linear_workspace", "som_linear", "som_linear_backward", "som_experts_workspace",
+    "som_experts", "som_experts_backward", "som_route", "som_route_backward",
+    "som_dispatch_workspace", "som_dispatch", "som_adamw_room", "som_adamw_create",
+    "som_adamw_destroy", "som_adamw_step",
 )
 
 
@@ -57,11 +57,26 @@ class _LinearCall(C.Structure):
                 ("inner", C.c_int32), ("outer", C.c_int32), ("x", C.c_void_p),
                 ("ldx", C.c_int64), ("w", C.c_void_p), ("bias", C.c_void_p),
                 ("residual", C.c_void_p), ("ldr", C.c_int64), ("y", C.c_void_p),
-                ("z", C.c_void_p), ("experts", C.c_int32), ("k", C.c_int32),
-                ("gather", C.c_int32), ("offsets", C.c_void_p), ("order", C.c_void_p),
-                ("dy", C.c_void_p), ("lddy", C.c_int64), ("dx", C.c_void_p),
-                ("dw", C.c_void_p), ("dbias", C.c_void_p), ("slope_z", C.c_void_p),
-                ("slope_activation", C.c_int32), ("workspace", C.c_void_p),
+                ("z", C.c_void_p), ("dy", C.c_void_p), ("lddy", C.c_int64),
+                ("dx", C.c_void_p), ("dw", C.c_void_p), ("dbias", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+                ("stream", C.c_void_p)]
+
+
+class _ExpertsCall(C.Structure):
+    """``som_experts_call`` of include/som_local.h."""
+
+    _fields_ = [("type", C.c_int32), ("activation", C.c_int32), ("n", C.c_int64),
+                ("k", C.c_int32), ("experts", C.c_int32), ("inner", C.c_int32),
+                ("hidden", C.c_int32), ("outer", C.c_int32), ("x", C.c_void_p),
+                ("ldx", C.c_int64), ("w1", C.c_void_p), ("b1", C.c_void_p),
+                ("w2", C.c_void_p), ("b2", C.c_void_p), ("residual", C.c_void_p),
+                ("ldr", C.c_int64), ("weight", C.c_void_p), ("offsets", C.c_void_p),
+                ("order", C.c_void_p), ("place", C.c_void_p), ("y", C.c_void_p),
+                ("z", C.c_void_p), ("scaled", C.c_void_p), ("dy", C.c_void_p),
+                ("lddy", C.c_int64), ("dx", C.c_void_p), ("dweight", C.c_void_p),
+                ("dw1", C.c_void_p), ("db1", C.c_void_p), ("dw2", C.c_void_p),
+                ("db2", C.c_void_p), ("workspace", C.c_void_p),
                 ("workspace_bytes", C.c_uint64), ("stream", C.c_void_p)]
 
 
@@ -75,6 +90,8 @@ class _RouteCall(C.Structure):
                 ("lds", C.c_int64), ("bias", C.c_void_p), ("index", C.c_void_p),
                 ("weight", C.c_void_p), ("dweight", C.c_void_p),
                 ("dweight_type", C.c_int32), ("dscores", C.c_void_p),
+                ("offsets", C.c_void_p), ("order", C.c_void_p), ("place", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
                 ("stream", C.c_void_p)]
 
 
@@ -98,12 +115,13 @@ def lib():
         "som_linear_workspace": [C.POINTER(_LinearCall), i32, C.POINTER(u64)],
         "som_linear": [C.POINTER(_LinearCall)],
         "som_linear_backward": [C.POINTER(_LinearCall)],
+        "som_experts_workspace": [C.POINTER(_ExpertsCall), i32, C.POINTER(u64)],
+        "som_experts": [C.POINTER(_ExpertsCall)],
+        "som_experts_backward": [C.POINTER(_ExpertsCall)],
         "som_route": [C.POINTER(_RouteCall)],
         "som_route_backward": [C.POINTER(_RouteCall)],
         "som_dispatch_workspace": [i64, i32, i32, C.POINTER(u64)],
         "som_dispatch": [vp, i64, i32, i32, vp, vp, vp, vp, u64, vp],
-        "som_combine": [i32, i64, i32, i32, vp, vp, vp, vp, i64, vp, vp],
-        "som_combine_backward": [i32, i64, i32, i32, vp, i64, vp, vp, vp, vp, vp, vp],
         "som_adamw_create": [C.POINTER(_AdamwTensor), i32, i32, vp, vp, vp, vp, vp,
                              C.POINTER(vp)],
         "som_adamw_destroy": [vp],
@@ -174,20 +192,27 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _work(nbytes: int, device):
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+def _stream(t) -> int:
+    """The current stream of t's device, which has to be the current one."""
+    index = t.device.index
+    if index != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors must be on the current device, not {t.device}")
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
-def _run_linear(call: _LinearCall, backward: bool, device) -> None:
+def _run(name: str, call, backward: bool, x) -> None:
+    """A call that takes work memory, on x's device."""
     L = lib()
     need = C.c_uint64()
-    name = "som_linear_backward" if backward else "som_linear"
-    _check(L.som_linear_workspace(C.byref(call), int(backward), C.byref(need)), name)
-    work = _work(need.value, device)
-    call.workspace = _ptr(work)
-    call.workspace_bytes = need.value
-    call.stream = _current_stream()
-    _check(getattr(L, name)(C.byref(call)), name)
+    call.stream = _stream(x)
+    at = C.byref(call)
+    run = f"som_{name}_backward" if backward else f"som_{name}"
+    _check(getattr(L, f"som_{name}_workspace")(at, backward, C.byref(need)), run)
+    if need.value:
+        work = torch.empty(need.value, dtype=torch.uint8, device=x.device)
+        call.workspace = work.data_ptr()
+        call.workspace_bytes = need.value
+    _check(getattr(L, run)(at), run)
 
 
 # ------------------------------------------------------------------ product
@@ -220,7 +245,7 @@ def linear(x, w, bias=None, activation: str = "none", residual=None, keep: bool 
     y = torch.empty((n, outer), dtype=x.dtype, device=x.device)
     z = torch.empty_like(y) if keep and activation != "none" else None
     call.y, call.z = _ptr(y), _ptr(z)
-    _run_linear(call, False, x.device)
+    _run("linear", call, False, x)
     return (y, z) if keep else y
 
 
@@ -240,35 +265,61 @@ def linear_backward(dy, x, w, z=None, activation: str = "none", bias: bool = Tru
     dw = torch.empty_like(w)
     dbias = torch.empty(outer, dtype=x.dtype, device=x.device) if bias else None
     call.dx, call.dw, call.dbias = _ptr(dx), _ptr(dw), _ptr(dbias)
-    _run_linear(call, True, x.device)
+    _run("linear", call, True, x)
     return dx, dw, dbias
 
 
 # ------------------------------------------------------------------ routing
-@dataclasses.dataclass
 class Routing:
     """Which experts the documents go to: index (n, k) int32, -1 for none;
-    weight (n, k) fp32; the slots i k + j in the order of their experts (order),
-    each slot's row in it (place, -1 for none) and each expert's first row
-    (offsets, experts + 1 entries); and how the choice was made."""
+    weight (n, k) fp32, or None for 1; the slots i k + j in the order of their
+    experts (``order``), each slot's row in it (``place``, -1 for none) and each
+    expert's first row (``offsets``, experts + 1 entries), all int32; and how the
+    choice was made (gate, renormalise, scale), for its gradient."""
 
-    index: torch.Tensor
-    weight: torch.Tensor
-    experts: int
-    offsets: torch.Tensor
-    order: torch.Tensor
-    place: torch.Tensor
-    gate: str = ""
-    renormalise: bool = True
-    scale: float = 1.0
+    __slots__ = ("index", "weight", "experts", "gate", "renormalise", "scale", "_ints")
+
+    def __init__(self, index, weight, experts: int, ints, gate: str = "",
+                 renormalise: bool = True, scale: float = 1.0):
+        self.index, self.weight, self.experts, self._ints = index, weight, experts, ints
+        self.gate, self.renormalise, self.scale = gate, renormalise, scale
+
+    # one allocation: order, place, offsets
+    @property
+    def order(self):
+        return self._ints[:self.index.numel()]
+
+    @property
+    def place(self):
+        slots = self.index.numel()
+        return self._ints[slots:2 * slots]
+
+    @property
+    def offsets(self):
+        return self._ints[2 * self.index.numel():]
 
     @property
     def load(self):
         """Documents of each expert, int32."""
         return self.offsets[1:] - self.offsets[:-1]
 
+    def _pointers(self):
+        """Addresses of offsets, order and place."""
+        at, slots = self._ints.data_ptr(), self.index.numel()
+        return at + 8 * slots, at, at + 4 * slots
 
-def dispatch(index, weight, experts: int, **how) -> Routing:
+
+def _order_of(index, weight, experts: int, device, **how):
+    """A Routing with room for its order, and the work memory the sort takes."""
+    n, k = index.shape
+    need = C.c_uint64()
+    _check(lib().som_dispatch_workspace(n, k, experts, C.byref(need)), "som_dispatch")
+    ints = torch.empty(2 * n * k + experts + 1, dtype=torch.int32, device=device)
+    work = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
+    return Routing(index, weight, experts, ints, **how), work, need.value
+
+
+def dispatch(index, weight, experts: int) -> Routing:
     """The Routing of a given assignment: index (n, k) int32 with entries in [0,
     experts) or -1, weight (n, k) fp32 (None: 1).  For example the best units of
     ``Map.bmu``."""
@@ -281,22 +332,17 @@ def dispatch(index, weight, experts: int, **how) -> Routing:
         if not isinstance(weight, torch.Tensor) or weight.dtype != torch.float32:
             raise TypeError("weight must be float32")
         _shaped(weight, index, (n, k), "weight")
-    L, need = lib(), C.c_uint64()
-    _check(L.som_dispatch_workspace(n, k, experts, C.byref(need)), "som_dispatch")
-    ints = torch.empty(2 * n * k + experts + 1, dtype=torch.int32, device=index.device)
-    order, place, offsets = ints[:n * k], ints[n * k:2 * n * k], ints[2 * n * k:]
-    work = _work(need.value, index.device)
-    _check(L.som_dispatch(_ptr(index), n, k, experts, _ptr(offsets), _ptr(order), _ptr(place),
-                          _ptr(work), need.value, _current_stream()), "som_dispatch")
-    return Routing(index, weight, experts, offsets, order, place, **how)
+    r, work, need = _order_of(index, weight, experts, index.device)
+    _check(lib().som_dispatch(index.data_ptr(), n, k, experts, *r._pointers(), _ptr(work), need,
+                              _stream(index)), "som_dispatch")
+    return r
 
 
 def _route_call(scores, k: int):
     code = _type(scores, "scores")
     _rows(scores, "scores")
-    return _RouteCall(type=code, n=scores.shape[0], experts=scores.shape[1], k=k,
-                      scores=_ptr(scores), lds=_ld(scores), groups=1, top_groups=1,
-                      group_best=1, stream=_current_stream())
+    n, experts = scores.shape
+    return _RouteCall(code, 0, n, experts, k, 1, 1, 1, 1, 1.0, scores.data_ptr(), _ld(scores))
 
 
 def route(scores, k: int, bias=None, gate: str = "softmax", groups: int = 1,
@@ -318,14 +364,20 @@ def route(scores, k: int, bias=None, gate: str = "softmax", groups: int = 1,
         if not isinstance(bias, torch.Tensor) or bias.dtype != torch.float32:
             raise TypeError("bias must be float32")
         _shaped(bias, scores, (experts,), "bias")
-        call.bias = _ptr(bias)
+        call.bias = bias.data_ptr()
     if k < 1:
         raise ValueError("k must be at least 1")
-    index = torch.empty((n, k), dtype=torch.int32, device=scores.device)
-    weight = torch.empty((n, k), dtype=torch.float32, device=scores.device)
-    call.index, call.weight = _ptr(index), _ptr(weight)
+    device = scores.device
+    index = torch.empty((n, k), dtype=torch.int32, device=device)
+    weight = torch.empty((n, k), dtype=torch.float32, device=device)
+    r, work, need = _order_of(index, weight, experts, device, gate=gate,
+                              renormalise=renormalise, scale=scale)
+    call.index, call.weight = index.data_ptr(), weight.data_ptr()
+    call.offsets, call.order, call.place = r._pointers()
+    call.workspace, call.workspace_bytes = _ptr(work), need
+    call.stream = _stream(scores)
     _check(lib().som_route(C.byref(call)), "som_route")
-    return dispatch(index, weight, experts, gate=gate, renormalise=renormalise, scale=scale)
+    return r
 
 
 def route_backward(dweight, scores, routing: Routing):
@@ -337,97 +389,18 @@ def route_backward(dweight, scores, routing: Routing):
     _shaped(scores, routing.index, (n, routing.experts), "scores", packed=False)
     call.gate = GATES[routing.gate]
     call.renormalise, call.scale = int(routing.renormalise), routing.scale
-    call.index, call.weight = _ptr(routing.index), _ptr(routing.weight)
+    call.index, call.weight = routing.index.data_ptr(), routing.weight.data_ptr()
     call.dweight_type = _type(dweight, "dweight")
     _shaped(dweight, scores, (n, k), "dweight")
-    call.dweight = _ptr(dweight)
+    call.dweight = dweight.data_ptr()
     dscores = torch.empty((n, routing.experts), dtype=scores.dtype, device=scores.device)
-    call.dscores = _ptr(dscores)
+    call.dscores = dscores.data_ptr()
+    call.stream = _stream(scores)
     _check(lib().som_route_backward(C.byref(call)), "som_route_backward")
     return dscores
 
 
 # ------------------------------------------------------------------ experts
-def _expert_call(x, routing: Routing, w, activation: str, gather: bool):
-    code = _type(x, "x")
-    _rows(x, "x")
-    n, k = routing.index.shape
-    if w.dim() != 3:
-        raise ValueError("the experts' matrices must be (experts, outer, inner)")
-    _like(w, x, (routing.experts, w.shape[1], x.shape[1]), "the experts' matrices")
-    if not w.numel():
-        raise ValueError("the experts' matrices must not be empty")
-    rows = n if gather else n * k
-    if x.shape[0] != rows:
-        raise ValueError(f"x must have {rows} rows")
-    if routing.index.device != x.device:
-        raise ValueError(f"the routing must be on {x.device}")
-    return _LinearCall(type=code, activation=_of(ACTIVATIONS, activation, "activation"), n=n,
-                       inner=x.shape[1], outer=w.shape[1], x=_ptr(x), ldx=_ld(x), w=_ptr(w),
-                       experts=routing.experts, k=k, gather=int(gather),
-                       offsets=_ptr(routing.offsets), order=_ptr(routing.order))
-
-
-def _expert_linear(x, routing, w, bias, activation, gather, keep):
-    call = _expert_call(x, routing, w, activation, gather)
-    rows, outer = routing.index.numel(), w.shape[1]
-    if bias is not None:
-        _like(bias, x, (routing.experts, outer), "the experts' bias")
-        call.bias = _ptr(bias)
-    y = torch.empty((rows, outer), dtype=x.dtype, device=x.device)
-    z = torch.empty_like(y) if keep and activation != "none" else None
-    call.y, call.z = _ptr(y), _ptr(z)
-    _run_linear(call, False, x.device)
-    return y, z
-
-
-def _expert_linear_backward(dy, x, routing, w, has_bias, gather, slope_z=None,
-                            slope_activation="none"):
-    """(dx, dw, dbias) from the gradient dy of the product itself."""
-    call = _expert_call(x, routing, w, "none", gather)
-    rows = routing.index.numel()
-    call.dy, call.lddy = _ptr(dy), _ld(dy)
-    dx = torch.empty((rows, x.shape[1]), dtype=x.dtype, device=x.device)
-    dw = torch.empty_like(w)
-    dbias = torch.empty(w.shape[:2], dtype=x.dtype, device=x.device) if has_bias else None
-    call.dx, call.dw, call.dbias = _ptr(dx), _ptr(dw), _ptr(dbias)
-    if slope_z is not None:
-        call.slope_z, call.slope_activation = _ptr(slope_z), ACTIVATIONS[slope_activation]
-    _run_linear(call, True, x.device)
-    return dx, dw, dbias
-
-
-def combine(y, routing: Routing, residual=None, weighted: bool = True):
-    """residual + the sum of each document's rows of y (one per slot, in the
-    experts' order), times ``routing.weight`` if ``weighted``."""
-    n, k = routing.index.shape
-    code = _type(y, "y")
-    _like(y, y, (n * k, y.shape[-1]), "y")
-    if residual is not None:
-        _like(residual, y, (n, y.shape[1]), "residual", packed=False)
-    out = torch.empty((n, y.shape[1]), dtype=y.dtype, device=y.device)
-    _check(lib().som_combine(code, n, k, y.shape[1], _ptr(y),
-                             _ptr(routing.weight) if weighted else None, _ptr(routing.place),
-                             _ptr(residual), _ld(residual) if residual is not None else 0,
-                             _ptr(out), _current_stream()), "som_combine")
-    return out
-
-
-def combine_backward(dout, y, routing: Routing):
-    """(dy, dweight) of ``combine`` from the gradient of its result."""
-    n, k = routing.index.shape
-    code = _type(y, "y")
-    _like(y, y, (n * k, y.shape[-1]), "y")
-    _like(dout, y, (n, y.shape[1]), "dout", packed=False)
-    dy = torch.empty_like(y)
-    dweight = torch.empty((n, k), dtype=y.dtype, device=y.device)
-    _check(lib().som_combine_backward(code, n, k, y.shape[1], _ptr(dout), _ld(dout), _ptr(y),
-                                      _ptr(routing.weight), _ptr(routing.place), _ptr(dy),
-                                      _ptr(dweight), _current_stream()),
-           "som_combine_backward")
-    return dy, dweight
-
-
 @dataclasses.dataclass
 class ExpertsGradient:
     """Gradients of ``experts``; those of absent arguments are None."""
@@ -440,6 +413,37 @@ class ExpertsGradient:
     b2: Optional[torch.Tensor]
 
 
+def _experts_call(x, routing: Routing, w1, b1, w2, b2, activation: str):
+    code = _type(x, "x")
+    _rows(x, "x")
+    n, k = routing.index.shape
+    e = routing.experts
+    if x.shape[0] != n:
+        raise ValueError(f"x must have {n} rows")
+    if w1.dim() != 3 or not w1.numel():
+        raise ValueError("w1 must be (experts, hidden, inner)")
+    hidden, inner = w1.shape[1], x.shape[1]
+    _like(w1, x, (e, hidden, inner), "w1")
+    if b1 is not None:
+        _like(b1, x, (e, hidden), "b1")
+    outer, act = hidden, 0
+    if w2 is not None:
+        act = _of(ACTIVATIONS, activation, "activation")
+        if w2.dim() != 3 or not w2.numel():
+            raise ValueError("w2 must be (experts, outer, hidden)")
+        outer = w2.shape[1]
+        _like(w2, x, (e, outer, hidden), "w2")
+        if b2 is not None:
+            _like(b2, x, (e, outer), "b2")
+    elif b2 is not None:
+        raise ValueError("b2 without w2")
+    if routing.index.device != x.device:
+        raise ValueError(f"the routing must be on {x.device}")
+    return _ExpertsCall(code, act, n, k, e, inner, hidden, outer, x.data_ptr(), _ld(x),
+                        w1.data_ptr(), _ptr(b1), _ptr(w2), _ptr(b2), None, 0,
+                        _ptr(routing.weight), *routing._pointers())
+
+
 def experts(x, routing: Routing, w1, b1=None, w2=None, b2=None, activation: str = "gelu",
             residual=None, keep: bool = False):
     """The routed experts' answers to the documents x (n, inner), joined:
@@ -449,31 +453,45 @@ def experts(x, routing: Routing, w1, b1=None, w2=None, b2=None, activation: str 
     with e = index[:, j], w1 (experts, hidden, inner), w2 (experts, outer,
     hidden); without w2 the local linear maps w1_e x + b1_e.  With ``keep``
     returns (y, kept), kept being what ``experts_backward`` needs."""
-    if w2 is None:
-        if b2 is not None:
-            raise ValueError("b2 without w2")
-        answer, _ = _expert_linear(x, routing, w1, b1, "none", True, False)
-        kept = (None, None, answer)
-    else:
-        h, z = _expert_linear(x, routing, w1, b1, activation, True, keep)
-        answer, _ = _expert_linear(h, routing, w2, b2, "none", False, False)
-        kept = (h, z, answer)
-    y = combine(answer, routing, residual)
+    call = _experts_call(x, routing, w1, b1, w2, b2, activation)
+    n = x.shape[0]
+    if residual is not None:
+        _like(residual, x, (n, call.outer), "residual", packed=False)
+        call.residual, call.ldr = residual.data_ptr(), _ld(residual)
+    y = torch.empty((n, call.outer), dtype=x.dtype, device=x.device)
+    call.y = y.data_ptr()
+    kept = None
+    if keep and w2 is not None:
+        kept = torch.empty((2, routing.index.numel(), call.hidden), dtype=x.dtype,
+                           device=x.device)
+        call.z, call.scaled = kept[0].data_ptr(), kept[1].data_ptr()
+    _run("experts", call, False, x)
     return (y, kept) if keep else y
 
 
-def experts_backward(dy, x, routing: Routing, w1, b1, w2, b2, kept: Any,
+def experts_backward(dy, x, routing: Routing, w1, b1, w2, b2, kept,
                      activation: str = "gelu") -> ExpertsGradient:
     """Gradients of ``experts`` from that of its result; the residual's is dy."""
-    h, z, answer = kept
-    danswer, dweight = combine_backward(dy, answer, routing)
-    dw2 = db2 = None
+    call = _experts_call(x, routing, w1, b1, w2, b2, activation)
+    n, k = routing.index.shape
+    _like(dy, x, (n, call.outer), "dy", packed=False)
+    call.dy, call.lddy = dy.data_ptr(), _ld(dy)
     if w2 is not None:
-        danswer, dw2, db2 = _expert_linear_backward(danswer, h, routing, w2, b2 is not None,
-                                                    False, z, activation)
-    dslots, dw1, db1 = _expert_linear_backward(danswer, x, routing, w1, b1 is not None, True)
-    dx = combine(dslots, routing, weighted=False)
-    return ExpertsGradient(dx, dweight, dw1, db1, dw2, db2)
+        if kept is None:
+            raise ValueError("the gradient needs what experts(keep=True) kept")
+        _like(kept, x, (2, n * k, call.hidden), "kept")
+        call.z, call.scaled = kept[0].data_ptr(), kept[1].data_ptr()
+
+    def like(t):
+        return None if t is None else torch.empty_like(t)
+
+    d = ExpertsGradient(torch.empty((n, x.shape[1]), dtype=x.dtype, device=x.device),
+                        torch.empty((n, k), dtype=x.dtype, device=x.device),
+                        like(w1), like(b1), like(w2), like(b2))
+    call.dx, call.dweight = d.x.data_ptr(), d.weight.data_ptr()
+    call.dw1, call.db1, call.dw2, call.db2 = _ptr(d.w1), _ptr(d.b1), _ptr(d.w2), _ptr(d.b2)
+    _run("experts", call, True, x)
+    return d
 
 
 def gate_from_map(weights, tau: float, dtype=torch.float32):
@@ -560,7 +578,7 @@ class AdamW:
             self._ptrs[i] = g.data_ptr() or None
         _check(lib().som_adamw_step(self.handle, self._ptrs, self._codes, self.steps + 1,
                                     self.lr if lr is None else lr, *self.betas, self.eps,
-                                    self.weight_decay, _current_stream()), "som_adamw_step")
+                                    self.weight_decay, _stream(self.params[0])), "som_adamw_step")
         self.steps += 1
 
     def close(self) -> None:

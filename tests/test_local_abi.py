@@ -25,6 +25,7 @@ def test_library_exports_every_declared_symbol():
 
 
 @pytest.mark.parametrize("struct,binding", [("som_linear_call", local._LinearCall),
+                                            ("som_experts_call", local._ExpertsCall),
                                             ("som_route_call", local._RouteCall),
                                             ("som_adamw_tensor", local._AdamwTensor)])
 def test_structures_have_the_header_s_fields_in_order(struct, binding):
@@ -52,10 +53,10 @@ def _linear(**change):
 @pytest.mark.parametrize("change,want", [
     (dict(type=3), "SOM_E_ARG"), (dict(activation=-1), "SOM_E_ARG"),
     (dict(activation=4), "SOM_E_ARG"), (dict(n=-1), "SOM_E_ARG"), (dict(inner=0), "SOM_E_ARG"),
-    (dict(outer=-2), "SOM_E_ARG"), (dict(ldx=7), "SOM_E_ARG"), (dict(experts=-1), "SOM_E_ARG"),
-    (dict(experts=2, k=0), "SOM_E_ARG"), (dict(k=2), "SOM_E_ARG"), (dict(gather=1), "SOM_E_ARG"),
-    (dict(experts=4, k=2, n=1 << 31), "SOM_E_UNSUPPORTED"),
-    (dict(experts=1 << 20, k=1, outer=1 << 20), "SOM_E_UNSUPPORTED"), ({}, "SOM_E_ARG")])
+    (dict(outer=-2), "SOM_E_ARG"), (dict(ldx=7), "SOM_E_ARG"),
+    (dict(inner=4000001, ldx=4000001), "SOM_E_UNSUPPORTED"),
+    (dict(outer=4000001), "SOM_E_UNSUPPORTED"), (dict(n=1 << 41), "SOM_E_UNSUPPORTED"),
+    ({}, "SOM_E_ARG")])
 def test_linear_refuses(change, want):
     L = local.lib()
     call = _linear(**change)          # without arrays: even good sizes are refused
@@ -63,6 +64,24 @@ def test_linear_refuses(change, want):
     assert status(L.som_linear_backward(C.byref(call))) == want
     need = C.c_uint64()
     assert status(L.som_linear_workspace(C.byref(call), 0, C.byref(need))) == (
+        want if change else "SOM_OK")
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(type=3), "SOM_E_ARG"), (dict(activation=9), "SOM_E_ARG"), (dict(n=-1), "SOM_E_ARG"),
+    (dict(k=0), "SOM_E_ARG"), (dict(experts=0), "SOM_E_ARG"), (dict(inner=0), "SOM_E_ARG"),
+    (dict(hidden=0), "SOM_E_ARG"), (dict(ldx=3), "SOM_E_ARG"),
+    (dict(w2=None, activation=1), "SOM_E_ARG"), (dict(w2=None, b2=1), "SOM_E_ARG"),
+    (dict(w2=None, outer=9), "SOM_E_ARG"), (dict(w2=None, z=1, scaled=1), "SOM_E_ARG"),
+    (dict(n=1 << 31), "SOM_E_UNSUPPORTED"), (dict(hidden=4000001), "SOM_E_UNSUPPORTED"),
+    (dict(experts=1 << 20, hidden=1 << 20), "SOM_E_UNSUPPORTED"), ({}, "SOM_E_ARG")])
+def test_experts_refuses(change, want):
+    values = dict(n=4, k=2, experts=3, inner=8, hidden=8, outer=8, ldx=8, lddy=8, w2=1)
+    values.update(change)
+    L, call, need = local.lib(), local._ExpertsCall(**values), C.c_uint64()
+    assert status(L.som_experts(C.byref(call))) == want
+    assert status(L.som_experts_backward(C.byref(call))) == want
+    assert status(L.som_experts_workspace(C.byref(call), 1, C.byref(need))) == (
         want if change else "SOM_OK")
 
 
@@ -75,8 +94,8 @@ def test_null_calls():
     assert L.som_route(None) == 1 and L.som_route_backward(None) == 1
     assert L.som_dispatch(None, 4, 2, 8, None, None, None, None, 0, None) == 1
     assert L.som_dispatch_workspace(4, 2, 8, None) == 1
-    assert L.som_combine(0, 4, 2, 8, None, None, None, None, 0, None, None) == 1
-    assert L.som_combine_backward(0, 4, 2, 8, None, 8, None, None, None, None, None, None) == 1
+    assert L.som_experts(None) == 1 and L.som_experts_backward(None) == 1
+    assert L.som_experts_workspace(None, 0, C.byref(need)) == 1
     assert L.som_adamw_destroy(None) == 0
     assert L.som_adamw_step(None, None, None, 1, 0.1, 0.9, 0.9, 1e-8, 0.0, None) == 1
     assert L.som_adamw_create(None, 1, 32, None, None, None, None, None, None) == 1
@@ -101,7 +120,6 @@ def test_slots_beyond_32_bits():
     call = local._RouteCall(n=1 << 31, experts=8, k=2, groups=1, top_groups=1, group_best=1,
                             scale=1.0, lds=8)
     assert status(L.som_route(C.byref(call))) == "SOM_E_UNSUPPORTED"
-    assert L.som_combine(0, 1 << 31, 2, 8, None, None, None, None, 0, None, None) == 6
 
 
 def test_workspace_grows_with_what_a_call_needs():
