@@ -139,7 +139,7 @@ struct SideRows {
     const void *p = nullptr;
     int64_t rows = 0, cols = 0, ld = 0;
     const int32_t **list = nullptr;  // names `listed` of the rows, list[r] / per
-    int32_t per = 1;
+    som::Divider per;
     int64_t listed = 0;
     som::RowsArgs copy{};
     bool copied = false;
@@ -243,7 +243,7 @@ SideRows side(const void *p, int64_t rows, int64_t cols, int64_t ld) {
 // where a copy in that order takes the rows' place.
 void by_slot(SideRows &s, const int32_t **list, const int32_t *order, int32_t k, int64_t slots) {
     *list = order;
-    s.list = list, s.per = k, s.listed = slots;
+    s.list = list, s.per = som::Divider(k), s.listed = slots;
 }
 
 // What a call enqueues, over the caller's work memory.
@@ -256,7 +256,6 @@ struct LinearForward {
         a.type = c.type;
         a.activation = c.activation;
         a.m = c.n, a.n = c.outer, a.k = c.inner;
-        a.per = 1;
         a.bias = c.bias;
         a.residual = c.residual, a.ldr = c.ldr;
         a.y = c.y, a.z = c.z;
@@ -286,8 +285,7 @@ struct LinearBackward {
             a.mode = som::kInput;
             a.type = c.type;
             a.m = c.n, a.n = c.inner, a.k = c.outer;
-            a.per = 1;
-            a.y = c.dx;
+                a.y = c.dx;
             w = side(c.w, c.outer, c.inner, c.inner);
             input.place(work, dz, w);
         }
@@ -296,8 +294,7 @@ struct LinearBackward {
             a.mode = som::kWeight;
             a.type = c.type;
             a.m = c.outer, a.n = c.inner, a.k = c.n;
-            a.per = 1;
-            a.y = c.dw;
+                a.y = c.dw;
             x = side(c.x, c.n, c.inner, c.ldx);
             weight.place(work, dz, x);
         }
@@ -327,6 +324,7 @@ struct ExpertsForward {
     ExpertsForward(const som_experts_call &c, Carver &work) {
         const int size = som::type_size(c.type);
         const int64_t slots = c.n * c.k;
+        const som::Divider per(c.k);
         two = c.w2 != nullptr;
         float *const answers = work.take<float>((uint64_t)slots * c.outer * 4);
         void *const hidden = two ? work.take((uint64_t)slots * c.hidden * size) : nullptr;
@@ -334,7 +332,7 @@ struct ExpertsForward {
         a.mode = som::kForward;
         a.type = c.type;
         a.m = slots, a.n = c.hidden, a.k = c.inner;
-        a.offsets = c.offsets, a.experts = c.experts, a.per = c.k;
+        a.offsets = c.offsets, a.experts = c.experts, a.per = per;
         a.slots = c.order, a.gates = c.weight;
         a.bias = c.b1;
         a.activation = c.activation;
@@ -350,7 +348,7 @@ struct ExpertsForward {
             b.mode = som::kForward;
             b.type = c.type;
             b.m = slots, b.n = c.outer, b.k = c.hidden;
-            b.offsets = c.offsets, b.experts = c.experts, b.per = c.k;
+            b.offsets = c.offsets, b.experts = c.experts, b.per = per;
             b.bias = c.b2;
             b.wide = 1;
             b.y = answers;
@@ -388,6 +386,7 @@ struct ExpertsBackward {
     ExpertsBackward(const som_experts_call &c, Carver &work) {
         const int size = som::type_size(c.type);
         const int64_t slots = c.n * c.k;
+        const som::Divider per(c.k);
         two = c.w2 != nullptr;
         has_rows = slots != 0;
         const int32_t width = two ? c.hidden : c.inner;   // of the last layer's input
@@ -402,7 +401,7 @@ struct ExpertsBackward {
             a.mode = som::kGate;
             a.type = c.type;
             a.m = slots, a.n = width, a.k = c.outer;
-            a.offsets = c.offsets, a.experts = c.experts, a.per = c.k;
+            a.offsets = c.offsets, a.experts = c.experts, a.per = per;
             a.slots = c.order, a.gates = c.weight;
             a.activation = two ? c.activation : SOM_ACT_NONE;
             a.argument = two ? c.z : c.x;
@@ -427,7 +426,7 @@ struct ExpertsBackward {
             a.mode = som::kWeight;
             a.type = c.type;
             a.m = c.outer, a.n = width, a.k = slots;
-            a.offsets = c.offsets, a.experts = c.experts, a.per = c.k;
+            a.offsets = c.offsets, a.experts = c.experts, a.per = per;
             a.list_of_a = 1;
             a.y = dw_last;
             dy_weight = side(c.dy, c.n, c.outer, c.lddy);
@@ -437,7 +436,7 @@ struct ExpertsBackward {
                 scaled.rows = slots;
                 scaled.make_copy(work, c.type);
                 scaled.copy.list = c.order;
-                scaled.copy.per = c.k;
+                scaled.copy.per = per;
                 scaled.copy.gates = c.weight;
             }
             last_weight.place(work, dy_weight, scaled);
@@ -449,7 +448,7 @@ struct ExpertsBackward {
             s.src = c.dy;
             s.rows = slots, s.cols = c.outer, s.ld = c.lddy;
             s.offsets = c.offsets, s.experts = c.experts;
-            s.list = c.order, s.per = c.k, s.gates = c.weight;
+            s.list = c.order, s.per = per, s.gates = c.weight;
             s.out = db_last;
             s.partial = work.take<float>((uint64_t)som::sums_partial(s) * 4);
             if (c.dweight && b_last) {
@@ -469,7 +468,7 @@ struct ExpertsBackward {
             a.mode = som::kWeight;
             a.type = c.type;
             a.m = c.hidden, a.n = c.inner, a.k = slots;
-            a.offsets = c.offsets, a.experts = c.experts, a.per = c.k;
+            a.offsets = c.offsets, a.experts = c.experts, a.per = per;
             a.y = c.dw1;
             dz_weight = side(dz, slots, c.hidden, c.hidden);
             x = side(c.x, c.n, c.inner, c.ldx);
@@ -490,7 +489,7 @@ struct ExpertsBackward {
             a.mode = som::kInput;
             a.type = c.type;
             a.m = slots, a.n = c.inner, a.k = c.hidden;
-            a.offsets = c.offsets, a.experts = c.experts, a.per = c.k;
+            a.offsets = c.offsets, a.experts = c.experts, a.per = per;
             a.wide = 1;
             a.y = parts;
             dz_input = side(dz, slots, c.hidden, c.hidden);

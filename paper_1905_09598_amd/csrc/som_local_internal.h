@@ -63,6 +63,23 @@ __device__ inline float activate(float z, int32_t kind, float *slope = nullptr) 
     }
 }
 
+// Division of whole numbers below 2^31 by one that is not known when compiling: a
+// product with a rounded-up reciprocal and a shift.
+struct Divider {
+    uint32_t by, magic, shift;
+    Divider() : by(1), magic(0), shift(0) {}
+    explicit Divider(uint32_t d) : by(d), magic(0), shift(0) {
+        uint32_t log = 0;
+        while ((uint64_t)1 << log < d) ++log;
+        if (log == 0) return;
+        shift = log - 1;
+        magic = (uint32_t)((((uint64_t)1 << (32 + shift)) / d) + 1);
+    }
+    __device__ uint32_t quotient(uint32_t v) const {
+        return magic ? __umulhi(v, magic) >> shift : v;
+    }
+};
+
 // Largest e in [0, experts) whose first tile offsets[e] / tile + e is at most
 // t, or with tile = 0 whose first row is at most t: 64 places tested at a time.
 // (An expert of c rows from row o on has the tiles from o / tile + e on; the next
@@ -108,7 +125,8 @@ struct ProductArgs {
     int64_t ldr;
     void *y, *z, *scaled;
     const int32_t *offsets, *list, *slots;
-    int32_t experts, per, list_of_a;
+    int32_t experts, list_of_a;
+    Divider per;
     const float *gates;               // by slot; gate: null for 1
     const void *argument;             // gate: rows of n, ld_argument apart
     int64_t ld_argument;
@@ -140,8 +158,9 @@ struct RowsArgs {
     void *dst;
     int64_t rows, cols, lds, ldz, ldd;
     const int32_t *list;
-    int32_t per;
+    Divider per;
     const float *gates;     // times gates[list[r]]
+    Divider pieces;         // of a row of dst
 };
 hipError_t launch_rows_copy(const RowsArgs &a, hipStream_t stream);
 
@@ -156,7 +175,7 @@ struct SumsArgs {
     const int32_t *offsets;
     int32_t experts;
     const int32_t *list;
-    int32_t per;
+    Divider per;
     const float *gates;
     const void *bias;
     float *dots;
@@ -178,6 +197,7 @@ struct CombineArgs {
     const void *residual;
     int64_t ldr;
     void *out;
+    Divider pieces;         // of a row of out
 };
 hipError_t launch_combine(const CombineArgs &a, hipStream_t stream);
 

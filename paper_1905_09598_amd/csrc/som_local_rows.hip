@@ -5,6 +5,8 @@
 // where the rows allow it.
 #include "som_local_internal.h"
 
+#include <algorithm>
+
 namespace som {
 namespace {
 
@@ -49,13 +51,13 @@ __device__ inline float slope_of(float z, int32_t kind) {
 template <typename T>
 __global__ __launch_bounds__(kThreads) void rows_copy_kernel(RowsArgs a) {
     constexpr int N = 16 / sizeof(T);
-    const int64_t pieces = a.ldd / N;   // of a row; ldd is a multiple of N
-    const int64_t q = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int64_t row = q / pieces, col = q % pieces * N;
+    const uint32_t q = blockIdx.x * kThreads + threadIdx.x, r = a.pieces.quotient(q);
+    const int64_t row = r, col = (int64_t)(q - r * a.pieces.by) * N;
     if (row >= a.rows) return;
     float v[N], z[N];
     const int64_t from = a.list ? a.list[row] : row;
-    read_some<T, N>(static_cast<const T *>(a.src) + (a.list ? from / a.per : from) * a.lds + col,
+    read_some<T, N>(static_cast<const T *>(a.src) +
+                         (a.list && from >= 0 ? (int64_t)a.per.quotient((uint32_t)from) : from) * a.lds + col,
                     from < 0 ? 0 : a.cols - col, v);
     if (a.gates) {
         const float g = from < 0 ? 0.f : a.gates[from];
@@ -114,7 +116,7 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(SumsArgs a) {
             if (LISTED && r < end) {
                 const int slot = a.list[r];
                 if (a.gates) gate[u] = a.gates[slot];
-                row = slot / a.per;
+                row = a.per.quotient(slot);
             }
             read_some<T, N>(static_cast<const T *>(a.src) + row * a.ld + col,
                             r < end ? left : 0, v[u]);
@@ -177,9 +179,8 @@ __global__ __launch_bounds__(kSumThreads) void join_sums_kernel(SumsArgs a) {
 template <typename T>
 __global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a) {
     constexpr int N = 16 / sizeof(T);
-    const int64_t pieces = (a.width + N - 1) / N;
-    const int64_t q = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int64_t i = q / pieces, col = q % pieces * N, left = a.width - col;
+    const uint32_t q = blockIdx.x * kThreads + threadIdx.x, r = a.pieces.quotient(q);
+    const int64_t i = r, col = (int64_t)(q - r * a.pieces.by) * N, left = a.width - col;
     if (i >= a.n) return;
     float sum[N], y[N], first[N];
 #pragma unroll
@@ -233,14 +234,34 @@ hipError_t by_type(int32_t type, F f) {
 
 }  // namespace
 
-hipError_t launch_rows_copy(const RowsArgs &a, hipStream_t stream) {
-    const int size = type_size(a.type);
-    const int64_t pieces = a.rows * (a.ldd * size / 16);
-    if (pieces == 0) return hipSuccess;
-    if ((pieces + kThreads - 1) / kThreads > INT32_MAX) return hipErrorInvalidValue;
-    const unsigned blocks = (unsigned)((pieces + kThreads - 1) / kThreads);
-    return by_type(a.type, [&](auto t) {
-        rows_copy_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a);
+// Launches `launch` on whole rows of `pieces` threads each, as many at a time as
+// keep the threads' numbers below 2^31.
+template <typename F>
+hipError_t in_rows(int64_t rows, int64_t pieces, F launch) {
+    if (pieces > INT32_MAX) return hipErrorInvalidValue;
+    const int64_t most = std::max<int64_t>(1, (INT32_MAX - kThreads) / pieces);
+    for (int64_t r = 0; r < rows; r += most) {
+        const int64_t some = std::min(most, rows - r);
+        const hipError_t e = launch(r, some, (unsigned)((some * pieces + kThreads - 1) / kThreads));
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+hipError_t launch_rows_copy(const RowsArgs &args, hipStream_t stream) {
+    const int size = type_size(args.type);
+    const int64_t pieces = args.ldd * size / 16;
+    return in_rows(args.rows, pieces, [&](int64_t r, int64_t rows, unsigned blocks) {
+        RowsArgs a = args;
+        a.pieces = Divider((uint32_t)pieces);
+        a.rows = rows;
+        if (a.list) a.list += r;
+        else a.src = static_cast<const char *>(a.src) + r * a.lds * size;
+        if (a.z) a.z = static_cast<const char *>(a.z) + r * a.ldz * size;
+        a.dst = static_cast<char *>(a.dst) + r * a.ldd * size;
+        return by_type(a.type, [&](auto t) {
+            rows_copy_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a);
+        });
     });
 }
 
@@ -282,14 +303,20 @@ hipError_t launch_sums(const SumsArgs &a, hipStream_t stream) {
     });
 }
 
-hipError_t launch_combine(const CombineArgs &a, hipStream_t stream) {
-    const int size = type_size(a.type);
-    const int64_t pieces = a.n * ((a.width * size + 15) / 16);
-    if (pieces == 0) return hipSuccess;
-    if ((pieces + kThreads - 1) / kThreads > INT32_MAX) return hipErrorInvalidValue;
-    const unsigned blocks = (unsigned)((pieces + kThreads - 1) / kThreads);
-    return by_type(a.type, [&](auto t) {
-        combine_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a);
+hipError_t launch_combine(const CombineArgs &args, hipStream_t stream) {
+    const int size = type_size(args.type);
+    const int64_t pieces = (args.width * size + 15) / 16;
+    return in_rows(args.n, pieces, [&](int64_t r, int64_t rows, unsigned blocks) {
+        CombineArgs a = args;
+        a.pieces = Divider((uint32_t)pieces);
+        a.n = rows;
+        if (a.weight) a.weight += r * a.k;
+        a.place += r * a.k;
+        if (a.residual) a.residual = static_cast<const char *>(a.residual) + r * a.ldr * size;
+        a.out = static_cast<char *>(a.out) + r * a.width * size;
+        return by_type(a.type, [&](auto t) {
+            combine_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a);
+        });
     });
 }
 

@@ -119,7 +119,7 @@ struct Side {
     // (along), or columns row0 .. of one whose element is p[c * ld + r] (across),
     // from contraction index k0 on; `list`: row r is the side's row list[r] / per.
     __device__ void begin(const T *p, int64_t ld, int64_t row0, int64_t rows, int64_t k0,
-                          const int32_t *list, int per) {
+                          const int32_t *list, Divider per) {
         base = reinterpret_cast<const char *>(p + (ACROSS ? k0 * ld : k0 + (list ? 0 : row0 * ld)));
         step = ACROSS ? kSlab * ld * (int64_t)sizeof(T) : 128;
 #pragma unroll
@@ -129,7 +129,7 @@ struct Side {
             } else {
                 const int r = place(j) >> 3;
                 int64_t row = row0 + r < rows ? r : rows - 1 - row0;
-                if (list) row = list[row0 + row] / per;
+                if (list) row = per.quotient(list[row0 + row]);
                 off[j] = (uint32_t)((row * ld + index(j)) * (int64_t)sizeof(T));
             }
         }
@@ -181,11 +181,11 @@ struct Side {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) row[j] = index(j) < left ? list[index(j)] : 0;
     }
-    __device__ void follow(const int32_t (&row)[kLoads], int per, int64_t ld, int64_t col0,
+    __device__ void follow(const int32_t (&row)[kLoads], Divider per, int64_t ld, int64_t col0,
                            int64_t cols) {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j)
-            off[j] = (uint32_t)(((int64_t)(row[j] / per) * ld + column(j, col0, cols)) *
+            off[j] = (uint32_t)(((int64_t)per.quotient(row[j]) * ld + column(j, col0, cols)) *
                                 (int64_t)sizeof(T));
     }
 };
@@ -352,7 +352,7 @@ struct Epilogue {
             const int slot = a.slots[row];
             r.gate = a.gates ? a.gates[slot] : 1.f;
             r.piece.read(static_cast<const T *>(a.argument) +
-                             (a.argument_listed ? slot / a.per : row) * a.ld_argument + col,
+                             (a.argument_listed ? (int64_t)a.per.quotient(slot) : row) * a.ld_argument + col,
                          left);
         }
     }
@@ -477,7 +477,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
         Fragments<T, kAcrossB, TN, FN> rb;
         sa.begin(pa, a.lda, row0, row_end, LIST == 2 ? 0 : k0, MODE == kWeight ? nullptr : a.list,
                  a.per);
-        sb.begin(pb, a.ldb, col0, a.n, LIST == 1 ? 0 : k0, nullptr, 1);
+        sb.begin(pb, a.ldb, col0, a.n, LIST == 1 ? 0 : k0, nullptr, a.per);
         ra.begin(wm);
         rb.begin(wn);
         int32_t entry[LIST == 2 ? SideA::kLoads : SideB::kLoads];
@@ -700,7 +700,7 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(ProductArgs a, int by_
     const T *wr = static_cast<const T *>(a.b) + batch * a.batch_b +
                   (col0 + i < a.n ? col0 + i : a.n - 1) * a.ldb;
     int64_t xrow = row0 + i < row_end ? row0 + i : row_end - 1;
-    if (a.list) xrow = a.list[xrow] / a.per;
+    if (a.list) xrow = a.per.quotient(a.list[xrow]);
     const T *xr = static_cast<const T *>(a.a) + xrow * a.lda;
     f4 acc = {0.f, 0.f, 0.f, 0.f};
     const auto slabs = [&](auto check, int64_t k) {

@@ -4,9 +4,10 @@
 // route: a row of scores lies in the registers of 16 lanes or of a wave, V
 // neighbours to a lane, so that the lowest lane and element of equal values is the
 // lowest expert; rows of more than 2048 experts lie in LDS, one to a workgroup.
-// The k choices are k maxima over the row: one per lane, joined across the
-// lanes.  Bound by these maxima (about 20 k instructions a row), not by the
-// read of the scores.
+// The k choices are k maxima over the row, of whole numbers in the values' order:
+// one per lane, joined across the lanes by rotations; only the lane that won
+// looks for its element.  Bound by these instructions (about 85 for the rows of
+// a wave and choice at V = 16), not by the read of the scores.
 #include "som_local_internal.h"
 
 #include <math.h>
@@ -47,7 +48,66 @@ __device__ inline unsigned long long row_ballot(bool is) {
     return LANES == 64 ? all : all >> (threadIdx.x & 48) & 0xffff;
 }
 
-__device__ inline float sigmoid(float s) { return 1.f / (1.f + expf(-s)); }
+// 1 / (1 + e^-s) in the roundings of its three operations.  The division: the
+// hardware's reciprocal is within one unit in the last place, and a step of
+// Newton's in fused operations rounds it correctly (Markstein), in a third of the
+// instructions; beyond 2^126, where the quotient is denormal, the division itself.
+__device__ inline float sigmoid(float s) {
+    const float d = 1.f + expf(-s);
+    if (!(d < 0x1p126f)) return 1.f / d;
+    const float r = __builtin_amdgcn_rcpf(d);
+    return fmaf(fmaf(-d, r, 1.f), r, r);
+}
+
+// Whole numbers in the order of the floats (equal zeros alike); kClosed for
+// -infinity, below all others.
+constexpr int kClosed = (int)0x80000000;
+__device__ inline int key_of(float v) {
+    const int b = __float_as_int(v + 0.f);
+    return v > -INFINITY ? b ^ (b >> 31 & 0x7fffffff) : kClosed;
+}
+
+template <int LANES>
+__device__ inline int across_max_key(int v) {
+    v = max(v, __builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_mov_dpp(v, 0x124, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_mov_dpp(v, 0x122, 0xf, 0xf, false));
+    v = max(v, __builtin_amdgcn_mov_dpp(v, 0x121, 0xf, 0xf, false));
+    if (LANES == 64) {
+        v = max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
+                max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+    }
+    return v;
+}
+
+// V neighbouring values of a row from element e0 on, `fill` past its end.
+template <typename T, int V>
+__device__ inline void read_row(const T *s, int e0, int experts, float fill, float (&x)[V]) {
+    typedef T Vec __attribute__((ext_vector_type(V)));
+    if (e0 + V <= experts) {
+        Vec q;
+        __builtin_memcpy(&q, __builtin_assume_aligned(s + e0, sizeof(T)), sizeof(T) * V);
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = (float)q[v];
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = e0 + v < experts ? (float)s[e0 + v] : fill;
+    }
+}
+template <typename T, int V>
+__device__ inline void write_row(T *s, int e0, int experts, const float (&x)[V]) {
+    typedef T Vec __attribute__((ext_vector_type(V)));
+    if (e0 + V <= experts) {
+        Vec q;
+#pragma unroll
+        for (int v = 0; v < V; ++v) q[v] = (T)x[v];
+        __builtin_memcpy(__builtin_assume_aligned(s + e0, sizeof(T)), &q, sizeof(T) * V);
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (e0 + v < experts) s[e0 + v] = (T)x[v];
+    }
+}
 
 // The value that the choice goes by; -infinity: closed.
 __device__ inline float choice_value(float s, bool softmax, const float *bias, int e) {
@@ -61,15 +121,23 @@ __device__ inline bool spoils(float s, bool softmax) {
     return s != s || (softmax && s == INFINITY);
 }
 
-// The groups that stay, as bits.  Lane g < groups holds group g's value.
+// The groups that stay, as bits.  Lane g << shift holds group g's value.
 template <int LANES>
-__device__ inline unsigned long long groups_that_stay(float value, int lane, int groups, int top) {
+__device__ inline unsigned long long groups_that_stay(float value, int lane, int shift, int groups,
+                                                      int top) {
+    const int mine = lane >> shift;
     int before = 0;
     for (int h = 0; h < groups; ++h) {
-        const float other = __shfl(value, h, LANES);
-        before += other > value || (other == value && h < lane) ? 1 : 0;
+        const float other = __shfl(value, h << shift, LANES);
+        before += other > value || (other == value && h < mine) ? 1 : 0;
     }
-    return row_ballot<LANES>(lane < groups && before < top && value > -INFINITY);
+    const bool stays = (lane & ((1 << shift) - 1)) == 0 && mine < groups && before < top &&
+                       value > -INFINITY;
+    const unsigned long long lanes = row_ballot<LANES>(stays);
+    if (shift == 0) return lanes;
+    unsigned long long bits = 0;
+    for (int h = 0; h < groups; ++h) bits |= (lanes >> (h << shift) & 1) << h;
+    return bits;
 }
 
 // A row's weights from its choices: lane j holds choice j (index at, -1 for none).
@@ -107,38 +175,20 @@ __device__ inline void write_choices(const RouteArgs &a, int64_t row, int lane, 
 
 // LANES lanes a row, V experts a lane.
 template <typename T, int LANES, int V>
-__global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, int vec) {
+__global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a) {
     constexpr int kRows = kRouteThreads / LANES;
-    extern __shared__ float shared[];  // with groups: kRows x (experts + 1) values
+    extern __shared__ float shared[];  // with groups that lanes do not hold whole: the values
+    __shared__ int chosen[kRows][LANES];
     const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
     const int64_t row = (int64_t)blockIdx.x * kRows + slot;
     const bool there = row < a.n;
     const T *s = static_cast<const T *>(a.scores) + (there ? row : a.n - 1) * a.lds;
     const int e0 = lane * V;
-    float x[V], pick[V];
-    if (vec && e0 + V <= a.experts) {
-        typedef T tv __attribute__((ext_vector_type(16 / sizeof(T))));
-        constexpr int kPer = 16 / sizeof(T);
-#pragma unroll
-        for (int p = 0; p < V / kPer; ++p) {
-            const tv q = reinterpret_cast<const tv *>(s + e0)[p];
-#pragma unroll
-            for (int c = 0; c < kPer; ++c) x[p * kPer + c] = (float)q[c];
-        }
-        if (V < kPer) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) x[v] = (float)s[e0 + v];
-        }
-    } else {
-#pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = e0 + v < a.experts ? (float)s[e0 + v] : -INFINITY;
-    }
+    float x[V];
+    read_row<T, V>(s, e0, a.experts, -INFINITY, x);
     bool spoilt = false;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        spoilt |= spoils(x[v], a.softmax);
-        pick[v] = e0 + v < a.experts ? choice_value(x[v], a.softmax, a.bias, e0 + v) : -INFINITY;
-    }
+    for (int v = 0; v < V; ++v) spoilt |= spoils(x[v], a.softmax);
     const bool bad = row_ballot<LANES>(spoilt) != 0;
 
     float low = -INFINITY, total = 1.f;
@@ -153,51 +203,74 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, int v
         total = across_sum<LANES>(total);
         total = total > 0.f ? total : 1.f;
     }
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        x[v] = e0 + v < a.experts ? choice_value(x[v], a.softmax, a.bias, e0 + v) : -INFINITY;
 
     if (a.groups > 1) {
-        const int per = a.experts / a.groups;
-        float *mine = shared + slot * (a.experts + 1);
+        const int per = a.experts / a.groups, lanes = per / V;
+        float best = -INFINITY, next = -INFINITY;
+        int shift = 0;
+        if (per % V == 0 && (lanes & (lanes - 1)) == 0) {   // whole lanes, a power of two
+            shift = 31 - __clz(lanes);
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (e0 + v < a.experts) mine[e0 + v] = pick[v];
-        __syncthreads();
-        float value = -INFINITY;
-        for (int g = lane; g < a.groups; g += LANES) {  // groups <= LANES
-            float best = -INFINITY, next = -INFINITY;
-            for (int e = 0; e < per; ++e) {
-                const float v = mine[g * per + e];
-                next = fmaxf(next, fminf(best, v));
-                best = fmaxf(best, v);
+            for (int v = 0; v < V; ++v) {
+                next = fmaxf(next, fminf(best, x[v]));
+                best = fmaxf(best, x[v]);
             }
-            value = a.group_best == 2 && next > -INFINITY ? best + next : best;
+            for (int o = 1; o < lanes; o <<= 1) {
+                const float b = __shfl_xor(best, o), n = __shfl_xor(next, o);
+                next = fmaxf(fmaxf(next, n), fminf(best, b));
+                best = fmaxf(best, b);
+            }
+        } else {
+            float *mine = shared + slot * (a.experts + 1);
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (e0 + v < a.experts) mine[e0 + v] = x[v];
+            __syncthreads();
+            if (lane < a.groups) {   // groups <= LANES
+#pragma unroll 4
+                for (int e = 0; e < per; ++e) {
+                    const float v = mine[lane * per + e];
+                    next = fmaxf(next, fminf(best, v));
+                    best = fmaxf(best, v);
+                }
+            }
         }
-        const unsigned long long stay = groups_that_stay<LANES>(value, lane, a.groups, a.top_groups);
+        const float value = a.group_best == 2 && next > -INFINITY ? best + next : best;
+        const unsigned long long stay =
+            groups_that_stay<LANES>(value, lane, shift, a.groups, a.top_groups);
         int left = per - e0 % per;
         unsigned long long bits = e0 < a.experts ? stay >> e0 / per : 0;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            if (!(bits & 1)) pick[v] = -INFINITY;
+            if (!(bits & 1)) x[v] = -INFINITY;
             if (--left == 0) bits >>= 1, left = per;
         }
     }
 
-    int at = -1;
+    int key[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) key[v] = key_of(x[v]);
     for (int j = 0; j < a.k; ++j) {
-        float best = pick[0];
+        int best = key[0];
 #pragma unroll
-        for (int v = 1; v < V; ++v) best = fmaxf(best, pick[v]);
-        const float top = across_max<LANES>(best);
+        for (int v = 1; v < V; ++v) best = max(best, key[v]);
+        const int top = across_max_key<LANES>(best);
         const unsigned long long who = row_ballot<LANES>(best == top);
-        const int first = __ffsll((long long)who) - 1;
-        int mine = 0;
+        if (__ffsll((long long)who) - 1 == lane) {
+            int mine = 0;
 #pragma unroll
-        for (int v = V - 1; v >= 0; --v) mine = pick[v] == top ? v : mine;
-        const int won = __shfl(e0 + mine, first, LANES);
-        if (lane == j) at = top > -INFINITY ? won : -1;
+            for (int v = V - 1; v >= 0; --v) mine = key[v] == top ? v : mine;
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (e0 + v == won) pick[v] = -INFINITY;
+            for (int v = 0; v < V; ++v) key[v] = v == mine ? kClosed : key[v];
+            chosen[slot][j] = top != kClosed ? e0 + mine : -1;
+        }
     }
+    // a row's lanes are in one wave
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int at = lane < a.k ? chosen[slot][lane] : -1;
     if (there) write_choices<T, LANES>(a, row, lane, at, bad, low, total);
 }
 
@@ -257,7 +330,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_long_kernel(RouteArgs a) 
         }
         __syncthreads();
         const float value = lane < a.groups ? group_value[lane] : -INFINITY;
-        const unsigned long long stay = groups_that_stay<64>(value, lane, a.groups, a.top_groups);
+        const unsigned long long stay = groups_that_stay<64>(value, lane, 0, a.groups, a.top_groups);
         for (int e = t; e < a.experts; e += kRouteThreads)
             if (!(stay >> (e / per) & 1)) pick[e] = -INFINITY;
     }
@@ -296,20 +369,22 @@ __global__ __launch_bounds__(kRouteThreads) void route_long_kernel(RouteArgs a) 
     if (wave == 0) write_choices<T, 64>(a, row, lane, at, bad, low, total);
 }
 
-// Gradient of the scores.  LANES lanes a row: lane j works out choice j's part,
-// then the row is written once, the choices' parts put in from LDS.  Bound by
-// the write of the rows (and their read, for a softmax over the whole row).
-template <typename T, typename G, int LANES>
-__global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(RouteArgs a, int width) {
-    constexpr int kRows = kRouteThreads / LANES;
-    extern __shared__ float shared[];  // kRows x width: the choices' parts
+// Gradient of the scores.  LANES lanes a row: lane j works out choice j's part and
+// puts it into the row in LDS, from where the row goes out once, V neighbours a
+// lane; a softmax over the whole row is worked out again from the scores.  Bound by
+// the write of the rows, and that read.  Rows of more than LANES V experts are
+// taken in pieces of that many.
+template <typename T, typename G, int LANES, int V>
+__global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(RouteArgs a) {
+    constexpr int kRows = kRouteThreads / LANES, kWide = LANES * V;
+    __shared__ __align__(16) float parts[kRows][kWide];
     const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
     const int64_t row = (int64_t)blockIdx.x * kRows + slot;
     const bool there = row < a.n;
     const int64_t r = there ? row : a.n - 1;
     const T *s = static_cast<const T *>(a.scores) + r * a.lds;
     T *out = static_cast<T *>(a.dscores) + r * a.experts;
-    float *mine = shared + slot * width;
+    float *mine = parts[slot];
     const int at = lane < a.k ? a.index[r * a.k + lane] : -1;
     const bool here = at >= 0 && at < a.experts;
     const float weight = lane < a.k ? a.weight[r * a.k + lane] : 0.f;
@@ -317,20 +392,29 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(RouteArgs
     const bool bad = row_ballot<LANES>(weight != weight) != 0;
     const float score = here ? (float)s[at] : -INFINITY;
     float part;               // of the chosen score
-    float mean = 0.f, low = 0.f, total = 1.f;
+    float mean = 0.f, low = 0.f, by_total = 1.f;
     const bool whole = a.softmax && !a.renormalise;
+    float x[V];
     if (a.softmax) {
         mean = across_sum<LANES>(g * weight);  // scale sum of g p
         part = weight * (g - (a.scale != 0.f ? mean / a.scale : 0.f));
         if (whole) {
             low = -INFINITY;
-            for (int e = lane; e < a.experts; e += LANES) low = fmaxf(low, (float)s[e]);
+            for (int e0 = lane * V; e0 < a.experts; e0 += kWide) {
+                read_row<T, V>(s, e0, a.experts, -INFINITY, x);
+#pragma unroll
+                for (int v = 0; v < V; ++v) low = fmaxf(low, x[v]);
+            }
             low = across_max<LANES>(low);
             low = low > -INFINITY ? low : 0.f;
-            total = 0.f;
-            for (int e = lane; e < a.experts; e += LANES) total += expf((float)s[e] - low);
+            float total = 0.f;
+            for (int e0 = lane * V; e0 < a.experts; e0 += kWide) {
+                if (a.experts > kWide) read_row<T, V>(s, e0, a.experts, -INFINITY, x);
+#pragma unroll
+                for (int v = 0; v < V; ++v) total += expf(x[v] - low);
+            }
             total = across_sum<LANES>(total);
-            total = total > 0.f ? total : 1.f;
+            by_total = total > 0.f ? 1.f / total : 1.f;
             part = a.scale * g;
         }
     } else {
@@ -344,31 +428,36 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(RouteArgs
         }
         part = by * g * p * (1.f - p);
     }
-    for (int e0 = 0; e0 < a.experts; e0 += width) {
-        const int e1 = e0 + width < a.experts ? e0 + width : a.experts;
-        for (int e = e0 + lane; e < e1; e += LANES) mine[e - e0] = bad ? NAN : 0.f;
-        __syncthreads();
-        if (here && at >= e0 && at < e1 && !bad) mine[at - e0] = part;
-        __syncthreads();
-        if (there) {
-            for (int e = e0 + lane; e < e1; e += LANES) {
-                float v = mine[e - e0];
-                if (whole) v = expf((float)s[e] - low) / total * (v - mean);
-                out[e] = (T)v;
-            }
+    const float none = bad ? NAN : 0.f;
+    for (int w0 = 0; w0 < a.experts; w0 += kWide) {
+        const int e0 = w0 + lane * V;
+#pragma unroll
+        for (int v = 0; v < V; ++v) mine[lane * V + v] = none;
+        // a row's lanes are in one wave
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (here && !bad && at >= w0 && at < w0 + kWide) mine[at - w0] = part;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        float d[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) d[v] = mine[lane * V + v];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (whole && e0 < a.experts) {
+            if (a.experts > kWide) read_row<T, V>(s, e0, a.experts, -INFINITY, x);
+#pragma unroll
+            for (int v = 0; v < V; ++v) d[v] = expf(x[v] - low) * by_total * (d[v] - mean);
         }
-        __syncthreads();
+        if (there) write_row<T, V>(out, e0, a.experts, d);
     }
 }
 
 // --------------------------------------------------------------- dispatch
 // A stable counting sort of the slots by expert.  Workgroup b takes the slots of
-// chunk b, its four waves a quarter each, in order.  count: the chunk's slots per
-// expert.  place: every workgroup adds up the counts of the chunks before it
-// and of all of them (read from the caches), so that no launch lies between; the
-// rank of a slot among its wave's 64 comes from the lanes that hold the same
-// expert.  Whole numbers only: the order does not depend on timing.
-constexpr int kChunk = 4096, kSortThreads = 256, kSortWaves = kSortThreads / 64;
+// chunk b, its waves a part each, in order, their experts in registers.  count: the
+// chunk's slots per expert.  place: every workgroup adds up the counts of the
+// chunks before it and of all of them (read from the caches), so that no launch
+// lies between; the rank of a slot among its wave's 64 comes from the lanes that
+// hold the same expert.  Whole numbers only: the order does not depend on timing.
+constexpr int kChunk = 4096, kSortThreads = 1024;
 
 __device__ inline int expert_at(const DispatchArgs &a, int64_t s, int64_t end) {
     const int e = s < end ? a.index[s] : -1;
@@ -390,53 +479,70 @@ __global__ __launch_bounds__(kSortThreads) void dispatch_count_kernel(DispatchAr
         a.counts[(int64_t)blockIdx.x * a.experts + e] = hist[e];
 }
 
-// WAVES: waves that rank (4, or 1 where four histograms do not fit in LDS).
+// WAVES: waves that rank (fewer where their histograms do not fit in LDS).
 template <int WAVES>
 __global__ __launch_bounds__(kSortThreads) void dispatch_place_kernel(DispatchArgs a) {
+    constexpr int kPart = kChunk / WAVES, kHeld = kPart / 64;
+    constexpr int kExperts = 256, kLanes = kSortThreads / kExperts;   // per pass over the experts
     extern __shared__ int base[];   // WAVES x experts
-    __shared__ int sums[kSortWaves + 1];
+    __shared__ int sums[kExperts / 64], found[2][kLanes][kExperts];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const int64_t s0 = (int64_t)blockIdx.x * kChunk;
+    const int64_t s0 = (int64_t)blockIdx.x * kChunk, w0 = s0 + (int64_t)wave * kPart;
     const int64_t end = s0 + kChunk < a.slots ? s0 + kChunk : a.slots;
-    constexpr int kPart = kChunk / WAVES;
+    int *mine = base + wave * a.experts;
+    int held[kHeld];
+    if (wave < WAVES) {
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) held[h] = expert_at(a, w0 + h * 64 + lane, end);
+    }
     for (int e = t; e < WAVES * a.experts; e += kSortThreads) base[e] = 0;
     __syncthreads();
-    if (WAVES > 1 || a.blocks == 1) {
-        for (int64_t s = s0 + t; s < end; s += kSortThreads) {
-            const int e = expert_at(a, s, end);
-            if (e >= 0) atomicAdd(&base[(int)((s - s0) / kPart) * a.experts + e], 1);
-        }
-        __syncthreads();
+    if (wave < WAVES && (WAVES > 1 || a.blocks == 1)) {
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h)
+            if (held[h] >= 0) atomicAdd(&mine[held[h]], 1);
     }
+    __syncthreads();
     // expert by expert, 256 at a time: the chunk's first row, then the waves'
     int before = 0;   // rows of the experts below these 256
-    for (int e0 = 0; e0 < a.experts; e0 += kSortThreads) {
-        const int e = e0 + t;
+    const int le = t % kExperts, part = t / kExperts;
+    for (int e0 = 0; e0 < a.experts; e0 += kExperts) {
+        const int e = e0 + le;
         int all = 0, prior = 0;
         if (e < a.experts) {
             if (a.blocks == 1) {
-#pragma unroll
-                for (int w = 0; w < WAVES; ++w) all += base[w * a.experts + e];
+                for (int w = part; w < WAVES; w += kLanes) all += base[w * a.experts + e];
             } else {
-                for (int b = 0; b < a.blocks; ++b) {
+#pragma unroll 8
+                for (int b = part; b < a.blocks; b += kLanes) {
                     const int c = a.counts[(int64_t)b * a.experts + e];
                     all += c;
                     prior += b < (int)blockIdx.x ? c : 0;
                 }
             }
         }
-        int sum = all;   // inclusive over the lanes
-        for (int o = 1; o < 64; o <<= 1) {
-            const int v = __shfl_up(sum, o);
-            if (lane >= o) sum += v;
-        }
-        if (lane == 63) sums[wave] = sum;
+        found[0][part][le] = all;
+        found[1][part][le] = prior;
         __syncthreads();
-        int first = before + sum - all;
-        for (int w = 0; w < wave; ++w) first += sums[w];
+        int sum = 0, first = 0;
+        if (part == 0) {
+            all = prior = 0;
+#pragma unroll
+            for (int l = 0; l < kLanes; ++l) all += found[0][l][le], prior += found[1][l][le];
+            sum = all;   // inclusive over the lanes
+            for (int o = 1; o < 64; o <<= 1) {
+                const int v = __shfl_up(sum, o);
+                if (lane >= o) sum += v;
+            }
+            if (lane == 63) sums[wave] = sum;
+        }
+        __syncthreads();
         int next = before;
-        for (int w = 0; w < kSortWaves; ++w) next += sums[w];
-        if (e < a.experts) {
+#pragma unroll
+        for (int w = 0; w < kExperts / 64; ++w) next += sums[w];
+        if (part == 0 && e < a.experts) {
+            first = before + sum - all;
+            for (int w = 0; w < wave; ++w) first += sums[w];
             if (blockIdx.x == 0) a.offsets[e] = first;
             int at = first + prior;
 #pragma unroll
@@ -454,11 +560,10 @@ __global__ __launch_bounds__(kSortThreads) void dispatch_place_kernel(DispatchAr
          p += (int64_t)gridDim.x * kSortThreads)
         a.order[p] = -1;
     if (wave >= WAVES) return;
-    int *mine = base + wave * a.experts;
-    const int64_t w0 = s0 + (int64_t)wave * kPart;
-    for (int64_t g0 = w0; g0 < w0 + kPart && g0 < end; g0 += 64) {
-        const int64_t s = g0 + lane;
-        const int e = expert_at(a, s, end);
+#pragma unroll
+    for (int h = 0; h < kHeld; ++h) {
+        const int64_t s = w0 + h * 64 + lane;
+        const int e = held[h];
         // the lanes that hold the same expert
         unsigned long long same = __ballot(e >= 0);
         for (int b = 1; b < a.experts; b <<= 1) {
@@ -466,8 +571,7 @@ __global__ __launch_bounds__(kSortThreads) void dispatch_place_kernel(DispatchAr
             same &= e & b ? ones : ~ones;
         }
         if (e >= 0) {
-            const int rank = __popcll(same & ((1ull << lane) - 1));
-            const int p = mine[e] + rank;
+            const int p = mine[e] + __popcll(same & ((1ull << lane) - 1));
             a.order[p] = (int)s;
             a.place[s] = p;
         } else if (s < end) {
@@ -483,7 +587,7 @@ __global__ __launch_bounds__(kSortThreads) void dispatch_place_kernel(DispatchAr
 // Lets a kernel have `bytes` of dynamic LDS where, with its own, they pass 64 KB.
 template <typename K>
 hipError_t room_for(K kernel, size_t bytes) {
-    if (bytes <= 60 * 1024) return hipSuccess;
+    if (bytes <= 48 * 1024) return hipSuccess;
     return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
@@ -492,19 +596,19 @@ template <typename T>
 hipError_t launch_route_type(const RouteArgs &a, hipStream_t stream) {
     const bool wide = a.k > 16 || a.groups > 16;
     const auto blocks = [&](int rows) { return (unsigned)((a.n + rows - 1) / rows); };
-    const int vec = a.lds % (16 / (int)sizeof(T)) == 0 &&
-                    reinterpret_cast<uintptr_t>(a.scores) % 16 == 0;
     const auto lds = [&](int rows) {
         return a.groups > 1 ? (size_t)rows * (a.experts + 1) * sizeof(float) : 0;
     };
     if (a.experts <= 64 && !wide)
-        route_kernel<T, 16, 4><<<blocks(16), kRouteThreads, lds(16), stream>>>(a, vec);
+        route_kernel<T, 16, 4><<<blocks(16), kRouteThreads, lds(16), stream>>>(a);
     else if (a.experts <= 256 && !wide)
-        route_kernel<T, 16, 16><<<blocks(16), kRouteThreads, lds(16), stream>>>(a, vec);
+        route_kernel<T, 16, 16><<<blocks(16), kRouteThreads, lds(16), stream>>>(a);
     else if (a.experts <= 512)
-        route_kernel<T, 64, 8><<<blocks(4), kRouteThreads, lds(4), stream>>>(a, vec);
+        route_kernel<T, 64, 8><<<blocks(4), kRouteThreads, lds(4), stream>>>(a);
+    else if (a.experts <= 1024)
+        route_kernel<T, 64, 16><<<blocks(4), kRouteThreads, lds(4), stream>>>(a);
     else if (a.experts <= 2048)
-        route_kernel<T, 64, 32><<<blocks(4), kRouteThreads, lds(4), stream>>>(a, vec);
+        route_kernel<T, 64, 32><<<blocks(4), kRouteThreads, lds(4), stream>>>(a);
     else {
         const hipError_t e = room_for(route_long_kernel<T>, a.experts * sizeof(float));
         if (e != hipSuccess) return e;
@@ -516,14 +620,12 @@ hipError_t launch_route_type(const RouteArgs &a, hipStream_t stream) {
 template <typename T, typename G>
 hipError_t launch_backward_types(const RouteArgs &a, hipStream_t stream) {
     const auto blocks = [&](int rows) { return (unsigned)((a.n + rows - 1) / rows); };
-    if (a.experts <= 512 && a.k <= 16)
-        route_backward_kernel<T, G, 16><<<blocks(16), kRouteThreads,
-                                          16 * a.experts * sizeof(float), stream>>>(a, a.experts);
-    else {
-        const int width = a.experts < 2048 ? a.experts : 2048;
-        route_backward_kernel<T, G, 64><<<blocks(4), kRouteThreads, 4 * width * sizeof(float),
-                                          stream>>>(a, width);
-    }
+    if (a.experts <= 64 && a.k <= 16)
+        route_backward_kernel<T, G, 16, 4><<<blocks(16), kRouteThreads, 0, stream>>>(a);
+    else if (a.experts <= 256 && a.k <= 16)
+        route_backward_kernel<T, G, 16, 16><<<blocks(16), kRouteThreads, 0, stream>>>(a);
+    else
+        route_backward_kernel<T, G, 64, 8><<<blocks(4), kRouteThreads, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -567,9 +669,11 @@ hipError_t launch_dispatch(const DispatchArgs &a, hipStream_t stream) {
         if (e != hipSuccess) return e;
         dispatch_count_kernel<<<a.blocks, kSortThreads, one, stream>>>(a);
     }
-    if (a.experts <= 2048) {
+    if (a.experts <= 512)
+        dispatch_place_kernel<16><<<a.blocks, kSortThreads, 16 * one, stream>>>(a);
+    else if (a.experts <= 2048)
         dispatch_place_kernel<4><<<a.blocks, kSortThreads, 4 * one, stream>>>(a);
-    } else {
+    else {
         const hipError_t e = room_for(dispatch_place_kernel<1>, one);
         if (e != hipSuccess) return e;
         dispatch_place_kernel<1><<<a.blocks, kSortThreads, one, stream>>>(a);
