@@ -26,12 +26,12 @@ __device__ inline float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.
 
 __device__ inline void normal(float z, float *below, float *bell) {
     const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
-    const float e = exp_fast(-0.5f * z * z);
-    float s = fmaf(t, 1.061405429f, -1.453152027f);
-    s = fmaf(t, s, 1.421413741f);
-    s = fmaf(t, s, -0.284496736f);
-    s = fmaf(t, s, 0.254829592f);
-    const float tail = 0.5f * t * s * e;
+    const float e = __builtin_amdgcn_exp2f(z * z * (-0.5f * 1.44269504f));
+    float s = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+    s = fmaf(t, s, 0.5f * 1.421413741f);
+    s = fmaf(t, s, 0.5f * -0.284496736f);
+    s = fmaf(t, s, 0.5f * 0.254829592f);
+    const float tail = t * s * e;
     *below = z > 0.f ? 1.f - tail : tail;
     *bell = e;
 }

@@ -342,7 +342,8 @@ struct Epilogue {
 #pragma unroll
         for (int e = 0; e < N; ++e) bias[e] = there ? (float)p.v[e] : 0.f;
     }
-    __device__ void read(int64_t row, Row &r) const {
+    __device__ static void read(const ProductArgs &a, int64_t row, int64_t col, Row &r) {
+        const int left = (int)(a.n - col < N ? a.n - col : N);
         if (MODE == kForward) {
             if (a.residual)
                 r.piece.read(static_cast<const T *>(a.residual) + row * a.ldr + col, left);
@@ -469,7 +470,31 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
     for (int x = 0; x < FM; ++x)
 #pragma unroll
         for (int y = 0; y < FN; ++y) acc[x][y] = f4{0.f, 0.f, 0.f, 0.f};
+    // The result's rows as they leave: N columns a lane, kPass rows of the wave at a
+    // time; what lies beside them in memory is read kGroup passes ahead.
+    constexpr int N = 16 / sizeof(T), kQuads = kTileN / 4;
+    constexpr int kFits = 2 * kBytes / (WM * WN * kTileN * 4);   // rows of a wave's part
+    constexpr int kMost = kFits >= 64 ? 64 : kFits >= 32 ? 32 : 16;
+    constexpr int kRowsAt = kTileM < kMost ? kTileM : kMost;
+    constexpr int kLanes = kTileN / N, kPass = 64 / kLanes;
+    constexpr int kGroup = kRowsAt / kPass < 4 ? kRowsAt / kPass : 4;
+    static_assert(WM * WN * kRowsAt * kTileN * 4 <= 2 * kBytes, "fits in the slabs' LDS");
+    using Row = typename Epilogue<T, MODE, N>::Row;
+    f4 *mine = reinterpret_cast<f4 *>(lds) + wave * (kRowsAt * kQuads);
+    const int64_t col = col0 + wn + lane % kLanes * N;
+    Row extra[kGroup];
+    const auto beside = [&](int r0, Row (&to)[kGroup]) {
+        if (a.splits > 1 || col >= a.n) return;
+#pragma unroll
+        for (int q = 0; q < kGroup; ++q) {
+            const int r = r0 + q * kPass + lane / kLanes;
+            if (r < kTileM && row0 + wm + r < row_end)
+                Epilogue<T, MODE, N>::read(a, row0 + wm + r, col, to[q]);
+        }
+    };
+
     const int64_t slabs = (k_end - k0 + kSlab - 1) / kSlab;
+    if (slabs == 0) beside(0, extra);
     if (slabs > 0) {
         SideA sa;
         SideB sb;
@@ -530,6 +555,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
             times(Int<0>());
             __builtin_amdgcn_sched_barrier(0);   // the products come before the waits
             if (k < 0) {
+                beside(0, extra);
                 times(Int<1>());
                 return;
             }
@@ -562,19 +588,10 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
     }
 
     // Through LDS, so that a lane holds 16 bytes of a row of the result: the
-    // waves' own parts, 64 rows at a time, quads of columns exchanged by row so that
-    // all banks are met.
+    // waves' own parts, up to 64 rows at a time, quads of columns exchanged by row so
+    // that all banks are met.
     __syncthreads();
-    constexpr int N = 16 / sizeof(T), kQuads = kTileN / 4;
-    constexpr int kFits = 2 * kBytes / (WM * WN * kTileN * 4);   // rows of a wave's part
-    constexpr int kMost = kFits >= 64 ? 64 : kFits >= 32 ? 32 : 16;
-    constexpr int kRowsAt = kTileM < kMost ? kTileM : kMost;
-    constexpr int kLanes = kTileN / N, kPass = 64 / kLanes;
-    constexpr int kGroup = kRowsAt / kPass < 4 ? kRowsAt / kPass : 4;
-    static_assert(WM * WN * kRowsAt * kTileN * 4 <= 2 * kBytes, "fits in the slabs' LDS");
-    f4 *mine = reinterpret_cast<f4 *>(lds) + wave * (kRowsAt * kQuads);
-    const int64_t col = col0 + wn + lane % kLanes * N;
-    Epilogue<T, MODE, N> end(a, col < a.n ? col : 0, batch);
+    const Epilogue<T, MODE, N> end(a, col < a.n ? col : 0, batch);
 #pragma unroll
     for (int x0 = 0; x0 < FM; x0 += kRowsAt / 16) {
 #pragma unroll
@@ -583,20 +600,15 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
             for (int y = 0; y < FN; ++y)
                 mine[(16 * x + i) * kQuads + ((4 * y + g) ^ (i & (kQuads - 1)))] = acc[x0 + x][y];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        const int64_t first = row0 + wm + 16 * x0 + lane / kLanes;
 #pragma unroll 1
         for (int p = 0; p < kRowsAt / kPass; p += kGroup) {
-            typename Epilogue<T, MODE, N>::Row extra[kGroup];
-            if (a.splits == 1 && col < a.n) {
-#pragma unroll
-                for (int q = 0; q < kGroup; ++q)
-                    if (first + (p + q) * kPass < row_end)
-                        end.read(first + (p + q) * kPass, extra[q]);
-            }
+            // what lies beside the next rows is read while these are worked on
+            Row next[kGroup];
+            beside(16 * x0 + (p + kGroup) * kPass, next);
 #pragma unroll
             for (int q = 0; q < kGroup; ++q) {
                 const int r = (p + q) * kPass + lane / kLanes;
-                const int64_t row = first + (p + q) * kPass;
+                const int64_t row = row0 + wm + 16 * x0 + r;
                 float v[N];
 #pragma unroll
                 for (int e = 0; e < N / 4; ++e) {
@@ -624,6 +636,8 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
                         a.dots[row * a.dot_cols + (col0 + wn) / kTileN] = dot;
                 }
             }
+#pragma unroll
+            for (int q = 0; q < kGroup; ++q) extra[q] = next[q];
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
@@ -658,7 +672,7 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a, int64_t ld) {
             float u[4] = {v[0], v[1], v[2], v[3]};
             const Epilogue<T, MODE, 4> end(a, col, batch);
             typename Epilogue<T, MODE, 4>::Row extra;
-            end.read(row, extra);
+            end.read(a, row, col, extra);
             end.write(row, extra, u);
         }
     }
@@ -732,7 +746,7 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(ProductArgs a, int by_
             float u[4] = {acc[0], acc[1], acc[2], acc[3]};
             const Epilogue<T, kForward, 4> end(a, col, batch);
             typename Epilogue<T, kForward, 4>::Row extra;
-            end.read(row, extra);
+            end.read(a, row, col, extra);
             end.write(row, extra, u);
         }
     }

@@ -51,12 +51,15 @@ __device__ inline unsigned long long row_ballot(bool is) {
 // 1 / (1 + e^-s) in the roundings of its three operations.  The division: the
 // hardware's reciprocal is within one unit in the last place, and a step of
 // Newton's in fused operations rounds it correctly (Markstein), in a third of the
-// instructions; beyond 2^126, where the quotient is denormal, the division itself.
+// instructions.  Beyond 2^126, where the reciprocal would be denormal, the
+// divisor is scaled; infinity gives 0.
 __device__ inline float sigmoid(float s) {
     const float d = 1.f + expf(-s);
-    if (!(d < 0x1p126f)) return 1.f / d;
-    const float r = __builtin_amdgcn_rcpf(d);
-    return fmaf(fmaf(-d, r, 1.f), r, r);
+    const bool far = d >= 0x1p126f;
+    const float b = far ? d * 0x1p-64f : d;
+    const float r = __builtin_amdgcn_rcpf(b);
+    const float q = fmaf(fmaf(-b, r, 1.f), r, r);
+    return far ? (d < INFINITY ? q * 0x1p-64f : 0.f) : q;
 }
 
 // Whole numbers in the order of the floats (equal zeros alike); kClosed for
@@ -78,6 +81,15 @@ __device__ inline int across_max_key(int v) {
                 max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
     }
     return v;
+}
+
+// Whether this is the first lane of its row for which `is` holds.
+template <int LANES>
+__device__ inline bool first_of_row(bool is, int lane) {
+    const unsigned long long all = __ballot(is);
+    if (LANES == 64) return is && (all & ((1ull << lane) - 1)) == 0;
+    const unsigned half = (unsigned)(threadIdx.x & 32 ? all >> 32 : all) >> (threadIdx.x & 16);
+    return is && (half & ((1u << lane) - 1)) == 0;
 }
 
 // V neighbouring values of a row from element e0 on, `fill` past its end.
@@ -110,9 +122,8 @@ __device__ inline void write_row(T *s, int e0, int experts, const float (&x)[V])
 }
 
 // The value that the choice goes by; -infinity: closed.
-__device__ inline float choice_value(float s, bool softmax, const float *bias, int e) {
-    float v = softmax ? s : sigmoid(s);
-    if (bias) v += bias[e];
+__device__ inline float choice_value(float s, bool softmax, float bias) {
+    const float v = (softmax ? s : sigmoid(s)) + bias;
     return s > -INFINITY && v > -INFINITY ? v : -INFINITY;
 }
 
@@ -203,9 +214,17 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a) {
         total = across_sum<LANES>(total);
         total = total > 0.f ? total : 1.f;
     }
+    float bias[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-        x[v] = e0 + v < a.experts ? choice_value(x[v], a.softmax, a.bias, e0 + v) : -INFINITY;
+    for (int v = 0; v < V; ++v) bias[v] = 0.f;
+    if (a.bias) read_row<float, V>(a.bias, e0, a.experts, 0.f, bias);
+    if (a.softmax) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = choice_value(x[v], true, bias[v]);
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = choice_value(x[v], false, bias[v]);
+    }
 
     if (a.groups > 1) {
         const int per = a.experts / a.groups, lanes = per / V;
@@ -258,15 +277,15 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a) {
 #pragma unroll
         for (int v = 1; v < V; ++v) best = max(best, key[v]);
         const int top = across_max_key<LANES>(best);
-        const unsigned long long who = row_ballot<LANES>(best == top);
-        if (__ffsll((long long)who) - 1 == lane) {
-            int mine = 0;
+        // the first lane that holds it, and its first element
+        int gone = -1;
 #pragma unroll
-            for (int v = V - 1; v >= 0; --v) mine = key[v] == top ? v : mine;
+        for (int v = V - 1; v >= 0; --v) gone = key[v] == top ? v : gone;
+        const bool won = first_of_row<LANES>(best == top, lane);
+        if (won) chosen[slot][j] = top != kClosed ? e0 + gone : -1;
+        gone = won ? gone : -1;
 #pragma unroll
-            for (int v = 0; v < V; ++v) key[v] = v == mine ? kClosed : key[v];
-            chosen[slot][j] = top != kClosed ? e0 + mine : -1;
-        }
+        for (int v = 0; v < V; ++v) key[v] = v == gone ? kClosed : key[v];
     }
     // a row's lanes are in one wave
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -291,7 +310,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_long_kernel(RouteArgs a) 
         const float x = (float)s[e];
         spoilt |= spoils(x, a.softmax);
         low = fmaxf(low, x);
-        pick[e] = choice_value(x, a.softmax, a.bias, e);
+        pick[e] = choice_value(x, a.softmax, a.bias ? a.bias[e] : 0.f);
     }
     const bool bad = __syncthreads_or(spoilt);
     float total = 1.f;
@@ -564,6 +583,7 @@ __global__ __launch_bounds__(kSortThreads) void dispatch_place_kernel(DispatchAr
     for (int h = 0; h < kHeld; ++h) {
         const int64_t s = w0 + h * 64 + lane;
         const int e = held[h];
+        if (w0 + h * 64 >= end) break;
         // the lanes that hold the same expert
         unsigned long long same = __ballot(e >= 0);
         for (int b = 1; b < a.experts; b <<= 1) {
