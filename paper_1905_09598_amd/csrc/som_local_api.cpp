@@ -74,7 +74,9 @@ ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus) {
             const double rounds = full <= 4.0 ? std::ceil(full) : full + 0.5;
             const double join = parts > 1 ? 4.0 + 0.2 * parts + floats * 4.0 * (1 / 3.0e6 + 1 / 4.0e6)
                                           : 0.0;
-            const double time = rounds * (((slabs + parts - 1) / parts) * each + s.ends) + join;
+            // finding a tile's expert and its rows takes several reads in turn
+            const double ends = s.ends + (a.offsets ? 8.0 : 0.0);
+            const double time = rounds * (((slabs + parts - 1) / parts) * each + ends) + join;
             if (time < best.time) {
                 best.time = time;
                 best.tile = s.tile;
@@ -783,14 +785,13 @@ som_status som_route(const som_route_call *c) {
             return SOM_E_ARG;
     }
     const hipStream_t s = reinterpret_cast<hipStream_t>(c->stream);
+    const som::DispatchArgs sort = dispatch_args(c->index, c->n, c->k, c->experts, c->offsets,
+                                                 c->order, c->place, c->workspace);
+    const som::RouteArgs a = route_args(*c);
+    const bool together = c->offsets && som::route_sorts(a);
     return from_hip(in_order(
-        [&] { return som::launch_route(route_args(*c), s); },
-        [&] {
-            return c->offsets ? som::launch_dispatch(
-                                    dispatch_args(c->index, c->n, c->k, c->experts, c->offsets,
-                                                  c->order, c->place, c->workspace), s)
-                              : hipSuccess;
-        }));
+        [&] { return som::launch_route(a, together ? &sort : nullptr, s); },
+        [&] { return c->offsets && !together ? som::launch_dispatch(sort, s) : hipSuccess; }));
 }
 
 }  // extern "C"

@@ -148,6 +148,21 @@ struct ProductPlan {
     int64_t partial_floats;
 };
 
+// The expert with the `rank`-th most rows (the lower of equals first), of up to 64;
+// of more, where the sizes of those that run together even out, expert `rank`.
+__device__ inline int expert_of_rank(const int32_t *offsets, int experts, int rank) {
+    if (experts > 64) return rank;
+    const int lane = threadIdx.x & 63;
+    const int rows = lane < experts ? offsets[lane + 1] - offsets[lane] : -1;
+    int before = 0;
+    for (int e = 0; e < experts; ++e) {
+        const int other = __builtin_amdgcn_readlane(rows, e);
+        before += other > rows || (other == rows && e < lane) ? 1 : 0;
+    }
+    const unsigned long long who = __ballot(lane < experts && before == rank);
+    return __builtin_amdgcn_readfirstlane(__ffsll((long long)who) - 1);
+}
+
 // Copies `rows` rows of `cols` elements, `lds` apart, to rows of ldd >= cols
 // elements filled up with zeros; with z (rows ldz apart), times act'(z); with a
 // list, row r is src's row list[r] / per, or zeros where list[r] is negative, times
@@ -228,7 +243,6 @@ struct RouteArgs {
     int32_t dweight_type;
     void *dscores;
 };
-hipError_t launch_route(const RouteArgs &a, hipStream_t stream);
 hipError_t launch_route_backward(const RouteArgs &a, hipStream_t stream);
 
 struct DispatchArgs {
@@ -241,6 +255,10 @@ struct DispatchArgs {
 };
 int32_t dispatch_blocks(int64_t slots);
 hipError_t launch_dispatch(const DispatchArgs &a, hipStream_t stream);
+// Whether the routing's kernel can sort its slots too (few, in one workgroup), and
+// the routing, with that sort if it is given.
+bool route_sorts(const RouteArgs &a);
+hipError_t launch_route(const RouteArgs &a, const DispatchArgs *sort, hipStream_t stream);
 
 // som_adamw.hip
 constexpr int kAdamwBlock = 256, kAdamwChunk = 2048, kAdamwGrads = 256;

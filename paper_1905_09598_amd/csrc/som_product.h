@@ -430,12 +430,17 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
     int64_t row0, row_end, col0, k0 = 0, k_end = a.k;
     int batch = 0;
     if (MODE == kWeight) {
-        const int64_t tm = (a.m + TM - 1) / TM;
-        int64_t t = xcd_tile(blockIdx.x, gridDim.x), m, n;
-        batch = (int)(t / (tm * tn));
-        band_tile(t - batch * tm * tn, tm, tn, &m, &n);
+        // expert by expert, the largest first, each over all XCDs: a tile's time is
+        // its expert's rows
+        const unsigned tm = (unsigned)((a.m + TM - 1) / TM), tiles = tm * (unsigned)tn;
+        batch = (int)(blockIdx.x / tiles);
+        int64_t m, n;
+        band_tile(xcd_tile(blockIdx.x - batch * tiles, tiles), tm, tn, &m, &n);
         row0 = m * TM, col0 = n * TN, row_end = a.m;
-        if (a.offsets) k0 = a.offsets[batch], k_end = a.offsets[batch + 1];
+        if (a.offsets) {
+            batch = expert_of_rank(a.offsets, a.experts, batch);
+            k0 = a.offsets[batch], k_end = a.offsets[batch + 1];
+        }
     } else {
         const int64_t tm = gridDim.x / tn;
         int64_t m, n;

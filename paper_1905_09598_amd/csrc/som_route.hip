@@ -184,9 +184,34 @@ __device__ inline void write_choices(const RouteArgs &a, int64_t row, int lane, 
     }
 }
 
+// The slots of a workgroup's rows in the order of their experts, where these are
+// all the slots (up to kSortSlots): a slot's row is the number of slots that come
+// before it.  expert: their experts, in LDS.
+constexpr int kSortSlots = 64;
+__device__ inline void sort_few(const DispatchArgs &a, const int *expert) {
+    const int slots = (int)a.slots, t = threadIdx.x;
+    if (t < slots) {
+        const int e = expert[t];
+        int before = 0, there = 0;
+        for (int s = 0; s < slots; ++s) {
+            const int o = expert[s];
+            there += o >= 0 ? 1 : 0;
+            before += o >= 0 && (o < e || (o == e && s < t)) ? 1 : 0;
+        }
+        a.place[t] = e >= 0 ? before : -1;
+        if (e >= 0) a.order[before] = t;
+        if (t >= there) a.order[t] = -1;
+    }
+    for (int e = t; e <= a.experts; e += kRouteThreads) {
+        int below = 0;
+        for (int s = 0; s < slots; ++s) below += expert[s] >= 0 && expert[s] < e ? 1 : 0;
+        a.offsets[e] = below;
+    }
+}
+
 // LANES lanes a row, V experts a lane.
 template <typename T, int LANES, int V>
-__global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a) {
+__global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, DispatchArgs sort) {
     constexpr int kRows = kRouteThreads / LANES;
     extern __shared__ float shared[];  // with groups that lanes do not hold whole: the values
     __shared__ int chosen[kRows][LANES];
@@ -291,6 +316,14 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     const int at = lane < a.k ? chosen[slot][lane] : -1;
     if (there) write_choices<T, LANES>(a, row, lane, at, bad, low, total);
+    if (sort.offsets) {   // one workgroup
+        int *expert = &chosen[0][0];
+        __syncthreads();
+        if (there && lane < a.k && row * a.k + lane < kSortSlots)
+            expert[row * a.k + lane] = bad ? -1 : at;
+        __syncthreads();
+        sort_few(sort, expert);
+    }
 }
 
 // One row a workgroup of 256 threads, its values in LDS; thread t looks after
@@ -613,22 +646,22 @@ hipError_t room_for(K kernel, size_t bytes) {
 }
 
 template <typename T>
-hipError_t launch_route_type(const RouteArgs &a, hipStream_t stream) {
+hipError_t launch_route_type(const RouteArgs &a, const DispatchArgs &sort, hipStream_t stream) {
     const bool wide = a.k > 16 || a.groups > 16;
     const auto blocks = [&](int rows) { return (unsigned)((a.n + rows - 1) / rows); };
     const auto lds = [&](int rows) {
         return a.groups > 1 ? (size_t)rows * (a.experts + 1) * sizeof(float) : 0;
     };
     if (a.experts <= 64 && !wide)
-        route_kernel<T, 16, 4><<<blocks(16), kRouteThreads, lds(16), stream>>>(a);
+        route_kernel<T, 16, 4><<<blocks(16), kRouteThreads, lds(16), stream>>>(a, sort);
     else if (a.experts <= 256 && !wide)
-        route_kernel<T, 16, 16><<<blocks(16), kRouteThreads, lds(16), stream>>>(a);
+        route_kernel<T, 16, 16><<<blocks(16), kRouteThreads, lds(16), stream>>>(a, sort);
     else if (a.experts <= 512)
-        route_kernel<T, 64, 8><<<blocks(4), kRouteThreads, lds(4), stream>>>(a);
+        route_kernel<T, 64, 8><<<blocks(4), kRouteThreads, lds(4), stream>>>(a, sort);
     else if (a.experts <= 1024)
-        route_kernel<T, 64, 16><<<blocks(4), kRouteThreads, lds(4), stream>>>(a);
+        route_kernel<T, 64, 16><<<blocks(4), kRouteThreads, lds(4), stream>>>(a, sort);
     else if (a.experts <= 2048)
-        route_kernel<T, 64, 32><<<blocks(4), kRouteThreads, lds(4), stream>>>(a);
+        route_kernel<T, 64, 32><<<blocks(4), kRouteThreads, lds(4), stream>>>(a, sort);
     else {
         const hipError_t e = room_for(route_long_kernel<T>, a.experts * sizeof(float));
         if (e != hipSuccess) return e;
@@ -660,12 +693,18 @@ hipError_t launch_backward_type(const RouteArgs &a, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_route(const RouteArgs &a, hipStream_t stream) {
+bool route_sorts(const RouteArgs &a) {
+    const int rows = a.experts <= 256 && a.k <= 16 && a.groups <= 16 ? 16 : 4;  // of a workgroup
+    return a.n > 0 && a.n <= rows && a.n * a.k <= kSortSlots && a.experts <= 2048;
+}
+
+hipError_t launch_route(const RouteArgs &a, const DispatchArgs *sort, hipStream_t stream) {
     if (a.n == 0) return hipSuccess;
+    const DispatchArgs with = sort ? *sort : DispatchArgs{};
     switch (a.type) {
-        case kF32: return launch_route_type<float>(a, stream);
-        case kBF16: return launch_route_type<__bf16>(a, stream);
-        default: return launch_route_type<_Float16>(a, stream);
+        case kF32: return launch_route_type<float>(a, with, stream);
+        case kBF16: return launch_route_type<__bf16>(a, with, stream);
+        default: return launch_route_type<_Float16>(a, with, stream);
     }
 }
 

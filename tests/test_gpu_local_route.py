@@ -200,6 +200,20 @@ def test_dispatch(n, k, experts):
     assert torch.equal(r.load.cpu().long(), count)
 
 
+@pytest.mark.parametrize("n,experts,k", [(1, 64, 2), (16, 256, 4), (17, 256, 4), (4, 300, 16),
+                                         (5, 300, 3), (1, 2048, 64), (2, 100, 40), (3, 20, 20),
+                                         (16, 30, 5)])
+def test_few_slots_are_sorted_with_the_routing(n, experts, k):
+    s = _scores(n, experts, torch.bfloat16, seed=n + k, closed=0.5)
+    s[n // 2] = -INF
+    if n > 2:
+        s[0, 0] = float("nan")
+    r, _ = _check(s, k)
+    again = local.dispatch(r.index, r.weight, experts)
+    for name in ("offsets", "order", "place"):
+        assert torch.equal(getattr(r, name), getattr(again, name))
+
+
 def test_dispatch_counts_strange_entries_as_absent():
     index = torch.tensor([[0, 7], [-5, 2], [3, 1 << 30]], dtype=torch.int32).cuda()
     r = local.dispatch(index, None, 3)
