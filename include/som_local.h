@@ -207,8 +207,8 @@ som_status som_dispatch(const int32_t *index, int64_t n, int32_t k, int32_t expe
  * elements on (som_adamw_room elements in all; what lies between tensors is
  * not touched).  With bits = 32 they are fp32 m and v.  With bits = 8 they are e4m3
  * codes (OCP: 448 the largest) of m and of sqrt(v) in units of one fp32 scale per
- * 256 elements, the largest magnitude / 448, at least 1e-30 / 448; a sqrt(v)
- * above 0 is never held as 0, so that no step divides by eps alone.  The step
+ * 256 elements, the largest magnitude (at least 1e-30) / 448; a sqrt(v) above 0
+ * is never held as 0, so that no step divides by eps alone.  The step
  * itself uses the new m and v before they are rounded.  With master the
  * parameters are kept in fp32 there and `param` is their rounding; without,
  * `param` itself is updated and rounded. */

@@ -135,8 +135,9 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamwArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (e >= left) m[e] = root[e] = 0.f;
+            // in units of 448 / top, as a reciprocal and a product
             const float tm = scale_top(wave_top(m)), tr = scale_top(wave_top(root));
-            const float im = 448.f / tm, ir = 448.f / tr;
+            const float im = (1.f / tm) * 448.f, ir = (1.f / tr) * 448.f;
             float qm[4], qr[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -150,8 +151,8 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamwArgs a) {
                 store_codes(static_cast<unsigned char *>(a.square) + st, to_codes(qr), left);
             }
             if (lane == 0) {
-                a.mean_scale[st / kAdamwBlock] = tm / 448.f;
-                a.square_scale[st / kAdamwBlock] = tr / 448.f;
+                a.mean_scale[st / kAdamwBlock] = tm * (1.f / 448.f);
+                a.square_scale[st / kAdamwBlock] = tr * (1.f / 448.f);
             }
         } else {
             write_typed<float>(a.mean, st, left, m);

@@ -447,9 +447,13 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(RouteArgs
     float mean = 0.f, low = 0.f, by_total = 1.f;
     const bool whole = a.softmax && !a.renormalise;
     float x[V];
+    // the share of each choice in its row's sum (renormalised): exactly 1 where there
+    // is one, so that its gradient is exactly 0
+    const float share = a.scale != 0.f ? weight / a.scale : 0.f;
+    const float inner = across_sum<LANES>(g * share);
     if (a.softmax) {
-        mean = across_sum<LANES>(g * weight);  // scale sum of g p
-        part = weight * (g - (a.scale != 0.f ? mean / a.scale : 0.f));
+        mean = a.scale * inner;
+        part = weight * (g - inner);
         if (whole) {
             low = -INFINITY;
             for (int e0 = lane * V; e0 < a.experts; e0 += kWide) {
@@ -474,9 +478,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(RouteArgs
         float by = a.scale;
         if (a.renormalise) {
             const float sum = across_sum<LANES>(p);
-            const float inner = across_sum<LANES>(g * p);
             by = sum > 0.f ? a.scale / sum : 0.f;
-            g -= sum > 0.f ? inner / sum : 0.f;
+            g -= inner;
         }
         part = by * g * p * (1.f - p);
     }

@@ -158,6 +158,13 @@ def test_gradient(n, experts, k, renormalise, gate, dtype):
                       64 * O.V * mag + O.stored(s64.grad.nan_to_num(0.0), T[dtype])), "dscores")
 
 
+@pytest.mark.parametrize("gate", list(local.GATES))
+def test_one_renormalised_choice_has_no_gradient(gate):
+    s = _scores(200, 9, torch.float32, seed=4)
+    r = local.route(s, 1, gate=gate, scale=1.7)
+    assert not local.route_backward(torch.randn(200, 1, device="cuda"), s, r).any()
+
+
 def test_gradient_is_the_slope_of_the_loss():
     for gate in local.GATES:
         for renormalise in (True, False):
