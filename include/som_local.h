@@ -107,7 +107,7 @@ typedef struct som_experts_call {
     int32_t type;              /* som_type of all matrices                           */
     int32_t activation;        /* som_activation                                     */
     int64_t n;                 /* documents; 0 is allowed                            */
-    int32_t k, experts;        /* choices of a document; n k <= 2^31 - 1             */
+    int32_t k, experts;        /* choices of a document, n k <= 2^31 - 1; 1 .. 16384 */
     int32_t inner, hidden;     /* 1 .. 4,000,000; x's width, w1's rows               */
     int32_t outer;             /* w2's rows; without w2 equal to hidden              */
     const void *x;
@@ -132,7 +132,8 @@ typedef struct som_experts_call {
 } som_experts_call;
 
 /* Errors: as som_linear, and SOM_E_ARG (b2 without w2, an activation, kept arrays
- * or another outer without w2, only one of z and scaled). */
+ * or another outer without w2, only one of z and scaled), SOM_E_UNSUPPORTED (more
+ * than 16384 experts, n k or experts times hidden or outer above 2^31 - 1). */
 som_status som_experts_workspace(const som_experts_call *call, int32_t backward,
                                  uint64_t *bytes);
 som_status som_experts(const som_experts_call *call);

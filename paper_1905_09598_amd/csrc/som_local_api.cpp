@@ -552,7 +552,7 @@ som_status experts_sizes_ok(const som_experts_call *c) {
                    c->activation != SOM_ACT_NONE))
         return SOM_E_ARG;
     if (c->inner > som::kMaxWidth || c->hidden > som::kMaxWidth || c->outer > som::kMaxWidth ||
-        (__int128)c->n * c->k > INT32_MAX ||
+        (__int128)c->n * c->k > INT32_MAX || c->experts > som::kMaxExperts ||
         (int64_t)c->experts * std::max(c->hidden, c->outer) > INT32_MAX)
         return SOM_E_UNSUPPORTED;
     return SOM_OK;

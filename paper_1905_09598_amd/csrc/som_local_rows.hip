@@ -84,22 +84,22 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(SumsArgs a) {
     constexpr int N = 16 / sizeof(T);
     __shared__ float part[kSumLanes][kSumPieces * N + 4];
     const int piece = threadIdx.x % kSumPieces, lane = threadIdx.x / kSumPieces;
-    int64_t first = (int64_t)blockIdx.y * kSumRows, end = a.rows;
+    int64_t first = (int64_t)blockIdx.x * kSumRows, end = a.rows;
     int e = 0;
     if (DIRECT) {
-        e = blockIdx.y;
+        e = blockIdx.x;
         first = a.offsets ? a.offsets[e] : 0;
         if (a.offsets) end = a.offsets[e + 1];
     } else {
         if (a.offsets) {
-            e = expert_of(a.offsets, a.experts, kSumRows, blockIdx.y);
-            first = a.offsets[e] + ((int64_t)blockIdx.y - (a.offsets[e] / kSumRows + e)) * kSumRows;
+            e = expert_of(a.offsets, a.experts, kSumRows, blockIdx.x);
+            first = a.offsets[e] + ((int64_t)blockIdx.x - (a.offsets[e] / kSumRows + e)) * kSumRows;
             end = a.offsets[e + 1];
         }
         end = first + kSumRows < end ? first + kSumRows : end;
         if (first >= end) return;
     }
-    const int64_t col = ((int64_t)blockIdx.x * kSumPieces + piece) * N, left = a.cols - col;
+    const int64_t col = ((int64_t)blockIdx.y * kSumPieces + piece) * N, left = a.cols - col;
     float sum[N], bias[N];
 #pragma unroll
     for (int c = 0; c < N; ++c) sum[c] = bias[c] = 0.f;
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(SumsArgs a) {
 #pragma unroll
                 for (int o = 1; o < kSumPieces; o <<= 1) dot += __shfl_xor(dot, o);
                 const int64_t r = r0 + u * kSumLanes;
-                if (piece == 0 && r < end) a.dots[r * a.dot_cols + blockIdx.x] = dot;
+                if (piece == 0 && r < end) a.dots[r * a.dot_cols + blockIdx.y] = dot;
             }
         }
     }
@@ -142,12 +142,12 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(SumsArgs a) {
     for (int c = 0; c < N; ++c) part[lane][piece * N + c] = sum[c];
     __syncthreads();
     const int c = threadIdx.x;
-    const int64_t at = (int64_t)blockIdx.x * kSumPieces * N + c;
+    const int64_t at = (int64_t)blockIdx.y * kSumPieces * N + c;
     if (c < kSumPieces * N && at < a.cols) {
         float v = 0.f;
         for (int l = 0; l < kSumLanes; ++l) v += part[l][c];
         if (DIRECT) static_cast<T *>(a.out)[e * a.cols + at] = (T)v;
-        else a.partial[blockIdx.y * a.cols + at] = v;
+        else a.partial[blockIdx.x * a.cols + at] = v;
     }
 }
 
@@ -286,8 +286,8 @@ hipError_t launch_sums(const SumsArgs &a, hipStream_t stream) {
     const bool direct = sums_direct(a);
     const int64_t high = direct ? experts : sums_parts(a);
     const int64_t wide = (a.cols * size + 16 * kSumPieces - 1) / (16 * kSumPieces);
-    if (high > 65535 || experts > 65535) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)wide, (unsigned)high);
+    if (high > INT32_MAX || wide > 65535 || experts > 65535) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)high, (unsigned)wide);
     constexpr int kCols = kSumThreads / kSumLanes;
     const dim3 join((unsigned)((a.cols + kCols - 1) / kCols), experts);
     return by_type(a.type, [&](auto t) {

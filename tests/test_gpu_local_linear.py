@@ -109,6 +109,18 @@ def test_rows_beyond_32_bits():
     _check(big, w, b, None, dy, "relu")
 
 
+def test_sums_of_many_rows():
+    # small whole numbers: every partial sum is exact, whatever the order
+    n = 8_500_000
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x, dy = (torch.randint(-1, 2, (n, 8), generator=g, device="cuda").to(torch.bfloat16)
+             for _ in range(2))
+    w = _draw(1, 8, 8, dtype=torch.bfloat16)
+    _, dw, db = local.linear_backward(dy, x, w)
+    assert torch.equal(db, dy.double().sum(0).to(torch.bfloat16))
+    assert torch.equal(dw, (dy.double().t() @ x.double()).to(torch.bfloat16))
+
+
 def test_long_contraction_is_split_and_joined():
     # few tiles, long sums: the contraction is split and joined in a fixed order
     for n, inner, outer in ((40, 20000, 24), (70, 9001, 30)):

@@ -153,3 +153,13 @@ def test_adamw_room_and_refusals():
     assert not out.value
     table[1].count = -1
     assert L.som_adamw_room(table, 3) == -1
+
+
+def test_experts_beyond_what_a_routing_holds():
+    L, need = local.lib(), C.c_uint64()
+    call = local._ExpertsCall(n=4, k=2, experts=16385, inner=8, hidden=8, outer=8, ldx=8,
+                              lddy=8, w2=1)
+    assert status(L.som_experts(C.byref(call))) == "SOM_E_UNSUPPORTED"
+    assert status(L.som_experts_backward(C.byref(call))) == "SOM_E_UNSUPPORTED"
+    call.experts = 16384
+    assert status(L.som_experts_workspace(C.byref(call), 1, C.byref(need))) == "SOM_OK"
