@@ -80,8 +80,8 @@ som_status som_linear_workspace(const som_linear_call *call, int32_t backward, u
 
 /* Errors of both: SOM_E_ARG (a bad type, activation or size, a missing or too
  * short array, a leading dimension below its row, a workspace that is missing,
- * misaligned or too small), SOM_E_UNSUPPORTED (inner or outer above 4,000,000,
- * more than 2^31 - 1 tiles), SOM_E_DEVICE. */
+ * misaligned or too small), SOM_E_UNSUPPORTED (inner or outer above 4,000,000;
+ * results of 2^36 elements, the columns counted in whole 64s), SOM_E_DEVICE. */
 som_status som_linear(const som_linear_call *call);
 som_status som_linear_backward(const som_linear_call *call);
 

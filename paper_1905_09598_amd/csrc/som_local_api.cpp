@@ -733,7 +733,7 @@ som_status som_dispatch_workspace(int64_t n, int32_t k, int32_t experts, uint64_
     if (!bytes || n < 0 || k < 1 || experts < 1 || experts > som::kMaxExperts) return SOM_E_ARG;
     if ((__int128)n * k > INT32_MAX) return SOM_E_UNSUPPORTED;
     const int32_t blocks = som::dispatch_blocks(n * k);
-    *bytes = blocks > 1 ? (uint64_t)blocks * experts * 4 : 0;
+    *bytes = blocks > 1 ? ((uint64_t)blocks + 1) * experts * 4 : 0;
     return SOM_OK;
 }
 

@@ -13,6 +13,11 @@ enum : int32_t { kForward = 0, kInput = 1, kWeight = 2, kGate = 3 };    // which
 
 inline int type_size(int32_t type) { return type == kF32 ? 4 : 2; }
 
+// A dimension of a grid counts its threads in 32 bits.
+inline bool grid_holds(int64_t blocks, int64_t threads) {
+    return blocks <= ((int64_t)UINT32_MAX) / threads;
+}
+
 // The activations and their slopes, on the hardware's exponential and reciprocal
 // (each within one unit in the last place): an exact division or the library's
 // error function would take longer than the products they follow (gelu of
@@ -250,8 +255,8 @@ struct DispatchArgs {
     int64_t slots;
     int32_t experts;
     int32_t *offsets, *order, *place;
-    int32_t *counts;        // blocks x experts
-    int32_t blocks;
+    int32_t *counts;        // (blocks + 1) x experts
+    int32_t blocks, scanned;
 };
 int32_t dispatch_blocks(int64_t slots);
 hipError_t launch_dispatch(const DispatchArgs &a, hipStream_t stream);

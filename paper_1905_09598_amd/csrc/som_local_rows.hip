@@ -286,7 +286,8 @@ hipError_t launch_sums(const SumsArgs &a, hipStream_t stream) {
     const bool direct = sums_direct(a);
     const int64_t high = direct ? experts : sums_parts(a);
     const int64_t wide = (a.cols * size + 16 * kSumPieces - 1) / (16 * kSumPieces);
-    if (high > INT32_MAX || wide > 65535 || experts > 65535) return hipErrorInvalidValue;
+    if (!grid_holds(high, kSumThreads) || wide > 65535 || experts > 65535)
+        return hipErrorInvalidValue;
     const dim3 grid((unsigned)high, (unsigned)wide);
     constexpr int kCols = kSumThreads / kSumLanes;
     const dim3 join((unsigned)((a.cols + kCols - 1) / kCols), experts);
@@ -320,11 +321,16 @@ hipError_t launch_combine(const CombineArgs &args, hipStream_t stream) {
     });
 }
 
-hipError_t launch_dweight(const DweightArgs &a, hipStream_t stream) {
-    if (a.slots == 0) return hipSuccess;
-    const unsigned blocks = (unsigned)((a.slots * 4 + kThreads - 1) / kThreads);
-    return by_type(a.type, [&](auto t) {
-        dweight_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a);
+hipError_t launch_dweight(const DweightArgs &args, hipStream_t stream) {
+    const int size = type_size(args.type);
+    return in_rows(args.slots, 4, [&](int64_t s, int64_t slots, unsigned blocks) {
+        DweightArgs a = args;
+        a.slots = slots;
+        a.place += s;
+        a.dweight = static_cast<char *>(a.dweight) + s * size;
+        return by_type(a.type, [&](auto t) {
+            dweight_kernel<decltype(t)><<<blocks, kThreads, 0, stream>>>(a);
+        });
     });
 }
 

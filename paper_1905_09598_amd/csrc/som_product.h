@@ -763,7 +763,7 @@ hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
     const int64_t tm = MODE == kWeight ? (a.m + TM - 1) / TM * (a.offsets ? a.experts : 1)
                        : a.offsets     ? a.m / TM + a.experts
                                        : (a.m + TM - 1) / TM;
-    if (tm * tn > INT32_MAX) return hipErrorInvalidValue;
+    if (!grid_holds(tm * tn, WM * WN * 64)) return hipErrorInvalidValue;
     constexpr int kLds = 2 * (TM + TN) * 128;
     const auto kernel = product_kernel<T, MODE, LIST, DMA, TM, TN, WM, WN>;
     if (kLds > 64 * 1024) {
@@ -774,7 +774,7 @@ hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
     kernel<<<dim3((unsigned)(tm * tn), a.splits), WM * WN * 64, kLds, stream>>>(a);
     if (MODE != kGate && a.splits > 1) {
         const int64_t quads = a.partial_rows * ((a.n + 3) / 4);
-        if ((quads + 255) / 256 > INT32_MAX) return hipErrorInvalidValue;
+        if (!grid_holds((quads + 255) / 256, 256)) return hipErrorInvalidValue;
         join_kernel<T, MODE><<<(unsigned)((quads + 255) / 256), 256, 0, stream>>>(a, tn * TN);
     }
     return hipGetLastError();
@@ -801,7 +801,7 @@ hipError_t launch_rows(const ProductArgs &a, hipStream_t stream) {
     const int by_row = a.offsets && a.m < tiles;
     const int64_t high = by_row ? a.m : tiles;
     const int64_t wide = (a.n + 15) / 16;
-    if (high > 65535 || wide > INT32_MAX) return hipErrorInvalidValue;
+    if (high > 65535 || !grid_holds(wide, WAVES * 64)) return hipErrorInvalidValue;
     const dim3 grid((unsigned)wide, (unsigned)high);
     rows_kernel<T, WAVES><<<grid, WAVES * 64, 0, stream>>>(a, by_row);
     return hipGetLastError();

@@ -229,6 +229,40 @@ def test_dispatch_counts_strange_entries_as_absent():
     assert r.place.cpu().tolist() == [0, -1, -1, 1, -1, -1]
 
 
+@pytest.mark.parametrize("n,k,experts", [(300_000, 1, 9), (20_000, 2, 4000), (9000, 40, 300)])
+def test_dispatch_of_many_slots(n, k, experts):
+    # the order of a stable sort; absent slots behind all others
+    g = torch.Generator().manual_seed(n)
+    index = torch.randint(-1, experts, (n, k), generator=g, dtype=torch.int32)
+    r = local.dispatch(index.cuda(), None, experts)
+    key = index.flatten().long()
+    count = torch.bincount(key[key >= 0], minlength=experts)
+    assert torch.equal(r.offsets.cpu().long()[1:], count.cumsum(0)) and r.offsets[0] == 0
+    order = torch.sort(torch.where(key < 0, experts, key), stable=True).indices
+    there = int(count.sum())
+    assert torch.equal(r.order.cpu().long()[:there], order[:there])
+    assert (r.order[there:] == -1).all()
+    place = torch.full((n * k,), -1)
+    place[order[:there]] = torch.arange(there)
+    assert torch.equal(r.place.cpu().long().flatten(), place)
+
+
+def test_rows_beyond_one_launch():
+    # a block of rows over and over: its answers over and over
+    g = torch.Generator().manual_seed(8)
+    block = torch.randn(1000, 4, generator=g).cuda()
+    n = 8_400_000
+    scores = block.repeat(n // 1000, 1)
+    few, many = local.route(block, 2), local.route(scores, 2)
+    assert (many.index.view(-1, 1000, 2) == few.index).all()
+    assert (many.weight.view(-1, 1000, 2) == few.weight).all()
+    assert torch.equal(many.offsets[1:], few.offsets[1:] * (n // 1000))
+    d = torch.randn(1000, 2, generator=g).cuda()
+    want = local.route_backward(d, block, few)
+    got = local.route_backward(d.repeat(n // 1000, 1), scores, many)
+    assert (got.view(-1, 1000, 4) == want).all()
+
+
 def test_capture_into_a_graph():
     s = _scores(5000, 96, torch.bfloat16, seed=2)
     dw = torch.randn(5000, 4, device="cuda")
