@@ -702,7 +702,7 @@ __device__ inline i4 piece(const T *row, int64_t k, int64_t k_end) {
 
 template <typename T, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void rows_kernel(ProductArgs a, int by_row) {
-    constexpr int kElems = 16 / sizeof(T), kSlab = 128 / sizeof(T), kAhead = 4;
+    constexpr int kElems = 16 / sizeof(T), kSlab = 128 / sizeof(T);
     __shared__ f4 part[WAVES][64];
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
     int batch = 0;
@@ -722,10 +722,12 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(ProductArgs a, int by_
     if (a.list) xrow = a.per.quotient(a.list[xrow]);
     const T *xr = static_cast<const T *>(a.a) + xrow * a.lda;
     f4 acc = {0.f, 0.f, 0.f, 0.f};
-    const auto slabs = [&](auto check, int64_t k) {
-        i4 fw[kAhead][2], fx[kAhead][2];
+    // `count` of the wave's slabs from k on
+    const auto slabs = [&](auto count, auto check, int64_t k) {
+        constexpr int kCount = decltype(count)::value;
+        i4 fw[kCount][2], fx[kCount][2];
 #pragma unroll
-        for (int s = 0; s < kAhead; ++s)
+        for (int s = 0; s < kCount; ++s)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int64_t c = k + (int64_t)s * WAVES * kSlab + (h * 4 + g) * kElems;
@@ -733,14 +735,18 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(ProductArgs a, int by_
                 fx[s][h] = piece<T, decltype(check)::value>(xr, c, a.k);
             }
 #pragma unroll
-        for (int s = 0; s < kAhead; ++s)
+        for (int s = 0; s < kCount; ++s)
 #pragma unroll
             for (int h = 0; h < 2; ++h) acc = multiply<T>(fw[s][h], fx[s][h], acc);
     };
+    const auto fits = [&](int count, int64_t k) {
+        return k + ((int64_t)(count - 1) * WAVES + 1) * kSlab <= a.k;
+    };
     int64_t k = (int64_t)wave * kSlab;
-    for (; k + ((kAhead - 1) * WAVES + 1) * kSlab <= a.k; k += (int64_t)kAhead * WAVES * kSlab)
-        slabs(Int<0>(), k);
-    if (k < a.k) slabs(Int<1>(), k);
+    for (; fits(4, k); k += 4 * WAVES * kSlab) slabs(Int<4>(), Int<0>(), k);
+    if (fits(2, k)) slabs(Int<2>(), Int<0>(), k), k += 2 * WAVES * kSlab;
+    if (fits(1, k)) slabs(Int<1>(), Int<0>(), k), k += WAVES * kSlab;
+    if (k < a.k) slabs(Int<1>(), Int<1>(), k);   // the last, in part
     part[wave][lane] = acc;
     __syncthreads();
     if (wave == 0) {
