@@ -53,22 +53,24 @@ __device__ inline unsigned long long row_ballot(bool is) {
 // Newton's in fused operations rounds it correctly (Markstein), in a third of the
 // instructions.  Beyond 2^126, where the reciprocal would be denormal, the
 // divisor is scaled; infinity gives 0.
+constexpr float kNear = 80.f;   // scores from -80 on are not that far
+template <bool NEAR = false>
 __device__ inline float sigmoid(float s) {
     const float d = 1.f + expf(-s);
-    const bool far = d >= 0x1p126f;
+    const bool far = !NEAR && d >= 0x1p126f;
     const float b = far ? d * 0x1p-64f : d;
     const float r = __builtin_amdgcn_rcpf(b);
     const float q = fmaf(fmaf(-b, r, 1.f), r, r);
     return far ? (d < INFINITY ? q * 0x1p-64f : 0.f) : q;
 }
 
-// Whole numbers in the order of the floats (equal zeros alike); kClosed for
-// -infinity, below all others.
-constexpr int kClosed = (int)0x80000000;
+// Whole numbers in the order of the floats (equal zeros alike), the least for
+// -infinity; those of NaN are never looked at.
 __device__ inline int key_of(float v) {
     const int b = __float_as_int(v + 0.f);
-    return v > -INFINITY ? b ^ (b >> 31 & 0x7fffffff) : kClosed;
+    return b ^ (b >> 31 & 0x7fffffff);
 }
+constexpr int kClosed = (int)(0xff800000u ^ 0x7fffffffu);
 
 template <int LANES>
 __device__ inline int across_max_key(int v) {
@@ -121,10 +123,10 @@ __device__ inline void write_row(T *s, int e0, int experts, const float (&x)[V])
     }
 }
 
-// The value that the choice goes by; -infinity: closed.
-__device__ inline float choice_value(float s, bool softmax, float bias) {
-    const float v = (softmax ? s : sigmoid(s)) + bias;
-    return s > -INFINITY && v > -INFINITY ? v : -INFINITY;
+// The value that the choice goes by; -infinity: closed.  p: the sigmoid of the score,
+// or the score itself.
+__device__ inline float choice_value(float s, float p, float bias) {
+    return s > -INFINITY ? fmaxf(p + bias, -INFINITY) : -INFINITY;   // NaN: -infinity
 }
 
 // Whether a score makes its whole row invalid.
@@ -245,21 +247,30 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, Dispa
     if (a.bias) read_row<float, V>(a.bias, e0, a.experts, 0.f, bias);
     if (a.softmax) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = choice_value(x[v], true, bias[v]);
+        for (int v = 0; v < V; ++v) x[v] = choice_value(x[v], x[v], bias[v]);
     } else {
+        float least = x[0];
 #pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = choice_value(x[v], false, bias[v]);
+        for (int v = 1; v < V; ++v) least = fminf(least, x[v]);
+        if (__all(least >= -kNear || e0 >= a.experts)) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[v] = choice_value(x[v], sigmoid<true>(x[v]), bias[v]);
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[v] = choice_value(x[v], sigmoid(x[v]), bias[v]);
+        }
     }
 
     if (a.groups > 1) {
         const int per = a.experts / a.groups, lanes = per / V;
         float best = -INFINITY, next = -INFINITY;
         int shift = 0;
-        if (per % V == 0 && (lanes & (lanes - 1)) == 0) {   // whole lanes, a power of two
+        const bool whole = per % V == 0 && (lanes & (lanes - 1)) == 0;   // lanes, a power of two
+        if (whole) {
             shift = 31 - __clz(lanes);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                next = fmaxf(next, fminf(best, x[v]));
+                next = __builtin_amdgcn_fmed3f(best, next, x[v]);   // next <= best
                 best = fmaxf(best, x[v]);
             }
             for (int o = 1; o < lanes; o <<= 1) {
@@ -285,12 +296,18 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, Dispa
         const float value = a.group_best == 2 && next > -INFINITY ? best + next : best;
         const unsigned long long stay =
             groups_that_stay<LANES>(value, lane, shift, a.groups, a.top_groups);
-        int left = per - e0 % per;
-        unsigned long long bits = e0 < a.experts ? stay >> e0 / per : 0;
+        if (whole) {
+            const bool stays = stay >> (lane >> shift) & 1;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            if (!(bits & 1)) x[v] = -INFINITY;
-            if (--left == 0) bits >>= 1, left = per;
+            for (int v = 0; v < V; ++v) x[v] = stays ? x[v] : -INFINITY;
+        } else {
+            int left = per - e0 % per;
+            unsigned long long bits = e0 < a.experts ? stay >> e0 / per : 0;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (!(bits & 1)) x[v] = -INFINITY;
+                if (--left == 0) bits >>= 1, left = per;
+            }
         }
     }
 
@@ -303,14 +320,17 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, Dispa
         for (int v = 1; v < V; ++v) best = max(best, key[v]);
         const int top = across_max_key<LANES>(best);
         // the first lane that holds it, and its first element
-        int gone = -1;
-#pragma unroll
-        for (int v = V - 1; v >= 0; --v) gone = key[v] == top ? v : gone;
         const bool won = first_of_row<LANES>(best == top, lane);
-        if (won) chosen[slot][j] = top != kClosed ? e0 + gone : -1;
-        gone = won ? gone : -1;
+        int at = 0;
+        bool seen = !won;
 #pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = v == gone ? kClosed : key[v];
+        for (int v = 0; v < V; ++v) {
+            const bool is = key[v] == top && !seen;
+            seen |= is;
+            at = is ? v : at;
+            key[v] = is ? kClosed : key[v];
+        }
+        if (won) chosen[slot][j] = top > kClosed ? e0 + at : -1;
     }
     // a row's lanes are in one wave
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -343,7 +363,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_long_kernel(RouteArgs a) 
         const float x = (float)s[e];
         spoilt |= spoils(x, a.softmax);
         low = fmaxf(low, x);
-        pick[e] = choice_value(x, a.softmax, a.bias ? a.bias[e] : 0.f);
+        pick[e] = choice_value(x, a.softmax ? x : sigmoid(x), a.bias ? a.bias[e] : 0.f);
     }
     const bool bad = __syncthreads_or(spoilt);
     float total = 1.f;
@@ -680,6 +700,14 @@ __global__ __launch_bounds__(kSortThreads) void dispatch_place_kernel(DispatchAr
     }
 }
 
+// Up to kSortSlots slots, in one workgroup.
+__global__ __launch_bounds__(kRouteThreads) void dispatch_few_kernel(DispatchArgs a) {
+    __shared__ int expert[kSortSlots];
+    if ((int)threadIdx.x < a.slots) expert[threadIdx.x] = expert_at(a, threadIdx.x, a.slots);
+    __syncthreads();
+    sort_few(a, expert);
+}
+
 // Lets a kernel have `bytes` of dynamic LDS where, with its own, they pass 64 KB.
 template <typename K>
 hipError_t room_for(K kernel, size_t bytes) {
@@ -789,6 +817,10 @@ int32_t dispatch_blocks(int64_t slots) {
 hipError_t launch_dispatch(const DispatchArgs &args, hipStream_t stream) {
     DispatchArgs a = args;
     const size_t one = a.experts * sizeof(int);
+    if (a.slots <= kSortSlots) {
+        dispatch_few_kernel<<<1, kRouteThreads, 0, stream>>>(a);
+        return hipGetLastError();
+    }
     a.scanned = a.blocks > kFewChunks || (int64_t)a.blocks * a.experts > kFewCounts;
     if (a.blocks > 1) {
         const hipError_t e = room_for(dispatch_count_kernel, one);
