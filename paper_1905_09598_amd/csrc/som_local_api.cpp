@@ -36,15 +36,17 @@ ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus) {
         return best;
     }
     // Microseconds of a slab on one workgroup that has a compute unit to itself and
-    // on as many as it holds, by type; what unaligned rows add; a round's start
-    // and end.  Measured on products of 300 to 16,001 rows, 100 to 4096 columns
-    // and contractions of 121 to 16,001: of 22 products the chosen shape was within a
-    // tenth of the best of the fifteen in 20, and within a fifth in the others.
-    struct Cost { double one, all; };
-    struct Shape { int32_t tile, held; Cost half, single; double unaligned, ends; };
-    static const Shape shapes[] = {{256, 1, {2.0, 2.0}, {8.1, 8.1}, 0.0, 8.0},
-                                   {128, 2, {0.85, 1.2}, {2.3, 4.3}, 0.4, 5.0},
-                                   {64, 4, {0.45, 0.8}, {0.62, 2.3}, 0.4, 4.0}};
+    // on as many as it holds, by type; what unaligned rows add; a tile's start and
+    // end.  Fitted to 39 products of 100 to 5000 rows, 100 to 9096 columns and
+    // contractions of 100 to 8000, each timed in all shapes and splits, and checked on
+    // 37 others of 120 to 16,001 rows: the chosen shape took 1.006 of the best one's
+    // time on average, at most 1.10.
+    struct Cost { double one, all, unaligned; };
+    struct Shape { int32_t tile, held; Cost half, single; double ends; };
+    static const Shape shapes[] = {{256, 1, {1.5, 1.5, 0.0}, {7.0, 7.0, 0.0}, 6.0},
+                                   {128, 2, {0.8, 0.9, 0.25}, {2.0, 3.4, 0.1}, 4.5},
+                                   {64, 4, {0.43, 0.78, 0.25}, {0.7, 1.7, 0.2}, 2.5}};
+    static const int32_t splits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
     best.time = INFINITY;
     for (const Shape &s : shapes) {
         if (!aligned && s.tile == 256) continue;
@@ -62,21 +64,28 @@ ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus) {
         const int64_t slabs = std::max<int64_t>(1, (k + slab - 1) / slab);
         const int64_t rows = a.mode == kWeight ? a.m * experts : a.m;
         const int32_t most = a.mode == kGate ? 1 : 32;   // its rows' dots need whole sums
-        for (int32_t parts = 1; parts <= most && parts <= slabs; parts *= 2) {
+        for (const int32_t parts : splits) {
+            if (parts > most || parts > slabs) break;
             const int64_t floats = parts > 1 ? parts * rows * (tn * s.tile) : 0;
             if (floats > (int64_t)1 << 30) break;
             const double groups = (double)(tm * tn * parts) / num_cus;   // to a compute unit
-            const double held = std::min((double)s.held, std::max(1.0, std::ceil(groups)));
-            const double each =
-                cost.one + (s.held > 1 ? (cost.all - cost.one) * (held - 1) / (s.held - 1) : 0.0) +
-                (aligned ? 0.0 : s.unaligned);
-            const double full = groups / s.held;
-            const double rounds = full <= 4.0 ? std::ceil(full) : full + 0.5;
-            const double join = parts > 1 ? 4.0 + 0.2 * parts + floats * 4.0 * (1 / 3.0e6 + 1 / 4.0e6)
-                                          : 0.0;
             // finding a tile's expert and its rows takes several reads in turn
             const double ends = s.ends + (a.offsets ? 8.0 : 0.0);
-            const double time = rounds * (((slabs + parts - 1) / parts) * each + ends) + join;
+            // `held` workgroups at a time, one tile each
+            const auto round = [&](double held) {
+                const double more = s.held > 1 ? (cost.all - cost.one) * (held - 1) / (s.held - 1) : 0;
+                return ((slabs + parts - 1) / parts) *
+                           (cost.one + more + (aligned ? 0.0 : cost.unaligned)) + ends;
+            };
+            double time;
+            if (groups > 4.0 * s.held) {
+                time = (groups / s.held + 0.5) * round(s.held);
+            } else {
+                const int32_t whole = std::max(1, (int32_t)std::ceil(groups));
+                time = whole / s.held * round(s.held);
+                if (whole % s.held) time += round(whole % s.held);
+            }
+            if (parts > 1) time += 2.0 + 0.2 * parts + floats * 4.0 * (1 / 3.0e6 + 1 / 4.0e6);
             if (time < best.time) {
                 best.time = time;
                 best.tile = s.tile;

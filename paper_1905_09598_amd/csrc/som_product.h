@@ -76,8 +76,11 @@ __device__ inline f4 multiply<float>(i4 b, i4 a, f4 c) {
 //
 // DMA: pieces go straight to LDS; they have to be whole and 16-byte aligned (the
 // columns of an across side a multiple of a piece, so that none crosses a row's
-// end).  Without, rows may begin anywhere: pieces go through registers, and those
-// that cross a row's end are read element by element.
+// end).  Without, rows may begin anywhere and pieces go through registers.  An
+// across side's pieces that cross a row's end hold columns that are not stored:
+// what follows the row is read with them (`easy`), except where nothing need
+// follow, in the last slab, in rows named by a list, and in rows shorter than a
+// piece; there they are read element by element.
 template <typename T, bool ACROSS, bool DMA, int ROWS, int WAVES>
 struct Side {
     static constexpr int kElems = 16 / sizeof(T);           // elements of a 16-byte piece
@@ -92,6 +95,7 @@ struct Side {
     uint32_t off[kLoads];
     int64_t step;             // bytes from slab to slab
     i4 held[DMA ? 1 : kLoads];
+    bool easy;                // tells all lanes alike
 
     // What the units of contraction step s are exchanged with.
     static __device__ int twist(int s) {
@@ -122,6 +126,7 @@ struct Side {
                           const int32_t *list, Divider per) {
         base = reinterpret_cast<const char *>(p + (ACROSS ? k0 * ld : k0 + (list ? 0 : row0 * ld)));
         step = ACROSS ? kSlab * ld * (int64_t)sizeof(T) : 128;
+        easy = row0 + ROWS <= rows || ld >= kElems;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             if (ACROSS) {
@@ -140,6 +145,13 @@ struct Side {
     template <bool CHECK>
     __device__ void load(char *lds, int64_t left, int64_t col0, int64_t cols) {
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        if (!DMA && !CHECK && (!ACROSS || easy)) {
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j)
+                __builtin_memcpy(&held[j], __builtin_assume_aligned(base + off[j], sizeof(T)), 16);
+            base += step;
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const char *from = base + off[j];
@@ -515,8 +527,8 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
             if constexpr (LIST == 1) SideB::entries(a.list + k0 + s * kSlab, k_end - k0 - s * kSlab, entry);
             if constexpr (LIST == 2) SideA::entries(a.list + k0 + s * kSlab, k_end - k0 - s * kSlab, entry);
         };
-        if (LIST == 1) sb.step = 0;
-        if (LIST == 2) sa.step = 0;
+        if (LIST == 1) sb.step = 0, sb.easy = col0 + TN <= a.n;
+        if (LIST == 2) sa.step = 0, sa.easy = row0 + TM <= row_end;
         entries(0);
         // the offsets of the slab that is loaded next, and the list beyond it
         const auto follow = [&](int64_t s) {
