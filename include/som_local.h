@@ -102,7 +102,8 @@ som_status som_linear_backward(const som_linear_call *call);
  * An expert without documents gets zeros.  The residual's gradient is dy.
  * Rounded to the element type on the way: h (scaled apart, from the same sums), z
  * where the slope is taken of it, dz; answers and each slot's part of dx are joined
- * in fp32. */
+ * in fp32.  dweight is formed as <w2_e^T dy_i, h> + <dy_i, b2_e> with h, in 16-bit
+ * types, the mean of act(z) and scaled / g. */
 typedef struct som_experts_call {
     int32_t type;              /* som_type of all matrices                           */
     int32_t activation;        /* som_activation                                     */

@@ -427,6 +427,7 @@ struct ExpertsBackward {
             a.argument = two ? c.z : c.x;
             a.ld_argument = two ? c.hidden : c.ldx;
             a.argument_listed = !two;
+            a.image = two && c.dweight && size == 2 ? c.scaled : nullptr;
             a.wide = !two;
             if (two) dz = work.take((uint64_t)slots * c.hidden * size);
             // without dx of local linear maps the products' rows are not wanted

@@ -136,6 +136,7 @@ struct ProductArgs {
     const void *argument;             // gate: rows of n, ld_argument apart
     int64_t ld_argument;
     int32_t argument_listed;          // row r's is the document's, slots[r] / per
+    const void *image;                // rows of n: gate act(argument), rounded; or null
     float *dots;                      // gate: m x dot_cols
     int32_t dot_cols;
     int32_t splits;       // parts of the contraction

@@ -340,6 +340,7 @@ struct Epilogue {
     int64_t col;
     int batch, left;
     float bias[N];
+    static constexpr bool kImage = MODE == kGate && sizeof(T) == 2;
     // Beside a row's sums: its residual (forward) or the argument of its activation
     // (gate), and the weight of its slot.
     struct Row {
@@ -375,8 +376,8 @@ struct Epilogue {
         for (int e = 0; e < N; ++e) out.v[e] = (T)v[e];
         out.write(static_cast<T *>(to) + at, left);
     }
-    // gate: returns the sum of the products with the activation.
-    __device__ float write(int64_t row, const Row &r, float (&v)[N]) const {
+    // gate: returns the sum of the products with the activation; image: a.image's.
+    __device__ float write(int64_t row, const Row &r, const Piece<T, N> &image, float (&v)[N]) const {
         const int64_t at = ((MODE == kWeight ? batch * a.m : 0) + row) * a.n + col;
         float dot = 0.f;
         if (MODE == kForward) {
@@ -400,6 +401,19 @@ struct Epilogue {
 #pragma unroll
             for (int e = 0; e < N; ++e) h[e] = (float)r.piece.v[e];
             slopes_all(h, slope, a.activation);
+            if (kImage && a.image) {
+                // image / gate is the same activation, rounded by itself (unless it was
+                // too small or too large for its type): the mean of the two is off by less
+                const float by = __builtin_amdgcn_rcpf(r.gate);
+                constexpr float least = std::is_same<T, __bf16>::value ? 0x1p-126f : 0x1p-14f;
+                constexpr float most = std::is_same<T, __bf16>::value ? 0x1p127f : 65504.f;
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float u = (float)image.v[e];
+                    const bool fine = fabsf(u) >= least && fabsf(u) <= most;
+                    h[e] = fine ? 0.5f * (h[e] + u * by) : h[e];
+                }
+            }
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 dot = e < left ? fmaf(v[e], h[e], dot) : dot;
@@ -622,6 +636,15 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
             // what lies beside the next rows is read while these are worked on
             Row next[kGroup];
             beside(16 * x0 + (p + kGroup) * kPass, next);
+            Piece<T, N> image[kGroup];
+            if (Epilogue<T, MODE, N>::kImage && a.image && col < a.n) {
+#pragma unroll
+                for (int q = 0; q < kGroup; ++q) {
+                    const int64_t row = row0 + wm + 16 * x0 + (p + q) * kPass + lane / kLanes;
+                    if (row < row_end)
+                        image[q].read(static_cast<const T *>(a.image) + row * a.n + col, end.left);
+                }
+            }
 #pragma unroll
             for (int q = 0; q < kGroup; ++q) {
                 const int r = (p + q) * kPass + lane / kLanes;
@@ -644,7 +667,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
                     for (int e = 0; e < N / 4; ++e)
                         to[e] = f4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
                 } else if (there) {
-                    dot = end.write(row, extra[q], v);
+                    dot = end.write(row, extra[q], image[q], v);
                 }
                 if (MODE == kGate) {   // the lanes of a row together
 #pragma unroll
@@ -690,7 +713,7 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a, int64_t ld) {
             const Epilogue<T, MODE, 4> end(a, col, batch);
             typename Epilogue<T, MODE, 4>::Row extra;
             end.read(a, row, col, extra);
-            end.write(row, extra, u);
+            end.write(row, extra, {}, u);
         }
     }
 }
@@ -770,7 +793,7 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(ProductArgs a, int by_
             const Epilogue<T, kForward, 4> end(a, col, batch);
             typename Epilogue<T, kForward, 4>::Row extra;
             end.read(a, row, col, extra);
-            end.write(row, extra, u);
+            end.write(row, extra, {}, u);
         }
     }
 }
