@@ -68,6 +68,37 @@ __device__ inline float activate(float z, int32_t kind, float *slope = nullptr) 
     }
 }
 
+// N neighbouring values of a row to and from memory, `left` of them there.  Rows
+// begin at any element: the hardware takes 16 bytes at any address.
+template <typename T, int N>
+struct Piece {
+    typedef T Vec __attribute__((ext_vector_type(N)));
+    Vec v;
+    __device__ void read(const T *p, int left) {
+        if (left >= N) {
+            __builtin_memcpy(&v, __builtin_assume_aligned(p, sizeof(T)), sizeof(Vec));
+        } else if (left > 0) {   // without branches, so that the reads are under way together
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const T u = p[e < left ? e : 0];
+                v[e] = e < left ? u : (T)0.f;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = (T)0.f;
+        }
+    }
+    __device__ void write(T *p, int left) const {
+        if (left >= N) {
+            __builtin_memcpy(__builtin_assume_aligned(p, sizeof(T)), &v, sizeof(Vec));
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (e < left) p[e] = v[e];
+        }
+    }
+};
+
 // Division of whole numbers below 2^31 by one that is not known when compiling: a
 // product with a rounded-up reciprocal and a shift.
 struct Divider {

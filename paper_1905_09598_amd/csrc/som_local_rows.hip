@@ -106,8 +106,10 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(SumsArgs a) {
     if (LISTED && a.dots && left > 0)
         read_some<T, N>(static_cast<const T *>(a.bias) + e * a.cols + col, left, bias);
     constexpr int kAhead = 4;   // rows whose reads are under way together
+    const int some = (int)(left < N ? left : N);
     for (int64_t r0 = first + lane; r0 < end; r0 += kAhead * kSumLanes) {
-        float v[kAhead][N], gate[kAhead];
+        Piece<T, N> v[kAhead];   // turned into floats when all of them are under way
+        float gate[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int64_t r = r0 + u * kSumLanes;
@@ -118,18 +120,17 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(SumsArgs a) {
                 if (a.gates) gate[u] = a.gates[slot];
                 row = a.per.quotient(slot);
             }
-            read_some<T, N>(static_cast<const T *>(a.src) + row * a.ld + col,
-                            r < end ? left : 0, v[u]);
+            v[u].read(static_cast<const T *>(a.src) + row * a.ld + col, r < end ? some : 0);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
 #pragma unroll
             for (int c = 0; c < N; ++c)
-                sum[c] = LISTED ? fmaf(gate[u], v[u][c], sum[c]) : sum[c] + v[u][c];
+                sum[c] = LISTED ? fmaf(gate[u], (float)v[u].v[c], sum[c]) : sum[c] + (float)v[u].v[c];
             if (LISTED && a.dots) {   // the 32 lanes of a row together
                 float dot = 0.f;
 #pragma unroll
-                for (int c = 0; c < N; ++c) dot = fmaf(v[u][c], bias[c], dot);
+                for (int c = 0; c < N; ++c) dot = fmaf((float)v[u].v[c], bias[c], dot);
 #pragma unroll
                 for (int o = 1; o < kSumPieces; o <<= 1) dot += __shfl_xor(dot, o);
                 const int64_t r = r0 + u * kSumLanes;

@@ -265,31 +265,6 @@ __device__ inline void band_tile(int64_t t, int64_t tm, int64_t tn, int64_t *m, 
     *n = in / high;
 }
 
-// N neighbouring values of a row to and from memory, `left` of them there.  Rows
-// begin at any element: the hardware takes 16 bytes at any address.
-template <typename T, int N>
-struct Piece {
-    typedef T Vec __attribute__((ext_vector_type(N)));
-    Vec v;
-    __device__ void read(const T *p, int left) {
-        if (left >= N) {
-            __builtin_memcpy(&v, __builtin_assume_aligned(p, sizeof(T)), sizeof(Vec));
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e) v[e] = e < left ? p[e] : (T)0.f;
-        }
-    }
-    __device__ void write(T *p, int left) const {
-        if (left >= N) {
-            __builtin_memcpy(__builtin_assume_aligned(p, sizeof(T)), &v, sizeof(Vec));
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (e < left) p[e] = v[e];
-        }
-    }
-};
-
 // The activation of N values.
 template <int N>
 __device__ inline void activate_all(float (&v)[N], int32_t kind) {
