@@ -100,6 +100,18 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(SumsArgs a) {
         if (first >= end) return;
     }
     const int64_t col = ((int64_t)blockIdx.y * kSumPieces + piece) * N, left = a.cols - col;
+    // the list's rows and weights, so that the reads of the rows wait for LDS alone
+    __shared__ int row_of[LISTED && !DIRECT ? kSumRows : 1];
+    __shared__ float gate_of[LISTED && !DIRECT ? kSumRows : 1];
+    if (LISTED && !DIRECT) {
+        const int64_t r = first + threadIdx.x;
+        if (threadIdx.x < kSumRows && r < end) {
+            const int slot = a.list[r];
+            row_of[threadIdx.x] = a.per.quotient(slot);
+            gate_of[threadIdx.x] = a.gates ? a.gates[slot] : 1.f;
+        }
+        __syncthreads();
+    }
     float sum[N], bias[N];
 #pragma unroll
     for (int c = 0; c < N; ++c) sum[c] = bias[c] = 0.f;
@@ -115,7 +127,11 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(SumsArgs a) {
             const int64_t r = r0 + u * kSumLanes;
             int64_t row = r;
             gate[u] = 1.f;
-            if (LISTED && r < end) {
+            if (LISTED && !DIRECT && r < end) {
+                row = row_of[r - first];
+                gate[u] = gate_of[r - first];
+            }
+            if (LISTED && DIRECT && r < end) {
                 const int slot = a.list[r];
                 if (a.gates) gate[u] = a.gates[slot];
                 row = a.per.quotient(slot);
