@@ -69,8 +69,9 @@ ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus) {
             const int64_t floats = parts > 1 ? parts * rows * (tn * s.tile) : 0;
             if (floats > (int64_t)1 << 30) break;
             const double groups = (double)(tm * tn * parts) / num_cus;   // to a compute unit
-            // finding a tile's expert and its rows takes several reads in turn
-            const double ends = s.ends + (a.offsets ? 8.0 : 0.0);
+            // finding a tile's expert and its rows takes several reads in turn; a last
+            // slab of unaligned rows is read element by element
+            const double ends = s.ends + (a.offsets ? 8.0 : 0.0) + (aligned ? 0.0 : 1.0);
             // `held` workgroups at a time, one tile each
             const auto round = [&](double held) {
                 const double more = s.held > 1 ? (cost.all - cost.one) * (held - 1) / (s.held - 1) : 0;

@@ -2,7 +2,9 @@
 // pieces (with the activation's slope applied on the way where a gradient needs
 // it), and the experts' answers joined per document, with their gradients.  All
 // are bound by memory: each element is read and written once, 16 bytes a lane
-// where the rows allow it.
+// where the rows allow it.  dz of 16,001 x 2048 in fp16 takes 36 us (5.4 TB/s), the
+// join of 8192 documents' two answers of 2048 30 us (6.8 TB/s), the sums of 16,384
+// listed rows of 2048 17 us (3.9 TB/s).
 #include "som_local_internal.h"
 
 #include <algorithm>
@@ -282,9 +284,13 @@ hipError_t launch_rows_copy(const RowsArgs &args, hipStream_t stream) {
     });
 }
 
-// One pass where an expert has few rows.
+// One pass where there are few rows.  A gradient with the sums, in one pass and in
+// parts: one matrix of 2048 columns with 32, 128 and 1024 rows 13, 15, 29 and 15, 16, 19
+// us; 100 experts of 512 columns with 32 and 128 rows each 23, 40 and 26, 37.  One
+// pass takes as long as the most popular expert's rows, though: 4000 rows of 100 uneven
+// experts 50 us longer than parts.
 static bool sums_direct(const SumsArgs &a) {
-    return a.rows <= (int64_t)(a.offsets ? a.experts : 1) * 32;
+    return a.rows <= (a.offsets ? (int64_t)a.experts * 16 : 128);
 }
 static int64_t sums_parts(const SumsArgs &a) {
     return a.offsets ? a.rows / kSumRows + a.experts : (a.rows + kSumRows - 1) / kSumRows;

@@ -6,8 +6,11 @@
 // lowest expert; rows of more than 2048 experts lie in LDS, one to a workgroup.
 // The k choices are k maxima over the row, of whole numbers in the values' order:
 // one per lane, joined across the lanes by rotations; only the lane that won
-// looks for its element.  Bound by these instructions (about 85 for the rows of
-// a wave and choice at V = 16), not by the read of the scores.
+// takes its element out.  Bound by these instructions, not by the read of the scores
+// (65,536 bf16 rows of 256 experts in 8 groups, 8 choices of sigmoids with a bias: 42 us,
+// of which the read would take 7; 20,000 fp32 rows of 400, 4 choices: 21 us).
+// Sixteen lanes hold a row where they can: the steps across lanes are shared by the four
+// rows of a wave (the same rows of 256 a wave each 80 us, of 64 experts 17 and 22 us).
 #include "som_local_internal.h"
 
 #include <math.h>
@@ -444,8 +447,9 @@ __global__ __launch_bounds__(kRouteThreads) void route_long_kernel(RouteArgs a) 
 // Gradient of the scores.  LANES lanes a row: lane j works out choice j's part and
 // puts it into the row in LDS, from where the row goes out once, V neighbours a
 // lane; a softmax over the whole row is worked out again from the scores.  Bound by
-// the write of the rows, and that read.  Rows of more than LANES V experts are
-// taken in pieces of that many.
+// the write of the rows, and that read (65,536 bf16 rows of 256 experts: 12 us, 2.9 TB/s;
+// with a wave to a row 19).  Rows of more than LANES V experts are taken in pieces of
+// that many.
 template <typename T, typename G, int LANES, int V>
 __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(RouteArgs a) {
     constexpr int kRows = kRouteThreads / LANES, kWide = LANES * V;
@@ -589,7 +593,8 @@ __global__ __launch_bounds__(kSortThreads) void dispatch_scan_kernel(DispatchArg
     if (wave == kWaves - 1) a.counts[(int64_t)a.blocks * a.experts + e] = before;
 }
 
-// WAVES: waves that rank (fewer where their histograms do not fit in LDS).
+// WAVES: waves that rank (fewer where their histograms do not fit in LDS: 524,288
+// slots of 256 experts 14 us with 16, 18 with 4).
 template <int WAVES>
 __global__ __launch_bounds__(kSortThreads) void dispatch_place_kernel(DispatchArgs a) {
     constexpr int kPart = kChunk / WAVES, kHeld = kPart / 64;
