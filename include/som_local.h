@@ -49,7 +49,14 @@ typedef enum som_activation {
  * Gradients (som_linear_backward), from dy, with dz = dy act'(z):
  *     dx = dz w    dw = dz^T x    dbias = sum of dz's rows
  * The residual's gradient is dy itself.  With an activation, dz is held in the
- * element type for the two products, as the matrix instructions take it. */
+ * element type for the two products, as the matrix instructions take it.
+ *
+ * relu's slope is that of the fp32 sum's sign (z as written for it keeps a sum
+ * that is positive above 0 where the type would round it to 0).  A sum of K products
+ * is off by up to about K 2^-24 of their magnitudes: where z in exact arithmetic
+ * is nearer to 0 than that, its slope can be 1 or 0, and such an element's whole part
+ * of the gradients is there or not (of sums of 2000 products about one sign in 16
+ * million is unlike the exact one).  som_experts' first layer is no different. */
 typedef struct som_linear_call {
     int32_t type;              /* som_type of all matrices                           */
     int32_t activation;        /* som_activation                                     */

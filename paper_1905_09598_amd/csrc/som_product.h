@@ -351,6 +351,16 @@ struct Epilogue {
         for (int e = 0; e < N; ++e) out.v[e] = (T)v[e];
         out.write(static_cast<T *>(to) + at, left);
     }
+    // z as a gradient takes it: relu's slope goes by its sign, so that what is positive
+    // stays positive where the type would round it to 0.
+    __device__ void keep(int64_t at, const float (&v)[N]) const {
+        if (a.activation != kActRelu) return store(a.z, at, v);
+        constexpr float least = std::is_same<T, _Float16>::value ? 0x1p-24f : 0x1p-133f;
+        float u[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) u[e] = v[e] > 0.f && sizeof(T) == 2 ? fmaxf(v[e], least) : v[e];
+        store(a.z, at, u);
+    }
     // gate: returns the sum of the products with the activation; image: a.image's.
     __device__ float write(int64_t row, const Row &r, const Piece<T, N> &image, float (&v)[N]) const {
         const int64_t at = ((MODE == kWeight ? batch * a.m : 0) + row) * a.n + col;
@@ -358,7 +368,7 @@ struct Epilogue {
         if (MODE == kForward) {
 #pragma unroll
             for (int e = 0; e < N; ++e) v[e] += bias[e];
-            if (a.z) store(a.z, at, v);
+            if (a.z) keep(at, v);
             activate_all(v, a.activation);
             if (a.scaled) {
                 float u[N];
