@@ -388,14 +388,17 @@ struct Epilogue {
             slopes_all(h, slope, a.activation);
             if (kImage && a.image) {
                 // image / gate is the same activation, rounded by itself (unless it was
-                // too small or too large for its type): the mean of the two is off by less
+                // too small or too large for its type): the mean of the two is off by less.
+                // Gates whose reciprocal is no normal number (a softmax has weights down to
+                // 0) take no part.
                 const float by = __builtin_amdgcn_rcpf(r.gate);
+                const bool usable = fabsf(r.gate) >= 0x1p-126f && fabsf(r.gate) <= 0x1p126f;
                 constexpr float least = std::is_same<T, __bf16>::value ? 0x1p-126f : 0x1p-14f;
                 constexpr float most = std::is_same<T, __bf16>::value ? 0x1p127f : 65504.f;
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     const float u = (float)image.v[e];
-                    const bool fine = fabsf(u) >= least && fabsf(u) <= most;
+                    const bool fine = usable && fabsf(u) >= least && fabsf(u) <= most;
                     h[e] = fine ? 0.5f * (h[e] + u * by) : h[e];
                 }
             }

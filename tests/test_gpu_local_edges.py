@@ -39,3 +39,34 @@ def test_relu_passes_the_gradient_of_a_z_that_rounds_to_zero(n):
     y, kept = local.experts(x, r, w1, None, w2, None, "relu", keep=True)
     g = local.experts_backward(torch.ones_like(y), x, r, w1, None, w2, None, kept, "relu")
     assert (g.x[:, 1] == 4 * 8).all()
+
+
+@pytest.mark.parametrize("n", [2, 90])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_gradient_of_weights_next_to_zero(dtype, n):
+    # weights whose reciprocal is beyond fp32, or denormal, beside ordinary ones, and
+    # activations large enough that weight times activation is a normal number
+    small = [2.5e-39, 1e-39, 1e-40, 1e-45, 0.0, 2.0 ** -126, 2e-38, 1e-30, 0.25, 1e38, 3.4e38]
+    index = torch.arange(n * 3, dtype=torch.int32, device="cuda").view(n, 3) % 4
+    weight = torch.tensor([small[s % len(small)] for s in range(n * 3)]).view(n, 3).cuda()
+    x = torch.ones(n, 64, dtype=dtype, device="cuda")
+    w1 = (1 + _draw(1, 4, 40, 64).abs()).to(dtype)          # z of 64 to some 200
+    w2, b2 = _draw(2, 4, 24, 40, dtype=dtype, scale=0.1), _draw(3, 4, 24, dtype=dtype)
+    dy = _draw(4, n, 24, dtype=dtype)
+    say("weights next to 0", dtype, n)
+    ordinary = local.dispatch(index, torch.full_like(weight, 0.5), 4)
+    r = local.dispatch(index, weight, 4)
+    grads = []
+    for route in (r, ordinary):
+        kept = local.experts(x, route, w1, None, w2, b2, "gelu", keep=True)[1]
+        grads.append(local.experts_backward(dy, x, route, w1, None, w2, b2, kept, "gelu").weight)
+    # <dy, answer> does not depend on the weights but by roundings: h to the element type
+    # (and an image of it), the result
+    e = index.cpu().long()
+    h = O.d(x)[:, None, None, :] @ O.d(w1)[e].transpose(2, 3)     # gelu(z) is z here
+    a = (O.d(w2)[e] @ h.transpose(2, 3)).squeeze(3) + O.d(b2)[e]
+    want = (O.d(dy)[:, None, :] * a).sum(2)
+    size = (O.d(dy).abs()[:, None, None, :] @ O.d(w2)[e].abs() @ h.transpose(2, 3)).view(n, 3)
+    bound = (2 * O.U[dtype] + 200 * O.V) * size + O.stored(want, dtype)
+    for got in grads:
+        O.close(got, (want, bound), "dweight")
