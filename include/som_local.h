@@ -101,16 +101,18 @@ som_status som_linear_backward(const som_linear_call *call);
  * nothing, unless its weight is NaN: then the document's y is NaN.
  *
  * For a gradient, forward has to keep z and scaled = g h (both n k x hidden,
- * rows in the experts' order; without w2 nothing is kept).  From dy,
+ * rows in the experts' order; without w2 nothing is kept).  In fp16, which does not
+ * hold small products, scaled is that of g / 2^e with |g| / 2^e in [1/2, 1) where
+ * |g| < 1/2, and the gradient takes 2^e dy.  From dy,
  *     dweight = <dy_i, answer>  (of the element type; 0 for absent slots)
  *     dz = g (w2_e^T dy_i) act'(z)
  *     dw2_e = sum of dy_i scaled^T,  db2_e = sum of g dy_i
  *     dw1_e = sum of dz x_i^T,  db1_e = sum of dz,  dx_i = sum over j of w1_e^T dz
  * An expert without documents gets zeros.  The residual's gradient is dy.
  * Rounded to the element type on the way: h (scaled apart, from the same sums), z
- * where the slope is taken of it, dz; answers and each slot's part of dx are joined
+ * where the slope is taken of it, dz, without w2 g dy_i for dw1; answers and each slot's part of dx are joined
  * in fp32.  dweight is formed as <w2_e^T dy_i, h> + <dy_i, b2_e> with h, in 16-bit
- * types, the mean of act(z) and scaled / g. */
+ * types, the mean of act(z) and scaled / g (its part of g). */
 typedef struct som_experts_call {
     int32_t type;              /* som_type of all matrices                           */
     int32_t activation;        /* som_activation                                     */

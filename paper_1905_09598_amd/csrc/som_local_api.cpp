@@ -396,7 +396,10 @@ struct ExpertsForward {
 // Their gradients.  The last layer (w2, or w1 alone) takes its gradient from the
 // documents' rows of dy, found by slot, and the weights come in after the sums:
 //     C = w^T dy,  dweight = <C, u> + <dy, bias>  with u the layer's input,
-//     the input's gradient g C (times the slope), dw = dy (g u)^T.
+//     the input's gradient g C (times the slope), dw = dy (g u)^T,
+// with g u as forward kept it; in fp16 the power of two of a small weight is with dy, and
+// local linear maps, which keep nothing, take all of g with dy: both in a copy of dy's
+// rows by slot.
 struct ExpertsBackward {
     SideRows dy_gate, dy_weight, w_last, scaled, dz_input, dz_weight, w1, x;
     Product gate, last_weight, input, first_weight;
@@ -449,17 +452,20 @@ struct ExpertsBackward {
             a.type = c.type;
             a.m = c.outer, a.n = width, a.k = slots;
             a.offsets = c.offsets, a.experts = c.experts, a.per = per;
-            a.list_of_a = 1;
             a.y = dw_last;
             dy_weight = side(c.dy, c.n, c.outer, c.lddy);
-            by_slot(dy_weight, &a.list, c.order, c.k, slots);
             scaled = side(two ? c.scaled : c.x, two ? slots : c.n, width, two ? width : c.ldx);
-            if (!two) {   // g x, by slot
-                scaled.rows = slots;
-                scaled.make_copy(work, c.type);
-                scaled.copy.list = c.order;
-                scaled.copy.per = per;
-                scaled.copy.gates = c.weight;
+            if (!two || (c.type == SOM_F16 && c.weight)) {
+                dy_weight.rows = slots;
+                dy_weight.make_copy(work, c.type);
+                dy_weight.copy.list = c.order;
+                dy_weight.copy.per = per;
+                dy_weight.copy.gates = c.weight;
+                dy_weight.copy.exponents = two;
+                if (!two) by_slot(scaled, &a.list, c.order, c.k, slots);
+            } else {
+                a.list_of_a = 1;
+                by_slot(dy_weight, &a.list, c.order, c.k, slots);
             }
             last_weight.place(work, dy_weight, scaled);
         }

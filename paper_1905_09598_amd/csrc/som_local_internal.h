@@ -140,9 +140,20 @@ __device__ inline int expert_of(const int32_t *offsets, int experts, int tile, i
 constexpr int64_t kMaxWidth = 4000000;
 inline bool tile_reaches(int64_t ld, int size) { return ld * size * 256 < ((int64_t)1 << 32); }
 
+// A weight is gate_kept * 2^gate_exponent.  fp16 holds no product of an activation and a
+// small weight: what is kept beside the activation is then the weight without its
+// power of two (magnitudes of 1/2 to 1; larger weights whole), and the power goes to the
+// other factor of the product, a gradient, which a loss scale keeps within the type.
+__device__ inline float gate_kept(float g) {
+    return fabsf(g) < 0.5f ? __builtin_amdgcn_frexp_mantf(g) : g;
+}
+__device__ inline int gate_exponent(float g) {
+    return fabsf(g) < 0.5f ? __builtin_amdgcn_frexp_expf(g) : 0;
+}
+
 // C = A B^T, C of m rows and n columns, contraction k (som_product.h).
 //   forward  A = x (m x k), B = w (n x k):      z = C + bias, y = act(z) + residual,
-//                                               scaled = gate act(z)
+//                                               scaled = gate act(z) (fp16: gate_kept act(z))
 //   input    A = dz (m x k), B = w (k x n):     y = C
 //   gate     A = dout (m x k), B = w (k x n):   y = gate C act'(argument),
 //                                               dots: parts of <C, act(argument)>
@@ -167,7 +178,7 @@ struct ProductArgs {
     const void *argument;             // gate: rows of n, ld_argument apart
     int64_t ld_argument;
     int32_t argument_listed;          // row r's is the document's, slots[r] / per
-    const void *image;                // rows of n: gate act(argument), rounded; or null
+    const void *image;                // rows of n: forward's scaled, of act(argument); or null
     float *dots;                      // gate: m x dot_cols
     int32_t dot_cols;
     int32_t splits;       // parts of the contraction
@@ -203,7 +214,7 @@ __device__ inline int expert_of_rank(const int32_t *offsets, int experts, int ra
 // Copies `rows` rows of `cols` elements, `lds` apart, to rows of ldd >= cols
 // elements filled up with zeros; with z (rows ldz apart), times act'(z); with a
 // list, row r is src's row list[r] / per, or zeros where list[r] is negative, times
-// gates[list[r]] if there are any.
+// gates[list[r]], or their powers of two alone (gate_exponent), if there are any.
 struct RowsArgs {
     int32_t type, activation;
     const void *src, *z;
@@ -212,6 +223,7 @@ struct RowsArgs {
     const int32_t *list;
     Divider per;
     const float *gates;     // times gates[list[r]]
+    int32_t exponents;      // the gates' powers of two alone
     Divider pieces;         // of a row of dst
 };
 hipError_t launch_rows_copy(const RowsArgs &a, hipStream_t stream);

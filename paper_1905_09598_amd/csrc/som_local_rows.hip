@@ -64,7 +64,7 @@ __global__ __launch_bounds__(kThreads) void rows_copy_kernel(RowsArgs a) {
     if (a.gates) {
         const float g = from < 0 ? 0.f : a.gates[from];
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] *= g;
+        for (int e = 0; e < N; ++e) v[e] = a.exponents ? ldexpf(v[e], gate_exponent(g)) : v[e] * g;
     }
     if (a.z) {
         read_some<T, N>(static_cast<const T *>(a.z) + row * a.ldz + col, a.cols - col, z);

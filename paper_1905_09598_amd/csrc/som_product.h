@@ -330,12 +330,16 @@ struct Epilogue {
 #pragma unroll
         for (int e = 0; e < N; ++e) bias[e] = there ? (float)p.v[e] : 0.f;
     }
+    // The part of a weight that an activation is kept with.
+    __device__ static float kept_part(float gate) {
+        return std::is_same<T, _Float16>::value ? gate_kept(gate) : gate;
+    }
     __device__ static void read(const ProductArgs &a, int64_t row, int64_t col, Row &r) {
         const int left = (int)(a.n - col < N ? a.n - col : N);
         if (MODE == kForward) {
             if (a.residual)
                 r.piece.read(static_cast<const T *>(a.residual) + row * a.ldr + col, left);
-            if (a.scaled) r.gate = a.gates ? a.gates[a.slots[row]] : 1.f;
+            if (a.scaled) r.gate = kept_part(a.gates ? a.gates[a.slots[row]] : 1.f);
         }
         if (MODE == kGate) {
             const int slot = a.slots[row];
@@ -391,8 +395,8 @@ struct Epilogue {
                 // too small or too large for its type): the mean of the two is off by less.
                 // Gates whose reciprocal is no normal number (a softmax has weights down to
                 // 0) take no part.
-                const float by = __builtin_amdgcn_rcpf(r.gate);
-                const bool usable = fabsf(r.gate) >= 0x1p-126f && fabsf(r.gate) <= 0x1p126f;
+                const float gate = kept_part(r.gate), by = __builtin_amdgcn_rcpf(gate);
+                const bool usable = fabsf(gate) >= 0x1p-126f && fabsf(gate) <= 0x1p126f;
                 constexpr float least = std::is_same<T, __bf16>::value ? 0x1p-126f : 0x1p-14f;
                 constexpr float most = std::is_same<T, __bf16>::value ? 0x1p127f : 65504.f;
 #pragma unroll

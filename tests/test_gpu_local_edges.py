@@ -70,3 +70,41 @@ def test_gradient_of_weights_next_to_zero(dtype, n):
     bound = (2 * O.U[dtype] + 200 * O.V) * size + O.stored(want, dtype)
     for got in grads:
         O.close(got, (want, bound), "dweight")
+
+
+@pytest.mark.parametrize("hidden", [40, 37])
+@pytest.mark.parametrize("n", [6, 150])
+def test_small_weights_in_half_precision_keep_their_bits(n, hidden):
+    # weights of 1e-4 to 1e-7 and a loss scale that makes up for them: weight times
+    # activation is subnormal in fp16 (of few bits, or 0), weight times gradient is not
+    say("small weights", n, hidden)
+    half, experts, k, inner, outer = torch.float16, 3, 2, 48, 24
+    index = torch.arange(n * k, dtype=torch.int32, device="cuda").view(n, k) % experts
+    g = torch.Generator().manual_seed(1)
+    weight = 10 ** -(4 + 3 * torch.rand(n, k, generator=g)).cuda()
+    weight[0, 0] *= -1
+    r = local.dispatch(index, weight, experts)
+    x = _draw(2, n, inner, dtype=half)
+    w1, b1 = _draw(3, experts, hidden, inner, dtype=half, scale=inner ** -0.5), None
+    w2 = _draw(4, experts, outer, hidden, dtype=half, scale=hidden ** -0.5)
+    dy = _draw(5, n, outer, dtype=half, scale=4000.0)
+    dy1 = _draw(6, n, hidden, dtype=half, scale=4000.0)
+    kept = local.experts(x, r, w1, b1, w2, None, "gelu", keep=True)[1]
+    two = local.experts_backward(dy, x, r, w1, b1, w2, None, kept, "gelu")
+    one = local.experts_backward(dy1, x, r, w1, b1, None, None, None)
+    tiny, u = O.TINY[half], O.U[half]
+    for e in range(experts):
+        row, j = (index.cpu() == e).nonzero(as_tuple=True)
+        xe, ge = O.d(x)[row], O.d(weight)[row, j].unsqueeze(1)
+        (h, herr), _ = O.linear(xe, O.d(w1[e]), None, "gelu", None, half)
+        da = ge * O.d(dy)[row]
+        want = da.t() @ h
+        # scaled, at least half of h: two roundings of its size; dy 2^e may be subnormal
+        bound = (2 * da.abs().t() @ herr + tiny * h.abs().sum(0)
+                 + (len(row) + 8) * O.V * (da.abs().t() @ h.abs()) + O.stored(want, half))
+        O.close(two.w2[e], (want, bound), "dw2")
+        da = ge * O.d(dy1)[row]
+        want = da.t() @ xe
+        bound = ((u + (len(row) + 8) * O.V) * (da.abs().t() @ xe.abs()) + tiny * xe.abs().sum(0)
+                 + O.stored(want, half))
+        O.close(one.w1[e], (want, bound), "dw1")
