@@ -51,8 +51,9 @@ typedef enum som_activation {
  * The residual's gradient is dy itself.  With an activation, dz is held in the
  * element type for the two products, as the matrix instructions take it.
  *
- * relu's slope is that of the fp32 sum's sign (z as written for it keeps a sum
- * that is positive above 0 where the type would round it to 0).  A sum of K products
+ * Written for an activation, z keeps finite sums finite where the type would round
+ * them to infinity, and relu's positive ones above 0 where it would round them to 0.
+ * relu's slope is that of the fp32 sum's sign.  A sum of K products
  * is off by up to about K 2^-24 of their magnitudes: where z in exact arithmetic
  * is nearer to 0 than that, its slope can be 1 or 0, and such an element's whole part
  * of the gradients is there or not (of sums of 2000 products about one sign in 16

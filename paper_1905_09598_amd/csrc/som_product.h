@@ -355,14 +355,19 @@ struct Epilogue {
         for (int e = 0; e < N; ++e) out.v[e] = (T)v[e];
         out.write(static_cast<T *>(to) + at, left);
     }
-    // z as a gradient takes it: relu's slope goes by its sign, so that what is positive
-    // stays positive where the type would round it to 0.
+    // z as a gradient takes it.  A finite sum stays finite (slopes of infinities are not
+    // numbers; at the type's largest magnitude they are 0 and 1), and for relu, whose slope
+    // goes by the sign, what is positive stays positive where the type would round it to 0.
     __device__ void keep(int64_t at, const float (&v)[N]) const {
-        if (a.activation != kActRelu) return store(a.z, at, v);
-        constexpr float least = std::is_same<T, _Float16>::value ? 0x1p-24f : 0x1p-133f;
+        if (a.activation == kActNone || sizeof(T) == 4) return store(a.z, at, v);
+        constexpr bool half = std::is_same<T, _Float16>::value;
+        constexpr float most = half ? 65504.f : 0x1.fep127f, least = half ? 0x1p-24f : 0x1p-133f;
         float u[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) u[e] = v[e] > 0.f && sizeof(T) == 2 ? fmaxf(v[e], least) : v[e];
+        for (int e = 0; e < N; ++e) {
+            u[e] = fabsf(v[e]) < INFINITY ? __builtin_amdgcn_fmed3f(v[e], -most, most) : v[e];
+            if (a.activation == kActRelu && v[e] > 0.f) u[e] = fmaxf(u[e], least);
+        }
         store(a.z, at, u);
     }
     // gate: returns the sum of the products with the activation; image: a.image's.

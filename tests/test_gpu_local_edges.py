@@ -108,3 +108,26 @@ def test_small_weights_in_half_precision_keep_their_bits(n, hidden):
         bound = ((u + (len(row) + 8) * O.V) * (da.abs().t() @ xe.abs()) + tiny * xe.abs().sum(0)
                  + O.stored(want, half))
         O.close(one.w1[e], (want, bound), "dw1")
+
+
+@pytest.mark.parametrize("n", [3, 200])
+@pytest.mark.parametrize("kind", ["relu", "gelu", "silu"])
+def test_gradient_of_a_z_beyond_half_precision(kind, n):
+    # z of -80,000 and 80,000: finite sums that fp16 rounds to infinities.  The slopes are
+    # 0 and 1, whatever the activation.
+    say("large z", kind, n)
+    half = torch.float16
+    x = torch.zeros(n, 16, dtype=half, device="cuda")
+    w = torch.zeros(8, 16, dtype=half, device="cuda")
+    x[:, 0], w[:4, 0], w[4:, 0], w[:, 1] = 400.0, 200.0, -200.0, 1.0
+    y, z = local.linear(x, w, None, kind, keep=True)
+    assert torch.isinf(y[:, :4]).all() and not y[:, 4:].any()
+    dx, dw, db = local.linear_backward(torch.ones_like(y), x, w, z, kind)
+    assert (dx[:, 1] == 4).all() and (dw[:4, 0] == 400.0 * n if n < 100 else dw[:4, 0] > 0).all()
+    assert not dw[4:].any() and db.tolist() == [n] * 4 + [0] * 4
+    # infinities of the data stay what they are
+    x[0, 0] = math.inf
+    z = local.linear(x, w, None, kind, keep=True)[1]
+    assert torch.isinf(z[0]).all() and torch.isfinite(z[1:]).all()
+    x[0, 0] = math.nan
+    assert torch.isnan(local.linear(x, w, None, kind, keep=True)[1][0]).all()
