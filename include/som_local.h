@@ -155,7 +155,8 @@ som_status som_experts_backward(const som_experts_call *call);
  *     v = s + bias (softmax)  or  p + bias (sigmoid)
  * An expert is closed to a document where s or v is -infinity or NaN.  With
  * groups > 1 the experts form `groups` equal groups of neighbours; a group's
- * value is the sum of its group_best (1 or 2) largest open v, and the
+ * value is the sum of its group_best (1 or 2) largest open v (fp32's lowest
+ * value where that is below it), and the
  * top_groups groups of the largest values stay, the others' experts are closed
  * too.  index[i][j] is the expert with the j-th largest v left (the lowest index
  * among equals), -1 where none is left.  The bias, one fp32 per expert, acts on

@@ -13,6 +13,7 @@
 // rows of a wave (the same rows of 256 a wave each 80 us, of 64 experts 17 and 22 us).
 #include "som_local_internal.h"
 
+#include <float.h>
 #include <math.h>
 
 namespace som {
@@ -130,6 +131,12 @@ __device__ inline void write_row(T *s, int e0, int experts, const float (&x)[V])
 // or the score itself.
 __device__ inline float choice_value(float s, float p, float bias) {
     return s > -INFINITY ? fmaxf(p + bias, -INFINITY) : -INFINITY;   // NaN: -infinity
+}
+
+// A group's value from its two largest; one with an open expert is open, also where
+// the sum of two lowest values passes fp32's range.
+__device__ inline float group_of(float best, float next, int count) {
+    return count == 2 && next > -INFINITY ? fmaxf(best + next, -FLT_MAX) : best;
 }
 
 // Whether a score makes its whole row invalid.
@@ -296,7 +303,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs a, Dispa
                 }
             }
         }
-        const float value = a.group_best == 2 && next > -INFINITY ? best + next : best;
+        const float value = group_of(best, next, a.group_best);
         const unsigned long long stay =
             groups_that_stay<LANES>(value, lane, shift, a.groups, a.top_groups);
         if (whole) {
@@ -400,8 +407,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_long_kernel(RouteArgs a) 
                 next = fmaxf(fmaxf(next, n), fminf(best, b));
                 best = fmaxf(best, b);
             }
-            if (lane == 0)
-                group_value[g] = a.group_best == 2 && next > -INFINITY ? best + next : best;
+            if (lane == 0) group_value[g] = group_of(best, next, a.group_best);
         }
         __syncthreads();
         const float value = lane < a.groups ? group_value[lane] : -INFINITY;

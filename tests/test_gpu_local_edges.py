@@ -131,3 +131,28 @@ def test_gradient_of_a_z_beyond_half_precision(kind, n):
     assert torch.isinf(z[0]).all() and torch.isfinite(z[1:]).all()
     x[0, 0] = math.nan
     assert torch.isnan(local.linear(x, w, None, kind, keep=True)[1][0]).all()
+
+
+@pytest.mark.parametrize("gate", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts", [12, 16, 64, 640, 4096])
+def test_groups_masked_by_the_lowest_value_stay_open(experts, gate):
+    # masks of the type's lowest value (finite): two of them add up to -infinity in fp32,
+    # which closes no expert.  Row 0: everything masked so; row 1: group 2 is not;
+    # row 2: closed (-infinity) but for two masked experts of group 1.
+    say("lowest values", experts, gate)
+    groups, per = 4, experts // 4
+    low = torch.finfo(torch.float32).min
+    s = torch.full((3, experts), low, device="cuda")
+    s[1, 2 * per:3 * per] = _draw(1, per).cuda()
+    s[2] = -math.inf
+    s[2, per], s[2, per + 1] = low, low
+    bias = None
+    if gate == "sigmoid":     # the choice's values are the bias's there: as low
+        bias, s = s[0].clone(), torch.zeros_like(s)
+        s[2] = -math.inf
+        s[2, per], s[2, per + 1] = 0.0, 0.0
+    r = local.route(s, 2, bias, gate, groups, 1, 2, renormalise=True)
+    index, weight = O.route(s.cpu(), 2, None if bias is None else bias.cpu(), gate, groups, 1, 2)
+    assert torch.equal(r.index.cpu().long(), index)
+    assert (index >= 0).all()
+    assert float((O.d(r.weight) - weight).abs().max()) < 1e-6
