@@ -435,7 +435,7 @@ struct ExpertsBackward {
             a.wide = !two;
             if (two) dz = work.take((uint64_t)slots * c.hidden * size);
             // without dx of local linear maps the products' rows are not wanted
-            if (!two && !parts) parts = work.take<float>((uint64_t)slots * c.inner * 4);
+            if (!two && !c.dx) parts = work.take<float>((uint64_t)slots * c.inner * 4);
             a.y = two ? dz : parts;
             dy_gate = side(c.dy, c.n, c.outer, c.lddy);
             by_slot(dy_gate, &a.list, c.order, c.k, slots);

@@ -163,3 +163,16 @@ def test_experts_beyond_what_a_routing_holds():
     assert status(L.som_experts_backward(C.byref(call))) == "SOM_E_UNSUPPORTED"
     call.experts = 16384
     assert status(L.som_experts_workspace(C.byref(call), 1, C.byref(need))) == "SOM_OK"
+
+
+def test_experts_workspace_counts_each_array_once():
+    # local linear maps: dx's parts and dweight alone take the same array
+    L, need = local.lib(), C.c_uint64()
+
+    def bytes_of(**wanted):
+        call = local._ExpertsCall(n=4096, k=2, experts=16, inner=2048, hidden=512, outer=512,
+                                  ldx=2048, lddy=512, **wanted)
+        assert status(L.som_experts_workspace(C.byref(call), 1, C.byref(need))) == "SOM_OK"
+        return need.value
+
+    assert bytes_of(dx=256) == bytes_of(dweight=256) == bytes_of(dx=256, dweight=256)
