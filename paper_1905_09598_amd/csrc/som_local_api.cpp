@@ -401,7 +401,7 @@ struct ExpertsForward {
 // local linear maps, which keep nothing, take all of g with dy: both in a copy of dy's
 // rows by slot.
 struct ExpertsBackward {
-    SideRows dy_gate, dy_weight, w_last, scaled, dz_input, dz_weight, w1, x;
+    SideRows dy_gate, dy_weight, w_last, scaled, dz_rows, w1, x;
     Product gate, last_weight, input, first_weight;
     som::SumsArgs last_sums{}, first_sums{};
     som::CombineArgs join{};
@@ -491,6 +491,7 @@ struct ExpertsBackward {
         dweight.dots[0] = gate.a.dots, dweight.cols[0] = gate.a.dot_cols;
         dweight.dots[1] = last_sums.dots, dweight.cols[1] = last_sums.dot_cols;
         dweight.dweight = c.dweight;
+        dz_rows = side(dz, slots, c.hidden, c.hidden);
         if (two && c.dw1) {
             ProductArgs &a = first_weight.a;
             a.mode = som::kWeight;
@@ -498,10 +499,9 @@ struct ExpertsBackward {
             a.m = c.hidden, a.n = c.inner, a.k = slots;
             a.offsets = c.offsets, a.experts = c.experts, a.per = per;
             a.y = c.dw1;
-            dz_weight = side(dz, slots, c.hidden, c.hidden);
             x = side(c.x, c.n, c.inner, c.ldx);
             by_slot(x, &a.list, c.order, c.k, slots);
-            first_weight.place(work, dz_weight, x);
+            first_weight.place(work, dz_rows, x);
         }
         if (two && c.db1) {
             som::SumsArgs &s = first_sums;
@@ -520,9 +520,8 @@ struct ExpertsBackward {
             a.offsets = c.offsets, a.experts = c.experts, a.per = per;
             a.wide = 1;
             a.y = parts;
-            dz_input = side(dz, slots, c.hidden, c.hidden);
             w1 = side(c.w1, (int64_t)c.experts * c.hidden, c.inner, c.inner);
-            input.place(work, dz_input, w1);
+            input.place(work, dz_rows, w1);
         }
         join.type = c.type, join.k = c.k;
         join.n = c.n, join.width = c.inner;
@@ -541,10 +540,10 @@ struct ExpertsBackward {
             [&] { return product(last_weight.a.y, last_weight); },
             [&] { return has_sums ? som::launch_sums(last_sums, s) : hipSuccess; },
             [&] { return dweight.dweight ? som::launch_dweight(dweight, s) : hipSuccess; },
-            [&] { return copy(dz_weight); }, [&] { return copy(x); },
+            [&] { return copy(dz_rows); }, [&] { return copy(x); },
             [&] { return product(first_weight.a.y, first_weight); },
             [&] { return first_sums.out ? som::launch_sums(first_sums, s) : hipSuccess; },
-            [&] { return copy(dz_input); }, [&] { return copy(w1); },
+            [&] { return copy(w1); },
             [&] { return product(has_input, input); },
             [&] { return join.out ? som::launch_combine(join, s) : hipSuccess; });
     }

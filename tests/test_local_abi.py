@@ -176,3 +176,20 @@ def test_experts_workspace_counts_each_array_once():
         return need.value
 
     assert bytes_of(dx=256) == bytes_of(dweight=256) == bytes_of(dx=256, dweight=256)
+
+
+def test_experts_copy_their_inner_gradient_once():
+    # rows of 2041: both products of the first layer's gradient read dz from a copy in whole
+    # pieces, and from the same one
+    L, need = local.lib(), C.c_uint64()
+
+    def bytes_of(**wanted):
+        call = local._ExpertsCall(type=2, activation=1, n=20000, k=2, experts=16, inner=2000,
+                                  hidden=2041, outer=2000, ldx=2000, lddy=2000, w2=256, **wanted)
+        assert status(L.som_experts_workspace(C.byref(call), 1, C.byref(need))) == "SOM_OK"
+        return need.value
+
+    gate = bytes_of(dweight=256)      # dz itself and what its product takes
+    copy = 40000 * 2048 * 2
+    assert bytes_of(dx=256) >= gate + copy and bytes_of(dw1=256) >= gate + copy
+    assert bytes_of(dx=256) + bytes_of(dw1=256) - bytes_of(dx=256, dw1=256) == gate + copy
