@@ -512,7 +512,9 @@ class AdamW:
     multiple of 256 elements on: ``mean`` and ``square`` (fp32, or
     float8_e4m3fn of m and of sqrt(v) with ``mean_scale`` and ``square_scale``,
     one fp32 per 256 elements), and with ``master`` the parameters in fp32.
-    ``state`` takes such arrays over (a checkpoint's, with ``step`` steps done)."""
+    ``state`` takes such arrays over (a checkpoint's, with ``step`` steps done).
+    The parameters have to stay where they are: ``step`` refuses one that has moved
+    or changed its size."""
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 0.01, bits: int = 32, master: bool = False,
@@ -563,6 +565,7 @@ class AdamW:
                                       C.byref(handle)), "som_adamw_create")
         self.handle = handle.value
         self._counts = [p.numel() for p in self.params]
+        self._places = [p.data_ptr() for p in self.params]
         self._ptrs = (C.c_void_p * len(self.params))()
         self._codes = (C.c_int32 * len(self.params))()
 
@@ -571,6 +574,9 @@ class AdamW:
         size, of any of the three types) and, if given, another learning rate."""
         if len(grads) != len(self.params):
             raise ValueError(f"{len(self.params)} gradients are wanted, got {len(grads)}")
+        if ([p.data_ptr() for p in self.params] != self._places
+                or [p.numel() for p in self.params] != self._counts):
+            raise ValueError("a parameter is no longer in the memory the optimizer was made with")
         for i, (g, count) in enumerate(zip(grads, self._counts)):
             self._codes[i] = _type(g, f"gradient {i}")
             if g.numel() != count or not g.is_contiguous():

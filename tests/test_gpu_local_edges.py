@@ -156,3 +156,25 @@ def test_groups_masked_by_the_lowest_value_stay_open(experts, gate):
     assert torch.equal(r.index.cpu().long(), index)
     assert (index >= 0).all()
     assert float((O.d(r.weight) - weight).abs().max()) < 1e-6
+
+
+def test_the_optimizer_refuses_parameters_that_have_moved():
+    # its table holds addresses: a tensor that lies elsewhere by now would not be updated,
+    # and what lies at its old place would be
+    say("moved parameters")
+    p = [_draw(1, 300), _draw(2, 50)]
+    opt = local.AdamW(p)
+    g = [_draw(3, 300), _draw(4, 50)]
+    opt.step(g)
+    old, before = p[1].data, p[1].clone()
+    p[1].data = old.clone()
+    first = p[0].clone()
+    with pytest.raises(ValueError):
+        opt.step(g)
+    assert torch.equal(p[0], first) and torch.equal(old, before) and opt.steps == 1
+    p[1].data = old                  # back in its place
+    opt.step(g)
+    assert opt.steps == 2 and not torch.equal(p[1], before)
+    p[0].data = p[0].data[:299]      # shorter
+    with pytest.raises(ValueError):
+        opt.step(g)
