@@ -565,6 +565,7 @@ class AdamW:
                                       C.byref(handle)), "som_adamw_create")
         self.handle = handle.value
         self._counts = [p.numel() for p in self.params]
+        self._device = device.index
         self._places = [p.data_ptr() for p in self.params]
         self._ptrs = (C.c_void_p * len(self.params))()
         self._codes = (C.c_int32 * len(self.params))()
@@ -574,14 +575,18 @@ class AdamW:
         size, of any of the three types) and, if given, another learning rate."""
         if len(grads) != len(self.params):
             raise ValueError(f"{len(self.params)} gradients are wanted, got {len(grads)}")
-        if ([p.data_ptr() for p in self.params] != self._places
-                or [p.numel() for p in self.params] != self._counts):
-            raise ValueError("a parameter is no longer in the memory the optimizer was made with")
         for i, (g, count) in enumerate(zip(grads, self._counts)):
-            self._codes[i] = _type(g, f"gradient {i}")
+            code = _TYPES.get(getattr(g, "dtype", None))
+            if code is None or g.get_device() != self._device:
+                _type(g, f"gradient {i}")
+                raise ValueError(f"gradient {i} must be on {self.params[0].device}")
+            self._codes[i] = code
             if g.numel() != count or not g.is_contiguous():
                 raise ValueError(f"gradient {i} must be contiguous with {count} elements")
             self._ptrs[i] = g.data_ptr() or None
+        if ([p.data_ptr() for p in self.params] != self._places
+                or [p.numel() for p in self.params] != self._counts):
+            raise ValueError("a parameter is no longer in the memory the optimizer was made with")
         _check(lib().som_adamw_step(self.handle, self._ptrs, self._codes, self.steps + 1,
                                     self.lr if lr is None else lr, *self.betas, self.eps,
                                     self.weight_decay, _stream(self.params[0])), "som_adamw_step")

@@ -193,3 +193,20 @@ def test_experts_copy_their_inner_gradient_once():
     copy = 40000 * 2048 * 2
     assert bytes_of(dx=256) >= gate + copy and bytes_of(dw1=256) >= gate + copy
     assert bytes_of(dx=256) + bytes_of(dw1=256) - bytes_of(dx=256, dw1=256) == gate + copy
+
+
+def test_the_optimizer_refuses_gradients_of_another_device():
+    import torch
+    from torch._subclasses.fake_tensor import FakeTensorMode
+
+    opt = local.AdamW.__new__(local.AdamW)     # as on the first of two GPUs
+    opt.handle, opt.params, opt._counts, opt._device = None, [torch.zeros(4)], [4], 0
+    opt._places, opt._codes, opt._ptrs = [opt.params[0].data_ptr()], [0], [0]
+    with FakeTensorMode():
+        other = torch.empty(4, device="cuda:1")
+    with pytest.raises(ValueError, match="gradient 0 must be on"):
+        opt.step([other])
+    with pytest.raises(TypeError, match="gradient 0"):
+        opt.step([torch.zeros(4)])
+    with pytest.raises(TypeError, match="gradient 0"):
+        opt.step([1.0])
