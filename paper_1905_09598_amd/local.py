@@ -8,7 +8,8 @@ current stream.  Nothing is kept between calls except by ``AdamW``, which holds
 the tensors it was made with.
 
 Tensors are fp32, bf16 or fp16, live on one GPU, and have their last dimension
-contiguous; matrices of weights are contiguous altogether.
+contiguous; matrices of weights are contiguous altogether.  The calls record no
+graph: outside ``torch.no_grad()`` they refuse tensors that require a gradient.
 
     scores = local.linear(x, w, bias)                  # the gate
     r = local.route(scores, k=2)                       # index, weight, order
@@ -138,6 +139,12 @@ def lib():
 
 
 # ---------------------------------------------------------------- arguments
+def _no_graph(t, what: str) -> None:
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{what} requires a gradient, which these calls do not record: call "
+                         "them under torch.no_grad() and form gradients by the _backward calls")
+
+
 def _type(t, what: str) -> int:
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{what} must be a torch tensor")
@@ -146,6 +153,7 @@ def _type(t, what: str) -> int:
         raise TypeError(f"{what} must be float32, bfloat16 or float16, got {t.dtype}")
     if not t.is_cuda:
         raise TypeError(f"{what} must live on the GPU")
+    _no_graph(t, what)
     return code
 
 
@@ -331,6 +339,7 @@ def dispatch(index, weight, experts: int) -> Routing:
     if weight is not None:
         if not isinstance(weight, torch.Tensor) or weight.dtype != torch.float32:
             raise TypeError("weight must be float32")
+        _no_graph(weight, "weight")
         _shaped(weight, index, (n, k), "weight")
     r, work, need = _order_of(index, weight, experts, index.device)
     _check(lib().som_dispatch(index.data_ptr(), n, k, experts, *r._pointers(), _ptr(work), need,
@@ -363,6 +372,7 @@ def route(scores, k: int, bias=None, gate: str = "softmax", groups: int = 1,
     if bias is not None:
         if not isinstance(bias, torch.Tensor) or bias.dtype != torch.float32:
             raise TypeError("bias must be float32")
+        _no_graph(bias, "bias")
         _shaped(bias, scores, (experts,), "bias")
         call.bias = bias.data_ptr()
     if k < 1:
@@ -528,7 +538,8 @@ class AdamW:
         table = (_AdamwTensor * len(self.params))()
         device = self.params[0].device
         for i, p in enumerate(self.params):
-            table[i] = _AdamwTensor(_ptr(p), p.numel(), _type(p, f"parameter {i}"))
+            with torch.no_grad():        # a module's parameters are welcome
+                table[i] = _AdamwTensor(_ptr(p), p.numel(), _type(p, f"parameter {i}"))
             if p.device != device or not p.is_contiguous():
                 raise ValueError(f"parameter {i} must be contiguous and on {device}")
         self.lr, self.betas, self.eps, self.weight_decay = lr, tuple(betas), eps, weight_decay
@@ -555,7 +566,7 @@ class AdamW:
         if state is None and self.master is not None:
             at = 0
             for p in self.params:
-                self.master[at:at + p.numel()].copy_(p.reshape(-1))
+                self.master[at:at + p.numel()].copy_(p.detach().reshape(-1))
                 at += -(-p.numel() // STATE_BLOCK) * STATE_BLOCK
         handle = C.c_void_p()
         with torch.cuda.device(device):

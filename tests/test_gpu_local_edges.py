@@ -178,3 +178,35 @@ def test_the_optimizer_refuses_parameters_that_have_moved():
     p[0].data = p[0].data[:299]      # shorter
     with pytest.raises(ValueError):
         opt.step(g)
+
+
+def test_tensors_of_a_graph_are_refused():
+    # results carry no graph: a loss on them would leave w without a gradient, silently
+    say("graphs")
+    x, w, b = _draw(1, 20, 16), _draw(2, 8, 16), _draw(3, 8)
+    y = local.linear(x, w, b)
+    r = local.route(y, 2)
+    w1, dy = _draw(4, 8, 4, 16), _draw(5, 20, 4)
+    weight = r.weight.clone()
+    calls = {
+        "x": (x, lambda: local.linear(x, w, b)), "w": (w, lambda: local.linear(x, w, b)),
+        "bias": (b, lambda: local.linear(x, w, b)), "scores": (y, lambda: local.route(y, 2)),
+        "balance": (b, lambda: local.route(y, 2, b)), "w1": (w1, lambda: local.experts(x, r, w1)),
+        "weight": (weight, lambda: local.dispatch(r.index, weight, 8)),
+        "dy": (dy, lambda: local.experts_backward(dy, x, r, w1, None, None, None, None)),
+        "dscores": (y, lambda: local.linear_backward(y, x, w)),
+        "dweight": (weight, lambda: local.route_backward(weight, y, r)),
+    }
+    for name, (t, call) in calls.items():
+        t.requires_grad_()
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+        t.requires_grad_(False)
+        call()
+    # the optimizer's parameters may belong to a module
+    p = torch.nn.Parameter(_draw(6, 30))
+    opt = local.AdamW([p], master=True)
+    opt.step([_draw(7, 30)])
+    assert not opt.master.requires_grad
