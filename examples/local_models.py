@@ -94,6 +94,7 @@ def run(n=8000, d=256, out=8, clusters=12, rows=6, cols=6, hidden=64, k=2, steps
     same = float((model._route(xs)[1].index[:, 0] == bmu).float().mean())
     say(f"the gate's first choice is the best-matching unit for {100 * same:.1f} % of the documents")
     first = last = None
+    batch = min(batch, n)
     for s in range(steps):
         at = (s * batch) % (n - batch + 1)
         loss = model.step(xs[at:at + batch], target[at:at + batch])

@@ -210,3 +210,20 @@ def test_tensors_of_a_graph_are_refused():
     opt = local.AdamW([p], master=True)
     opt.step([_draw(7, 30)])
     assert not opt.master.requires_grad
+
+
+@pytest.mark.parametrize("n", [300, 1999, 2000])
+def test_example_with_fewer_documents_than_a_batch(n):
+    from test_gpu_local_example import _example
+    say("example", n)
+    seen = []
+    module = _example()
+
+    class Counting(module.LocalModels):
+        def step(self, x, target):
+            seen.append((len(x), len(target)))
+            return super().step(x, target)
+
+    module.LocalModels = Counting
+    module.run(n=n, steps=4, say=say)
+    assert seen == [(n, n)] * 4
