@@ -86,6 +86,12 @@ typedef struct som_linear_call {
  * sizes, leading dimensions, pointer alignments and which pointers are NULL. */
 som_status som_linear_workspace(const som_linear_call *call, int32_t backward, uint64_t *bytes);
 
+/* How the call's products run, in the order y; dx, dw: the rows and columns of a
+ * workgroup's tile (256, 128 or 64; 16: the kernel of few rows), negative where its
+ * operands go through registers and not straight into LDS, 0 for a product that the
+ * call does not have.  A function of the same things as the work memory. */
+som_status som_linear_route(const som_linear_call *call, int32_t backward, int32_t tiles[2]);
+
 /* Errors of both: SOM_E_ARG (a bad type, activation or size, a missing or too
  * short array, a leading dimension below its row, a workspace that is missing,
  * misaligned or too small), SOM_E_UNSUPPORTED (inner or outer above 4,000,000;
@@ -147,6 +153,9 @@ typedef struct som_experts_call {
  * than 16384 experts, n k or experts times hidden or outer above 2^31 - 1). */
 som_status som_experts_workspace(const som_experts_call *call, int32_t backward,
                                  uint64_t *bytes);
+/* As som_linear_route, in the order w1's, w2's;  dy w2 (dy w1 without w2), its
+ * matrix's gradient, dz w1, dw1. */
+som_status som_experts_route(const som_experts_call *call, int32_t backward, int32_t tiles[4]);
 som_status som_experts(const som_experts_call *call);
 som_status som_experts_backward(const som_experts_call *call);
 

@@ -241,6 +241,11 @@ struct Product {
     }
 };
 
+// How it runs, as som_linear_route says it; 0 if it is not wanted.
+int32_t tile_of(const Product &p, bool wanted = true) {
+    return !wanted ? 0 : p.plan.waves || p.plan.aligned ? p.plan.tile : -p.plan.tile;
+}
+
 hipError_t run_copy(const SideRows &side, hipStream_t s) {
     return side.copied ? som::launch_rows_copy(side.copy, s) : hipSuccess;
 }
@@ -284,6 +289,7 @@ struct LinearForward {
         w = side(c.w, c.outer, c.inner, c.inner);
         product.place(work, x, w);
     }
+    void route(int32_t *tiles) const { tiles[0] = tile_of(product); }
     hipError_t enqueue(hipStream_t s) const {
         return in_order([&] { return run_copy(x, s); }, [&] { return run_copy(w, s); },
                         [&] { return run(product, s); });
@@ -326,6 +332,9 @@ struct LinearBackward {
             sums.out = c.dbias;
             sums.partial = work.take<float>((uint64_t)som::sums_partial(sums) * 4);
         }
+    }
+    void route(int32_t *tiles) const {
+        tiles[0] = tile_of(input, has_input), tiles[1] = tile_of(weight, has_weight);
     }
     hipError_t enqueue(hipStream_t s) const {
         const auto copy = [&](const SideRows &r) { return has_rows ? run_copy(r, s) : hipSuccess; };
@@ -383,6 +392,7 @@ struct ExpertsForward {
         join.residual = c.residual, join.ldr = c.ldr;
         join.out = c.y;
     }
+    void route(int32_t *tiles) const { tiles[0] = tile_of(first), tiles[1] = tile_of(second, two); }
     hipError_t enqueue(hipStream_t s) const {
         return in_order([&] { return run_copy(x, s); }, [&] { return run_copy(w1, s); },
                         [&] { return run(first, s); },
@@ -528,6 +538,10 @@ struct ExpertsBackward {
         join.y = parts, join.place = c.place;
         join.out = c.dx;
     }
+    void route(int32_t *tiles) const {
+        tiles[0] = tile_of(gate, has_gate), tiles[1] = tile_of(last_weight, last_weight.a.y);
+        tiles[2] = tile_of(input, has_input), tiles[3] = tile_of(first_weight, first_weight.a.y);
+    }
     hipError_t enqueue(hipStream_t s) const {
         const auto copy = [&](const SideRows &r) { return has_rows ? run_copy(r, s) : hipSuccess; };
         const auto product = [&](bool wanted, const Product &p) {
@@ -614,6 +628,15 @@ uint64_t workspace(const Call &c, bool backward) {
     return need.used;
 }
 
+template <typename Forward, typename Backward, typename Call>
+void route(const Call &c, bool backward, int32_t *tiles, int32_t count) {
+    std::fill(tiles, tiles + count, 0);
+    Carver need(nullptr);
+    if (c.n == 0) return;
+    if (backward) Backward(c, need).route(tiles);
+    else Forward(c, need).route(tiles);
+}
+
 }  // namespace
 
 extern "C" {
@@ -622,6 +645,13 @@ som_status som_linear_workspace(const som_linear_call *c, int32_t backward, uint
     if (!bytes) return SOM_E_ARG;
     const som_status st = linear_sizes_ok(c);
     if (st == SOM_OK) *bytes = c->n ? workspace<LinearForward, LinearBackward>(*c, backward) : 0;
+    return st;
+}
+
+som_status som_linear_route(const som_linear_call *c, int32_t backward, int32_t tiles[2]) {
+    if (!tiles) return SOM_E_ARG;
+    const som_status st = linear_sizes_ok(c);
+    if (st == SOM_OK) route<LinearForward, LinearBackward>(*c, backward, tiles, 2);
     return st;
 }
 
@@ -658,6 +688,13 @@ som_status som_experts_workspace(const som_experts_call *c, int32_t backward, ui
     if (!bytes) return SOM_E_ARG;
     const som_status st = experts_sizes_ok(c);
     if (st == SOM_OK) *bytes = c->n ? workspace<ExpertsForward, ExpertsBackward>(*c, backward) : 0;
+    return st;
+}
+
+som_status som_experts_route(const som_experts_call *c, int32_t backward, int32_t tiles[4]) {
+    if (!tiles) return SOM_E_ARG;
+    const som_status st = experts_sizes_ok(c);
+    if (st == SOM_OK) route<ExpertsForward, ExpertsBackward>(*c, backward, tiles, 4);
     return st;
 }
 

@@ -44,8 +44,9 @@ STATE_BLOCK = 256
 
 # Every symbol include/som_local.h declares.
 EXPORTED = (
-    "som_linear_workspace", "som_linear", "som_linear_backward", "som_experts_workspace",
-    "som_experts", "som_experts_backward", "som_route", "som_route_backward",
+    "som_linear_workspace", "som_linear_route", "som_linear", "som_linear_backward",
+    "som_experts_workspace", "som_experts_route", "som_experts", "som_experts_backward",
+    "som_route", "som_route_backward",
     "som_dispatch_workspace", "som_dispatch", "som_adamw_room", "som_adamw_create",
     "som_adamw_destroy", "som_adamw_step",
 )
@@ -114,9 +115,11 @@ def lib():
     vp, i32, i64, u64, f64 = C.c_void_p, C.c_int32, C.c_int64, C.c_uint64, C.c_double
     sig = {
         "som_linear_workspace": [C.POINTER(_LinearCall), i32, C.POINTER(u64)],
+        "som_linear_route": [C.POINTER(_LinearCall), i32, C.POINTER(i32)],
         "som_linear": [C.POINTER(_LinearCall)],
         "som_linear_backward": [C.POINTER(_LinearCall)],
         "som_experts_workspace": [C.POINTER(_ExpertsCall), i32, C.POINTER(u64)],
+        "som_experts_route": [C.POINTER(_ExpertsCall), i32, C.POINTER(i32)],
         "som_experts": [C.POINTER(_ExpertsCall)],
         "som_experts_backward": [C.POINTER(_ExpertsCall)],
         "som_route": [C.POINTER(_RouteCall)],

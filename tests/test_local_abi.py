@@ -210,3 +210,30 @@ def test_the_optimizer_refuses_gradients_of_another_device():
         opt.step([torch.zeros(4)])
     with pytest.raises(TypeError, match="gradient 0"):
         opt.step([1.0])
+
+
+def test_how_products_run_is_told():
+    L, tiles = local.lib(), (C.c_int32 * 4)()
+    call = _linear(n=16001, inner=2048, outer=2048, ldx=2048, lddy=2048, type=1)
+    assert status(L.som_linear_route(C.byref(call), 0, tiles)) == "SOM_OK"
+    assert tiles[0] in (64, 128, 256) and tiles[1] == 0
+    assert status(L.som_linear_route(C.byref(call), 1, tiles)) == "SOM_OK"
+    assert list(tiles[:2]) == [0, 0]                    # no gradient is wanted
+    call.dw = 256
+    assert status(L.som_linear_route(C.byref(call), 1, tiles)) == "SOM_OK"
+    assert tiles[0] == 0 and tiles[1] in (64, 128, 256)
+    for n, want in ((0, 0), (3, 16)):
+        call.n = n
+        assert status(L.som_linear_route(C.byref(call), 0, tiles)) == "SOM_OK"
+        assert tiles[0] == want
+    assert status(L.som_linear_route(C.byref(call), 0, None)) == "SOM_E_ARG"
+    assert status(L.som_linear_route(None, 0, tiles)) == "SOM_E_ARG"
+    call = local._ExpertsCall(n=4000, k=2, experts=3, inner=333, hidden=777, outer=333, ldx=333,
+                              lddy=333, w2=256, dweight=256)
+    assert status(L.som_experts_route(C.byref(call), 0, tiles)) == "SOM_OK"
+    assert tiles[0] and tiles[1] and not tiles[2] and not tiles[3]
+    assert status(L.som_experts_route(C.byref(call), 1, tiles)) == "SOM_OK"
+    assert tiles[0] and not any(tiles[1:])
+    assert status(L.som_experts_route(C.byref(call), 1, None)) == "SOM_E_ARG"
+    call.k = 0
+    assert status(L.som_experts_route(C.byref(call), 1, tiles)) == "SOM_E_ARG"
