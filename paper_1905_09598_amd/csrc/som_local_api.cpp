@@ -588,6 +588,17 @@ som_status experts_sizes_ok(const som_experts_call *c) {
     return SOM_OK;
 }
 
+// The call as it will run: the routing's arrays, which it needs, may not be there yet
+// when its work memory is asked for.
+som_experts_call routed(const som_experts_call &c) {
+    static const int32_t there = 0;
+    som_experts_call r = c;
+    if (!r.offsets) r.offsets = &there;
+    if (!r.order) r.order = &there;
+    if (!r.place) r.place = &there;
+    return r;
+}
+
 bool experts_common_ok(const som_experts_call &c) {
     const int size = som::type_size(c.type);
     const int64_t slots = c.n * c.k, e = c.experts;
@@ -687,14 +698,14 @@ som_status som_linear_backward(const som_linear_call *c) {
 som_status som_experts_workspace(const som_experts_call *c, int32_t backward, uint64_t *bytes) {
     if (!bytes) return SOM_E_ARG;
     const som_status st = experts_sizes_ok(c);
-    if (st == SOM_OK) *bytes = c->n ? workspace<ExpertsForward, ExpertsBackward>(*c, backward) : 0;
+    if (st == SOM_OK) *bytes = c->n ? workspace<ExpertsForward, ExpertsBackward>(routed(*c), backward) : 0;
     return st;
 }
 
 som_status som_experts_route(const som_experts_call *c, int32_t backward, int32_t tiles[4]) {
     if (!tiles) return SOM_E_ARG;
     const som_status st = experts_sizes_ok(c);
-    if (st == SOM_OK) route<ExpertsForward, ExpertsBackward>(*c, backward, tiles, 4);
+    if (st == SOM_OK) route<ExpertsForward, ExpertsBackward>(routed(*c), backward, tiles, 4);
     return st;
 }
 

@@ -237,3 +237,23 @@ def test_how_products_run_is_told():
     assert status(L.som_experts_route(C.byref(call), 1, None)) == "SOM_E_ARG"
     call.k = 0
     assert status(L.som_experts_route(C.byref(call), 1, tiles)) == "SOM_E_ARG"
+
+
+def test_experts_workspace_before_the_routing_is_there():
+    # the routing's arrays are always needed, so that asking without them asks the same
+    L, need = local.lib(), C.c_uint64()
+    for type_ in (0, 1, 2):
+        for n, k, experts, inner, hidden in ((300, 2, 40, 64, 72), (5000, 1, 3, 501, 2001),
+                                             (20000, 2, 16, 2000, 2041), (3, 2, 8, 128, 64)):
+            call = local._ExpertsCall(type=type_, n=n, k=k, experts=experts, inner=inner,
+                                      hidden=hidden, outer=inner, ldx=inner, lddy=inner, w2=256,
+                                      b2=256, dx=256, dweight=256, dw1=256, db1=256, dw2=256,
+                                      db2=256)
+            for backward in (0, 1):
+                got = []
+                for array in (0, 256):
+                    call.offsets = call.order = call.place = array
+                    assert status(L.som_experts_workspace(C.byref(call), backward,
+                                                          C.byref(need))) == "SOM_OK"
+                    got.append(need.value)
+                assert got[0] == got[1], (type_, n, k, experts, inner, hidden, backward)
