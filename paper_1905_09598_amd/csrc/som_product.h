@@ -362,11 +362,17 @@ struct Epilogue {
         if (a.activation == kActNone || sizeof(T) == 4) return store(a.z, at, v);
         constexpr bool half = std::is_same<T, _Float16>::value;
         constexpr float most = half ? 65504.f : 0x1.fep127f, least = half ? 0x1p-24f : 0x1p-133f;
-        float u[N];
+        float u[N], top = 0.f;
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            u[e] = fabsf(v[e]) < INFINITY ? __builtin_amdgcn_fmed3f(v[e], -most, most) : v[e];
-            if (a.activation == kActRelu && v[e] > 0.f) u[e] = fmaxf(u[e], least);
+        for (int e = 0; e < N; ++e) u[e] = v[e], top = fmaxf(top, fabsf(v[e]));
+        if (top > most) {   // seldom
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                u[e] = fabsf(v[e]) < INFINITY ? __builtin_amdgcn_fmed3f(v[e], -most, most) : v[e];
+        }
+        if (a.activation == kActRelu) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) u[e] = v[e] > 0.f ? fmaxf(u[e], least) : u[e];
         }
         store(a.z, at, u);
     }
@@ -402,12 +408,13 @@ struct Epilogue {
                 // 0) take no part.
                 const float gate = kept_part(r.gate), by = __builtin_amdgcn_rcpf(gate);
                 const bool usable = fabsf(gate) >= 0x1p-126f && fabsf(gate) <= 0x1p126f;
-                constexpr float least = std::is_same<T, __bf16>::value ? 0x1p-126f : 0x1p-14f;
+                const float least =
+                    !usable ? INFINITY : std::is_same<T, __bf16>::value ? 0x1p-126f : 0x1p-14f;
                 constexpr float most = std::is_same<T, __bf16>::value ? 0x1p127f : 65504.f;
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     const float u = (float)image.v[e];
-                    const bool fine = usable && fabsf(u) >= least && fabsf(u) <= most;
+                    const bool fine = fabsf(u) >= least && fabsf(u) <= most;
                     h[e] = fine ? 0.5f * (h[e] + u * by) : h[e];
                 }
             }
