@@ -49,7 +49,7 @@ typedef enum som_activation {
  * Gradients (som_linear_backward), from dy, with dz = dy act'(z):
  *     dx = dz w    dw = dz^T x    dbias = sum of dz's rows
  * The residual's gradient is dy itself.  With an activation, dz is held in the
- * element type for the two products, as the matrix instructions take it.
+ * element type, as the matrix instructions take it, for the two products and dbias.
  *
  * Written for an activation, z keeps finite sums finite where the type would round
  * them to infinity, and relu's positive ones above 0 where it would round them to 0.

@@ -409,7 +409,7 @@ struct ExpertsForward {
 //     the input's gradient g C (times the slope), dw = dy (g u)^T,
 // with g u as forward kept it; in fp16 the power of two of a small weight is with dy, and
 // local linear maps, which keep nothing, take all of g with dy: both in a copy of dy's
-// rows by slot.
+// rows by slot (4000 rows of 2000 in fp16: 8 us, of 640 for the whole training pass).
 struct ExpertsBackward {
     SideRows dy_gate, dy_weight, w_last, scaled, dz_rows, w1, x;
     Product gate, last_weight, input, first_weight;

@@ -443,12 +443,14 @@ struct Epilogue {
 //   load the slab after the next in its place; read the next slab's first half;
 //   multiply the second half
 // so that the matrix cores always have fragments in hand, and a load has a slab's
-// time to arrive.  Bound by the matrix instructions and the reads of LDS that feed them:
-// the larger the tile, the fewer reads a product.  8192 x 2048 x 8192 in bf16 takes
-// 229 us in tiles of 256 (1200 TFLOP/s), 256 in 128s and 360 in 64s, 281 with bias,
-// gelu and a residual (one workgroup holds a compute unit, and nothing else runs
-// beside its epilogue); 16,001 x 2048 x 2048 in fp16 124, 138 and 191 us.  Small
-// tiles fill the chip where there are few (plan_product).
+// time to arrive.  8192 x 2048 x 8192 in bf16 takes 229 us in tiles of 256 (1200 TFLOP/s),
+// 256 in 128s and 360 in 64s, 282 with bias, gelu and a residual (one workgroup holds a
+// compute unit, and nothing else runs beside its epilogue); 16,001 x 2048 x 2048 in fp16
+// 124, 138 and 191 us: the larger the tile, the fewer reads a product.  The first, with
+// its epilogue, holds the matrix cores for 43 % of its cycles and LDS for 18 %, without a
+// bank conflict, at 2.05 GHz, and fetches 269 MB of the 201 it needs: bound by what the
+// slabs and the epilogue wait for.  Small tiles fill the chip where there are few
+// (plan_product).
 template <typename T, int MODE, int LIST, bool DMA, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) {
     constexpr bool kAcrossA = MODE == kWeight, kAcrossB = MODE != kForward;
@@ -731,9 +733,10 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a, int64_t ld) {
 // takes 16 columns of C, its waves take the contraction's slabs in turn, straight
 // from memory into the fragments (no LDS: w is used once, x comes from the
 // caches), four slabs in flight, and join their sums through LDS in order.
-// Measured here and in tiles (us): one row of 2048 by 10,000 in bf16 9.9 (4.1 TB/s) and
-// 13.8, sixteen rows 14.0 and 13.7, sixteen rows of 2048 by 1024 6.1 and 8.6, of 10,000
-// by 2048 18.1 and 17.7: up to sixteen rows, one fragment, go this way.
+// Measured here and in tiles (us): one row of 2048 by 10,000 in bf16 10.4 (3.9 TB/s) and
+// 13.8; sixteen rows, one fragment, 14.0 and 13.7, of 2048 by 1024 6.1 and 8.6, of 10,000
+// by 2048 18.1 and 17.7.  Up to sixteen rows go this way: at sixteen tiles take 2 % less
+// where the result is wide, or the contraction long, and 40 % more where neither is.
 template <typename T, bool CHECK>
 __device__ inline i4 piece(const T *row, int64_t k, int64_t k_end) {
     constexpr int kElems = 16 / sizeof(T);
