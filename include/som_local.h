@@ -159,6 +159,44 @@ som_status som_experts_route(const som_experts_call *call, int32_t backward, int
 som_status som_experts(const som_experts_call *call);
 som_status som_experts_backward(const som_experts_call *call);
 
+/* Layer norm of n rows,
+ *     y = (x - mean) rstd weight + bias,    rstd = 1 / sqrt(var + eps),
+ * mean and var (the mean square of x - mean) over a row.  Forward writes mean and rstd
+ * of each row to `kept`, unless it is NULL; backward reads them there.  From dy, with
+ * g = dy weight and xh = (x - mean) rstd,
+ *     dx = rstd (g - mean(g) - xh mean(g xh)) + beside
+ *     dweight = sum over rows of dy xh     dbias = sum over rows of dy
+ * `beside` is the gradient of the path that goes past the norm (a residual's).  Without
+ * rows dweight and dbias are zeros. */
+typedef struct som_norm_call {
+    int32_t type;              /* som_type of all matrices                           */
+    int32_t width;             /* 1 .. 4,000,000                                     */
+    int64_t n;                 /* rows; 0 is allowed                                 */
+    const void *x;
+    int64_t ldx;               /* elements from row to row, >= width                 */
+    const void *weight;        /* width; NULL for 1                                  */
+    const void *bias;          /* width; NULL for 0 (forward only)                   */
+    float eps;                 /* >= 0                                               */
+    void *y;                   /* packed, forward's result                           */
+    float *kept;               /* n x 2: mean, rstd                                  */
+    const void *dy;            /* backward                                           */
+    int64_t lddy;              /* >= width                                           */
+    const void *beside;        /* NULL for none                                      */
+    int64_t ldb;               /* >= width                                           */
+    void *dx;                  /* packed; each gradient NULL if not wanted           */
+    void *dweight, *dbias;
+    void *workspace;
+    uint64_t workspace_bytes;
+    void *stream;
+} som_norm_call;
+
+/* Bytes of work memory: forward none, backward the parts of dweight and dbias.  A
+ * function of type, n, width and which of the two are NULL.
+ * Errors: as som_linear. */
+som_status som_norm_workspace(const som_norm_call *call, int32_t backward, uint64_t *bytes);
+som_status som_norm(const som_norm_call *call);
+som_status som_norm_backward(const som_norm_call *call);
+
 /* Routing of n documents by their scores s (n x experts) to k experts each.
  *     p = softmax(s) over the row, or 1 / (1 + e^-s)
  *     v = s + bias (softmax)  or  p + bias (sigmoid)

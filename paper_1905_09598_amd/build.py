@@ -25,7 +25,8 @@ SOURCES = ["som_api.cpp", "som_train.hip", "som_train_pipe.hip", "som_train_pipe
            "som_eval.hip", "som_eval_half.hip", "som_util.hip", "som_pca.hip", "som_sparse.hip", "som_batch.hip",
            "som_stream.hip",
            "som_local_api.cpp", "som_local_rows.hip", "som_product_f32.hip",
-           "som_product_bf16.hip", "som_product_f16.hip", "som_route.hip", "som_adamw.hip"]
+           "som_product_bf16.hip", "som_product_f16.hip", "som_route.hip", "som_adamw.hip",
+           "som_norm.hip"]
 ARCH = "gfx950"
 
 
@@ -55,8 +56,9 @@ def common_flags() -> list:
 UNIFORM_EXIT_SOURCES = ("som_train.hip", "som_train_pipe.hip", "som_train_panel.hip")
 
 
-# The optimizer rounds every operation by itself (som_adamw.hip).
-UNCONTRACTED_SOURCES = ("som_adamw.hip",)
+# The optimizer and layer norm round every operation by itself (som_adamw.hip,
+# som_norm.hip: a mean that is a product has to be the same number wherever it is used).
+UNCONTRACTED_SOURCES = ("som_adamw.hip", "som_norm.hip")
 
 
 def unit_flags(src: str) -> list:

@@ -741,6 +741,83 @@ som_status som_experts_backward(const som_experts_call *c) {
     return enqueue<ExpertsBackward>(*c);
 }
 
+static som_status norm_ok(const som_norm_call *c) {
+    if (!c || !type_ok(c->type) || c->n < 0 || c->width < 1 || c->ldx < c->width ||
+        !(c->eps >= 0.f) || isinf(c->eps))
+        return SOM_E_ARG;
+    if (c->width > som::kMaxWidth || c->n > (int64_t)1 << 40) return SOM_E_UNSUPPORTED;
+    return SOM_OK;
+}
+
+static som::NormArgs norm_args(const som_norm_call &c) {
+    som::NormArgs a{};
+    a.type = c.type;
+    a.n = c.n, a.width = c.width;
+    a.x = c.x, a.ldx = c.ldx;
+    a.weight = c.weight, a.bias = c.bias;
+    a.eps = c.eps;
+    a.y = c.y, a.kept = c.kept;
+    a.dy = c.dy, a.lddy = c.lddy;
+    a.beside = c.beside, a.ldb = c.ldb;
+    a.dx = c.dx, a.dweight = c.dweight, a.dbias = c.dbias;
+    if (c.dweight || c.dbias) a.parts = som::norm_parts(a, compute_units());
+    return a;
+}
+
+static uint64_t norm_parts_bytes(const som::NormArgs &a) {
+    return (uint64_t)a.parts * 2 * a.width * 4;
+}
+
+static bool norm_common_ok(const som_norm_call &c) {
+    const int size = som::type_size(c.type);
+    return rows_ok(c.x, c.n, c.width, c.ldx, size) &&
+           rows_ok_or_null(c.weight, 1, c.width, c.width, size);
+}
+
+som_status som_norm_workspace(const som_norm_call *c, int32_t backward, uint64_t *bytes) {
+    if (!bytes) return SOM_E_ARG;
+    const som_status st = norm_ok(c);
+    if (st == SOM_OK) {
+        Carver need(nullptr);
+        if (backward) need.take(norm_parts_bytes(norm_args(*c)));
+        *bytes = need.used;
+    }
+    return st;
+}
+
+som_status som_norm(const som_norm_call *c) {
+    const som_status st = norm_ok(c);
+    if (st != SOM_OK) return st;
+    const int size = som::type_size(c->type);
+    if (!norm_common_ok(*c) || !rows_ok_or_null(c->bias, 1, c->width, c->width, size) ||
+        !rows_ok(c->y, c->n, c->width, c->width, size) || !rows_ok_or_null(c->kept, c->n, 2, 2, 4))
+        return SOM_E_ARG;
+    if (c->n == 0) return SOM_OK;
+    return from_hip(som::launch_norm(norm_args(*c), compute_units(),
+                                     reinterpret_cast<hipStream_t>(c->stream)));
+}
+
+som_status som_norm_backward(const som_norm_call *c) {
+    const som_status st = norm_ok(c);
+    if (st != SOM_OK) return st;
+    const int size = som::type_size(c->type);
+    if (!norm_common_ok(*c) || !rows_ok(c->kept, c->n, 2, 2, 4) ||
+        !rows_ok(c->dy, c->n, c->width, c->lddy, size) ||
+        !rows_ok_or_null(c->beside, c->n, c->width, c->ldb, size) ||
+        !rows_ok_or_null(c->dx, c->n, c->width, c->width, size) ||
+        !rows_ok_or_null(c->dweight, 1, c->width, c->width, size) ||
+        !rows_ok_or_null(c->dbias, 1, c->width, c->width, size))
+        return SOM_E_ARG;
+    Carver work(c->workspace);
+    som::NormArgs a = norm_args(*c);
+    a.partial = work.take<float>(norm_parts_bytes(a));
+    const som_status ok = work_ok(work, c->workspace, c->workspace_bytes);
+    if (ok != SOM_OK) return ok;
+    if (!a.parts && (c->n == 0 || !c->dx)) return SOM_OK;
+    return from_hip(som::launch_norm_backward(a, compute_units(),
+                                              reinterpret_cast<hipStream_t>(c->stream)));
+}
+
 static som_status route_ok(const som_route_call *c) {
     if (!c || !type_ok(c->type) || (c->gate != SOM_GATE_SOFTMAX && c->gate != SOM_GATE_SIGMOID))
         return SOM_E_ARG;

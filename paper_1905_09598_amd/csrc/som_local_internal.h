@@ -332,6 +332,26 @@ struct AdamwArgs {
 };
 hipError_t launch_adamw(const AdamwArgs &a, bool eight, hipStream_t stream);
 
+// som_norm.hip; the fields are som_norm_call's.
+struct NormArgs {
+    int32_t type;
+    int64_t n, width;
+    const void *x, *weight, *bias;
+    int64_t ldx;
+    float eps;
+    void *y;
+    float *kept;
+    const void *dy, *beside;
+    int64_t lddy, ldb;
+    void *dx, *dweight, *dbias;
+    float *partial;         // parts x 2 x width
+    int32_t parts, lanes;   // groups of rows; lanes of a row
+    float over;             // 1 / width
+};
+int32_t norm_parts(const NormArgs &a, int num_cus);   // a function of type, n and width
+hipError_t launch_norm(const NormArgs &a, int num_cus, hipStream_t stream);
+hipError_t launch_norm_backward(const NormArgs &a, int num_cus, hipStream_t stream);
+
 ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus);
 // Parts of a row's dots: columns of one wave each.
 inline int32_t plan_dot_cols(const ProductPlan &p, int64_t n) {

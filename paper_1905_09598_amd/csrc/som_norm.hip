@@ -1,0 +1,539 @@
+// Layer norm of rows and its gradient:
+//     y = (x - mean) rstd weight + bias,   rstd = 1 / sqrt(var + eps),
+//     dx = rstd (g - mean(g) - xh mean(g xh)) + beside,   g = dy weight,  xh = (x - mean) rstd,
+//     dweight = sum over rows of dy xh,   dbias = sum over rows of dy.
+// Bound by memory: forward reads x and writes y, backward reads x and dy (and beside)
+// and writes dx, once each.  A row stays in registers, 16-byte pieces of it to a lane,
+// between the statistics and what they are for; rows of up to a wave's pieces are taken
+// by 1 to 64 lanes, longer ones by a workgroup, and only rows beyond what a workgroup
+// holds are read again.  A workgroup takes rows in turn with the weight in registers;
+// backward adds up its columns' parts of dweight and dbias there, and norm_join_kernel
+// adds up the workgroups' in order (no atomics: a result does not depend on timing).
+#include "som_local_internal.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace som {
+namespace {
+
+// The sum over the lanes of a row: `lanes` neighbours (a power of two), or with WIDE
+// the whole workgroup, through LDS (`part`: kPart floats, of which calls in turn take one
+// half and the other, so that one barrier a call will do).
+constexpr int kPart = 2 * 16 * 2;
+template <bool WIDE, int VALUES>
+__device__ inline void row_sum(float (&v)[VALUES], int lanes, float *part, int &turn) {
+#pragma unroll
+    for (int i = 0; i < VALUES; ++i)
+        for (int o = 1; o < (WIDE ? 64 : lanes); o <<= 1) v[i] += __shfl_xor(v[i], o);
+    if (!WIDE) return;
+    const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6;
+    float *const mine = part + (turn ^= 1) * (kPart / 2);
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+        for (int i = 0; i < VALUES; ++i) mine[wave * VALUES + i] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < VALUES; ++i) {
+        v[i] = 0.f;
+        for (int w = 0; w < waves; ++w) v[i] += mine[w * VALUES + i];
+    }
+}
+
+// A thread's part of a row of at least N elements: P pieces of N neighbours.  A piece
+// that crosses the row's end begins earlier instead, so that every read is whole: its
+// first `skip` elements belong to the piece before it, are left out of sums, and are
+// written by both alike.  A piece that begins beyond the end has skip = N.
+template <bool WIDE, int P, int N>
+struct Part {
+    int lane, row, rows;   // its place among the row's lanes; its row of the workgroup's `rows`
+    int at[P], skip[P];
+    __device__ Part(int lanes, int width) {
+        lane = WIDE ? threadIdx.x : threadIdx.x & (lanes - 1);
+        row = WIDE ? 0 : threadIdx.x / lanes;
+        rows = WIDE ? 1 : blockDim.x / lanes;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int col = (lane + p * lanes) * N;
+            at[p] = col + N <= width ? col : width - N;
+            skip[p] = col - at[p] < N ? col - at[p] : N;
+        }
+    }
+    __device__ bool mine(int p) const { return skip[p] < N; }
+    // 0 in place of what belongs to another piece.
+    __device__ void clear(int p, float (&v)[N]) const {
+        if (skip[p] > 0) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = e < skip[p] ? 0.f : v[e];
+        }
+    }
+    template <typename T>
+    __device__ void read(const void *rows_at, int64_t first, int p, bool there, Piece<T, N> &v) const {
+        if (there && mine(p)) v.read(static_cast<const T *>(rows_at) + first + at[p], N);
+        else v.read(nullptr, 0);
+    }
+};
+
+template <typename T, int P, bool WIDE>
+__global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
+    constexpr int N = 16 / sizeof(T);
+    __shared__ float part[kPart];
+    int turn = 0;
+    const Part<WIDE, P, N> me(a.lanes, (int)a.width);
+    Piece<T, N> weight[P], bias[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        me.template read<T>(a.weight, 0, p, a.weight != nullptr, weight[p]);
+        me.template read<T>(a.bias, 0, p, a.bias != nullptr, bias[p]);
+    }
+    for (int64_t r0 = (int64_t)blockIdx.x * me.rows; r0 < a.n; r0 += (int64_t)gridDim.x * me.rows) {
+        const int64_t row = r0 + me.row;
+        const bool there = row < a.n;
+        Piece<T, N> x[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) me.template read<T>(a.x, row * a.ldx, p, there, x[p]);
+        float sum[1] = {0.f}, both[2] = {0.f, 0.f}, d[P][N];
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) d[p][e] = (float)x[p].v[e];
+            me.clear(p, d[p]);
+#pragma unroll
+            for (int e = 0; e < N; ++e) sum[0] += d[p][e];
+        }
+        row_sum<WIDE>(sum, a.lanes, part, turn);
+        const float m = sum[0] * a.over;
+        // The mean's own rounding is found from the differences and taken out of them, so
+        // that rows far from 0 keep their bits.
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) d[p][e] = (float)x[p].v[e] - m;
+            me.clear(p, d[p]);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                both[0] += d[p][e];
+                both[1] = fmaf(d[p][e], d[p][e], both[1]);
+            }
+        }
+        row_sum<WIDE>(both, a.lanes, part, turn);
+        const float off = both[0] * a.over;
+        const float rstd = rsqrtf(fmaxf(fmaf(-off, off, both[1] * a.over), 0.f) + a.eps);
+        if (!there) continue;
+        if (a.kept && me.lane == 0) {
+            a.kept[2 * row] = m + off;
+            a.kept[2 * row + 1] = rstd;
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            Piece<T, N> y;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                float v = ((float)x[p].v[e] - m - off) * rstd;
+                if (a.weight) v *= (float)weight[p].v[e];
+                if (a.bias) v += (float)bias[p].v[e];
+                y.v[e] = (T)v;
+            }
+            if (me.mine(p)) y.write(static_cast<T *>(a.y) + row * a.width + me.at[p], N);
+        }
+    }
+}
+
+// Rows that a workgroup does not hold, and rows shorter than a piece: read three times,
+// the later ones mostly from the caches.
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
+    constexpr int N = 16 / sizeof(T);
+    __shared__ float part[kPart];
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+        const T *const x = static_cast<const T *>(a.x) + row * a.ldx;
+        float sum[1] = {0.f}, both[2] = {0.f, 0.f};
+        for (int64_t c = (int64_t)threadIdx.x * N; c < a.width; c += (int64_t)blockDim.x * N) {
+            Piece<T, N> v;
+            v.read(x + c, (int)std::min<int64_t>(N, a.width - c));
+#pragma unroll
+            for (int e = 0; e < N; ++e) sum[0] += (float)v.v[e];
+        }
+        row_sum<true>(sum, 0, part, turn);
+        const float m = sum[0] * a.over;
+        for (int64_t c = (int64_t)threadIdx.x * N; c < a.width; c += (int64_t)blockDim.x * N) {
+            const int left = (int)std::min<int64_t>(N, a.width - c);
+            Piece<T, N> v;
+            v.read(x + c, left);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float d = e < left ? (float)v.v[e] - m : 0.f;
+                both[0] += d;
+                both[1] = fmaf(d, d, both[1]);
+            }
+        }
+        row_sum<true>(both, 0, part, turn);
+        const float off = both[0] * a.over;
+        const float rstd = rsqrtf(fmaxf(fmaf(-off, off, both[1] * a.over), 0.f) + a.eps);
+        if (a.kept && threadIdx.x == 0) {
+            a.kept[2 * row] = m + off;
+            a.kept[2 * row + 1] = rstd;
+        }
+        for (int64_t c = (int64_t)threadIdx.x * N; c < a.width; c += (int64_t)blockDim.x * N) {
+            const int left = (int)std::min<int64_t>(N, a.width - c);
+            Piece<T, N> v, weight, bias;
+            v.read(x + c, left);
+            if (a.weight) weight.read(static_cast<const T *>(a.weight) + c, left);
+            if (a.bias) bias.read(static_cast<const T *>(a.bias) + c, left);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                float u = ((float)v.v[e] - m - off) * rstd;
+                if (a.weight) u *= (float)weight.v[e];
+                if (a.bias) u += (float)bias.v[e];
+                v.v[e] = (T)u;
+            }
+            v.write(static_cast<T *>(a.y) + row * a.width + c, left);
+        }
+    }
+}
+
+// COLUMNS: also the workgroup's parts of dweight and dbias.
+template <typename T, int P, bool WIDE, bool COLUMNS>
+__global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs a) {
+    constexpr int N = 16 / sizeof(T);
+    extern __shared__ float lds[];
+    float *const part = lds;          // kPart
+    int turn = 0;
+    const Part<WIDE, P, N> me(a.lanes, (int)a.width);
+    Piece<T, N> weight[P];
+    float dweight[P][N], dbias[P][N];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        me.template read<T>(a.weight, 0, p, a.weight != nullptr, weight[p]);
+#pragma unroll
+        for (int e = 0; e < N; ++e) dweight[p][e] = dbias[p][e] = 0.f;
+    }
+    for (int64_t r0 = (int64_t)blockIdx.x * me.rows; r0 < a.n; r0 += (int64_t)gridDim.x * me.rows) {
+        const int64_t row = r0 + me.row;
+        const bool there = row < a.n;
+        Piece<T, N> x[P], dy[P], beside[P];
+        const float mean = there ? a.kept[2 * row] : 0.f, rstd = there ? a.kept[2 * row + 1] : 0.f;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            me.template read<T>(a.x, row * a.ldx, p, there, x[p]);
+            me.template read<T>(a.dy, row * a.lddy, p, there, dy[p]);
+            if (a.beside) me.template read<T>(a.beside, row * a.ldb, p, there, beside[p]);
+        }
+        float both[2] = {0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            float u[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) u[e] = (float)dy[p].v[e];
+            me.clear(p, u);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float xh = ((float)x[p].v[e] - mean) * rstd;
+                const float g = a.weight ? u[e] * (float)weight[p].v[e] : u[e];
+                both[0] += g;
+                both[1] = fmaf(g, xh, both[1]);
+                if (COLUMNS) {
+                    dweight[p][e] = fmaf(u[e], xh, dweight[p][e]);
+                    dbias[p][e] += u[e];
+                }
+            }
+        }
+        if (!a.dx) continue;   // for all lanes alike
+        row_sum<WIDE>(both, a.lanes, part, turn);
+        if (!there) continue;
+        const float g0 = both[0] * a.over, g1 = both[1] * a.over;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            Piece<T, N> dx;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float u = (float)dy[p].v[e];
+                const float xh = ((float)x[p].v[e] - mean) * rstd;
+                const float g = a.weight ? u * (float)weight[p].v[e] : u;
+                float v = rstd * (g - g0 - xh * g1);
+                if (a.beside) v += (float)beside[p].v[e];
+                dx.v[e] = (T)v;
+            }
+            if (me.mine(p)) dx.write(static_cast<T *>(a.dx) + row * a.width + me.at[p], N);
+        }
+    }
+    if (!COLUMNS) return;
+    float *const to = a.partial + (int64_t)blockIdx.x * 2 * a.width;
+    if (WIDE) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                if (e >= me.skip[p]) {
+                    to[me.at[p] + e] = dweight[p][e];
+                    to[a.width + me.at[p] + e] = dbias[p][e];
+                }
+            }
+        return;
+    }
+    // the rows of a wave by exchange, the four waves through LDS: each column's two sums
+    float *const shared = lds + kPart;   // 4 x width x 2
+    const int wave = threadIdx.x >> 6, span = (int)a.width * 2;
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            for (int o = a.lanes; o < 64; o <<= 1) {
+                dweight[p][e] += __shfl_xor(dweight[p][e], o);
+                dbias[p][e] += __shfl_xor(dbias[p][e], o);
+            }
+            if ((threadIdx.x & 63) < a.lanes && e >= me.skip[p]) {
+                float *const at = shared + wave * span + (me.at[p] + e) * 2;
+                at[0] = dweight[p][e];
+                at[1] = dbias[p][e];
+            }
+        }
+    __syncthreads();
+    for (int c = threadIdx.x; c < span; c += blockDim.x) {
+        float v = 0.f;
+        for (int w = 0; w < 4; ++w) v += shared[w * span + c];
+        to[(c & 1) * a.width + (c >> 1)] = v;
+    }
+}
+
+// dx of such rows.
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_long_backward_kernel(NormArgs a) {
+    constexpr int N = 16 / sizeof(T);
+    __shared__ float part[kPart];
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+        const T *const x = static_cast<const T *>(a.x) + row * a.ldx;
+        const T *const dy = static_cast<const T *>(a.dy) + row * a.lddy;
+        const float mean = a.kept[2 * row], rstd = a.kept[2 * row + 1];
+        const auto values = [&](int64_t c, int left, float (&g)[N], float (&xh)[N]) {
+            Piece<T, N> u, v, weight;
+            u.read(dy + c, left);
+            v.read(x + c, left);
+            if (a.weight) weight.read(static_cast<const T *>(a.weight) + c, left);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                g[e] = a.weight ? (float)u.v[e] * (float)weight.v[e] : (float)u.v[e];
+                xh[e] = e < left ? ((float)v.v[e] - mean) * rstd : 0.f;
+            }
+        };
+        float both[2] = {0.f, 0.f}, g[N], xh[N];
+        for (int64_t c = (int64_t)threadIdx.x * N; c < a.width; c += (int64_t)blockDim.x * N) {
+            values(c, (int)std::min<int64_t>(N, a.width - c), g, xh);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                both[0] += g[e];
+                both[1] = fmaf(g[e], xh[e], both[1]);
+            }
+        }
+        row_sum<true>(both, 0, part, turn);
+        const float g0 = both[0] * a.over, g1 = both[1] * a.over;
+        for (int64_t c = (int64_t)threadIdx.x * N; c < a.width; c += (int64_t)blockDim.x * N) {
+            const int left = (int)std::min<int64_t>(N, a.width - c);
+            values(c, left, g, xh);
+            Piece<T, N> beside, dx;
+            if (a.beside) beside.read(static_cast<const T *>(a.beside) + row * a.ldb + c, left);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                float v = rstd * (g[e] - g0 - xh[e] * g1);
+                if (a.beside) v += (float)beside.v[e];
+                dx.v[e] = (T)v;
+            }
+            dx.write(static_cast<T *>(a.dx) + row * a.width + c, left);
+        }
+    }
+}
+
+// Their parts of dweight and dbias, 256 pieces of a row to a workgroup.
+template <typename T>
+__global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a) {
+    constexpr int N = 16 / sizeof(T);
+    const int64_t col = ((int64_t)blockIdx.y * 256 + threadIdx.x) * N;
+    if (col >= a.width) return;
+    const int left = (int)std::min<int64_t>(N, a.width - col);
+    float dweight[N], dbias[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) dweight[e] = dbias[e] = 0.f;
+    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+        const float mean = a.kept[2 * row], rstd = a.kept[2 * row + 1];
+        Piece<T, N> u, v;
+        u.read(static_cast<const T *>(a.dy) + row * a.lddy + col, left);
+        v.read(static_cast<const T *>(a.x) + row * a.ldx + col, left);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            dweight[e] = fmaf((float)u.v[e], ((float)v.v[e] - mean) * rstd, dweight[e]);
+            dbias[e] += (float)u.v[e];
+        }
+    }
+    float *const to = a.partial + (int64_t)blockIdx.x * 2 * a.width + col;
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        if (e < left) {
+            to[e] = dweight[e];
+            to[a.width + e] = dbias[e];
+        }
+}
+
+// dweight and dbias from their parts, in order: 32 columns of both, eight lanes each.
+template <typename T>
+__global__ __launch_bounds__(256) void norm_join_kernel(NormArgs a) {
+    __shared__ float part[8][32];
+    const int c = threadIdx.x & 31, lane = threadIdx.x >> 5;
+    const int64_t col = (int64_t)blockIdx.x * 32 + c;
+    float v = 0.f;
+    if (col < 2 * a.width) {
+#pragma unroll 4
+        for (int p = lane; p < a.parts; p += 8) v += a.partial[p * 2 * a.width + col];
+    }
+    part[lane][c] = v;
+    __syncthreads();
+    if (lane == 0 && col < 2 * a.width) {
+        for (int l = 1; l < 8; ++l) v += part[l][c];
+        if (col < a.width) {
+            if (a.dweight) static_cast<T *>(a.dweight)[col] = (T)v;
+        } else if (a.dbias) {
+            static_cast<T *>(a.dbias)[col - a.width] = (T)v;
+        }
+    }
+}
+
+// How rows are taken: pieces to a lane, lanes to a row, threads of a workgroup.
+struct Shape {
+    int pieces, lanes, threads;
+    bool wide, held;
+};
+
+Shape shape_of(const NormArgs &a, int most_wave, int most_wide) {
+    const int n = 16 / type_size(a.type);
+    const int64_t pieces = (a.width + n - 1) / n;
+    Shape s{};
+    s.wide = pieces > 64 * most_wave;
+    s.held = pieces <= (int64_t)1024 * most_wide && a.width >= n;
+    if (!s.held) {
+        s.threads = a.width < n ? 64 : 1024;
+    } else if (!s.wide) {
+        s.pieces = (int)(pieces + 63) / 64;
+        s.lanes = 1;
+        while (s.lanes * s.pieces < pieces) s.lanes *= 2;
+        s.threads = 256;
+    } else {
+        s.pieces = most_wide;
+        s.lanes = (int)((pieces + 64 * s.pieces - 1) / (64 * s.pieces)) * 64;
+        // as few pieces to a lane as these lanes allow
+        while (s.pieces > 1 && (int64_t)s.lanes * (s.pieces - 1) >= pieces) --s.pieces;
+        s.threads = s.lanes;
+    }
+    return s;
+}
+
+template <typename F>
+hipError_t by_type(int32_t type, F f) {
+    switch (type) {
+        case kF32: f(float()); break;
+        case kBF16: f(__bf16()); break;
+        default: f(_Float16()); break;
+    }
+    return hipGetLastError();
+}
+
+template <int V>
+using Int = std::integral_constant<int, V>;
+
+// f(Int<pieces>()), of up to MOST.
+template <int MOST, typename F>
+void by_pieces(int pieces, F f) {
+    if constexpr (MOST > 1) {
+        if (pieces < MOST) return by_pieces<MOST - 1>(pieces, f);
+    }
+    f(Int<MOST>());
+}
+
+// Pieces that a lane has registers for: of a row that a few lanes take, and of one that a
+// workgroup takes (of 1024 threads, 128 registers each).
+constexpr int kWavePieces = 2;
+template <typename T>
+constexpr int kForwardPieces = sizeof(T) == 4 ? 4 : 2;
+template <typename T>
+constexpr int kBackwardPieces = sizeof(T) == 4 ? 3 : 2;
+Shape forward_shape(const NormArgs &a) {
+    return shape_of(a, kWavePieces, a.type == kF32 ? kForwardPieces<float> : kForwardPieces<__bf16>);
+}
+Shape backward_shape(const NormArgs &a) {
+    return shape_of(a, kWavePieces, a.type == kF32 ? kBackwardPieces<float> : kBackwardPieces<__bf16>);
+}
+
+// Workgroups that a launch of row after row takes.
+int64_t groups_of(const NormArgs &a, const Shape &s, int num_cus) {
+    const int64_t rows = s.held && !s.wide ? s.threads / s.lanes : 1;
+    const int64_t fit = std::max(1, 2048 / s.threads);   // of a compute unit
+    return std::min((a.n + rows - 1) / rows, num_cus * fit);
+}
+
+}  // namespace
+
+int32_t norm_parts(const NormArgs &a, int num_cus) {
+    const Shape s = backward_shape(a);
+    const int64_t rows = s.held && !s.wide ? s.threads / s.lanes : 1;
+    const int64_t groups = s.held ? std::min(groups_of(a, s, num_cus), (a.n + 4 * rows - 1) / (4 * rows))
+                                  : std::min<int64_t>((a.n + 15) / 16, num_cus);
+    return (int32_t)std::max<int64_t>(1, groups);
+}
+
+hipError_t launch_norm(const NormArgs &args, int num_cus, hipStream_t stream) {
+    NormArgs a = args;
+    const Shape s = forward_shape(a);
+    const unsigned groups = (unsigned)groups_of(a, s, num_cus);
+    a.lanes = s.lanes;
+    a.over = 1.f / (float)a.width;
+    return by_type(a.type, [&](auto t) {
+        using T = decltype(t);
+        if (!s.held) {
+            norm_long_kernel<T><<<groups, s.threads, 0, stream>>>(a);
+            return;
+        }
+        by_pieces<kForwardPieces<T>>(s.pieces, [&](auto p) {
+            constexpr int P = decltype(p)::value;
+            if (s.wide) norm_kernel<T, P, true><<<groups, s.threads, 0, stream>>>(a);
+            else norm_kernel<T, P, false><<<groups, s.threads, 0, stream>>>(a);
+        });
+    });
+}
+
+hipError_t launch_norm_backward(const NormArgs &args, int num_cus, hipStream_t stream) {
+    NormArgs a = args;
+    const Shape s = backward_shape(a);
+    const bool columns = a.dweight || a.dbias;
+    a.lanes = s.lanes;
+    a.over = 1.f / (float)a.width;
+    const unsigned groups = columns ? (unsigned)a.parts : (unsigned)groups_of(a, s, num_cus);
+    const int64_t wide = (a.width * type_size(a.type) + 16 * 256 - 1) / (16 * 256);
+    return by_type(a.type, [&](auto t) {
+        using T = decltype(t);
+        if (s.held) {
+            by_pieces<kBackwardPieces<T>>(s.pieces, [&](auto p) {
+                constexpr int P = decltype(p)::value;
+                const unsigned lds =
+                    (unsigned)((kPart + (columns && !s.wide ? 4 * a.width * 2 : 0)) * sizeof(float));
+                if (s.wide && columns)
+                    norm_backward_kernel<T, P, true, true><<<groups, s.threads, lds, stream>>>(a);
+                else if (s.wide)
+                    norm_backward_kernel<T, P, true, false><<<groups, s.threads, lds, stream>>>(a);
+                else if (columns)
+                    norm_backward_kernel<T, P, false, true><<<groups, s.threads, lds, stream>>>(a);
+                else
+                    norm_backward_kernel<T, P, false, false><<<groups, s.threads, lds, stream>>>(a);
+            });
+        } else {
+            const unsigned rows = (unsigned)groups_of(a, s, num_cus);
+            if (a.dx && a.n) norm_long_backward_kernel<T><<<rows, s.threads, 0, stream>>>(a);
+            if (columns)
+                norm_columns_kernel<T><<<dim3(groups, (unsigned)wide), 256, 0, stream>>>(a);
+        }
+        if (columns)
+            norm_join_kernel<T><<<(unsigned)((2 * a.width + 31) / 32), 256, 0, stream>>>(a);
+    });
+}
+
+}  // namespace som

@@ -33,7 +33,7 @@ from . import SomError, _check, lib as _lib
 
 __all__ = [
     "ACTIVATIONS", "GATES", "EXPORTED", "SomError", "Routing", "ExpertsGradient", "AdamW", "linear",
-    "linear_backward", "route", "route_backward", "dispatch", "experts", "experts_backward",
+    "linear_backward", "norm", "norm_backward", "route", "route_backward", "dispatch", "experts", "experts_backward",
     "gate_from_map",
 ]
 
@@ -46,6 +46,7 @@ STATE_BLOCK = 256
 EXPORTED = (
     "som_linear_workspace", "som_linear_route", "som_linear", "som_linear_backward",
     "som_experts_workspace", "som_experts_route", "som_experts", "som_experts_backward",
+    "som_norm_workspace", "som_norm", "som_norm_backward",
     "som_route", "som_route_backward",
     "som_dispatch_workspace", "som_dispatch", "som_adamw_room", "som_adamw_create",
     "som_adamw_destroy", "som_adamw_step",
@@ -79,6 +80,18 @@ class _ExpertsCall(C.Structure):
                 ("lddy", C.c_int64), ("dx", C.c_void_p), ("dweight", C.c_void_p),
                 ("dw1", C.c_void_p), ("db1", C.c_void_p), ("dw2", C.c_void_p),
                 ("db2", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_uint64), ("stream", C.c_void_p)]
+
+
+class _NormCall(C.Structure):
+    """``som_norm_call`` of include/som_local.h."""
+
+    _fields_ = [("type", C.c_int32), ("width", C.c_int32), ("n", C.c_int64),
+                ("x", C.c_void_p), ("ldx", C.c_int64), ("weight", C.c_void_p),
+                ("bias", C.c_void_p), ("eps", C.c_float), ("y", C.c_void_p),
+                ("kept", C.c_void_p), ("dy", C.c_void_p), ("lddy", C.c_int64),
+                ("beside", C.c_void_p), ("ldb", C.c_int64), ("dx", C.c_void_p),
+                ("dweight", C.c_void_p), ("dbias", C.c_void_p), ("workspace", C.c_void_p),
                 ("workspace_bytes", C.c_uint64), ("stream", C.c_void_p)]
 
 
@@ -122,6 +135,9 @@ def lib():
         "som_experts_route": [C.POINTER(_ExpertsCall), i32, C.POINTER(i32)],
         "som_experts": [C.POINTER(_ExpertsCall)],
         "som_experts_backward": [C.POINTER(_ExpertsCall)],
+        "som_norm_workspace": [C.POINTER(_NormCall), i32, C.POINTER(u64)],
+        "som_norm": [C.POINTER(_NormCall)],
+        "som_norm_backward": [C.POINTER(_NormCall)],
         "som_route": [C.POINTER(_RouteCall)],
         "som_route_backward": [C.POINTER(_RouteCall)],
         "som_dispatch_workspace": [i64, i32, i32, C.POINTER(u64)],
@@ -278,6 +294,61 @@ def linear_backward(dy, x, w, z=None, activation: str = "none", bias: bool = Tru
     call.dx, call.dw, call.dbias = _ptr(dx), _ptr(dw), _ptr(dbias)
     _run("linear", call, True, x)
     return dx, dw, dbias
+
+
+# --------------------------------------------------------------- layer norm
+def _norm_call(x, weight, eps: float):
+    code = _type(x, "x")
+    _rows(x, "x")
+    if not x.shape[1]:
+        raise ValueError("x must have columns")
+    call = _NormCall(type=code, width=x.shape[1], n=x.shape[0], x=_ptr(x), ldx=_ld(x), eps=eps)
+    if weight is not None:
+        _like(weight, x, (x.shape[1],), "weight")
+        call.weight = _ptr(weight)
+    return call
+
+
+def norm(x, weight=None, bias=None, eps: float = 1e-5, keep: bool = False):
+    """Layer norm of the rows of x (n, width): (x - mean) / sqrt(var + eps), times
+    weight (width,), plus bias (width,).
+
+    With ``keep`` returns (y, kept): each row's mean and 1 / sqrt(var + eps), (n, 2)
+    fp32, which the gradient needs."""
+    call = _norm_call(x, weight, eps)
+    if bias is not None:
+        _like(bias, x, (x.shape[1],), "bias")
+        call.bias = _ptr(bias)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    kept = torch.empty((x.shape[0], 2), dtype=torch.float32, device=x.device) if keep else None
+    call.y, call.kept = _ptr(y), _ptr(kept)
+    call.stream = _stream(x)
+    _check(lib().som_norm(C.byref(call)), "som_norm")
+    return (y, kept) if keep else y
+
+
+def norm_backward(dy, x, weight, kept, beside=None, bias: bool = True):
+    """(dx, dweight, dbias) of ``norm`` from the gradient dy of its result.
+
+    ``beside`` (n, width) is added to dx: the gradient of what goes past the norm.
+    dweight is None where weight is, dbias without ``bias``."""
+    call = _norm_call(x, weight, 0.0)
+    n, width = x.shape
+    _like(dy, x, (n, width), "dy", packed=False)
+    call.dy, call.lddy = _ptr(dy), _ld(dy)
+    if not isinstance(kept, torch.Tensor) or kept.dtype != torch.float32:
+        raise TypeError("kept must be float32 (norm with keep=True)")
+    _shaped(kept, x, (n, 2), "kept")
+    call.kept = _ptr(kept)
+    if beside is not None:
+        _like(beside, x, (n, width), "beside", packed=False)
+        call.beside, call.ldb = _ptr(beside), _ld(beside)
+    dx = torch.empty((n, width), dtype=x.dtype, device=x.device)
+    dweight = torch.empty_like(weight) if weight is not None else None
+    dbias = torch.empty(width, dtype=x.dtype, device=x.device) if bias else None
+    call.dx, call.dweight, call.dbias = _ptr(dx), _ptr(dweight), _ptr(dbias)
+    _run("norm", call, True, x)
+    return dx, dweight, dbias
 
 
 # ------------------------------------------------------------------ routing
