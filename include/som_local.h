@@ -258,6 +258,49 @@ som_status som_dispatch(const int32_t *index, int64_t n, int32_t k, int32_t expe
                         int32_t *offsets, int32_t *order, int32_t *place, void *work,
                         uint64_t work_bytes, void *stream);
 
+/* The loss of n rows of logits s (n x classes) by what a teacher says of its k best
+ * classes, by labels, or both, and its gradient.  With T = temperature, the teacher's
+ * logits t_j of the classes index_j, and its probability r (`rest`) of all classes that
+ * it does not name,
+ *     p_j = (1 - r) e^(t_j / T) / sum over j of e^(t_j / T),     a = softmax(s / T),
+ *     soft = T^2 ( sum over j of p_j (log p_j - log a[index_j]) + r (log r - log a_R) ),
+ *     hard = -log softmax(s)[label],       loss = mix soft + (1 - mix) hard,
+ * a_R being the sum of a over the classes that are not named.  0 log 0 is 0.  For example
+ * the units nearest to a document, their scores, and what a softmax over all units leaves.
+ * With the gradient `scale dloss_i` of a row's loss (dloss NULL: scale), P_c the
+ * sum of the p_j with index_j = c, and only over the row's own parts,
+ *     dlogits_c = scale dloss_i ( mix T (a_c - P_c)              of a named class
+ *                                 mix T (a_c - r a_c / a_R)      of another
+ *                               + (1 - mix) (softmax(s)_c - [c = label]) )
+ * An index or a label outside [0, classes) counts as absent.  A row without an index
+ * that is there (or whose t are all -infinity) has no soft part, one without a label no
+ * hard one.  A class may be named more than once: its p add up.  Logits of -infinity
+ * close a class: it has a = 0; a row without an open class has loss and gradient 0.  A row
+ * whose logits or t hold a NaN or +infinity has NaN for both.  r below 0 counts as 0. */
+typedef struct som_distill_call {
+    int32_t type;              /* som_type of logits and dlogits                     */
+    int32_t teacher_type;      /* som_type of teacher                                */
+    int64_t n;                 /* rows; 0 is allowed                                 */
+    int32_t classes;           /* 1 .. 1,048,576                                     */
+    int32_t k;                 /* classes that the teacher names, <= 64; 0: none     */
+    const void *logits;
+    int64_t lds;               /* elements from row to row, >= classes               */
+    const int32_t *index;      /* n x k, packed                                      */
+    const void *teacher;       /* n x k, packed                                      */
+    const float *rest;         /* n; NULL for 0                                      */
+    const int32_t *label;      /* n; NULL for none                                   */
+    float temperature;         /* > 0                                                */
+    float mix;                 /* in [0, 1]; 0 without a teacher, 1 without labels   */
+    const float *dloss;        /* n; NULL for 1                                      */
+    float scale;
+    float *loss;               /* n; NULL if not wanted                              */
+    void *dlogits;             /* packed n x classes; NULL if not wanted             */
+    void *stream;
+} som_distill_call;
+
+/* Errors: SOM_E_ARG, SOM_E_UNSUPPORTED (more than 1,048,576 classes), SOM_E_DEVICE. */
+som_status som_distill(const som_distill_call *call);
+
 /* AdamW over many tensors at once.  Step t of element p with gradient g:
  *     m = beta1 m + (1 - beta1) g        v = beta2 v + (1 - beta2) g^2
  *     p = p (1 - lr weight_decay)

@@ -1,0 +1,456 @@
+// A loss from a teacher's top logits and from labels, and its gradient, in one read of
+// the logits (the formulas are som_local.h's).  Of a row s of `classes` logits with its
+// maximum m, and c = log2(e) / temperature:
+//     Z = sum of 2^((s - m) c),    R = the same over the classes that the teacher left out,
+//     E = sum of e^(s - m)         (labels only)
+// give the loss, and with them the gradient is an exponential or two of each logit again.
+// Bound by memory, logits read and gradients written once, and behind that by the
+// exponentials: a quarter of the rate of other instructions, two to four a logit.
+// A row stays in registers as it was read, 16-byte pieces of it to a lane, of 1 to 64
+// lanes or of a workgroup; only rows beyond what a workgroup holds are read twice.  R is
+// summed by itself (Z less the teacher's classes would cancel): the teacher's classes are
+// marked by bits in LDS, of which a piece of a row takes its own in one read.
+#include "som_row.h"
+
+#include <algorithm>
+#include <math.h>
+
+namespace som {
+namespace {
+
+constexpr float kLog2e = 1.44269504f;
+
+// What the teacher says of a workgroup's rows, in LDS: for each row bits of its classes,
+// its entries (a class, or -1 for none, and its probability) and its rest.
+struct Taught {
+    uint32_t *bits;
+    int *index;
+    float *p, *rest;
+    int words, k;
+    __device__ Taught(char *lds, int rows, int row, const DistillArgs &a) {
+        words = a.words, k = a.k;
+        const int each = words + 2 * k + 2;
+        bits = reinterpret_cast<uint32_t *>(lds) + row * each;
+        index = reinterpret_cast<int *>(bits + words);
+        p = reinterpret_cast<float *>(index + k);
+        rest = p + k;   // the rest; 1 where there is a teacher, 0 where not, NaN for NaN
+    }
+    // The marks of the N classes from `at` on.
+    template <int N>
+    __device__ uint32_t marks(int at) const {
+        const uint32_t *const w = bits + (at >> 5);
+        const uint64_t both = (uint64_t)w[1] << 32 | w[0];
+        return (uint32_t)(both >> (at & 31)) & ((1u << N) - 1);
+    }
+    // The teacher's probability of class c (entries of the same class add up).
+    __device__ float of(int c) const {
+        float v = 0.f;
+        for (int j = 0; j < k; ++j) v += index[j] == c ? p[j] : 0.f;
+        return v;
+    }
+};
+
+__device__ inline float wide(const void *p, int32_t type, int64_t i) {
+    return type == kF32    ? static_cast<const float *>(p)[i]
+           : type == kBF16 ? (float)static_cast<const __bf16 *>(p)[i]
+                           : (float)static_cast<const _Float16 *>(p)[i];
+}
+
+// Sum and maximum over `lanes` neighbours, at most a wave.
+__device__ inline float lanes_sum(float v, int lanes) {
+    for (int o = 1; o < lanes; o <<= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// The entries of a row, by `lanes` lanes of one wave that cover the row's `lane` 0 ..
+// The bits are zeros before.
+__device__ inline void teach(const DistillArgs &a, const Taught &t, int64_t row, bool there, int lane,
+                             int lanes) {
+    float best = -INFINITY, sum = 0.f;
+    for (int j = lane; j < a.k; j += lanes) {
+        const int64_t s = row * a.k + j;
+        int c = there ? a.index[s] : -1;
+        if (c < 0 || c >= a.classes) c = -1;
+        const float v = c >= 0 ? wide(a.teacher, a.teacher_type, s) / a.temperature : -INFINITY;
+        t.index[j] = c;
+        t.p[j] = v;
+        if (c >= 0) atomicOr(t.bits + (c >> 5), 1u << (c & 31));
+        best = fmaxf(best, v);
+    }
+    for (int o = 1; o < lanes; o <<= 1) best = fmaxf(best, __shfl_xor(best, o));
+    const float from = best > -INFINITY ? best : 0.f;   // nothing: e^-inf below is 0
+    for (int j = lane; j < a.k; j += lanes) {
+        const float e = expf(t.p[j] - from);
+        t.p[j] = e;
+        sum += e;
+    }
+    sum = lanes_sum(sum, lanes);
+    float rest = 0.f;
+    if (a.rest && there) {
+        rest = a.rest[row];
+        rest = rest <= 0.f || sum == 0.f ? 0.f : rest;
+    }
+    const float by = (1.f - rest) / (sum == 0.f ? 1.f : sum);
+    for (int j = lane; j < a.k; j += lanes) t.p[j] *= by;
+    if (lane == 0) {
+        t.rest[0] = rest;
+        t.rest[1] = sum == 0.f ? 0.f : sum / sum;
+    }
+}
+
+// Keeps a row's pieces as they were read between its passes, not the floats that the last
+// pass made of them, which would take more registers than there are.
+template <typename T, int P>
+__device__ inline void keep_raw(Piece<T, 16 / sizeof(T)> (&x)[P]) {
+    typedef int Raw __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        Raw raw = __builtin_bit_cast(Raw, x[p].v);
+        asm volatile("" : "+v"(raw));
+        x[p].v = __builtin_bit_cast(decltype(x[p].v), raw);
+    }
+}
+
+// What a row's sums give.
+struct Factors {
+    float z, r, e;                  // the sums
+    float top, chosen, other, one;  // m; factors of 2^((s - m) c) and of e^(s - m)
+    float given;                    // of the teacher's probability
+    float label;                    // of the label's class
+    bool shut;                      // a row without an open class
+    int at;                         // the label's class, or -1
+    template <bool HARD>
+    __device__ static Factors of(const DistillArgs &a, const Taught &t, int64_t row, float top,
+                                 float z, float r, float e) {
+        Factors f;
+        f.z = z, f.r = r, f.e = e, f.top = top;
+        f.shut = z == 0.f;
+        f.at = -1;
+        if (HARD) {
+            f.at = a.label[row];
+            if (f.at < 0 || f.at >= a.classes) f.at = -1;
+        }
+        const float scale = a.scale * (a.dloss ? a.dloss[row] : 1.f);
+        const float soft = scale * a.mix * a.temperature, hard = scale * (1.f - a.mix);
+        f.chosen = f.other = f.given = f.one = f.label = 0.f;
+        if (f.shut) return f;
+        if (a.k && a.mix != 0.f && !(t.rest[1] == 0.f)) {
+            f.given = soft * t.rest[1];
+            f.chosen = f.given / z;
+            f.other = f.chosen;
+            // the classes that the teacher left out, whose sum is to be its rest
+            if (t.rest[0] != 0.f) f.other = r == 0.f ? 0.f : f.chosen * (1.f - t.rest[0] * (z / r));
+        }
+        if (HARD && f.at >= 0) f.one = hard / e, f.label = hard;
+        return f;
+    }
+};
+
+// The row's loss, by `lanes` lanes of one wave.
+template <typename T, bool HARD>
+__device__ inline float loss_of(const DistillArgs &a, const Taught &t, const Factors &f, const T *s,
+                                int lane, int lanes) {
+    if (f.shut) return 0.f;
+    float soft = 0.f, all = 0.f;
+    // half of a logit's distance from the maximum: the whole may pass fp32's range where
+    // its product with a probability does not
+    const auto half_below = [&](T v) { return 0.5f * (float)v - 0.5f * f.top; };
+    if (a.k && a.mix != 0.f) {
+        const float log_z = logf(f.z);
+        for (int j = lane; j < a.k; j += lanes) {
+            const float p = t.p[j];
+            if (t.index[j] < 0 || p == 0.f) continue;
+            soft = fmaf(p, logf(p) + log_z, soft);
+            soft -= 2.f * (p * (half_below(s[t.index[j]]) / a.temperature));
+        }
+        soft = lanes_sum(soft, lanes);
+        const float rest = t.rest[0];
+        if (rest != 0.f) soft = fmaf(rest, logf(rest) - (logf(f.r) - log_z), soft);
+        if (t.rest[1] != 1.f) soft = t.rest[1];   // 0 or NaN
+        all = a.mix * a.temperature * a.temperature * soft;
+    }
+    if (HARD && f.at >= 0) {
+        const float part = 1.f - a.mix;
+        all += fmaf(part, logf(f.e), -2.f * (part * half_below(s[f.at])));
+    }
+    return all;
+}
+
+// The gradient of N neighbouring logits v of classes `at` .., marked `marks`.
+template <bool HARD, int N>
+__device__ inline void slopes(const Taught &t, const Factors &f, float c, int at, uint32_t marks,
+                              float (&v)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const float u = v[e] - f.top;
+        const float w = f.other * __builtin_amdgcn_exp2f(u * c);
+        v[e] = HARD ? fmaf(f.one, __builtin_amdgcn_exp2f(u * kLog2e), w) : w;
+        if (marks >> e & 1) {   // few
+            v[e] = f.chosen * __builtin_amdgcn_exp2f(u * c) - f.given * t.of(at + e);
+            if (HARD) v[e] = fmaf(f.one, __builtin_amdgcn_exp2f(u * kLog2e), v[e]);
+        }
+        if (HARD && f.at == at + e) v[e] -= f.label;
+        if (f.shut) v[e] = 0.f;
+    }
+}
+
+template <typename T, int P, bool WIDE, bool HARD>
+__global__ __launch_bounds__(1024) void distill_kernel(DistillArgs a) {
+    constexpr int N = 16 / sizeof(T);
+    extern __shared__ char lds[];
+    __shared__ float part[WIDE ? kPart : 1];
+    int turn = 0;
+    const Part<WIDE, P, N> me(a.lanes, a.classes);
+    const int64_t row = (int64_t)blockIdx.x * me.rows + me.row;
+    const bool there = row < a.n;
+    const T *const s = static_cast<const T *>(a.logits) + row * a.lds;
+    Piece<T, N> x[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) me.template read<T>(s, 0, p, there, x[p]);
+    const Taught t(lds, me.rows, me.row, a);
+    const bool first = !WIDE || threadIdx.x < 64;      // those that deal with entries
+    const int lanes = WIDE ? 64 : a.lanes;
+    if (a.k) {
+        for (int w = me.lane; w < a.words; w += a.lanes) t.bits[w] = 0;
+        __syncthreads();
+        if (first) teach(a, t, row, there, me.lane, lanes);
+        if (!WIDE) __syncthreads();                    // otherwise the maximum's
+    }
+    // -infinity where a piece is not this lane's
+    const auto values = [&](int p, float (&v)[N]) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = (float)x[p].v[e];
+        if (me.skip[p] > 0) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = e < me.skip[p] ? -INFINITY : v[e];
+        }
+    };
+    float top[1] = {-INFINITY};
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        float v[N];
+        values(p, v);
+#pragma unroll
+        for (int e = 0; e < N; ++e) top[0] = fmaxf(top[0], v[e]);
+    }
+    row_max<WIDE>(top, a.lanes, part, turn);
+    keep_raw<T, P>(x);
+    const float from = top[0] > -INFINITY ? top[0] : 0.f, c = kLog2e / a.temperature;
+    // the teacher's classes, the others, and all with the exponentials of labels
+    float sums[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        float v[N];
+        values(p, v);
+        const uint32_t marks = a.k && me.mine(p) ? t.template marks<N>(me.at[p]) : 0u;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            v[e] -= from;
+            if (HARD) sums[2] += __builtin_amdgcn_exp2f(v[e] * kLog2e);
+            v[e] = __builtin_amdgcn_exp2f(v[e] * c);
+        }
+        if (marks) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                sums[0] += marks >> e & 1 ? v[e] : 0.f;
+                v[e] = marks >> e & 1 ? 0.f : v[e];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) sums[1] += v[e];
+    }
+    row_sum<WIDE>(sums, a.lanes, part, turn);
+    keep_raw<T, P>(x);
+    if (!there) return;
+    const Factors f =
+        Factors::of<HARD>(a, t, row, from, sums[0] + sums[1], sums[1], sums[2]);
+    if (a.loss && first) {
+        const float loss = loss_of<T, HARD>(a, t, f, s, me.lane, lanes);
+        if (me.lane == 0) a.loss[row] = loss;
+    }
+    if (!a.dlogits) return;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        if (!me.mine(p)) continue;
+        float v[N];
+        Piece<T, N> out;
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = (float)x[p].v[e];
+        slopes<HARD>(t, f, c, me.at[p], a.k ? t.template marks<N>(me.at[p]) : 0u, v);
+#pragma unroll
+        for (int e = 0; e < N; ++e) out.v[e] = (T)v[e];
+        out.write(static_cast<T *>(a.dlogits) + row * a.classes + me.at[p], N);
+    }
+}
+
+// Rows that a workgroup does not hold, and rows shorter than a piece: read twice, with
+// the maximum and the sums of what a lane has seen so far in the first pass.
+template <typename T, bool HARD>
+__global__ __launch_bounds__(1024) void distill_long_kernel(DistillArgs a) {
+    constexpr int N = 16 / sizeof(T);
+    extern __shared__ char lds[];
+    __shared__ float part[kPart];
+    int turn = 0;
+    const int64_t row = blockIdx.x;
+    const T *const s = static_cast<const T *>(a.logits) + row * a.lds;
+    const Taught t(lds, 1, 0, a);
+    const bool first = threadIdx.x < 64;
+    if (a.k) {
+        for (int w = threadIdx.x; w < a.words; w += blockDim.x) t.bits[w] = 0;
+        __syncthreads();
+        if (first) teach(a, t, row, true, threadIdx.x, 64);
+        __syncthreads();
+    }
+    const float c = kLog2e / a.temperature;
+    const int stride = blockDim.x * N;
+    float top[1] = {-INFINITY}, from = 0.f, sums[3] = {0.f, 0.f, 0.f};
+    for (int at = threadIdx.x * N; at < a.classes; at += stride) {
+        const int left = a.classes - at < N ? a.classes - at : N;
+        Piece<T, N> x;
+        x.read(s + at, left);
+        float v[N], most = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            v[e] = e < left ? (float)x.v[e] : -INFINITY;
+            most = fmaxf(most, v[e]);
+        }
+        if (most > top[0]) {
+            const float u = top[0] > -INFINITY ? from - most : 0.f;   // sums of nothing stay 0
+            sums[0] *= __builtin_amdgcn_exp2f(u * c);
+            sums[1] *= __builtin_amdgcn_exp2f(u * c);
+            if (HARD) sums[2] *= __builtin_amdgcn_exp2f(u * kLog2e);
+            top[0] = from = most;
+        }
+        const uint32_t marks = a.k ? t.template marks<N>(at) : 0u;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            v[e] -= from;
+            if (HARD) sums[2] += __builtin_amdgcn_exp2f(v[e] * kLog2e);
+            v[e] = __builtin_amdgcn_exp2f(v[e] * c);
+        }
+        if (marks) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                sums[0] += marks >> e & 1 ? v[e] : 0.f;
+                v[e] = marks >> e & 1 ? 0.f : v[e];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) sums[1] += v[e];
+    }
+    const float mine = top[0];
+    row_max<true>(top, 0, part, turn);
+    const float all = top[0] > -INFINITY ? top[0] : 0.f;
+    if (mine > -INFINITY) {
+        sums[0] *= __builtin_amdgcn_exp2f((mine - all) * c);
+        sums[1] *= __builtin_amdgcn_exp2f((mine - all) * c);
+        if (HARD) sums[2] *= __builtin_amdgcn_exp2f((mine - all) * kLog2e);
+    }
+    row_sum<true>(sums, 0, part, turn);
+    const Factors f = Factors::of<HARD>(a, t, row, all, sums[0] + sums[1], sums[1], sums[2]);
+    if (a.loss && first) {
+        const float loss = loss_of<T, HARD>(a, t, f, s, threadIdx.x, 64);
+        if (threadIdx.x == 0) a.loss[row] = loss;
+    }
+    if (!a.dlogits) return;
+    for (int at = threadIdx.x * N; at < a.classes; at += stride) {
+        const int left = a.classes - at < N ? a.classes - at : N;
+        Piece<T, N> x;
+        x.read(s + at, left);
+        float v[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = (float)x.v[e];
+        slopes<HARD>(t, f, c, at, a.k ? t.template marks<N>(at) : 0u, v);
+#pragma unroll
+        for (int e = 0; e < N; ++e) x.v[e] = (T)v[e];
+        x.write(static_cast<T *>(a.dlogits) + row * a.classes + at, left);
+    }
+}
+
+// Pieces that a lane holds: 1 or 2 of a wave's rows, 4 or 8 of a workgroup's (16 are more
+// than the registers of 1024 threads).
+constexpr int kWavePieces = 2, kWidePieces = 8;
+
+Shape distill_shape(const DistillArgs &a) {
+    Shape s = shape_of(a.type, a.classes, kWavePieces, kWidePieces, 64);
+    if (s.held && s.wide) {
+        const int n = 16 / type_size(a.type), pieces = (a.classes + n - 1) / n;
+        s.pieces = pieces > 1024 * 4 ? 8 : 4;
+        s.threads = s.lanes = (pieces + 64 * s.pieces - 1) / (64 * s.pieces) * 64;
+    }
+    return s;
+}
+
+template <typename T, int P, bool WIDE, bool HARD>
+hipError_t launch_held(const DistillArgs &a, const Shape &s, unsigned groups, unsigned lds,
+                       hipStream_t stream) {
+    distill_kernel<T, P, WIDE, HARD><<<groups, s.threads, lds, stream>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, bool HARD>
+hipError_t launch_typed(const DistillArgs &a, const Shape &s, unsigned groups, unsigned lds,
+                        hipStream_t stream) {
+    if (!s.held) {
+        const auto kernel = distill_long_kernel<T, HARD>;
+        if (lds > 60 * 1024) {
+            const hipError_t e =
+                hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                    hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            if (e != hipSuccess) return e;
+        }
+        kernel<<<groups, s.threads, lds, stream>>>(a);
+        return hipGetLastError();
+    }
+    if (!s.wide) {
+        return s.pieces == 1 ? launch_held<T, 1, false, HARD>(a, s, groups, lds, stream)
+                             : launch_held<T, 2, false, HARD>(a, s, groups, lds, stream);
+    }
+    return s.pieces == 4 ? launch_held<T, 4, true, HARD>(a, s, groups, lds, stream)
+                         : launch_held<T, 8, true, HARD>(a, s, groups, lds, stream);
+}
+
+}  // namespace
+
+hipError_t launch_distill(const DistillArgs &args, hipStream_t stream) {
+    const Shape s = distill_shape(args);
+    const int rows = s.held && !s.wide ? s.threads / s.lanes : 1;
+    DistillArgs a = args;
+    a.lanes = s.lanes;
+    a.words = a.k ? (a.classes + 31) / 32 + 1 : 0;
+    const unsigned lds = (unsigned)rows * (a.words + 2 * a.k + 2) * 4;
+    const int size = type_size(a.type);
+    const bool hard = a.label && a.mix != 1.f;
+    // as many rows at a time as a grid holds
+    const int64_t most = (int64_t)(UINT32_MAX / 1024) * rows;
+    for (int64_t r = 0; r < args.n; r += most) {
+        a.n = std::min(most, args.n - r);
+        const unsigned groups = (unsigned)((a.n + rows - 1) / rows);
+        hipError_t e;
+        switch (a.type) {
+            case kF32:
+                e = hard ? launch_typed<float, true>(a, s, groups, lds, stream)
+                         : launch_typed<float, false>(a, s, groups, lds, stream);
+                break;
+            case kBF16:
+                e = hard ? launch_typed<__bf16, true>(a, s, groups, lds, stream)
+                         : launch_typed<__bf16, false>(a, s, groups, lds, stream);
+                break;
+            default:
+                e = hard ? launch_typed<_Float16, true>(a, s, groups, lds, stream)
+                         : launch_typed<_Float16, false>(a, s, groups, lds, stream);
+        }
+        if (e != hipSuccess) return e;
+        a.logits = static_cast<const char *>(a.logits) + a.n * a.lds * size;
+        if (a.index) a.index += a.n * a.k;
+        if (a.teacher) a.teacher = static_cast<const char *>(a.teacher) + a.n * a.k * type_size(a.teacher_type);
+        if (a.rest) a.rest += a.n;
+        if (a.label) a.label += a.n;
+        if (a.dloss) a.dloss += a.n;
+        if (a.loss) a.loss += a.n;
+        if (a.dlogits) a.dlogits = static_cast<char *>(a.dlogits) + a.n * a.classes * size;
+    }
+    return hipSuccess;
+}
+
+}  // namespace som

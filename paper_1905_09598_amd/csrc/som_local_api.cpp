@@ -818,6 +818,38 @@ som_status som_norm_backward(const som_norm_call *c) {
                                               reinterpret_cast<hipStream_t>(c->stream)));
 }
 
+som_status som_distill(const som_distill_call *c) {
+    if (!c || !type_ok(c->type) || c->n < 0 || c->classes < 1 || c->lds < c->classes || c->k < 0 ||
+        c->k > som::kMaxTaught || !(c->temperature > 0.f) || isinf(c->temperature) ||
+        !(c->mix >= 0.f && c->mix <= 1.f) || !isfinite(c->scale))
+        return SOM_E_ARG;
+    if ((c->k && !type_ok(c->teacher_type)) || (!c->k && (c->index || c->teacher || c->rest)) ||
+        (!c->k && c->mix != 0.f) || (c->n && !c->label && c->mix != 1.f))
+        return SOM_E_ARG;
+    if (c->classes > som::kMaxClasses || c->n > (int64_t)1 << 40) return SOM_E_UNSUPPORTED;
+    const int size = som::type_size(c->type);
+    if (!rows_ok(c->logits, c->n, c->classes, c->lds, size) ||
+        !rows_ok_or_null(c->rest, 1, c->n, c->n, 4) || !rows_ok_or_null(c->label, 1, c->n, c->n, 4) ||
+        !rows_ok_or_null(c->dloss, 1, c->n, c->n, 4) || !rows_ok_or_null(c->loss, 1, c->n, c->n, 4) ||
+        !rows_ok_or_null(c->dlogits, c->n, c->classes, c->classes, size))
+        return SOM_E_ARG;
+    if (c->k && (!rows_ok(c->index, c->n, c->k, c->k, 4) ||
+                 !rows_ok(c->teacher, c->n, c->k, c->k, som::type_size(c->teacher_type))))
+        return SOM_E_ARG;
+    if (c->n == 0 || (!c->loss && !c->dlogits)) return SOM_OK;
+    som::DistillArgs a{};
+    a.type = c->type, a.teacher_type = c->teacher_type;
+    a.n = c->n, a.classes = c->classes;
+    a.k = c->mix == 0.f ? 0 : c->k;
+    a.logits = c->logits, a.lds = c->lds;
+    a.index = c->index, a.teacher = c->teacher, a.rest = c->rest;
+    a.label = c->label;
+    a.temperature = c->temperature, a.mix = c->mix;
+    a.dloss = c->dloss, a.scale = c->scale;
+    a.loss = c->loss, a.dlogits = c->dlogits;
+    return from_hip(som::launch_distill(a, reinterpret_cast<hipStream_t>(c->stream)));
+}
+
 static som_status route_ok(const som_route_call *c) {
     if (!c || !type_ok(c->type) || (c->gate != SOM_GATE_SOFTMAX && c->gate != SOM_GATE_SIGMOID))
         return SOM_E_ARG;

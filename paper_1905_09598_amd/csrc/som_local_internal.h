@@ -352,6 +352,27 @@ int32_t norm_parts(const NormArgs &a, int num_cus);   // a function of type, n a
 hipError_t launch_norm(const NormArgs &a, int num_cus, hipStream_t stream);
 hipError_t launch_norm_backward(const NormArgs &a, int num_cus, hipStream_t stream);
 
+// som_distill.hip; the fields are som_distill_call's.
+constexpr int kMaxClasses = 1 << 20, kMaxTaught = 64;
+struct DistillArgs {
+    int32_t type, teacher_type;
+    int64_t n;
+    int32_t classes, k;     // k = 0: no teacher
+    const void *logits;
+    int64_t lds;
+    const int32_t *index;
+    const void *teacher;
+    const float *rest;
+    const int32_t *label;
+    float temperature, mix;
+    const float *dloss;
+    float scale;
+    float *loss;
+    void *dlogits;
+    int32_t lanes, words;   // lanes of a row; words of a row's bits, one more than they take
+};
+hipError_t launch_distill(const DistillArgs &a, hipStream_t stream);
+
 ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus);
 // Parts of a row's dots: columns of one wave each.
 inline int32_t plan_dot_cols(const ProductPlan &p, int64_t n) {

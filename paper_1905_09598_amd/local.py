@@ -33,7 +33,7 @@ from . import SomError, _check, lib as _lib
 
 __all__ = [
     "ACTIVATIONS", "GATES", "EXPORTED", "SomError", "Routing", "ExpertsGradient", "AdamW", "linear",
-    "linear_backward", "norm", "norm_backward", "route", "route_backward", "dispatch", "experts", "experts_backward",
+    "linear_backward", "norm", "norm_backward", "route", "route_backward", "dispatch", "distill", "distill_backward", "experts", "experts_backward",
     "gate_from_map",
 ]
 
@@ -48,7 +48,7 @@ EXPORTED = (
     "som_experts_workspace", "som_experts_route", "som_experts", "som_experts_backward",
     "som_norm_workspace", "som_norm", "som_norm_backward",
     "som_route", "som_route_backward",
-    "som_dispatch_workspace", "som_dispatch", "som_adamw_room", "som_adamw_create",
+    "som_dispatch_workspace", "som_dispatch", "som_distill", "som_adamw_room", "som_adamw_create",
     "som_adamw_destroy", "som_adamw_step",
 )
 
@@ -110,6 +110,17 @@ class _RouteCall(C.Structure):
                 ("stream", C.c_void_p)]
 
 
+class _DistillCall(C.Structure):
+    """``som_distill_call`` of include/som_local.h."""
+
+    _fields_ = [("type", C.c_int32), ("teacher_type", C.c_int32), ("n", C.c_int64),
+                ("classes", C.c_int32), ("k", C.c_int32), ("logits", C.c_void_p),
+                ("lds", C.c_int64), ("index", C.c_void_p), ("teacher", C.c_void_p),
+                ("rest", C.c_void_p), ("label", C.c_void_p), ("temperature", C.c_float),
+                ("mix", C.c_float), ("dloss", C.c_void_p), ("scale", C.c_float),
+                ("loss", C.c_void_p), ("dlogits", C.c_void_p), ("stream", C.c_void_p)]
+
+
 class _AdamwTensor(C.Structure):
     """``som_adamw_tensor`` of include/som_local.h."""
 
@@ -142,6 +153,7 @@ def lib():
         "som_route_backward": [C.POINTER(_RouteCall)],
         "som_dispatch_workspace": [i64, i32, i32, C.POINTER(u64)],
         "som_dispatch": [vp, i64, i32, i32, vp, vp, vp, vp, u64, vp],
+        "som_distill": [C.POINTER(_DistillCall)],
         "som_adamw_create": [C.POINTER(_AdamwTensor), i32, i32, vp, vp, vp, vp, vp,
                              C.POINTER(vp)],
         "som_adamw_destroy": [vp],
@@ -576,6 +588,81 @@ def experts_backward(dy, x, routing: Routing, w1, b1, w2, b2, kept,
     call.dw1, call.db1, call.dw2, call.db2 = _ptr(d.w1), _ptr(d.b1), _ptr(d.w2), _ptr(d.b2)
     _run("experts", call, True, x)
     return d
+
+
+# ------------------------------------------------------------- distillation
+def _distill_call(logits, index, teacher, temperature, rest, label, mix, dloss):
+    code = _type(logits, "logits")
+    _rows(logits, "logits")
+    n, classes = logits.shape
+    if not classes:
+        raise ValueError("logits must have columns")
+    call = _DistillCall(type=code, n=n, classes=classes, logits=_ptr(logits), lds=_ld(logits),
+                        temperature=temperature, mix=mix, scale=1.0)
+    if (index is None) != (teacher is None):
+        raise ValueError("index and teacher come together")
+
+    def plain(t, dtype, shape, what):
+        if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda:
+            raise TypeError(f"{what} must be {str(dtype).removeprefix('torch.')} on the GPU")
+        _no_graph(t, what)
+        _shaped(t, logits, shape, what)
+        return _ptr(t)
+
+    if index is not None:
+        if index.dim() != 2:
+            raise ValueError("index must be (n, k)")
+        call.k = index.shape[1]
+        if not call.k:
+            raise ValueError("index must have columns")
+        call.index = plain(index, torch.int32, (n, call.k), "index")
+        call.teacher_type = _type(teacher, "teacher")
+        _shaped(teacher, logits, (n, call.k), "teacher")
+        call.teacher = _ptr(teacher)
+    if rest is not None:
+        call.rest = plain(rest, torch.float32, (n,), "rest")
+    if label is not None:
+        call.label = plain(label, torch.int32, (n,), "label")
+    if isinstance(dloss, torch.Tensor):
+        call.dloss = plain(dloss, torch.float32, (n,), "dloss")
+    elif dloss is not None:
+        call.scale = dloss
+    call.stream = _stream(logits)
+    return call
+
+
+def distill(logits, index=None, teacher=None, temperature: float = 1.0, rest=None, label=None,
+            mix: float = 1.0, dloss=None):
+    """The loss (n,) fp32 of logits (n, classes) by a teacher's logits ``teacher`` (n, k)
+    of the classes ``index`` (n, k) int32, -1 for absent, and by labels (n,) int32, -1 for
+    none: mix times the first, at the temperature, plus 1 - mix times the second.
+
+    rest (n,) fp32 is the teacher's probability of all classes that it does not name;
+    None: 0, its probabilities are shared among those it names.  mix has to be 0
+    without a teacher and 1 without labels.
+
+    With ``dloss``, the gradient of the rows' losses ((n,) fp32, or a number for all),
+    returns (loss, dlogits), both from one read of the logits."""
+    call = _distill_call(logits, index, teacher, temperature, rest, label, mix, dloss)
+    loss = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
+    call.loss = _ptr(loss)
+    dlogits = None
+    if dloss is not None:
+        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        call.dlogits = _ptr(dlogits)
+    _check(lib().som_distill(C.byref(call)), "som_distill")
+    return loss if dloss is None else (loss, dlogits)
+
+
+def distill_backward(dloss, logits, index=None, teacher=None, temperature: float = 1.0,
+                     rest=None, label=None, mix: float = 1.0):
+    """dlogits of ``distill`` from the gradient of the rows' losses ((n,) fp32, or a
+    number for all): for a loss whose gradient is known only later."""
+    call = _distill_call(logits, index, teacher, temperature, rest, label, mix, dloss)
+    dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    call.dlogits = _ptr(dlogits)
+    _check(lib().som_distill(C.byref(call)), "som_distill")
+    return dlogits
 
 
 def gate_from_map(weights, tau: float, dtype=torch.float32):

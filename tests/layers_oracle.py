@@ -85,3 +85,105 @@ class Norm:
         return {"dx": (dx, err + stored(dx, self.dtype)),
                 "dweight": (dw, dw_err + stored(dw, self.dtype)),
                 "dbias": (db, db_err + stored(db, self.dtype))}
+
+
+# ------------------------------------------------------------- distillation
+class Distill:
+    """loss (n,) and dlogits (n, classes) with their bounds.  index (n, k) with entries
+    outside [0, classes) absent, teacher (n, k) in 64 bits, rest, label may be None."""
+
+    def __init__(self, s, index, teacher, heat, rest, label, mix, dloss, dtype):
+        n, classes = s.shape
+        zero = torch.zeros(n, 1, dtype=torch.float64, device=s.device)
+        shut = ~(s > -math.inf).any(1, keepdim=True) & ~torch.isnan(s).any(1, keepdim=True)
+        top = s.max(1, keepdim=True).values
+        u = torch.where(shut, zero, (s - top) / heat)
+        e, self.loss_err = u.exp(), 0
+
+        def weighed(e, u):      # a sum of exponentials, and its relative error
+            z = e.sum(1, keepdim=True)
+            slack = (e * (u.abs().nan_to_num(posinf=0.0) * 4 + 8)).sum(1, keepdim=True) * V
+            return z, slack / torch.where(z > 0, z, z + 1) + (classes + 8) * V
+
+        z, dz = weighed(e, u)
+        a = e / z
+        da = (u.abs().nan_to_num(posinf=0.0) * 4 + 10) * V + dz
+        soft, soft_err = zero, zero
+        grad = torch.zeros_like(s)
+        grad_err = torch.zeros_like(s)
+        scale = dloss.unsqueeze(1)
+        if index is not None and mix != 0:
+            k = index.shape[1]
+            there = (index >= 0) & (index < classes)
+            at = index.long().clamp(0, classes - 1)
+            t = torch.where(there, teacher / heat, torch.full_like(teacher, -math.inf))
+            odd = torch.isnan(t).any(1, keepdim=True) | (t == math.inf).any(1, keepdim=True)
+            taught = (t > -math.inf).any(1, keepdim=True) | odd
+            best = torch.where(taught, t.max(1, keepdim=True).values, zero)
+            q = (t - best).exp()
+            total = q.sum(1, keepdim=True)
+            r = zero if rest is None else torch.where(taught, rest.unsqueeze(1).clamp(min=0), zero)
+            p = (1 - r) * q / torch.where(taught, total, total + 1)
+            dp = ((t - best).abs().nan_to_num(posinf=0.0) * 4 + k + 14) * V
+            dp = dp.max(1, keepdim=True).values + dp
+            live = there & (p != 0) | odd
+            ut = u.gather(1, at)
+            loga = ut - z.log()
+            dlog = (ut.abs().nan_to_num(posinf=0.0) * 6 + 4 * z.log().abs()) * V + dz
+            term = torch.where(live, p * (torch.where(live, p, p * 0 + 1).log() - loga), p * 0)
+            away = (p.clamp(min=1e-300).log().abs() + loga.abs().nan_to_num(posinf=0.0))
+            wobble = torch.where(live, p * (dp * (away + 1) + dlog + 4 * V * away), p * 0)
+            soft = term.sum(1, keepdim=True)
+            soft_err = wobble.sum(1, keepdim=True) + (k + 8) * V * term.abs().sum(1, keepdim=True)
+            member = torch.zeros(n, classes + 1, dtype=torch.bool, device=s.device)
+            member.scatter_(1, torch.where(there, at, classes), True)
+            member = member[:, :classes]
+            er = torch.where(member, zero, e)
+            zr, dzr = weighed(er, u)
+            has = r > 0
+            safe = torch.where(has, r, zero + 1)
+            left = safe * (safe.log() - (zr / z).log())
+            soft = soft + torch.where(has, left, zero)
+            soft_err = soft_err + torch.where(
+                has, safe * (dz + dzr + 8 * V * (safe.log().abs() + zr.log().abs() + z.log().abs())),
+                zero).nan_to_num(posinf=0.0)
+            soft = torch.where(taught, soft, zero)
+            soft = torch.where(odd, zero * math.nan, soft)
+            given = torch.zeros(n, classes + 1, dtype=torch.float64, device=s.device)
+            given.scatter_add_(1, torch.where(there, at, classes), torch.where(there, p, p * 0))
+            given = given[:, :classes]
+            ratio = torch.where(has & (zr > 0), r * z / torch.where(zr > 0, zr, zr + 1), zero)
+            g = torch.where(member, a - given, torch.where(a > 0, a * (1 - ratio), a))
+            ge = torch.where(member, a * da + given * (dp.max(1, keepdim=True).values + k * V),
+                             a * (da * (1 + ratio) + ratio * (dz + dzr + 6 * V)))
+            ge = ge + 6 * V * (a * (1 + ratio) + given)
+            g = torch.where(odd, g * math.nan, g)
+            grad = torch.where(taught, mix * heat * g, zero)
+            grad_err = torch.where(taught, mix * heat * ge, zero)
+        loss = mix * heat * heat * soft if mix != 0 else zero
+        loss_err = mix * heat * heat * (soft_err + 4 * V * soft.abs())
+        if label is not None and mix != 1:
+            known = ((label >= 0) & (label < classes)).unsqueeze(1)
+            which = label.long().clamp(0, classes - 1).unsqueeze(1)
+            u1 = torch.where(shut, zero, s - top)
+            e1 = u1.exp()
+            z1, dz1 = weighed(e1, u1)
+            a1 = e1 / z1
+            ul = u1.gather(1, which)
+            hard = z1.log() - ul
+            hard_err = dz1 + 6 * V * (z1.log().abs() + ul.abs().nan_to_num(posinf=0.0))
+            loss = loss + torch.where(known, (1 - mix) * hard, zero)
+            loss_err = loss_err + torch.where(known, (1 - mix) * hard_err, zero)
+            one = torch.zeros_like(s).scatter_(1, which, 1.0)
+            da1 = (u1.abs().nan_to_num(posinf=0.0) * 4 + 10) * V + dz1
+            grad = grad + torch.where(known, (1 - mix) * (a1 - one), zero)
+            grad_err = grad_err + torch.where(known, (1 - mix) * (a1 * da1 + 6 * V * (a1 + one)), zero)
+        loss = torch.where(shut, zero, loss).squeeze(1)
+        grad = torch.where(shut, zero, grad) * scale
+        grad_err = torch.where(shut, zero, grad_err) * scale.abs() + 8 * V * grad.abs()
+        # the loss is fp32: beyond its largest number, (2 - 2^-24) 2^127 with half a step, it
+        # rounds to infinity
+        loss = torch.where(loss >= (2 - 2.0 ** -24) * 2.0 ** 127, loss * math.inf, loss)
+        tiny = 2.0 ** -140      # sums and products next to fp32's least value
+        self.loss = (loss, (loss_err.squeeze(1) + 8 * V * loss.abs() + tiny).nan_to_num(posinf=0.0))
+        self.dlogits = (grad, (grad_err + stored(grad, dtype) + tiny).nan_to_num(posinf=0.0))

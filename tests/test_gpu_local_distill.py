@@ -1,0 +1,233 @@
+"""Distillation and its gradient against 64 bits: every element within a bound derived
+from the roundings (layers_oracle)."""
+import math
+
+import pytest
+import torch
+
+import layers_oracle as O
+import paper_1905_09598_amd as som
+from gpu_util import say, torch_cuda
+from paper_1905_09598_amd import local
+
+pytestmark = pytest.mark.gpu
+T = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+def _inputs(n, classes, k, dtype, seed=0, teacher=torch.float32):
+    g = torch.Generator().manual_seed(seed)
+    s = (2.5 * torch.randn(n, classes, generator=g)).to(dtype).cuda()
+    index = torch.stack([torch.randperm(max(classes, k), generator=g)[:k] for _ in range(min(n, 50))])
+    index = index.repeat(-(-n // 50), 1)[:n].int().cuda()      # beyond the classes: absent
+    t = (2 * torch.randn(n, k, generator=g)).to(teacher).cuda()
+    rest = (0.6 * torch.rand(n, generator=g)).cuda()
+    label = torch.randint(-1, classes + 1, (n,), generator=g).int().cuda()
+    dloss = (0.1 + torch.rand(n, generator=g)).cuda()
+    return s, index, t, rest, label, dloss
+
+
+def _check(s, index, t, heat, rest, label, mix, dloss):
+    loss, dlogits = local.distill(s, index, t, heat, rest, label, mix, dloss)
+    o = O.Distill(O.d(s), index, O.d(t), heat, O.d(rest), label, mix, O.d(dloss), s.dtype)
+    O.close(loss, o.loss, "loss")
+    O.close(dlogits, o.dlogits, "dlogits")
+    assert torch.equal(local.distill(s, index, t, heat, rest, label, mix).nan_to_num(), loss.nan_to_num())
+    back = local.distill_backward(dloss, s, index, t, heat, rest, label, mix)
+    assert torch.equal(back.nan_to_num(), dlogits.nan_to_num())
+    return loss, dlogits
+
+
+# rows of less than a piece, of a few lanes, of a wave, of a workgroup, at and past what
+# a workgroup holds (16-bit rows of 32,768 and 65,536, fp32 of 16,384 and 32,768)
+SIZES = [(1, 1, 1), (5, 2, 1), (70, 3, 2), (9, 7, 3), (200, 8, 2), (17, 9, 4), (33, 64, 8),
+         (100, 100, 4), (7, 257, 64), (20, 513, 3), (3, 1024, 5), (40, 1025, 8), (6, 4545, 16),
+         (3, 10000, 8), (2, 16385, 4), (2, 32768, 9), (2, 32769, 7), (2, 50001, 8), (2, 65536, 8),
+         (2, 65545, 30), (1, 200003, 32)]
+
+
+@pytest.mark.parametrize("dtype", T)
+@pytest.mark.parametrize("n,classes,k", SIZES)
+def test_rows_of_every_length(n, classes, k, dtype):
+    torch_cuda()
+    say("distill", n, classes, k, dtype)
+    s, index, t, rest, label, dloss = _inputs(n, classes, k, T[dtype], seed=n + classes)
+    _check(s, index, t, 2.0, rest, label, 0.6, dloss)
+    _check(s, index, t, 1.0, None, None, 1.0, dloss)
+
+
+@pytest.mark.parametrize("dtype", T)
+@pytest.mark.parametrize("classes", [6, 300, 2051])
+def test_parts_and_temperatures(classes, dtype):
+    s, index, t, rest, label, dloss = _inputs(60, classes, 5, T[dtype], seed=7, teacher=T[dtype])
+    for heat in (0.25, 1.5, 10.0):
+        for r in (None, rest):
+            _check(s, index, t, heat, r, label, 0.3, dloss)
+            _check(s, index, t, heat, r, None, 1.0, dloss)
+            _check(s, index, t, heat, r, label, 1.0, dloss)     # labels of no weight
+        _check(s, index, t, heat, rest, label, 0.0, dloss)      # a teacher of no weight
+    loss, dlogits = local.distill(s, label=label, mix=0.0, dloss=0.5)
+    o = O.Distill(O.d(s), None, None, 1.0, None, label, 0.0, torch.full_like(O.d(dloss), 0.5), s.dtype)
+    O.close(loss, o.loss, "loss")
+    O.close(dlogits, o.dlogits, "dlogits")
+
+
+@pytest.mark.parametrize("classes", [5, 130, 5000, 70001])
+def test_absent_repeated_and_closed_classes(classes):
+    s, index, t, rest, label, dloss = _inputs(40, classes, 6, torch.float32, seed=11)
+    label = label.clamp(0, classes - 1)
+    index[0], index[1, :3], index[2, 1:] = -1, -5, classes + 7
+    index[3] = index[3, 0]                       # one class, six times
+    index[4, 1], index[5, 2:4] = index[4, 0], index[5, 0]
+    t[6], t[7, 2] = -math.inf, -math.inf
+    s[8:16][torch.rand(8, classes, generator=torch.Generator().manual_seed(1)).cuda() < 0.5] = -math.inf
+    s[8:16, 0] = 1.0
+    s[16] = -math.inf                            # a row without an open class
+    s[17], s[18] = torch.finfo(torch.float32).min, -1e38
+    s[18, classes // 2] = 3e38
+    rest[19], rest[20], rest[21] = 0.0, 1.0, -1e-7
+    loss, dlogits = _check(s, index, t, 2.0, rest, label, 0.5, dloss)
+    assert float(loss[16]) == 0 and float(dlogits[16].abs().max()) == 0
+    loss, dlogits = _check(s, index, t, 1.0, None, None, 1.0, dloss)
+    assert float(loss[0]) == 0 and float(dlogits[0].abs().max()) == 0
+    assert float(loss[6]) == 0 and float(dlogits[6].abs().max()) == 0
+
+
+@pytest.mark.parametrize("classes", [6, 700, 80000])
+def test_the_rest_without_another_class(classes):
+    """All open classes are named: what is left for the others is lost (infinity)."""
+    s, _, t, rest, _, dloss = _inputs(4, classes, 3, torch.float32, seed=3)
+    index = torch.tensor([[0, 1, 2]] * 4, dtype=torch.int32, device="cuda")
+    s[:, 3:] = -math.inf
+    rest[1] = 0.0
+    loss, dlogits = _check(s, index, t, 1.0, rest, None, 1.0, dloss)
+    assert torch.isinf(loss).tolist() == [True, False, True, True]
+    assert torch.isfinite(dlogits).all() and float(dlogits[:, 3:].abs().max()) == 0
+
+
+@pytest.mark.parametrize("classes", [6, 700, 80000])
+def test_numbers_that_are_none(classes):
+    s, index, t, rest, label, dloss = _inputs(8, classes, 3, torch.float32, seed=4)
+    index = index.clamp(0, classes - 1)
+    s[1, classes - 1], s[2, 0], t[3, 1], t[4, 0] = math.nan, math.inf, math.nan, math.inf
+    s[5, 2], s[5, 3:] = math.nan, -math.inf
+    s[5, :2] = -math.inf
+    loss, dlogits = local.distill(s, index, t, 1.0, rest, label.clamp(0, classes - 1), 0.5, dloss)
+    bad = torch.tensor([False, True, True, True, True, True, False, False], device="cuda")
+    assert torch.equal(torch.isnan(loss), bad)
+    assert torch.equal(torch.isnan(dlogits).all(1), bad) and torch.equal(torch.isnan(dlogits).any(1), bad)
+
+
+def test_a_teacher_that_the_student_matches():
+    """Every class named, the same logits: loss and gradient are 0 to rounding."""
+    s = torch.randn(10, 50, generator=torch.Generator().manual_seed(1)).cuda()
+    index = torch.arange(50, dtype=torch.int32, device="cuda").expand(10, 50).contiguous()
+    loss, dlogits = local.distill(s, index, s.clone(), 3.0, dloss=1.0)
+    assert float(loss.abs().max()) < 9 * 50 * 2 ** -20 and float(dlogits.abs().max()) < 3 * 2 ** -18
+
+
+@pytest.mark.parametrize("classes", [7, 301, 4001, 66000])
+@pytest.mark.parametrize("offset,gap", [(0, 8), (1, 3), (5, 0)])
+def test_row_strides_and_odd_beginnings(classes, offset, gap):
+    s, index, t, rest, label, dloss = _inputs(6, classes, 4, torch.bfloat16, seed=2)
+    wide = torch.full((6, offset + classes + gap), float("nan"), dtype=s.dtype, device="cuda")
+    v = wide[:, offset:offset + classes]
+    v.copy_(s)
+    for u, w in zip(local.distill(v, index, t, 2.0, rest, label, 0.5, dloss),
+                    local.distill(s, index, t, 2.0, rest, label, 0.5, dloss)):
+        assert torch.equal(u, w)
+
+
+def test_rows_beyond_the_last_are_left_and_none_are_fine():
+    s, index, t, rest, label, dloss = _inputs(3, 40, 2, torch.float32, seed=5)
+    held = torch.full((8, 40), 7.0, device="cuda")
+    call = local._distill_call(s, index, t, 1.0, rest, label, 0.5, dloss)
+    loss = torch.full((8,), 7.0, device="cuda")
+    call.loss, call.dlogits = loss.data_ptr(), held.data_ptr()
+    som._check(local.lib().som_distill(local.C.byref(call)), "som_distill")
+    assert torch.equal(held[3:], torch.full_like(held[3:], 7.0)) and float(loss[3:].min()) == 7
+    loss, dlogits = local.distill(s[:0], index[:0], t[:0], 1.0, rest[:0], label[:0], 0.5, dloss[:0])
+    assert loss.shape == (0,) and dlogits.shape == (0, 40)
+
+
+def test_many_rows_and_offsets_beyond_32_bits():
+    s, index, t, rest, label, dloss = _inputs(100001, 12, 3, torch.bfloat16, seed=9)
+    _check(s, index, t, 1.0, rest, label, 0.5, dloss)
+    wide = torch.empty((1 << 31) + 4096, dtype=torch.bfloat16, device="cuda")
+    v = torch.as_strided(wide, (3, 900), (1 << 30, 1))
+    s, index, t, rest, label, dloss = _inputs(3, 900, 3, torch.bfloat16, seed=9)
+    v.copy_(s)
+    for u, w in zip(local.distill(v, index, t, 2.0, rest, label, 0.5, dloss),
+                    local.distill(s, index, t, 2.0, rest, label, 0.5, dloss)):
+        assert torch.equal(u, w)
+
+
+def test_from_a_routing():
+    """A map's nearest units teach a gate: the routing's index, its scores and its rest."""
+    g = torch.Generator().manual_seed(6)
+    scores, s = (torch.randn(200, 64, generator=g).cuda() for _ in range(2))
+    r = local.route(scores, 4, renormalise=False)
+    t = scores.gather(1, r.index.long())
+    rest = (1 - r.weight.sum(1)).clamp(min=0)
+    loss, dlogits = _check(s, r.index, t, 1.0, rest, None, 1.0, torch.ones(200, device="cuda"))
+    # at the same scores the gate is right
+    loss, dlogits = local.distill(scores, r.index, t, 1.0, rest, dloss=1.0)
+    assert float(dlogits.abs().max()) < 2 ** -20 and float(loss.abs().max()) < 2 ** -18
+
+
+def test_streams_graphs_and_repeats():
+    s, index, t, rest, label, dloss = _inputs(300, 3000, 8, torch.bfloat16, seed=1)
+
+    def once():
+        return local.distill(s, index, t, 2.0, rest, label, 0.5, dloss)
+
+    want = once()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = once()
+    side.synchronize()
+    for u, v in zip(want, got):
+        assert torch.equal(u, v)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = once()
+    for seed in (5, 6, 7):
+        s.copy_(_inputs(300, 3000, 8, torch.bfloat16, seed=seed)[0])
+        graph.replay()
+        torch.cuda.synchronize()
+        for u, v in zip(held, once()):
+            assert torch.equal(u, v)
+
+
+def test_refusals():
+    s, index, t, rest, label, dloss = _inputs(4, 16, 2, torch.float32)
+    bad = [
+        (TypeError, lambda: local.distill(s.double(), index, t)),
+        (TypeError, lambda: local.distill(s.cpu(), index, t)),
+        (ValueError, lambda: local.distill(s[0], index, t)),
+        (ValueError, lambda: local.distill(s[:, :0], index, t)),
+        (ValueError, lambda: local.distill(s, index)), (ValueError, lambda: local.distill(s, None, t)),
+        (TypeError, lambda: local.distill(s, index.long(), t)),
+        (ValueError, lambda: local.distill(s, index[:3], t)),
+        (ValueError, lambda: local.distill(s, index[:, :0], t[:, :0])),
+        (ValueError, lambda: local.distill(s, index, t[:, :1])),
+        (TypeError, lambda: local.distill(s, index, t.double())),
+        (TypeError, lambda: local.distill(s, index, t, rest=rest.double())),
+        (ValueError, lambda: local.distill(s, index, t, rest=rest[:2])),
+        (TypeError, lambda: local.distill(s, index, t, label=label.long(), mix=0.5)),
+        (TypeError, lambda: local.distill(s, index, t, dloss=dloss.double())),
+        (ValueError, lambda: local.distill(s, index, t, dloss=dloss[:1])),
+        (ValueError, lambda: local.distill(s.clone().requires_grad_(), index, t)),
+        (som.SomError, lambda: local.distill(s, index, t, temperature=0.0)),
+        (som.SomError, lambda: local.distill(s, index, t, temperature=-1.0)),
+        (som.SomError, lambda: local.distill(s, index, t, temperature=math.nan)),
+        (som.SomError, lambda: local.distill(s, index, t, label=label, mix=1.5)),
+        (som.SomError, lambda: local.distill(s, index, t, mix=0.5)),
+        (som.SomError, lambda: local.distill(s, label=label, mix=0.5)),
+        (som.SomError, lambda: local.distill(s, index, t, dloss=math.inf)),
+        (som.SomError, lambda: local.distill(s.new_zeros(4, 200), torch.zeros(
+            4, 65, dtype=torch.int32, device="cuda"), torch.zeros(4, 65, device="cuda"))),
+    ]
+    for error, call in bad:
+        with pytest.raises(error):
+            call()

@@ -1,0 +1,83 @@
+"""The 64-bit formulas that the layers' kernels are held to: their gradients against
+differences of their values (on the CPU)."""
+import math
+
+import pytest
+import torch
+
+import layers_oracle as O
+
+F64 = torch.float64
+
+
+def _slopes(f, x, step=1e-6):
+    """Central differences of f's scalar at x, element by element."""
+    out = torch.zeros_like(x)
+    flat, to = x.view(-1), out.view(-1)
+    for i in range(flat.numel()):
+        was = float(flat[i])
+        flat[i] = was + step
+        up = float(f())
+        flat[i] = was - step
+        to[i] = (up - float(f())) / (2 * step)
+        flat[i] = was
+    return out
+
+
+def _near(a, b, what):
+    assert torch.allclose(a, b, rtol=2e-6, atol=2e-8), (what, float((a - b).abs().max()))
+
+
+def test_layer_norm():
+    g = torch.Generator().manual_seed(1)
+    x, dy = torch.randn(3, 7, generator=g, dtype=F64), torch.randn(3, 7, generator=g, dtype=F64)
+    w, b = torch.randn(7, generator=g, dtype=F64), torch.randn(7, generator=g, dtype=F64)
+    beside = torch.randn(3, 7, generator=g, dtype=F64)
+
+    def value():
+        return (O.Norm(x, w, b, 1e-3, torch.float32).y[0] * dy).sum() + (x * beside).sum()
+
+    got = O.Norm(x, w, b, 1e-3, torch.float32).backward(dy, beside)
+    for name, t in (("dx", x), ("dweight", w), ("dbias", b)):
+        _near(got[name][0], _slopes(value, t), name)
+
+
+@pytest.mark.parametrize("rest,mix,heat", [(False, 1.0, 1.0), (True, 1.0, 2.0), (True, 0.4, 1.5),
+                                           (False, 0.0, 3.0)])
+def test_distillation(rest, mix, heat):
+    g = torch.Generator().manual_seed(2)
+    n, classes = 5, 9
+    s = torch.randn(n, classes, generator=g, dtype=F64)
+    index = torch.tensor([[1, 4, 7], [0, -1, 8], [2, 2, 3], [-1, -1, -1], [9, 5, 6]], dtype=torch.int32)
+    teacher = torch.randn(n, 3, generator=g, dtype=F64)
+    left = torch.tensor([0.2, 0.0, 0.5, 0.3, 0.9], dtype=F64) if rest else None
+    label = torch.tensor([3, -1, 2, 8, 9], dtype=torch.int32)
+    dloss = torch.rand(n, generator=g, dtype=F64) + 0.5
+
+    def of():
+        return O.Distill(s, index, teacher, heat, left, label, mix, dloss, torch.float32)
+
+    _near(of().dlogits[0], _slopes(lambda: (of().loss[0] * dloss).sum(), s), "dlogits")
+
+
+def test_distillation_from_the_whole_teacher_is_a_divergence():
+    """With every class named, loss = T² KL(teacher, student); its least value is 0."""
+    g = torch.Generator().manual_seed(3)
+    s, t = torch.randn(4, 6, generator=g, dtype=F64), torch.randn(4, 6, generator=g, dtype=F64)
+    index = torch.arange(6, dtype=torch.int32).expand(4, 6).contiguous()
+    one = torch.ones(4, dtype=F64)
+    o = O.Distill(s, index, t, 2.0, None, None, 1.0, one, torch.float32)
+    p = (t / 2).softmax(1)
+    _near(o.loss[0], 4 * (p * (p.log() - (s / 2).log_softmax(1))).sum(1), "loss")
+    same = O.Distill(s, index, s, 2.0, None, None, 1.0, one, torch.float32)
+    assert float(same.loss[0].abs().max()) < 1e-14 and float(same.dlogits[0].abs().max()) < 1e-14
+
+
+def test_distillation_of_closed_classes():
+    s = torch.tensor([[0.0, -math.inf, 1.0], [-math.inf] * 3], dtype=F64)
+    index = torch.tensor([[0], [1]], dtype=torch.int32)
+    o = O.Distill(s, index, torch.zeros(2, 1, dtype=F64), 1.0, None, None, 1.0,
+                  torch.ones(2, dtype=F64), torch.float32)
+    a = math.e / (1 + math.e)
+    _near(o.dlogits[0], torch.tensor([[-a, 0.0, a], [0.0, 0.0, 0.0]], dtype=F64), "dlogits")
+    _near(o.loss[0], torch.tensor([-math.log(1 - a), 0.0], dtype=F64), "loss")
