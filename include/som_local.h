@@ -99,6 +99,40 @@ som_status som_linear_route(const som_linear_call *call, int32_t backward, int32
 som_status som_linear(const som_linear_call *call);
 som_status som_linear_backward(const som_linear_call *call);
 
+/* A gated layer, of x (n x inner) and two matrices w (2 x hidden x inner) at once:
+ *     [u v] = x w^T + bias,    y = act(u) v         (each n x hidden)
+ * For a gradient, forward has to keep z = [u v], n x 2 hidden in fp32 whatever the type:
+ * rounded to 16 bits its errors would reach all of the gradient.  From dy,
+ *     dz = [ dy v act'(u)   dy act(u) ]
+ *     dx = dz w    dw = dz^T x    dbias = sum of dz's rows
+ * dz is held in the element type for the two products, not for dbias. */
+typedef struct som_gated_call {
+    int32_t type;              /* som_type of all matrices but z                     */
+    int32_t activation;        /* som_activation                                     */
+    int64_t n;                 /* rows (documents); 0 is allowed                     */
+    int32_t inner;             /* 1 .. 4,000,000                                     */
+    int32_t hidden;            /* 1 .. 2,000,000                                     */
+    const void *x;
+    int64_t ldx;               /* elements from row to row, >= inner                 */
+    const void *w;             /* packed 2 x hidden x inner                          */
+    const void *bias;          /* 2 x hidden; NULL for none                          */
+    void *y;                   /* packed, forward's result                           */
+    float *z;                  /* packed; forward writes it unless NULL, backward
+                                  reads it                                           */
+    const void *dy;            /* backward                                           */
+    int64_t lddy;              /* >= hidden                                          */
+    void *dx, *dw, *dbias;     /* packed; each NULL if not wanted                    */
+    void *workspace;
+    uint64_t workspace_bytes;
+    void *stream;
+} som_gated_call;
+
+/* As som_linear's; som_gated_route's tiles hold half as many columns of each matrix. */
+som_status som_gated_workspace(const som_gated_call *call, int32_t backward, uint64_t *bytes);
+som_status som_gated_route(const som_gated_call *call, int32_t backward, int32_t tiles[2]);
+som_status som_gated(const som_gated_call *call);
+som_status som_gated_backward(const som_gated_call *call);
+
 /* The experts' answers to the documents x (n x inner) that are routed to them,
  * joined: for document i with experts e = index[i][j] and weights g = weight[i][j],
  *     z = w1_e x_i + b1_e,   h = act(z),   answer = w2_e h + b2_e,

@@ -1,0 +1,94 @@
+// The pass between the gradient of a gated layer y = act(u) v and the products for its
+// input's and its matrices' gradients:
+//     dz = [ dy v act'(u)    dy act(u) ]
+// and the sums of dz's columns, from fp32 u and v as forward kept them (in 16 bits their
+// roundings would reach all of the gradient: errors of 1.8 times one rounding, 1.4 as it
+// is).  Bound by memory: 2 reads of 4 bytes, one of dy, two writes to each.  A thread
+// keeps to its columns, 16 bytes of dy, and goes down a group of rows with the sums of
+// its columns in registers; the groups' sums are joined in order (som_norm.hip).  dz is
+// rounded to the element type for the matrix instructions, the sums are of dz before that.
+#include "som_local_internal.h"
+
+#include <algorithm>
+
+namespace som {
+namespace {
+
+constexpr int kThreads = 256;
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void gated_slopes_kernel(GatedArgs a) {
+    constexpr int N = 16 / sizeof(T), kAhead = 2;   // rows whose reads are under way together
+    const int64_t col = ((int64_t)blockIdx.y * kThreads + threadIdx.x) * N;
+    if (col >= a.hidden) return;
+    const int left = (int)(a.hidden - col < N ? a.hidden - col : N);
+    float sum[2][N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) sum[0][e] = sum[1][e] = 0.f;
+    for (int64_t r0 = blockIdx.x; r0 < a.n; r0 += (int64_t)gridDim.x * kAhead) {
+        Piece<T, N> dy[kAhead];
+        Piece<float, N> z[kAhead][2];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            const int64_t r = r0 + (int64_t)q * gridDim.x;
+            const int some = r < a.n ? left : 0;
+            dy[q].read(static_cast<const T *>(a.dy) + r * a.lddy + col, some);
+            z[q][0].read(a.z + r * 2 * a.hidden + col, some);
+            z[q][1].read(a.z + (r * 2 + 1) * a.hidden + col, some);
+        }
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            const int64_t r = r0 + (int64_t)q * gridDim.x;
+            if (r >= a.n) break;
+            Piece<T, N> out[2];
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                float slope;
+                const float act = activate(z[q][0].v[e], a.activation, &slope);
+                const float d = (float)dy[q].v[e], du = d * z[q][1].v[e] * slope, dv = d * act;
+                sum[0][e] += du;
+                sum[1][e] += dv;
+                out[0].v[e] = (T)du;
+                out[1].v[e] = (T)dv;
+            }
+            T *const to = static_cast<T *>(a.dz) + r * a.ldd + col;
+            out[0].write(to, left);
+            out[1].write(to + a.hidden, left);
+            if (col + N >= a.hidden)        // the last of the row: its filling
+                for (int64_t c = 2 * a.hidden; c < a.ldd; ++c)
+                    static_cast<T *>(a.dz)[r * a.ldd + c] = (T)0.f;
+        }
+    }
+    if (!a.partial) return;
+    float *const to = a.partial + (int64_t)blockIdx.x * 2 * a.hidden + col;
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        if (e < left) {
+            to[e] = sum[0][e];
+            to[a.hidden + e] = sum[1][e];
+        }
+}
+
+int64_t wide_of(const GatedArgs &a) {
+    return (a.hidden * type_size(a.type) + 16 * kThreads - 1) / (16 * kThreads);
+}
+
+}  // namespace
+
+// Groups of rows: eight workgroups to a compute unit, of eight rows or more.
+int32_t gated_parts(const GatedArgs &a, int num_cus) {
+    const int64_t most = std::max<int64_t>(1, (int64_t)num_cus * 8 / wide_of(a));
+    return (int32_t)std::max<int64_t>(1, std::min(most, (a.n + 7) / 8));
+}
+
+hipError_t launch_gated_slopes(const GatedArgs &a, hipStream_t stream) {
+    const dim3 grid((unsigned)a.parts, (unsigned)wide_of(a));
+    switch (a.type) {
+        case kF32: gated_slopes_kernel<float><<<grid, kThreads, 0, stream>>>(a); break;
+        case kBF16: gated_slopes_kernel<__bf16><<<grid, kThreads, 0, stream>>>(a); break;
+        default: gated_slopes_kernel<_Float16><<<grid, kThreads, 0, stream>>>(a); break;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace som

@@ -23,7 +23,10 @@ ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus) {
     best.aligned = aligned;
     const int64_t experts = a.offsets ? a.experts : 1;
     const int64_t slab = 128 / type_size(a.type);
-    if (a.mode == kForward && a.m <= 16 * experts) {
+    const bool along = a.mode == kForward || a.mode == kPair;
+    // a gated layer's tiles hold the same columns of two matrices
+    const int64_t columns = a.mode == kPair ? 2 * a.n : a.n;
+    if (along && a.m <= 16 * experts) {
         best.tile = 16;
         const int64_t groups = (a.n + 15) / 16 * std::min(a.m, a.m / best.tile + experts);
         // as few waves to a workgroup as keep the chip's loads in flight (16 waves of
@@ -51,7 +54,7 @@ ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus) {
     for (const Shape &s : shapes) {
         if (!aligned && s.tile == 256) continue;
         const Cost &cost = a.type == kF32 ? s.single : s.half;
-        const int64_t tn = (a.n + s.tile - 1) / s.tile;
+        const int64_t tn = (columns + s.tile - 1) / s.tile;
         int64_t tm, k = a.k;
         if (a.mode == kWeight) {
             tm = (a.m + s.tile - 1) / s.tile * experts;
@@ -342,6 +345,93 @@ struct LinearBackward {
                         [&] { return has_input ? run(input, s) : hipSuccess; },
                         [&] { return has_weight ? run(weight, s) : hipSuccess; },
                         [&] { return sums.out ? som::launch_sums(sums, s) : hipSuccess; });
+    }
+};
+
+struct GatedForward {
+    SideRows x, w;
+    Product product;
+    GatedForward(const som_gated_call &c, Carver &work) {
+        ProductArgs &a = product.a;
+        a.mode = som::kPair;
+        a.type = c.type;
+        a.activation = c.activation;
+        a.m = c.n, a.n = c.hidden, a.k = c.inner;
+        a.bias = c.bias;
+        a.y = c.y, a.z = c.z;
+        x = side(c.x, c.n, c.inner, c.ldx);
+        w = side(c.w, 2 * (int64_t)c.hidden, c.inner, c.inner);
+        product.place(work, x, w);
+    }
+    void route(int32_t *tiles) const { tiles[0] = tile_of(product); }
+    hipError_t enqueue(hipStream_t s) const {
+        return in_order([&] { return run_copy(x, s); }, [&] { return run_copy(w, s); },
+                        [&] { return run(product, s); });
+    }
+};
+
+// dz of both matrices side by side, n x 2 hidden, then the products of one layer of
+// 2 hidden rows.
+struct GatedBackward {
+    SideRows x, w, dz;
+    Product input, weight;
+    som::GatedArgs slopes{};
+    void *dbias;
+    bool has_input, has_weight, has_rows;
+    GatedBackward(const som_gated_call &c, Carver &work) {
+        const int size = som::type_size(c.type);
+        const int64_t both = 2 * (int64_t)c.hidden;
+        has_rows = c.n != 0;
+        has_input = c.dx != nullptr && c.n;
+        has_weight = c.dw != nullptr;
+        dbias = c.dbias;
+        slopes.type = c.type, slopes.activation = c.activation;
+        slopes.n = c.n, slopes.hidden = c.hidden;
+        slopes.dy = c.dy, slopes.lddy = c.lddy;
+        slopes.z = c.z;
+        slopes.ldd = rounded(both, 16 / size);
+        dz = side(work.take((uint64_t)c.n * slopes.ldd * size), c.n, both, slopes.ldd);
+        dz.copied = true;   // in whole pieces
+        slopes.dz = const_cast<void *>(dz.p);
+        slopes.parts = som::gated_parts(slopes, compute_units());
+        if (c.dbias) slopes.partial = work.take<float>((uint64_t)slopes.parts * both * 4);
+        if (has_input) {
+            ProductArgs &a = input.a;
+            a.mode = som::kInput;
+            a.type = c.type;
+            a.m = c.n, a.n = c.inner, a.k = both;
+            a.y = c.dx;
+            w = side(c.w, both, c.inner, c.inner);
+            input.place(work, dz, w);
+        }
+        if (has_weight) {
+            ProductArgs &a = weight.a;
+            a.mode = som::kWeight;
+            a.type = c.type;
+            a.m = both, a.n = c.inner, a.k = c.n;
+            a.y = c.dw;
+            x = side(c.x, c.n, c.inner, c.ldx);
+            weight.place(work, dz, x);
+        }
+    }
+    void route(int32_t *tiles) const {
+        tiles[0] = tile_of(input, has_input), tiles[1] = tile_of(weight, has_weight);
+    }
+    hipError_t enqueue(hipStream_t s) const {
+        const auto copy = [&](const SideRows &r) { return has_rows ? run_copy(r, s) : hipSuccess; };
+        return in_order([&] { return som::launch_gated_slopes(slopes, s); },
+                        [&] { return copy(w); }, [&] { return copy(x); },
+                        [&] { return has_input ? run(input, s) : hipSuccess; },
+                        [&] { return has_weight ? run(weight, s) : hipSuccess; },
+                        [&] {
+                            return dbias ? som::launch_join_parts(
+                                               slopes.type, slopes.partial, slopes.parts, slopes.hidden,
+                                               dbias,
+                                               static_cast<char *>(dbias) +
+                                                   slopes.hidden * som::type_size(slopes.type),
+                                               s)
+                                         : hipSuccess;
+                        });
     }
 };
 
@@ -693,6 +783,61 @@ som_status som_linear_backward(const som_linear_call *c) {
         !rows_ok_or_null(c->dbias, 1, c->outer, c->outer, size))
         return SOM_E_ARG;
     return enqueue<LinearBackward>(*c);
+}
+
+static som_status gated_sizes_ok(const som_gated_call *c) {
+    if (!c || !type_ok(c->type) || !activation_ok(c->activation) || c->n < 0 || c->inner <= 0 ||
+        c->hidden <= 0 || c->ldx < c->inner)
+        return SOM_E_ARG;
+    if (c->inner > som::kMaxWidth || c->hidden > som::kMaxWidth / 2 || c->n > (int64_t)1 << 40)
+        return SOM_E_UNSUPPORTED;
+    return SOM_OK;
+}
+
+static bool gated_common_ok(const som_gated_call &c) {
+    const int size = som::type_size(c.type);
+    return rows_ok(c.w, 2 * (int64_t)c.hidden, c.inner, c.inner, size) &&
+           rows_ok(c.x, c.n, c.inner, c.ldx, size);
+}
+
+som_status som_gated_workspace(const som_gated_call *c, int32_t backward, uint64_t *bytes) {
+    if (!bytes) return SOM_E_ARG;
+    const som_status st = gated_sizes_ok(c);
+    if (st == SOM_OK)
+        *bytes = c->n || backward ? workspace<GatedForward, GatedBackward>(*c, backward) : 0;
+    return st;
+}
+
+som_status som_gated_route(const som_gated_call *c, int32_t backward, int32_t tiles[2]) {
+    if (!tiles) return SOM_E_ARG;
+    const som_status st = gated_sizes_ok(c);
+    if (st == SOM_OK) route<GatedForward, GatedBackward>(*c, backward, tiles, 2);
+    return st;
+}
+
+som_status som_gated(const som_gated_call *c) {
+    const som_status st = gated_sizes_ok(c);
+    if (st != SOM_OK) return st;
+    const int64_t both = 2 * (int64_t)c->hidden;
+    const int size = som::type_size(c->type);
+    if (!gated_common_ok(*c) || !rows_ok(c->y, c->n, c->hidden, c->hidden, size) ||
+        !rows_ok_or_null(c->z, c->n, both, both, 4) || !rows_ok_or_null(c->bias, 1, both, both, size))
+        return SOM_E_ARG;
+    return c->n ? enqueue<GatedForward>(*c) : SOM_OK;
+}
+
+som_status som_gated_backward(const som_gated_call *c) {
+    const som_status st = gated_sizes_ok(c);
+    if (st != SOM_OK) return st;
+    const int64_t both = 2 * (int64_t)c->hidden;
+    const int size = som::type_size(c->type);
+    if (!gated_common_ok(*c) || !rows_ok(c->dy, c->n, c->hidden, c->lddy, size) ||
+        !rows_ok(c->z, c->n, both, both, 4) ||
+        !rows_ok_or_null(c->dx, c->n, c->inner, c->inner, size) ||
+        !rows_ok_or_null(c->dw, both, c->inner, c->inner, size) ||
+        !rows_ok_or_null(c->dbias, 1, both, both, size))
+        return SOM_E_ARG;
+    return enqueue<GatedBackward>(*c);
 }
 
 som_status som_experts_workspace(const som_experts_call *c, int32_t backward, uint64_t *bytes) {

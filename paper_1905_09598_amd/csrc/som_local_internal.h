@@ -9,7 +9,7 @@ namespace som {
 
 enum : int32_t { kF32 = 0, kBF16 = 1, kF16 = 2 };                       // som_type
 enum : int32_t { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };  // som_activation
-enum : int32_t { kForward = 0, kInput = 1, kWeight = 2, kGate = 3 };    // which product
+enum : int32_t { kForward = 0, kInput = 1, kWeight = 2, kGate = 3, kPair = 4 };  // which product
 
 inline int type_size(int32_t type) { return type == kF32 ? 4 : 2; }
 
@@ -158,6 +158,8 @@ __device__ inline int gate_exponent(float g) {
 //   gate     A = dout (m x k), B = w (k x n):   y = gate C act'(argument),
 //                                               dots: parts of <C, act(argument)>
 //   weight   A = dz (k x m), B = x (k x n):     y = C
+//   pair     A = x (m x k), B = w (2 n x k):      z = C + bias in fp32 (m x 2 n),
+//                                               y = act(z's first n) times its others
 // Routed (offsets): the m rows of forward, input and gate lie by expert, offsets[e]
 // .. of B + e batch_b; weight sums offsets[e] .. into y + e m n.  Rows past
 // offsets[experts] are not touched.  list: row r of A (forward, gate) or row s of B
@@ -372,6 +374,27 @@ struct DistillArgs {
     int32_t lanes, words;   // lanes of a row; words of a row's bits, one more than they take
 };
 hipError_t launch_distill(const DistillArgs &a, hipStream_t stream);
+
+// Sums of parts (parts x 2 x width, in order) to two rows of width, each NULL if not
+// wanted (som_norm.hip).
+hipError_t launch_join_parts(int32_t type, const float *partial, int32_t parts, int64_t width,
+                             void *first, void *second, hipStream_t stream);
+
+// som_gated.hip: dz (rows of ldd >= 2 hidden, filled up with zeros) of a gated layer from
+// dy and z, and the parts of its columns' sums (parts x 2 hidden, or NULL).
+struct GatedArgs {
+    int32_t type, activation;
+    int64_t n, hidden;
+    const void *dy;
+    int64_t lddy;
+    const float *z;
+    void *dz;
+    int64_t ldd;
+    float *partial;
+    int32_t parts;
+};
+int32_t gated_parts(const GatedArgs &a, int num_cus);   // a function of type, n and hidden
+hipError_t launch_gated_slopes(const GatedArgs &a, hipStream_t stream);
 
 ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus);
 // Parts of a row's dots: columns of one wave each.

@@ -7,7 +7,7 @@
 // between the statistics and what they are for; rows of up to a wave's pieces are taken
 // by 1 to 64 lanes, longer ones by a workgroup, and only rows beyond what a workgroup
 // holds are read again.  A workgroup takes rows in turn with the weight in registers;
-// backward adds up its columns' parts of dweight and dbias there, and norm_join_kernel
+// backward adds up its columns' parts of dweight and dbias there, and join_parts_kernel
 // adds up the workgroups' in order (no atomics: a result does not depend on timing).
 #include "som_row.h"
 
@@ -317,26 +317,24 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a) {
         }
 }
 
-// dweight and dbias from their parts, in order: 32 columns of both, eight lanes each.
+// Two rows of `width` from their parts, in order: 32 columns of both, eight lanes each.
 template <typename T>
-__global__ __launch_bounds__(256) void norm_join_kernel(NormArgs a) {
+__global__ __launch_bounds__(256) void join_parts_kernel(const float *partial, int32_t parts,
+                                                         int64_t width, T *first, T *second) {
     __shared__ float part[8][32];
     const int c = threadIdx.x & 31, lane = threadIdx.x >> 5;
     const int64_t col = (int64_t)blockIdx.x * 32 + c;
     float v = 0.f;
-    if (col < 2 * a.width) {
+    if (col < 2 * width) {
 #pragma unroll 4
-        for (int p = lane; p < a.parts; p += 8) v += a.partial[p * 2 * a.width + col];
+        for (int p = lane; p < parts; p += 8) v += partial[p * 2 * width + col];
     }
     part[lane][c] = v;
     __syncthreads();
-    if (lane == 0 && col < 2 * a.width) {
+    if (lane == 0 && col < 2 * width) {
         for (int l = 1; l < 8; ++l) v += part[l][c];
-        if (col < a.width) {
-            if (a.dweight) static_cast<T *>(a.dweight)[col] = (T)v;
-        } else if (a.dbias) {
-            static_cast<T *>(a.dbias)[col - a.width] = (T)v;
-        }
+        T *const to = col < width ? first : second;
+        if (to) to[col < width ? col : col - width] = (T)v;
     }
 }
 
@@ -370,6 +368,15 @@ int32_t norm_parts(const NormArgs &a, int num_cus) {
     const int64_t groups = s.held ? std::min(groups_of(a, s, num_cus), (a.n + 4 * rows - 1) / (4 * rows))
                                   : std::min<int64_t>((a.n + 15) / 16, num_cus);
     return (int32_t)std::max<int64_t>(1, groups);
+}
+
+hipError_t launch_join_parts(int32_t type, const float *partial, int32_t parts, int64_t width,
+                             void *first, void *second, hipStream_t stream) {
+    return by_type(type, [&](auto t) {
+        using T = decltype(t);
+        join_parts_kernel<T><<<(unsigned)((2 * width + 31) / 32), 256, 0, stream>>>(
+            partial, parts, width, static_cast<T *>(first), static_cast<T *>(second));
+    });
 }
 
 hipError_t launch_norm(const NormArgs &args, int num_cus, hipStream_t stream) {
@@ -423,7 +430,7 @@ hipError_t launch_norm_backward(const NormArgs &args, int num_cus, hipStream_t s
                 norm_columns_kernel<T><<<dim3(groups, (unsigned)wide), 256, 0, stream>>>(a);
         }
         if (columns)
-            norm_join_kernel<T><<<(unsigned)((2 * a.width + 31) / 32), 256, 0, stream>>>(a);
+            (void)launch_join_parts(a.type, a.partial, a.parts, a.width, a.dweight, a.dbias, stream);
     });
 }
 

@@ -140,6 +140,23 @@ struct Side {
         }
     }
 
+    // along, of the two matrices of a pair (`rows` rows each, one behind the other): a
+    // wave's columns of the tile are, by halves, the same columns of the one and of the
+    // other (product_kernel), which takes as many rows as a wave here loads.
+    __device__ void begin_pair(const T *p, int64_t ld, int64_t row0, int64_t rows, int64_t k0) {
+        constexpr int kHalf = ROWS / WAVES;
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        base = reinterpret_cast<const char *>(p + ((wave & 1) * rows + row0) * ld + k0);
+        step = 128;
+        easy = true;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int64_t r = (wave >> 1) * kHalf + (place(j) >> 3) % kHalf;
+            const int64_t row = row0 + r < rows ? r : rows - 1 - row0;
+            off[j] = (uint32_t)((row * ld + index(j)) * (int64_t)sizeof(T));
+        }
+    }
+
     // Load the next slab, with DMA into `lds`.  CHECK: `left` contraction indices are
     // left, the rest are zeros.  across: columns col0 .. of `cols`.
     template <bool CHECK>
@@ -436,6 +453,44 @@ struct Epilogue {
     }
 };
 
+// The same for the two sums of a gated layer's element: u of the first matrix and v of
+// the second, with their biases, kept in fp32, give act(u) v.
+template <typename T, int N>
+struct PairEpilogue {
+    const ProductArgs &a;
+    int64_t col;
+    int left;
+    float bias[2][N];
+    __device__ PairEpilogue(const ProductArgs &args, int64_t c) : a(args), col(c) {
+        left = (int)(a.n - col < N ? a.n - col : N);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            Piece<T, N> p;
+            p.read(static_cast<const T *>(a.bias) + h * a.n + col, a.bias ? left : 0);
+#pragma unroll
+            for (int e = 0; e < N; ++e) bias[h][e] = (float)p.v[e];
+        }
+    }
+    __device__ void write(int64_t row, float (&u)[N], float (&v)[N]) const {
+        Piece<float, N> kept[2];
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            kept[0].v[e] = u[e] += bias[0][e];
+            kept[1].v[e] = v[e] += bias[1][e];
+        }
+        if (a.z) {
+            float *const to = static_cast<float *>(a.z) + row * 2 * a.n + col;
+            kept[0].write(to, left);
+            kept[1].write(to + a.n, left);
+        }
+        activate_all(u, a.activation);
+        Piece<T, N> out;
+#pragma unroll
+        for (int e = 0; e < N; ++e) out.v[e] = (T)(u[e] * v[e]);
+        out.write(static_cast<T *>(a.y) + row * a.n + col, left);
+    }
+};
+
 // A workgroup's tile: WM x WN waves of (TM / WM) x (TN / WN).  Per slab, with the
 // fragments of its first half in registers:
 //   read the second half's fragments; multiply the first
@@ -453,7 +508,9 @@ struct Epilogue {
 // (plan_product).
 template <typename T, int MODE, int LIST, bool DMA, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) {
-    constexpr bool kAcrossA = MODE == kWeight, kAcrossB = MODE != kForward;
+    constexpr bool kPaired = MODE == kPair;
+    constexpr bool kAcrossA = MODE == kWeight, kAcrossB = MODE != kForward && !kPaired;
+    constexpr int kCols = kPaired ? TN / 2 : TN;         // of the result
     constexpr bool LISTED = LIST != 0;
     using SideA = Side<T, kAcrossA, DMA, TM, WM * WN>;
     using SideB = Side<T, kAcrossB, DMA, TN, WM * WN>;
@@ -461,9 +518,10 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
     constexpr int FM = kTileM / 16, FN = kTileN / 16;    // its fragments
     constexpr int kSlab = SideA::kSlab;
     constexpr int kBytes = (TM + TN) * 128;              // of a slab
+    static_assert(!kPaired || TN / (WM * WN) == kTileN / 2, "begin_pair's halves are a wave's");
     extern __shared__ __align__(16) char lds[];
 
-    const int64_t tn = (a.n + TN - 1) / TN;
+    const int64_t tn = (a.n + kCols - 1) / kCols;
     int64_t row0, row_end, col0, k0 = 0, k_end = a.k;
     int batch = 0;
     if (MODE == kWeight) {
@@ -482,7 +540,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
         const int64_t tm = gridDim.x / tn;
         int64_t m, n;
         band_tile(xcd_tile(blockIdx.x, gridDim.x), tm, tn, &m, &n);
-        col0 = n * TN;
+        col0 = n * kCols;
         if (a.offsets) {
             batch = expert_of(a.offsets, a.experts, TM, m);
             const int64_t first = a.offsets[batch];
@@ -518,15 +576,15 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
     constexpr int kFits = 2 * kBytes / (WM * WN * kTileN * 4);   // rows of a wave's part
     constexpr int kMost = kFits >= 64 ? 64 : kFits >= 32 ? 32 : 16;
     constexpr int kRowsAt = kTileM < kMost ? kTileM : kMost;
-    constexpr int kLanes = kTileN / N, kPass = 64 / kLanes;
+    constexpr int kLanes = kTileN / (kPaired ? 2 : 1) / N, kPass = 64 / kLanes;
     constexpr int kGroup = kRowsAt / kPass < 4 ? kRowsAt / kPass : 4;
     static_assert(WM * WN * kRowsAt * kTileN * 4 <= 2 * kBytes, "fits in the slabs' LDS");
     using Row = typename Epilogue<T, MODE, N>::Row;
     f4 *mine = reinterpret_cast<f4 *>(lds) + wave * (kRowsAt * kQuads);
-    const int64_t col = col0 + wn + lane % kLanes * N;
+    const int64_t col = col0 + wn / (kPaired ? 2 : 1) + lane % kLanes * N;
     Row extra[kGroup];
     const auto beside = [&](int r0, Row (&to)[kGroup]) {
-        if (a.splits > 1 || col >= a.n) return;
+        if (kPaired || a.splits > 1 || col >= a.n) return;
 #pragma unroll
         for (int q = 0; q < kGroup; ++q) {
             const int r = r0 + q * kPass + lane / kLanes;
@@ -544,7 +602,8 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
         Fragments<T, kAcrossB, TN, FN> rb;
         sa.begin(pa, a.lda, row0, row_end, LIST == 2 ? 0 : k0, MODE == kWeight ? nullptr : a.list,
                  a.per);
-        sb.begin(pb, a.ldb, col0, a.n, LIST == 1 ? 0 : k0, nullptr, a.per);
+        if (kPaired) sb.begin_pair(pb, a.ldb, col0, a.n, k0);
+        else sb.begin(pb, a.ldb, col0, a.n, LIST == 1 ? 0 : k0, nullptr, a.per);
         ra.begin(wm);
         rb.begin(wn);
         int32_t entry[LIST == 2 ? SideA::kLoads : SideB::kLoads];
@@ -633,15 +692,58 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
     // waves' own parts, up to 64 rows at a time, quads of columns exchanged by row so
     // that all banks are met.
     __syncthreads();
-    const Epilogue<T, MODE, N> end(a, col < a.n ? col : 0, batch);
-#pragma unroll
-    for (int x0 = 0; x0 < FM; x0 += kRowsAt / 16) {
+    const auto through = [&](int x0) {
 #pragma unroll
         for (int x = 0; x < kRowsAt / 16; ++x)
 #pragma unroll
             for (int y = 0; y < FN; ++y)
                 mine[(16 * x + i) * kQuads + ((4 * y + g) ^ (i & (kQuads - 1)))] = acc[x0 + x][y];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
+    // this lane's N sums of row r, from quad `first` on
+    const auto sums = [&](int r, int first, float (&v)[N]) {
+#pragma unroll
+        for (int e = 0; e < N / 4; ++e) {
+            const f4 u = mine[r * kQuads + ((first + lane % kLanes * (N / 4) + e) ^
+                                            (r & 15 & (kQuads - 1)))];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[4 * e + c] = u[c];
+        }
+    };
+    if constexpr (kPaired) {
+        const PairEpilogue<T, N> end(a, col < a.n ? col : 0);
+#pragma unroll
+        for (int x0 = 0; x0 < FM; x0 += kRowsAt / 16) {
+            through(x0);
+#pragma unroll 1
+            for (int p = 0; p < kRowsAt / kPass; ++p) {
+                const int r = p * kPass + lane / kLanes;
+                const int64_t row = row0 + wm + 16 * x0 + r;
+                float u[N], v[N];
+                sums(r, 0, u);
+                sums(r, kQuads / 2, v);
+                if (row >= row_end || col >= a.n) continue;
+                if (a.splits > 1) {   // columns are padded to whole tiles
+                    float *const to =
+                        a.partial + (blockIdx.y * a.partial_rows + row) * (tn * TN) + col;
+#pragma unroll
+                    for (int e = 0; e < N / 4; ++e) {
+                        reinterpret_cast<f4 *>(to)[e] = f4{u[4 * e], u[4 * e + 1], u[4 * e + 2], u[4 * e + 3]};
+                        reinterpret_cast<f4 *>(to + tn * kCols)[e] =
+                            f4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
+                    }
+                } else {
+                    end.write(row, u, v);
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+        return;
+    }
+    const Epilogue<T, MODE, N> end(a, col < a.n ? col : 0, batch);
+#pragma unroll
+    for (int x0 = 0; x0 < FM; x0 += kRowsAt / 16) {
+        through(x0);
 #pragma unroll 1
         for (int p = 0; p < kRowsAt / kPass; p += kGroup) {
             // what lies beside the next rows is read while these are worked on
@@ -661,13 +763,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
                 const int r = (p + q) * kPass + lane / kLanes;
                 const int64_t row = row0 + wm + 16 * x0 + r;
                 float v[N];
-#pragma unroll
-                for (int e = 0; e < N / 4; ++e) {
-                    const f4 u = mine[r * kQuads + ((lane % kLanes * (N / 4) + e) ^
-                                                    (r & 15 & (kQuads - 1)))];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) v[4 * e + c] = u[c];
-                }
+                sums(r, 0, v);
                 const bool there = row < row_end && col < a.n;
                 float dot = 0.f;
                 if (there && a.splits > 1) {  // columns are padded to whole tiles
@@ -729,6 +825,23 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a, int64_t ld) {
     }
 }
 
+// The same of a gated layer's products.
+template <typename T>
+__global__ __launch_bounds__(256) void join_pair_kernel(ProductArgs a, int64_t ld) {
+    const int64_t quads = (a.n + 3) / 4;
+    const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = q / quads, col = q % quads * 4;
+    if (row >= a.m) return;
+    f4 u = {0.f, 0.f, 0.f, 0.f}, v = u;
+    for (int s = 0; s < a.splits; ++s) {
+        const float *const from = a.partial + (s * a.partial_rows + row) * ld + col;
+        u += *reinterpret_cast<const f4 *>(from);
+        v += *reinterpret_cast<const f4 *>(from + ld / 2);
+    }
+    float us[4] = {u[0], u[1], u[2], u[3]}, vs[4] = {v[0], v[1], v[2], v[3]};
+    PairEpilogue<T, 4>(a, col).write(row, us, vs);
+}
+
 // Forward product of few rows, 16 at a time: bound by one read of w.  A workgroup
 // takes 16 columns of C, its waves take the contraction's slabs in turn, straight
 // from memory into the fragments (no LDS: w is used once, x comes from the
@@ -750,10 +863,11 @@ __device__ inline i4 piece(const T *row, int64_t k, int64_t k_end) {
     return __builtin_bit_cast(i4, p.v);
 }
 
-template <typename T, int WAVES>
+template <typename T, int WAVES, bool PAIRED>
 __global__ __launch_bounds__(WAVES * 64) void rows_kernel(ProductArgs a, int by_row) {
     constexpr int kElems = 16 / sizeof(T), kSlab = 128 / sizeof(T);
-    __shared__ f4 part[WAVES][64];
+    constexpr int kSides = PAIRED ? 2 : 1;   // matrices, one behind the other
+    __shared__ f4 part[WAVES][kSides][64];
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
     int batch = 0;
     int64_t row0 = (int64_t)blockIdx.y * 16, row_end = a.m;
@@ -766,28 +880,38 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(ProductArgs a, int by_
         if (row0 >= row_end || (by_row && (t - first) % 16 != 0)) return;
     }
     const int64_t col0 = (int64_t)blockIdx.x * 16;
-    const T *wr = static_cast<const T *>(a.b) + batch * a.batch_b +
-                  (col0 + i < a.n ? col0 + i : a.n - 1) * a.ldb;
+    const T *wr[kSides];
+#pragma unroll
+    for (int t = 0; t < kSides; ++t)
+        wr[t] = static_cast<const T *>(a.b) + batch * a.batch_b +
+                (t * a.n + (col0 + i < a.n ? col0 + i : a.n - 1)) * a.ldb;
     int64_t xrow = row0 + i < row_end ? row0 + i : row_end - 1;
     if (a.list) xrow = a.per.quotient(a.list[xrow]);
     const T *xr = static_cast<const T *>(a.a) + xrow * a.lda;
-    f4 acc = {0.f, 0.f, 0.f, 0.f};
+    f4 acc[kSides];
+#pragma unroll
+    for (int t = 0; t < kSides; ++t) acc[t] = f4{0.f, 0.f, 0.f, 0.f};
     // `count` of the wave's slabs from k on
     const auto slabs = [&](auto count, auto check, int64_t k) {
         constexpr int kCount = decltype(count)::value;
-        i4 fw[kCount][2], fx[kCount][2];
+        i4 fw[kCount][kSides][2], fx[kCount][2];
 #pragma unroll
         for (int s = 0; s < kCount; ++s)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int64_t c = k + (int64_t)s * WAVES * kSlab + (h * 4 + g) * kElems;
-                fw[s][h] = piece<T, decltype(check)::value>(wr, c, a.k);
+#pragma unroll
+                for (int t = 0; t < kSides; ++t)
+                    fw[s][t][h] = piece<T, decltype(check)::value>(wr[t], c, a.k);
                 fx[s][h] = piece<T, decltype(check)::value>(xr, c, a.k);
             }
 #pragma unroll
         for (int s = 0; s < kCount; ++s)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) acc = multiply<T>(fw[s][h], fx[s][h], acc);
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int t = 0; t < kSides; ++t)
+                    acc[t] = multiply<T>(fw[s][t][h], fx[s][h], acc[t]);
     };
     const auto fits = [&](int count, int64_t k) {
         return k + ((int64_t)(count - 1) * WAVES + 1) * kSlab <= a.k;
@@ -797,14 +921,22 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(ProductArgs a, int by_
     if (fits(2, k)) slabs(Int<2>(), Int<0>(), k), k += 2 * WAVES * kSlab;
     if (fits(1, k)) slabs(Int<1>(), Int<0>(), k), k += WAVES * kSlab;
     if (k < a.k) slabs(Int<1>(), Int<1>(), k);   // the last, in part
-    part[wave][lane] = acc;
+#pragma unroll
+    for (int t = 0; t < kSides; ++t) part[wave][t][lane] = acc[t];
     __syncthreads();
     if (wave == 0) {
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) acc += part[w][lane];
+        for (int w = 1; w < WAVES; ++w)
+#pragma unroll
+            for (int t = 0; t < kSides; ++t) acc[t] += part[w][t][lane];
         const int64_t row = row0 + i, col = col0 + 4 * g;
         if (row < row_end && col < a.n) {
-            float u[4] = {acc[0], acc[1], acc[2], acc[3]};
+            float u[4] = {acc[0][0], acc[0][1], acc[0][2], acc[0][3]};
+            if constexpr (PAIRED) {
+                float v[4] = {acc[1][0], acc[1][1], acc[1][2], acc[1][3]};
+                PairEpilogue<T, 4>(a, col).write(row, u, v);
+                return;
+            }
             const Epilogue<T, kForward, 4> end(a, col, batch);
             typename Epilogue<T, kForward, 4>::Row extra;
             end.read(a, row, col, extra);
@@ -815,7 +947,8 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(ProductArgs a, int by_
 
 template <typename T, int MODE, int LIST, bool DMA, int TM, int TN, int WM, int WN>
 hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
-    const int64_t tn = (a.n + TN - 1) / TN;
+    constexpr int kCols = MODE == kPair ? TN / 2 : TN;
+    const int64_t tn = (a.n + kCols - 1) / kCols;
     const int64_t tm = MODE == kWeight ? (a.m + TM - 1) / TM * (a.offsets ? a.experts : 1)
                        : a.offsets     ? a.m / TM + a.experts
                                        : (a.m + TM - 1) / TM;
@@ -831,7 +964,9 @@ hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
     if (MODE != kGate && a.splits > 1) {
         const int64_t quads = a.partial_rows * ((a.n + 3) / 4);
         if (!grid_holds((quads + 255) / 256, 256)) return hipErrorInvalidValue;
-        join_kernel<T, MODE><<<(unsigned)((quads + 255) / 256), 256, 0, stream>>>(a, tn * TN);
+        const unsigned blocks = (unsigned)((quads + 255) / 256);
+        if constexpr (MODE == kPair) join_pair_kernel<T><<<blocks, 256, 0, stream>>>(a, tn * TN);
+        else join_kernel<T, MODE><<<blocks, 256, 0, stream>>>(a, tn * TN);
     }
     return hipGetLastError();
 }
@@ -859,7 +994,8 @@ hipError_t launch_rows(const ProductArgs &a, hipStream_t stream) {
     const int64_t wide = (a.n + 15) / 16;
     if (high > 65535 || !grid_holds(wide, WAVES * 64)) return hipErrorInvalidValue;
     const dim3 grid((unsigned)wide, (unsigned)high);
-    rows_kernel<T, WAVES><<<grid, WAVES * 64, 0, stream>>>(a, by_row);
+    if (a.mode == kPair) rows_kernel<T, WAVES, true><<<grid, WAVES * 64, 0, stream>>>(a, by_row);
+    else rows_kernel<T, WAVES, false><<<grid, WAVES * 64, 0, stream>>>(a, by_row);
     return hipGetLastError();
 }
 
@@ -875,6 +1011,7 @@ hipError_t launch_product(ProductArgs a, const ProductPlan &p, hipStream_t strea
         case kForward: return launch_mode<T, kForward, 0>(a, p, stream);
         case kInput: return launch_mode<T, kInput, 0>(a, p, stream);
         case kGate: return launch_mode<T, kGate, 0>(a, p, stream);
+        case kPair: return launch_mode<T, kPair, 0>(a, p, stream);
         default:
             return !a.list       ? launch_mode<T, kWeight, 0>(a, p, stream)
                    : a.list_of_a ? launch_mode<T, kWeight, 2>(a, p, stream)

@@ -33,7 +33,7 @@ from . import SomError, _check, lib as _lib
 
 __all__ = [
     "ACTIVATIONS", "GATES", "EXPORTED", "SomError", "Routing", "ExpertsGradient", "AdamW", "linear",
-    "linear_backward", "norm", "norm_backward", "route", "route_backward", "dispatch", "distill", "distill_backward", "experts", "experts_backward",
+    "linear_backward", "gated", "gated_backward", "norm", "norm_backward", "route", "route_backward", "dispatch", "distill", "distill_backward", "experts", "experts_backward",
     "gate_from_map",
 ]
 
@@ -45,6 +45,7 @@ STATE_BLOCK = 256
 # Every symbol include/som_local.h declares.
 EXPORTED = (
     "som_linear_workspace", "som_linear_route", "som_linear", "som_linear_backward",
+    "som_gated_workspace", "som_gated_route", "som_gated", "som_gated_backward",
     "som_experts_workspace", "som_experts_route", "som_experts", "som_experts_backward",
     "som_norm_workspace", "som_norm", "som_norm_backward",
     "som_route", "som_route_backward",
@@ -64,6 +65,18 @@ class _LinearCall(C.Structure):
                 ("dx", C.c_void_p), ("dw", C.c_void_p), ("dbias", C.c_void_p),
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
                 ("stream", C.c_void_p)]
+
+
+class _GatedCall(C.Structure):
+    """``som_gated_call`` of include/som_local.h."""
+
+    _fields_ = [("type", C.c_int32), ("activation", C.c_int32), ("n", C.c_int64),
+                ("inner", C.c_int32), ("hidden", C.c_int32), ("x", C.c_void_p),
+                ("ldx", C.c_int64), ("w", C.c_void_p), ("bias", C.c_void_p),
+                ("y", C.c_void_p), ("z", C.c_void_p), ("dy", C.c_void_p),
+                ("lddy", C.c_int64), ("dx", C.c_void_p), ("dw", C.c_void_p),
+                ("dbias", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_uint64), ("stream", C.c_void_p)]
 
 
 class _ExpertsCall(C.Structure):
@@ -142,6 +155,10 @@ def lib():
         "som_linear_route": [C.POINTER(_LinearCall), i32, C.POINTER(i32)],
         "som_linear": [C.POINTER(_LinearCall)],
         "som_linear_backward": [C.POINTER(_LinearCall)],
+        "som_gated_workspace": [C.POINTER(_GatedCall), i32, C.POINTER(u64)],
+        "som_gated_route": [C.POINTER(_GatedCall), i32, C.POINTER(i32)],
+        "som_gated": [C.POINTER(_GatedCall)],
+        "som_gated_backward": [C.POINTER(_GatedCall)],
         "som_experts_workspace": [C.POINTER(_ExpertsCall), i32, C.POINTER(u64)],
         "som_experts_route": [C.POINTER(_ExpertsCall), i32, C.POINTER(i32)],
         "som_experts": [C.POINTER(_ExpertsCall)],
@@ -305,6 +322,54 @@ def linear_backward(dy, x, w, z=None, activation: str = "none", bias: bool = Tru
     dbias = torch.empty(outer, dtype=x.dtype, device=x.device) if bias else None
     call.dx, call.dw, call.dbias = _ptr(dx), _ptr(dw), _ptr(dbias)
     _run("linear", call, True, x)
+    return dx, dw, dbias
+
+
+# -------------------------------------------------------------- gated layer
+def _gated_call(x, w, activation: str):
+    code = _type(x, "x")
+    _rows(x, "x")
+    if w.dim() != 3 or w.shape[0] != 2 or not w.numel():
+        raise ValueError("w must be (2, hidden, inner)")
+    _like(w, x, (2, w.shape[1], x.shape[1]), "w")
+    return _GatedCall(type=code, activation=_of(ACTIVATIONS, activation, "activation"),
+                      n=x.shape[0], inner=x.shape[1], hidden=w.shape[1], x=_ptr(x), ldx=_ld(x),
+                      w=_ptr(w))
+
+
+def gated(x, w, bias=None, activation: str = "silu", keep: bool = False):
+    """y = act(x w₀ᵀ + bias₀) · (x w₁ᵀ + bias₁) for x (n, inner), w (2, hidden, inner)
+    and bias (2, hidden), both products in one kernel.
+
+    With ``keep`` returns (y, z): the two factors before the activation, (n, 2,
+    hidden) fp32 whatever x's type, as the gradient needs them."""
+    call = _gated_call(x, w, activation)
+    n, hidden = x.shape[0], w.shape[1]
+    if bias is not None:
+        _like(bias, x, (2, hidden), "bias")
+        call.bias = _ptr(bias)
+    y = torch.empty((n, hidden), dtype=x.dtype, device=x.device)
+    z = torch.empty((n, 2, hidden), dtype=torch.float32, device=x.device) if keep else None
+    call.y, call.z = _ptr(y), _ptr(z)
+    _run("gated", call, False, x)
+    return (y, z) if keep else y
+
+
+def gated_backward(dy, x, w, z, activation: str = "silu", bias: bool = True):
+    """(dx, dw, dbias) of ``gated`` from the gradient dy of its result; dbias is None
+    without ``bias``."""
+    call = _gated_call(x, w, activation)
+    n, hidden = x.shape[0], w.shape[1]
+    _like(dy, x, (n, hidden), "dy", packed=False)
+    if not isinstance(z, torch.Tensor) or z.dtype != torch.float32:
+        raise TypeError("z must be float32 (gated with keep=True)")
+    _shaped(z, x, (n, 2, hidden), "z")
+    call.dy, call.lddy, call.z = _ptr(dy), _ld(dy), _ptr(z)
+    dx = torch.empty((n, x.shape[1]), dtype=x.dtype, device=x.device)
+    dw = torch.empty_like(w)
+    dbias = torch.empty((2, hidden), dtype=x.dtype, device=x.device) if bias else None
+    call.dx, call.dw, call.dbias = _ptr(dx), _ptr(dw), _ptr(dbias)
+    _run("gated", call, True, x)
     return dx, dw, dbias
 
 

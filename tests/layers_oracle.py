@@ -10,6 +10,7 @@ import math
 
 import torch
 
+import local_oracle as L
 from local_oracle import V, stored
 
 
@@ -187,3 +188,46 @@ class Distill:
         tiny = 2.0 ** -140      # sums and products next to fp32's least value
         self.loss = (loss, (loss_err.squeeze(1) + 8 * V * loss.abs() + tiny).nan_to_num(posinf=0.0))
         self.dlogits = (grad, (grad_err + stored(grad, dtype) + tiny).nan_to_num(posinf=0.0))
+
+
+# -------------------------------------------------------------- gated layer
+def gated(x, w, b, kind, dtype):
+    """((y, bound), (z, bound)) with z (n, 2, hidden)."""
+    k, hidden = x.shape[1], w.shape[1]
+    flat = w.reshape(2 * hidden, k)
+    z = x @ flat.t()
+    size = x.abs() @ flat.abs().t()
+    if b is not None:
+        z, size = z + b.reshape(-1), size + b.abs().reshape(-1)
+    zerr = (k + 8) * V * size
+    u, v = z[:, :hidden], z[:, hidden:]
+    h, herr = L.act(u, kind), L.SLOPE[kind] * zerr[:, :hidden] + 8 * V * u.abs()
+    y = h * v
+    err = herr * (v.abs() + zerr[:, hidden:]) + h.abs() * zerr[:, hidden:] + 4 * V * y.abs()
+    n = x.shape[0]
+    return (y, err + stored(y, dtype)), (z.view(n, 2, hidden), zerr.view(n, 2, hidden))
+
+
+def gated_backward(dy, x, w, z, kind, dtype):
+    """{"dx", "dw", "db"} from z = (value, bound)."""
+    n, k = x.shape
+    hidden = w.shape[1]
+    u, v = z[0][:, 0], z[0][:, 1]
+    ue, ve = z[1][:, 0], z[1][:, 1]
+    slope, h = L.act_slope(u, kind), L.act(u, kind)
+    se = L.BEND[kind] * ue + 16 * V
+    if kind == "relu":      # next to the kink either slope is right
+        se = se + (u.abs() <= ue).double()
+    he = L.SLOPE[kind] * ue + 8 * V * u.abs()
+    dz = torch.cat([dy * v * slope, dy * h], 1)
+    raw = torch.cat([dy.abs() * (se * (v.abs() + ve) + slope.abs() * ve), dy.abs() * he], 1)
+    raw = raw + 4 * V * dz.abs()
+    err = raw + stored(dz, dtype)        # held in dtype for the two products
+    flat = w.reshape(2 * hidden, k)
+    dx, dw, db = dz @ flat, dz.t() @ x, dz.sum(0)
+    dx_err = (2 * hidden + 8) * V * (dz.abs() @ flat.abs()) + err @ flat.abs()
+    dw_err = (n + 8) * V * (dz.abs().t() @ x.abs()) + err.t() @ x.abs()
+    db_err = (n + 8) * V * dz.abs().sum(0) + raw.sum(0)
+    return {"dx": (dx, dx_err + stored(dx, dtype)),
+            "dw": ((dw).view(2, hidden, k), (dw_err + stored(dw, dtype)).view(2, hidden, k)),
+            "db": (db.view(2, hidden), (db_err + stored(db, dtype)).view(2, hidden))}

@@ -81,3 +81,18 @@ def test_distillation_of_closed_classes():
     a = math.e / (1 + math.e)
     _near(o.dlogits[0], torch.tensor([[-a, 0.0, a], [0.0, 0.0, 0.0]], dtype=F64), "dlogits")
     _near(o.loss[0], torch.tensor([-math.log(1 - a), 0.0], dtype=F64), "loss")
+
+
+@pytest.mark.parametrize("kind", ["none", "relu", "gelu", "silu"])
+def test_gated_layer(kind):
+    g = torch.Generator().manual_seed(4)
+    x, w = torch.randn(3, 5, generator=g, dtype=F64), torch.randn(2, 4, 5, generator=g, dtype=F64)
+    b, dy = torch.randn(2, 4, generator=g, dtype=F64), torch.randn(3, 4, generator=g, dtype=F64)
+
+    def value():
+        return (O.gated(x, w, b, kind, torch.float32)[0][0] * dy).sum()
+
+    z = O.gated(x, w, b, kind, torch.float32)[1]
+    got = O.gated_backward(dy, x, w, z, kind, torch.float32)
+    for name, t in (("dx", x), ("dw", w), ("db", b)):
+        _near(got[name][0], _slopes(value, t), name)
