@@ -99,6 +99,55 @@ som_status som_linear_route(const som_linear_call *call, int32_t backward, int32
 som_status som_linear(const som_linear_call *call);
 som_status som_linear_backward(const som_linear_call *call);
 
+/* Rows in 8 bits.  Blocks of 128 neighbours of a row are held as e4m3 codes (OCP: 448 the
+ * largest) of its values divided by a power of two, the block's scale 2^(s - 127): the
+ * least one that brings the largest finite magnitude to 448 or below, 2^-126 at least.
+ * Codes are rounded to the nearest, ties to even; NaN and infinities become the code of
+ * NaN.  Rows of codes are filled up with zeros to whole blocks, 128 ceil(width / 128)
+ * bytes a row, rows of scales (a byte each) with 127 to a multiple of four. */
+typedef struct som_blocks_call {
+    int32_t type;              /* som_type of x                                      */
+    int32_t width;             /* 1 .. 4,000,000                                     */
+    int64_t n;                 /* rows; 0 is allowed                                 */
+    const void *x;
+    int64_t ldx;               /* elements from row to row, >= width                 */
+    void *codes;               /* written; 16-byte aligned                           */
+    void *scale;               /* written; 4-byte aligned                            */
+    void *stream;
+} som_blocks_call;
+
+/* Errors: SOM_E_ARG, SOM_E_UNSUPPORTED (width above 4,000,000), SOM_E_DEVICE. */
+som_status som_to_blocks(const som_blocks_call *call);
+
+/* som_linear's forward product with w and x in 8 bits as som_to_blocks gives them,
+ *     y = act(x w^T + bias) + residual.
+ * x comes in `type` and is brought to 8 bits by the call, or in 8 bits already.  bias,
+ * residual and y are of `type`, which has 16 bits: the matrix instruction's sums of
+ * products of 8 bits are exact to about 16 (of eight products at a time, what lies 2^-13
+ * below the largest is dropped).  A row's filling has to be zeros.  For the gradient
+ * of x, dx = dz w, w's transpose is brought to 8 bits too. */
+typedef struct som_linear8_call {
+    int32_t type;              /* SOM_BF16 or SOM_F16                                */
+    int32_t activation;        /* som_activation                                     */
+    int64_t n;                 /* rows (documents); 0 is allowed                     */
+    int32_t inner, outer;      /* 1 .. 4,000,000                                     */
+    const void *x;             /* of type; NULL if x_codes is given                  */
+    int64_t ldx;               /* >= inner                                           */
+    const void *x_codes, *x_scale;   /* of n rows; NULL if x is given                */
+    const void *w_codes, *w_scale;   /* of outer rows                                */
+    const void *bias;          /* outer; NULL for none                               */
+    const void *residual;      /* NULL for none                                      */
+    int64_t ldr;               /* >= outer                                           */
+    void *y;                   /* packed                                             */
+    void *workspace;
+    uint64_t workspace_bytes;
+    void *stream;
+} som_linear8_call;
+
+/* Errors: as som_linear. */
+som_status som_linear8_workspace(const som_linear8_call *call, uint64_t *bytes);
+som_status som_linear8(const som_linear8_call *call);
+
 /* A gated layer, of x (n x inner) and two matrices w (2 x hidden x inner) at once:
  *     [u v] = x w^T + bias,    y = act(u) v         (each n x hidden)
  * For a gradient, forward has to keep z = [u v], n x 2 hidden in fp32 whatever the type:

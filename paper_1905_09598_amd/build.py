@@ -26,7 +26,7 @@ SOURCES = ["som_api.cpp", "som_train.hip", "som_train_pipe.hip", "som_train_pipe
            "som_stream.hip",
            "som_local_api.cpp", "som_local_rows.hip", "som_product_f32.hip",
            "som_product_bf16.hip", "som_product_f16.hip", "som_route.hip", "som_adamw.hip",
-           "som_norm.hip", "som_distill.hip", "som_gated.hip"]
+           "som_norm.hip", "som_distill.hip", "som_gated.hip", "som_product_e4m3.hip"]
 ARCH = "gfx950"
 
 

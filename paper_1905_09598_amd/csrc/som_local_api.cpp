@@ -22,7 +22,7 @@ ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus) {
     ProductPlan best{};
     best.aligned = aligned;
     const int64_t experts = a.offsets ? a.experts : 1;
-    const int64_t slab = 128 / type_size(a.type);
+    const int64_t slab = a.eight ? 128 : 128 / type_size(a.type);
     const bool along = a.mode == kForward || a.mode == kPair;
     // a gated layer's tiles hold the same columns of two matrices
     const int64_t columns = a.mode == kPair ? 2 * a.n : a.n;
@@ -32,8 +32,9 @@ ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus) {
         // as few waves to a workgroup as keep the chip's loads in flight (16 waves of
         // four slabs a compute unit), so that all workgroups run at once
         best.waves = 4;
+        const int64_t turn = a.eight ? 4 * slab : slab;   // of a wave
         while (best.waves < 16 && groups * best.waves < (int64_t)num_cus * 16 &&
-               a.k > best.waves * slab)
+               a.k > best.waves * turn)
             best.waves *= 2;
         best.splits = 1;
         return best;
@@ -345,6 +346,53 @@ struct LinearBackward {
                         [&] { return has_input ? run(input, s) : hipSuccess; },
                         [&] { return has_weight ? run(weight, s) : hipSuccess; },
                         [&] { return sums.out ? som::launch_sums(sums, s) : hipSuccess; });
+    }
+};
+
+// Rows of `width` values in 8 bits: of their codes and of their scales.
+int64_t codes_of(int64_t width) { return rounded(width, 128); }
+int64_t scales_of(int64_t width) { return rounded(width, 512) / 128; }
+
+// x is brought to 8 bits first, unless it is there or has few rows.
+struct Linear8 {
+    ProductArgs a{};
+    ProductPlan plan{};
+    som::BlocksArgs blocks{};
+    som::Rows8Args few{};
+    bool first;
+    Linear8(const som_linear8_call &c, Carver &work) {
+        a.mode = som::kForward;
+        a.eight = 1;
+        a.type = c.type;
+        a.activation = c.activation;
+        a.m = c.n, a.n = c.outer, a.k = codes_of(c.inner);
+        a.lda = a.ldb = a.k;
+        a.ld_scale = scales_of(c.inner);
+        a.a = c.x_codes, a.scale_a = static_cast<const unsigned char *>(c.x_scale);
+        a.b = c.w_codes, a.scale_b = static_cast<const unsigned char *>(c.w_scale);
+        a.bias = c.bias;
+        a.residual = c.residual, a.ldr = c.ldr;
+        a.y = c.y;
+        plan = som::plan_product(a, true, compute_units());
+        first = !c.x_codes && !plan.waves;
+        if (!c.x_codes) few.x = c.x, few.ldx = c.ldx, few.width = c.inner;
+        if (first) {
+            blocks.type = c.type;
+            blocks.n = c.n, blocks.width = c.inner;
+            blocks.x = c.x, blocks.ldx = c.ldx;
+            blocks.ld_codes = a.k, blocks.ld_scale = a.ld_scale;
+            blocks.codes = work.take<unsigned char>((uint64_t)c.n * a.k);
+            blocks.scale = work.take<unsigned char>((uint64_t)c.n * a.ld_scale);
+            a.a = blocks.codes, a.scale_a = blocks.scale;
+        }
+        if (plan.splits > 1) {
+            a.partial = work.take<float>((uint64_t)plan.partial_floats * 4);
+            a.partial_rows = a.m;
+        }
+    }
+    hipError_t enqueue(hipStream_t s) const {
+        return in_order([&] { return first ? som::launch_to_blocks(blocks, s) : hipSuccess; },
+                        [&] { return som::launch_product8(a, few, plan, s); });
     }
 };
 
@@ -884,6 +932,63 @@ som_status som_experts_backward(const som_experts_call *c) {
         !rows_ok_or_null(c->db2, e, c->outer, c->outer, size))
         return SOM_E_ARG;
     return enqueue<ExpertsBackward>(*c);
+}
+
+// Codes and scales of rows rows of `width` values.
+static bool blocks_ok(const void *codes, const void *scale, int64_t rows, int64_t width) {
+    const int64_t c = codes_of(width), s = scales_of(width);
+    return rows_ok(codes, rows, c, c, 1) && rows_ok(scale, rows, s, s, 1) &&
+           (rows == 0 || (reinterpret_cast<uintptr_t>(codes) % 16 == 0 &&
+                          reinterpret_cast<uintptr_t>(scale) % 4 == 0));
+}
+
+som_status som_to_blocks(const som_blocks_call *c) {
+    if (!c || !type_ok(c->type) || c->n < 0 || c->width < 1 || c->ldx < c->width) return SOM_E_ARG;
+    if (c->width > som::kMaxWidth || c->n > (int64_t)1 << 40) return SOM_E_UNSUPPORTED;
+    if (!rows_ok(c->x, c->n, c->width, c->ldx, som::type_size(c->type)) ||
+        !blocks_ok(c->codes, c->scale, c->n, c->width))
+        return SOM_E_ARG;
+    som::BlocksArgs a{};
+    a.type = c->type;
+    a.n = c->n, a.width = c->width;
+    a.x = c->x, a.ldx = c->ldx;
+    a.codes = static_cast<unsigned char *>(c->codes), a.ld_codes = codes_of(c->width);
+    a.scale = static_cast<unsigned char *>(c->scale), a.ld_scale = scales_of(c->width);
+    return from_hip(som::launch_to_blocks(a, reinterpret_cast<hipStream_t>(c->stream)));
+}
+
+static som_status linear8_sizes_ok(const som_linear8_call *c) {
+    if (!c || (c->type != SOM_BF16 && c->type != SOM_F16) || !activation_ok(c->activation) ||
+        c->n < 0 || c->inner <= 0 || c->outer <= 0 || (c->n && !c->x_codes && c->ldx < c->inner))
+        return SOM_E_ARG;
+    if (c->inner > som::kMaxWidth || c->outer > som::kMaxWidth || c->n > (int64_t)1 << 40)
+        return SOM_E_UNSUPPORTED;
+    return SOM_OK;
+}
+
+som_status som_linear8_workspace(const som_linear8_call *c, uint64_t *bytes) {
+    if (!bytes) return SOM_E_ARG;
+    const som_status st = linear8_sizes_ok(c);
+    if (st == SOM_OK) {
+        Carver need(nullptr);
+        if (c->n) Linear8(*c, need);
+        *bytes = need.used;
+    }
+    return st;
+}
+
+som_status som_linear8(const som_linear8_call *c) {
+    const som_status st = linear8_sizes_ok(c);
+    if (st != SOM_OK) return st;
+    const int size = som::type_size(c->type);
+    if ((c->x_codes ? c->x != nullptr || !blocks_ok(c->x_codes, c->x_scale, c->n, c->inner)
+                    : c->x_scale != nullptr || !rows_ok(c->x, c->n, c->inner, c->ldx, size)) ||
+        !blocks_ok(c->w_codes, c->w_scale, c->outer, c->inner) ||
+        !rows_ok(c->y, c->n, c->outer, c->outer, size) ||
+        !rows_ok_or_null(c->bias, 1, c->outer, c->outer, size) ||
+        !rows_ok_or_null(c->residual, c->n, c->outer, c->ldr, size))
+        return SOM_E_ARG;
+    return c->n ? enqueue<Linear8>(*c) : SOM_OK;
 }
 
 static som_status norm_ok(const som_norm_call *c) {

@@ -183,6 +183,9 @@ struct ProductArgs {
     const void *image;                // rows of n: forward's scaled, of act(argument); or null
     float *dots;                      // gate: m x dot_cols
     int32_t dot_cols;
+    int32_t eight;                    // both sides in 8 bits, k in whole blocks of 128
+    const unsigned char *scale_a, *scale_b;   // their powers of two, rows ld_scale apart
+    int64_t ld_scale;
     int32_t splits;       // parts of the contraction
     float *partial;       // splits x partial_rows x whole tiles
     int64_t partial_rows;
@@ -375,6 +378,23 @@ struct DistillArgs {
 };
 hipError_t launch_distill(const DistillArgs &a, hipStream_t stream);
 
+// som_product_e4m3.hip: rows in 8 bits, codes ld_codes and scales ld_scale apart.
+struct BlocksArgs {
+    int32_t type;
+    int64_t n, width;
+    const void *x;
+    int64_t ldx;
+    unsigned char *codes, *scale;
+    int64_t ld_codes, ld_scale;
+    Divider units;          // of four blocks, of a row
+};
+hipError_t launch_to_blocks(const BlocksArgs &a, hipStream_t stream);
+// x as the caller has it, for the kernel of few rows; NULL if it is held in 8 bits.
+struct Rows8Args {
+    const void *x;
+    int64_t ldx, width;
+};
+
 // Sums of parts (parts x 2 x width, in order) to two rows of width, each NULL if not
 // wanted (som_norm.hip).
 hipError_t launch_join_parts(int32_t type, const float *partial, int32_t parts, int64_t width,
@@ -406,5 +426,8 @@ inline int32_t plan_dot_cols(const ProductPlan &p, int64_t n) {
 hipError_t launch_product_f32(ProductArgs a, const ProductPlan &p, hipStream_t stream);
 hipError_t launch_product_bf16(ProductArgs a, const ProductPlan &p, hipStream_t stream);
 hipError_t launch_product_f16(ProductArgs a, const ProductPlan &p, hipStream_t stream);
+// type: of the result, in 16 bits.
+hipError_t launch_product8(const ProductArgs &a, const Rows8Args &b, const ProductPlan &p,
+                           hipStream_t stream);
 
 }  // namespace som

@@ -24,6 +24,11 @@
 //           16-bit types are transposed by the reading instruction.
 // Rows beyond C are read from its last row, columns from its first, and not
 // stored; the contraction is filled up from 16 bytes of zeros.
+//
+// Forward products also take both sides in 8 bits (e4m3, T = Eight), rows of whole blocks
+// of 128 with one power of two each.  A slab is then one block, and one instruction
+// (16x16x128) takes all of it with the powers of two of its rows and columns; four
+// slabs' powers are a word of a row, which comes with each slab through LDS.
 #pragma once
 
 #include "som_local_internal.h"
@@ -37,6 +42,7 @@ namespace {
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef int i4 __attribute__((ext_vector_type(4)));
 typedef short s4 __attribute__((ext_vector_type(4)));
+typedef int i8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef const __attribute__((address_space(1))) void *GlobalPtr;
@@ -67,6 +73,21 @@ __device__ inline f4 multiply<float>(i4 b, i4 a, f4 c) {
     for (int j = 0; j < 4; ++j)
         c = __builtin_amdgcn_mfma_f32_16x16x4f32(bf[j], af[j], c, 0, 0, 0);
     return c;
+}
+
+// (The halves of a slab of 8 bits are multiplied together, multiply_scaled.)
+template <>
+__device__ inline f4 multiply<unsigned char>(i4, i4, f4 c) {
+    return c;
+}
+
+// Codes of 8 bits.  The instruction brings eight products at a time to the largest one's
+// exponent and drops what lies 13 bits or more below it (measured: 2048 products of
+// normal values are off by 1.6e-5 of their sum, a tenth of fp16's rounding), so results
+// are of 16 bits.
+typedef unsigned char Eight;
+__device__ inline f4 multiply_scaled(i8 b, int scale_b, i8 a, int scale_a, f4 c) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, 0, 0, 0, scale_b, 0, scale_a);
 }
 
 // ---------------------------------------------------------------- one side
@@ -506,8 +527,10 @@ struct PairEpilogue {
 // bank conflict, at 2.05 GHz, and fetches 269 MB of the 201 it needs: bound by what the
 // slabs and the epilogue wait for.  Small tiles fill the chip where there are few
 // (plan_product).
-template <typename T, int MODE, int LIST, bool DMA, int TM, int TN, int WM, int WN>
+template <typename T, typename Out, int MODE, int LIST, bool DMA, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) {
+    constexpr bool kEight = sizeof(T) == 1;
+    static_assert(!kEight || (MODE == kForward && DMA && LIST == 0), "forward, whole rows");
     constexpr bool kPaired = MODE == kPair;
     constexpr bool kAcrossA = MODE == kWeight, kAcrossB = MODE != kForward && !kPaired;
     constexpr int kCols = kPaired ? TN / 2 : TN;         // of the result
@@ -518,6 +541,8 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
     constexpr int FM = kTileM / 16, FN = kTileN / 16;    // its fragments
     constexpr int kSlab = SideA::kSlab;
     constexpr int kBytes = (TM + TN) * 128;              // of a slab
+    constexpr int kPowers = WM * WN * 64 * 4;            // 8 bits: a word to a thread, and row
+    static_assert(!kEight || TM + TN <= WM * WN * 64, "a thread to a row");
     static_assert(!kPaired || TN / (WM * WN) == kTileN / 2, "begin_pair's halves are a wave's");
     extern __shared__ __align__(16) char lds[];
 
@@ -553,7 +578,8 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
     }
     // this workgroup's part of the contraction
     if (a.splits > 1) {
-        const int64_t part = ((k_end - k0 + a.splits - 1) / a.splits + kSlab - 1) / kSlab * kSlab;
+        constexpr int kWhole = kEight ? 4 * kSlab : kSlab;   // words of powers are read whole
+        const int64_t part = ((k_end - k0 + a.splits - 1) / a.splits + kWhole - 1) / kWhole * kWhole;
         const int64_t from = k0 + part * blockIdx.y;
         k_end = from + part < k_end ? from + part : k_end;
         k0 = from < k_end ? from : k_end;
@@ -572,14 +598,14 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
         for (int y = 0; y < FN; ++y) acc[x][y] = f4{0.f, 0.f, 0.f, 0.f};
     // The result's rows as they leave: N columns a lane, kPass rows of the wave at a
     // time; what lies beside them in memory is read kGroup passes ahead.
-    constexpr int N = 16 / sizeof(T), kQuads = kTileN / 4;
+    constexpr int N = 16 / sizeof(Out), kQuads = kTileN / 4;
     constexpr int kFits = 2 * kBytes / (WM * WN * kTileN * 4);   // rows of a wave's part
     constexpr int kMost = kFits >= 64 ? 64 : kFits >= 32 ? 32 : 16;
     constexpr int kRowsAt = kTileM < kMost ? kTileM : kMost;
     constexpr int kLanes = kTileN / (kPaired ? 2 : 1) / N, kPass = 64 / kLanes;
     constexpr int kGroup = kRowsAt / kPass < 4 ? kRowsAt / kPass : 4;
     static_assert(WM * WN * kRowsAt * kTileN * 4 <= 2 * kBytes, "fits in the slabs' LDS");
-    using Row = typename Epilogue<T, MODE, N>::Row;
+    using Row = typename Epilogue<Out, MODE, N>::Row;
     f4 *mine = reinterpret_cast<f4 *>(lds) + wave * (kRowsAt * kQuads);
     const int64_t col = col0 + wn / (kPaired ? 2 : 1) + lane % kLanes * N;
     Row extra[kGroup];
@@ -589,7 +615,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
         for (int q = 0; q < kGroup; ++q) {
             const int r = r0 + q * kPass + lane / kLanes;
             if (r < kTileM && row0 + wm + r < row_end)
-                Epilogue<T, MODE, N>::read(a, row0 + wm + r, col, to[q]);
+                Epilogue<Out, MODE, N>::read(a, row0 + wm + r, col, to[q]);
         }
     };
 
@@ -615,6 +641,14 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
         if (LIST == 2) sa.step = 0, sa.easy = row0 + TM <= row_end;
         entries(0);
         // the offsets of the slab that is loaded next, and the list beyond it
+        // 8 bits: this thread's row of powers, of A's rows, then B's
+        const unsigned char *powers = nullptr;
+        if constexpr (kEight) {
+            const int t = (int)threadIdx.x < TM + TN ? threadIdx.x : 0;
+            const int64_t row = t < TM ? (row0 + t < row_end ? row0 + t : row_end - 1)
+                                       : (col0 + t - TM < a.n ? col0 + t - TM : a.n - 1);
+            powers = (t < TM ? a.scale_a : a.scale_b) + row * a.ld_scale + k0 / kSlab;
+        }
         const auto follow = [&](int64_t s) {
             if constexpr (LIST == 1) sb.follow(entry, a.per, a.ldb, col0, a.n);
             if constexpr (LIST == 2) sa.follow(entry, a.per, a.lda, row0, row_end);
@@ -625,6 +659,10 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
             const int64_t left = k_end - k0 - s * kSlab;
             sa.template load<decltype(check)::value>(to, left, row0, row_end);
             sb.template load<decltype(check)::value>(to + TM * 128, left, col0, a.n);
+            if constexpr (kEight)   // the word that holds this slab's powers, of every row
+                __builtin_amdgcn_global_load_lds((GlobalPtr)(powers + ((s < slabs ? s : slabs - 1) & ~3)),
+                                                 (LdsPtr)(lds + 2 * kBytes + (s & 1) * kPowers + wave * 256),
+                                                 4, 0, 0);
         };
         const auto store = [&](int64_t s) {
             sa.store(lds + (s & 1) * kBytes);
@@ -669,23 +707,97 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
             times(Int<1>());
             __builtin_amdgcn_sched_barrier(0);
         };
+        // 8 bits: fragments of whole slabs and their powers; B's all at once, A's kStep rows of
+        // fragments at a time, of which the next are read while these are multiplied
+        constexpr int kStep = FM > 4 ? FM / 4 : FM / 2, kSteps = FM / kStep;
+        static_assert(kSteps % 2 == 0, "a slab begins in the first of two places");
+        i8 ea[2][kEight ? kStep : 1], eb[kEight ? FN : 1];
+        int pa_[kEight ? FM : 1], pb_[kEight ? FN : 1];
+        const auto whole = [&](const auto &side, int at, int f) {
+            const i4 u = side.read(lds, at, f, 0), v = side.read(lds, at, f, 1);
+            return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        const auto read_a = [&](int64_t s, auto step) {
+            constexpr int q = decltype(step)::value;
+#pragma unroll
+            for (int x = 0; x < kStep; ++x)
+                ea[q & 1][x] = whole(ra, (int)(s & 1) * kBytes, q * kStep + x);
+        };
+        const auto read_b = [&](int64_t s) {
+#pragma unroll
+            for (int y = 0; y < FN; ++y) eb[y] = whole(rb, (int)(s & 1) * kBytes + TM * 128, y);
+        };
+        const auto read_powers = [&](int64_t s) {
+            const auto *const from = reinterpret_cast<const unsigned char *>(lds) + 2 * kBytes +
+                                     (s & 1) * kPowers + (s & 3) + 4 * i;
+#pragma unroll
+            for (int x = 0; x < FM; ++x) pa_[x] = from[4 * (wm + 16 * x)];
+#pragma unroll
+            for (int y = 0; y < FN; ++y) pb_[y] = from[4 * (TM + wn + 16 * y)];
+        };
+        const auto times_scaled = [&](auto step) {
+            constexpr int q = decltype(step)::value;
+#pragma unroll
+            for (int x = 0; x < kStep; ++x)
+#pragma unroll
+                for (int y = 0; y < FN; ++y)
+                    acc[q * kStep + x][y] = multiply_scaled(eb[y], pb_[y], ea[q & 1][x],
+                                                            pa_[q * kStep + x], acc[q * kStep + x][y]);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        // last: there is no slab after it.  The slab before the last has none to load and loads
+        // the last again, into a place that is not read: in a loop of one body that begins
+        // with reads of its own the sums stay where they are (with the powers read at its
+        // end, and two bodies, the compiler moved them: 640 bytes a lane out of registers).
+        const auto slab_scaled = [&](auto last, int s) {
+            read_powers(s);
+            read_a(s, Int<1>());
+            times_scaled(Int<0>());
+            if constexpr (kSteps == 4) {
+                read_a(s, Int<2>());
+                times_scaled(Int<1>());
+                read_a(s, Int<3>());
+                times_scaled(Int<2>());
+            }
+            if constexpr (decltype(last)::value) {
+                times_scaled(Int<kSteps - 1>());
+            } else {
+                wait_loads<0>();
+                __syncthreads();
+                sa.step = sb.step = s + 3 < (int)slabs ? 128 : 0;
+                load(Int<0>(), s + 2);
+                read_a(s + 1, Int<0>());
+                times_scaled(Int<kSteps - 1>());
+                read_b(s + 1);
+            }
+        };
         follow(0);
         load(Int<1>(), 0);
         store(0);
         if (slabs > 1) {
             follow(1);
+            if (kEight) sa.step = sb.step = 2 < slabs ? 128 : 0;
             load(Int<1>(), 1);
         }
         // all but the second slab's loads have landed
-        if (DMA && slabs > 1 && !LISTED) wait_loads<SideA::kLoads + SideB::kLoads>();
+        if (DMA && slabs > 1 && !LISTED) wait_loads<SideA::kLoads + SideB::kLoads + kEight>();
         else if (DMA) wait_loads<0>();
         __syncthreads();
-        read(0, Int<0>());
         int64_t s = 0;
-        for (; s + 3 < slabs; ++s) slab(Int<2>(), s);
-        if (s + 2 < slabs) slab(Int<1>(), s++);
-        if (s + 1 < slabs) slab(Int<0>(), s++);
-        slab(Int<-1>(), s);
+        if constexpr (kEight) {
+            read_a(0, Int<0>());
+            read_b(0);
+            for (int t = 0; t + 1 < (int)slabs; ++t) slab_scaled(Int<0>(), t);
+            slab_scaled(Int<1>(), (int)slabs - 1);
+            wait_loads<0>();    // the last slab's second load too, before LDS is written
+            beside(0, extra);   // not before: there are no registers left
+        } else {
+            read(0, Int<0>());
+            for (; s + 3 < slabs; ++s) slab(Int<2>(), s);
+            if (s + 2 < slabs) slab(Int<1>(), s++);
+            if (s + 1 < slabs) slab(Int<0>(), s++);
+            slab(Int<-1>(), s);
+        }
     }
 
     // Through LDS, so that a lane holds 16 bytes of a row of the result: the
@@ -711,7 +823,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
         }
     };
     if constexpr (kPaired) {
-        const PairEpilogue<T, N> end(a, col < a.n ? col : 0);
+        const PairEpilogue<Out, N> end(a, col < a.n ? col : 0);
 #pragma unroll
         for (int x0 = 0; x0 < FM; x0 += kRowsAt / 16) {
             through(x0);
@@ -740,7 +852,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
         }
         return;
     }
-    const Epilogue<T, MODE, N> end(a, col < a.n ? col : 0, batch);
+    const Epilogue<Out, MODE, N> end(a, col < a.n ? col : 0, batch);
 #pragma unroll
     for (int x0 = 0; x0 < FM; x0 += kRowsAt / 16) {
         through(x0);
@@ -749,13 +861,13 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) 
             // what lies beside the next rows is read while these are worked on
             Row next[kGroup];
             beside(16 * x0 + (p + kGroup) * kPass, next);
-            Piece<T, N> image[kGroup];
-            if (Epilogue<T, MODE, N>::kImage && a.image && col < a.n) {
+            Piece<Out, N> image[kGroup];
+            if (Epilogue<Out, MODE, N>::kImage && a.image && col < a.n) {
 #pragma unroll
                 for (int q = 0; q < kGroup; ++q) {
                     const int64_t row = row0 + wm + 16 * x0 + (p + q) * kPass + lane / kLanes;
                     if (row < row_end)
-                        image[q].read(static_cast<const T *>(a.image) + row * a.n + col, end.left);
+                        image[q].read(static_cast<const Out *>(a.image) + row * a.n + col, end.left);
                 }
             }
 #pragma unroll
@@ -945,7 +1057,7 @@ __global__ __launch_bounds__(WAVES * 64) void rows_kernel(ProductArgs a, int by_
     }
 }
 
-template <typename T, int MODE, int LIST, bool DMA, int TM, int TN, int WM, int WN>
+template <typename T, typename Out, int MODE, int LIST, bool DMA, int TM, int TN, int WM, int WN>
 hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
     constexpr int kCols = MODE == kPair ? TN / 2 : TN;
     const int64_t tn = (a.n + kCols - 1) / kCols;
@@ -953,8 +1065,8 @@ hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
                        : a.offsets     ? a.m / TM + a.experts
                                        : (a.m + TM - 1) / TM;
     if (!grid_holds(tm * tn, WM * WN * 64)) return hipErrorInvalidValue;
-    constexpr int kLds = 2 * (TM + TN) * 128;
-    const auto kernel = product_kernel<T, MODE, LIST, DMA, TM, TN, WM, WN>;
+    constexpr int kLds = 2 * ((TM + TN) * 128 + (sizeof(T) == 1 ? WM * WN * 64 * 4 : 0));
+    const auto kernel = product_kernel<T, Out, MODE, LIST, DMA, TM, TN, WM, WN>;
     if (kLds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
@@ -965,8 +1077,8 @@ hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
         const int64_t quads = a.partial_rows * ((a.n + 3) / 4);
         if (!grid_holds((quads + 255) / 256, 256)) return hipErrorInvalidValue;
         const unsigned blocks = (unsigned)((quads + 255) / 256);
-        if constexpr (MODE == kPair) join_pair_kernel<T><<<blocks, 256, 0, stream>>>(a, tn * TN);
-        else join_kernel<T, MODE><<<blocks, 256, 0, stream>>>(a, tn * TN);
+        if constexpr (MODE == kPair) join_pair_kernel<Out><<<blocks, 256, 0, stream>>>(a, tn * TN);
+        else join_kernel<Out, MODE><<<blocks, 256, 0, stream>>>(a, tn * TN);
     }
     return hipGetLastError();
 }
@@ -975,12 +1087,12 @@ hipError_t launch_tiles(const ProductArgs &a, hipStream_t stream) {
 template <typename T, int MODE, int LIST>
 hipError_t launch_mode(const ProductArgs &a, const ProductPlan &p, hipStream_t stream) {
     if (!p.aligned)
-        return p.tile == 128 ? launch_tiles<T, MODE, LIST, false, 128, 128, 2, 2>(a, stream)
-                             : launch_tiles<T, MODE, LIST, false, 64, 64, 2, 2>(a, stream);
+        return p.tile == 128 ? launch_tiles<T, T, MODE, LIST, false, 128, 128, 2, 2>(a, stream)
+                             : launch_tiles<T, T, MODE, LIST, false, 64, 64, 2, 2>(a, stream);
     switch (p.tile) {
-        case 256: return launch_tiles<T, MODE, LIST, true, 256, 256, 2, 4>(a, stream);
-        case 128: return launch_tiles<T, MODE, LIST, true, 128, 128, 2, 2>(a, stream);
-        default: return launch_tiles<T, MODE, LIST, true, 64, 64, 2, 2>(a, stream);
+        case 256: return launch_tiles<T, T, MODE, LIST, true, 256, 256, 2, 4>(a, stream);
+        case 128: return launch_tiles<T, T, MODE, LIST, true, 128, 128, 2, 2>(a, stream);
+        default: return launch_tiles<T, T, MODE, LIST, true, 64, 64, 2, 2>(a, stream);
     }
 }
 

@@ -33,7 +33,7 @@ from . import SomError, _check, lib as _lib
 
 __all__ = [
     "ACTIVATIONS", "GATES", "EXPORTED", "SomError", "Routing", "ExpertsGradient", "AdamW", "linear",
-    "linear_backward", "gated", "gated_backward", "norm", "norm_backward", "route", "route_backward", "dispatch", "distill", "distill_backward", "experts", "experts_backward",
+    "linear_backward", "Blocks", "to_blocks", "linear8", "gated", "gated_backward", "norm", "norm_backward", "route", "route_backward", "dispatch", "distill", "distill_backward", "experts", "experts_backward",
     "gate_from_map",
 ]
 
@@ -41,10 +41,12 @@ ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 GATES = {"softmax": 0, "sigmoid": 1}
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 STATE_BLOCK = 256
+BLOCK = 128
 
 # Every symbol include/som_local.h declares.
 EXPORTED = (
     "som_linear_workspace", "som_linear_route", "som_linear", "som_linear_backward",
+    "som_to_blocks", "som_linear8_workspace", "som_linear8",
     "som_gated_workspace", "som_gated_route", "som_gated", "som_gated_backward",
     "som_experts_workspace", "som_experts_route", "som_experts", "som_experts_backward",
     "som_norm_workspace", "som_norm", "som_norm_backward",
@@ -63,6 +65,26 @@ class _LinearCall(C.Structure):
                 ("residual", C.c_void_p), ("ldr", C.c_int64), ("y", C.c_void_p),
                 ("z", C.c_void_p), ("dy", C.c_void_p), ("lddy", C.c_int64),
                 ("dx", C.c_void_p), ("dw", C.c_void_p), ("dbias", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+                ("stream", C.c_void_p)]
+
+
+class _BlocksCall(C.Structure):
+    """``som_blocks_call`` of include/som_local.h."""
+
+    _fields_ = [("type", C.c_int32), ("width", C.c_int32), ("n", C.c_int64),
+                ("x", C.c_void_p), ("ldx", C.c_int64), ("codes", C.c_void_p),
+                ("scale", C.c_void_p), ("stream", C.c_void_p)]
+
+
+class _Linear8Call(C.Structure):
+    """``som_linear8_call`` of include/som_local.h."""
+
+    _fields_ = [("type", C.c_int32), ("activation", C.c_int32), ("n", C.c_int64),
+                ("inner", C.c_int32), ("outer", C.c_int32), ("x", C.c_void_p),
+                ("ldx", C.c_int64), ("x_codes", C.c_void_p), ("x_scale", C.c_void_p),
+                ("w_codes", C.c_void_p), ("w_scale", C.c_void_p), ("bias", C.c_void_p),
+                ("residual", C.c_void_p), ("ldr", C.c_int64), ("y", C.c_void_p),
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
                 ("stream", C.c_void_p)]
 
@@ -155,6 +177,9 @@ def lib():
         "som_linear_route": [C.POINTER(_LinearCall), i32, C.POINTER(i32)],
         "som_linear": [C.POINTER(_LinearCall)],
         "som_linear_backward": [C.POINTER(_LinearCall)],
+        "som_to_blocks": [C.POINTER(_BlocksCall)],
+        "som_linear8_workspace": [C.POINTER(_Linear8Call), C.POINTER(u64)],
+        "som_linear8": [C.POINTER(_Linear8Call)],
         "som_gated_workspace": [C.POINTER(_GatedCall), i32, C.POINTER(u64)],
         "som_gated_route": [C.POINTER(_GatedCall), i32, C.POINTER(i32)],
         "som_gated": [C.POINTER(_GatedCall)],
@@ -323,6 +348,104 @@ def linear_backward(dy, x, w, z=None, activation: str = "none", bias: bool = Tru
     call.dx, call.dw, call.dbias = _ptr(dx), _ptr(dw), _ptr(dbias)
     _run("linear", call, True, x)
     return dx, dw, dbias
+
+
+# ------------------------------------------------------- products in 8 bits
+class Blocks:
+    """A matrix of rows of ``width`` values in 8 bits: ``codes`` (rows, width filled up with
+    zeros to whole blocks of 128) float8_e4m3fn, ``scale`` (rows, its blocks filled up
+    with ones to a multiple of four) float8_e8m0fnu, one to a block.  Made by
+    ``to_blocks``, or of such arrays (a checkpoint's)."""
+
+    __slots__ = ("codes", "scale", "width")
+
+    def __init__(self, codes, scale, width: int):
+        blocks = -(-width // BLOCK)
+        for t, dtype, cols, what in ((codes, torch.float8_e4m3fn, blocks * BLOCK, "codes"),
+                                     (scale, torch.float8_e8m0fnu, -(-blocks // 4) * 4, "scale")):
+            if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda:
+                raise TypeError(f"{what} must be {str(dtype).removeprefix('torch.')} on the GPU")
+            if t.dim() != 2 or t.shape[1] != cols or width < 1 or not t.is_contiguous():
+                raise ValueError(f"{what} must be (rows, {cols}) and contiguous")
+        if codes.shape[0] != scale.shape[0] or codes.device != scale.device:
+            raise ValueError("codes and scale must have the same rows, on one GPU")
+        self.codes, self.scale, self.width = codes, scale, width
+
+    @property
+    def shape(self):
+        return (self.codes.shape[0], self.width)
+
+    @property
+    def device(self):
+        return self.codes.device
+
+    def float(self):
+        """The values that are held, fp32."""
+        blocks = self.codes.shape[1] // BLOCK
+        v = self.codes.float().view(-1, blocks, BLOCK)
+        v = v * self.scale[:, :blocks].float().unsqueeze(2)
+        return v.view(-1, blocks * BLOCK)[:, :self.width]
+
+
+def to_blocks(x) -> Blocks:
+    """The rows of x (n, width) in 8 bits, 128 neighbours to a scale: the least power of
+    two that brings their largest magnitude to 448 or below."""
+    code = _type(x, "x")
+    _rows(x, "x")
+    n, width = x.shape
+    if not width:
+        raise ValueError("x must have columns")
+    blocks = -(-width // BLOCK)
+    codes = torch.empty((n, blocks * BLOCK), dtype=torch.float8_e4m3fn, device=x.device)
+    scale = torch.empty((n, -(-blocks // 4) * 4), dtype=torch.float8_e8m0fnu, device=x.device)
+    call = _BlocksCall(code, width, n, _ptr(x), _ld(x), _ptr(codes), _ptr(scale), _stream(x))
+    _check(lib().som_to_blocks(C.byref(call)), "som_to_blocks")
+    return Blocks(codes, scale, width)
+
+
+def linear8(x, w: Blocks, bias=None, activation: str = "none", residual=None, dtype=None):
+    """y = act(x wᵀ + bias) + residual with both matrices in 8 bits: w (outer, inner)
+    Blocks, x (n, inner) bf16 or fp16, which the call brings to 8 bits as ``to_blocks``
+    does, or Blocks, with the ``dtype`` that y is to have."""
+    if not isinstance(w, Blocks):
+        raise TypeError("w must be Blocks (to_blocks)")
+    n, inner = x.shape
+    outer = w.shape[0]
+    if isinstance(x, Blocks):
+        if dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError("dtype must be bfloat16 or float16")
+        call = _Linear8Call(x_codes=_ptr(x.codes), x_scale=_ptr(x.scale))
+        like = torch.empty(0, dtype=dtype, device=x.device)
+    else:
+        _type(x, "x")
+        _rows(x, "x")
+        if x.dtype == torch.float32 or dtype not in (None, x.dtype):
+            raise TypeError("x must be bfloat16 or float16, and dtype the same")
+        call = _Linear8Call(x=_ptr(x), ldx=_ld(x))
+        like = x
+    if w.width != inner or not outer:
+        raise ValueError(f"w must hold rows of {inner}")
+    if w.device != x.device:
+        raise ValueError(f"w must be on {x.device}")
+    call.type, call.activation = _TYPES[like.dtype], _of(ACTIVATIONS, activation, "activation")
+    call.n, call.inner, call.outer = n, inner, outer
+    call.w_codes, call.w_scale = _ptr(w.codes), _ptr(w.scale)
+    if bias is not None:
+        _like(bias, like, (outer,), "bias")
+        call.bias = _ptr(bias)
+    if residual is not None:
+        _like(residual, like, (n, outer), "residual", packed=False)
+        call.residual, call.ldr = _ptr(residual), _ld(residual)
+    y = torch.empty((n, outer), dtype=like.dtype, device=x.device)
+    call.y, call.stream = _ptr(y), _stream(y)
+    L, need = lib(), C.c_uint64()
+    at = C.byref(call)
+    _check(L.som_linear8_workspace(at, C.byref(need)), "som_linear8")
+    if need.value:
+        work = torch.empty(need.value, dtype=torch.uint8, device=x.device)
+        call.workspace, call.workspace_bytes = work.data_ptr(), need.value
+    _check(L.som_linear8(at), "som_linear8")
+    return y
 
 
 # -------------------------------------------------------------- gated layer

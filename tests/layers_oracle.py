@@ -231,3 +231,50 @@ def gated_backward(dy, x, w, z, kind, dtype):
     return {"dx": (dx, dx_err + stored(dx, dtype)),
             "dw": ((dw).view(2, hidden, k), (dw_err + stored(dw, dtype)).view(2, hidden, k)),
             "db": (db.view(2, hidden), (db_err + stored(db, dtype)).view(2, hidden))}
+
+
+# ------------------------------------------------------------ blocks of 8 bits
+BLOCK = 128
+
+
+def blocks(x):
+    """(values, exponents): what e4m3 holds of the rows of x (n, width) with a power of
+    two to 128 neighbours, each rounded to the nearest, ties to even.  In 64 bits every
+    step is exact."""
+    n, width = x.shape
+    count = -(-width // BLOCK)
+    full = torch.zeros(n, count * BLOCK, dtype=torch.float64, device=x.device)
+    full[:, :width] = x
+    full = full.view(n, count, BLOCK)
+    size = torch.where(torch.isfinite(full), full.abs(), torch.zeros_like(full)).amax(2)
+    m, e = torch.frexp(size)                    # size = m 2^e, 1/2 <= m < 1; 448 = 0.875 2^9
+    e = torch.where(size > 0, e - 9 + (m > 0.875).int(), torch.full_like(e, -126)).clamp(min=-126)
+    u = full * torch.exp2(-e.double()).unsqueeze(2)
+    finite = torch.isfinite(u)
+    step = torch.exp2(torch.floor(torch.log2(torch.where(finite, u.abs(), u * 0 + 1).clamp(min=2.0 ** -6))) - 3)
+    held = torch.where(finite, (u / step).round() * step, torch.full_like(u, math.nan))
+    return (held * torch.exp2(e.double()).unsqueeze(2)).view(n, -1)[:, :width], e
+
+
+def linear8(x, w, b, kind, r, dtype):
+    """(y, bound) of a product of held values x (n, inner) and w (outer, inner).
+
+    The matrix instruction brings eight neighbouring products at a time to the largest
+    one's exponent and drops what lies 13 bits below it: each of the eight is off by less
+    than 2^-13 of the power of two at or below the largest, all by at most 2^-10 of it."""
+    n, inner = x.shape
+    pad = -inner % 8
+    xs = torch.nn.functional.pad(x, (0, pad)).view(n, 1, -1, 8)
+    ws = torch.nn.functional.pad(w, (0, pad)).view(1, w.shape[0], -1, 8)
+    most = torch.zeros(n, w.shape[0], dtype=torch.float64, device=x.device)
+    for i in range(0, n, 64):       # eight products at a time, of 64 rows
+        most[i:i + 64] = (xs[i:i + 64] * ws).abs().amax(3).sum(2)
+    z = x @ w.t() + (0 if b is None else b)
+    size = x.abs() @ w.abs().t() + (0 if b is None else b.abs())
+    zerr = 2.0 ** -10 * most + (inner + 8) * V * size
+    y = L.act(z, kind)
+    err = L.SLOPE[kind] * zerr + 8 * V * z.abs()
+    if r is not None:
+        y = y + r
+        err = err + 4 * V * r.abs()
+    return y, err + stored(y, dtype)
