@@ -9,7 +9,9 @@
 // A row stays in registers as it was read, 16-byte pieces of it to a lane, of 1 to 64
 // lanes or of a workgroup; only rows beyond what a workgroup holds are read twice.  R is
 // summed by itself (Z less the teacher's classes would cancel): the teacher's classes are
-// marked by bits in LDS, of which a piece of a row takes its own in one read.
+// marked by bits in LDS, of which a piece of a row takes its own in one read.  All
+// gradients are written as if no class were named, and the few that are once more behind a
+// barrier: testing for them on the way took 35 us of 198 (16,001 bf16 rows of 10,000).
 #include "som_row.h"
 
 #include <algorithm>
@@ -21,19 +23,18 @@ namespace {
 constexpr float kLog2e = 1.44269504f;
 
 // What the teacher says of a workgroup's rows, in LDS: for each row bits of its classes,
-// its entries (a class, or -1 for none, and its probability) and its rest.
+// its entries (a class, or -1 for none, its probability and its logit) and its rest.
+inline __host__ __device__ int taught_words(const DistillArgs &a) { return a.words + 3 * a.k + 2; }
 struct Taught {
     uint32_t *bits;
     int *index;
-    float *p, *rest;
-    int words, k;
-    __device__ Taught(char *lds, int rows, int row, const DistillArgs &a) {
-        words = a.words, k = a.k;
-        const int each = words + 2 * k + 2;
-        bits = reinterpret_cast<uint32_t *>(lds) + row * each;
-        index = reinterpret_cast<int *>(bits + words);
-        p = reinterpret_cast<float *>(index + k);
-        rest = p + k;   // the rest; 1 where there is a teacher, 0 where not, NaN for NaN
+    float *p, *logit, *rest;
+    __device__ Taught(char *lds, int row, const DistillArgs &a) {
+        bits = reinterpret_cast<uint32_t *>(lds) + row * taught_words(a);
+        index = reinterpret_cast<int *>(bits + a.words);
+        p = reinterpret_cast<float *>(index + a.k);
+        logit = p + a.k;
+        rest = logit + a.k;   // the rest; 1 where there is a teacher, 0 where not, NaN for NaN
     }
     // The marks of the N classes from `at` on.
     template <int N>
@@ -41,12 +42,6 @@ struct Taught {
         const uint32_t *const w = bits + (at >> 5);
         const uint64_t both = (uint64_t)w[1] << 32 | w[0];
         return (uint32_t)(both >> (at & 31)) & ((1u << N) - 1);
-    }
-    // The teacher's probability of class c (entries of the same class add up).
-    __device__ float of(int c) const {
-        float v = 0.f;
-        for (int j = 0; j < k; ++j) v += index[j] == c ? p[j] : 0.f;
-        return v;
     }
 };
 
@@ -62,19 +57,22 @@ __device__ inline float lanes_sum(float v, int lanes) {
     return v;
 }
 
-// The entries of a row, by `lanes` lanes of one wave that cover the row's `lane` 0 ..
+// The entries of row s, by `lanes` lanes of one wave that cover the row's `lane` 0 ..
 // The bits are zeros before.
-__device__ inline void teach(const DistillArgs &a, const Taught &t, int64_t row, bool there, int lane,
-                             int lanes) {
-    float best = -INFINITY, sum = 0.f;
+template <typename T>
+__device__ inline void teach(const DistillArgs &a, const Taught &t, const T *s, int64_t row,
+                             bool there, int lane, int lanes) {
+    float best = -INFINITY, sum = 0.f, rest = a.rest && there ? a.rest[row] : 0.f;
     for (int j = lane; j < a.k; j += lanes) {
-        const int64_t s = row * a.k + j;
-        int c = there ? a.index[s] : -1;
+        const int64_t at = row * a.k + j;
+        int c = there ? a.index[at] : -1;
+        const float said = there ? wide(a.teacher, a.teacher_type, at) : 0.f;
         if (c < 0 || c >= a.classes) c = -1;
-        const float v = c >= 0 ? wide(a.teacher, a.teacher_type, s) / a.temperature : -INFINITY;
+        const float v = c >= 0 ? said / a.temperature : -INFINITY;
         t.index[j] = c;
         t.p[j] = v;
-        if (c >= 0) atomicOr(t.bits + (c >> 5), 1u << (c & 31));
+        t.logit[j] = c >= 0 ? (float)s[c] : 0.f;
+        if (a.words && c >= 0) atomicOr(t.bits + (c >> 5), 1u << (c & 31));
         best = fmaxf(best, v);
     }
     for (int o = 1; o < lanes; o <<= 1) best = fmaxf(best, __shfl_xor(best, o));
@@ -85,11 +83,7 @@ __device__ inline void teach(const DistillArgs &a, const Taught &t, int64_t row,
         sum += e;
     }
     sum = lanes_sum(sum, lanes);
-    float rest = 0.f;
-    if (a.rest && there) {
-        rest = a.rest[row];
-        rest = rest <= 0.f || sum == 0.f ? 0.f : rest;
-    }
+    rest = rest <= 0.f || sum == 0.f ? 0.f : rest;
     const float by = (1.f - rest) / (sum == 0.f ? 1.f : sum);
     for (int j = lane; j < a.k; j += lanes) t.p[j] *= by;
     if (lane == 0) {
@@ -111,6 +105,41 @@ __device__ inline void keep_raw(Piece<T, 16 / sizeof(T)> (&x)[P]) {
     }
 }
 
+// How labels' exponentials come.  At temperatures of 1, 2 and 4 they are the others', squared
+// none, one or two times, off by no more than by themselves: the error of the product in the
+// exponent doubles with the exponent either way.  (16,001 bf16 rows of 10,000 at 2: XXX.)
+enum : int { kNoLabels = 0, kOwn = 1, kSame = 2, kSquared = 3, kTwice = 4 };
+
+// 2^((v - top) c) of N logits and, with labels, e^(v - top).
+template <int HARD, int N>
+__device__ inline void powers(const float (&v)[N], float top, float c, float (&soft)[N],
+                              float (&hard)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const float u = v[e] - top;
+        soft[e] = __builtin_amdgcn_exp2f(u * c);
+        if (HARD == kOwn) hard[e] = __builtin_amdgcn_exp2f(u * kLog2e);
+        if (HARD >= kSame) hard[e] = soft[e];
+        if (HARD >= kSquared) hard[e] *= hard[e];
+        if (HARD >= kTwice) hard[e] *= hard[e];
+    }
+}
+
+// What a row has beside its teacher, read while its logits are on their way.
+struct Beside {
+    float scale, logit;   // of the gradient; the label's
+    int at;               // the label's class, or -1
+    template <int HARD, typename T>
+    __device__ static Beside of(const DistillArgs &a, const T *s, int64_t row, bool there) {
+        Beside b;
+        b.scale = a.dloss && there ? a.scale * a.dloss[row] : a.scale;
+        b.at = HARD && there ? a.label[row] : -1;
+        if (b.at >= a.classes || b.at < 0) b.at = -1;
+        b.logit = b.at >= 0 ? (float)s[b.at] : 0.f;
+        return b;
+    }
+};
+
 // What a row's sums give.
 struct Factors {
     float z, r, e;                  // the sums
@@ -118,20 +147,13 @@ struct Factors {
     float given;                    // of the teacher's probability
     float label;                    // of the label's class
     bool shut;                      // a row without an open class
-    int at;                         // the label's class, or -1
-    template <bool HARD>
-    __device__ static Factors of(const DistillArgs &a, const Taught &t, int64_t row, float top,
+    template <int HARD>
+    __device__ static Factors of(const DistillArgs &a, const Taught &t, const Beside &b, float top,
                                  float z, float r, float e) {
         Factors f;
         f.z = z, f.r = r, f.e = e, f.top = top;
         f.shut = z == 0.f;
-        f.at = -1;
-        if (HARD) {
-            f.at = a.label[row];
-            if (f.at < 0 || f.at >= a.classes) f.at = -1;
-        }
-        const float scale = a.scale * (a.dloss ? a.dloss[row] : 1.f);
-        const float soft = scale * a.mix * a.temperature, hard = scale * (1.f - a.mix);
+        const float soft = b.scale * a.mix * a.temperature, hard = b.scale * (1.f - a.mix);
         f.chosen = f.other = f.given = f.one = f.label = 0.f;
         if (f.shut) return f;
         if (a.k && a.mix != 0.f && !(t.rest[1] == 0.f)) {
@@ -141,27 +163,27 @@ struct Factors {
             // the classes that the teacher left out, whose sum is to be its rest
             if (t.rest[0] != 0.f) f.other = r == 0.f ? 0.f : f.chosen * (1.f - t.rest[0] * (z / r));
         }
-        if (HARD && f.at >= 0) f.one = hard / e, f.label = hard;
+        if (HARD && b.at >= 0) f.one = hard / e, f.label = hard;
         return f;
     }
 };
 
 // The row's loss, by `lanes` lanes of one wave.
-template <typename T, bool HARD>
-__device__ inline float loss_of(const DistillArgs &a, const Taught &t, const Factors &f, const T *s,
+template <int HARD>
+__device__ inline float loss_of(const DistillArgs &a, const Taught &t, const Factors &f, const Beside &b,
                                 int lane, int lanes) {
     if (f.shut) return 0.f;
     float soft = 0.f, all = 0.f;
     // half of a logit's distance from the maximum: the whole may pass fp32's range where
     // its product with a probability does not
-    const auto half_below = [&](T v) { return 0.5f * (float)v - 0.5f * f.top; };
+    const auto half_below = [&](float v) { return 0.5f * v - 0.5f * f.top; };
     if (a.k && a.mix != 0.f) {
         const float log_z = logf(f.z);
         for (int j = lane; j < a.k; j += lanes) {
             const float p = t.p[j];
             if (t.index[j] < 0 || p == 0.f) continue;
             soft = fmaf(p, logf(p) + log_z, soft);
-            soft -= 2.f * (p * (half_below(s[t.index[j]]) / a.temperature));
+            soft -= 2.f * (p * (half_below(t.logit[j]) / a.temperature));
         }
         soft = lanes_sum(soft, lanes);
         const float rest = t.rest[0];
@@ -169,32 +191,54 @@ __device__ inline float loss_of(const DistillArgs &a, const Taught &t, const Fac
         if (t.rest[1] != 1.f) soft = t.rest[1];   // 0 or NaN
         all = a.mix * a.temperature * a.temperature * soft;
     }
-    if (HARD && f.at >= 0) {
+    if (HARD && b.at >= 0) {
         const float part = 1.f - a.mix;
-        all += fmaf(part, logf(f.e), -2.f * (part * half_below(s[f.at])));
+        all += fmaf(part, logf(f.e), -2.f * (part * half_below(b.logit)));
     }
     return all;
 }
 
-// The gradient of N neighbouring logits v of classes `at` .., marked `marks`.
-template <bool HARD, int N>
-__device__ inline void slopes(const Taught &t, const Factors &f, float c, int at, uint32_t marks,
-                              float (&v)[N]) {
+// The gradient of N neighbouring logits v, as of classes that neither the teacher nor the
+// label names.
+template <int HARD, int N>
+__device__ inline void slopes(const Factors &f, float c, float (&v)[N]) {
+    float soft[N], hard[N];
+    powers<HARD>(v, f.top, c, soft, hard);
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-        const float u = v[e] - f.top;
-        const float w = f.other * __builtin_amdgcn_exp2f(u * c);
-        v[e] = HARD ? fmaf(f.one, __builtin_amdgcn_exp2f(u * kLog2e), w) : w;
-        if (marks >> e & 1) {   // few
-            v[e] = f.chosen * __builtin_amdgcn_exp2f(u * c) - f.given * t.of(at + e);
-            if (HARD) v[e] = fmaf(f.one, __builtin_amdgcn_exp2f(u * kLog2e), v[e]);
-        }
-        if (HARD && f.at == at + e) v[e] -= f.label;
-        if (f.shut) v[e] = 0.f;
+        v[e] = f.other * soft[e];
+        if (HARD) v[e] = fmaf(f.one, hard[e], v[e]);
     }
 }
 
-template <typename T, int P, bool WIDE, bool HARD>
+// The named classes' gradients, written over those, by `lanes` lanes of one wave.  All of
+// a row's other writes come before (a barrier); classes that are named more than once
+// are written by several lanes, all alike.
+template <typename T, int HARD>
+__device__ inline void named(const DistillArgs &a, const Taught &t, const Factors &f, const Beside &b,
+                             T *to, float c, int lane, int lanes) {
+    for (int j = lane; j < a.k + (HARD ? 1 : 0); j += lanes) {
+        const int at = j < a.k ? t.index[j] : b.at;
+        if (at < 0) continue;
+        float p = 0.f;
+        bool taught = false;
+        for (int i = 0; i < a.k; ++i) {
+            const bool same = t.index[i] == at;
+            p += same ? t.p[i] : 0.f;
+            taught = taught || same;
+        }
+        const float logit[1] = {j < a.k ? t.logit[j] : b.logit};
+        float soft[1], hard[1];
+        powers<HARD>(logit, f.top, c, soft, hard);
+        float v = (taught ? f.chosen : f.other) * soft[0];
+        if (taught) v -= f.given * p;
+        if (HARD) v = fmaf(f.one, hard[0], v);
+        if (HARD && at == b.at) v -= f.label;
+        to[at] = (T)v;
+    }
+}
+
+template <typename T, int P, bool WIDE, int HARD>
 __global__ __launch_bounds__(1024) void distill_kernel(DistillArgs a) {
     constexpr int N = 16 / sizeof(T);
     extern __shared__ char lds[];
@@ -207,13 +251,14 @@ __global__ __launch_bounds__(1024) void distill_kernel(DistillArgs a) {
     Piece<T, N> x[P];
 #pragma unroll
     for (int p = 0; p < P; ++p) me.template read<T>(s, 0, p, there, x[p]);
-    const Taught t(lds, me.rows, me.row, a);
+    const Beside beside = Beside::of<HARD>(a, s, row, there);
+    const Taught t(lds, me.row, a);
     const bool first = !WIDE || threadIdx.x < 64;      // those that deal with entries
     const int lanes = WIDE ? 64 : a.lanes;
     if (a.k) {
         for (int w = me.lane; w < a.words; w += a.lanes) t.bits[w] = 0;
         __syncthreads();
-        if (first) teach(a, t, row, there, me.lane, lanes);
+        if (first) teach(a, t, s, row, there, me.lane, lanes);
         if (!WIDE) __syncthreads();                    // otherwise the maximum's
     }
     // -infinity where a piece is not this lane's
@@ -242,12 +287,13 @@ __global__ __launch_bounds__(1024) void distill_kernel(DistillArgs a) {
     for (int p = 0; p < P; ++p) {
         float v[N];
         values(p, v);
-        const uint32_t marks = a.k && me.mine(p) ? t.template marks<N>(me.at[p]) : 0u;
+        const uint32_t marks = a.words && me.mine(p) ? t.template marks<N>(me.at[p]) : 0u;
+        float soft[N], hard[N];
+        powers<HARD>(v, from, c, soft, hard);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            v[e] -= from;
-            if (HARD) sums[2] += __builtin_amdgcn_exp2f(v[e] * kLog2e);
-            v[e] = __builtin_amdgcn_exp2f(v[e] * c);
+            v[e] = soft[e];
+            if (HARD) sums[2] += hard[e];
         }
         if (marks) {
 #pragma unroll
@@ -263,80 +309,101 @@ __global__ __launch_bounds__(1024) void distill_kernel(DistillArgs a) {
     keep_raw<T, P>(x);
     if (!there) return;
     const Factors f =
-        Factors::of<HARD>(a, t, row, from, sums[0] + sums[1], sums[1], sums[2]);
-    if (a.loss && first) {
-        const float loss = loss_of<T, HARD>(a, t, f, s, me.lane, lanes);
-        if (me.lane == 0) a.loss[row] = loss;
-    }
-    if (!a.dlogits) return;
+        Factors::of<HARD>(a, t, beside, from, sums[0] + sums[1], sums[1], sums[2]);
+    T *const to = static_cast<T *>(a.dlogits) + row * a.classes;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        if (!me.mine(p)) continue;
+        if (!a.dlogits || !me.mine(p)) continue;
         float v[N];
         Piece<T, N> out;
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = (float)x[p].v[e];
-        slopes<HARD>(t, f, c, me.at[p], a.k ? t.template marks<N>(me.at[p]) : 0u, v);
+        slopes<HARD>(f, c, v);
 #pragma unroll
         for (int e = 0; e < N; ++e) out.v[e] = (T)v[e];
-        out.write(static_cast<T *>(a.dlogits) + row * a.classes + me.at[p], N);
+        out.write(to + me.at[p], N);
+    }
+    if (WIDE) __syncthreads();
+    else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");   // one wave
+    if (!first) return;
+    if (a.dlogits) named<T, HARD>(a, t, f, beside, to, c, me.lane, lanes);
+    if (a.loss) {
+        const float loss = loss_of<HARD>(a, t, f, beside, me.lane, lanes);
+        if (me.lane == 0) a.loss[row] = loss;
     }
 }
 
 // Rows that a workgroup does not hold, and rows shorter than a piece: read twice, with
 // the maximum and the sums of what a lane has seen so far in the first pass.
-template <typename T, bool HARD>
+template <typename T, int HARD>
 __global__ __launch_bounds__(1024) void distill_long_kernel(DistillArgs a) {
-    constexpr int N = 16 / sizeof(T);
+    constexpr int N = 16 / sizeof(T), kAhead = 4;
     extern __shared__ char lds[];
     __shared__ float part[kPart];
     int turn = 0;
     const int64_t row = blockIdx.x;
     const T *const s = static_cast<const T *>(a.logits) + row * a.lds;
-    const Taught t(lds, 1, 0, a);
+    const Beside beside = Beside::of<HARD>(a, s, row, true);
+    const Taught t(lds, 0, a);
     const bool first = threadIdx.x < 64;
     if (a.k) {
         for (int w = threadIdx.x; w < a.words; w += blockDim.x) t.bits[w] = 0;
         __syncthreads();
-        if (first) teach(a, t, row, true, threadIdx.x, 64);
+        if (first) teach(a, t, s, row, true, threadIdx.x, 64);
         __syncthreads();
     }
     const float c = kLog2e / a.temperature;
     const int stride = blockDim.x * N;
     float top[1] = {-INFINITY}, from = 0.f, sums[3] = {0.f, 0.f, 0.f};
-    for (int at = threadIdx.x * N; at < a.classes; at += stride) {
-        const int left = a.classes - at < N ? a.classes - at : N;
-        Piece<T, N> x;
-        x.read(s + at, left);
-        float v[N], most = -INFINITY;
+    // kAhead pieces of this lane are read together, from class `at` on
+    const auto read = [&](int at, Piece<T, N> (&x)[kAhead]) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            v[e] = e < left ? (float)x.v[e] : -INFINITY;
-            most = fmaxf(most, v[e]);
+        for (int q = 0; q < kAhead; ++q) {
+            const int left = a.classes - (at + q * stride);
+            x[q].read(s + at + q * stride, left < 0 ? 0 : left < N ? left : N);
         }
-        if (most > top[0]) {
-            const float u = top[0] > -INFINITY ? from - most : 0.f;   // sums of nothing stay 0
-            sums[0] *= __builtin_amdgcn_exp2f(u * c);
-            sums[1] *= __builtin_amdgcn_exp2f(u * c);
-            if (HARD) sums[2] *= __builtin_amdgcn_exp2f(u * kLog2e);
-            top[0] = from = most;
-        }
-        const uint32_t marks = a.k ? t.template marks<N>(at) : 0u;
+    };
+    for (int first_at = threadIdx.x * N; first_at < a.classes; first_at += kAhead * stride) {
+        Piece<T, N> x[kAhead];
+        read(first_at, x);
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            v[e] -= from;
-            if (HARD) sums[2] += __builtin_amdgcn_exp2f(v[e] * kLog2e);
-            v[e] = __builtin_amdgcn_exp2f(v[e] * c);
-        }
-        if (marks) {
+        for (int q = 0; q < kAhead; ++q) {
+            const int at = first_at + q * stride, left = a.classes - at;
+            if (left <= 0) break;
+            float v[N], most = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = (float)x[q].v[e];
+            if (left < N) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[e] = e < left ? v[e] : -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e) most = fmaxf(most, v[e]);
+            if (most > top[0]) {
+                const float u = top[0] > -INFINITY ? from - most : 0.f;   // sums of nothing stay 0
+                sums[0] *= __builtin_amdgcn_exp2f(u * c);
+                sums[1] *= __builtin_amdgcn_exp2f(u * c);
+                if (HARD) sums[2] *= __builtin_amdgcn_exp2f(u * kLog2e);
+                top[0] = from = most;
+            }
+            const uint32_t marks = a.words ? t.template marks<N>(at) : 0u;
+            float soft[N], hard[N];
+            powers<HARD>(v, from, c, soft, hard);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                sums[0] += marks >> e & 1 ? v[e] : 0.f;
-                v[e] = marks >> e & 1 ? 0.f : v[e];
+                v[e] = soft[e];
+                if (HARD) sums[2] += hard[e];
             }
-        }
+            if (marks) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) sums[1] += v[e];
+                for (int e = 0; e < N; ++e) {
+                    sums[0] += marks >> e & 1 ? v[e] : 0.f;
+                    v[e] = marks >> e & 1 ? 0.f : v[e];
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e) sums[1] += v[e];
+        }
     }
     const float mine = top[0];
     row_max<true>(top, 0, part, turn);
@@ -347,24 +414,31 @@ __global__ __launch_bounds__(1024) void distill_long_kernel(DistillArgs a) {
         if (HARD) sums[2] *= __builtin_amdgcn_exp2f((mine - all) * kLog2e);
     }
     row_sum<true>(sums, 0, part, turn);
-    const Factors f = Factors::of<HARD>(a, t, row, all, sums[0] + sums[1], sums[1], sums[2]);
+    const Factors f = Factors::of<HARD>(a, t, beside, all, sums[0] + sums[1], sums[1], sums[2]);
     if (a.loss && first) {
-        const float loss = loss_of<T, HARD>(a, t, f, s, threadIdx.x, 64);
+        const float loss = loss_of<HARD>(a, t, f, beside, threadIdx.x, 64);
         if (threadIdx.x == 0) a.loss[row] = loss;
     }
     if (!a.dlogits) return;
-    for (int at = threadIdx.x * N; at < a.classes; at += stride) {
-        const int left = a.classes - at < N ? a.classes - at : N;
-        Piece<T, N> x;
-        x.read(s + at, left);
-        float v[N];
+    T *const to = static_cast<T *>(a.dlogits) + row * a.classes;
+    for (int first_at = threadIdx.x * N; first_at < a.classes; first_at += kAhead * stride) {
+        Piece<T, N> x[kAhead];
+        read(first_at, x);
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = (float)x.v[e];
-        slopes<HARD>(t, f, c, at, a.k ? t.template marks<N>(at) : 0u, v);
+        for (int q = 0; q < kAhead; ++q) {
+            const int at = first_at + q * stride, left = a.classes - at;
+            if (left <= 0) break;
+            float v[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) x.v[e] = (T)v[e];
-        x.write(static_cast<T *>(a.dlogits) + row * a.classes + at, left);
+            for (int e = 0; e < N; ++e) v[e] = (float)x[q].v[e];
+            slopes<HARD>(f, c, v);
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[q].v[e] = (T)v[e];
+            x[q].write(to + at, left < N ? left : N);
+        }
     }
+    __syncthreads();
+    if (first) named<T, HARD>(a, t, f, beside, to, c, threadIdx.x, 64);
 }
 
 // Pieces that a lane holds: 1 or 2 of a wave's rows, 4 or 8 of a workgroup's (16 are more
@@ -381,14 +455,14 @@ Shape distill_shape(const DistillArgs &a) {
     return s;
 }
 
-template <typename T, int P, bool WIDE, bool HARD>
+template <typename T, int P, bool WIDE, int HARD>
 hipError_t launch_held(const DistillArgs &a, const Shape &s, unsigned groups, unsigned lds,
                        hipStream_t stream) {
     distill_kernel<T, P, WIDE, HARD><<<groups, s.threads, lds, stream>>>(a);
     return hipGetLastError();
 }
 
-template <typename T, bool HARD>
+template <typename T, int HARD>
 hipError_t launch_typed(const DistillArgs &a, const Shape &s, unsigned groups, unsigned lds,
                         hipStream_t stream) {
     if (!s.held) {
@@ -410,6 +484,18 @@ hipError_t launch_typed(const DistillArgs &a, const Shape &s, unsigned groups, u
                          : launch_held<T, 8, true, HARD>(a, s, groups, lds, stream);
 }
 
+template <typename T>
+hipError_t launch_labels(const DistillArgs &a, int hard, const Shape &s, unsigned groups, unsigned lds,
+                         hipStream_t stream) {
+    switch (hard) {
+        case kNoLabels: return launch_typed<T, kNoLabels>(a, s, groups, lds, stream);
+        case kOwn: return launch_typed<T, kOwn>(a, s, groups, lds, stream);
+        case kSame: return launch_typed<T, kSame>(a, s, groups, lds, stream);
+        case kSquared: return launch_typed<T, kSquared>(a, s, groups, lds, stream);
+        default: return launch_typed<T, kTwice>(a, s, groups, lds, stream);
+    }
+}
+
 }  // namespace
 
 hipError_t launch_distill(const DistillArgs &args, hipStream_t stream) {
@@ -417,10 +503,14 @@ hipError_t launch_distill(const DistillArgs &args, hipStream_t stream) {
     const int rows = s.held && !s.wide ? s.threads / s.lanes : 1;
     DistillArgs a = args;
     a.lanes = s.lanes;
-    a.words = a.k ? (a.classes + 31) / 32 + 1 : 0;
-    const unsigned lds = (unsigned)rows * (a.words + 2 * a.k + 2) * 4;
+    a.words = a.k && a.rest ? (a.classes + 31) / 32 + 1 : 0;   // its sum leaves classes out
+    const unsigned lds = (unsigned)rows * taught_words(a) * 4;
     const int size = type_size(a.type);
-    const bool hard = a.label && a.mix != 1.f;
+    const int hard = !a.label || a.mix == 1.f   ? kNoLabels
+                     : a.temperature == 1.f ? kSame
+                     : a.temperature == 2.f ? kSquared
+                     : a.temperature == 4.f ? kTwice
+                                            : kOwn;
     // as many rows at a time as a grid holds
     const int64_t most = (int64_t)(UINT32_MAX / 1024) * rows;
     for (int64_t r = 0; r < args.n; r += most) {
@@ -428,17 +518,9 @@ hipError_t launch_distill(const DistillArgs &args, hipStream_t stream) {
         const unsigned groups = (unsigned)((a.n + rows - 1) / rows);
         hipError_t e;
         switch (a.type) {
-            case kF32:
-                e = hard ? launch_typed<float, true>(a, s, groups, lds, stream)
-                         : launch_typed<float, false>(a, s, groups, lds, stream);
-                break;
-            case kBF16:
-                e = hard ? launch_typed<__bf16, true>(a, s, groups, lds, stream)
-                         : launch_typed<__bf16, false>(a, s, groups, lds, stream);
-                break;
-            default:
-                e = hard ? launch_typed<_Float16, true>(a, s, groups, lds, stream)
-                         : launch_typed<_Float16, false>(a, s, groups, lds, stream);
+            case kF32: e = launch_labels<float>(a, hard, s, groups, lds, stream); break;
+            case kBF16: e = launch_labels<__bf16>(a, hard, s, groups, lds, stream); break;
+            default: e = launch_labels<_Float16>(a, hard, s, groups, lds, stream);
         }
         if (e != hipSuccess) return e;
         a.logits = static_cast<const char *>(a.logits) + a.n * a.lds * size;
