@@ -92,19 +92,6 @@ __device__ inline void teach(const DistillArgs &a, const Taught &t, const T *s, 
     }
 }
 
-// Keeps a row's pieces as they were read between its passes, not the floats that the last
-// pass made of them, which would take more registers than there are.
-template <typename T, int P>
-__device__ inline void keep_raw(Piece<T, 16 / sizeof(T)> (&x)[P]) {
-    typedef int Raw __attribute__((ext_vector_type(4)));
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-        Raw raw = __builtin_bit_cast(Raw, x[p].v);
-        asm volatile("" : "+v"(raw));
-        x[p].v = __builtin_bit_cast(decltype(x[p].v), raw);
-    }
-}
-
 // How labels' exponentials come.  At temperatures of 1, 2 and 4 they are the others', squared
 // none, one or two times, off by no more than by themselves: the error of the product in the
 // exponent doubles with the exponent either way.  (16,001 bf16 rows of 10,000 at 2: XXX.)

@@ -135,9 +135,12 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
     }
 }
 
-// COLUMNS: also the workgroup's parts of dweight and dbias.
-template <typename T, int P, bool WIDE, bool COLUMNS>
-__global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs a) {
+// COLUMNS: also the workgroup's parts of dweight and dbias.  AHEAD: a row's reads are on
+// their way while the one before it is worked on; that takes the registers of a larger
+// workgroup than kAheadThreads.
+constexpr int kAheadThreads = 768;
+template <typename T, int P, bool WIDE, bool COLUMNS, bool AHEAD>
+__global__ __launch_bounds__(AHEAD ? kAheadThreads : 1024) void norm_backward_kernel(NormArgs a) {
     constexpr int N = 16 / sizeof(T);
     extern __shared__ float lds[];
     float *const part = lds;          // kPart
@@ -151,17 +154,35 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormArgs a) {
 #pragma unroll
         for (int e = 0; e < N; ++e) dweight[p][e] = dbias[p][e] = 0.f;
     }
-    for (int64_t r0 = (int64_t)blockIdx.x * me.rows; r0 < a.n; r0 += (int64_t)gridDim.x * me.rows) {
-        const int64_t row = r0 + me.row;
-        const bool there = row < a.n;
+    const int64_t step = (int64_t)gridDim.x * me.rows;
+    struct Row {
         Piece<T, N> x[P], dy[P], beside[P];
-        const float mean = there ? a.kept[2 * row] : 0.f, rstd = there ? a.kept[2 * row + 1] : 0.f;
+        float mean, rstd;
+    } next;
+    const auto read = [&](int64_t row, Row &to) {
+        const bool there = row < a.n;
+        to.mean = there ? a.kept[2 * row] : 0.f;
+        to.rstd = there ? a.kept[2 * row + 1] : 0.f;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            me.template read<T>(a.x, row * a.ldx, p, there, x[p]);
-            me.template read<T>(a.dy, row * a.lddy, p, there, dy[p]);
-            if (a.beside) me.template read<T>(a.beside, row * a.ldb, p, there, beside[p]);
+            me.template read<T>(a.x, row * a.ldx, p, there, to.x[p]);
+            me.template read<T>(a.dy, row * a.lddy, p, there, to.dy[p]);
+            if (a.beside) me.template read<T>(a.beside, row * a.ldb, p, there, to.beside[p]);
         }
+    };
+    if (AHEAD) read((int64_t)blockIdx.x * me.rows + me.row, next);
+    for (int64_t r0 = (int64_t)blockIdx.x * me.rows; r0 < a.n; r0 += step) {
+        const int64_t row = r0 + me.row;
+        const bool there = row < a.n;
+        Row here;
+        if (AHEAD) {
+            here = next;
+            read(row + step, next);
+        } else {
+            read(row, here);
+        }
+        const auto &x = here.x, &dy = here.dy, &beside = here.beside;
+        const float mean = here.mean, rstd = here.rstd;
         float both[2] = {0.f, 0.f};
 #pragma unroll
         for (int p = 0; p < P; ++p) {
@@ -353,19 +374,32 @@ Shape backward_shape(const NormArgs &a) {
                     a.type == kF32 ? kBackwardPieces<float> : kBackwardPieces<__bf16>, 256);
 }
 
-// Workgroups that a launch of row after row takes.
-int64_t groups_of(const NormArgs &a, const Shape &s, int num_cus) {
+constexpr int64_t kPartRows = 3;
+
+// Workgroups of a launch of row after row: as many as run at a time, of `waves` waves to a
+// compute unit.  More of them, which have to wait, read worse (20,000 fp16 rows of 10,000,
+// two workgroups to a compute unit 165 us, three 189, a row each 216).
+int64_t groups_of(const NormArgs &a, const Shape &s, int waves, int num_cus) {
     const int64_t rows = s.held && !s.wide ? s.threads / s.lanes : 1;
-    const int64_t fit = std::max(1, 2048 / s.threads);   // of a compute unit
+    const int64_t fit = std::max(1, waves * 64 / s.threads);
     return std::min((a.n + rows - 1) / rows, num_cus * fit);
 }
+// Waves that a compute unit holds, by the registers that a row's values take.
+int forward_waves(const NormArgs &a, const Shape &s) {
+    const int values = s.pieces * (16 / type_size(a.type));
+    return values <= 8 ? 32 : a.type == kF32 && values > 12 ? 20 : 24;
+}
+int backward_waves(const Shape &s) { return s.pieces <= 1 ? 20 : 12; }
 
 }  // namespace
 
+// Groups of rows whose parts of dweight and dbias are added up apart: the workgroups, each
+// of kPartRows rows or more.
 int32_t norm_parts(const NormArgs &a, int num_cus) {
     const Shape s = backward_shape(a);
     const int64_t rows = s.held && !s.wide ? s.threads / s.lanes : 1;
-    const int64_t groups = s.held ? std::min(groups_of(a, s, num_cus), (a.n + 4 * rows - 1) / (4 * rows))
+    const int64_t groups = s.held ? std::min(groups_of(a, s, backward_waves(s), num_cus),
+                                             (a.n + kPartRows * rows - 1) / (kPartRows * rows))
                                   : std::min<int64_t>((a.n + 15) / 16, num_cus);
     return (int32_t)std::max<int64_t>(1, groups);
 }
@@ -382,7 +416,7 @@ hipError_t launch_join_parts(int32_t type, const float *partial, int32_t parts, 
 hipError_t launch_norm(const NormArgs &args, int num_cus, hipStream_t stream) {
     NormArgs a = args;
     const Shape s = forward_shape(a);
-    const unsigned groups = (unsigned)groups_of(a, s, num_cus);
+    const unsigned groups = (unsigned)groups_of(a, s, s.held ? forward_waves(a, s) : 32, num_cus);
     a.lanes = s.lanes;
     a.over = 1.f / (float)a.width;
     return by_type(a.type, [&](auto t) {
@@ -405,7 +439,7 @@ hipError_t launch_norm_backward(const NormArgs &args, int num_cus, hipStream_t s
     const bool columns = a.dweight || a.dbias;
     a.lanes = s.lanes;
     a.over = 1.f / (float)a.width;
-    const unsigned groups = columns ? (unsigned)a.parts : (unsigned)groups_of(a, s, num_cus);
+    const unsigned groups = columns ? (unsigned)a.parts : (unsigned)groups_of(a, s, backward_waves(s), num_cus);
     const int64_t wide = (a.width * type_size(a.type) + 16 * 256 - 1) / (16 * 256);
     return by_type(a.type, [&](auto t) {
         using T = decltype(t);
@@ -414,17 +448,20 @@ hipError_t launch_norm_backward(const NormArgs &args, int num_cus, hipStream_t s
                 constexpr int P = decltype(p)::value;
                 const unsigned lds =
                     (unsigned)((kPart + (columns && !s.wide ? 4 * a.width * 2 : 0)) * sizeof(float));
-                if (s.wide && columns)
-                    norm_backward_kernel<T, P, true, true><<<groups, s.threads, lds, stream>>>(a);
-                else if (s.wide)
-                    norm_backward_kernel<T, P, true, false><<<groups, s.threads, lds, stream>>>(a);
-                else if (columns)
-                    norm_backward_kernel<T, P, false, true><<<groups, s.threads, lds, stream>>>(a);
-                else
-                    norm_backward_kernel<T, P, false, false><<<groups, s.threads, lds, stream>>>(a);
+                const auto launch = [&](auto wide, auto cols, auto ahead) {
+                    norm_backward_kernel<T, P, decltype(wide)::value, decltype(cols)::value,
+                                         decltype(ahead)::value><<<groups, s.threads, lds, stream>>>(a);
+                };
+                const auto by_columns = [&](auto wide, auto ahead) {
+                    if (columns) launch(wide, Int<1>(), ahead);
+                    else launch(wide, Int<0>(), ahead);
+                };
+                if (!s.wide) by_columns(Int<0>(), Int<1>());
+                else if (s.threads <= kAheadThreads) by_columns(Int<1>(), Int<1>());
+                else by_columns(Int<1>(), Int<0>());
             });
         } else {
-            const unsigned rows = (unsigned)groups_of(a, s, num_cus);
+            const unsigned rows = (unsigned)groups_of(a, s, 32, num_cus);
             if (a.dx && a.n) norm_long_backward_kernel<T><<<rows, s.threads, 0, stream>>>(a);
             if (columns)
                 norm_columns_kernel<T><<<dim3(groups, (unsigned)wide), 256, 0, stream>>>(a);

@@ -78,6 +78,19 @@ struct Part {
     }
 };
 
+// Keeps a row's pieces as they were read between its passes, not the floats that the last
+// pass made of them, which would take more registers than there are.
+template <typename T, int P>
+__device__ inline void keep_raw(Piece<T, 16 / sizeof(T)> (&x)[P]) {
+    typedef int Raw __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        Raw raw = __builtin_bit_cast(Raw, x[p].v);
+        asm volatile("" : "+v"(raw));
+        x[p].v = __builtin_bit_cast(decltype(x[p].v), raw);
+    }
+}
+
 // How rows are taken: pieces to a lane, lanes to a row, threads of a workgroup.
 struct Shape {
     int pieces, lanes, threads;
