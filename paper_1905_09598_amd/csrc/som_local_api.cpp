@@ -353,7 +353,7 @@ struct LinearBackward {
 int64_t codes_of(int64_t width) { return rounded(width, 128); }
 int64_t scales_of(int64_t width) { return rounded(width, 512) / 128; }
 
-// x is brought to 8 bits first, unless it is there or has few rows.
+// x is brought to 8 bits first, unless it is there or has few and short rows.
 struct Linear8 {
     ProductArgs a{};
     ProductPlan plan{};
@@ -374,8 +374,8 @@ struct Linear8 {
         a.residual = c.residual, a.ldr = c.ldr;
         a.y = c.y;
         plan = som::plan_product(a, true, compute_units());
-        first = !c.x_codes && !plan.waves;
-        if (!c.x_codes) few.x = c.x, few.ldx = c.ldx, few.width = c.inner;
+        first = !c.x_codes && (!plan.waves || som::rows8_lds(a) > som::kRows8Lds);
+        if (!c.x_codes && !first) few.x = c.x, few.ldx = c.ldx, few.width = c.inner;
         if (first) {
             blocks.type = c.type;
             blocks.n = c.n, blocks.width = c.inner;

@@ -389,7 +389,10 @@ struct BlocksArgs {
     Divider units;          // of four blocks, of a row
 };
 hipError_t launch_to_blocks(const BlocksArgs &a, hipStream_t stream);
-// x as the caller has it, for the kernel of few rows; NULL if it is held in 8 bits.
+// x as the caller has it, for the kernel of few rows, which brings it to 8 bits in LDS
+// (rows8_lds bytes, at most kRows8Lds); NULL if it is held in 8 bits.
+constexpr int64_t kRows8Lds = 40 * 1024;
+int64_t rows8_lds(const ProductArgs &a);
 struct Rows8Args {
     const void *x;
     int64_t ldx, width;

@@ -338,24 +338,33 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a) {
         }
 }
 
-// Two rows of `width` from their parts, in order: 32 columns of both, eight lanes each.
+// Two rows of `width` from their parts, in order: four neighbouring columns a thread, 32 of
+// them to a workgroup, the parts in turn over 32 lanes (512 parts of 8192: 6 us).
 template <typename T>
 __global__ __launch_bounds__(256) void join_parts_kernel(const float *partial, int32_t parts,
                                                          int64_t width, T *first, T *second) {
-    __shared__ float part[8][32];
-    const int c = threadIdx.x & 31, lane = threadIdx.x >> 5;
-    const int64_t col = (int64_t)blockIdx.x * 32 + c;
-    float v = 0.f;
-    if (col < 2 * width) {
+    constexpr int kLanes = 32, kQuads = 256 / kLanes;
+    __shared__ float part[kLanes][4 * kQuads + 1];
+    const int q = threadIdx.x % kQuads, lane = threadIdx.x / kQuads;
+    const int64_t from = ((int64_t)blockIdx.x * kQuads + q) * 4, left = 2 * width - from;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-        for (int p = lane; p < parts; p += 8) v += partial[p * 2 * width + col];
+    for (int p = lane; p < parts; p += kLanes) {
+        Piece<float, 4> u;
+        u.read(partial + p * 2 * width + from, (int)(left < 0 ? 0 : left < 4 ? left : 4));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += u.v[e];
     }
-    part[lane][c] = v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) part[lane][4 * q + e] = v[e];
     __syncthreads();
-    if (lane == 0 && col < 2 * width) {
-        for (int l = 1; l < 8; ++l) v += part[l][c];
+    const int c = threadIdx.x;
+    const int64_t col = (int64_t)blockIdx.x * kQuads * 4 + c;
+    if (c < 4 * kQuads && col < 2 * width) {
+        float sum = 0.f;
+        for (int l = 0; l < kLanes; ++l) sum += part[l][c];
         T *const to = col < width ? first : second;
-        if (to) to[col < width ? col : col - width] = (T)v;
+        if (to) to[col < width ? col : col - width] = (T)sum;
     }
 }
 
