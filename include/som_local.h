@@ -372,12 +372,13 @@ typedef struct som_distill_call {
     const void *teacher;       /* n x k, packed                                      */
     const float *rest;         /* n; NULL for 0                                      */
     const int32_t *label;      /* n; NULL for none                                   */
-    float temperature;         /* > 0                                                */
+    float temperature;         /* 2^-20 .. 2^20                                      */
     float mix;                 /* in [0, 1]; 0 without a teacher, 1 without labels   */
     const float *dloss;        /* n; NULL for 1                                      */
     float scale;
     float *loss;               /* n; NULL if not wanted                              */
-    void *dlogits;             /* packed n x classes; NULL if not wanted             */
+    void *dlogits;             /* packed n x classes; NULL if not wanted; may be
+                                  logits, where those are packed                     */
     void *stream;
 } som_distill_call;
 

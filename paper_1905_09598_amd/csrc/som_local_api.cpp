@@ -1070,7 +1070,8 @@ som_status som_norm_backward(const som_norm_call *c) {
 
 som_status som_distill(const som_distill_call *c) {
     if (!c || !type_ok(c->type) || c->n < 0 || c->classes < 1 || c->lds < c->classes || c->k < 0 ||
-        c->k > som::kMaxTaught || !(c->temperature > 0.f) || isinf(c->temperature) ||
+        c->k > som::kMaxTaught ||
+        !(c->temperature >= som::kLeastTemperature && c->temperature <= 1.f / som::kLeastTemperature) ||
         !(c->mix >= 0.f && c->mix <= 1.f) || !isfinite(c->scale))
         return SOM_E_ARG;
     if ((c->k && !type_ok(c->teacher_type)) || (!c->k && (c->index || c->teacher || c->rest)) ||

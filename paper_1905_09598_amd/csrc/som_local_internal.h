@@ -359,6 +359,7 @@ hipError_t launch_norm_backward(const NormArgs &a, int num_cus, hipStream_t stre
 
 // som_distill.hip; the fields are som_distill_call's.
 constexpr int kMaxClasses = 1 << 20, kMaxTaught = 64;
+constexpr float kLeastTemperature = 0x1p-20f;   // and 1 over it the most
 struct DistillArgs {
     int32_t type, teacher_type;
     int64_t n;

@@ -149,6 +149,23 @@ def test_rows_beyond_the_last_are_left_and_none_are_fine():
     assert loss.shape == (0,) and dlogits.shape == (0, 40)
 
 
+@pytest.mark.parametrize("classes", [7, 300, 5000, 70000])
+def test_gradient_in_the_logits_place(classes):
+    s, index, t, rest, label, dloss = _inputs(9, classes, 4, torch.bfloat16, seed=2)
+    want = local.distill(s, index, t, 2.0, rest, label, 0.5, dloss)
+    call = local._distill_call(s, index, t, 2.0, rest, label, 0.5, dloss)
+    loss = torch.empty(9, device="cuda")
+    call.loss, call.dlogits = loss.data_ptr(), s.data_ptr()
+    som._check(local.lib().som_distill(local.C.byref(call)), "som_distill")
+    assert torch.equal(loss, want[0]) and torch.equal(s, want[1])
+
+
+@pytest.mark.parametrize("heat", [2.0 ** -20, 2.0 ** 20])
+def test_temperatures_at_their_ends(heat):
+    s, index, t, rest, label, dloss = _inputs(30, 90, 4, torch.float32, seed=8)
+    _check(s, index, t, heat, rest, label, 0.5, dloss)
+
+
 def test_many_rows_and_offsets_beyond_32_bits():
     s, index, t, rest, label, dloss = _inputs(100001, 12, 3, torch.bfloat16, seed=9)
     _check(s, index, t, 1.0, rest, label, 0.5, dloss)
@@ -220,6 +237,8 @@ def test_refusals():
         (ValueError, lambda: local.distill(s.clone().requires_grad_(), index, t)),
         (som.SomError, lambda: local.distill(s, index, t, temperature=0.0)),
         (som.SomError, lambda: local.distill(s, index, t, temperature=-1.0)),
+        (som.SomError, lambda: local.distill(s, index, t, temperature=2.0 ** -21)),
+        (som.SomError, lambda: local.distill(s, index, t, temperature=math.inf)),
         (som.SomError, lambda: local.distill(s, index, t, temperature=math.nan)),
         (som.SomError, lambda: local.distill(s, index, t, label=label, mix=1.5)),
         (som.SomError, lambda: local.distill(s, index, t, mix=0.5)),
