@@ -396,8 +396,8 @@ def to_blocks(x) -> Blocks:
     if not width:
         raise ValueError("x must have columns")
     blocks = -(-width // BLOCK)
-    codes = torch.empty((n, blocks * BLOCK), dtype=torch.float8_e4m3fn, device=x.device)
-    scale = torch.empty((n, -(-blocks // 4) * 4), dtype=torch.float8_e8m0fnu, device=x.device)
+    codes = x.new_empty((n, blocks * BLOCK), dtype=torch.float8_e4m3fn)
+    scale = x.new_empty((n, -(-blocks // 4) * 4), dtype=torch.float8_e8m0fnu)
     call = _BlocksCall(code, width, n, _ptr(x), _ld(x), _ptr(codes), _ptr(scale), _stream(x))
     _check(lib().som_to_blocks(C.byref(call)), "som_to_blocks")
     return Blocks(codes, scale, width)
@@ -436,13 +436,13 @@ def linear8(x, w: Blocks, bias=None, activation: str = "none", residual=None, dt
     if residual is not None:
         _like(residual, like, (n, outer), "residual", packed=False)
         call.residual, call.ldr = _ptr(residual), _ld(residual)
-    y = torch.empty((n, outer), dtype=like.dtype, device=x.device)
+    y = like.new_empty((n, outer))
     call.y, call.stream = _ptr(y), _stream(y)
     L, need = lib(), C.c_uint64()
     at = C.byref(call)
     _check(L.som_linear8_workspace(at, C.byref(need)), "som_linear8")
     if need.value:
-        work = torch.empty(need.value, dtype=torch.uint8, device=x.device)
+        work = like.new_empty(need.value, dtype=torch.uint8)
         call.workspace, call.workspace_bytes = work.data_ptr(), need.value
     _check(L.som_linear8(at), "som_linear8")
     return y
@@ -471,8 +471,8 @@ def gated(x, w, bias=None, activation: str = "silu", keep: bool = False):
     if bias is not None:
         _like(bias, x, (2, hidden), "bias")
         call.bias = _ptr(bias)
-    y = torch.empty((n, hidden), dtype=x.dtype, device=x.device)
-    z = torch.empty((n, 2, hidden), dtype=torch.float32, device=x.device) if keep else None
+    y = x.new_empty((n, hidden))
+    z = x.new_empty((n, 2, hidden), dtype=torch.float32) if keep else None
     call.y, call.z = _ptr(y), _ptr(z)
     _run("gated", call, False, x)
     return (y, z) if keep else y
@@ -488,9 +488,9 @@ def gated_backward(dy, x, w, z, activation: str = "silu", bias: bool = True):
         raise TypeError("z must be float32 (gated with keep=True)")
     _shaped(z, x, (n, 2, hidden), "z")
     call.dy, call.lddy, call.z = _ptr(dy), _ld(dy), _ptr(z)
-    dx = torch.empty((n, x.shape[1]), dtype=x.dtype, device=x.device)
+    dx = x.new_empty((n, x.shape[1]))
     dw = torch.empty_like(w)
-    dbias = torch.empty((2, hidden), dtype=x.dtype, device=x.device) if bias else None
+    dbias = x.new_empty((2, hidden)) if bias else None
     call.dx, call.dw, call.dbias = _ptr(dx), _ptr(dw), _ptr(dbias)
     _run("gated", call, True, x)
     return dx, dw, dbias
@@ -519,8 +519,8 @@ def norm(x, weight=None, bias=None, eps: float = 1e-5, keep: bool = False):
     if bias is not None:
         _like(bias, x, (x.shape[1],), "bias")
         call.bias = _ptr(bias)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    kept = torch.empty((x.shape[0], 2), dtype=torch.float32, device=x.device) if keep else None
+    y = x.new_empty(x.shape)
+    kept = x.new_empty((x.shape[0], 2), dtype=torch.float32) if keep else None
     call.y, call.kept = _ptr(y), _ptr(kept)
     call.stream = _stream(x)
     _check(lib().som_norm(C.byref(call)), "som_norm")
@@ -543,9 +543,9 @@ def norm_backward(dy, x, weight, kept, beside=None, bias: bool = True):
     if beside is not None:
         _like(beside, x, (n, width), "beside", packed=False)
         call.beside, call.ldb = _ptr(beside), _ld(beside)
-    dx = torch.empty((n, width), dtype=x.dtype, device=x.device)
+    dx = x.new_empty((n, width))
     dweight = torch.empty_like(weight) if weight is not None else None
-    dbias = torch.empty(width, dtype=x.dtype, device=x.device) if bias else None
+    dbias = x.new_empty(width) if bias else None
     call.dx, call.dweight, call.dbias = _ptr(dx), _ptr(dweight), _ptr(dbias)
     _run("norm", call, True, x)
     return dx, dweight, dbias
@@ -832,11 +832,11 @@ def distill(logits, index=None, teacher=None, temperature: float = 1.0, rest=Non
     With ``dloss``, the gradient of the rows' losses ((n,) fp32, or a number for all),
     returns (loss, dlogits), both from one read of the logits."""
     call = _distill_call(logits, index, teacher, temperature, rest, label, mix, dloss)
-    loss = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
+    loss = logits.new_empty(logits.shape[0], dtype=torch.float32)
     call.loss = _ptr(loss)
     dlogits = None
     if dloss is not None:
-        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        dlogits = logits.new_empty(logits.shape)
         call.dlogits = _ptr(dlogits)
     _check(lib().som_distill(C.byref(call)), "som_distill")
     return loss if dloss is None else (loss, dlogits)
@@ -847,7 +847,7 @@ def distill_backward(dloss, logits, index=None, teacher=None, temperature: float
     """dlogits of ``distill`` from the gradient of the rows' losses ((n,) fp32, or a
     number for all): for a loss whose gradient is known only later."""
     call = _distill_call(logits, index, teacher, temperature, rest, label, mix, dloss)
-    dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    dlogits = logits.new_empty(logits.shape)
     call.dlogits = _ptr(dlogits)
     _check(lib().som_distill(C.byref(call)), "som_distill")
     return dlogits
