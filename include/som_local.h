@@ -1,8 +1,9 @@
 /*
  * som_local.h -- C ABI of libsom for local models on a trained map: a gate that
  * sends each document to a few experts (for example the units of a map), the
- * experts' matrix products, their gradients, and the optimizer that trains
- * both.
+ * experts' matrix products, layer norm, gated layers, the loss by which the map and
+ * labels teach a model, their gradients, the optimizer that trains them, and
+ * products in 8 bits that serve them.
  *
  * With prototypes w_u, the scores -|x - w_u|^2 / (2 tau) of a document x are, up
  * to a constant per document, x . (w_u / tau) - |w_u|^2 / (2 tau): one product with

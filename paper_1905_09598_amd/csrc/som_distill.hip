@@ -11,7 +11,10 @@
 // summed by itself (Z less the teacher's classes would cancel): the teacher's classes are
 // marked by bits in LDS, of which a piece of a row takes its own in one read.  All
 // gradients are written as if no class were named, and the few that are once more behind a
-// barrier: testing for them on the way took 35 us of 198 (16,001 bf16 rows of 10,000).
+// barrier.  What a row has beside its logits is read while they are on their way.  16,001
+// bf16 rows of 10,000, eight named classes and labels, take 152 us (4.2 TB/s); with the
+// named classes tested for on the way, and the rest read when it was needed, 198.  Rows of
+// 200,003 are read twice: 512 of them 146 us (instructions 83 of it by count).
 #include "som_row.h"
 
 #include <algorithm>
@@ -94,7 +97,8 @@ __device__ inline void teach(const DistillArgs &a, const Taught &t, const T *s, 
 
 // How labels' exponentials come.  At temperatures of 1, 2 and 4 they are the others', squared
 // none, one or two times, off by no more than by themselves: the error of the product in the
-// exponent doubles with the exponent either way.  (16,001 bf16 rows of 10,000 at 2: XXX.)
+// exponent doubles with the exponent either way.  (16,001 bf16 rows of 10,000 at 2: 178 us
+// with exponentials of their own, 166 so.)
 enum : int { kNoLabels = 0, kOwn = 1, kSame = 2, kSquared = 3, kTwice = 4 };
 
 // 2^((v - top) c) of N logits and, with labels, e^(v - top).
@@ -130,15 +134,17 @@ struct Beside {
 // What a row's sums give.
 struct Factors {
     float z, r, e;                  // the sums
+    float t;                        // of the teacher's classes: z - r
     float top, chosen, other, one;  // m; factors of 2^((s - m) c) and of e^(s - m)
     float given;                    // of the teacher's probability
     float label;                    // of the label's class
     bool shut;                      // a row without an open class
     template <int HARD>
     __device__ static Factors of(const DistillArgs &a, const Taught &t, const Beside &b, float top,
-                                 float z, float r, float e) {
+                                 const float (&sums)[3]) {
         Factors f;
-        f.z = z, f.r = r, f.e = e, f.top = top;
+        const float z = sums[0] + sums[1], r = sums[1], e = sums[2];
+        f.z = z, f.r = r, f.e = e, f.t = sums[0], f.top = top;
         f.shut = z == 0.f;
         const float soft = b.scale * a.mix * a.temperature, hard = b.scale * (1.f - a.mix);
         f.chosen = f.other = f.given = f.one = f.label = 0.f;
@@ -147,8 +153,12 @@ struct Factors {
             f.given = soft * t.rest[1];
             f.chosen = f.given / z;
             f.other = f.chosen;
-            // the classes that the teacher left out, whose sum is to be its rest
-            if (t.rest[0] != 0.f) f.other = r == 0.f ? 0.f : f.chosen * (1.f - t.rest[0] * (z / r));
+            // the classes that the teacher left out, whose sum is to be its rest: from the
+            // smaller of the two parts of z, so that what is left of 1 keeps its bits
+            const float rest = t.rest[0];
+            if (rest != 0.f && r == 0.f) f.other = 0.f;
+            else if (rest != 0.f)
+                f.other = f.chosen * (f.t < r ? ((1.f - rest) - f.t / z) * (z / r) : 1.f - rest * (z / r));
         }
         if (HARD && b.at >= 0) f.one = hard / e, f.label = hard;
         return f;
@@ -174,7 +184,10 @@ __device__ inline float loss_of(const DistillArgs &a, const Taught &t, const Fac
         }
         soft = lanes_sum(soft, lanes);
         const float rest = t.rest[0];
-        if (rest != 0.f) soft = fmaf(rest, logf(rest) - (logf(f.r) - log_z), soft);
+        if (rest != 0.f) {   // next to 1 a share's logarithm comes from the other share
+            const float share = f.t < f.r ? log1pf(-f.t / f.z) : logf(f.r / f.z);
+            soft = fmaf(rest, logf(rest) - share, soft);
+        }
         if (t.rest[1] != 1.f) soft = t.rest[1];   // 0 or NaN
         all = a.mix * a.temperature * a.temperature * soft;
     }
@@ -296,7 +309,7 @@ __global__ __launch_bounds__(1024) void distill_kernel(DistillArgs a) {
     keep_raw<T, P>(x);
     if (!there) return;
     const Factors f =
-        Factors::of<HARD>(a, t, beside, from, sums[0] + sums[1], sums[1], sums[2]);
+        Factors::of<HARD>(a, t, beside, from, sums);
     T *const to = static_cast<T *>(a.dlogits) + row * a.classes;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -401,7 +414,7 @@ __global__ __launch_bounds__(1024) void distill_long_kernel(DistillArgs a) {
         if (HARD) sums[2] *= __builtin_amdgcn_exp2f((mine - all) * kLog2e);
     }
     row_sum<true>(sums, 0, part, turn);
-    const Factors f = Factors::of<HARD>(a, t, beside, all, sums[0] + sums[1], sums[1], sums[2]);
+    const Factors f = Factors::of<HARD>(a, t, beside, all, sums);
     if (a.loss && first) {
         const float loss = loss_of<HARD>(a, t, f, beside, threadIdx.x, 64);
         if (threadIdx.x == 0) a.loss[row] = loss;

@@ -1,5 +1,6 @@
 """Local models on a trained map: the gate's product, the routing of documents
-to experts, the experts' products, their gradients and the optimizer.
+to experts, the experts' products, layer norm, gated layers, distillation from the
+map, products in 8 bits, their gradients and the optimizer.
 
 Thin binding of ``include/som_local.h`` (which has every formula).  All
 arithmetic runs in the library's HIP kernels; this module marshals arguments,
@@ -20,6 +21,17 @@ graph: outside ``torch.no_grad()`` they refuse tensors that require a gradient.
     optimizer.step([dw, dbias, d.w1, d.b1, d.w2, d.b2])
 
 ``gate_from_map`` gives the gate whose scores are a trained map's.
+
+A model taught by the map and by labels, and its head served in 8 bits:
+
+    y, kept = local.norm(x, nw, nb, keep=True)
+    h, z = local.gated(y, w1, b1, keep=True)
+    s = local.linear(h, w2, b2)
+    loss, ds = local.distill(s, r.index, teacher, rest=rest, label=label, mix=0.7, dloss=1 / n)
+    dh, dw2, db2 = local.linear_backward(ds, h, w2)
+    dy, dw1, db1 = local.gated_backward(dh, y, w1, z)
+    dx, dnw, dnb = local.norm_backward(dy, x, nw, kept)
+    s = local.linear8(h, local.to_blocks(w2), b2)
 """
 from __future__ import annotations
 

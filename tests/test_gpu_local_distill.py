@@ -178,6 +178,38 @@ def test_many_rows_and_offsets_beyond_32_bits():
         assert torch.equal(u, w)
 
 
+@pytest.mark.parametrize("classes", [3000, 75233])
+@pytest.mark.parametrize("share", [0.01, 0.99])
+def test_shares_next_to_one(classes, share):
+    """What the teacher names, or what it does not, is a hundredth, and the student agrees
+    to a tenth of that: a loss of about 1e-4 made of terms of about 10.  The shares come
+    from the smaller part of the sum: off by at most (classes + 40) V of themselves, and
+    the loss with them; each named class's logarithms, of magnitudes up to 20 in all, by
+    8 V of that, times the named share."""
+    g = torch.Generator().manual_seed(13)
+    n, k = 40, 8
+    s = torch.randn(n, classes, generator=g, dtype=torch.float64)
+    index = torch.stack([torch.randperm(classes, generator=g)[:k] for _ in range(n)])
+    s.scatter_(1, index, -100.0)
+    others = s.exp().sum(1)
+    named = (others * share / (1 - share) / k).log().unsqueeze(1)
+    s.scatter_(1, index, (named + 0.1 * torch.randn(n, k, generator=g)).double())
+    s = s.float().cuda()
+    index, t = index.int().cuda(), (0.1 * torch.randn(n, k, generator=g)).cuda()
+    rest = torch.full((n,), 1 - share, device="cuda")
+    ones = torch.ones(n, device="cuda")
+    loss, dlogits = local.distill(s, index, t, 1.0, rest, dloss=1.0)
+    o = O.Distill(O.d(s), index, O.d(t), 1.0, O.d(rest), None, 1.0, O.d(ones), torch.float32)
+    V = O.V
+    least = min(share, 1 - share)
+    allowed = share * 8 * V * 20 + 8 * V * least + 4 * V * o.loss[0].abs()
+    # a sum of positive terms in parts of at most 200 and their joins, not one chain
+    allowed = allowed + least * (200 + 40) * V * 2
+    assert ((loss.double() - o.loss[0]).abs() < allowed).all(), float(
+        ((loss.double() - o.loss[0]).abs() / allowed).max())
+    O.close(dlogits, o.dlogits, "dlogits")
+
+
 def test_from_a_routing():
     """A map's nearest units teach a gate: the routing's index, its scores and its rest."""
     g = torch.Generator().manual_seed(6)
