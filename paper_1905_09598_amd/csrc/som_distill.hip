@@ -86,7 +86,7 @@ __device__ inline void teach(const DistillArgs &a, const Taught &t, const T *s, 
         sum += e;
     }
     sum = lanes_sum(sum, lanes);
-    rest = rest <= 0.f || sum == 0.f ? 0.f : rest;
+    rest = rest <= 0.f || sum == 0.f ? 0.f : rest > 1.f ? 1.f : rest;
     const float by = (1.f - rest) / (sum == 0.f ? 1.f : sum);
     for (int j = lane; j < a.k; j += lanes) t.p[j] *= by;
     if (lane == 0) {

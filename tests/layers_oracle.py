@@ -123,7 +123,7 @@ class Distill:
             best = torch.where(taught, t.max(1, keepdim=True).values, zero)
             q = (t - best).exp()
             total = q.sum(1, keepdim=True)
-            r = zero if rest is None else torch.where(taught, rest.unsqueeze(1).clamp(min=0), zero)
+            r = zero if rest is None else torch.where(taught, rest.unsqueeze(1).clamp(min=0, max=1), zero)
             p = (1 - r) * q / torch.where(taught, total, total + 1)
             dp = ((t - best).abs().nan_to_num(posinf=0.0) * 4 + k + 14) * V
             dp = dp.max(1, keepdim=True).values + dp

@@ -84,7 +84,7 @@ def test_absent_repeated_and_closed_classes(classes):
     s[16] = -math.inf                            # a row without an open class
     s[17], s[18] = torch.finfo(torch.float32).min, -1e38
     s[18, classes // 2] = 3e38
-    rest[19], rest[20], rest[21] = 0.0, 1.0, -1e-7
+    rest[19], rest[20], rest[21], rest[22] = 0.0, 1.0, -1e-7, 1.5
     loss, dlogits = _check(s, index, t, 2.0, rest, label, 0.5, dloss)
     assert float(loss[16]) == 0 and float(dlogits[16].abs().max()) == 0
     loss, dlogits = _check(s, index, t, 1.0, None, None, 1.0, dloss)
