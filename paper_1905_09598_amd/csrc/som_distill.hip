@@ -54,7 +54,7 @@ __device__ inline float wide(const void *p, int32_t type, int64_t i) {
                            : (float)static_cast<const _Float16 *>(p)[i];
 }
 
-// Sum and maximum over `lanes` neighbours, at most a wave.
+// The sum over `lanes` neighbours, at most a wave.
 __device__ inline float lanes_sum(float v, int lanes) {
     for (int o = 1; o < lanes; o <<= 1) v += __shfl_xor(v, o);
     return v;
@@ -308,8 +308,7 @@ __global__ __launch_bounds__(1024) void distill_kernel(DistillArgs a) {
     row_sum<WIDE>(sums, a.lanes, part, turn);
     keep_raw<T, P>(x);
     if (!there) return;
-    const Factors f =
-        Factors::of<HARD>(a, t, beside, from, sums);
+    const Factors f = Factors::of<HARD>(a, t, beside, from, sums);
     T *const to = static_cast<T *>(a.dlogits) + row * a.classes;
 #pragma unroll
     for (int p = 0; p < P; ++p) {

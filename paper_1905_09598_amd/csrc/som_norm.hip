@@ -453,7 +453,7 @@ hipError_t launch_norm_backward(const NormArgs &args, int num_cus, hipStream_t s
     a.over = 1.f / (float)a.width;
     const unsigned groups = columns ? (unsigned)a.parts : (unsigned)groups_of(a, s, backward_waves(s), num_cus);
     const int64_t wide = (a.width * type_size(a.type) + 16 * 256 - 1) / (16 * 256);
-    return by_type(a.type, [&](auto t) {
+    const hipError_t e = by_type(a.type, [&](auto t) {
         using T = decltype(t);
         if (s.held) {
             by_pieces<kBackwardPieces<T>>(s.pieces, [&](auto p) {
@@ -478,9 +478,9 @@ hipError_t launch_norm_backward(const NormArgs &args, int num_cus, hipStream_t s
             if (columns)
                 norm_columns_kernel<T><<<dim3(groups, (unsigned)wide), 256, 0, stream>>>(a);
         }
-        if (columns)
-            (void)launch_join_parts(a.type, a.partial, a.parts, a.width, a.dweight, a.dbias, stream);
     });
+    if (e != hipSuccess || !columns) return e;
+    return launch_join_parts(a.type, a.partial, a.parts, a.width, a.dweight, a.dbias, stream);
 }
 
 }  // namespace som
