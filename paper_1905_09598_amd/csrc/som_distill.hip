@@ -440,16 +440,24 @@ __global__ __launch_bounds__(1024) void distill_long_kernel(DistillArgs a) {
     if (first) named<T, HARD>(a, t, f, beside, to, c, threadIdx.x, 64);
 }
 
-// Pieces that a lane holds: 1 or 2 of a wave's rows, 4 or 8 of a workgroup's (16 are more
-// than the registers of 1024 threads).
-constexpr int kWavePieces = 2, kWidePieces = 8;
+// Pieces that a lane holds: 1, 2 or 4 of a row that a wave or less takes, 4 or 8 of one that
+// a workgroup takes (16 are more than the registers of 1024 threads).  Short rows wait for
+// their reads and reductions, not for memory: of many rows a lane takes more pieces, so that
+// a wave has more rows under way (60,000 bf16 rows of 400: one piece 71 us, four 35; of 1000
+// two 88, four 62), of few rows one, so that they are on more compute units.  Rows of more
+// than 128 pieces go to a workgroup (60,000 of 1030: 89 us, to the lanes of a wave 104).
+constexpr int kNarrowPieces = 4, kWidePieces = 8;
+constexpr int64_t kManyWaves = 4096;   // 16 to a compute unit
 
 Shape distill_shape(const DistillArgs &a) {
-    Shape s = shape_of(a.type, a.classes, kWavePieces, kWidePieces, 64);
+    Shape s = shape_of(a.type, a.classes, 2, kWidePieces, 64);
     if (s.held && s.wide) {
         const int n = 16 / type_size(a.type), pieces = (a.classes + n - 1) / n;
         s.pieces = pieces > 1024 * 4 ? 8 : 4;
         s.threads = s.lanes = (pieces + 64 * s.pieces - 1) / (64 * s.pieces) * 64;
+    } else if (s.held) {
+        while (s.pieces < kNarrowPieces && s.lanes > 1 && a.n * s.lanes > kManyWaves * 64)
+            s.pieces *= 2, s.lanes /= 2;
     }
     return s;
 }
@@ -476,8 +484,9 @@ hipError_t launch_typed(const DistillArgs &a, const Shape &s, unsigned groups, u
         return hipGetLastError();
     }
     if (!s.wide) {
-        return s.pieces == 1 ? launch_held<T, 1, false, HARD>(a, s, groups, lds, stream)
-                             : launch_held<T, 2, false, HARD>(a, s, groups, lds, stream);
+        return s.pieces == 1   ? launch_held<T, 1, false, HARD>(a, s, groups, lds, stream)
+               : s.pieces == 2 ? launch_held<T, 2, false, HARD>(a, s, groups, lds, stream)
+                               : launch_held<T, 4, false, HARD>(a, s, groups, lds, stream);
     }
     return s.pieces == 4 ? launch_held<T, 4, true, HARD>(a, s, groups, lds, stream)
                          : launch_held<T, 8, true, HARD>(a, s, groups, lds, stream);

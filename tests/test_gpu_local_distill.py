@@ -167,8 +167,10 @@ def test_temperatures_at_their_ends(heat):
 
 
 def test_many_rows_and_offsets_beyond_32_bits():
-    s, index, t, rest, label, dloss = _inputs(100001, 12, 3, torch.bfloat16, seed=9)
-    _check(s, index, t, 1.0, rest, label, 0.5, dloss)
+    for n, classes, k in ((100001, 12, 3), (30001, 70, 40), (9000, 400, 8), (6001, 1003, 5),
+                          (5003, 1900, 4)):
+        s, index, t, rest, label, dloss = _inputs(n, classes, k, torch.bfloat16, seed=9)
+        _check(s, index, t, 1.0, rest, label, 0.5, dloss)
     wide = torch.empty((1 << 31) + 4096, dtype=torch.bfloat16, device="cuda")
     v = torch.as_strided(wide, (3, 900), (1 << 30, 1))
     s, index, t, rest, label, dloss = _inputs(3, 900, 3, torch.bfloat16, seed=9)
