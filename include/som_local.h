@@ -349,7 +349,8 @@ som_status som_dispatch(const int32_t *index, int64_t n, int32_t k, int32_t expe
  *     p_j = (1 - r) e^(t_j / T) / sum over j of e^(t_j / T),     a = softmax(s / T),
  *     soft = T^2 ( sum over j of p_j (log p_j - log a[index_j]) + r (log r - log a_R) ),
  *     hard = -log softmax(s)[label],       loss = mix soft + (1 - mix) hard,
- * a_R being the sum of a over the classes that are not named.  0 log 0 is 0.  For example
+ * a_R being the sum of a over the classes that are not named, 0 only if none of them is
+ * open (its logarithm holds below what a type holds).  0 log 0 is 0.  For example
  * the units nearest to a document, their scores, and what a softmax over all units leaves.
  * With the gradient `scale dloss_i` of a row's loss (dloss NULL: scale), P_c the
  * sum of the p_j with index_j = c, and only over the row's own parts,

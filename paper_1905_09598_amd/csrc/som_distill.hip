@@ -131,6 +131,13 @@ struct Beside {
     }
 };
 
+// Of rows whose classes that the teacher left out have less than this of the sum, R and its
+// exponentials are taken from those classes' own maximum: counted from the row's they would
+// be 0 from 87 temperatures below it on, where R's logarithm and their shares of the rest
+// are numbers like others.  (What 2^-60 is next to: an element left out at 2^-126 is 2^-66
+// of it.)
+constexpr float kApart = 0x1p-60f;
+
 // What a row's sums give.
 struct Factors {
     float z, r, e;                  // the sums
@@ -139,12 +146,25 @@ struct Factors {
     float given;                    // of the teacher's probability
     float label;                    // of the label's class
     bool shut;                      // a row without an open class
+    bool apart;                     // r counts from `lead`, the maximum of those classes,
+    float lead, left;               // and `left` is the factor of their 2^((s - lead) c)
+    // Whether it does; alike for all lanes of a row.
+    __device__ static bool is_apart(const DistillArgs &a, const Taught &t, const float (&sums)[3]) {
+        return a.words && t.rest[0] > 0.f && sums[1] < kApart;
+    }
+    // Takes r from there: far, unless none of those classes is open.
+    __device__ void part(const Taught &t, float from, float far) {
+        if (!(from > -INFINITY)) return;
+        apart = true, lead = from, r = far;
+        if (given != 0.f) other = chosen, left = given * t.rest[0] / far;
+    }
     template <int HARD>
     __device__ static Factors of(const DistillArgs &a, const Taught &t, const Beside &b, float top,
                                  const float (&sums)[3]) {
         Factors f;
         const float z = sums[0] + sums[1], r = sums[1], e = sums[2];
         f.z = z, f.r = r, f.e = e, f.t = sums[0], f.top = top;
+        f.apart = false, f.lead = f.left = 0.f;
         f.shut = z == 0.f;
         const float soft = b.scale * a.mix * a.temperature, hard = b.scale * (1.f - a.mix);
         f.chosen = f.other = f.given = f.one = f.label = 0.f;
@@ -170,7 +190,7 @@ template <int HARD>
 __device__ inline float loss_of(const DistillArgs &a, const Taught &t, const Factors &f, const Beside &b,
                                 int lane, int lanes) {
     if (f.shut) return 0.f;
-    float soft = 0.f, all = 0.f;
+    float soft = 0.f, away = 0.f, all = 0.f;   // away: a distance between logits
     // half of a logit's distance from the maximum: the whole may pass fp32's range where
     // its product with a probability does not
     const auto half_below = [&](float v) { return 0.5f * v - 0.5f * f.top; };
@@ -185,11 +205,12 @@ __device__ inline float loss_of(const DistillArgs &a, const Taught &t, const Fac
         soft = lanes_sum(soft, lanes);
         const float rest = t.rest[0];
         if (rest != 0.f) {   // next to 1 a share's logarithm comes from the other share
-            const float share = f.t < f.r ? log1pf(-f.t / f.z) : logf(f.r / f.z);
+            const float share = !f.apart && f.t < f.r ? log1pf(-f.t / f.z) : logf(f.r / f.z);
             soft = fmaf(rest, logf(rest) - share, soft);
+            if (f.apart) away = -2.f * (rest * half_below(f.lead));
         }
         if (t.rest[1] != 1.f) soft = t.rest[1];   // 0 or NaN
-        all = a.mix * a.temperature * a.temperature * soft;
+        all = a.mix * a.temperature * fmaf(a.temperature, soft, away);
     }
     if (HARD && b.at >= 0) {
         const float part = 1.f - a.mix;
@@ -208,6 +229,38 @@ __device__ inline void slopes(const Factors &f, float c, float (&v)[N]) {
     for (int e = 0; e < N; ++e) {
         v[e] = f.other * soft[e];
         if (HARD) v[e] = fmaf(f.one, hard[e], v[e]);
+    }
+}
+
+// Rows whose R counts from its own classes' maximum, by all of a row's lanes: seldom, so they
+// are read again, a class at a time, for which the registers that hold a row need not make
+// room.  The sum from the maximum `lead` of the classes that the teacher left out.
+template <bool WIDE, typename T>
+__device__ inline float apart_sum(const DistillArgs &a, const Taught &t, const T *s, int lane, int lanes,
+                                  float c, float *part, int &turn, float *lead) {
+    float most[1] = {-INFINITY}, sum[1] = {0.f};
+#pragma unroll 1
+    for (int at = lane; at < a.classes; at += lanes)
+        if (!t.template marks<1>(at)) most[0] = fmaxf(most[0], (float)s[at]);
+    row_max<WIDE>(most, lanes, part, turn);
+#pragma unroll 1
+    for (int at = lane; at < a.classes; at += lanes)
+        if (!t.template marks<1>(at)) sum[0] += __builtin_amdgcn_exp2f(((float)s[at] - most[0]) * c);
+    row_sum<WIDE>(sum, lanes, part, turn);
+    *lead = most[0];
+    return sum[0];
+}
+// The gradient, as slopes gives it.
+template <int HARD, typename T>
+__device__ inline void apart_slopes(const DistillArgs &a, const Factors &f, const T *s, T *to, int lane,
+                                    int lanes, float c) {
+#pragma unroll 1
+    for (int at = lane; at < a.classes; at += lanes) {
+        const float logit = (float)s[at];
+        float v[1] = {logit};
+        slopes<HARD>(f, c, v);
+        if (f.apart) v[0] = fmaf(-f.left, __builtin_amdgcn_exp2f((logit - f.lead) * c), v[0]);
+        to[at] = (T)v[0];
     }
 }
 
@@ -232,6 +285,7 @@ __device__ inline void named(const DistillArgs &a, const Taught &t, const Factor
         powers<HARD>(logit, f.top, c, soft, hard);
         float v = (taught ? f.chosen : f.other) * soft[0];
         if (taught) v -= f.given * p;
+        else if (f.apart) v = fmaf(-f.left, __builtin_amdgcn_exp2f((logit[0] - f.lead) * c), v);
         if (HARD) v = fmaf(f.one, hard[0], v);
         if (HARD && at == b.at) v -= f.label;
         to[at] = (T)v;
@@ -304,15 +358,20 @@ __global__ __launch_bounds__(1024) void distill_kernel(DistillArgs a) {
         }
 #pragma unroll
         for (int e = 0; e < N; ++e) sums[1] += v[e];
+        // one piece after the other: together, without labels' exponentials between, they take
+        // 72 registers and not 58 (16,001 bf16 rows of 10,000: 157 us and not 152)
+        if (!HARD) asm volatile("" : "+v"(sums[1]));
     }
     row_sum<WIDE>(sums, a.lanes, part, turn);
     keep_raw<T, P>(x);
-    if (!there) return;
-    const Factors f = Factors::of<HARD>(a, t, beside, from, sums);
     T *const to = static_cast<T *>(a.dlogits) + row * a.classes;
+    Factors f = Factors::of<HARD>(a, t, beside, from, sums);
+    bool apart = Factors::is_apart(a, t, sums);
+    if (WIDE) apart = __builtin_amdgcn_readfirstlane(apart);   // as it is for all
+    if (!there) return;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        if (!a.dlogits || !me.mine(p)) continue;
+        if (!a.dlogits || apart || !me.mine(p)) continue;
         float v[N];
         Piece<T, N> out;
 #pragma unroll
@@ -321,6 +380,12 @@ __global__ __launch_bounds__(1024) void distill_kernel(DistillArgs a) {
 #pragma unroll
         for (int e = 0; e < N; ++e) out.v[e] = (T)v[e];
         out.write(to + me.at[p], N);
+    }
+    if (apart) {   // here, where the row's registers are free
+        float lead;
+        const float far = apart_sum<WIDE>(a, t, s, me.lane, a.lanes, c, part, turn, &lead);
+        f.part(t, lead, far);
+        if (a.dlogits) apart_slopes<HARD>(a, f, s, to, me.lane, a.lanes, c);
     }
     if (WIDE) __syncthreads();
     else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");   // one wave
@@ -413,14 +478,20 @@ __global__ __launch_bounds__(1024) void distill_long_kernel(DistillArgs a) {
         if (HARD) sums[2] *= __builtin_amdgcn_exp2f((mine - all) * kLog2e);
     }
     row_sum<true>(sums, 0, part, turn);
-    const Factors f = Factors::of<HARD>(a, t, beside, all, sums);
+    Factors f = Factors::of<HARD>(a, t, beside, all, sums);
+    if (Factors::is_apart(a, t, sums)) {
+        float lead;
+        const float far = apart_sum<true>(a, t, s, threadIdx.x, blockDim.x, c, part, turn, &lead);
+        f.part(t, lead, far);
+    }
     if (a.loss && first) {
         const float loss = loss_of<HARD>(a, t, f, beside, threadIdx.x, 64);
         if (threadIdx.x == 0) a.loss[row] = loss;
     }
     if (!a.dlogits) return;
     T *const to = static_cast<T *>(a.dlogits) + row * a.classes;
-    for (int first_at = threadIdx.x * N; first_at < a.classes; first_at += kAhead * stride) {
+    if (f.apart) apart_slopes<HARD>(a, f, s, to, threadIdx.x, blockDim.x, c);
+    for (int first_at = threadIdx.x * N; !f.apart && first_at < a.classes; first_at += kAhead * stride) {
         Piece<T, N> x[kAhead];
         read(first_at, x);
 #pragma unroll

@@ -139,25 +139,40 @@ class Distill:
             member = torch.zeros(n, classes + 1, dtype=torch.bool, device=s.device)
             member.scatter_(1, torch.where(there, at, classes), True)
             member = member[:, :classes]
-            er = torch.where(member, zero, e)
-            zr, dzr = weighed(er, u)
+            # the classes left out, from the largest of them: their share of z can be far
+            # below what 64 bits hold
+            ur = torch.where(member, zero - math.inf, u)
+            lead = ur.max(1, keepdim=True).values
+            open_ = lead > -math.inf
+            lead = torch.where(open_ | torch.isnan(lead), lead, zero)
+            er = (ur - lead).exp()
+            # the exponents count from the row's maximum or from theirs: from the row's, where
+            # they leave no more than 2^-60 of its sum, they lose too many
+            off = (ur - lead).abs() + lead.abs().clamp(max=60 * math.log(2))
+            zr, dzr = weighed(er, off)
+            log_ar = lead + zr.log() - z.log()
             has = r > 0
             safe = torch.where(has, r, zero + 1)
-            left = safe * (safe.log() - (zr / z).log())
+            left = safe * (safe.log() - log_ar)
             soft = soft + torch.where(has, left, zero)
             soft_err = soft_err + torch.where(
-                has, safe * (dz + dzr + 8 * V * (safe.log().abs() + zr.log().abs() + z.log().abs())),
+                has, safe * (dz + dzr + 8 * V * (safe.log().abs() + lead.abs() + zr.log().abs()
+                                                 + z.log().abs())),
                 zero).nan_to_num(posinf=0.0)
             soft = torch.where(taught, soft, zero)
             soft = torch.where(odd, zero * math.nan, soft)
             given = torch.zeros(n, classes + 1, dtype=torch.float64, device=s.device)
             given.scatter_add_(1, torch.where(there, at, classes), torch.where(there, p, p * 0))
             given = given[:, :classes]
-            ratio = torch.where(has & (zr > 0), r * z / torch.where(zr > 0, zr, zr + 1), zero)
-            g = torch.where(member, a - given, torch.where(a > 0, a * (1 - ratio), a))
+            of_rest = torch.where(has & open_, r * er / torch.where(open_, zr, zr + 1), zero)
+            g = torch.where(member, a - given, torch.where(torch.isinf(ur), a, a - of_rest))
             ge = torch.where(member, a * da + given * (dp.max(1, keepdim=True).values + k * V),
-                             a * (da * (1 + ratio) + ratio * (dz + dzr + 6 * V)))
-            ge = ge + 6 * V * (a * (1 + ratio) + given)
+                             a * da + of_rest * (dz + dzr + (off.nan_to_num(posinf=0.0) * 4 + 16) * V))
+            ge = ge + 6 * V * (a + of_rest + given)
+            # The hardware's exponential has no subnormals: what is below 2^-126 is 0.  a, of a
+            # sum of 1 or more, is off by as much; a share of the rest, of a sum of 2^-60 or
+            # more (or from its own maximum), by up to 2^-126 / 2^-60 of it.
+            ge = ge + 2.0 ** -126 + torch.where(has & open_ & ~member, r * 2.0 ** -66, zero)
             g = torch.where(odd, g * math.nan, g)
             grad = torch.where(taught, mix * heat * g, zero)
             grad_err = torch.where(taught, mix * heat * ge, zero)
@@ -178,7 +193,8 @@ class Distill:
             one = torch.zeros_like(s).scatter_(1, which, 1.0)
             da1 = (u1.abs().nan_to_num(posinf=0.0) * 4 + 10) * V + dz1
             grad = grad + torch.where(known, (1 - mix) * (a1 - one), zero)
-            grad_err = grad_err + torch.where(known, (1 - mix) * (a1 * da1 + 6 * V * (a1 + one)), zero)
+            grad_err = grad_err + torch.where(
+                known, (1 - mix) * (a1 * da1 + 6 * V * (a1 + one) + 2.0 ** -126), zero)
         loss = torch.where(shut, zero, loss).squeeze(1)
         grad = torch.where(shut, zero, grad) * scale
         grad_err = torch.where(shut, zero, grad_err) * scale.abs() + 8 * V * grad.abs()

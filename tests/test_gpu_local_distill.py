@@ -117,6 +117,36 @@ def test_numbers_that_are_none(classes):
     assert torch.equal(torch.isnan(dlogits).all(1), bad) and torch.equal(torch.isnan(dlogits).any(1), bad)
 
 
+@pytest.mark.parametrize("dtype", T)
+@pytest.mark.parametrize("classes", [6, 23, 300, 1030, 9000, 66000])
+def test_named_classes_far_ahead_of_the_others(classes, dtype):
+    """What the teacher leaves out is far below what it names, further than an exponential
+    reaches: loss and gradient are numbers like others, in rows of a lane, a wave, a
+    workgroup and beyond one."""
+    say("far ahead", classes, dtype)
+    heat = 2.0 if dtype == "fp32" else 0.5
+    s, _, t, rest, label, dloss = _inputs(24, classes, 3, T[dtype], seed=21)
+    index = torch.randint(0, classes, (24, 3), generator=torch.Generator().manual_seed(1)).int().cuda()
+    rest, label = rest + 0.2, label.clamp(0, classes - 1)
+    gaps = torch.tensor([30, 40, 43, 60, 80, 86, 87, 88, 90, 95, 103, 110, 130, 160, 200, 400], device="cuda")
+    named = torch.zeros(24, classes, dtype=torch.bool, device="cuda").scatter_(1, index.long(), True)
+    s[:16] = torch.where(named[:16], s[:16], (s[:16] - heat * gaps[:, None]).to(s.dtype))
+    s[3:16:4][named[3:16:4]] = 1.0                       # equal leaders
+    others = ~named[4:8] & (torch.rand(4, classes, generator=torch.Generator().manual_seed(2)) < 0.5).cuda()
+    s[4:8] = s[4:8].masked_fill(others, -math.inf)       # closed classes among them
+    s[16:20] = s[16:20].masked_fill(named[16:20], -math.inf)      # and none of the named open
+    s[20:22] = torch.where(named[20:22], s[20:22] - 300, s[20:22])
+    s[22:24] = torch.where(named[22:24], s[22:24], (s[22:24] * 2.0 - 500).to(s.dtype))
+    loss, dlogits = _check(s, index, t, heat, rest, None, 1.0, dloss)
+    assert torch.isfinite(loss[:4]).all() and torch.isfinite(loss[8:16]).all()
+    some = ~named[:16] & (s[:16] > -math.inf)
+    assert float(dlogits[:16][some].max()) <= 0 and float(dlogits[:16][some].min()) < -1e-3 / classes
+    _check(s, index, t, heat, rest, label, 0.5, dloss)
+    _check(s, index, t, 1.0, rest, label, 0.5, dloss)
+    if dtype == "fp32":
+        _check(s, index, t, 2.0 ** -20, rest, label, 0.5, dloss)
+
+
 def test_a_teacher_that_the_student_matches():
     """Every class named, the same logits: loss and gradient are 0 to rounding."""
     s = torch.randn(10, 50, generator=torch.Generator().manual_seed(1)).cuda()

@@ -24,8 +24,8 @@ def _slopes(f, x, step=1e-6):
     return out
 
 
-def _near(a, b, what):
-    assert torch.allclose(a, b, rtol=2e-6, atol=2e-8), (what, float((a - b).abs().max()))
+def _near(a, b, what, more=0.0):
+    assert torch.allclose(a, b, rtol=2e-6, atol=2e-8 + more), (what, float((a - b).abs().max()))
 
 
 def test_layer_norm():
@@ -81,6 +81,30 @@ def test_distillation_of_closed_classes():
     a = math.e / (1 + math.e)
     _near(o.dlogits[0], torch.tensor([[-a, 0.0, a], [0.0, 0.0, 0.0]], dtype=F64), "dlogits")
     _near(o.loss[0], torch.tensor([-math.log(1 - a), 0.0], dtype=F64), "loss")
+
+
+@pytest.mark.parametrize("gap", [0.0, 40.0, 110.0, 2000.0])
+def test_distillation_whose_named_classes_lead_the_others(gap):
+    """The others' share in logarithms: e^-2000 is below what 64 bits hold, its logarithm is
+    not.  A difference of two losses of L, each off by up to 8 roundings of 2^-53, over 2e-6
+    is off by 8 2^-53 L 10^6."""
+    g = torch.Generator().manual_seed(6)
+    s = torch.randn(3, 7, generator=g, dtype=F64)
+    s[:, 2:] -= gap
+    index = torch.tensor([[0, 1]] * 3, dtype=torch.int32)
+    t, rest = torch.randn(3, 2, generator=g, dtype=F64), torch.tensor([0.3, 0.9, 0.0], dtype=F64)
+    one = torch.ones(3, dtype=F64)
+
+    def of():
+        return O.Distill(s, index, t, 1.5, rest, None, 1.0, one, torch.float32)
+
+    loga = torch.log_softmax(s / 1.5, 1)
+    p = (1 - rest).unsqueeze(1) * (t / 1.5).softmax(1)
+    far = torch.logsumexp(s[:, 2:] / 1.5, 1) - torch.logsumexp(s / 1.5, 1)
+    share = torch.where(rest > 0, rest * (rest.clamp(min=1e-9).log() - far), 0 * rest)
+    _near(of().loss[0], 2.25 * ((p * (p.log() - loga[:, :2])).sum(1) + share), "loss")
+    _near(of().dlogits[0], _slopes(lambda: of().loss[0].sum(), s), "dlogits",
+          8 * 2.0 ** -53 * float(of().loss[0].sum()) * 1e6)
 
 
 @pytest.mark.parametrize("kind", ["none", "relu", "gelu", "silu"])
