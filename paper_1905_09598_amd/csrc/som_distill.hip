@@ -190,9 +190,9 @@ template <int HARD>
 __device__ inline float loss_of(const DistillArgs &a, const Taught &t, const Factors &f, const Beside &b,
                                 int lane, int lanes) {
     if (f.shut) return 0.f;
-    float soft = 0.f, away = 0.f, all = 0.f;   // away: a distance between logits
-    // half of a logit's distance from the maximum: the whole may pass fp32's range where
-    // its product with a probability does not
+    float soft = 0.f, away = 0.f, all = 0.f;   // of logarithms; of distances below the maximum
+    // half of a logit's distance from the maximum, and not over the temperature: the whole,
+    // and what a low temperature makes of it, may pass fp32's range where the loss does not
     const auto half_below = [&](float v) { return 0.5f * v - 0.5f * f.top; };
     if (a.k && a.mix != 0.f) {
         const float log_z = logf(f.z);
@@ -200,17 +200,19 @@ __device__ inline float loss_of(const DistillArgs &a, const Taught &t, const Fac
             const float p = t.p[j];
             if (t.index[j] < 0 || p == 0.f) continue;
             soft = fmaf(p, logf(p) + log_z, soft);
-            soft -= 2.f * (p * (half_below(t.logit[j]) / a.temperature));
+            away = fmaf(-p, half_below(t.logit[j]), away);
         }
         soft = lanes_sum(soft, lanes);
+        away = lanes_sum(away, lanes);
         const float rest = t.rest[0];
         if (rest != 0.f) {   // next to 1 a share's logarithm comes from the other share
             const float share = !f.apart && f.t < f.r ? log1pf(-f.t / f.z) : logf(f.r / f.z);
             soft = fmaf(rest, logf(rest) - share, soft);
-            if (f.apart) away = -2.f * (rest * half_below(f.lead));
+            if (f.apart) away = fmaf(-rest, half_below(f.lead), away);
         }
         if (t.rest[1] != 1.f) soft = t.rest[1];   // 0 or NaN
-        all = a.mix * a.temperature * fmaf(a.temperature, soft, away);
+        const float by = a.mix * a.temperature;
+        all = fmaf(2.f * by, away, by * a.temperature * soft);
     }
     if (HARD && b.at >= 0) {
         const float part = 1.f - a.mix;

@@ -196,6 +196,19 @@ def test_temperatures_at_their_ends(heat):
     _check(s, index, t, heat, rest, label, 0.5, dloss)
 
 
+@pytest.mark.parametrize("classes", [6, 700, 40000])
+def test_low_temperatures_of_far_logits(classes):
+    """Distances that pass fp32's range over the temperature, and losses that do not."""
+    s, _, t, rest, label, dloss = _inputs(6, classes, 3, torch.float32, seed=23)
+    index = torch.tensor([[1, 2, 3]] * 6, dtype=torch.int32, device="cuda")
+    s[0, 1], s[1, 0], s[2, 4:], s[3, 1:4] = -3e37, 2e38, -1e38, -2e38
+    s[4], s[4, 2], s[5, 1], s[5, 0] = -1e30, 1e38, -3e38, 3e38
+    for heat in (2.0 ** -20, 2.0 ** -4, 0.125):
+        loss, _ = _check(s, index, t, heat, rest, None, 1.0, dloss)
+        assert torch.isfinite(loss).all()
+        _check(s, index, t, heat, rest, label, 0.5, dloss)
+
+
 def test_many_rows_and_offsets_beyond_32_bits():
     for n, classes, k in ((100001, 12, 3), (30001, 70, 40), (9000, 400, 8), (6001, 1003, 5),
                           (5003, 1900, 4)):
