@@ -71,7 +71,7 @@ __device__ inline void teach(const DistillArgs &a, const Taught &t, const T *s, 
         int c = there ? a.index[at] : -1;
         const float said = there ? wide(a.teacher, a.teacher_type, at) : 0.f;
         if (c < 0 || c >= a.classes) c = -1;
-        const float v = c >= 0 ? said / a.temperature : -INFINITY;
+        const float v = c >= 0 ? said : -INFINITY;
         t.index[j] = c;
         t.p[j] = v;
         t.logit[j] = c >= 0 ? (float)s[c] : 0.f;
@@ -81,7 +81,8 @@ __device__ inline void teach(const DistillArgs &a, const Taught &t, const T *s, 
     for (int o = 1; o < lanes; o <<= 1) best = fmaxf(best, __shfl_xor(best, o));
     const float from = best > -INFINITY ? best : 0.f;   // nothing: e^-inf below is 0
     for (int j = lane; j < a.k; j += lanes) {
-        const float e = expf(t.p[j] - from);
+        // over the temperature behind the difference: before it fp32 may not hold them
+        const float e = expf((t.p[j] - from) / a.temperature);
         t.p[j] = e;
         sum += e;
     }

@@ -209,6 +209,19 @@ def test_low_temperatures_of_far_logits(classes):
         _check(s, index, t, heat, rest, label, 0.5, dloss)
 
 
+@pytest.mark.parametrize("classes", [6, 700, 40000])
+def test_low_temperatures_of_a_far_teacher(classes):
+    """A teacher's logits that pass fp32's range over the temperature: they count by their
+    differences."""
+    s, _, t, rest, _, dloss = _inputs(6, classes, 3, torch.float32, seed=24)
+    index = torch.tensor([[1, 2, 3]] * 6, dtype=torch.int32, device="cuda")
+    t[0], t[1], t[2, 0], t[3, 1], t[4, 2] = 1e38, -3e38, 2e38, -1e38, -math.inf
+    t[5, 0], t[5, 1] = 3e38, -3e38
+    for heat in (2.0 ** -20, 2.0 ** -4, 0.5):
+        loss, _ = _check(s, index, t, heat, rest, None, 1.0, dloss)
+        assert torch.isfinite(loss).all() and float(loss.min()) > 0
+
+
 def test_many_rows_and_offsets_beyond_32_bits():
     for n, classes, k in ((100001, 12, 3), (30001, 70, 40), (9000, 400, 8), (6001, 1003, 5),
                           (5003, 1900, 4)):
