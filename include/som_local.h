@@ -361,8 +361,9 @@ som_status som_dispatch(const int32_t *index, int64_t n, int32_t k, int32_t expe
  * that is there (or whose t are all -infinity) has no soft part, one without a label no
  * hard one.  A class may be named more than once: its p add up.  Logits of -infinity
  * close a class: it has a = 0; a row without an open class has loss and gradient 0.  A row
- * whose logits or t hold a NaN or +infinity has NaN for both.  r below 0 counts as 0, above
- * 1 as 1. */
+ * whose logits hold a NaN or +infinity has NaN for both, also one without a teacher's class
+ * and a label; so has one with such a t of a class that is there, unless mix is 0 (t is not
+ * read then).  r below 0 counts as 0, above 1 as 1. */
 typedef struct som_distill_call {
     int32_t type;              /* som_type of logits and dlogits                     */
     int32_t teacher_type;      /* som_type of teacher                                */

@@ -168,7 +168,9 @@ struct Factors {
         f.apart = false, f.lead = f.left = 0.f;
         f.shut = z == 0.f;
         const float soft = b.scale * a.mix * a.temperature, hard = b.scale * (1.f - a.mix);
-        f.chosen = f.other = f.given = f.one = f.label = 0.f;
+        // a logit that is none: all of the row is none, also without a part of its own
+        f.chosen = f.other = z == z ? 0.f : z;
+        f.given = f.one = f.label = 0.f;
         if (f.shut) return f;
         if (a.k && a.mix != 0.f && !(t.rest[1] == 0.f)) {
             f.given = soft * t.rest[1];
@@ -191,6 +193,7 @@ template <int HARD>
 __device__ inline float loss_of(const DistillArgs &a, const Taught &t, const Factors &f, const Beside &b,
                                 int lane, int lanes) {
     if (f.shut) return 0.f;
+    if (f.z != f.z) return f.z;
     float soft = 0.f, away = 0.f, all = 0.f;   // of logarithms; of distances below the maximum
     // half of a logit's distance from the maximum, and not over the temperature: the whole,
     // and what a low temperature makes of it, may pass fp32's range where the loss does not

@@ -147,6 +147,25 @@ def test_named_classes_far_ahead_of_the_others(classes, dtype):
         _check(s, index, t, 2.0 ** -20, rest, label, 0.5, dloss)
 
 
+@pytest.mark.parametrize("dtype", T)
+@pytest.mark.parametrize("classes", [6, 30, 700, 12000, 80000])
+def test_numbers_that_are_none_in_rows_without_parts(classes, dtype):
+    """Neither a teacher's class nor a label: 0 and 0, unless a logit is none."""
+    s, index, t, rest, label, dloss = _inputs(12, classes, 3, T[dtype], seed=4)
+    index[:8], label[:10] = -1, -1
+    s[1, classes - 1], s[2, 0], s[3, 1], s[8, 2] = math.nan, math.inf, math.nan, math.inf
+    s[3, 2:] = -math.inf
+    t[4, 1], t[5] = math.nan, math.inf             # of classes that are not there
+    bad = torch.tensor([i in (1, 2, 3, 8) for i in range(12)], device="cuda")
+    for said, mix in (((index, t, 1.0, rest, label), 0.5), ((index, t, 2.0, rest, None), 1.0),
+                      ((index, t, 1.5, None, label), 0.5), ((None, None, 1.0, None, label), 0.0)):
+        loss, dlogits = local.distill(s, *said, mix, dloss)
+        assert torch.equal(torch.isnan(loss), bad)
+        assert torch.equal(torch.isnan(dlogits).all(1), bad) and torch.equal(torch.isnan(dlogits).any(1), bad)
+        still = torch.tensor([0, 4, 5, 6, 7], device="cuda")
+        assert float(loss[still].abs().max()) == 0 and float(dlogits[still].abs().max()) == 0
+
+
 def test_a_teacher_that_the_student_matches():
     """Every class named, the same logits: loss and gradient are 0 to rounding."""
     s = torch.randn(10, 50, generator=torch.Generator().manual_seed(1)).cuda()
