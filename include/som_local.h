@@ -381,12 +381,13 @@ typedef struct som_distill_call {
     const float *dloss;        /* n; NULL for 1                                      */
     float scale;
     float *loss;               /* n; NULL if not wanted                              */
-    void *dlogits;             /* packed n x classes; NULL if not wanted; may be
-                                  logits, where those are packed                     */
+    void *dlogits;             /* packed n x classes; NULL if not wanted; logits
+                                  themselves, where those are packed, or elsewhere   */
     void *stream;
 } som_distill_call;
 
-/* Errors: SOM_E_ARG, SOM_E_UNSUPPORTED (more than 1,048,576 classes), SOM_E_DEVICE. */
+/* Errors: SOM_E_ARG (dlogits that overlap logits in another way too),
+ * SOM_E_UNSUPPORTED (more than 1,048,576 classes), SOM_E_DEVICE. */
 som_status som_distill(const som_distill_call *call);
 
 /* AdamW over many tensors at once.  Step t of element p with gradient g:

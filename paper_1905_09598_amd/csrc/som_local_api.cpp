@@ -1088,6 +1088,13 @@ som_status som_distill(const som_distill_call *c) {
                  !rows_ok(c->teacher, c->n, c->k, c->k, som::type_size(c->teacher_type))))
         return SOM_E_ARG;
     if (c->n == 0 || (!c->loss && !c->dlogits)) return SOM_OK;
+    // in the logits' place a row is read before it is written, beside them another's are not
+    if (c->dlogits && (c->dlogits != c->logits || (c->lds != c->classes && c->n > 1))) {
+        const char *const from = static_cast<const char *>(c->logits);
+        const char *const to = static_cast<const char *>(c->dlogits);
+        if (to < from + ((c->n - 1) * c->lds + c->classes) * size && from < to + c->n * c->classes * size)
+            return SOM_E_ARG;
+    }
     som::DistillArgs a{};
     a.type = c->type, a.teacher_type = c->teacher_type;
     a.n = c->n, a.classes = c->classes;

@@ -209,6 +209,24 @@ def test_gradient_in_the_logits_place(classes):
     assert torch.equal(loss, want[0]) and torch.equal(s, want[1])
 
 
+def test_gradient_over_other_rows_logits_is_refused():
+    s, index, t, rest, label, dloss = _inputs(4, 40, 2, torch.float32, seed=5)
+    room = torch.zeros(4 * 48 + 200, device="cuda")
+    at = room.data_ptr()
+    loss = torch.empty(4, device="cuda")
+
+    def run(n, lds, first, to):
+        call = local._distill_call(s, index, t, 1.0, rest, label, 0.5, dloss)
+        call.n, call.lds, call.logits, call.dlogits, call.loss = n, lds, at + 4 * first, at + 4 * to, loss.data_ptr()
+        return som.STATUS[local.lib().som_distill(local.C.byref(call))]
+
+    for n, lds, first, to in ((4, 48, 0, 0), (2, 41, 8, 8), (4, 40, 0, 4), (4, 40, 4, 0), (3, 48, 0, 135),
+                              (3, 48, 119, 0), (1, 40, 0, 39)):
+        assert run(n, lds, first, to) == "SOM_E_ARG", (n, lds, first, to)
+    for n, lds, first, to in ((4, 40, 0, 0), (1, 48, 0, 0), (3, 48, 0, 136), (3, 48, 120, 0)):
+        assert run(n, lds, first, to) == "SOM_OK", (n, lds, first, to)
+
+
 @pytest.mark.parametrize("heat", [2.0 ** -20, 2.0 ** 20])
 def test_temperatures_at_their_ends(heat):
     s, index, t, rest, label, dloss = _inputs(30, 90, 4, torch.float32, seed=8)
