@@ -2,6 +2,8 @@
 // models (som_local.h).  Not part of the public ABI.
 #pragma once
 
+#include "som_grid.h"
+
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -12,11 +14,6 @@ enum : int32_t { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };  // s
 enum : int32_t { kForward = 0, kInput = 1, kWeight = 2, kGate = 3, kPair = 4 };  // which product
 
 inline int type_size(int32_t type) { return type == kF32 ? 4 : 2; }
-
-// A dimension of a grid counts its threads in 32 bits.
-inline bool grid_holds(int64_t blocks, int64_t threads) {
-    return blocks <= ((int64_t)UINT32_MAX) / threads;
-}
 
 // The activations and their slopes, on the hardware's exponential and reciprocal
 // (each within one unit in the last place): an exact division or the library's

@@ -199,8 +199,7 @@ hipError_t launch_to_blocks(const BlocksArgs &args, hipStream_t stream) {
     BlocksArgs a = args;
     const int64_t units = a.ld_scale / 4, size = type_size(a.type);
     a.units = Divider((uint32_t)units);
-    // as many rows at a time as keep the numbers of their units below 2^31
-    const int64_t most = std::max<int64_t>(1, (INT32_MAX - 4) / units);
+    const int64_t most = rows_at_once(units, 4, 256);
     for (int64_t r = 0; r < args.n; r += most) {
         a.n = std::min(most, args.n - r);
         const unsigned groups = (unsigned)((a.n * units + 3) / 4);

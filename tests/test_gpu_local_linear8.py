@@ -113,6 +113,28 @@ def test_blocks_of_strided_rows(offset, gap, dtype):
     _check_blocks(v)
 
 
+def test_blocks_and_products_of_more_rows_than_one_launch_takes():
+    """Four rows of up to 512 values to a workgroup of 256 threads, of which a grid counts
+    2^32 - 1: 67,108,860 rows."""
+    most = (2 ** 32 - 1) // 256 * 4
+    n, ends = most + 1003, [0, 500, most - 300, most, most + 300, most + 1003]
+    say("blocks", n)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(n, 3, generator=g, device="cuda", dtype=torch.bfloat16)
+    b = local.to_blocks(x)
+    w8 = local.to_blocks(_draw(2, 2, 3, dtype=torch.bfloat16))
+    bias = _draw(3, 2, dtype=torch.bfloat16)
+    for first, last in zip(ends[::2], ends[1::2]):
+        part = _check_blocks(x[first:last].contiguous())
+        assert torch.equal(b.codes.view(torch.uint8)[first:last], part.codes.view(torch.uint8))
+        assert torch.equal(b.scale.view(torch.uint8)[first:last], part.scale.view(torch.uint8))
+    del b
+    y = local.linear8(x, w8, bias)
+    for first, last in zip(ends[::2], ends[1::2]):
+        held = local.to_blocks(x[first:last].contiguous())
+        O.close(y[first:last], O.linear8(O.d(held.float()), O.d(w8.float()), O.d(bias), "none", None, x.dtype), "y")
+
+
 def _case(n, inner, outer, dtype, seed=0):
     return (_draw(seed, n, inner, dtype=dtype), _draw(seed + 1, outer, inner, dtype=dtype,
                                                       scale=inner ** -0.5),
