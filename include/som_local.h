@@ -145,8 +145,10 @@ typedef struct som_linear8_call {
     void *stream;
 } som_linear8_call;
 
-/* Errors: as som_linear. */
+/* Errors: as som_linear.  Route: the rows and columns of a workgroup's tile (256, 128 or
+ * 64; 16: the kernel of few rows), and the parts of the contraction that are planned. */
 som_status som_linear8_workspace(const som_linear8_call *call, uint64_t *bytes);
+som_status som_linear8_route(const som_linear8_call *call, int32_t route[2]);
 som_status som_linear8(const som_linear8_call *call);
 
 /* A gated layer, of x (n x inner) and two matrices w (2 x hidden x inner) at once:

@@ -977,6 +977,19 @@ som_status som_linear8_workspace(const som_linear8_call *c, uint64_t *bytes) {
     return st;
 }
 
+som_status som_linear8_route(const som_linear8_call *c, int32_t route[2]) {
+    if (!route) return SOM_E_ARG;
+    const som_status st = linear8_sizes_ok(c);
+    if (st != SOM_OK) return st;
+    route[0] = route[1] = 0;
+    if (c->n) {
+        Carver need(nullptr);
+        const Linear8 call(*c, need);
+        route[0] = call.plan.tile, route[1] = call.plan.splits;
+    }
+    return SOM_OK;
+}
+
 som_status som_linear8(const som_linear8_call *c) {
     const som_status st = linear8_sizes_ok(c);
     if (st != SOM_OK) return st;

@@ -58,7 +58,7 @@ BLOCK = 128
 # Every symbol include/som_local.h declares.
 EXPORTED = (
     "som_linear_workspace", "som_linear_route", "som_linear", "som_linear_backward",
-    "som_to_blocks", "som_linear8_workspace", "som_linear8",
+    "som_to_blocks", "som_linear8_workspace", "som_linear8_route", "som_linear8",
     "som_gated_workspace", "som_gated_route", "som_gated", "som_gated_backward",
     "som_experts_workspace", "som_experts_route", "som_experts", "som_experts_backward",
     "som_norm_workspace", "som_norm", "som_norm_backward",
@@ -191,6 +191,7 @@ def lib():
         "som_linear_backward": [C.POINTER(_LinearCall)],
         "som_to_blocks": [C.POINTER(_BlocksCall)],
         "som_linear8_workspace": [C.POINTER(_Linear8Call), C.POINTER(u64)],
+        "som_linear8_route": [C.POINTER(_Linear8Call), C.POINTER(i32)],
         "som_linear8": [C.POINTER(_Linear8Call)],
         "som_gated_workspace": [C.POINTER(_GatedCall), i32, C.POINTER(u64)],
         "som_gated_route": [C.POINTER(_GatedCall), i32, C.POINTER(i32)],

@@ -188,6 +188,40 @@ def test_tiles_and_splits(n, inner, outer, dtype):
     _check(x, w, b, r, "none")
 
 
+def _route(n, inner, outer, dtype):
+    call = local._Linear8Call(type=local._TYPES[dtype], n=n, inner=inner, outer=outer, ldx=inner)
+    route = (local.C.c_int32 * 2)()
+    som._check(local.lib().som_linear8_route(local.C.byref(call), route), "som_linear8_route")
+    return route[0], route[1]
+
+
+# every tile, whole and in parts, by the library's own answer; contractions of 1 to 106 blocks,
+# so that words of powers begin and end at every place of a slab loop
+ROUTES = [(256, False, 4097, 1300, 2048), (256, False, 4097, 640, 2048), (256, False, 1064, 1029, 7750),
+          (256, True, 1601, 11700, 2707), (128, False, 637, 128, 8192), (128, False, 2711, 1031, 1481),
+          (128, False, 2000, 1537, 3000), (128, True, 827, 13541, 2099), (64, False, 1500, 600, 2500),
+          (64, False, 1100, 2300, 520), (64, True, 200, 9000, 100), (64, True, 300, 4545, 300),
+          (64, True, 17, 1231, 8), (16, False, 16, 5000, 300), (16, False, 5, 20001, 40)]
+
+
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("tile,parts,n,inner,outer", ROUTES)
+def test_every_tile_whole_and_in_parts(tile, parts, n, inner, outer, dtype):
+    """Rows and blocks whose sizes lie far apart, so that no power of two of another row or
+    block passes for their own."""
+    say("linear8", tile, parts, n, inner, outer, dtype)
+    route = _route(n, inner, outer, T[dtype])
+    assert route[0] == tile and (route[1] > 1) == parts, route
+    x, w, b, r = _case(n, inner, outer, T[dtype], seed=n)
+    g = torch.Generator().manual_seed(3)
+    far = 20 if dtype == "bf16" else 3
+    for t in (x, w):
+        count = -(-inner // 128)
+        s = torch.exp2(torch.randint(-far, far, (t.shape[0], count), generator=g).float()).cuda()
+        t.mul_(s.repeat_interleave(128, 1)[:, :inner].to(t.dtype))
+    _check(x, w, b, r, "none" if dtype == "bf16" else "silu")
+
+
 @pytest.mark.parametrize("n", [3, 150])
 def test_blocks_of_their_own_powers(n):
     """Rows and blocks whose sizes lie far apart: every power of two goes to its own."""

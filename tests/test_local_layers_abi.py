@@ -123,6 +123,24 @@ def test_linear8_refuses(change, want):
         want if change else "SOM_OK")
 
 
+@pytest.mark.parametrize("n,inner,outer", [(0, 40, 24), (1, 8, 8), (16, 2048, 10000), (17, 1231, 8),
+                                           (637, 128, 8192), (1601, 11700, 2707)])
+def test_linear8_route_agrees_with_its_work_memory(n, inner, outer):
+    """In 8 bits already, a product needs memory for the parts of its contraction alone."""
+    L, need, route = local.lib(), C.c_uint64(), (C.c_int32 * 2)(-1, -1)
+    call = local._Linear8Call(type=1, n=n, inner=inner, outer=outer, ldx=inner, x_codes=256)
+    assert status(L.som_linear8_route(C.byref(call), route)) == "SOM_OK"
+    assert status(L.som_linear8_workspace(C.byref(call), C.byref(need))) == "SOM_OK"
+    tile, parts = route
+    assert (tile, parts) == (0, 0) if n == 0 else tile in (16, 64, 128, 256) and parts >= 1
+    assert (tile == 16) == (0 < n <= 16)
+    wide = -(-outer // tile) * tile if n else 0
+    assert need.value == (-(-parts * n * wide * 4 // 256) * 256 if parts > 1 else 0)
+    assert L.som_linear8_route(C.byref(call), None) == 1 and L.som_linear8_route(None, route) == 1
+    call.type = 0
+    assert status(L.som_linear8_route(C.byref(call), route)) == "SOM_E_ARG"
+
+
 def test_null_calls():
     L, need = local.lib(), C.c_uint64()
     for name in ("som_norm", "som_norm_backward", "som_gated", "som_gated_backward", "som_distill",
