@@ -157,7 +157,9 @@ som_status som_linear8(const som_linear8_call *call);
  * rounded to 16 bits its errors would reach all of the gradient.  From dy,
  *     dz = [ dy v act'(u)   dy act(u) ]
  *     dx = dz w    dw = dz^T x    dbias = sum of dz's rows
- * dz is held in the element type for the two products, not for dbias. */
+ * dz is held in the element type for the two products, not for dbias; in fp16, over a power
+ * of two that the products take back where its largest finite magnitude is outside
+ * [1/4, 65520): elements keep all bits down to 2^-12 of the largest. */
 typedef struct som_gated_call {
     int32_t type;              /* som_type of all matrices but z                     */
     int32_t activation;        /* som_activation                                     */

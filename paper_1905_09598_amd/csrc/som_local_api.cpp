@@ -443,6 +443,12 @@ struct GatedBackward {
         slopes.dz = const_cast<void *>(dz.p);
         slopes.parts = som::gated_parts(slopes, compute_units());
         if (c.dbias) slopes.partial = work.take<float>((uint64_t)slopes.parts * both * 4);
+        const int64_t largest = som::gated_largest(slopes);
+        if (largest) {
+            slopes.largest = work.take<float>((uint64_t)largest * 4);
+            slopes.power = work.take<int32_t>(4);
+            input.a.power = weight.a.power = slopes.power;
+        }
         if (has_input) {
             ProductArgs &a = input.a;
             a.mode = som::kInput;

@@ -183,6 +183,7 @@ struct ProductArgs {
     int32_t eight;                    // both sides in 8 bits, k in whole blocks of 128
     const unsigned char *scale_a, *scale_b;   // their powers of two, rows ld_scale apart
     int64_t ld_scale;
+    const int32_t *power;             // input, weight in fp16: y = 2^power C; NULL for 0
     int32_t splits;       // parts of the contraction
     float *partial;       // splits x partial_rows x whole tiles
     int64_t partial_rows;
@@ -402,7 +403,8 @@ hipError_t launch_join_parts(int32_t type, const float *partial, int32_t parts, 
                              void *first, void *second, hipStream_t stream);
 
 // som_gated.hip: dz (rows of ldd >= 2 hidden, filled up with zeros) of a gated layer from
-// dy and z, and the parts of its columns' sums (parts x 2 hidden, or NULL).
+// dy and z, and the parts of its columns' sums (parts x 2 hidden, or NULL).  In fp16 what is
+// written is dz / 2^power; largest: gated_largest floats.
 struct GatedArgs {
     int32_t type, activation;
     int64_t n, hidden;
@@ -413,8 +415,11 @@ struct GatedArgs {
     int64_t ldd;
     float *partial;
     int32_t parts;
+    float *largest;
+    int32_t *power;
 };
 int32_t gated_parts(const GatedArgs &a, int num_cus);   // a function of type, n and hidden
+int64_t gated_largest(const GatedArgs &a);              // and of parts; 0: not fp16
 hipError_t launch_gated_slopes(const GatedArgs &a, hipStream_t stream);
 
 ProductPlan plan_product(const ProductArgs &a, bool aligned, int num_cus);

@@ -351,9 +351,10 @@ template <typename T, int MODE, int N>
 struct Epilogue {
     const ProductArgs &a;
     int64_t col;
-    int batch, left;
+    int batch, left, power;
     float bias[N];
     static constexpr bool kImage = MODE == kGate && sizeof(T) == 2;
+    static constexpr bool kPower = (MODE == kInput || MODE == kWeight) && std::is_same<T, _Float16>::value;
     // Beside a row's sums: its residual (forward) or the argument of its activation
     // (gate), and the weight of its slot.
     struct Row {
@@ -362,6 +363,7 @@ struct Epilogue {
     };
     __device__ Epilogue(const ProductArgs &args, int64_t c, int b) : a(args), col(c), batch(b) {
         left = (int)(a.n - col < N ? a.n - col : N);
+        power = kPower && a.power ? *a.power : 0;
         Piece<T, N> p;
         const bool there = MODE == kForward && a.bias && left > 0;
         if (there) p.read(static_cast<const T *>(a.bias) + batch * a.n + col, left);
@@ -418,6 +420,10 @@ struct Epilogue {
     __device__ float write(int64_t row, const Row &r, const Piece<T, N> &image, float (&v)[N]) const {
         const int64_t at = ((MODE == kWeight ? batch * a.m : 0) + row) * a.n + col;
         float dot = 0.f;
+        if (kPower && a.power) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = __builtin_amdgcn_ldexpf(v[e], power);
+        }
         if (MODE == kForward) {
 #pragma unroll
             for (int e = 0; e < N; ++e) v[e] += bias[e];

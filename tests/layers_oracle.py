@@ -224,8 +224,21 @@ def gated(x, w, b, kind, dtype):
     return (y, err + stored(y, dtype)), (z.view(n, 2, hidden), zerr.view(n, 2, hidden))
 
 
-def gated_backward(dy, x, w, z, kind, dtype):
-    """{"dx", "dw", "db"} from z = (value, bound)."""
+def held(dz):
+    """How far fp16 is off that holds dz over a power of two with which the largest
+    magnitude lies in [2^14, 2^15), unless it lies in [1/4, 65,520) already: half a step,
+    2^-11 of the value or 2^-25 and the power, whichever is more."""
+    size = dz.abs()
+    largest = float(torch.where(torch.isfinite(size), size, size * 0).max()) if size.numel() else 0.0
+    power = 0
+    if largest and not 0.2499 <= largest < 65600:      # next to the ends either is right
+        power = math.frexp(largest)[1] - 14
+    return torch.maximum(size * 2.0 ** -11, torch.full_like(size, 2.0 ** (power - 25)))
+
+
+def gated_backward(dy, x, w, z, kind, dtype, powers=False):
+    """{"dx", "dw", "db"} from z = (value, bound).  powers: fp16's dz is held over a power of
+    two (held), not as it is."""
     n, k = x.shape
     hidden = w.shape[1]
     u, v = z[0][:, 0], z[0][:, 1]
@@ -238,7 +251,7 @@ def gated_backward(dy, x, w, z, kind, dtype):
     dz = torch.cat([dy * v * slope, dy * h], 1)
     raw = torch.cat([dy.abs() * (se * (v.abs() + ve) + slope.abs() * ve), dy.abs() * he], 1)
     raw = raw + 4 * V * dz.abs()
-    err = raw + stored(dz, dtype)        # held in dtype for the two products
+    err = raw + (held(dz) if powers else stored(dz, dtype))      # for the two products
     flat = w.reshape(2 * hidden, k)
     dx, dw, db = dz @ flat, dz.t() @ x, dz.sum(0)
     dx_err = (2 * hidden + 8) * V * (dz.abs() @ flat.abs()) + err @ flat.abs()

@@ -108,6 +108,75 @@ def test_row_strides_and_odd_beginnings(n, offset, gap, dtype):
     _check(x, w, b, dy, "gelu")
 
 
+def _scaled(n, inner, hidden, x, w, u, v, dy, seed=1):
+    """fp16 inputs of these sizes: x and w of normal values, biases about u and v."""
+    t = torch.float16
+    b = torch.cat([_draw(seed + 2, 1, hidden, dtype=torch.float32, scale=u),
+                   v * (1 + 0.2 * _draw(seed + 4, 1, hidden, dtype=torch.float32))]).to(t)
+    return (_draw(seed, n, inner, dtype=t, scale=x), _draw(seed + 1, 2, hidden, inner, dtype=t, scale=w),
+            b, _draw(seed + 3, n, hidden, dtype=t, scale=dy))
+
+
+def _check_powers(x, w, b, dy, kind):
+    z = local.gated(x, w, b, kind, keep=True)[1]
+    wz = O.gated(O.d(x), O.d(w), O.d(b), kind, x.dtype)[1]
+    got = dict(zip(("dx", "dw", "db"), local.gated_backward(dy, x, w, z, kind)))
+    g = O.gated_backward(O.d(dy), O.d(x), O.d(w), wz, kind, x.dtype, powers=True)
+    for name, t in got.items():
+        value, bound = g[name]
+        ordinary = value.abs() < 65000      # beyond, fp16 rounds to infinity
+        assert name == "db" or ordinary.all(), name
+        O.close(t[ordinary], (value[ordinary], bound[ordinary]), name)
+
+
+# sizes of x, w, u, v and dy: dy v of 10^6 and more, whose products with w and x are ordinary
+# numbers; dy v of 10^-7 and less, whose products with large x or w are; and dy v between
+@pytest.mark.parametrize("kind", ["silu", "gelu", "none"])
+@pytest.mark.parametrize("n,inner,hidden", [(1, 40, 24), (70, 129, 33), (600, 520, 264), (5000, 64, 500)])
+@pytest.mark.parametrize("x,w,u,v,dy", [(3e-5, 1e-4, 1.0, 20000.0, 100.0), (1e-6, 1e-6, 1.0, 3e4, 2e3),
+                                        (2000.0, 1e-4, 0.5, 0.01, 1e-5), (0.001, 50.0, 0.5, 0.02, 3e-6),
+                                        (300.0, 0.003, 0.5, 1.0, 2e-4), (1.0, 0.05, 1.0, 1.0, 1.0)])
+def test_gradients_of_every_size_in_fp16(x, w, u, v, dy, n, inner, hidden, kind):
+    say("gated powers", x, w, v, dy, n, inner, hidden, kind)
+    _check_powers(*_scaled(n, inner, hidden, x, w, u, v, dy), kind)
+
+
+def test_fp16_gradients_without_a_largest_number():
+    """All zeros; numbers that are none, which leave the others' power alone."""
+    x, w, b, dy = _scaled(90, 72, 40, 1.0, 0.1, 1.0, 1.0, 1e-6)
+    z = local.gated(x, w, b, keep=True)[1]
+    for t in local.gated_backward(torch.zeros_like(dy), x, w, z):
+        assert float(t.abs().max()) == 0
+    clean = local.gated_backward(dy, x, w, z)
+    dy[5, 3], dy[6, 4] = math.inf, math.nan
+    dx, dw, db = local.gated_backward(dy, x, w, z)
+    keep = torch.tensor([i not in (5, 6) for i in range(90)], device="cuda")
+    assert torch.equal(dx[keep], clean[0][keep]) and not torch.isfinite(dx[5:7]).any()
+    rows = torch.tensor([i not in (3, 4) for i in range(40)], device="cuda")
+    assert torch.equal(dw[:, rows], clean[1][:, rows]) and torch.equal(db[:, rows], clean[2][:, rows])
+
+
+def test_fp16_powers_of_replays_are_their_own():
+    """A captured gradient takes the power of two that each replay's values ask for."""
+    x, w, b, dy = _scaled(300, 256, 96, 0.001, 0.01, 1.0, 100.0, 1.0)
+    z = local.gated(x, w, b, keep=True)[1]
+    first = dy.clone()
+    local.gated_backward(dy, x, w, z)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = local.gated_backward(dy, x, w, z)
+    for size in (1.0, 2.0 ** 10, 2.0 ** -16, 1.0, 2.0 ** -18, 2.0 ** 9):
+        dy.copy_(first * size)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, c in zip(got, local.gated_backward(dy, x, w, z)):
+            assert torch.equal(a, c)
+        g = O.gated_backward(O.d(dy), O.d(x), O.d(w), O.gated(O.d(x), O.d(w), O.d(b), "silu", x.dtype)[1], "silu",
+                             x.dtype, powers=True)
+        O.close(got[1], g["dw"], "dw")
+
+
 @pytest.mark.parametrize("dtype", T)
 def test_many_rows_of_few_columns(dtype):
     _check(*_case(20000, 16, 5, T[dtype], seed=3), kind="gelu")
