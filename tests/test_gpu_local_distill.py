@@ -273,6 +273,25 @@ def test_many_rows_and_offsets_beyond_32_bits():
         assert torch.equal(u, w)
 
 
+@pytest.mark.parametrize("dtype", T)
+@pytest.mark.parametrize("n,classes,k", [(100001, 12, 3), (30001, 70, 40), (9000, 230, 8), (9000, 400, 8),
+                                         (6001, 1003, 5), (5003, 520, 4)])
+def test_many_rows_of_few_lanes(n, classes, k, dtype):
+    """Of many short rows a lane takes up to four pieces; rows whose named classes lead far
+    beside rows in the same wave where they do not."""
+    say("many rows", n, classes, k, dtype)
+    s, index, t, rest, label, dloss = _inputs(n, classes, k, T[dtype], seed=classes)
+    named = torch.zeros(n, classes + 1, dtype=torch.bool, device="cuda")
+    named.scatter_(1, torch.where((index >= 0) & (index < classes), index, classes).long(), True)
+    far = torch.arange(n, device="cuda")[:, None] % 7 == 3
+    s = torch.where(far & ~named[:, :classes], s - 120, s)
+    _check(s, index, t, 1.0, rest, label, 0.5, dloss)
+    _check(s, index, t, 1.5, rest, None, 1.0, dloss)
+    # the same document in a small batch, where a row is on more lanes: within their roundings
+    part = torch.cat([torch.arange(40), torch.arange(n - 9, n)]).cuda()
+    _check(s[part], index[part], t[part], 1.5, rest[part], None, 1.0, dloss[part])
+
+
 @pytest.mark.parametrize("classes", [3000, 75233])
 @pytest.mark.parametrize("share", [0.01, 0.99])
 def test_shares_next_to_one(classes, share):
