@@ -9,10 +9,11 @@
 // A row stays in registers as it was read, 16-byte pieces of it to a lane, of 1 to 64
 // lanes or of a workgroup; only rows beyond what a workgroup holds are read twice.  R is
 // summed by itself (Z less the teacher's classes would cancel): the teacher's classes are
-// marked by bits in LDS, of which a piece of a row takes its own in one read.  All
+// marked by bits in LDS, of which a piece of a row takes its own in one read.  Where R is
+// next to nothing it is summed once more, from its own classes' maximum (kApart).  All
 // gradients are written as if no class were named, and the few that are once more behind a
 // barrier.  What a row has beside its logits is read while they are on their way.  16,001
-// bf16 rows of 10,000, eight named classes and labels, take 152 us (4.2 TB/s); with the
+// bf16 rows of 10,000, eight named classes and labels, take 157 us (4.1 TB/s); with the
 // named classes tested for on the way, and the rest read when it was needed, 198.  Rows of
 // 200,003 are read twice: 512 of them 146 us (instructions 83 of it by count).
 #include "som_row.h"
@@ -98,8 +99,8 @@ __device__ inline void teach(const DistillArgs &a, const Taught &t, const T *s, 
 
 // How labels' exponentials come.  At temperatures of 1, 2 and 4 they are the others', squared
 // none, one or two times, off by no more than by themselves: the error of the product in the
-// exponent doubles with the exponent either way.  (16,001 bf16 rows of 10,000 at 2: 178 us
-// with exponentials of their own, 166 so.)
+// exponent doubles with the exponent either way.  (16,001 bf16 rows of 10,000 at 2: 175 us
+// with exponentials of their own, 160 so.)
 enum : int { kNoLabels = 0, kOwn = 1, kSame = 2, kSquared = 3, kTwice = 4 };
 
 // 2^((v - top) c) of N logits and, with labels, e^(v - top).
@@ -520,9 +521,9 @@ __global__ __launch_bounds__(1024) void distill_long_kernel(DistillArgs a) {
 // Pieces that a lane holds: 1, 2 or 4 of a row that a wave or less takes, 4 or 8 of one that
 // a workgroup takes (16 are more than the registers of 1024 threads).  Short rows wait for
 // their reads and reductions, not for memory: of many rows a lane takes more pieces, so that
-// a wave has more rows under way (60,000 bf16 rows of 400: one piece 71 us, four 35; of 1000
-// two 88, four 62), of few rows one, so that they are on more compute units.  Rows of more
-// than 128 pieces go to a workgroup (60,000 of 1030: 89 us, to the lanes of a wave 104).
+// a wave has more rows under way (60,000 bf16 rows of 400: one piece 71 us, four 36; of 1000
+// two 88, four 63), of few rows one, so that they are on more compute units.  Rows of more
+// than 128 pieces go to a workgroup (60,000 of 1030: 91 us, to the lanes of a wave 104).
 constexpr int kNarrowPieces = 4, kWidePieces = 8;
 constexpr int64_t kManyWaves = 4096;   // 16 to a compute unit
 

@@ -7,13 +7,13 @@
 // keeps to its columns, 16 bytes of dy, and goes down a group of rows with the sums of
 // its columns in registers; the groups' sums are joined in order (som_norm.hip).  dz is
 // rounded to the element type for the matrix instructions, the sums are of dz before that.
-// 8192 x 4096 in bf16: 90 us (5.2 TB/s).
+// 8192 x 4096 in bf16: 113 us (4.2 TB/s).
 // fp16 does not hold all of dz's range, where the gradients of x and w may be ordinary
-// numbers: dy v passes 65,504 from v of 1000 on, and dy of a mean's loss begins next to its
-// subnormals.  There the pass keeps its largest magnitude too, and a second launch, which
+// numbers: dy v can pass 65,520 where neither does, and dy of a mean's loss begins next to
+// its subnormals.  There the pass keeps its largest magnitude too, and a second launch, which
 // otherwise only looks, writes dz once more over a power of two where that is outside
-// [1/4, 65,520); the products take the power to their sums.  2.6 us where it only looks,
-// 95 of 8192 x 4096 where it writes.
+// [1/4, 65,520); the products take the power to their sums.  2.4 us where it only looks,
+// 85 of 8192 x 4096 where it writes.
 #include "som_local_internal.h"
 
 #include <algorithm>
@@ -143,8 +143,8 @@ int64_t wide_of(const GatedArgs &a) {
 }  // namespace
 
 // Groups of rows: of as many threads as two workgroups to a compute unit have, and two
-// rows or more to a group (8192 x 4096 in bf16 with the join of the sums: two 95 us, four
-// 103, eight 113, sixteen 129).
+// rows or more to a group (8192 x 4096 in bf16 with the join of the sums: two 117 us, four
+// 122, eight 128, sixteen 146).
 int32_t gated_parts(const GatedArgs &a, int num_cus) {
     const int64_t rows = kThreads / lanes_of(a);
     const int64_t most = std::max<int64_t>(1, (int64_t)num_cus * 2 / wide_of(a)) * rows;

@@ -533,10 +533,11 @@ struct PairEpilogue {
 // bank conflict, at 2.05 GHz, and fetches 269 MB of the 201 it needs: bound by what the
 // slabs and the epilogue wait for.  Small tiles fill the chip where there are few
 // (plan_product).  A gated layer's pair of matrices (8192 x 2048 by twice 4096 in bf16,
-// silu) takes 225 us where one matrix of 8192 rows takes 243, which has twice the columns to
-// store; the two sums in fp32 for a gradient take 35 more.  In 8 bits 8192 x 2048 x 8192
-// takes 155 us (1770 TFLOP/s), 192 with gelu, bias and a residual, 8192^3 442 (2490): a slab
-// takes as long as one of 16 bits, of twice the work.
+// silu) takes 217 to 225 us where one matrix of 8192 rows takes 236 to 243, which has twice
+// the columns to store; the two sums in fp32 for a gradient take 35 to 56 more.  In 8 bits
+// 8192 x 2048 x 8192 takes 144 to 155 us (1770 to 1910 TFLOP/s), 178 to 211 with gelu, bias
+// and a residual, 8192^3 436 (2520): a slab takes as long as one of 16 bits, of twice the
+// work.
 template <typename T, typename Out, int MODE, int LIST, bool DMA, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN * 64, 2) void product_kernel(ProductArgs a) {
     constexpr bool kEight = sizeof(T) == 1;
