@@ -250,7 +250,8 @@ som_status som_experts_backward(const som_experts_call *call);
 /* Layer norm of n rows,
  *     y = (x - mean) rstd weight + bias,    rstd = 1 / sqrt(var + eps),
  * mean and var (the mean square of x - mean) over a row.  Forward writes mean and rstd
- * of each row to `kept`, unless it is NULL; backward reads them there.  From dy, with
+ * of each row to `kept`, unless it is NULL; backward reads them there, and takes the
+ * rounding of that mean, which x shows, out of what it gives.  From dy, with
  * g = dy weight and xh = (x - mean) rstd,
  *     dx = rstd (g - mean(g) - xh mean(g xh)) + beside
  *     dweight = sum over rows of dy xh     dbias = sum over rows of dy

@@ -303,7 +303,7 @@ template <typename T, int P, bool WIDE, int HARD>
 __global__ __launch_bounds__(1024) void distill_kernel(DistillArgs a) {
     constexpr int N = 16 / sizeof(T);
     extern __shared__ char lds[];
-    __shared__ float part[WIDE ? kPart : 1];
+    __shared__ __align__(16) float part[WIDE ? kPart : 1];
     int turn = 0;
     const Part<WIDE, P, N> me(a.lanes, a.classes);
     const int64_t row = (int64_t)blockIdx.x * me.rows + me.row;
@@ -410,7 +410,7 @@ template <typename T, int HARD>
 __global__ __launch_bounds__(1024) void distill_long_kernel(DistillArgs a) {
     constexpr int N = 16 / sizeof(T), kAhead = 4;
     extern __shared__ char lds[];
-    __shared__ float part[kPart];
+    __shared__ __align__(16) float part[kPart];
     int turn = 0;
     const int64_t row = blockIdx.x;
     const T *const s = static_cast<const T *>(a.logits) + row * a.lds;

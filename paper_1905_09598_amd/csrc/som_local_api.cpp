@@ -1033,8 +1033,10 @@ static som::NormArgs norm_args(const som_norm_call &c) {
     return a;
 }
 
-static uint64_t norm_parts_bytes(const som::NormArgs &a) {
-    return (uint64_t)a.parts * 2 * a.width * 4;
+// The work memory of backward.
+static void norm_place(som::NormArgs &a, Carver &work) {
+    a.partial = work.take<float>((uint64_t)a.parts * 2 * a.width * 4);
+    if (som::norm_long_columns(a)) a.off = work.take<float>((uint64_t)a.n * 4);
 }
 
 static bool norm_common_ok(const som_norm_call &c) {
@@ -1048,7 +1050,8 @@ som_status som_norm_workspace(const som_norm_call *c, int32_t backward, uint64_t
     const som_status st = norm_ok(c);
     if (st == SOM_OK) {
         Carver need(nullptr);
-        if (backward) need.take(norm_parts_bytes(norm_args(*c)));
+        som::NormArgs a = norm_args(*c);
+        if (backward) norm_place(a, need);
         *bytes = need.used;
     }
     return st;
@@ -1079,7 +1082,7 @@ som_status som_norm_backward(const som_norm_call *c) {
         return SOM_E_ARG;
     Carver work(c->workspace);
     som::NormArgs a = norm_args(*c);
-    a.partial = work.take<float>(norm_parts_bytes(a));
+    norm_place(a, work);
     const som_status ok = work_ok(work, c->workspace, c->workspace_bytes);
     if (ok != SOM_OK) return ok;
     if (!a.parts && (c->n == 0 || !c->dx)) return SOM_OK;

@@ -348,10 +348,12 @@ struct NormArgs {
     int64_t lddy, ldb;
     void *dx, *dweight, *dbias;
     float *partial;         // parts x 2 x width
+    float *off;             // n, where norm_long_columns
     int32_t parts, lanes;   // groups of rows; lanes of a row
     float over;             // 1 / width
 };
 int32_t norm_parts(const NormArgs &a, int num_cus);   // a function of type, n and width
+bool norm_long_columns(const NormArgs &a);            // and of which gradients are wanted
 hipError_t launch_norm(const NormArgs &a, int num_cus, hipStream_t stream);
 hipError_t launch_norm_backward(const NormArgs &a, int num_cus, hipStream_t stream);
 

@@ -23,7 +23,7 @@ namespace {
 template <typename T, int P, bool WIDE>
 __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
     constexpr int N = 16 / sizeof(T);
-    __shared__ float part[kPart];
+    __shared__ __align__(16) float part[kPart];
     int turn = 0;
     const Part<WIDE, P, N> me(a.lanes, (int)a.width);
     Piece<T, N> weight[P], bias[P];
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
     constexpr int N = 16 / sizeof(T);
-    __shared__ float part[kPart];
+    __shared__ __align__(16) float part[kPart];
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const T *const x = static_cast<const T *>(a.x) + row * a.ldx;
@@ -139,6 +139,20 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
     }
 }
 
+// What backward's sums of a row give: of g, of g (x - mean), of x - mean.  kept holds the
+// mean as fp32 rounds it, so what the differences from it add up to is taken out again, as
+// forward does: the gradients of rows far from 0 keep their bits.  With xh of the rounded mean,
+//     dx = rstd (g - level - xh slope) + beside,    dweight = sum of dy (xh - off).
+struct Shares {
+    float off, slope, level;
+    __device__ Shares(const float (&sums)[3], float rstd, float over) {
+        const float g = sums[0] * over;
+        off = sums[2] * over * rstd;
+        slope = sums[1] * over * rstd - off * g;
+        level = g - off * slope;
+    }
+};
+
 // COLUMNS: also the workgroup's parts of dweight and dbias.  AHEAD: a row's reads are on
 // their way while the one before it is worked on; that takes the registers of a larger
 // workgroup than kAheadThreads.
@@ -146,7 +160,7 @@ constexpr int kAheadThreads = 768;
 template <typename T, int P, bool WIDE, bool COLUMNS, bool AHEAD>
 __global__ __launch_bounds__(AHEAD ? kAheadThreads : 1024) void norm_backward_kernel(NormArgs a) {
     constexpr int N = 16 / sizeof(T);
-    extern __shared__ float lds[];
+    extern __shared__ __align__(16) float lds[];
     float *const part = lds;          // kPart
     int turn = 0;
     const Part<WIDE, P, N> me(a.lanes, (int)a.width);
@@ -185,31 +199,33 @@ __global__ __launch_bounds__(AHEAD ? kAheadThreads : 1024) void norm_backward_ke
         } else {
             read(row, here);
         }
-        const auto &x = here.x, &dy = here.dy, &beside = here.beside;
+        auto &x = here.x, &dy = here.dy;
+        const auto &beside = here.beside;
         const float mean = here.mean, rstd = here.rstd;
-        float both[2] = {0.f, 0.f};
+        float sums[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            float u[N];
+            float u[N], d[N];
 #pragma unroll
-            for (int e = 0; e < N; ++e) u[e] = (float)dy[p].v[e];
+            for (int e = 0; e < N; ++e) u[e] = (float)dy[p].v[e], d[e] = (float)x[p].v[e] - mean;
             me.clear(p, u);
+            me.clear(p, d);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                const float xh = ((float)x[p].v[e] - mean) * rstd;
                 const float g = a.weight ? u[e] * (float)weight[p].v[e] : u[e];
-                both[0] += g;
-                both[1] = fmaf(g, xh, both[1]);
-                if (COLUMNS) {
-                    dweight[p][e] = fmaf(u[e], xh, dweight[p][e]);
-                    dbias[p][e] += u[e];
-                }
+                sums[0] += g;
+                sums[1] = fmaf(g, d[e], sums[1]);
+                sums[2] += d[e];
             }
+            // fp32's pieces one after the other: three of them together take more registers
+            // than there are (20,000 rows of 4545: 270 us, so 224)
+            if (sizeof(T) == 4) asm volatile("" : "+v"(sums[0]), "+v"(sums[1]), "+v"(sums[2]));
         }
-        if (!a.dx) continue;   // for all lanes alike
-        row_sum<WIDE>(both, a.lanes, part, turn);
+        row_sum<WIDE>(sums, a.lanes, part, turn);
+        keep_raw<T, P>(x);
+        keep_raw<T, P>(dy);
         if (!there) continue;
-        const float g0 = both[0] * a.over, g1 = both[1] * a.over;
+        const Shares s(sums, rstd, a.over);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             Piece<T, N> dx;
@@ -217,12 +233,16 @@ __global__ __launch_bounds__(AHEAD ? kAheadThreads : 1024) void norm_backward_ke
             for (int e = 0; e < N; ++e) {
                 const float u = (float)dy[p].v[e];
                 const float xh = ((float)x[p].v[e] - mean) * rstd;
+                if (COLUMNS) {
+                    dweight[p][e] = fmaf(u, xh - s.off, dweight[p][e]);
+                    dbias[p][e] += u;
+                }
                 const float g = a.weight ? u * (float)weight[p].v[e] : u;
-                float v = rstd * (g - g0 - xh * g1);
+                float v = rstd * (g - s.level - xh * s.slope);
                 if (a.beside) v += (float)beside[p].v[e];
                 dx.v[e] = (T)v;
             }
-            if (me.mine(p)) dx.write(static_cast<T *>(a.dx) + row * a.width + me.at[p], N);
+            if (a.dx && me.mine(p)) dx.write(static_cast<T *>(a.dx) + row * a.width + me.at[p], N);
         }
     }
     if (!COLUMNS) return;
@@ -264,17 +284,17 @@ __global__ __launch_bounds__(AHEAD ? kAheadThreads : 1024) void norm_backward_ke
     }
 }
 
-// dx of such rows.
+// dx of such rows, and what their means are off for their columns' sums.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_long_backward_kernel(NormArgs a) {
     constexpr int N = 16 / sizeof(T);
-    __shared__ float part[kPart];
+    __shared__ __align__(16) float part[kPart];
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         const T *const x = static_cast<const T *>(a.x) + row * a.ldx;
         const T *const dy = static_cast<const T *>(a.dy) + row * a.lddy;
         const float mean = a.kept[2 * row], rstd = a.kept[2 * row + 1];
-        const auto values = [&](int64_t c, int left, float (&g)[N], float (&xh)[N]) {
+        const auto values = [&](int64_t c, int left, float (&g)[N], float (&d)[N]) {
             Piece<T, N> u, v, weight;
             u.read(dy + c, left);
             v.read(x + c, left);
@@ -282,28 +302,31 @@ __global__ __launch_bounds__(1024) void norm_long_backward_kernel(NormArgs a) {
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 g[e] = a.weight ? (float)u.v[e] * (float)weight.v[e] : (float)u.v[e];
-                xh[e] = e < left ? ((float)v.v[e] - mean) * rstd : 0.f;
+                d[e] = e < left ? (float)v.v[e] - mean : 0.f;
             }
         };
-        float both[2] = {0.f, 0.f}, g[N], xh[N];
+        float sums[3] = {0.f, 0.f, 0.f}, g[N], d[N];
         for (int64_t c = (int64_t)threadIdx.x * N; c < a.width; c += (int64_t)blockDim.x * N) {
-            values(c, (int)std::min<int64_t>(N, a.width - c), g, xh);
+            values(c, (int)std::min<int64_t>(N, a.width - c), g, d);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                both[0] += g[e];
-                both[1] = fmaf(g[e], xh[e], both[1]);
+                sums[0] += g[e];
+                sums[1] = fmaf(g[e], d[e], sums[1]);
+                sums[2] += d[e];
             }
         }
-        row_sum<true>(both, 0, part, turn);
-        const float g0 = both[0] * a.over, g1 = both[1] * a.over;
+        row_sum<true>(sums, 0, part, turn);
+        const Shares s(sums, rstd, a.over);
+        if (a.off && threadIdx.x == 0) a.off[row] = s.off;
+        if (!a.dx) continue;
         for (int64_t c = (int64_t)threadIdx.x * N; c < a.width; c += (int64_t)blockDim.x * N) {
             const int left = (int)std::min<int64_t>(N, a.width - c);
-            values(c, left, g, xh);
+            values(c, left, g, d);
             Piece<T, N> beside, dx;
             if (a.beside) beside.read(static_cast<const T *>(a.beside) + row * a.ldb + c, left);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                float v = rstd * (g[e] - g0 - xh[e] * g1);
+                float v = rstd * (g[e] - s.level - d[e] * rstd * s.slope);
                 if (a.beside) v += (float)beside.v[e];
                 dx.v[e] = (T)v;
             }
@@ -323,13 +346,13 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a) {
 #pragma unroll
     for (int e = 0; e < N; ++e) dweight[e] = dbias[e] = 0.f;
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
-        const float mean = a.kept[2 * row], rstd = a.kept[2 * row + 1];
+        const float mean = a.kept[2 * row], rstd = a.kept[2 * row + 1], off = a.off[row];
         Piece<T, N> u, v;
         u.read(static_cast<const T *>(a.dy) + row * a.lddy + col, left);
         v.read(static_cast<const T *>(a.x) + row * a.ldx + col, left);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            dweight[e] = fmaf((float)u.v[e], ((float)v.v[e] - mean) * rstd, dweight[e]);
+            dweight[e] = fmaf((float)u.v[e], ((float)v.v[e] - mean) * rstd - off, dweight[e]);
             dbias[e] += (float)u.v[e];
         }
     }
@@ -417,6 +440,8 @@ int32_t norm_parts(const NormArgs &a, int num_cus) {
     return (int32_t)std::max<int64_t>(1, groups);
 }
 
+bool norm_long_columns(const NormArgs &a) { return !backward_shape(a).held && (a.dweight || a.dbias); }
+
 hipError_t launch_join_parts(int32_t type, const float *partial, int32_t parts, int64_t width,
                              void *first, void *second, hipStream_t stream) {
     return by_type(type, [&](auto t) {
@@ -475,7 +500,7 @@ hipError_t launch_norm_backward(const NormArgs &args, int num_cus, hipStream_t s
             });
         } else {
             const unsigned rows = (unsigned)groups_of(a, s, 32, num_cus);
-            if (a.dx && a.n) norm_long_backward_kernel<T><<<rows, s.threads, 0, stream>>>(a);
+            if (a.n) norm_long_backward_kernel<T><<<rows, s.threads, 0, stream>>>(a);
             if (columns)
                 norm_columns_kernel<T><<<dim3(groups, (unsigned)wide), 256, 0, stream>>>(a);
         }

@@ -14,25 +14,34 @@ namespace {
 constexpr int kPartValues = 4, kPart = 2 * 16 * kPartValues;
 
 // Joins VALUES values over the lanes of a row: `lanes` neighbours (a power of two), or
-// with WIDE the whole workgroup, in the same order for every lane.
+// with WIDE the whole workgroup, in the same order for every lane.  The values' exchanges
+// are under way together; a wave's lie side by side and are read as one.
 template <bool WIDE, int VALUES, typename F>
 __device__ inline void row_join(float (&v)[VALUES], int lanes, float *part, int &turn, F join) {
     static_assert(VALUES <= kPartValues, "room for them");
+    typedef float Values __attribute__((ext_vector_type(kPartValues)));
+    for (int o = 1; o < (WIDE ? 64 : lanes); o <<= 1) {
 #pragma unroll
-    for (int i = 0; i < VALUES; ++i)
-        for (int o = 1; o < (WIDE ? 64 : lanes); o <<= 1) v[i] = join(v[i], __shfl_xor(v[i], o));
+        for (int i = 0; i < VALUES; ++i) v[i] = join(v[i], __shfl_xor(v[i], o));
+    }
     if (!WIDE) return;
     const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6;
-    float *const mine = part + (turn ^= 1) * (kPart / 2);
+    Values *const mine = reinterpret_cast<Values *>(part) + (turn ^= 1) * (kPart / 2 / kPartValues);
     if ((threadIdx.x & 63) == 0) {
+        Values all = {};
 #pragma unroll
-        for (int i = 0; i < VALUES; ++i) mine[wave * VALUES + i] = v[i];
+        for (int i = 0; i < VALUES; ++i) all[i] = v[i];
+        mine[wave] = all;
     }
     __syncthreads();
+    Values all = mine[0];
 #pragma unroll
-    for (int i = 0; i < VALUES; ++i) {
-        v[i] = mine[i];
-        for (int w = 1; w < waves; ++w) v[i] = join(v[i], mine[w * VALUES + i]);
+    for (int i = 0; i < VALUES; ++i) v[i] = all[i];
+#pragma unroll 4
+    for (int w = 1; w < waves; ++w) {
+        all = mine[w];
+#pragma unroll
+        for (int i = 0; i < VALUES; ++i) v[i] = join(v[i], all[i]);
     }
 }
 template <bool WIDE, int VALUES>

@@ -66,17 +66,26 @@ class Norm:
         # backward reads the mean as rounded
         self.xh_err = self.rstd * (self.mean[1] + 4 * V * self.off.abs()) + self.xh.abs() * self.rho
 
-    def backward(self, dy, beside):
-        """{"dx", "dweight", "dbias"}"""
+    def backward(self, dy, beside, found=False):
+        """{"dx", "dweight", "dbias"}.  found: the mean's rounding is found from the row's
+        differences from it and taken out."""
         n, k = dy.shape
-        xh, e = self.xh, self.xh_err
+        xh, e, shift = self.xh, self.xh_err, 0.0
+        if found:
+            # the rounded mean is off by `miss`; the differences' sum finds that but for its
+            # roundings and theirs, and xh of the rounded mean is `shift` larger
+            miss = V * self.mean[0].abs() + self.mean[1]
+            centre = (k + 8) * V * (self.off.abs().mean(1, keepdim=True) + miss)
+            e = self.rstd * (centre + 6 * V * (self.off.abs() + miss)) + xh.abs() * self.rho
+            shift = self.rstd * miss
         g = dy if self.w is None else dy * self.w
         s0, e0 = g.mean(1, keepdim=True), (k + 8) * V * g.abs().mean(1, keepdim=True)
         s1 = (g * xh).mean(1, keepdim=True)
-        e1 = ((k + 8) * V * (g * xh).abs() + g.abs() * e).mean(1, keepdim=True)
+        e1 = ((k + 8) * V * g.abs() * (xh.abs() + shift) + g.abs() * e).mean(1, keepdim=True)
+        e1 = e1 + shift * (e0 + 4 * V * s0.abs())
         dx = self.rstd * (g - s0 - xh * s1)
-        size = self.rstd * (g.abs() + s0.abs() + (xh * s1).abs())
-        err = self.rstd * (e0 + xh.abs() * e1 + e * (s1.abs() + e1)) + (self.rho + 8 * V) * size
+        size = self.rstd * (g.abs() + s0.abs() + (xh.abs() + shift) * s1.abs())
+        err = self.rstd * (e0 + (xh.abs() + shift) * e1 + e * (s1.abs() + e1)) + (self.rho + 8 * V) * size
         if beside is not None:
             dx = dx + beside
             err = err + 2 * V * beside.abs()

@@ -107,6 +107,30 @@ def test_rows_far_from_zero(width):
     _check(x, None, None, _draw(2, 20, width, dtype=torch.float32), None)
 
 
+@pytest.mark.parametrize("shift", [1.0, 1e4, 1e6])
+@pytest.mark.parametrize("n,width", [(1, 3), (40, 7), (700, 40), (300, 257), (50, 1500), (9, 4545), (20, 12288),
+                                     (5, 12289), (30, 20001)])
+def test_gradients_of_rows_far_from_zero(n, width, shift):
+    """As forward does, the gradients take the rounding of the mean that they read out of it."""
+    x = _draw(1, n, width, dtype=torch.float32, shift=shift)
+    x[::2] = -x[::2]
+    w, dy = _draw(2, width, dtype=torch.float32, shift=1.0), _draw(3, n, width, dtype=torch.float32, shift=0.5)
+    beside = _draw(4, n, width, dtype=torch.float32)
+    _, kept = local.norm(x, w, keep=True)
+    want = O.Norm(O.d(x), O.d(w), None, 1e-5, x.dtype).backward(O.d(dy), O.d(beside), found=True)
+    for name, got in zip(("dx", "dweight", "dbias"), local.norm_backward(dy, x, w, kept, beside)):
+        O.close(got, want[name], name)
+    # each gradient by itself
+    for wanted in ("dx", "dweight"):
+        call = local._norm_call(x, w, 0.0)
+        call.dy, call.lddy, call.kept = dy.data_ptr(), width, kept.data_ptr()
+        call.beside, call.ldb = beside.data_ptr(), width
+        out = torch.full_like(x if wanted == "dx" else w, 7.0)
+        setattr(call, wanted, out.data_ptr())
+        local._run("norm", call, True, x)
+        O.close(out, want[wanted], wanted)
+
+
 def test_constant_rows_and_other_ends():
     x = torch.full((4, 300), 3.25, device="cuda")
     y, kept = local.norm(x, eps=1e-5, keep=True)
