@@ -15,18 +15,20 @@ constexpr int kPartValues = 4, kPart = 2 * 16 * kPartValues;
 
 // Joins VALUES values over the lanes of a row: `lanes` neighbours (a power of two), or
 // with WIDE the whole workgroup, in the same order for every lane.  The values' exchanges
-// are under way together; a wave's lie side by side and are read as one.
+// are under way together; a wave's lie side by side and are read as one (of four waves
+// ahead: of eight they take 16 registers more).
 template <bool WIDE, int VALUES, typename F>
 __device__ inline void row_join(float (&v)[VALUES], int lanes, float *part, int &turn, F join) {
     static_assert(VALUES <= kPartValues, "room for them");
-    typedef float Values __attribute__((ext_vector_type(kPartValues)));
+    constexpr int kRoom = VALUES == 3 ? 4 : VALUES;
+    typedef float Values __attribute__((ext_vector_type(kRoom)));
     for (int o = 1; o < (WIDE ? 64 : lanes); o <<= 1) {
 #pragma unroll
         for (int i = 0; i < VALUES; ++i) v[i] = join(v[i], __shfl_xor(v[i], o));
     }
     if (!WIDE) return;
     const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6;
-    Values *const mine = reinterpret_cast<Values *>(part) + (turn ^= 1) * (kPart / 2 / kPartValues);
+    Values *const mine = reinterpret_cast<Values *>(part) + (turn ^= 1) * (kPart / 2 / kRoom);
     if ((threadIdx.x & 63) == 0) {
         Values all = {};
 #pragma unroll
