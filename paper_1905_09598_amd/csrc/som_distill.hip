@@ -13,7 +13,7 @@
 // next to nothing it is summed once more, from its own classes' maximum (kApart).  All
 // gradients are written as if no class were named, and the few that are once more behind a
 // barrier.  What a row has beside its logits is read while they are on their way.  16,001
-// bf16 rows of 10,000, eight named classes and labels, take 157 us (4.1 TB/s); with the
+// bf16 rows of 10,000, eight named classes and labels, take 151 us (4.2 TB/s); with the
 // named classes tested for on the way, and the rest read when it was needed, 198.  Rows of
 // 200,003 are read twice: 512 of them 146 us (instructions 83 of it by count).
 #include "som_row.h"
@@ -99,8 +99,8 @@ __device__ inline void teach(const DistillArgs &a, const Taught &t, const T *s, 
 
 // How labels' exponentials come.  At temperatures of 1, 2 and 4 they are the others', squared
 // none, one or two times, off by no more than by themselves: the error of the product in the
-// exponent doubles with the exponent either way.  (16,001 bf16 rows of 10,000 at 2: 175 us
-// with exponentials of their own, 160 so.)
+// exponent doubles with the exponent either way.  (16,001 bf16 rows of 10,000 at 2: 167 us
+// with exponentials of their own, 156 so.)
 enum : int { kNoLabels = 0, kOwn = 1, kSame = 2, kSquared = 3, kTwice = 4 };
 
 // 2^((v - top) c) of N logits and, with labels, e^(v - top).
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(1024) void distill_kernel(DistillArgs a) {
 #pragma unroll
         for (int e = 0; e < N; ++e) sums[1] += v[e];
         // one piece after the other: together, without labels' exponentials between, they take
-        // 72 registers and not 58 (16,001 bf16 rows of 10,000: 157 us and not 152)
+        // 72 registers and not 58 (16,001 bf16 rows of 10,000: 151 us and not 144)
         if (!HARD) asm volatile("" : "+v"(sums[1]));
     }
     row_sum<WIDE>(sums, a.lanes, part, turn);

@@ -12,7 +12,7 @@
 // numbers: dy v can pass 65,520 where neither does, and dy of a mean's loss begins next to
 // its subnormals.  There the pass keeps its largest magnitude too, and a second launch, which
 // otherwise only looks, writes dz once more over a power of two where that is outside
-// [1/4, 65,520); the products take the power to their sums.  2.4 us where it only looks,
+// [1/4, 65,520); the products take the power to their sums.  2 to 4 us where it only looks,
 // 85 of 8192 x 4096 where it writes.
 #include "som_local_internal.h"
 

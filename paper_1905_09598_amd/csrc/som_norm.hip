@@ -12,7 +12,7 @@
 // 20,000 fp16 rows of 10,000: forward 156 to 190 us (800 MB, 4.2 to 5.1 TB/s), backward
 // with `beside` 289 to 310 (1.6 GB, 5.2 to 5.5 TB/s); 637 fp32 rows of 4545: 8 and 14,
 // which is the reads, reductions and writes of one to three rows in turn.  5000 fp32 rows
-// of 20,000, which a workgroup does not hold: 235 and 467 (with the call's second kernel).
+// of 20,000, which a workgroup does not hold: 231 and 466 (with the call's second kernel).
 #include "som_row.h"
 
 #include <algorithm>
