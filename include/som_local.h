@@ -355,7 +355,9 @@ som_status som_dispatch(const int32_t *index, int64_t n, int32_t k, int32_t expe
  *     soft = T^2 ( sum over j of p_j (log p_j - log a[index_j]) + r (log r - log a_R) ),
  *     hard = -log softmax(s)[label],       loss = mix soft + (1 - mix) hard,
  * a_R being the sum of a over the classes that are not named, 0 only if none of them is
- * open (its logarithm holds below what a type holds).  0 log 0 is 0.  For example
+ * open (its logarithm holds below what a type holds).  0 log 0 is 0; a p_j below fp32's
+ * least number counts as 0.  The logarithms are fp32's: where the loss is a small difference
+ * of them, it is off by T^2 times a few 2^-24 of their sizes.  For example
  * the units nearest to a document, their scores, and what a softmax over all units leaves.
  * With the gradient `scale dloss_i` of a row's loss (dloss NULL: scale), P_c the
  * sum of the p_j with index_j = c, and only over the row's own parts,
